@@ -100,7 +100,10 @@ typedef enum {
   HYB_OP_PREFILL = 2,
   HYB_OP_SOFTMAX_PREFIX = 3,
   HYB_OP_BACKWARD = 4,
-  HYB_OP_BACKWARD_FULL = 5
+  HYB_OP_BACKWARD_FULL = 5,
+  HYB_OP_WINDOW_STEP = 6,
+  HYB_OP_WINDOW_PREFILL = 7,
+  HYB_OP_WINDOW_BACKWARD = 8
 } hyb_op_t;
 
 typedef struct {
@@ -300,9 +303,183 @@ int hybrid_attn_backward_full(const hyb_dims_t* dims, int32_t seq_len,
                               float* loss, void* ws, size_t ws_bytes,
                               void* stream);
 
+/* softmax_prefix_step_paged for a layer that attends to a window of the cache
+ * and its first tokens: of request b's cached tokens the active block's queries
+ * see the last `window` and the first n_sinks (all of them where those
+ * overlap), and the whole block.  A cached token's distance counts from the
+ * block's start, so every query of the block sees the same ones; a block of one
+ * token (L = 1) is autoregressive decoding with a window of window + 1 tokens.
+ * window and n_sinks are >= 0; a window of at least the prefix gives
+ * softmax_prefix_step_paged.  block_len (device [B] or NULL): active tokens of
+ * each block, as for hybrid_attn_step.
+ * Arguments otherwise as for softmax_prefix_step_paged.  Tokens that are not
+ * seen play no part, whatever their rows hold (NaN included), and of a page
+ * table row only entries 0 .. ceil(min(n_sinks, prefix) / page_size) - 1 and
+ * (prefix - window) / page_size (rounded down) .. ceil(prefix / page_size) - 1
+ * are read, so pages that left the window may be freed and reused.
+ * ws/ws_bytes: at least hybrid_workspace_bytes(dims, HYB_OP_WINDOW_STEP, min(max_pages *
+ * page_size, n_sinks + window + 64)) bytes. */
+int softmax_window_step_paged(const hyb_dims_t* dims, const void* q,
+                              const void* k, const void* v,
+                              const void* k_pages, const void* v_pages,
+                              int32_t n_pages, int32_t page_size,
+                              const int32_t* page_table, int32_t max_pages,
+                              const int32_t* prefix_len, int32_t window,
+                              int32_t n_sinks, const int32_t* block_len,
+                              void* out, void* ws, size_t ws_bytes,
+                              void* stream);
+
+/* The same attention over whole sequences (block-causal, Figure 2 pattern with
+ * softmax): token i of the block that starts at s = (i / L) * L sees the tokens
+ * j < s + L with j >= s - window or j < n_sinks.  L = 1 is causal attention
+ * with a window of window + 1 tokens; window >= seq_len is full block-causal
+ * softmax, the teacher whose outputs hybrid_attn_backward takes as target.
+ * q, out [B][T][Hq][d], k, v [B][T][Hkv][d], T = seq_len >= 1 (any, at most
+ * 2^30; the last block may be partial).  seq_lens (device [B] or NULL): tokens
+ * of each sequence, clamped to [0, T]; later rows of q, k, v play no part
+ * (their values may be anything) and later rows of out and lse are not
+ * written.  The values of a sequence's own tokens must be finite.  lse (fp32
+ * [B][Hq][T], or NULL): log of the sum of exp(q.k / sqrt(d)) over the tokens
+ * seen, which the gradient takes.  feat_dim and n_slots are not used (feat_dim
+ * must still be valid).  ws/ws_bytes: at least hybrid_workspace_bytes(dims,
+ * HYB_OP_WINDOW_PREFILL, seq_len) bytes (NULL when that is 0).  out and lse must not
+ * overlap each other, an input or the workspace.
+ * bf16: the weights enter P V rounded to bf16, lse sums them unrounded. */
+int softmax_window_prefill(const hyb_dims_t* dims, int32_t seq_len,
+                           int32_t window, int32_t n_sinks, const void* q,
+                           const void* k, const void* v,
+                           const int32_t* seq_lens, void* out, float* lse,
+                           void* ws, size_t ws_bytes, void* stream);
+
+/* Gradient of softmax_window_prefill with respect to q, k and v for the
+ * upstream gradient dout [B][T][Hq][d] (dims->dtype).  out (dims->dtype) and
+ * lse are what the forward call left.  dq [B][T][Hq][d], dk, dv [B][T][Hkv][d]
+ * in dims->dtype, or fp32 with HYB_OUT_F32 (on bf16 the weights and dS enter
+ * the products rounded to bf16 all the same); dk and dv sum over the query
+ * heads that share a KV head.  All three are required and overwritten; rows
+ * past seq_lens[b] are zero.  ws/ws_bytes: at least hybrid_workspace_bytes(dims,
+ * HYB_OP_WINDOW_BACKWARD, seq_len) bytes.  No output may overlap another
+ * output, an input or the workspace.  Deterministic (no atomics). */
+int softmax_window_backward(const hyb_dims_t* dims, int32_t seq_len,
+                            int32_t window, int32_t n_sinks, const void* q,
+                            const void* k, const void* v,
+                            const int32_t* seq_lens, const void* out,
+                            const float* lse, const void* dout, void* dq,
+                            void* dk, void* dv, void* ws, size_t ws_bytes,
+                            void* stream);
+
+/* Norm and rotation of queries and keys -- what stands between the projections
+ * and every attention entry point of this library. */
+typedef enum {
+  HYB_ROPE_HALF = 0,       /* pair i: entries i and i + rot_dim/2           */
+  HYB_ROPE_INTERLEAVED = 1 /* pair i: entries 2i and 2i + 1                 */
+} hyb_rope_layout_t;
+
+typedef struct {
+  int32_t tokens;     /* N >= 0 (0: nothing to do; the gradient of the
+                         weights is then zero)                               */
+  int32_t n_q_heads;  /* Hq >= 1                                             */
+  int32_t n_kv_heads; /* Hkv >= 1                                            */
+  int32_t head_dim;   /* d: 64 or 128                                        */
+  int32_t rot_dim;    /* entries of a head that are rotated: its first
+                         rot_dim, a multiple of 8 from 0 to d                */
+  int32_t layout;     /* hyb_rope_layout_t                                   */
+  int32_t dtype;      /* hyb_dtype_t of q, k, v, the weights and the pages   */
+  int32_t grad_dtype; /* hyb_dtype_t of dq_out, dk_out (gradient only)       */
+  int32_t flags;      /* 0 or HYB_OUT_F32: q_out, k_out, dq, dk are fp32     */
+  float eps;          /* added to the mean square, > 0                       */
+  float rot_scale;    /* scales sine and cosine (1 unless the position
+                         scaling asks for another), finite                   */
+  /* elements from a token's row to the next; 0: contiguous.  A multiple of 8,
+   * at least the row's length. */
+  int64_t q_stride, k_stride, v_stride; /* of the inputs                     */
+  int64_t q_out_stride, k_out_stride;   /* of q_out, k_out, dq, dk           */
+} hyb_rope_dims_t;
+
+/* For every token t and head: n = x * w / sqrt(mean(x^2) + eps) over the d
+ * entries, then each pair (a, b) of n's first rot_dim entries becomes
+ * rot_scale * (a cos - b sin, b cos + a sin) of the angle positions[t] *
+ * inv_freq[i]; the rest of n stays as it is.  q [N][Hq][d] and k [N][Hkv][d]
+ * may be views of one packed projection (row strides in dims); wq, wk [d]
+ * (dims->dtype), shared by the heads; NULL: that side is not normalised.
+ * positions int32 [N] (any value); inv_freq double [rot_dim / 2], radians per
+ * position: angles are formed in 64 bits, so far positions keep their phase, and
+ * every scaling of positions for long contexts is a table (may be NULL
+ * when rot_dim is 0).  Arithmetic is fp32, rounded once.  q_out and k_out may
+ * be interleaved in one buffer, and must not overlap each other or an input. */
+int hybrid_qk_norm_rope(const hyb_rope_dims_t* dims, const void* q,
+                        const void* k, const void* wq, const void* wk,
+                        const int32_t* positions, const double* inv_freq,
+                        void* q_out, void* k_out, void* stream);
+
+/* The same with the keys and values written into a paged cache (the pools of
+ * softmax_prefix_step_paged and softmax_window_step_paged): token t's k_out
+ * row and its row of v [N][Hkv][d] go to row slots[t] % page_size of page slots[t] /
+ * page_size, in dims->dtype.  A slot outside [0, n_pages * page_size) writes
+ * nothing (tokens of a padded batch: -1).  Two tokens of one call must not
+ * name the same slot.  k_out may be NULL (the block's own step needs it); other
+ * rows of the pools are left as they were.  slots int32 [N] as kv_pages_plan gives them;
+ * n_pages >= 1, page_size 1 or more.  The pools must not overlap each
+ * other, an output or an input. */
+int hybrid_qk_norm_rope_paged(const hyb_rope_dims_t* dims, const void* q,
+                              const void* k, const void* v, const void* wq,
+                              const void* wk, const int32_t* positions,
+                              const double* inv_freq, const int32_t* slots,
+                              void* q_out, void* k_out, void* k_pages,
+                              void* v_pages, int32_t n_pages,
+                              int32_t page_size, void* stream);
+
+/* Gradient of hybrid_qk_norm_rope: dq, dk (with respect to q, k; rows at the
+ * output strides) and dwq, dwk (fp32 [d], summed over tokens and heads,
+ * overwritten; required exactly where the weight is given) for the upstream
+ * gradients dq_out [N][Hq][d], dk_out [N][Hkv][d] (contiguous, grad_dtype: the
+ * fp32 dq, dk of hybrid_attn_backward_full and the dq, dk of
+ * softmax_window_backward fit as they are).  ws/ws_bytes: at least
+ * hybrid_rope_workspace_bytes(dims) bytes when a weight is given (else may be
+ * NULL).  Outputs and the workspace must not overlap each other or an input.
+ * Deterministic. */
+int hybrid_qk_norm_rope_backward(const hyb_rope_dims_t* dims, const void* q,
+                                 const void* k, const void* wq, const void* wk,
+                                 const int32_t* positions,
+                                 const double* inv_freq, const void* dq_out,
+                                 const void* dk_out, void* dq, void* dk,
+                                 float* dwq, float* dwk, void* ws,
+                                 size_t ws_bytes, void* stream);
+
+/* Workspace bytes of hybrid_qk_norm_rope_backward; 0 for invalid dims. */
+size_t hybrid_rope_workspace_bytes(const hyb_rope_dims_t* dims);
+
+/* Pages and cache rows of a batch's new tokens, from lengths that live on the
+ * device (no host wait; a captured call plans from the lengths of each replay).
+ * Request b holds prefix_len[b] cached tokens (clamped to [0, max_pages *
+ * page_size]) and brings new_len[b] >= 0 more (negative: 0).  Its table row
+ * page_table[b] ([B][max_pages], in and out) keeps the entries of the tokens it
+ * holds; the entries its new tokens need besides take free_pages[0], [1], ..
+ * in the order of the requests and of their tokens, and are written (-1 once
+ * the n_free pages are used up).  Per new token, packed in the same order:
+ * slots int32 [max_tokens], its row in the pools (page * page_size + row), or
+ * -1 where it has no page (none left, past max_pages, or a negative or too
+ * large page number in the table); positions int32 [max_tokens], its index in
+ * its request.  Rows past the last token get slot -1 and position 0; tokens
+ * past max_tokens are dropped (their pages are still taken).  token_start
+ * int32 [B + 1]: first packed row of each request, then the total.  counts
+ * int32 [2]: pages taken, pages that were missing.  Sums past 2^31 - 1 stay there.
+ * batch is 1 .. 4096 (0: nothing to do); page_size a power of two from 1 to 65536;
+ * max_pages * page_size < 2^31 - 64; n_free >= 0 (free_pages may be NULL when
+ * 0); max_tokens >= 0 (slots and positions may be NULL when 0).  Outputs must not overlap
+ * each other, the table or an input. */
+int kv_pages_plan(int32_t batch, int32_t max_pages, int32_t page_size,
+                  int32_t n_free, int32_t max_tokens,
+                  const int32_t* prefix_len, const int32_t* new_len,
+                  const int32_t* free_pages, int32_t* page_table,
+                  int32_t* slots, int32_t* positions, int32_t* token_start,
+                  int32_t* counts, void* stream);
+
 /* Workspace bytes the given op needs for these dims; `extent` is seq_len for
- * HYB_OP_PREFILL, HYB_OP_BACKWARD and HYB_OP_BACKWARD_FULL, max_prefix for
- * HYB_OP_SOFTMAX_PREFIX, ignored otherwise.  Returns 0 for invalid dims. */
+ * HYB_OP_PREFILL, HYB_OP_BACKWARD, HYB_OP_BACKWARD_FULL, HYB_OP_WINDOW_PREFILL
+ * and HYB_OP_WINDOW_BACKWARD, max_prefix for HYB_OP_SOFTMAX_PREFIX, the cached
+ * tokens a request sees at most for HYB_OP_WINDOW_STEP, ignored otherwise.
+ * Returns 0 for invalid dims. */
 size_t hybrid_workspace_bytes(const hyb_dims_t* dims, int32_t op,
                               int32_t extent);
 

@@ -3,6 +3,8 @@
 // call enqueues nothing and touches no buffer.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <string>
@@ -335,8 +337,12 @@ int softmax_prefix_impl(const hyb_dims_t* dims, const void* q, const void* k,
                         int32_t max_prefix, bool paged,
                         const int32_t* page_table, int32_t n_pages,
                         int32_t page_size, int32_t max_pages, void* out,
-                        void* ws, size_t ws_bytes, void* stream) {
+                        void* ws, size_t ws_bytes, void* stream,
+                        int32_t window = -1, int32_t n_sinks = 0,
+                        const int32_t* block_len = nullptr) {
   hyb::Shape s;
+  const bool win = window >= 0;  // (paged only)
+  const char* name = win ? "softmax_window_step_paged" : "softmax_prefix_step";
   TRY(check_dims(dims, false, &s));
   TRY(no_step_flags(dims));
   int page_shift = 0;
@@ -357,7 +363,7 @@ int softmax_prefix_impl(const hyb_dims_t* dims, const void* q, const void* k,
     return fail(HYB_EINVAL, "max_prefix %d < 0", max_prefix);
   if (s.Hq / s.Hkv > 8)
     return fail(HYB_EUNSUPPORTED,
-                "softmax_prefix_step supports up to 8 query heads per KV head");
+                "%s supports up to 8 query heads per KV head", name);
   if (s.B == 0) return ok();
   TRY(check_ptr(q, "q"));
   TRY(check_ptr(k, "k"));
@@ -369,12 +375,16 @@ int softmax_prefix_impl(const hyb_dims_t* dims, const void* q, const void* k,
     TRY(check_ptr(v_cache, paged ? "v_pages" : "v_cache"));
     if (paged) TRY(check_ptr(page_table, "page_table"));
   }
+  TRY(check_ptr(block_len, "block_len", false));
+  // cached tokens that a query sees, at most (a window's ends share tiles with
+  // hidden tokens)
+  const int max_seen =
+      win ? (int)std::min<long long>(max_prefix, (long long)window + n_sinks + 64) : max_prefix;
   const size_t need =
-      hybrid_workspace_bytes(dims, HYB_OP_SOFTMAX_PREFIX, max_prefix);
+      hybrid_workspace_bytes(dims, HYB_OP_SOFTMAX_PREFIX, max_seen);
   if (need > 0 && (!ws || ws_bytes < need))
-    return fail(HYB_EWORKSPACE,
-                "softmax_prefix_step needs %zu workspace bytes, got %zu", need,
-                ws ? ws_bytes : (size_t)0);
+    return fail(HYB_EWORKSPACE, "%s needs %zu workspace bytes, got %zu", name,
+                need, ws ? ws_bytes : (size_t)0);
   TRY(check_ptr(ws, "ws", false));
   const size_t es = elem_bytes(s.dtype);
   const size_t nq = (size_t)s.B * s.L * s.Hq * s.D * es;
@@ -387,6 +397,7 @@ int softmax_prefix_impl(const hyb_dims_t* dims, const void* q, const void* k,
       overlap(out, no, v, nkv) || overlap(out, no, k_cache, nc) ||
       overlap(out, no, v_cache, nc) || overlap(out, no, ws, need) ||
       overlap(out, no, prefix_len, (size_t)s.B * 4) ||
+      overlap(out, no, block_len, (size_t)s.B * 4) ||
       overlap(out, no, page_table, nt))
     return fail(HYB_EINVAL, "out overlaps an input or the workspace");
   // the split kernels write the workspace while they read the inputs
@@ -394,16 +405,17 @@ int softmax_prefix_impl(const hyb_dims_t* dims, const void* q, const void* k,
                    overlap(ws, need, v, nkv) || overlap(ws, need, k_cache, nc) ||
                    overlap(ws, need, v_cache, nc) ||
                    overlap(ws, need, prefix_len, (size_t)s.B * 4) ||
+                   overlap(ws, need, block_len, (size_t)s.B * 4) ||
                    overlap(ws, need, page_table, nt)))
     return fail(HYB_EINVAL, "the workspace overlaps an input");
   hyb::SoftmaxPrefixArgs a{s,         q,   k,  v,
                            k_cache,   v_cache, prefix_len, max_prefix,
-                           out,       ws,  hyb::softmax_prefix_splits(s, max_prefix),
+                           out,       ws,  hyb::softmax_prefix_splits(s, max_seen),
                            paged && max_prefix > 0 ? page_table : nullptr,
-                           page_shift, max_pages, n_pages};
+                           page_shift, max_pages, n_pages, max_seen,
+                           window,    n_sinks, block_len};
   (void)hipGetLastError();
-  return launched(hyb::launch_softmax_prefix(a, (hipStream_t)stream),
-                  "softmax_prefix_step");
+  return launched(hyb::launch_softmax_prefix(a, (hipStream_t)stream), name);
 }
 
 }  // namespace
@@ -430,6 +442,386 @@ int softmax_prefix_step_paged(const hyb_dims_t* dims, const void* q,
   return softmax_prefix_impl(dims, q, k, v, k_pages, v_pages, prefix_len, 0,
                              true, page_table, n_pages, page_size, max_pages,
                              out, ws, ws_bytes, stream);
+}
+
+int softmax_window_step_paged(const hyb_dims_t* dims, const void* q,
+                              const void* k, const void* v,
+                              const void* k_pages, const void* v_pages,
+                              int32_t n_pages, int32_t page_size,
+                              const int32_t* page_table, int32_t max_pages,
+                              const int32_t* prefix_len, int32_t window,
+                              int32_t n_sinks, const int32_t* block_len,
+                              void* out, void* ws, size_t ws_bytes,
+                              void* stream) {
+  if (window < 0 || n_sinks < 0)
+    return fail(HYB_EINVAL, "window %d and n_sinks %d must be >= 0", window, n_sinks);
+  return softmax_prefix_impl(dims, q, k, v, k_pages, v_pages, prefix_len, 0,
+                             true, page_table, n_pages, page_size, max_pages,
+                             out, ws, ws_bytes, stream, window, n_sinks, block_len);
+}
+
+}  // extern "C"
+
+namespace {
+
+struct Buf {
+  const void* p;
+  size_t n;
+};
+
+// Outputs (with the workspace) must not overlap each other or an input.
+int check_overlaps(const Buf* written, int nw, const Buf* read_only, int nr) {
+  for (int i = 0; i < nw; ++i) {
+    for (int j = i + 1; j < nw; ++j)
+      if (overlap(written[i].p, written[i].n, written[j].p, written[j].n))
+        return fail(HYB_EINVAL, "outputs or the workspace overlap each other");
+    for (int j = 0; j < nr; ++j)
+      if (overlap(written[i].p, written[i].n, read_only[j].p, read_only[j].n))
+        return fail(HYB_EINVAL, "an output or the workspace overlaps an input");
+  }
+  return HYB_OK;
+}
+
+// What softmax_window_prefill and its gradient check alike.
+int check_window(const hyb_dims_t* dims, int32_t seq_len, int32_t window,
+                 int32_t n_sinks, hyb::Shape* s) {
+  TRY(check_dims(dims, false, s));
+  TRY(no_step_flags(dims));
+  if (seq_len <= 0 || seq_len > (1 << 30))
+    return fail(HYB_EINVAL, "seq_len %d is not in 1 .. 2^30", seq_len);
+  if (window < 0 || n_sinks < 0)
+    return fail(HYB_EINVAL, "window %d and n_sinks %d must be >= 0", window, n_sinks);
+  if (hyb::window_workgroups(*s, seq_len) > 0x7fffffffL)
+    return fail(HYB_EINVAL, "batch * heads * seq_len exceeds the grid limit");
+  return HYB_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int softmax_window_prefill(const hyb_dims_t* dims, int32_t seq_len,
+                           int32_t window, int32_t n_sinks, const void* q,
+                           const void* k, const void* v,
+                           const int32_t* seq_lens, void* out, float* lse,
+                           void* ws, size_t ws_bytes, void* stream) {
+  hyb::Shape s;
+  TRY(check_window(dims, seq_len, window, n_sinks, &s));
+  if (s.B == 0) return ok();
+  TRY(check_ptr(q, "q"));
+  TRY(check_ptr(k, "k"));
+  TRY(check_ptr(v, "v"));
+  TRY(check_ptr(seq_lens, "seq_lens", false));
+  TRY(check_ptr(out, "out"));
+  TRY(check_ptr(lse, "lse", false));
+  const size_t need = hybrid_workspace_bytes(dims, HYB_OP_WINDOW_PREFILL, seq_len);
+  if (need > 0 && (!ws || ws_bytes < need))
+    return fail(HYB_EWORKSPACE, "softmax_window_prefill needs %zu workspace bytes, got %zu",
+                need, ws ? ws_bytes : (size_t)0);
+  TRY(check_ptr(ws, "ws", false));
+  const size_t rows = (size_t)s.B * seq_len, es = elem_bytes(s.dtype);
+  const Buf written[] = {{out, rows * s.Hq * s.D * out_bytes(s)}, {lse, rows * s.Hq * 4}, {ws, need}};
+  const Buf read_only[] = {{q, rows * s.Hq * s.D * es},
+                           {k, rows * s.Hkv * s.D * es},
+                           {v, rows * s.Hkv * s.D * es},
+                           {seq_lens, (size_t)s.B * 4}};
+  TRY(check_overlaps(written, 3, read_only, 4));
+  hyb::WindowArgs a{s, seq_len, window, n_sinks, q, k, v, seq_lens, out, lse};
+  (void)hipGetLastError();
+  return launched(hyb::launch_window_prefill(a, (hipStream_t)stream), "softmax_window_prefill");
+}
+
+int softmax_window_backward(const hyb_dims_t* dims, int32_t seq_len,
+                            int32_t window, int32_t n_sinks, const void* q,
+                            const void* k, const void* v,
+                            const int32_t* seq_lens, const void* out,
+                            const float* lse, const void* dout, void* dq,
+                            void* dk, void* dv, void* ws, size_t ws_bytes,
+                            void* stream) {
+  hyb::Shape s;
+  TRY(check_window(dims, seq_len, window, n_sinks, &s));
+  if (s.B == 0) return ok();
+  TRY(check_ptr(q, "q"));
+  TRY(check_ptr(k, "k"));
+  TRY(check_ptr(v, "v"));
+  TRY(check_ptr(seq_lens, "seq_lens", false));
+  TRY(check_ptr(out, "out"));
+  TRY(check_ptr(lse, "lse"));
+  TRY(check_ptr(dout, "dout"));
+  TRY(check_ptr(dq, "dq"));
+  TRY(check_ptr(dk, "dk"));
+  TRY(check_ptr(dv, "dv"));
+  const size_t need = hybrid_workspace_bytes(dims, HYB_OP_WINDOW_BACKWARD, seq_len);
+  if (!ws || ws_bytes < need)
+    return fail(HYB_EWORKSPACE, "softmax_window_backward needs %zu workspace bytes, got %zu",
+                need, ws ? ws_bytes : (size_t)0);
+  TRY(check_ptr(ws, "ws"));
+  const size_t rows = (size_t)s.B * seq_len, es = elem_bytes(s.dtype);
+  const size_t nq = rows * s.Hq * s.D, nkv = rows * s.Hkv * s.D;
+  const Buf written[] = {{dq, nq * out_bytes(s)}, {dk, nkv * out_bytes(s)}, {dv, nkv * out_bytes(s)}, {ws, need}};
+  const Buf read_only[] = {{q, nq * es},   {k, nkv * es},    {v, nkv * es},  {seq_lens, (size_t)s.B * 4},
+                           {out, nq * es}, {dout, nq * es}, {lse, rows * s.Hq * 4}};
+  TRY(check_overlaps(written, 4, read_only, 7));
+  // (out and lse are only read)
+  hyb::WindowArgs a{s, seq_len, window, n_sinks, q, k, v, seq_lens,
+                    const_cast<void*>(out), const_cast<float*>(lse), dout, dq, dk, dv, (float*)ws};
+  (void)hipGetLastError();
+  return launched(hyb::launch_window_backward(a, (hipStream_t)stream), "softmax_window_backward");
+}
+
+}  // extern "C"
+
+namespace {
+
+// Rows of n bytes at p, `stride` bytes apart.
+struct Rows {
+  const void* p;
+  size_t n, stride;
+};
+bool rows_overlap(const Rows& a, const Rows& b, long count) {
+  if (!a.p || !b.p || count == 0) return false;
+  const size_t na = (count - 1) * a.stride + a.n, nb = (count - 1) * b.stride + b.n;
+  if (!overlap(a.p, na, b.p, nb)) return false;
+  if (count == 1 || a.stride != b.stride) return true;
+  // the same stride: where b's rows fall between a's
+  const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+  const size_t d = y >= x ? (y - x) % a.stride : (a.stride - (x - y) % a.stride) % a.stride;
+  return d < a.n || d + b.n > a.stride;
+}
+
+int check_rope(const hyb_rope_dims_t* d, hyb::RopeArgs* a) {
+  if (!d) return fail(HYB_ENULL, "dims is NULL");
+  if ((d->dtype != HYB_F32 && d->dtype != HYB_BF16) || (d->grad_dtype != HYB_F32 && d->grad_dtype != HYB_BF16))
+    return fail(HYB_EDTYPE, "dtype %d or grad_dtype %d is neither HYB_F32 nor HYB_BF16", d->dtype, d->grad_dtype);
+  if (d->tokens < 0) return fail(HYB_EINVAL, "tokens %d < 0", d->tokens);
+  if (d->n_q_heads < 1 || d->n_kv_heads < 1 || d->n_q_heads > (1 << 20) || d->n_kv_heads > (1 << 20))
+    return fail(HYB_EINVAL, "head counts must be 1 .. 2^20 (Hq=%d, Hkv=%d)", d->n_q_heads, d->n_kv_heads);
+  if (d->head_dim != 64 && d->head_dim != 128)
+    return fail(HYB_EUNSUPPORTED, "head_dim %d not supported (64 or 128)", d->head_dim);
+  if (d->rot_dim < 0 || d->rot_dim > d->head_dim || d->rot_dim % 8)
+    return fail(HYB_EUNSUPPORTED, "rot_dim %d not supported (a multiple of 8, 0 .. head_dim)", d->rot_dim);
+  if (d->layout != HYB_ROPE_HALF && d->layout != HYB_ROPE_INTERLEAVED)
+    return fail(HYB_EINVAL, "unknown layout %d", d->layout);
+  if (d->flags & ~HYB_OUT_F32) return fail(HYB_EINVAL, "unknown flags 0x%x", d->flags);
+  if (!(d->eps > 0.0f) || !std::isfinite(d->eps) || !std::isfinite(d->rot_scale))
+    return fail(HYB_EINVAL, "eps must be positive and finite, rot_scale finite");
+  const long nq = (long)d->n_q_heads * d->head_dim, nk = (long)d->n_kv_heads * d->head_dim;
+  const long given[5] = {d->q_stride, d->k_stride, d->v_stride, d->q_out_stride, d->k_out_stride};
+  const long least[5] = {nq, nk, nk, nq, nk};
+  long* set[5] = {&a->q_stride, &a->k_stride, &a->v_stride, &a->q_out_stride, &a->k_out_stride};
+  for (int i = 0; i < 5; ++i) {
+    if (given[i] != 0 && (given[i] < least[i] || given[i] > (1L << 31)))
+      return fail(HYB_EINVAL, "a row stride of %ld is shorter than the row, or longer than 2^31", given[i]);
+    if (given[i] % 8) return fail(HYB_EALIGN, "a row stride of %ld is not a multiple of 8 elements", given[i]);
+    *set[i] = given[i] ? given[i] : least[i];
+  }
+  a->N = d->tokens;
+  a->Hq = d->n_q_heads;
+  a->Hkv = d->n_kv_heads;
+  a->D = d->head_dim;
+  a->rot = d->rot_dim;
+  a->interleaved = d->layout == HYB_ROPE_INTERLEAVED;
+  a->dtype = d->dtype;
+  a->grad_dtype = d->grad_dtype;
+  a->out_f32 = d->dtype == HYB_F32 || (d->flags & HYB_OUT_F32);
+  a->eps = d->eps;
+  a->rot_scale = d->rot_scale;
+  return HYB_OK;
+}
+
+// Written rows must not overlap each other or anything that is read.
+int check_rows(const Rows* written, int nw, const Rows* read_only, int nr, long count) {
+  for (int i = 0; i < nw; ++i) {
+    for (int j = i + 1; j < nw; ++j)
+      if (rows_overlap(written[i], written[j], count))
+        return fail(HYB_EINVAL, "the outputs overlap each other");
+    for (int j = 0; j < nr; ++j)
+      if (rows_overlap(written[i], read_only[j], count))
+        return fail(HYB_EINVAL, "an output overlaps an input");
+  }
+  return HYB_OK;
+}
+
+// Whole buffers against each other and against rows.
+int check_buffers(const Buf* bufs, int n, bool written, const Rows* rows, int nr, long count) {
+  for (int i = 0; i < n; ++i) {
+    for (int j = i + 1; written && j < n; ++j)
+      if (overlap(bufs[i].p, bufs[i].n, bufs[j].p, bufs[j].n))
+        return fail(HYB_EINVAL, "outputs or the workspace overlap each other");
+    for (int j = 0; j < nr; ++j)
+      if (rows[j].p && overlap(bufs[i].p, bufs[i].n, rows[j].p, (count - 1) * rows[j].stride + rows[j].n))
+        return fail(HYB_EINVAL, "an output or the workspace overlaps another argument");
+  }
+  return HYB_OK;
+}
+
+int rope_impl(const hyb_rope_dims_t* dims, const void* q, const void* k,
+              const void* v, const void* wq, const void* wk,
+              const int32_t* positions, const double* inv_freq,
+              const int32_t* slots, void* q_out, void* k_out, void* k_pages,
+              void* v_pages, int32_t n_pages, int32_t page_size, bool paged,
+              void* stream) {
+  hyb::RopeArgs a{};
+  TRY(check_rope(dims, &a));
+  if (paged && (n_pages < 1 || page_size < 1))
+    return fail(HYB_EINVAL, "n_pages %d and page_size %d must be >= 1", n_pages, page_size);
+  if (a.N == 0) return ok();
+  TRY(check_ptr(q, "q"));
+  TRY(check_ptr(k, "k"));
+  TRY(check_ptr(wq, "wq", false));
+  TRY(check_ptr(wk, "wk", false));
+  TRY(check_ptr(positions, "positions"));
+  TRY(check_ptr(inv_freq, "inv_freq", a.rot > 0));
+  TRY(check_ptr(q_out, "q_out"));
+  TRY(check_ptr(k_out, "k_out", !paged));
+  if (paged) {
+    TRY(check_ptr(v, "v"));
+    TRY(check_ptr(slots, "slots"));
+    TRY(check_ptr(k_pages, "k_pages"));
+    TRY(check_ptr(v_pages, "v_pages"));
+  }
+  const size_t es = elem_bytes(a.dtype), eo = a.out_f32 ? 4 : es;
+  const size_t nq = (size_t)a.Hq * a.D, nk = (size_t)a.Hkv * a.D;
+  const Rows outs[2] = {{q_out, nq * eo, a.q_out_stride * eo}, {k_out, nk * eo, a.k_out_stride * eo}};
+  const Rows ins[3] = {{q, nq * es, a.q_stride * es}, {k, nk * es, a.k_stride * es}, {v, nk * es, a.v_stride * es}};
+  TRY(check_rows(outs, 2, ins, 3, a.N));
+  const Buf small[] = {{wq, a.D * es}, {wk, a.D * es}, {positions, (size_t)a.N * 4},
+                       {inv_freq, (size_t)a.rot * 4}, {slots, (size_t)a.N * 4}};
+  TRY(check_buffers(small, 5, false, outs, 2, a.N));
+  if (paged) {
+    a.n_rows = (long)n_pages * page_size;
+    const Buf pools[2] = {{k_pages, a.n_rows * nk * es}, {v_pages, a.n_rows * nk * es}};
+    TRY(check_buffers(pools, 2, true, outs, 2, a.N));
+    TRY(check_buffers(pools, 2, true, ins, 3, a.N));
+    TRY(check_overlaps(pools, 2, small, 5));
+  }
+  a.q = q, a.k = k, a.v = v, a.wq = wq, a.wk = wk;
+  a.positions = positions, a.inv_freq = inv_freq;
+  a.q_out = q_out, a.k_out = k_out;
+  a.slots = slots, a.k_pages = k_pages, a.v_pages = v_pages;
+  (void)hipGetLastError();
+  return launched(hyb::launch_rope(a, (hipStream_t)stream), paged ? "qk_norm_rope_paged" : "qk_norm_rope");
+}
+
+}  // namespace
+
+extern "C" {
+
+int hybrid_qk_norm_rope(const hyb_rope_dims_t* dims, const void* q,
+                        const void* k, const void* wq, const void* wk,
+                        const int32_t* positions, const double* inv_freq,
+                        void* q_out, void* k_out, void* stream) {
+  return rope_impl(dims, q, k, nullptr, wq, wk, positions, inv_freq, nullptr, q_out, k_out, nullptr, nullptr, 0, 0,
+                   false, stream);
+}
+
+int hybrid_qk_norm_rope_paged(const hyb_rope_dims_t* dims, const void* q,
+                              const void* k, const void* v, const void* wq,
+                              const void* wk, const int32_t* positions,
+                              const double* inv_freq, const int32_t* slots,
+                              void* q_out, void* k_out, void* k_pages,
+                              void* v_pages, int32_t n_pages,
+                              int32_t page_size, void* stream) {
+  return rope_impl(dims, q, k, v, wq, wk, positions, inv_freq, slots, q_out, k_out, k_pages, v_pages, n_pages,
+                   page_size, true, stream);
+}
+
+size_t hybrid_rope_workspace_bytes(const hyb_rope_dims_t* dims) {
+  hyb::RopeArgs a{};
+  const std::string saved = g_err;
+  const int rc = check_rope(dims, &a);
+  g_err = saved;
+  return rc == HYB_OK ? hyb::rope_backward_ws_bytes(a) : 0;
+}
+
+int hybrid_qk_norm_rope_backward(const hyb_rope_dims_t* dims, const void* q,
+                                 const void* k, const void* wq, const void* wk,
+                                 const int32_t* positions,
+                                 const double* inv_freq, const void* dq_out,
+                                 const void* dk_out, void* dq, void* dk,
+                                 float* dwq, float* dwk, void* ws,
+                                 size_t ws_bytes, void* stream) {
+  hyb::RopeArgs a{};
+  TRY(check_rope(dims, &a));
+  TRY(check_ptr(wq, "wq", false));
+  TRY(check_ptr(wk, "wk", false));
+  if ((wq != nullptr) != (dwq != nullptr) || (wk != nullptr) != (dwk != nullptr))
+    return fail(HYB_ENULL, "dwq and dwk are required exactly where wq and wk are given");
+  TRY(check_ptr(dwq, "dwq", false));
+  TRY(check_ptr(dwk, "dwk", false));
+  const bool none = a.N == 0;
+  if (none && !dwq && !dwk) return ok();
+  TRY(check_ptr(q, "q", !none));
+  TRY(check_ptr(k, "k", !none));
+  TRY(check_ptr(positions, "positions", !none));
+  TRY(check_ptr(inv_freq, "inv_freq", !none && a.rot > 0));
+  TRY(check_ptr(dq_out, "dq_out", !none));
+  TRY(check_ptr(dk_out, "dk_out", !none));
+  TRY(check_ptr(dq, "dq", !none));
+  TRY(check_ptr(dk, "dk", !none));
+  const size_t need = wq || wk ? hyb::rope_backward_ws_bytes(a) : 0;
+  if (need > 0 && (!ws || ws_bytes < need))
+    return fail(HYB_EWORKSPACE, "qk_norm_rope_backward needs %zu workspace bytes, got %zu", need,
+                ws ? ws_bytes : (size_t)0);
+  TRY(check_ptr(ws, "ws", false));
+  const size_t es = elem_bytes(a.dtype), eo = a.out_f32 ? 4 : es, eg = elem_bytes(a.grad_dtype);
+  const size_t nq = (size_t)a.Hq * a.D, nk = (size_t)a.Hkv * a.D;
+  const Rows outs[2] = {{dq, nq * eo, a.q_out_stride * eo}, {dk, nk * eo, a.k_out_stride * eo}};
+  const Rows ins[4] = {{q, nq * es, a.q_stride * es}, {k, nk * es, a.k_stride * es},
+                       {dq_out, nq * eg, nq * eg}, {dk_out, nk * eg, nk * eg}};
+  const Buf sums[3] = {{dwq, (size_t)a.D * 4}, {dwk, (size_t)a.D * 4}, {ws, need}};
+  const Buf small[4] = {{wq, a.D * es}, {wk, a.D * es}, {positions, (size_t)a.N * 4}, {inv_freq, (size_t)a.rot * 4}};
+  TRY(check_overlaps(sums, 3, small, 4));
+  if (!none) {
+    TRY(check_rows(outs, 2, ins, 4, a.N));
+    TRY(check_buffers(small, 4, false, outs, 2, a.N));
+    TRY(check_buffers(sums, 3, true, outs, 2, a.N));
+    TRY(check_buffers(sums, 3, true, ins, 4, a.N));
+  }
+  a.q = q, a.k = k, a.wq = wq, a.wk = wk;
+  a.positions = positions, a.inv_freq = inv_freq;
+  a.dq_out = dq_out, a.dk_out = dk_out, a.dq = dq, a.dk = dk;
+  a.dwq = dwq, a.dwk = dwk;
+  a.ws = need > 0 ? (float*)ws : nullptr;
+  (void)hipGetLastError();
+  return launched(hyb::launch_rope_backward(a, (hipStream_t)stream), "qk_norm_rope_backward");
+}
+
+int kv_pages_plan(int32_t batch, int32_t max_pages, int32_t page_size,
+                  int32_t n_free, int32_t max_tokens,
+                  const int32_t* prefix_len, const int32_t* new_len,
+                  const int32_t* free_pages, int32_t* page_table,
+                  int32_t* slots, int32_t* positions, int32_t* token_start,
+                  int32_t* counts, void* stream) {
+  if (batch < 0 || max_pages < 0 || n_free < 0 || max_tokens < 0)
+    return fail(HYB_EINVAL, "batch %d, max_pages %d, n_free %d and max_tokens %d must be >= 0", batch, max_pages,
+                n_free, max_tokens);
+  if (batch > hyb::kMaxPlanBatch)
+    return fail(HYB_EUNSUPPORTED, "batch %d not supported (at most %d)", batch, hyb::kMaxPlanBatch);
+  if (page_size < 1 || page_size > (1 << 16) || (page_size & (page_size - 1)))
+    return fail(HYB_EUNSUPPORTED, "page_size %d not supported (a power of two, 1 .. 65536)", page_size);
+  if ((long long)max_pages * page_size > 0x7fffffffLL - 64)
+    return fail(HYB_EINVAL, "max_pages * page_size exceeds the index range");
+  if (batch == 0) return ok();
+  TRY(check_ptr(prefix_len, "prefix_len"));
+  TRY(check_ptr(new_len, "new_len"));
+  TRY(check_ptr(free_pages, "free_pages", n_free > 0));
+  TRY(check_ptr(page_table, "page_table", max_pages > 0));
+  TRY(check_ptr(slots, "slots", max_tokens > 0));
+  TRY(check_ptr(positions, "positions", max_tokens > 0));
+  TRY(check_ptr(token_start, "token_start"));
+  TRY(check_ptr(counts, "counts"));
+  const Buf written[] = {{page_table, (size_t)batch * max_pages * 4}, {slots, (size_t)max_tokens * 4},
+                         {positions, (size_t)max_tokens * 4}, {token_start, (size_t)(batch + 1) * 4}, {counts, 8}};
+  const Buf read_only[] = {{prefix_len, (size_t)batch * 4}, {new_len, (size_t)batch * 4},
+                           {free_pages, (size_t)n_free * 4}};
+  TRY(check_overlaps(written, 5, read_only, 3));
+  int shift = 0;
+  while ((1 << shift) < page_size) ++shift;
+  hyb::PagesArgs a{batch, max_pages, shift, n_free, max_tokens, prefix_len, new_len, free_pages,
+                   page_table, slots, positions, token_start, counts};
+  (void)hipGetLastError();
+  return launched(hyb::launch_pages_plan(a, (hipStream_t)stream), "kv_pages_plan");
 }
 
 }  // extern "C"
@@ -557,12 +949,17 @@ size_t hybrid_workspace_bytes(const hyb_dims_t* dims, int32_t op,
       if (extent == 0 || extent % s.L != 0) return 0;
       return hyb::prefill_ws_bytes(s, extent);
     case HYB_OP_SOFTMAX_PREFIX:
+    case HYB_OP_WINDOW_STEP:
       return hyb::softmax_prefix_ws_bytes(
           s, hyb::softmax_prefix_splits(s, extent));
     case HYB_OP_BACKWARD:
     case HYB_OP_BACKWARD_FULL:
       if (extent == 0 || extent % s.L != 0 || !hyb::backward_supported(s)) return 0;
       return hyb::backward_ws_bytes(s, extent, op == HYB_OP_BACKWARD_FULL);
+    case HYB_OP_WINDOW_PREFILL:
+      return 0;
+    case HYB_OP_WINDOW_BACKWARD:
+      return hyb::window_backward_ws_bytes(s, extent);
   }
   return 0;
 }

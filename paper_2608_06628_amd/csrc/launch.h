@@ -77,9 +77,70 @@ struct SoftmaxPrefixArgs {
   // (clamped to the pool); max_prefix = max_pages << page_shift.
   const int32_t* page_table;
   int page_shift, max_pages, n_pages;
+  // Cached keys of a request that its queries see, at most.
+  int max_seen;
+  // window >= 0 (paged only): of the cache the last `window` tokens and the
+  // first n_sinks are seen; block_len (nullable): active tokens of the block.
+  int window = -1, n_sinks = 0;
+  const int32_t* block_len = nullptr;
 };
 
+// Norm and rotation of queries and keys (rope.hip), forward and gradient.
+// Strides are in elements from one token's row to the next.
+struct RopeArgs {
+  long N;  // tokens
+  int Hq, Hkv, D, rot, interleaved, dtype, grad_dtype, out_f32;
+  float eps, rot_scale;
+  long q_stride, k_stride, v_stride, q_out_stride, k_out_stride;
+  const void *q, *k, *v;
+  const void *wq, *wk;  // null: that side is not normalised
+  const int32_t* positions;
+  const double* inv_freq;
+  void *q_out, *k_out;  // k_out may be null with slots
+  // paged: row slots[t] of the pools (n_rows rows of Hkv heads); out of range: none
+  const int32_t* slots;
+  void *k_pages, *v_pages;
+  long n_rows;
+  // gradient
+  const void *dq_out, *dk_out;  // contiguous rows, grad_dtype
+  void *dq, *dk;                // rows at q_out_stride, k_out_stride
+  float *dwq, *dwk;
+  float* ws;  // null when neither side is normalised
+};
+
+// Softmax over a sequence's window and first tokens (window.hip).  Shape.L is
+// the block; rows past seq_lens[b] (nullable; clamped to 0 .. T) play no part.
+struct WindowArgs {
+  Shape s;
+  int T, window, n_sinks;
+  const void *q, *k, *v;
+  const int32_t* seq_lens;
+  void* out;   // forward: written; gradient: read, in the type of q
+  float* lse;  // [B][Hq][T]; forward: written (nullable); gradient: read
+  // gradient
+  const void* dout = nullptr;
+  void *dq = nullptr, *dk = nullptr, *dv = nullptr;
+  float* delta = nullptr;  // workspace [B][Hq][T]
+};
+
+// Pages and slots of new tokens (pages.hip).
+struct PagesArgs {
+  int B, max_pages, page_shift, n_free, max_tokens;
+  const int32_t *prefix_len, *new_len, *free_pages;
+  int32_t* page_table;
+  int32_t *slots, *positions, *token_start, *counts;
+};
+constexpr int kMaxPlanBatch = 4096;  // requests of one plan
+
 hipError_t launch_step(const StepArgs& a, hipStream_t st);
+hipError_t launch_rope(const RopeArgs& a, hipStream_t st);
+hipError_t launch_rope_backward(const RopeArgs& a, hipStream_t st);
+size_t rope_backward_ws_bytes(const RopeArgs& a);
+hipError_t launch_pages_plan(const PagesArgs& a, hipStream_t st);
+hipError_t launch_window_prefill(const WindowArgs& a, hipStream_t st);
+hipError_t launch_window_backward(const WindowArgs& a, hipStream_t st);
+long window_workgroups(const Shape& s, int T);
+size_t window_backward_ws_bytes(const Shape& s, int T);
 // The step for small batches: one wave per (request, head, 32-column slice).
 hipError_t launch_step_small(const StepArgs& a, hipStream_t st);
 // Whether the automatic choice takes the split kernel for these dims.

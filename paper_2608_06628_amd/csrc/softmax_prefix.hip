@@ -63,13 +63,61 @@ __device__ inline int sp_page(const SoftmaxPrefixArgs& a, const int32_t* ptab, i
   return min(max(pg, 0), a.n_pages - 1);
 }
 
-// Keys of request b: its cached prefix (clamped) and the block.
-__device__ inline int sp_keys(const SoftmaxPrefixArgs& a, int b) {
-  return min(max(a.prefix_len[b], 0), a.max_prefix) + a.s.L;
+// Active tokens of request b's block.
+template <bool WIN>
+__device__ inline int sp_block(const SoftmaxPrefixArgs& a, int b) {
+  if constexpr (WIN) {
+    if (a.block_len) return min(max(a.block_len[b], 0), a.s.L);
+  }
+  return a.s.L;
 }
 
+// Keys of request b: its cached prefix (clamped) and the block.
+template <bool WIN>
+__device__ inline int sp_keys(const SoftmaxPrefixArgs& a, int b) {
+  return min(max(a.prefix_len[b], 0), a.max_prefix) + sp_block<WIN>(a, b);
+}
+
+// With WIN a cached token is visible among the first n_sinks or the last
+// `window` of the prefix: the keys hs .. he - 1 are hidden.  The tiles keep
+// their places in the cache (so a tile still lies in one page), and those that
+// are hidden whole are skipped: tile tv of the request's list is tile tv of
+// its keys, or tv + skip from st on.  Of the list at most two tiles are hidden
+// in part (the last of the sinks, the first of the window, or one that is
+// both); their hidden rows read a visible row of the tile and are masked in
+// the scores, so nothing of what they hold plays a part.
+struct SpSeen {
+  int hs = 0, he = 0;    // hidden keys (none: hs = he)
+  int st = 0, skip = 0;  // tiles before the skipped ones; skipped tiles
+  __device__ inline int tile(int tv) const { return tv < st ? tv : tv + skip; }
+  __device__ inline bool hides(int j) const { return j >= hs && j < he; }
+  // a tile's first key j0: whether some of the tile's keys are hidden, and the
+  // row that stands in for them
+  __device__ inline bool cuts(int j0) const { return j0 < he && j0 + kTile > hs && hs < he; }
+  __device__ inline int stand_in(int j0) const { return he < j0 + kTile ? he : hs - 1; }
+};
+template <bool WIN>
+__device__ inline SpSeen sp_seen(const SoftmaxPrefixArgs& a, int b) {
+  SpSeen v;
+  if constexpr (WIN) {
+    const int P = min(max(a.prefix_len[b], 0), a.max_prefix);
+    const int w0 = P - min(a.window, P);
+    if (a.n_sinks < w0) {
+      v.hs = a.n_sinks;
+      v.he = w0;
+      v.st = (v.hs + kTile - 1) / kTile;
+      v.skip = max(0, w0 / kTile - v.st);
+    }
+  }
+  return v;
+}
+
+template <bool WIN>
 __device__ inline int sp_tiles(const SoftmaxPrefixArgs& a, int b) {
-  return (sp_keys(a, b) + kTile - 1) / kTile;
+  if constexpr (WIN) {
+    if (sp_block<WIN>(a, b) == 0) return 0;  // (nothing to answer)
+  }
+  return (sp_keys<WIN>(a, b) + kTile - 1) / kTile - sp_seen<WIN>(a, b).skip;
 }
 
 // How the requests' keys are cut.  The lengths are known on the device only,
@@ -152,6 +200,7 @@ __device__ inline int wave_scan(int x) {
 // behind a later barrier: on its own it would cost d = 64 one of five workgroups
 // on a CU.)
 constexpr int kPlanInts = kPlanTiles + 2;
+template <bool WIN>
 __device__ inline SpPlan sp_plan(const SoftmaxPrefixArgs& a, const SpCut& cut, int* tiles) {
   const int B = a.s.B, tid = threadIdx.x;
   if (a.n_split == 1) return SpPlan{1 << 24, true};
@@ -160,7 +209,7 @@ __device__ inline SpPlan sp_plan(const SoftmaxPrefixArgs& a, const SpCut& cut, i
     int total = 0, most = 0;
     const int end = B <= kPlanTiles ? (B + 15) & ~15 : B;  // (padded with empty requests)
     for (int b0 = tid; b0 < end; b0 += kWave) {
-      const int nt = b0 < B ? sp_tiles(a, b0) : 0;
+      const int nt = b0 < B ? sp_tiles<WIN>(a, b0) : 0;
       if (B <= kPlanTiles) tiles[b0] = nt;
       total += nt;
       most = max(most, nt);
@@ -194,7 +243,7 @@ __device__ inline SpPlan sp_plan(const SoftmaxPrefixArgs& a, const SpCut& cut, i
         sum += ranges(x.x) + ranges(x.y) + ranges(x.z) + ranges(x.w);
       }
     } else {
-      for (int b0 = sub; b0 < B; b0 += kWave / kCand) sum += ranges(sp_tiles(a, b0));
+      for (int b0 = sub; b0 < B; b0 += kWave / kCand) sum += ranges(sp_tiles<WIN>(a, b0));
     }
     static_assert(kCand == 16, "the lanes that share a candidate are a row apart");
     sum += __builtin_bit_cast(int, xor16(__builtin_bit_cast(float, sum)));
@@ -223,34 +272,48 @@ __device__ inline SpPlan sp_plan(const SoftmaxPrefixArgs& a, const SpCut& cut, i
 __device__ inline int sp_ranges(const SpPlan& p, int nt) { return (nt + p.c - 1) / p.c; }
 
 // Range number r of the plan: its request, its place there, how many ranges
-// that request has and its keys lo .. hi-1.  b = -1: no such range.  Where every
+// that request has and its keys lo .. hi-1 (with WIN: those of its tiles t0 ..
+// t0 + nt - 1 that are visible).  b = -1: no such range.  Where every
 // request is one range, that is request r; else the ranges of the requests
 // before are summed, 64 requests at a time.  (Summed in every case, calls of
 // many short requests paid for it: 4096 requests of 64 keys 907 us, now 377;
 // 4096 of 32 at 8 KV heads of d = 64 584 us, now 141.)
 struct SpRange {
   int b, s, n, lo, hi;
+  int t0 = 0, nt = 0;  // WIN only
 };
+template <bool WIN>
 __device__ inline SpRange sp_share(const SoftmaxPrefixArgs& a, int b, int s, int n) {
   // an even share of the tiles: the first tiles % n ranges take one more
-  const int keys = sp_keys(a, b), tiles = (keys + kTile - 1) / kTile;
+  const int keys = sp_keys<WIN>(a, b);
+  const int tiles = WIN ? sp_tiles<WIN>(a, b) : (keys + kTile - 1) / kTile;
   const int each = tiles / n, more = tiles % n;
   const int t0 = s * each + min(s, more);
-  return SpRange{b, s, n, t0 * kTile, min((t0 + each + (s < more ? 1 : 0)) * kTile, keys)};
+  if constexpr (WIN) {
+    const SpSeen v = sp_seen<WIN>(a, b);
+    const int nt = each + (s < more ? 1 : 0);
+    return SpRange{b, s, n, v.tile(t0) * kTile, min((v.tile(t0 + nt - 1) + 1) * kTile, keys), t0, nt};
+  } else {
+    return SpRange{b, s, n, t0 * kTile, min((t0 + each + (s < more ? 1 : 0)) * kTile, keys)};
+  }
 }
+template <bool WIN>
 __device__ inline SpRange sp_range(const SoftmaxPrefixArgs& a, const SpPlan& p, int r, int lane) {
   const int B = a.s.B;
   const SpRange none{-1, 0, 0, 0, 0};
-  if (p.whole) return r < B ? SpRange{r, 0, 1, 0, sp_keys(a, r)} : none;
+  if constexpr (WIN) {
+    if (p.whole) return r < B && sp_tiles<WIN>(a, r) > 0 ? sp_share<WIN>(a, r, 0, 1) : none;
+  }
+  if (p.whole) return r < B ? SpRange{r, 0, 1, 0, sp_keys<WIN>(a, r)} : none;
   int base = 0;
   for (int b0 = 0; b0 < B; b0 += kWave) {
-    const int n = b0 + lane < B ? sp_ranges(p, sp_tiles(a, b0 + lane)) : 0;
+    const int n = b0 + lane < B ? sp_ranges(p, sp_tiles<WIN>(a, b0 + lane)) : 0;
     const int end = wave_scan(n);
     const int all = __builtin_amdgcn_readlane(end, kWave - 1);
     if (r < base + all) {
       const int at = __builtin_ctzll(__ballot(r < base + end));
       const int nb = __builtin_amdgcn_readlane(n, at);
-      return sp_share(a, b0 + at, r - base - (__builtin_amdgcn_readlane(end, at) - nb), nb);
+      return sp_share<WIN>(a, b0 + at, r - base - (__builtin_amdgcn_readlane(end, at) - nb), nb);
     }
     base += all;
   }
@@ -310,7 +373,7 @@ struct SpRef {
 // LDS: the tile after next is loaded into registers while the current one is
 // computed, and the next one is moved from registers into the free buffer at
 // the end of the step, so one barrier per tile orders everything.
-template <typename T, int D, int NG, bool PAGED>
+template <typename T, int D, int NG, bool PAGED, bool WIN = false>
 __global__ __launch_bounds__(kWave* NG) void hyb_sp_partial_kernel(
     SoftmaxPrefixArgs a, SpCut cut) {
   typedef SpCfg<T, D, NG> C;
@@ -326,10 +389,12 @@ __global__ __launch_bounds__(kWave* NG) void hyb_sp_partial_kernel(
   const int Pmax = a.max_prefix;
   const int g = blockIdx.x % Hkv, r = blockIdx.x / Hkv, h = g * G + w;
   static_assert(sizeof(sh.v[1]) >= kPlanInts * sizeof(int), "the plan's scratch fits a tile");
-  const SpRange rg = sp_range(a, sp_plan(a, cut, reinterpret_cast<int*>(sh.v[1])), r, lane);
+  const SpRange rg = sp_range<WIN>(a, sp_plan<WIN>(a, cut, reinterpret_cast<int*>(sh.v[1])), r, lane);
   if (rg.b < 0) return;  // uniform: past the plan's last range
   const int b = rg.b, lo = rg.lo, hi = rg.hi;
-  const int P = sp_keys(a, b) - L;
+  const int Lb = sp_block<WIN>(a, b);  // active queries
+  const int P = sp_keys<WIN>(a, b) - Lb;
+  const SpSeen seen = sp_seen<WIN>(a, b);
   const size_t qstride = (size_t)Hq * D, kstride = (size_t)Hkv * D;
 
   op_t qop[C::KD];
@@ -338,7 +403,7 @@ __global__ __launch_bounds__(kWave* NG) void hyb_sp_partial_kernel(
                     (size_t)li * qstride + hh * E;
 #pragma unroll
     for (int ks = 0; ks < C::KD; ++ks)
-      qop[ks] = li < L ? load_op<T>(qrow + ks * KW) : M::zero();
+      qop[ks] = li < Lb ? load_op<T>(qrow + ks * KW) : M::zero();
   }
   // contiguous: this request's rows; paged: the pool, at KV head g
   const T* kc = (const T*)a.k_cache + ((PAGED ? 0 : (size_t)b * Pmax * Hkv) + g) * D;
@@ -368,7 +433,8 @@ __global__ __launch_bounds__(kWave* NG) void hyb_sp_partial_kernel(
     for (int c = 0; c < NCH; ++c) {
       const int idx = tid + c * kWave * NG, key = idx / CPR, part = idx % CPR;
       if (idx < kTile * CPR) {  // (NG not a power of two: a partial last set)
-        const int j = min(j0 + key, hi - 1);
+        int j = min(j0 + key, hi - 1);
+        if constexpr (WIN) j = seen.hides(j) ? seen.stand_in(j0) : j;
         const size_t o = (size_t)part * EPC;
         const size_t cr = j < P ? crow(j) : 0;
         const T* ks = j < P ? kc + cr : kbk + (size_t)(j - P) * kstride;
@@ -424,16 +490,20 @@ __global__ __launch_bounds__(kWave* NG) void hyb_sp_partial_kernel(
 #pragma unroll
   for (int ct = 0; ct < C::NCT; ++ct) acc[ct] = f32x16{};
 
+  // First key of the tile x tiles after the one at j0, the range's n-th.
+  auto after = [&](int j0, int n, int x) __attribute__((always_inline)) {
+    return WIN ? (n + x < rg.nt ? seen.tile(rg.t0 + n + x) * kTile : hi) : j0 + x * kTile;
+  };
   TileRegs nx = {}, af = {};
   if (lo < hi) {
     put(fetch(lo), 0);
-    if (lo + kTile < hi) nx = fetch(lo + kTile);
+    if (after(lo, 0, 1) < hi) nx = fetch(after(lo, 0, 1));
   }
   __syncthreads();
   int n = 0;
-  for (int j0 = lo; j0 < hi; j0 += kTile, ++n) {
+  for (int j0 = lo; j0 < hi; j0 = after(j0, n, 1), ++n) {
     const int buf = n & 1;
-    if (j0 + 2 * kTile < hi) af = fetch(j0 + 2 * kTile);  // tile after next
+    if (after(j0, n, 2) < hi) af = fetch(after(j0, n, 2));  // tile after next
 
     f32x16 sc = {};
 #pragma unroll
@@ -441,12 +511,13 @@ __global__ __launch_bounds__(kWave* NG) void hyb_sp_partial_kernel(
       sc = M::mma(load_op<T>(&sh.k[buf][li][ks * KW + hh * E]), qop[ks], sc);
     // Scaled scores; keys past the range only in the range's last tile
     // (a wave-uniform test, so full tiles carry no masks).
-    const bool full = j0 + kTile <= hi;
+    const bool full = j0 + kTile <= hi && !(WIN && seen.cuts(j0));
     float p[16];
     float mt = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      p[i] = (full || j0 + row_of(i, hh) < hi) ? sc[i] * scale : -INFINITY;
+      const int j = j0 + row_of(i, hh);
+      p[i] = (full || (j < hi && !(WIN && seen.hides(j)))) ? sc[i] * scale : -INFINITY;
       mt = fmaxf(mt, p[i]);
     }
     mt = fmaxf(mt, xor32(mt));
@@ -483,13 +554,13 @@ __global__ __launch_bounds__(kWave* NG) void hyb_sp_partial_kernel(
 #pragma unroll
       for (int ks = 0; ks < C::KL; ++ks)
         acc[ct] = M::mma(vt_op(buf, ct, ks), cvt_op<T>(&p[ks * E]), acc[ct]);
-    if (j0 + kTile < hi) put(nx, buf ^ 1);  // next tile into the free buffer
+    if (after(j0, n, 1) < hi) put(nx, buf ^ 1);  // next tile into the free buffer
     nx = af;
     __syncthreads();
   }
 
   // Partial result of this range: unnormalised O, running max and sum.
-  if (li >= L) return;
+  if (li >= Lb) return;
   if (rg.n == 1) {
     // one range: the result is final, normalised here
     const float inv = 1.0f / l;
@@ -562,7 +633,7 @@ struct alignas(16) SpSlot {
   bf16 v[kTile * D];
 };
 
-template <int D, int NG, bool PAGED>
+template <int D, int NG, bool PAGED, bool WIN = false>
 __global__ __launch_bounds__(kWave* NG, D == 64 && NG == 8 ? 4 : 2) void hyb_sp_ring_kernel(SoftmaxPrefixArgs a, SpCut cut) {
   typedef Mma<bf16> M;
   typedef typename M::op_t op_t;
@@ -584,19 +655,21 @@ __global__ __launch_bounds__(kWave* NG, D == 64 && NG == 8 ? 4 : 2) void hyb_sp_
   // together.
   const int g = blockIdx.x % Hkv, r = blockIdx.x / Hkv, h = g * G + w;
   static_assert(sizeof(s3.v) >= kPlanInts * sizeof(int), "the plan's scratch fits a tile");
-  const SpRange rg = sp_range(a, sp_plan(a, cut, reinterpret_cast<int*>(s3.v)), r, lane);
+  const SpRange rg = sp_range<WIN>(a, sp_plan<WIN>(a, cut, reinterpret_cast<int*>(s3.v)), r, lane);
   if (rg.b < 0) return;  // uniform: past the plan's last range
   const int b = rg.b, lo = rg.lo, hi = rg.hi;
-  const int P = sp_keys(a, b) - L;
-  const int ntiles = (hi - lo + kTile - 1) / kTile;
+  const int Lb = sp_block<WIN>(a, b);  // active queries
+  const int P = sp_keys<WIN>(a, b) - Lb;
+  const SpSeen seen = sp_seen<WIN>(a, b);
+  const int ntiles = WIN ? rg.nt : (hi - lo + kTile - 1) / kTile;
   const size_t qstride = (size_t)Hq * D, kstride = (size_t)Hkv * D;
 
   op_t qop[KD];
   {
     const bf16* qrow =
-        (const bf16*)a.q + ((size_t)b * L * Hq + h) * D + (size_t)min(li, L - 1) * qstride + hh * E;
+        (const bf16*)a.q + ((size_t)b * L * Hq + h) * D + (size_t)min(li, Lb - 1) * qstride + hh * E;
 #pragma unroll
-    for (int ks = 0; ks < KD; ++ks) qop[ks] = keep_if<bf16>(li < L, load_op<bf16>(qrow + ks * KW));
+    for (int ks = 0; ks < KD; ++ks) qop[ks] = keep_if<bf16>(li < Lb, load_op<bf16>(qrow + ks * KW));
   }
   // contiguous: this request's rows; paged: the pool, at KV head g
   const bf16* kc = (const bf16*)a.k_cache + ((PAGED ? 0 : (size_t)b * Pmax * Hkv) + g) * D;
@@ -604,14 +677,28 @@ __global__ __launch_bounds__(kWave* NG, D == 64 && NG == 8 ? 4 : 2) void hyb_sp_
   const bf16* kbk = (const bf16*)a.k + ((size_t)b * L * Hkv + g) * D;
   const bf16* vbk = (const bf16*)a.v + ((size_t)b * L * Hkv + g) * D;
   // Paged: the pages of the cached keys of this range, lo .. min(hi, P) - 1,
-  // staged in LDS (page index p0 + e at e), clamped to the pool.
+  // staged in LDS (page index p0 + e at e; behind page pa, the last before the
+  // skipped tiles, p0 + e + pskip), clamped to the pool.
   __shared__ int pages[PAGED ? kMaxRangePages : 1];
   const int p0 = lo >> a.page_shift;
+  int pa = 0x7fffffff, pskip = 0;
+  if constexpr (WIN) {
+    if (seen.skip > 0 && rg.t0 < seen.st && rg.t0 + rg.nt > seen.st) {
+      pa = (seen.st * kTile - 1) >> a.page_shift;
+      pskip = max(0, ((seen.st + seen.skip) * kTile >> a.page_shift) - pa - 1);
+    }
+  }
+  auto page_of = [&](int pi) __attribute__((always_inline)) {
+    return pages[pi - p0 - (WIN && pi > pa ? pskip : 0)];
+  };
   if constexpr (PAGED) {
     const int32_t* ptab = a.page_table + (size_t)b * a.max_pages;
     const int chi = min(hi, P);
-    const int np = chi > lo ? ((chi - 1) >> a.page_shift) - p0 + 1 : 0;
-    for (int e = tid; e < np; e += kWave * NG) pages[e] = sp_page(a, ptab, (p0 + e) << a.page_shift);
+    const int np = chi > lo ? ((chi - 1) >> a.page_shift) - p0 + 1 - pskip : 0;
+    for (int e = tid; e < np; e += kWave * NG) {
+      const int pi = p0 + e + (WIN && p0 + e > pa ? pskip : 0);
+      pages[e] = sp_page(a, ptab, pi << a.page_shift);
+    }
     __syncthreads();
   }
 
@@ -638,19 +725,23 @@ __global__ __launch_bounds__(kWave* NG, D == 64 && NG == 8 ? 4 : 2) void hyb_sp_
   // code was twice as long, and a short range, which runs it once, waited for its
   // instructions: with one head per KV head at d = 128 one request of 300 keys
   // took 21.4 us, now 15.7, 32 of 512 28.1 and 24.1, 32 of 4096 138 and 115.)
-  const int nlate = ntiles - (cend > lo ? (cend - lo) / kTile : 0);
+  // With WIN (every tile of the list is one of the whole, 32-aligned tiles of
+  // the keys) those wholly in the cache are the tiles below P / 32.
+  const int nlate =
+      WIN ? ntiles - min(max(P / kTile - seen.skip - rg.t0, 0), ntiles) : ntiles - (cend > lo ? (cend - lo) / kTile : 0);
   auto first_key = [&](int n) __attribute__((always_inline)) {
-    return lo + (n < nlate ? ntiles - 1 - n : n - nlate) * kTile;
+    const int i = n < nlate ? ntiles - 1 - n : n - nlate;
+    return WIN ? seen.tile(rg.t0 + i) * kTile : lo + i * kTile;
   };
   constexpr int NKV = NG == 1 ? 2 : 1;      // kinds of copies per wave
   constexpr int IPK = IPW / NKV;            // copies per kind
   // This wave's copies u0 .. u0 + IPK - 1, of kind kv, of tile n into dst.
   auto issue_cached = [&](int kv, int u0, int n, bf16* dst) __attribute__((always_inline)) {
-    const int j0 = lo + (n - nlate) * kTile;
+    const int j0 = WIN ? first_key(n) : lo + (n - nlate) * kTile;
     const bf16* cb = sp_pick(kv == 0, kc, vc);
     if constexpr (PAGED) {
       const int pi = j0 >> a.page_shift;
-      cb += ((ptrdiff_t)__builtin_amdgcn_readfirstlane(pages[pi - p0]) - pi) *
+      cb += ((ptrdiff_t)__builtin_amdgcn_readfirstlane(page_of(pi)) - pi) *
             ((ptrdiff_t)kstride << a.page_shift);
     }
     cb += (size_t)j0 * kstride;
@@ -670,7 +761,7 @@ __global__ __launch_bounds__(kWave* NG, D == 64 && NG == 8 ? 4 : 2) void hyb_sp_
       // row j0: that page's base, shifted so that base + j * kstride is row j
       if (j0 < P) {
         const int pi = j0 >> a.page_shift;
-        cb += ((ptrdiff_t)pages[pi - p0] - pi) * ((ptrdiff_t)kstride << a.page_shift);
+        cb += ((ptrdiff_t)page_of(pi) - pi) * ((ptrdiff_t)kstride << a.page_shift);
       }
     }
     const bf16* blk = sp_pick(kv == 0, kbk, vbk);
@@ -678,7 +769,8 @@ __global__ __launch_bounds__(kWave* NG, D == 64 && NG == 8 ? 4 : 2) void hyb_sp_
     for (int u = u0; u < u0 + IPK; ++u) {
       const int i = (w * IPW + u) % IK;
       const int t = i * RPI + lane / CPR, pos = lane % CPR;
-      const int j = min(j0 + t, hi - 1);
+      int j = min(j0 + t, hi - 1);
+      if constexpr (WIN) j = seen.hides(j) ? seen.stand_in(j0) : j;
       const bf16* row = sp_pick(j < P, cb, blk) + (size_t)(j < P ? j : j - P) * kstride;
       __builtin_amdgcn_global_load_lds(
           (const __attribute__((address_space(1))) void*)(row + (pos ^ (kv == 0 ? RG::swz(t) : RG::vswz(t))) * EPC),
@@ -689,8 +781,8 @@ __global__ __launch_bounds__(kWave* NG, D == 64 && NG == 8 ? 4 : 2) void hyb_sp_
   // (early: tiles 0 and 1, which may reach past the cache).
   auto issue = [&](auto early, int nk, SpSlot<D>& sk, int nv, SpSlot<D>& sv) __attribute__((always_inline)) {
     auto one = [&](int kv, int u0, int n, bf16* dst) __attribute__((always_inline)) {
-      if constexpr (decltype(early)::value) {
-        if (n < nlate) {
+      if constexpr (decltype(early)::value || WIN) {
+        if (n < nlate || (WIN && seen.cuts(first_key(n)))) {
           issue_general(kv, u0, n, dst);
           return;
         }
@@ -741,11 +833,14 @@ __global__ __launch_bounds__(kWave* NG, D == 64 && NG == 8 ? 4 : 2) void hyb_sp_
   // are masked.
   auto take_scores = [&](auto check, int n, const f32x16& s) __attribute__((always_inline)) {
     sc = s;
-    if constexpr (decltype(check)::value) {
+    if constexpr (decltype(check)::value || WIN) {
       const int j0 = first_key(n);
-      if (j0 + kTile > hi) {  // uniform
+      if (j0 + kTile > hi || (WIN && seen.cuts(j0))) {  // uniform
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sc[i] = j0 + row_of(i, hh) < hi ? sc[i] : -INFINITY;
+        for (int i = 0; i < 16; ++i) {
+          const int j = j0 + row_of(i, hh);
+          sc[i] = j < hi && !(WIN && seen.hides(j)) ? sc[i] : -INFINITY;
+        }
       }
     }
     float mt = sc[0];
@@ -890,7 +985,7 @@ __global__ __launch_bounds__(kWave* NG, D == 64 && NG == 8 ? 4 : 2) void hyb_sp_
   const int rest = ntiles - n;  // 1 .. R
   compute(yes, ntiles - 1, nullptr, rest == 2 ? s1.v : rest == 3 ? s2.v : rest == 4 ? s3.v : s0.v);
 
-  if (li >= L) return;
+  if (li >= Lb) return;
   const float l = lsum[0];
   if (rg.n == 1) {
     // one range: the result is final, normalised here
@@ -930,12 +1025,12 @@ __global__ __launch_bounds__(kWave* NG, D == 64 && NG == 8 ? 4 : 2) void hyb_sp_
 // requests of 1024 keys 12.3 us, where 1024 workgroups of two units with
 // the rows requested after the maxima took 13.7 us (8 requests: 7.2, now
 // 5.4).
-template <typename T, int D>
+template <typename T, int D, bool WIN = false>
 __global__ __launch_bounds__(256) void hyb_sp_combine_kernel(SoftmaxPrefixArgs a, SpCut cut) {
   constexpr int TPR = D / 4;              // threads per row
   constexpr int RPB = 256 / TPR;          // rows per unit
   __shared__ alignas(16) int plan[kPlanInts];
-  const SpPlan p = sp_plan(a, cut, plan);
+  const SpPlan p = sp_plan<WIN>(a, cut, plan);
   if (p.whole) return;  // every row is already written out
   const int Hq = a.s.Hq, L = a.s.L, lane = threadIdx.x & (kWave - 1);
   const int upb = (L + RPB - 1) / RPB;    // units of a (request, head)
@@ -944,13 +1039,13 @@ __global__ __launch_bounds__(256) void hyb_sp_combine_kernel(SoftmaxPrefixArgs a
   const size_t step = (size_t)Hq * L;  // rows from one range to the next
   for (int u = blockIdx.x; u < a.s.B * Hq * upb; u += gridDim.x) {
     const int bh = u / upb, b = bh / Hq, h = bh % Hq;
-    const int n = sp_ranges(p, sp_tiles(a, b));
-    if (n == 1) continue;  // uniform: already written out
+    const int n = sp_ranges(p, sp_tiles<WIN>(a, b));
+    if (n == 1 || (WIN && n == 0)) continue;  // uniform: already written out (or no query)
     int base = 0;
-    for (int b0 = lane; b0 < b; b0 += kWave) base += sp_ranges(p, sp_tiles(a, b0));
+    for (int b0 = lane; b0 < b; b0 += kWave) base += sp_ranges(p, sp_tiles<WIN>(a, b0));
     base = wave_all(base, AddOp{});
     const int i = u % upb * RPB + threadIdx.x / TPR, c = (threadIdx.x % TPR) * 4;
-    if (i >= L) continue;  // (no barrier or exchange follows in this unit)
+    if (i >= (WIN ? sp_block<WIN>(a, b) : L)) continue;  // (no barrier or exchange follows in this unit)
     const size_t row0 = sp_row(a, base, h, i);
     float M = -INFINITY;
     f32x4 num = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -1043,7 +1138,7 @@ static hipError_t sp_launch(K kernel, int resident, int waves, bool ring, const 
   cut.sat = ring ? max(1, min(cut.slots, (waves > 4 ? 256 : 512) / a.s.Hkv)) : cut.slots;
   // Ranges of a plan at most: three rounds, within the workspace, and at
   // least what the longest range allows.
-  const int need = (int)(((long)a.max_prefix + a.s.L + kMaxRange - 1) / kMaxRange);
+  const int need = (int)(((long)a.max_seen + a.s.L + kMaxRange - 1) / kMaxRange);
   cut.limit = min(a.s.B * ns, max(a.s.B * need, 3 * cut.sat));
   cut.layer = max(1, 256 / a.s.Hkv);
   // Where ranges of at most 512 keys of full-length requests fit one round,
@@ -1051,7 +1146,7 @@ static hipError_t sp_launch(K kernel, int resident, int waves, bool ring, const 
   // lengths, and working a plan out costs each kernel a few us (32 requests of
   // 1024 keys 43.8 against 37.4 us so, 8 of 4096 43.5 and 39.4, one of 8192
   // 32.7 and 28.8).
-  const int tmax = (int)(((long)a.max_prefix + a.s.L + kTile - 1) / kTile);
+  const int tmax = (int)(((long)a.max_seen + a.s.L + kTile - 1) / kTile);
   const int even = (tmax + ns - 1) / ns;
   cut.c = 0;
   if ((long)a.s.B * ns <= cut.slots && even <= 16) {
@@ -1063,7 +1158,7 @@ static hipError_t sp_launch(K kernel, int resident, int waves, bool ring, const 
   return hipGetLastError();
 }
 
-template <typename T, int D, bool PAGED>
+template <typename T, int D, bool PAGED, bool WIN>
 static hipError_t sp_go(const SoftmaxPrefixArgs& a, hipStream_t st) {
   SpCut cut;
   hipError_t e;
@@ -1072,8 +1167,9 @@ static hipError_t sp_go(const SoftmaxPrefixArgs& a, hipStream_t st) {
 #define HYB_SP_CASE(NG, RING, ...)                                              \
   case NG: {                                                                    \
     static const int resident =                                                 \
-        min(sp_resident(__VA_ARGS__, true>, NG), sp_resident(__VA_ARGS__, false>, NG)); \
-    e = sp_launch(__VA_ARGS__, PAGED>, resident, NG, RING, a, st, &cut);        \
+        WIN ? sp_resident(__VA_ARGS__, true, true>, NG)                         \
+            : min(sp_resident(__VA_ARGS__, true>, NG), sp_resident(__VA_ARGS__, false>, NG)); \
+    e = sp_launch(__VA_ARGS__, PAGED, WIN>, resident, NG, RING, a, st, &cut);   \
     break;                                                                      \
   }
   // bf16 with 1, 2, 4 or 8 query heads per KV head: the copy ring; else the
@@ -1106,20 +1202,22 @@ static hipError_t sp_go(const SoftmaxPrefixArgs& a, hipStream_t st) {
 #undef HYB_SP_CASE
   if (e != hipSuccess || a.n_split == 1) return e;  // one range: already written out
   const long units = (long)a.s.B * a.s.Hq * ((a.s.L + 1024 / D - 1) / (1024 / D));
-  hipLaunchKernelGGL((hyb_sp_combine_kernel<T, D>), dim3((unsigned)std::min<long>(units, 2048)), dim3(256), 0, st,
+  hipLaunchKernelGGL((hyb_sp_combine_kernel<T, D, WIN>), dim3((unsigned)std::min<long>(units, 2048)), dim3(256), 0, st,
                      a, cut);
   return hipGetLastError();
 }
 
-template <bool PAGED>
+template <bool PAGED, bool WIN = false>
 static hipError_t sp_dispatch(const SoftmaxPrefixArgs& a, hipStream_t st) {
   if (a.s.dtype == 1)
-    return a.s.D == 64 ? sp_go<bf16, 64, PAGED>(a, st) : sp_go<bf16, 128, PAGED>(a, st);
-  return a.s.D == 64 ? sp_go<float, 64, PAGED>(a, st) : sp_go<float, 128, PAGED>(a, st);
+    return a.s.D == 64 ? sp_go<bf16, 64, PAGED, WIN>(a, st) : sp_go<bf16, 128, PAGED, WIN>(a, st);
+  return a.s.D == 64 ? sp_go<float, 64, PAGED, WIN>(a, st) : sp_go<float, 128, PAGED, WIN>(a, st);
 }
 
 hipError_t launch_softmax_prefix(const SoftmaxPrefixArgs& a, hipStream_t st) {
   if (a.s.Hq / a.s.Hkv > kMaxGroup) return hipErrorInvalidValue;
+  // (without pages no token is cached: max_prefix is 0 and the pools are not read)
+  if (a.window >= 0) return sp_dispatch<true, true>(a, st);
   if (a.page_table) {
     if (a.page_shift < 5 || a.n_pages < 1) return hipErrorInvalidValue;
     return sp_dispatch<true>(a, st);

@@ -1,0 +1,424 @@
+// window.hip -- softmax attention over a sequence in which a token sees its
+// own block, the `window` tokens before the block and the first n_sinks
+// tokens, and its gradient: the block-causal pattern of Figure 2 with the
+// softmax of Section 2.2 in place of the state, as the softmax layers that
+// stay beside the hybrid ones run it over a prompt, as the teacher of the
+// attention transfer runs it (window >= T: every earlier block), and as their
+// end-to-end training differentiates it.
+//
+// For query i with block start s = (i / L) L:
+//   seen(i) = { j < min(s + L, len) : j >= s - window or j < n_sinks }
+//   out_i = sum_j P_ij v_j,  P_ij = exp(q_i k_j / sqrt(d) - lse_i)
+//   dP_ij = dout_i v_j,  dS_ij = P_ij (dP_ij - delta_i),  delta_i = dout_i out_i
+//   dv_j = sum_i P_ij dout_i,  dq_i = sum_j dS_ij k_j / sqrt(d),
+//   dk_j = sum_i dS_ij q_i / sqrt(d)
+// A query always sees itself, so no row is empty.
+//
+// Bound: the matrix cores (4 d flops per pair of query and key forward, 14 d
+// backward, where the scores and dP are formed by both gradient kernels so
+// that each gradient is summed by the wave that owns its rows: no atomics,
+// the same bits every time).  Products are 32x32 tiles, transposed so that
+// each accumulator tile is the next product's operand without leaving its
+// registers (device.h).
+#include <algorithm>
+#include <type_traits>
+
+#include "device.h"
+#include "launch.h"
+
+namespace hyb {
+
+// Reference of a query that has seen no key yet: finite, so that a tile in
+// which it sees none leaves weights of exactly zero.
+constexpr float kNoRef = -1e30f;
+
+__device__ inline int win_len(const WindowArgs& a, int b) {
+  return a.seq_lens ? min(max(a.seq_lens[b], 0), a.T) : a.T;
+}
+
+// What query i (below len) sees: keys lo .. end - 1, and those below sinks.
+struct WinRow {
+  int lo, end;
+  __device__ inline WinRow(const WindowArgs& a, int len, int i) {
+    const int s0 = i / a.s.L * a.s.L;
+    lo = max(0, s0 - a.window);
+    end = min(s0 + min(a.s.L, len - s0), len);
+  }
+  __device__ inline bool sees(int j, int sinks) const { return j < end && (j >= lo || j < sinks); }
+};
+
+// The key tiles that the queries i0 .. i1 - 1 see some of: tiles 0 .. st - 1
+// (the sinks) and from st + skip on, n in all.
+struct WinTiles {
+  int st, skip, n;
+  __device__ inline WinTiles(const WindowArgs& a, int len, int i0, int i1, int tile) {
+    const int lo = WinRow(a, len, i0).lo, end = WinRow(a, len, i1 - 1).end;
+    st = (min(a.n_sinks, lo) + tile - 1) / tile;
+    skip = max(0, lo / tile - st);
+    n = (end + tile - 1) / tile - skip;
+  }
+  __device__ inline int first(int x, int tile) const { return (x < st ? x : x + skip) * tile; }
+};
+
+// Queries i0 .. i1 - 1 and the keys j0 .. j0 + n - 1: whether every query sees
+// every key, and whether any sees any.
+__device__ inline bool win_full(const WinRow& r0, const WinRow& r1, int sinks, int j0, int n) {
+  return j0 + n <= r0.end && (j0 >= r1.lo || j0 + n <= sinks);
+}
+__device__ inline bool win_none(const WinRow& r0, const WinRow& r1, int sinks, int j0, int n) {
+  return j0 >= r1.end || (j0 + n <= r0.lo && j0 >= sinks);
+}
+
+// ---- plain kernels (fp32) ---------------------------------------------------
+//
+// One wave per 32 rows (queries of a head; keys of a KV head in the dK, dV
+// kernel), four waves per workgroup sharing the tiles they loop over through
+// LDS.  fp32 products run at 1/16 of the bf16 rate, so the loop waits for its
+// MFMAs whatever the staging does.
+
+constexpr int kWinWaves = 4;
+
+template <typename T, int D>
+struct WinCfg {
+  typedef Mma<T> M;
+  static constexpr int KD = D / M::KW, KL = kTile / M::KW, NCT = D / kTile;
+  static constexpr int EPC = 16 / (int)sizeof(T), CPR = D / EPC;
+  static constexpr int LD = D + 2 * EPC;  // row pitch in LDS
+  typedef T Tile[kTile][LD];
+  typedef typename M::op_t Ops[KD];
+  typedef f32x16 Acc[NCT];
+};
+
+// Rows row0 .. row0 + 31 of src (row stride in elements), zero from row `rows`
+// on, into a tile; all threads of the workgroup.
+template <typename T, int D>
+__device__ inline void win_stage(typename WinCfg<T, D>::Tile& dst, const T* src, size_t stride, int row0, int rows) {
+  typedef WinCfg<T, D> C;
+  for (int x = threadIdx.x; x < kTile * C::CPR; x += kWave * kWinWaves) {
+    const int r = x / C::CPR, c = x % C::CPR * C::EPC;
+    uint4 v = {0, 0, 0, 0};
+    if (row0 + r < rows) v = *reinterpret_cast<const uint4*>(src + (size_t)(row0 + r) * stride + c);
+    *reinterpret_cast<uint4*>(&dst[r][c]) = v;
+  }
+}
+// A row as an operand (zero past the last row).
+template <typename T, int D>
+__device__ inline void win_row_ops(typename WinCfg<T, D>::Ops& op, const T* row, bool ok, int hh) {
+  typedef Mma<T> M;
+#pragma unroll
+  for (int ks = 0; ks < WinCfg<T, D>::KD; ++ks) op[ks] = ok ? load_op<T>(row + ks * M::KW + hh * M::E) : M::zero();
+}
+// tile rows times the operands of 32 columns: rows in accumulator order.
+template <typename T, int D>
+__device__ inline f32x16 win_rows_mma(const typename WinCfg<T, D>::Tile& t, const typename Mma<T>::op_t* op, int li,
+                                      int hh) {
+  typedef Mma<T> M;
+  f32x16 s = {};
+#pragma unroll
+  for (int ks = 0; ks < WinCfg<T, D>::KD; ++ks) s = M::mma(load_op<T>(&t[li][ks * M::KW + hh * M::E]), op[ks], s);
+  return s;
+}
+// acc[D][32] += tile^T x, x in accumulator order over the tile's rows.
+template <typename T, int D>
+__device__ inline void win_cols_mma(typename WinCfg<T, D>::Acc& acc, const typename WinCfg<T, D>::Tile& t,
+                                    const float (&x)[16], int li, int hh) {
+  typedef WinCfg<T, D> C;
+  typedef Mma<T> M;
+#pragma unroll
+  for (int ct = 0; ct < C::NCT; ++ct)
+#pragma unroll
+    for (int ks = 0; ks < C::KL; ++ks) {
+      typename M::op_t a;
+      if constexpr (M::E == 1) {
+        a = t[row_of(ks, hh)][ct * kTile + li];
+      } else {
+#pragma unroll
+        for (int e = 0; e < M::E; ++e) a[e] = t[row_of(ks * M::E + e, hh)][ct * kTile + li];
+      }
+      acc[ct] = M::mma(a, cvt_op<T>(&x[ks * M::E]), acc[ct]);
+    }
+}
+// acc^T (times f) to row `row` of out.
+template <typename T, int D>
+__device__ inline void win_store(void* out, size_t row, const typename WinCfg<T, D>::Acc& acc, float f, int hh,
+                                 bool f32) {
+#pragma unroll
+  for (int ct = 0; ct < WinCfg<T, D>::NCT; ++ct)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const float o[4] = {acc[ct][i] * f, acc[ct][i + 1] * f, acc[ct][i + 2] * f, acc[ct][i + 3] * f};
+      store_out4<T>(out, row * D + ct * kTile + row_of(i, hh), o, f32);
+    }
+}
+
+// Units of the query kernels: 32 queries of one head; the heads of a KV head
+// vary fastest, so that a workgroup's waves share their keys.
+struct WinUnit {
+  int b, g, h, i0;  // request, KV head, query head, first query
+  bool any;
+};
+__device__ inline WinUnit win_unit(const WindowArgs& a, int len, int b, int g, int u) {
+  const int G = a.s.Hq / a.s.Hkv;
+  const int i0 = u / G * kTile;
+  return WinUnit{b, g, g * G + u % G, i0, i0 < len};
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_fwd_kernel(WindowArgs a, int wgs) {
+  typedef WinCfg<T, D> C;
+  typedef Mma<T> M;
+  __shared__ alignas(16) typename C::Tile kt, vt;
+  const int lane = threadIdx.x & (kWave - 1), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int li = lane & 31, hh = lane >> 5;
+  const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv;
+  const int bg = blockIdx.x / wgs, x = wgs - 1 - blockIdx.x % wgs, b = bg / Hkv, g = bg % Hkv;  // longest first
+  const int len = win_len(a, b);
+  const WinUnit me = win_unit(a, len, b, g, x * kWinWaves + w);
+  const int first = x * kWinWaves / G * kTile, last = min(((x + 1) * kWinWaves - 1) / G * kTile + kTile, len);
+  if (first >= len) return;  // uniform
+  const WinTiles tl(a, len, first, last, kTile);
+  const size_t qs = (size_t)Hq * D, ks_ = (size_t)Hkv * D;
+  const T* K = (const T*)a.k + ((size_t)b * a.T * Hkv + g) * D;
+  const T* V = (const T*)a.v + ((size_t)b * a.T * Hkv + g) * D;
+  const int i = min(me.i0 + li, len - 1);
+  const WinRow row(a, len, i), r0(a, len, min(me.i0, len - 1)), r1(a, len, min(me.i0 + kTile, len) - 1);
+  typename M::op_t qop[C::KD];
+  win_row_ops<T, D>(qop, (const T*)a.q + ((size_t)b * a.T * Hq + me.h) * D + i * qs, true, hh);
+  const float scale = kLog2e / sqrtf((float)D);
+  float m = kNoRef, l = 0.0f;
+  f32x16 acc[C::NCT];
+#pragma unroll
+  for (int ct = 0; ct < C::NCT; ++ct) acc[ct] = f32x16{};
+  for (int n = 0; n < tl.n; ++n) {
+    const int j0 = tl.first(n, kTile);
+    __syncthreads();
+    win_stage<T, D>(kt, K, ks_, j0, len);
+    win_stage<T, D>(vt, V, ks_, j0, len);
+    __syncthreads();
+    if (!me.any || win_none(r0, r1, a.n_sinks, j0, kTile)) continue;  // uniform over the wave
+    const f32x16 sc = win_rows_mma<T, D>(kt, qop, li, hh);
+    const bool full = win_full(r0, r1, a.n_sinks, j0, kTile);
+    float p[16], mt = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      p[e] = full || row.sees(j0 + row_of(e, hh), a.n_sinks) ? sc[e] * scale : -INFINITY;
+      mt = fmaxf(mt, p[e]);
+    }
+    mt = fmaxf(mt, xor32(mt));
+    const float mn = fmaxf(m, mt);
+    if (__any(mn > m)) {
+      const float corr = __builtin_amdgcn_exp2f(m - mn);
+      l *= corr;
+#pragma unroll
+      for (int ct = 0; ct < C::NCT; ++ct) acc[ct] *= corr;
+      m = mn;
+    }
+    float ps = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      p[e] = __builtin_amdgcn_exp2f(p[e] - m);
+      ps += p[e];
+    }
+    l += ps + xor32(ps);
+    win_cols_mma<T, D>(acc, vt, p, li, hh);
+  }
+  if (!me.any || me.i0 + li >= len) return;
+  win_store<T, D>(a.out, ((size_t)b * a.T + i) * Hq + me.h, acc, 1.0f / l, hh, a.s.out_f32);
+  if (a.lse && hh == 0) a.lse[((size_t)b * Hq + me.h) * a.T + i] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
+// delta_i = dout_i out_i of every row, [B][Hq][T] (zero past a length); D / 8
+// lanes per row.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void hyb_win_delta_kernel(WindowArgs a) {
+  constexpr int LPR = D / 8;
+  const long rows = (long)a.s.B * a.T * a.s.Hq;
+  for (long r = (long)blockIdx.x * (256 / LPR) + threadIdx.x / LPR; r < rows; r += (long)gridDim.x * (256 / LPR)) {
+    const int h = (int)(r % a.s.Hq);
+    const long bi = r / a.s.Hq;
+    const int b = (int)(bi / a.T), i = (int)(bi % a.T);
+    float s = 0.0f;
+    if (i < win_len(a, b)) {
+      const T* x = (const T*)a.out + r * D + threadIdx.x % LPR * 8;
+      const T* y = (const T*)a.dout + r * D + threadIdx.x % LPR * 8;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s += (float)x[e] * (float)y[e];
+    }
+#pragma unroll
+    for (int o = 1; o < LPR; o <<= 1) s += __shfl_xor(s, o);
+    if (threadIdx.x % LPR == 0) a.delta[((size_t)b * a.s.Hq + h) * a.T + i] = s;
+  }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dq_kernel(WindowArgs a, int wgs) {
+  typedef WinCfg<T, D> C;
+  typedef Mma<T> M;
+  __shared__ alignas(16) typename C::Tile kt, vt;
+  const int lane = threadIdx.x & (kWave - 1), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int li = lane & 31, hh = lane >> 5;
+  const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv;
+  const int bg = blockIdx.x / wgs, x = wgs - 1 - blockIdx.x % wgs, b = bg / Hkv, g = bg % Hkv;
+  const int len = win_len(a, b);
+  const WinUnit me = win_unit(a, len, b, g, x * kWinWaves + w);
+  const int first = x * kWinWaves / G * kTile, last = min(((x + 1) * kWinWaves - 1) / G * kTile + kTile, len);
+  const size_t qs = (size_t)Hq * D, ks_ = (size_t)Hkv * D;
+  f32x16 acc[C::NCT];
+#pragma unroll
+  for (int ct = 0; ct < C::NCT; ++ct) acc[ct] = f32x16{};
+  if (first < len) {  // uniform
+    const WinTiles tl(a, len, first, last, kTile);
+    const T* K = (const T*)a.k + ((size_t)b * a.T * Hkv + g) * D;
+    const T* V = (const T*)a.v + ((size_t)b * a.T * Hkv + g) * D;
+    const int i = min(me.i0 + li, len - 1);
+    const WinRow row(a, len, i), r0(a, len, min(me.i0, len - 1)), r1(a, len, min(me.i0 + kTile, len) - 1);
+    typename M::op_t qop[C::KD], dop[C::KD];
+    const size_t at = ((size_t)b * a.T * Hq + me.h) * D + i * qs;
+    win_row_ops<T, D>(qop, (const T*)a.q + at, true, hh);
+    win_row_ops<T, D>(dop, (const T*)a.dout + at, true, hh);
+    const float scale = kLog2e / sqrtf((float)D);
+    const size_t st = ((size_t)b * Hq + me.h) * a.T + i;
+    const float lse = a.lse[st] * kLog2e, delta = a.delta[st];
+    for (int n = 0; n < tl.n; ++n) {
+      const int j0 = tl.first(n, kTile);
+      __syncthreads();
+      win_stage<T, D>(kt, K, ks_, j0, len);
+      win_stage<T, D>(vt, V, ks_, j0, len);
+      __syncthreads();
+      if (!me.any || win_none(r0, r1, a.n_sinks, j0, kTile)) continue;
+      const f32x16 sc = win_rows_mma<T, D>(kt, qop, li, hh);
+      const f32x16 dp = win_rows_mma<T, D>(vt, dop, li, hh);
+      const bool full = win_full(r0, r1, a.n_sinks, j0, kTile);
+      float ds[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float p = full || row.sees(j0 + row_of(e, hh), a.n_sinks)
+                            ? __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale, -lse))
+                            : 0.0f;
+        ds[e] = p * (dp[e] - delta);
+      }
+      win_cols_mma<T, D>(acc, kt, ds, li, hh);
+    }
+  }
+  if (me.i0 + li >= a.T) return;  // rows past the length: zero
+  win_store<T, D>(a.dq, ((size_t)b * a.T + me.i0 + li) * Hq + me.h, acc,
+                  me.i0 + li < len ? 1.0f / sqrtf((float)D) : 0.0f, hh, a.s.out_f32);
+}
+
+// The queries that see some of the keys j0 .. j1 - 1 (j1 <= len): from q0 to q1 - 1.
+struct WinQueries {
+  int q0, q1;
+  __device__ inline WinQueries(const WindowArgs& a, int len, int j0, int j1) {
+    const int L = a.s.L;
+    q0 = j0 / L * L;
+    const long last = ((long)(j1 - 1) + a.window) / L * L + L;  // blocks that start by j1 - 1 + window
+    q1 = j0 < a.n_sinks ? len : (int)min(last, (long)len);
+  }
+};
+
+// dK, dV: a wave owns 32 keys, and loops over the queries of all heads of
+// its KV head.
+template <typename T, int D>
+__global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dkv_kernel(WindowArgs a, int wgs) {
+  typedef WinCfg<T, D> C;
+  typedef Mma<T> M;
+  __shared__ alignas(16) typename C::Tile qt, dt;
+  __shared__ alignas(16) float lse[kTile], delta[kTile];
+  const int lane = threadIdx.x & (kWave - 1), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int li = lane & 31, hh = lane >> 5;
+  const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv;
+  const int bg = blockIdx.x / wgs, x = blockIdx.x % wgs, b = bg / Hkv, g = bg % Hkv;
+  const int len = win_len(a, b);
+  const int w0 = x * kWinWaves * kTile, j0 = w0 + w * kTile, j = j0 + li;  // first key of the workgroup, of the wave
+  const size_t qs = (size_t)Hq * D, ks_ = (size_t)Hkv * D;
+  f32x16 dk[C::NCT], dv[C::NCT];
+#pragma unroll
+  for (int ct = 0; ct < C::NCT; ++ct) dk[ct] = dv[ct] = f32x16{};
+  if (w0 < len) {  // uniform
+    const WinQueries all(a, len, w0, min(w0 + kWinWaves * kTile, len));
+    typename M::op_t kop[C::KD], vop[C::KD];
+    const size_t at = ((size_t)b * a.T * Hkv + g) * D + (size_t)min(j, len - 1) * ks_;
+    win_row_ops<T, D>(kop, (const T*)a.k + at, j < len, hh);
+    win_row_ops<T, D>(vop, (const T*)a.v + at, j < len, hh);
+    const float scale = kLog2e / sqrtf((float)D);
+    for (int h = g * G; h < g * G + G; ++h) {
+      const size_t head = ((size_t)b * a.T * Hq + h) * D, st = ((size_t)b * Hq + h) * a.T;
+      for (int i0 = all.q0 / kTile * kTile; i0 < all.q1; i0 += kTile) {
+        __syncthreads();
+        win_stage<T, D>(qt, (const T*)a.q + head, qs, i0, len);
+        win_stage<T, D>(dt, (const T*)a.dout + head, qs, i0, len);
+        if (threadIdx.x < kTile) {
+          const int i = min(i0 + (int)threadIdx.x, len - 1);
+          lse[threadIdx.x] = a.lse[st + i] * kLog2e;
+          delta[threadIdx.x] = a.delta[st + i];
+        }
+        __syncthreads();
+        const WinRow r0(a, len, i0), r1(a, len, min(i0 + kTile, len) - 1);
+        if (j0 >= len || win_none(r0, r1, a.n_sinks, j0, kTile)) continue;
+        const f32x16 sc = win_rows_mma<T, D>(qt, kop, li, hh);
+        const f32x16 dp = win_rows_mma<T, D>(dt, vop, li, hh);
+        const bool full = i0 + kTile <= len && win_full(r0, r1, a.n_sinks, j0, kTile);
+        float p[16], ds[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int r = row_of(e, hh), i = i0 + r;
+          const bool sees = full || (i < len && WinRow(a, len, min(i, len - 1)).sees(j, a.n_sinks));
+          p[e] = sees ? __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale, -lse[r])) : 0.0f;
+          ds[e] = p[e] * (dp[e] - delta[r]);
+        }
+        win_cols_mma<T, D>(dv, dt, p, li, hh);
+        win_cols_mma<T, D>(dk, qt, ds, li, hh);
+      }
+    }
+  }
+  if (j >= a.T) return;
+  const size_t row = ((size_t)b * a.T + j) * Hkv + g;
+  win_store<T, D>(a.dk, row, dk, j < len ? 1.0f / sqrtf((float)D) : 0.0f, hh, a.s.out_f32);
+  win_store<T, D>(a.dv, row, dv, j < len ? 1.0f : 0.0f, hh, a.s.out_f32);
+}
+
+static int win_wgs(const WindowArgs& a) {  // workgroups of a (request, KV head): its queries' units, four at a time
+  const long units = ((long)a.T + kTile - 1) / kTile * (a.s.Hq / a.s.Hkv);
+  return (int)((units + kWinWaves - 1) / kWinWaves);
+}
+
+template <typename T, int D>
+static hipError_t win_prefill_go(const WindowArgs& a, hipStream_t st) {
+  const int wgs = win_wgs(a);
+  hipLaunchKernelGGL((hyb_win_fwd_kernel<T, D>), dim3((unsigned)(a.s.B * a.s.Hkv * wgs)), dim3(kWave * kWinWaves), 0,
+                     st, a, wgs);
+  return hipGetLastError();
+}
+
+template <typename T, int D>
+static hipError_t win_backward_go(const WindowArgs& a, hipStream_t st) {
+  const long rows = (long)a.s.B * a.T * a.s.Hq;
+  hipLaunchKernelGGL((hyb_win_delta_kernel<T, D>), dim3((unsigned)std::min<long>((rows * D / 8 + 255) / 256, 4096)),
+                     dim3(256), 0, st, a);
+  const int wgs = win_wgs(a), kwgs = (a.T + kWinWaves * kTile - 1) / (kWinWaves * kTile);
+  hipLaunchKernelGGL((hyb_win_dq_kernel<T, D>), dim3((unsigned)(a.s.B * a.s.Hkv * wgs)), dim3(kWave * kWinWaves), 0,
+                     st, a, wgs);
+  hipLaunchKernelGGL((hyb_win_dkv_kernel<T, D>), dim3((unsigned)(a.s.B * a.s.Hkv * kwgs)), dim3(kWave * kWinWaves), 0,
+                     st, a, kwgs);
+  return hipGetLastError();
+}
+
+hipError_t launch_window_prefill(const WindowArgs& a, hipStream_t st) {
+  if (a.s.dtype == 1) return a.s.D == 64 ? win_prefill_go<bf16, 64>(a, st) : win_prefill_go<bf16, 128>(a, st);
+  return a.s.D == 64 ? win_prefill_go<float, 64>(a, st) : win_prefill_go<float, 128>(a, st);
+}
+
+hipError_t launch_window_backward(const WindowArgs& a, hipStream_t st) {
+  if (a.s.dtype == 1) return a.s.D == 64 ? win_backward_go<bf16, 64>(a, st) : win_backward_go<bf16, 128>(a, st);
+  return a.s.D == 64 ? win_backward_go<float, 64>(a, st) : win_backward_go<float, 128>(a, st);
+}
+
+// Workgroups of the largest launch (the grid's limit is checked by the caller).
+long window_workgroups(const Shape& s, int T) {
+  const long units = ((long)T + kTile - 1) / kTile * (s.Hq / s.Hkv);
+  return (long)s.B * s.Hkv * ((units + kWinWaves - 1) / kWinWaves);
+}
+
+size_t window_backward_ws_bytes(const Shape& s, int T) { return (size_t)s.B * s.Hq * T * sizeof(float); }
+
+}  // namespace hyb
