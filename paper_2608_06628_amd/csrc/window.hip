@@ -377,9 +377,235 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dkv_kernel(WindowArg
   win_store<T, D>(a.dv, row, dv, j < len ? 1.0f : 0.0f, hh, a.s.out_f32);
 }
 
-static int win_wgs(const WindowArgs& a) {  // workgroups of a (request, KV head): its queries' units, four at a time
+// ---- bf16 forward -----------------------------------------------------------
+//
+// The K and V tiles (32 rows) reach LDS by direct global->LDS copies into rings
+// of R = 4 slots, chunk c of row t at c ^ swz(t) (V: vswz), so that the rows
+// which one operand read touches fall in distinct banks.  A wave owns a unit of
+// 32 queries; two workgroups share a CU, so that one's products run beside the
+// other's weights.  (Two units per wave, which halves the LDS reads, leave one
+// wave per SIMD and were slower: 8 x 8192 tokens, window 4096, 1935 us, now 1625.)
+// Step n forms the scores of tile n + 1 while it takes the weights of tile n,
+// then P V of tile n while it takes the maximum of tile n + 1: two independent
+// chains, whose MFMAs and VALU instructions interleave.
+template <int D>
+struct WinRing {
+  static constexpr int EPC = 8, CPR = D / EPC;
+  static constexpr int RPI = kWave / CPR;  // rows per copy instruction
+  static constexpr int RP256 = 256 / (D * 2);
+  static constexpr int IK = kTile / RPI;   // copies per tile
+  static constexpr int R = 4;
+  __device__ static constexpr int swz(int t) { return (t / RP256) % CPR; }
+  __device__ static constexpr int vswz(int t) { return 4 * ((t / RP256) % (CPR / 4)); }
+};
+
+// Where a (request, KV head)'s workgroups run: all on one XCD where their number
+// allows it (workgroups go to the 8 XCDs in turn), one (request, KV head) after
+// the other, so that what they read stays in that XCD's L2.
+__device__ inline void win_place(int bid, int nbg, int wgs, int& bg, int& x) {
+  if (nbg % kNumXcd == 0) {
+    const int s = bid / kNumXcd;
+    bg = bid % kNumXcd + kNumXcd * (s / wgs);
+    x = s % wgs;
+  } else {
+    bg = bid % nbg;
+    x = bid / nbg;
+  }
+}
+
+// The reference of a query's weights moves only when a tile's maximum passes it
+// by 2^8: until then weights are up to 2^8, which neither type minds, and the
+// accumulators need no rescale.
+constexpr float kRefSlack = 8.0f;
+
+template <int D>
+__global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_ring_kernel(WindowArgs a, int wgs) {
+  typedef Mma<bf16> M;
+  typedef M::op_t op_t;
+  typedef WinRing<D> RG;
+  constexpr int E = M::E, KW = M::KW, KD = D / KW, KL = kTile / KW, NCT = D / kTile, R = RG::R;
+  constexpr int IPW = 2 * RG::IK / kWinWaves;  // copies per wave and step: waves 0, 1 K's, waves 2, 3 V's
+  __shared__ alignas(16) bf16 kr[R][kTile * D], vr[R][kTile * D];
+
+  const int lane = threadIdx.x & (kWave - 1), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int li = lane & 31, hh = lane >> 5;
+  const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv;
+  int bg, x;
+  win_place(blockIdx.x, a.s.B * Hkv, wgs, bg, x);
+  x = wgs - 1 - x;  // the longest first
+  const int b = bg / Hkv, g = bg % Hkv;
+  const int len = win_len(a, b);
+  const WinUnit me = win_unit(a, len, b, g, x * kWinWaves + w);
+  const int first = x * kWinWaves / G * kTile, last = min(((x + 1) * kWinWaves - 1) / G * kTile + kTile, len);
+  if (first >= len) return;  // uniform
+  const WinTiles tl(a, len, first, last, kTile);
+  const int ntiles = tl.n;
+  const size_t qs = (size_t)Hq * D, ks_ = (size_t)Hkv * D;
+  const bf16* K = (const bf16*)a.k + ((size_t)b * a.T * Hkv + g) * D;
+  const bf16* V = (const bf16*)a.v + ((size_t)b * a.T * Hkv + g) * D;
+
+  op_t qop[KD];
+  {
+    const bf16* row = (const bf16*)a.q + ((size_t)b * a.T * Hq + me.h) * D + min(me.i0 + li, len - 1) * qs + hh * E;
+#pragma unroll
+    for (int ks = 0; ks < KD; ++ks) qop[ks] = load_op<bf16>(row + ks * KW);
+  }
+  float m = kNoRef, l = 0.0f;
+  f32x16 acc[NCT];
+#pragma unroll
+  for (int ct = 0; ct < NCT; ++ct) acc[ct] = f32x16{};
+  const WinRow row(a, len, min(me.i0 + li, len - 1));
+  const WinRow r0(a, len, min(me.i0, len - 1)), r1(a, len, min(me.i0 + kTile, len) - 1);
+
+  // Copies: lane's row and chunk of its wave's copies u; rows past the length
+  // read the last row (masked below).
+  int trow[IPW], tcol[IPW];
+#pragma unroll
+  for (int u = 0; u < IPW; ++u) {
+    const int i = (w * IPW + u) % RG::IK;
+    trow[u] = i * RG::RPI + lane / RG::CPR;
+    const int pos = lane % RG::CPR;
+    tcol[u] = (pos ^ (w < kWinWaves / 2 ? RG::swz(trow[u]) : RG::vswz(trow[u]))) * RG::EPC;
+  }
+  auto issue = [&](int n, bf16* dst) __attribute__((always_inline)) {
+    if (n >= ntiles) return;
+    const int j0 = tl.first(n, kTile), left = len - 1 - j0;
+    const bf16* base = (w < kWinWaves / 2 ? K : V) + (size_t)j0 * ks_;
+    const __amdgpu_buffer_rsrc_t rs =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(base), 0, (int)(kTile * ks_ * sizeof(bf16)), kBufferWord3);
+#pragma unroll
+    for (int u = 0; u < IPW; ++u)
+      buf_to_lds16(rs, dst + (w * IPW + u) % RG::IK * RG::RPI * D,
+                   (int)((min(trow[u], left) * (int)ks_ + tcol[u]) * sizeof(bf16)), 0);
+  };
+  // K of tile nk or V of tile nv, whichever this wave copies.
+  auto issue_step = [&](int nk, bf16* dk, int nv, bf16* dv) __attribute__((always_inline)) {
+    if (w < kWinWaves / 2)
+      issue(nk, dk);
+    else if (nv >= 0)
+      issue(nv, dv);
+  };
+
+  const float scale = kLog2e / sqrtf((float)D);
+  f32x16 sc;
+  // Takes the scores of tile n: masks, maximum, reference.
+  auto take = [&](int n, const f32x16& s) __attribute__((always_inline)) {
+    sc = s;
+    const int j0 = tl.first(n, kTile);
+    if (!win_full(r0, r1, a.n_sinks, j0, kTile)) {  // uniform
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sc[e] = row.sees(j0 + row_of(e, hh), a.n_sinks) ? sc[e] : -INFINITY;
+    }
+    float mt = sc[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) mt = fmaxf(mt, sc[e]);
+    mt = fmaxf(mt, xor32(mt)) * scale;
+    if (__any(mt > m + kRefSlack)) {
+      const float mn = mt > m + kRefSlack ? mt : m;
+      const float corr = __builtin_amdgcn_exp2f(m - mn);
+      l *= corr;
+#pragma unroll
+      for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[ct][e] *= corr;
+      m = mn;
+    }
+  };
+  auto scores = [&](const bf16* kt) __attribute__((always_inline)) {
+    op_t kop[KD];
+#pragma unroll
+    for (int ks = 0; ks < KD; ++ks)
+      kop[ks] = load_op<bf16>(&kt[li * D + ((2 * ks + hh) ^ RG::swz(li)) * RG::EPC]);
+    f32x16 s = {};
+#pragma unroll
+    for (int ks = 0; ks < KD; ++ks) s = M::mma(kop[ks], qop[ks], s);
+    return s;
+  };
+  // Weights and P V of tile n (V in vt), scores of tile n + 1 (K in kt).
+  auto compute = [&](auto lastc, int n, const bf16* kt, const bf16* vt) __attribute__((always_inline)) {
+    constexpr bool LAST = decltype(lastc)::value;
+    f32x16 sn;
+    if constexpr (!LAST) sn = scores(kt);
+    float p[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale, -m));
+    float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 16; e += 2) {
+      s0 += p[e];
+      s1 += p[e + 1];
+    }
+    l += s0 + s1;
+    op_t pop[KL];
+#pragma unroll
+    for (int ks = 0; ks < KL; ++ks) pop[ks] = cvt_op<bf16>(&p[ks * E]);
+    const int qi = lane & 15;
+#pragma unroll
+    for (int ct = 0; ct < NCT; ++ct) {
+      const int col = ct * kTile + 16 * ((lane >> 4) & 1) + 4 * (qi & 3);
+#pragma unroll
+      for (int ks = 0; ks < KL; ++ks) {
+        const int r = 16 * ks + 4 * hh + qi / 4;
+        const bf16* src = &vt[r * D + ((col / RG::EPC) ^ RG::vswz(qi / 4)) * RG::EPC + col % RG::EPC];
+        acc[ct] = M::mma(lds_tr_op(src, src + 8 * D), pop[ks], acc[ct]);
+      }
+    }
+    if constexpr (!LAST) take(n + 1, sn);
+  };
+  auto wait_step = [&](int later) __attribute__((always_inline)) {
+    if (later >= 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * IPW) : "memory");
+    else if (later == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * IPW) : "memory");
+    else if (later == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(IPW) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  };
+  const int ahead = w < kWinWaves / 2 ? 1 : 0;  // K runs a tile ahead
+  auto step = [&](int n, auto S) __attribute__((always_inline)) {
+    constexpr int SV = decltype(S)::value;
+    wait_step(min(2, ntiles - 1 - n - ahead));
+    lds_barrier_nodrain();  // K n+1 and V n visible; K n's and V n-1's slots free
+    issue_step(n + R, kr[SV], n + R - 1, vr[(SV + R - 1) % R]);
+    compute(std::false_type{}, n, kr[(SV + 1) % R], vr[SV]);
+  };
+  issue_step(0, kr[0], -1, nullptr);
+  issue_step(1, kr[1], 0, vr[0]);
+  issue_step(2, kr[2], 1, vr[1]);
+  issue_step(3, kr[3], 2, vr[2]);
+  wait_step(ahead ? min(3, ntiles - 1) : 3);
+  lds_barrier_nodrain();
+  take(0, scores(kr[0]));
+  int n = 0;
+  for (; n + R < ntiles; n += R) {
+    step(n, std::integral_constant<int, 0>{});
+    step(n + 1, std::integral_constant<int, 1>{});
+    step(n + 2, std::integral_constant<int, 2>{});
+    step(n + 3, std::integral_constant<int, 3>{});
+  }
+  if (n + 1 < ntiles) step(n, std::integral_constant<int, 0>{});
+  if (n + 2 < ntiles) step(n + 1, std::integral_constant<int, 1>{});
+  if (n + 3 < ntiles) step(n + 2, std::integral_constant<int, 2>{});
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  lds_barrier_nodrain();
+  compute(std::true_type{}, ntiles - 1, nullptr, vr[ntiles - 1 - n]);
+
+  l += xor32(l);
+  const int i = me.i0 + li;
+  if (i >= len) return;
+  win_store<bf16, D>(a.out, ((size_t)b * a.T + i) * Hq + me.h, acc, 1.0f / l, hh, a.s.out_f32);
+  if (a.lse && hh == 0) a.lse[((size_t)b * Hq + me.h) * a.T + i] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
+// Workgroups of a (request, KV head): its queries' units, one per wave.
+static int win_wgs(const WindowArgs& a) {
   const long units = ((long)a.T + kTile - 1) / kTile * (a.s.Hq / a.s.Hkv);
   return (int)((units + kWinWaves - 1) / kWinWaves);
+}
+
+template <int D>
+static hipError_t win_ring_go(const WindowArgs& a, hipStream_t st) {
+  const int wgs = win_wgs(a);
+  hipLaunchKernelGGL(hyb_win_ring_kernel<D>, dim3((unsigned)(a.s.B * a.s.Hkv * wgs)), dim3(kWave * kWinWaves), 0,
+                     st, a, wgs);
+  return hipGetLastError();
 }
 
 template <typename T, int D>
@@ -404,7 +630,7 @@ static hipError_t win_backward_go(const WindowArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_window_prefill(const WindowArgs& a, hipStream_t st) {
-  if (a.s.dtype == 1) return a.s.D == 64 ? win_prefill_go<bf16, 64>(a, st) : win_prefill_go<bf16, 128>(a, st);
+  if (a.s.dtype == 1) return a.s.D == 64 ? win_ring_go<64>(a, st) : win_ring_go<128>(a, st);
   return a.s.D == 64 ? win_prefill_go<float, 64>(a, st) : win_prefill_go<float, 128>(a, st);
 }
 
