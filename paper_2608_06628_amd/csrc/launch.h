@@ -120,7 +120,8 @@ struct WindowArgs {
   // gradient
   const void* dout = nullptr;
   void *dq = nullptr, *dk = nullptr, *dv = nullptr;
-  float* delta = nullptr;  // workspace [B][Hq][T]
+  float* ws = nullptr;    // fp32: delta [B][Hq][T]; bf16: the rows' statistics, then
+  float* sums = nullptr;  // the partial sums of dk, dv (set by the launcher)
 };
 
 // Pages and slots of new tokens (pages.hip).

@@ -246,7 +246,7 @@ __global__ __launch_bounds__(256) void hyb_win_delta_kernel(WindowArgs a) {
     }
 #pragma unroll
     for (int o = 1; o < LPR; o <<= 1) s += __shfl_xor(s, o);
-    if (threadIdx.x % LPR == 0) a.delta[((size_t)b * a.s.Hq + h) * a.T + i] = s;
+    if (threadIdx.x % LPR == 0) a.ws[((size_t)b * a.s.Hq + h) * a.T + i] = s;
   }
 }
 
@@ -278,7 +278,7 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dq_kernel(WindowArgs
     win_row_ops<T, D>(dop, (const T*)a.dout + at, true, hh);
     const float scale = kLog2e / sqrtf((float)D);
     const size_t st = ((size_t)b * Hq + me.h) * a.T + i;
-    const float lse = a.lse[st] * kLog2e, delta = a.delta[st];
+    const float lse = a.lse[st] * kLog2e, delta = a.ws[st];
     for (int n = 0; n < tl.n; ++n) {
       const int j0 = tl.first(n, kTile);
       __syncthreads();
@@ -350,7 +350,7 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dkv_kernel(WindowArg
         if (threadIdx.x < kTile) {
           const int i = min(i0 + (int)threadIdx.x, len - 1);
           lse[threadIdx.x] = a.lse[st + i] * kLog2e;
-          delta[threadIdx.x] = a.delta[st + i];
+          delta[threadIdx.x] = a.ws[st + i];
         }
         __syncthreads();
         const WinRow r0(a, len, i0), r1(a, len, min(i0 + kTile, len) - 1);
@@ -594,6 +594,414 @@ __global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_ring_kernel(Windo
   if (a.lse && hh == 0) a.lse[((size_t)b * Hq + me.h) * a.T + i] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
+// ---- bf16 gradient ----------------------------------------------------------
+//
+// Three kernels: delta and the rows' statistics, dQ (a wave owns 32 queries and
+// loops over key tiles), dK with dV (a wave owns 32 keys and loops over the
+// query tiles of its KV head's heads).  Tiles come through rings as in the forward;
+// here a tile is read both by rows and, by transposing reads, by columns.
+template <int D>
+struct WinTile {
+  static constexpr int EPC = 8, CPR = D / EPC;
+  static constexpr int RPI = kWave / CPR, IK = kTile / RPI;
+  static constexpr int kBytes = kTile * D * 2;
+  // Chunk c of row t sits at c ^ swz(t): the 16 rows that fill the banks have
+  // 16 places for one chunk (row reads), and four rows from a multiple of four on
+  // fall in different groups of four chunks (transposing reads).
+  __device__ static constexpr int swz(int t) {
+    return D == 128 ? ((t & 3) << 2) | ((t >> 2) & 3) : ((t & 2) << 1) | ((t >> 2) & 3);
+  }
+  int row, col;  // byte offsets of this lane's row and column operands
+  __device__ inline explicit WinTile(int lane) {
+    const int li = lane & 31, hh = lane >> 5, qi = lane & 15, b = (lane >> 4) & 1;
+    row = li * 2 * D + 16 * (hh ^ swz(li));
+    const int r = 4 * hh + qi / 4;
+    col = r * 2 * D + 16 * ((2 * b + (qi & 3) / 2) ^ swz(r)) + 8 * (qi & 1);
+  }
+  // entries 16 ks + 8 hh .. + 7 of row li
+  __device__ inline bf16x8 row_op(const bf16* t, int ks) const {
+    return *reinterpret_cast<const bf16x8*>(reinterpret_cast<const char*>(t) + (row ^ (32 * ks)));
+  }
+  // column 32 ct + li at the rows row_of(8 ks + e, hh)
+  __device__ inline bf16x8 col_op(const bf16* t, int ct, int ks) const {
+    const char* p = reinterpret_cast<const char*>(t) + 16 * ks * 2 * D;
+    return lds_tr_op(p + (col ^ (64 * ct)), p + (col ^ (64 * ct) ^ 32) + 8 * 2 * D);
+  }
+};
+
+// The keys' side of WinRow: key j is seen by the queries q0 .. q1 - 1.
+struct WinKey {
+  int q0, q1;
+  __device__ inline WinKey(const WindowArgs& a, int len, int j) {
+    const int L = a.s.L;
+    q0 = j / L * L;
+    const long end = ((long)j + a.window) / L * L + L;
+    q1 = j < a.n_sinks ? len : (int)min(end, (long)len);
+  }
+};
+
+// Statistics of a row for the dK, dV kernel, as operands of one more step of its
+// products: lse sqrt(d) and delta, each as three bf16 pieces (24 bits), which
+// that kernel multiplies by -1.  [B][Hq][Tp][16], Tp = T rounded up to a tile.
+__host__ __device__ constexpr int win_tp(int T) { return (T + kTile - 1) / kTile * kTile; }
+__device__ inline bf16x8 win_pieces(float x) {
+  bf16x8 o = {};
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    o[i] = (bf16)x;
+    x -= (float)o[i];
+  }
+  return o;
+}
+__device__ inline float win_value(bf16x8 p) { return ((float)p[2] + (float)p[1]) + (float)p[0]; }
+
+template <int D>
+__global__ __launch_bounds__(256) void hyb_win_stats_kernel(WindowArgs a) {
+  constexpr int LPR = D / 8;
+  const int Hq = a.s.Hq, Tp = win_tp(a.T);
+  const long rows = (long)a.s.B * Tp * Hq;
+  for (long r = (long)blockIdx.x * (256 / LPR) + threadIdx.x / LPR; r < rows; r += (long)gridDim.x * (256 / LPR)) {
+    const int h = (int)(r % Hq);
+    const long bi = r / Hq;
+    const int b = (int)(bi / Tp), i = (int)(bi % Tp);
+    float s = 0.0f, e = 0.0f;
+    if (i < win_len(a, b)) {
+      const size_t at = (((size_t)b * a.T + i) * Hq + h) * D + threadIdx.x % LPR * 8;
+      const bf16x8 x = load_op<bf16>((const bf16*)a.out + at), y = load_op<bf16>((const bf16*)a.dout + at);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s += (float)x[k] * (float)y[k];
+      e = a.lse[((size_t)b * Hq + h) * a.T + i] * sqrtf((float)D);
+    }
+#pragma unroll
+    for (int o = 1; o < LPR; o <<= 1) s += __shfl_xor(s, o);
+    if (threadIdx.x % LPR < 2)
+      reinterpret_cast<bf16x8*>(a.ws)[(((size_t)b * Hq + h) * Tp + i) * 2 + threadIdx.x % LPR] =
+          win_pieces(threadIdx.x % LPR == 0 ? e : s);
+  }
+}
+
+template <int D>
+__global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_dq_ring_kernel(WindowArgs a, int wgs) {
+  typedef Mma<bf16> M;
+  typedef M::op_t op_t;
+  typedef WinTile<D> WT;
+  constexpr int E = M::E, KW = M::KW, KD = D / KW, KL = kTile / KW, NCT = D / kTile, R = 4;
+  constexpr int IPW = 2 * WT::IK / kWinWaves;  // copies per wave and step: waves 0, 1 K's, waves 2, 3 V's
+  __shared__ alignas(16) bf16 kr[R][kTile * D], vr[R][kTile * D];
+
+  const int lane = threadIdx.x & (kWave - 1), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int li = lane & 31, hh = lane >> 5;
+  const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv;
+  int bg, x;
+  win_place(blockIdx.x, a.s.B * Hkv, wgs, bg, x);
+  x = wgs - 1 - x;  // the longest first
+  const int b = bg / Hkv, g = bg % Hkv;
+  const int len = win_len(a, b);
+  const WinUnit me = win_unit(a, len, b, g, x * kWinWaves + w);
+  const int first = x * kWinWaves / G * kTile, last = min(((x + 1) * kWinWaves - 1) / G * kTile + kTile, len);
+  f32x16 acc[NCT];
+#pragma unroll
+  for (int ct = 0; ct < NCT; ++ct) acc[ct] = f32x16{};
+  const int row = me.i0 + li;
+  if (first < len) {  // uniform
+    const WinTiles tl(a, len, first, last, kTile);
+    const int ntiles = tl.n;
+    const size_t qs = (size_t)Hq * D, ks_ = (size_t)Hkv * D;
+    const bf16* K = (const bf16*)a.k + ((size_t)b * a.T * Hkv + g) * D;
+    const bf16* V = (const bf16*)a.v + ((size_t)b * a.T * Hkv + g) * D;
+    const int i = min(row, len - 1);
+    const WinRow mine(a, len, i), r0(a, len, min(me.i0, len - 1)), r1(a, len, min(me.i0 + kTile, len) - 1);
+    const WT wt(lane);
+    op_t qop[KD], dop[KD];
+    {
+      const size_t at = ((size_t)b * a.T * Hq + me.h) * D + i * qs + hh * E;
+#pragma unroll
+      for (int ks = 0; ks < KD; ++ks) {
+        qop[ks] = load_op<bf16>((const bf16*)a.q + at + ks * KW);
+        dop[ks] = load_op<bf16>((const bf16*)a.dout + at + ks * KW);
+      }
+    }
+    const float scale = kLog2e / sqrtf((float)D);
+    const float lse = a.lse[((size_t)b * Hq + me.h) * a.T + i] * kLog2e;
+    const float delta =
+        win_value(reinterpret_cast<const bf16x8*>(a.ws)[(((size_t)b * Hq + me.h) * win_tp(a.T) + i) * 2 + 1]);
+
+    int trow[IPW], tcol[IPW];
+#pragma unroll
+    for (int u = 0; u < IPW; ++u) {
+      trow[u] = (w * IPW + u) % WT::IK * WT::RPI + lane / WT::CPR;
+      tcol[u] = (lane % WT::CPR ^ WT::swz(trow[u])) * WT::EPC;
+    }
+    auto issue = [&](int n, bf16* dk, bf16* dv) __attribute__((always_inline)) {
+      if (n >= ntiles) return;
+      const bool isk = w < kWinWaves / 2;
+      bf16* dst = isk ? dk : dv;
+      const int j0 = tl.first(n, kTile), left = len - 1 - j0;
+      const bf16* base = (isk ? K : V) + (size_t)j0 * ks_;
+      const __amdgpu_buffer_rsrc_t rs =
+          __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(base), 0, (int)(kTile * ks_ * sizeof(bf16)), kBufferWord3);
+#pragma unroll
+      for (int u = 0; u < IPW; ++u)
+        buf_to_lds16(rs, dst + (w * IPW + u) % WT::IK * WT::RPI * D,
+                     (int)((min(trow[u], left) * (int)ks_ + tcol[u]) * sizeof(bf16)), 0);
+    };
+    f32x16 sc, dp;
+    // Scores and dP of tile n, masked.
+    auto products = [&](const bf16* kt, const bf16* vt, f32x16& s, f32x16& d) __attribute__((always_inline)) {
+      s = f32x16{};
+      d = f32x16{};
+#pragma unroll
+      for (int ks = 0; ks < KD; ++ks) s = M::mma(wt.row_op(kt, ks), qop[ks], s);
+#pragma unroll
+      for (int ks = 0; ks < KD; ++ks) d = M::mma(wt.row_op(vt, ks), dop[ks], d);
+    };
+    auto take = [&](int n, const f32x16& s, const f32x16& d) __attribute__((always_inline)) {
+      sc = s;
+      dp = d;
+      const int j0 = tl.first(n, kTile);
+      if (!win_full(r0, r1, a.n_sinks, j0, kTile)) {  // uniform
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[e] = mine.sees(j0 + row_of(e, hh), a.n_sinks) ? sc[e] : -INFINITY;
+      }
+    };
+    auto compute = [&](auto lastc, int n, const bf16* kn, const bf16* vn, const bf16* kt) __attribute__((always_inline)) {
+      constexpr bool LAST = decltype(lastc)::value;
+      f32x16 sn, dn;
+      if constexpr (!LAST) products(kn, vn, sn, dn);
+      float ds[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        ds[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale, -lse)) * (dp[e] - delta);
+      op_t sop[KL];
+#pragma unroll
+      for (int ks = 0; ks < KL; ++ks) sop[ks] = cvt_op<bf16>(&ds[ks * E]);
+#pragma unroll
+      for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+        for (int ks = 0; ks < KL; ++ks) acc[ct] = M::mma(wt.col_op(kt, ct, ks), sop[ks], acc[ct]);
+      if constexpr (!LAST) take(n + 1, sn, dn);
+    };
+    // Tile n + 1 is read at step n, by rows, and tile n by columns; tile n + 3
+    // goes to the slot of tile n - 1.
+    auto step = [&](int n, auto S) __attribute__((always_inline)) {
+      constexpr int SV = decltype(S)::value;
+      if (n + 2 < ntiles) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(IPW) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      lds_barrier_nodrain();
+      issue(n + 3, kr[(SV + 3) % R], vr[(SV + 3) % R]);
+      compute(std::false_type{}, n, kr[(SV + 1) % R], vr[(SV + 1) % R], kr[SV]);
+    };
+    issue(0, kr[0], vr[0]);
+    issue(1, kr[1], vr[1]);
+    issue(2, kr[2], vr[2]);
+    if (ntiles > 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * IPW) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    lds_barrier_nodrain();
+    {
+      f32x16 s, d;
+      products(kr[0], vr[0], s, d);
+      take(0, s, d);
+    }
+    int n = 0;
+    for (; n + R < ntiles; n += R) {
+      step(n, std::integral_constant<int, 0>{});
+      step(n + 1, std::integral_constant<int, 1>{});
+      step(n + 2, std::integral_constant<int, 2>{});
+      step(n + 3, std::integral_constant<int, 3>{});
+    }
+    if (n + 1 < ntiles) step(n, std::integral_constant<int, 0>{});
+    if (n + 2 < ntiles) step(n + 1, std::integral_constant<int, 1>{});
+    if (n + 3 < ntiles) step(n + 2, std::integral_constant<int, 2>{});
+    compute(std::true_type{}, ntiles - 1, nullptr, nullptr, kr[ntiles - 1 - n]);
+  }
+  if (row >= a.T) return;  // rows past the length: zero
+  win_store<bf16, D>(a.dq, ((size_t)b * a.T + row) * Hq + me.h, acc, row < len ? 1.0f / sqrtf((float)D) : 0.0f, hh,
+                     a.s.out_f32);
+}
+
+template <int D>
+__global__ __launch_bounds__(kWave* kWinWaves, 1) void hyb_win_dkv_ring_kernel(WindowArgs a, int wgs, int parts) {
+  typedef Mma<bf16> M;
+  typedef M::op_t op_t;
+  typedef WinTile<D> WT;
+  constexpr int E = M::E, KW = M::KW, KD = D / KW, KL = kTile / KW, NCT = D / kTile, R = 4;
+  constexpr int IPQ = 2 * WT::IK / kWinWaves;  // copies per wave and step: waves 0, 1 Q's, waves 2, 3 dO's
+  constexpr int IPW = IPQ + 1;                 // and a quarter of the statistics each
+  struct alignas(16) Slot {
+    bf16 q[kTile * D], d[kTile * D], st[kTile * 16];
+  };
+  __shared__ Slot ring[R];
+
+  const int lane = threadIdx.x & (kWave - 1), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int li = lane & 31, hh = lane >> 5;
+  const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv, Tp = win_tp(a.T);
+  int bg, x;
+  win_place(blockIdx.x, a.s.B * Hkv, wgs * parts, bg, x);
+  const int part = x % parts;
+  x /= parts;  // the longest (first keys) first
+  const int b = bg / Hkv, g = bg % Hkv;
+  const int h0 = g * G + part * G / parts, h1 = g * G + (part + 1) * G / parts;  // this part's heads
+  const int len = win_len(a, b);
+  const int w0 = x * kWinWaves * kTile, j0 = w0 + w * kTile, j = j0 + li;
+  f32x16 dk[NCT], dv[NCT];
+#pragma unroll
+  for (int ct = 0; ct < NCT; ++ct) dk[ct] = dv[ct] = f32x16{};
+  if (w0 < len) {  // uniform
+    const size_t qs = (size_t)Hq * D, ks_ = (size_t)Hkv * D;
+    // query tiles t0 .. t0 + nq - 1 of every head
+    const WinQueries all(a, len, w0, min(w0 + kWinWaves * kTile, len));
+    const int t0 = all.q0 / kTile, nq = (all.q1 + kTile - 1) / kTile - t0, nsteps = nq * (h1 - h0);
+    const WinKey mine(a, len, min(j, len - 1));
+    // query tiles that every key of the wave is seen by: f0 <= i0 and i0 + 32 <= f1
+    const int jl = min(j0 + kTile, len) - 1;
+    const int f0 = WinKey(a, len, max(jl, 0)).q0, f1 = WinKey(a, len, min(max(j0, min(a.n_sinks, jl)), max(jl, 0))).q1;
+    const WT wt(lane);
+    op_t kop[KD], vop[KD];
+    {
+      const size_t at = ((size_t)b * a.T * Hkv + g) * D + min(j, len - 1) * ks_ + hh * E;
+#pragma unroll
+      for (int ks = 0; ks < KD; ++ks) {
+        kop[ks] = load_op<bf16>((const bf16*)a.k + at + ks * KW);
+        vop[ks] = load_op<bf16>((const bf16*)a.v + at + ks * KW);
+      }
+    }
+    op_t ms = {}, md = {};  // -1 for the three pieces of lse (hh = 0), of delta (hh = 1)
+#pragma unroll
+    for (int e = 0; e < 3; ++e) {
+      ms[e] = (bf16)(hh == 0 ? -1.0f : 0.0f);
+      md[e] = (bf16)(hh == 1 ? -1.0f : 0.0f);
+    }
+    const float scale = kLog2e / sqrtf((float)D);
+
+    int trow[IPQ], tcol[IPQ];
+#pragma unroll
+    for (int u = 0; u < IPQ; ++u) {
+      trow[u] = (w * IPQ + u) % WT::IK * WT::RPI + lane / WT::CPR;
+      tcol[u] = (lane % WT::CPR ^ WT::swz(trow[u])) * WT::EPC;
+    }
+    int inh = h0, inq = 0;  // head and query tile of the next copies
+    auto issue = [&](int n, Slot& s) __attribute__((always_inline)) {
+      if (n >= nsteps) return;
+      const int i0 = (t0 + inq) * kTile, left = len - 1 - i0;
+      const bool isq = w < kWinWaves / 2;
+      const bf16* base = (const bf16*)(isq ? a.q : a.dout) + ((size_t)b * a.T * Hq + inh) * D + (size_t)i0 * qs;
+      const __amdgpu_buffer_rsrc_t rs =
+          __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(base), 0, (int)(kTile * qs * sizeof(bf16)), kBufferWord3);
+      bf16* dst = isq ? s.q : s.d;
+#pragma unroll
+      for (int u = 0; u < IPQ; ++u)
+        buf_to_lds16(rs, dst + (w * IPQ + u) % WT::IK * WT::RPI * D,
+                     (int)((min(trow[u], left) * (int)qs + tcol[u]) * sizeof(bf16)), 0);
+      const float* st = (const float*)a.ws + (((size_t)b * Hq + inh) * Tp + i0) * 8 + w * kWave + lane;
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)st,
+                                       (__attribute__((address_space(3))) void*)((float*)s.st + w * kWave), 4, 0, 0);
+      if (++inq == nq) inq = 0, ++inh;
+    };
+    f32x16 sc, dp;
+    int cq = 0;  // query tile of the next scores
+    auto products = [&](const Slot& s, f32x16& p, f32x16& d) __attribute__((always_inline)) {
+      const op_t st = *reinterpret_cast<const op_t*>(&s.st[li * 16 + hh * 8]);
+      p = M::mma(st, ms, f32x16{});
+      d = M::mma(st, md, f32x16{});
+#pragma unroll
+      for (int ks = 0; ks < KD; ++ks) p = M::mma(wt.row_op(s.q, ks), kop[ks], p);
+#pragma unroll
+      for (int ks = 0; ks < KD; ++ks) d = M::mma(wt.row_op(s.d, ks), vop[ks], d);
+    };
+    auto take = [&](const f32x16& p, const f32x16& d) __attribute__((always_inline)) {
+      sc = p;
+      dp = d;
+      const int i0 = (t0 + cq) * kTile;
+      if (!(i0 >= f0 && i0 + kTile <= f1)) {  // uniform
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int i = i0 + row_of(e, hh);
+          sc[e] = i >= mine.q0 && i < mine.q1 ? sc[e] : -INFINITY;
+        }
+      }
+      if (++cq == nq) cq = 0;
+    };
+    auto compute = [&](auto lastc, const Slot& next, const Slot& s) __attribute__((always_inline)) {
+      constexpr bool LAST = decltype(lastc)::value;
+      f32x16 pn, dn;
+      if constexpr (!LAST) products(next, pn, dn);
+      float p[16], ds[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        p[e] = __builtin_amdgcn_exp2f(sc[e] * scale);
+        ds[e] = p[e] * dp[e];
+      }
+      op_t pop[KL], sop[KL];
+#pragma unroll
+      for (int ks = 0; ks < KL; ++ks) {
+        pop[ks] = cvt_op<bf16>(&p[ks * E]);
+        sop[ks] = cvt_op<bf16>(&ds[ks * E]);
+      }
+#pragma unroll
+      for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+        for (int ks = 0; ks < KL; ++ks) {
+          dv[ct] = M::mma(wt.col_op(s.d, ct, ks), pop[ks], dv[ct]);
+          dk[ct] = M::mma(wt.col_op(s.q, ct, ks), sop[ks], dk[ct]);
+        }
+      if constexpr (!LAST) take(pn, dn);
+    };
+    auto step = [&](int n, auto S) __attribute__((always_inline)) {
+      constexpr int SV = decltype(S)::value;
+      if (n + 2 < nsteps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(IPW) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      lds_barrier_nodrain();
+      issue(n + 3, ring[(SV + 3) % R]);
+      compute(std::false_type{}, ring[(SV + 1) % R], ring[SV]);
+    };
+    issue(0, ring[0]);
+    issue(1, ring[1]);
+    issue(2, ring[2]);
+    if (nsteps > 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * IPW) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    lds_barrier_nodrain();
+    {
+      f32x16 p, d;
+      products(ring[0], p, d);
+      take(p, d);
+    }
+    int n = 0;
+    for (; n + R < nsteps; n += R) {
+      step(n, std::integral_constant<int, 0>{});
+      step(n + 1, std::integral_constant<int, 1>{});
+      step(n + 2, std::integral_constant<int, 2>{});
+      step(n + 3, std::integral_constant<int, 3>{});
+    }
+    if (n + 1 < nsteps) step(n, std::integral_constant<int, 0>{});
+    if (n + 2 < nsteps) step(n + 1, std::integral_constant<int, 1>{});
+    if (n + 3 < nsteps) step(n + 2, std::integral_constant<int, 2>{});
+    compute(std::true_type{}, ring[0], ring[nsteps - 1 - n]);
+  }
+  if (j >= a.T) return;
+  const size_t row = ((size_t)b * a.T + j) * Hkv + g;
+  const float fk = j < len ? 1.0f / sqrtf((float)D) : 0.0f, fv = j < len ? 1.0f : 0.0f;
+  if (parts == 1) {
+    win_store<bf16, D>(a.dk, row, dk, fk, hh, a.s.out_f32);
+    win_store<bf16, D>(a.dv, row, dv, fv, hh, a.s.out_f32);
+  } else {
+    const size_t rows = (size_t)a.s.B * a.T * Hkv;
+    win_store<bf16, D>(a.sums, part * 2 * rows + row, dk, fk, hh, true);
+    win_store<bf16, D>(a.sums, (part * 2 + 1) * rows + row, dv, fv, hh, true);
+  }
+}
+
+// dK and dV from the parts' sums, in order; four entries per thread.
+template <int D>
+__global__ __launch_bounds__(256) void hyb_win_sum_kernel(WindowArgs a, int parts) {
+  const size_t n = (size_t)a.s.B * a.T * a.s.Hkv * D / 4;
+  for (size_t x = (size_t)blockIdx.x * 256 + threadIdx.x; x < 2 * n; x += (size_t)gridDim.x * 256) {
+    f32x4 s = {};
+    for (int p = 0; p < parts; ++p) s += reinterpret_cast<const f32x4*>(a.sums)[p * 2 * n + x];
+    const float o[4] = {s[0], s[1], s[2], s[3]};
+    store_out4<bf16>(x < n ? a.dk : a.dv, 4 * (x < n ? x : x - n), o, a.s.out_f32);
+  }
+}
+
 // Workgroups of a (request, KV head): its queries' units, one per wave.
 static int win_wgs(const WindowArgs& a) {
   const long units = ((long)a.T + kTile - 1) / kTile * (a.s.Hq / a.s.Hkv);
@@ -629,13 +1037,44 @@ static hipError_t win_backward_go(const WindowArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+// Parts that a KV head's query heads are cut into where its keys alone make few
+// workgroups: each sums its heads' dK and dV in the workspace.
+static int win_parts(const Shape& s, int T) {
+  const long wgs = (long)s.B * s.Hkv * ((T + kWinWaves * kTile - 1) / (kWinWaves * kTile));
+  const int G = s.Hq / s.Hkv;
+  int p = 1;
+  while (p < G && wgs * p < 512) ++p;
+  return p;
+}
+static size_t win_stats_bytes(const Shape& s, int T) { return (size_t)s.B * s.Hq * win_tp(T) * 32; }
+
+template <int D>
+static hipError_t win_backward_ring_go(WindowArgs a, hipStream_t st) {
+  const int parts = win_parts(a.s, a.T);
+  a.sums = (float*)((char*)a.ws + win_stats_bytes(a.s, a.T));
+  const long rows = (long)a.s.B * win_tp(a.T) * a.s.Hq;
+  hipLaunchKernelGGL(hyb_win_stats_kernel<D>, dim3((unsigned)std::min<long>((rows * D / 8 + 255) / 256, 4096)),
+                     dim3(256), 0, st, a);
+  const int wgs = win_wgs(a), kwgs = (a.T + kWinWaves * kTile - 1) / (kWinWaves * kTile);
+  hipLaunchKernelGGL(hyb_win_dq_ring_kernel<D>, dim3((unsigned)(a.s.B * a.s.Hkv * wgs)), dim3(kWave * kWinWaves), 0, st,
+                     a, wgs);
+  hipLaunchKernelGGL(hyb_win_dkv_ring_kernel<D>, dim3((unsigned)(a.s.B * a.s.Hkv * kwgs * parts)),
+                     dim3(kWave * kWinWaves), 0, st, a, kwgs, parts);
+  if (parts > 1) {
+    const long n = (long)a.s.B * a.T * a.s.Hkv * D / 2;
+    hipLaunchKernelGGL(hyb_win_sum_kernel<D>, dim3((unsigned)std::min<long>((n + 255) / 256, 4096)), dim3(256), 0, st, a,
+                       parts);
+  }
+  return hipGetLastError();
+}
+
 hipError_t launch_window_prefill(const WindowArgs& a, hipStream_t st) {
   if (a.s.dtype == 1) return a.s.D == 64 ? win_ring_go<64>(a, st) : win_ring_go<128>(a, st);
   return a.s.D == 64 ? win_prefill_go<float, 64>(a, st) : win_prefill_go<float, 128>(a, st);
 }
 
 hipError_t launch_window_backward(const WindowArgs& a, hipStream_t st) {
-  if (a.s.dtype == 1) return a.s.D == 64 ? win_backward_go<bf16, 64>(a, st) : win_backward_go<bf16, 128>(a, st);
+  if (a.s.dtype == 1) return a.s.D == 64 ? win_backward_ring_go<64>(a, st) : win_backward_ring_go<128>(a, st);
   return a.s.D == 64 ? win_backward_go<float, 64>(a, st) : win_backward_go<float, 128>(a, st);
 }
 
@@ -645,6 +1084,10 @@ long window_workgroups(const Shape& s, int T) {
   return (long)s.B * s.Hkv * ((units + kWinWaves - 1) / kWinWaves);
 }
 
-size_t window_backward_ws_bytes(const Shape& s, int T) { return (size_t)s.B * s.Hq * T * sizeof(float); }
+size_t window_backward_ws_bytes(const Shape& s, int T) {
+  if (s.dtype != 1) return (size_t)s.B * s.Hq * T * sizeof(float);  // delta
+  const int parts = win_parts(s, T);
+  return win_stats_bytes(s, T) + (parts > 1 ? (size_t)parts * 2 * s.B * T * s.Hkv * s.D * sizeof(float) : 0);
+}
 
 }  // namespace hyb
