@@ -26,6 +26,9 @@
 #include "device.h"
 #include "launch.h"
 
+#ifndef WIN_ORDER
+#define WIN_ORDER 1
+#endif
 namespace hyb {
 
 // Reference of a query that has seen no key yet: finite, so that a tile in
@@ -403,7 +406,7 @@ struct WinRing {
 // allows it (workgroups go to the 8 XCDs in turn), one (request, KV head) after
 // the other, so that what they read stays in that XCD's L2.
 __device__ inline void win_place(int bid, int nbg, int wgs, int& bg, int& x) {
-  if (nbg % kNumXcd == 0) {
+  if (WIN_ORDER == 0 && nbg % kNumXcd == 0) {
     const int s = bid / kNumXcd;
     bg = bid % kNumXcd + kNumXcd * (s / wgs);
     x = s % wgs;
@@ -819,20 +822,41 @@ __global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_dq_ring_kernel(Wi
                      a.s.out_f32);
 }
 
+// A workgroup owns 128 keys and has two halves of four waves, a wave 32 keys of
+// its half: the halves take the query tiles in turn and their sums are joined
+// in LDS at the end.  (So that two waves share a SIMD with the LDS of one
+// workgroup: dK and dV take 128 registers, K 32, the scores and dP 32; V is read
+// from LDS.)
+constexpr int kWinKeyWaves = 8;
+
 template <int D>
-__global__ __launch_bounds__(kWave* kWinWaves, 1) void hyb_win_dkv_ring_kernel(WindowArgs a, int wgs, int parts) {
+__global__ __launch_bounds__(kWave* kWinKeyWaves, 2) void hyb_win_dkv_ring_kernel(WindowArgs a, int wgs,
+                                                                                           int parts) {
   typedef Mma<bf16> M;
   typedef M::op_t op_t;
   typedef WinTile<D> WT;
-  constexpr int E = M::E, KW = M::KW, KD = D / KW, KL = kTile / KW, NCT = D / kTile, R = 4;
-  constexpr int IPQ = 2 * WT::IK / kWinWaves;  // copies per wave and step: waves 0, 1 Q's, waves 2, 3 dO's
-  constexpr int IPW = IPQ + 1;                 // and a quarter of the statistics each
+  constexpr int E = M::E, KW = M::KW, KD = D / KW, KL = kTile / KW, NCT = D / kTile, R = 3;
+  constexpr int IPQ = 2 * WT::IK / 4;  // a half's copies per wave and step: two waves Q's, two dO's
+  constexpr int IPW = IPQ + 1;         // and a quarter of the statistics each
   struct alignas(16) Slot {
     bf16 q[kTile * D], d[kTile * D], st[kTile * 16];
   };
-  __shared__ Slot ring[R];
+  struct Loop {
+    Slot ring[2][R];
+    bf16 v[4][kTile * D];
+  };
+  struct Join {
+    f32x4 x[2][4][NCT * 4][kWave];
+  };
+  union Smem {
+    Loop loop;
+    Join join;
+    __device__ Smem() {}
+  };
+  __shared__ Smem sh;
 
-  const int lane = threadIdx.x & (kWave - 1), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int half = wave >> 2, w = wave & 3;
   const int li = lane & 31, hh = lane >> 5;
   const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv, Tp = win_tp(a.T);
   int bg, x;
@@ -842,28 +866,36 @@ __global__ __launch_bounds__(kWave* kWinWaves, 1) void hyb_win_dkv_ring_kernel(W
   const int b = bg / Hkv, g = bg % Hkv;
   const int h0 = g * G + part * G / parts, h1 = g * G + (part + 1) * G / parts;  // this part's heads
   const int len = win_len(a, b);
-  const int w0 = x * kWinWaves * kTile, j0 = w0 + w * kTile, j = j0 + li;
-  f32x16 dk[NCT], dv[NCT];
+  const int w0 = x * 4 * kTile, j0 = w0 + w * kTile, j = j0 + li;
+  f32x16 acc[2][NCT];  // dK, dV
 #pragma unroll
-  for (int ct = 0; ct < NCT; ++ct) dk[ct] = dv[ct] = f32x16{};
+  for (int ct = 0; ct < NCT; ++ct) acc[0][ct] = acc[1][ct] = f32x16{};
   if (w0 < len) {  // uniform
     const size_t qs = (size_t)Hq * D, ks_ = (size_t)Hkv * D;
-    // query tiles t0 .. t0 + nq - 1 of every head
-    const WinQueries all(a, len, w0, min(w0 + kWinWaves * kTile, len));
-    const int t0 = all.q0 / kTile, nq = (all.q1 + kTile - 1) / kTile - t0, nsteps = nq * (h1 - h0);
+    // query tiles t0 .. t0 + nq - 1 of every head; a half takes every second
+    const WinQueries all(a, len, w0, min(w0 + 4 * kTile, len));
+    const int t0 = all.q0 / kTile, nq = (all.q1 + kTile - 1) / kTile - t0, ntiles = nq * (h1 - h0);
+    const int nsteps = (ntiles + 1) / 2, mysteps = (ntiles + 1 - half) / 2;
     const WinKey mine(a, len, min(j, len - 1));
     // query tiles that every key of the wave is seen by: f0 <= i0 and i0 + 32 <= f1
-    const int jl = min(j0 + kTile, len) - 1;
-    const int f0 = WinKey(a, len, max(jl, 0)).q0, f1 = WinKey(a, len, min(max(j0, min(a.n_sinks, jl)), max(jl, 0))).q1;
+    const int jl = max(min(j0 + kTile, len) - 1, 0);
+    const int f0 = WinKey(a, len, jl).q0, f1 = WinKey(a, len, min(max(j0, a.n_sinks), jl)).q1;
     const WT wt(lane);
-    op_t kop[KD], vop[KD];
+    // this half's share of V: tiles 2 half and 2 half + 1 of the keys, a copy per wave and round
+#pragma unroll
+    for (int u = 0; u < 2 * WT::IK / 4; ++u) {
+      const int c = u * 4 + w, t = 2 * half + c / WT::IK, r = c % WT::IK * WT::RPI + lane / WT::CPR;
+      const bf16* src = (const bf16*)a.v + ((size_t)b * a.T * Hkv + g) * D + min(w0 + t * kTile + r, len - 1) * ks_ +
+                        (lane % WT::CPR ^ WT::swz(r)) * WT::EPC;
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                       (__attribute__((address_space(3))) void*)(sh.loop.v[t] + c % WT::IK * WT::RPI * D),
+                                       16, 0, 0);
+    }
+    op_t kop[KD];
     {
       const size_t at = ((size_t)b * a.T * Hkv + g) * D + min(j, len - 1) * ks_ + hh * E;
 #pragma unroll
-      for (int ks = 0; ks < KD; ++ks) {
-        kop[ks] = load_op<bf16>((const bf16*)a.k + at + ks * KW);
-        vop[ks] = load_op<bf16>((const bf16*)a.v + at + ks * KW);
-      }
+      for (int ks = 0; ks < KD; ++ks) kop[ks] = load_op<bf16>((const bf16*)a.k + at + ks * KW);
     }
     op_t ms = {}, md = {};  // -1 for the three pieces of lse (hh = 0), of delta (hh = 1)
 #pragma unroll
@@ -879,11 +911,14 @@ __global__ __launch_bounds__(kWave* kWinWaves, 1) void hyb_win_dkv_ring_kernel(W
       trow[u] = (w * IPQ + u) % WT::IK * WT::RPI + lane / WT::CPR;
       tcol[u] = (lane % WT::CPR ^ WT::swz(trow[u])) * WT::EPC;
     }
-    int inh = h0, inq = 0;  // head and query tile of the next copies
+    // Head and query tile of this half's next copies and next products.
+    int inh = h0, inq = half, cq = half;
+    if (inq >= nq) inq -= nq, ++inh;
+    if (cq >= nq) cq -= nq;
     auto issue = [&](int n, Slot& s) __attribute__((always_inline)) {
-      if (n >= nsteps) return;
+      if (n >= mysteps) return;
       const int i0 = (t0 + inq) * kTile, left = len - 1 - i0;
-      const bool isq = w < kWinWaves / 2;
+      const bool isq = w < 2;
       const bf16* base = (const bf16*)(isq ? a.q : a.dout) + ((size_t)b * a.T * Hq + inh) * D + (size_t)i0 * qs;
       const __amdgpu_buffer_rsrc_t rs =
           __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(base), 0, (int)(kTile * qs * sizeof(bf16)), kBufferWord3);
@@ -895,22 +930,16 @@ __global__ __launch_bounds__(kWave* kWinWaves, 1) void hyb_win_dkv_ring_kernel(W
       const float* st = (const float*)a.ws + (((size_t)b * Hq + inh) * Tp + i0) * 8 + w * kWave + lane;
       __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)st,
                                        (__attribute__((address_space(3))) void*)((float*)s.st + w * kWave), 4, 0, 0);
-      if (++inq == nq) inq = 0, ++inh;
+      inq += 2;
+      while (inq >= nq) inq -= nq, ++inh;
     };
-    f32x16 sc, dp;
-    int cq = 0;  // query tile of the next scores
-    auto products = [&](const Slot& s, f32x16& p, f32x16& d) __attribute__((always_inline)) {
+    auto compute = [&](const Slot& s) __attribute__((always_inline)) {
       const op_t st = *reinterpret_cast<const op_t*>(&s.st[li * 16 + hh * 8]);
-      p = M::mma(st, ms, f32x16{});
-      d = M::mma(st, md, f32x16{});
+      f32x16 sc = M::mma(st, ms, f32x16{}), dp = M::mma(st, md, f32x16{});
 #pragma unroll
-      for (int ks = 0; ks < KD; ++ks) p = M::mma(wt.row_op(s.q, ks), kop[ks], p);
+      for (int ks = 0; ks < KD; ++ks) sc = M::mma(wt.row_op(s.q, ks), kop[ks], sc);
 #pragma unroll
-      for (int ks = 0; ks < KD; ++ks) d = M::mma(wt.row_op(s.d, ks), vop[ks], d);
-    };
-    auto take = [&](const f32x16& p, const f32x16& d) __attribute__((always_inline)) {
-      sc = p;
-      dp = d;
+      for (int ks = 0; ks < KD; ++ks) dp = M::mma(wt.row_op(s.d, ks), wt.row_op(sh.loop.v[w], ks), dp);
       const int i0 = (t0 + cq) * kTile;
       if (!(i0 >= f0 && i0 + kTile <= f1)) {  // uniform
 #pragma unroll
@@ -919,75 +948,79 @@ __global__ __launch_bounds__(kWave* kWinWaves, 1) void hyb_win_dkv_ring_kernel(W
           sc[e] = i >= mine.q0 && i < mine.q1 ? sc[e] : -INFINITY;
         }
       }
-      if (++cq == nq) cq = 0;
-    };
-    auto compute = [&](auto lastc, const Slot& next, const Slot& s) __attribute__((always_inline)) {
-      constexpr bool LAST = decltype(lastc)::value;
-      f32x16 pn, dn;
-      if constexpr (!LAST) products(next, pn, dn);
-      float p[16], ds[16];
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(sc[e] * scale);
-        ds[e] = p[e] * dp[e];
-      }
+      cq += 2;
+      while (cq >= nq) cq -= nq;
       op_t pop[KL], sop[KL];
 #pragma unroll
       for (int ks = 0; ks < KL; ++ks) {
-        pop[ks] = cvt_op<bf16>(&p[ks * E]);
-        sop[ks] = cvt_op<bf16>(&ds[ks * E]);
+        float p[E], ds[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(sc[ks * E + e] * scale);
+          ds[e] = p[e] * dp[ks * E + e];
+        }
+        pop[ks] = cvt_op<bf16>(p);
+        sop[ks] = cvt_op<bf16>(ds);
       }
 #pragma unroll
       for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
         for (int ks = 0; ks < KL; ++ks) {
-          dv[ct] = M::mma(wt.col_op(s.d, ct, ks), pop[ks], dv[ct]);
-          dk[ct] = M::mma(wt.col_op(s.q, ct, ks), sop[ks], dk[ct]);
+          acc[1][ct] = M::mma(wt.col_op(s.d, ct, ks), pop[ks], acc[1][ct]);
+          acc[0][ct] = M::mma(wt.col_op(s.q, ct, ks), sop[ks], acc[0][ct]);
         }
-      if constexpr (!LAST) take(pn, dn);
     };
+    // Tile n + 2 of the half goes to the slot of tile n - 1.
     auto step = [&](int n, auto S) __attribute__((always_inline)) {
       constexpr int SV = decltype(S)::value;
-      if (n + 2 < nsteps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(IPW) : "memory");
+      if (n + 1 < mysteps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(IPW) : "memory");
       else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       lds_barrier_nodrain();
-      issue(n + 3, ring[(SV + 3) % R]);
-      compute(std::false_type{}, ring[(SV + 1) % R], ring[SV]);
+      issue(n + 2, sh.loop.ring[half][(SV + 2) % R]);
+      if (n < mysteps) compute(sh.loop.ring[half][SV]);
     };
-    issue(0, ring[0]);
-    issue(1, ring[1]);
-    issue(2, ring[2]);
-    if (nsteps > 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * IPW) : "memory");
-    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    lds_barrier_nodrain();
-    {
-      f32x16 p, d;
-      products(ring[0], p, d);
-      take(p, d);
-    }
-    int n = 0;
-    for (; n + R < nsteps; n += R) {
+    issue(0, sh.loop.ring[half][0]);
+    issue(1, sh.loop.ring[half][1]);
+    for (int n = 0; n < nsteps; n += R) {
       step(n, std::integral_constant<int, 0>{});
-      step(n + 1, std::integral_constant<int, 1>{});
-      step(n + 2, std::integral_constant<int, 2>{});
-      step(n + 3, std::integral_constant<int, 3>{});
+      if (n + 1 < nsteps) step(n + 1, std::integral_constant<int, 1>{});
+      if (n + 2 < nsteps) step(n + 2, std::integral_constant<int, 2>{});
     }
-    if (n + 1 < nsteps) step(n, std::integral_constant<int, 0>{});
-    if (n + 2 < nsteps) step(n + 1, std::integral_constant<int, 1>{});
-    if (n + 3 < nsteps) step(n + 2, std::integral_constant<int, 2>{});
-    compute(std::true_type{}, ring[0], ring[nsteps - 1 - n]);
+    // The halves' sums: each hands over one of dK and dV and keeps the other.
+    lds_barrier_nodrain();
+#pragma unroll
+    for (int o = 0; o < 2; ++o)
+      if (o != half)
+#pragma unroll
+        for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            sh.join.x[o][w][ct * 4 + e][lane] = f32x4{acc[o][ct][4 * e], acc[o][ct][4 * e + 1], acc[o][ct][4 * e + 2],
+                                                      acc[o][ct][4 * e + 3]};
+    lds_barrier_nodrain();
+#pragma unroll
+    for (int o = 0; o < 2; ++o)
+      if (o == half)
+#pragma unroll
+        for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const f32x4 y = sh.join.x[o][w][ct * 4 + e][lane];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) acc[o][ct][4 * e + k] += y[k];
+          }
   }
   if (j >= a.T) return;
-  const size_t row = ((size_t)b * a.T + j) * Hkv + g;
-  const float fk = j < len ? 1.0f / sqrtf((float)D) : 0.0f, fv = j < len ? 1.0f : 0.0f;
-  if (parts == 1) {
-    win_store<bf16, D>(a.dk, row, dk, fk, hh, a.s.out_f32);
-    win_store<bf16, D>(a.dv, row, dv, fv, hh, a.s.out_f32);
-  } else {
-    const size_t rows = (size_t)a.s.B * a.T * Hkv;
-    win_store<bf16, D>(a.sums, part * 2 * rows + row, dk, fk, hh, true);
-    win_store<bf16, D>(a.sums, (part * 2 + 1) * rows + row, dv, fv, hh, true);
-  }
+  const size_t row = ((size_t)b * a.T + j) * Hkv + g, rows = (size_t)a.s.B * a.T * Hkv;
+  const float f = j >= len ? 0.0f : half == 0 ? 1.0f / sqrtf((float)D) : 1.0f;
+#pragma unroll
+  for (int o = 0; o < 2; ++o)
+    if (o == half) {
+      if (parts == 1)
+        win_store<bf16, D>(o == 0 ? a.dk : a.dv, row, acc[o], f, hh, a.s.out_f32);
+      else
+        win_store<bf16, D>(a.sums, (part * 2 + o) * rows + row, acc[o], f, hh, true);
+    }
 }
 
 // dK and dV from the parts' sums, in order; four entries per thread.
@@ -1059,7 +1092,7 @@ static hipError_t win_backward_ring_go(WindowArgs a, hipStream_t st) {
   hipLaunchKernelGGL(hyb_win_dq_ring_kernel<D>, dim3((unsigned)(a.s.B * a.s.Hkv * wgs)), dim3(kWave * kWinWaves), 0, st,
                      a, wgs);
   hipLaunchKernelGGL(hyb_win_dkv_ring_kernel<D>, dim3((unsigned)(a.s.B * a.s.Hkv * kwgs * parts)),
-                     dim3(kWave * kWinWaves), 0, st, a, kwgs, parts);
+                     dim3(kWave * kWinKeyWaves), 0, st, a, kwgs, parts);
   if (parts > 1) {
     const long n = (long)a.s.B * a.T * a.s.Hkv * D / 2;
     hipLaunchKernelGGL(hyb_win_sum_kernel<D>, dim3((unsigned)std::min<long>((n + 255) / 256, 4096)), dim3(256), 0, st, a,
