@@ -26,9 +26,6 @@
 #include "device.h"
 #include "launch.h"
 
-#ifndef WIN_ORDER
-#define WIN_ORDER 1
-#endif
 namespace hyb {
 
 // Reference of a query that has seen no key yet: finite, so that a tile in
@@ -402,18 +399,15 @@ struct WinRing {
   __device__ static constexpr int vswz(int t) { return 4 * ((t / RP256) % (CPR / 4)); }
 };
 
-// Where a (request, KV head)'s workgroups run: all on one XCD where their number
-// allows it (workgroups go to the 8 XCDs in turn), one (request, KV head) after
-// the other, so that what they read stays in that XCD's L2.
-__device__ inline void win_place(int bid, int nbg, int wgs, int& bg, int& x) {
-  if (WIN_ORDER == 0 && nbg % kNumXcd == 0) {
-    const int s = bid / kNumXcd;
-    bg = bid % kNumXcd + kNumXcd * (s / wgs);
-    x = s % wgs;
-  } else {
-    bg = bid % nbg;
-    x = bid / nbg;
-  }
+// The workgroups' order: the x-th workgroups of all (request, KV head)s one after
+// the other, so that with the longest first the chip ends with short ones; a
+// (request, KV head) stays on one XCD where their number is a multiple of 8
+// (workgroups go to the XCDs in turn), which keeps what it reads in that XCD's L2.
+// (One (request, KV head) after the other left the last one's long workgroups
+// to the end: gradient of 8 x 2048 tokens 618 us, now 503.)
+__device__ inline void win_place(int bid, int nbg, int& bg, int& x) {
+  bg = bid % nbg;
+  x = bid / nbg;
 }
 
 // The reference of a query's weights moves only when a tile's maximum passes it
@@ -434,7 +428,7 @@ __global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_ring_kernel(Windo
   const int li = lane & 31, hh = lane >> 5;
   const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv;
   int bg, x;
-  win_place(blockIdx.x, a.s.B * Hkv, wgs, bg, x);
+  win_place(blockIdx.x, a.s.B * Hkv, bg, x);
   x = wgs - 1 - x;  // the longest first
   const int b = bg / Hkv, g = bg % Hkv;
   const int len = win_len(a, b);
@@ -599,8 +593,8 @@ __global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_ring_kernel(Windo
 
 // ---- bf16 gradient ----------------------------------------------------------
 //
-// Three kernels: delta and the rows' statistics, dQ (a wave owns 32 queries and
-// loops over key tiles), dK with dV (a wave owns 32 keys and loops over the
+// Two kernels: dQ with delta and the rows' statistics (a wave owns 32 queries and
+// loops over key tiles), then dK with dV (a wave owns 32 keys and loops over the
 // query tiles of its KV head's heads).  Tiles come through rings as in the forward;
 // here a tile is read both by rows and, by transposing reads, by columns.
 template <int D>
@@ -656,33 +650,6 @@ __device__ inline bf16x8 win_pieces(float x) {
   }
   return o;
 }
-__device__ inline float win_value(bf16x8 p) { return ((float)p[2] + (float)p[1]) + (float)p[0]; }
-
-template <int D>
-__global__ __launch_bounds__(256) void hyb_win_stats_kernel(WindowArgs a) {
-  constexpr int LPR = D / 8;
-  const int Hq = a.s.Hq, Tp = win_tp(a.T);
-  const long rows = (long)a.s.B * Tp * Hq;
-  for (long r = (long)blockIdx.x * (256 / LPR) + threadIdx.x / LPR; r < rows; r += (long)gridDim.x * (256 / LPR)) {
-    const int h = (int)(r % Hq);
-    const long bi = r / Hq;
-    const int b = (int)(bi / Tp), i = (int)(bi % Tp);
-    float s = 0.0f, e = 0.0f;
-    if (i < win_len(a, b)) {
-      const size_t at = (((size_t)b * a.T + i) * Hq + h) * D + threadIdx.x % LPR * 8;
-      const bf16x8 x = load_op<bf16>((const bf16*)a.out + at), y = load_op<bf16>((const bf16*)a.dout + at);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) s += (float)x[k] * (float)y[k];
-      e = a.lse[((size_t)b * Hq + h) * a.T + i] * sqrtf((float)D);
-    }
-#pragma unroll
-    for (int o = 1; o < LPR; o <<= 1) s += __shfl_xor(s, o);
-    if (threadIdx.x % LPR < 2)
-      reinterpret_cast<bf16x8*>(a.ws)[(((size_t)b * Hq + h) * Tp + i) * 2 + threadIdx.x % LPR] =
-          win_pieces(threadIdx.x % LPR == 0 ? e : s);
-  }
-}
-
 template <int D>
 __global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_dq_ring_kernel(WindowArgs a, int wgs) {
   typedef Mma<bf16> M;
@@ -696,7 +663,7 @@ __global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_dq_ring_kernel(Wi
   const int li = lane & 31, hh = lane >> 5;
   const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv;
   int bg, x;
-  win_place(blockIdx.x, a.s.B * Hkv, wgs, bg, x);
+  win_place(blockIdx.x, a.s.B * Hkv, bg, x);
   x = wgs - 1 - x;  // the longest first
   const int b = bg / Hkv, g = bg % Hkv;
   const int len = win_len(a, b);
@@ -706,6 +673,13 @@ __global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_dq_ring_kernel(Wi
 #pragma unroll
   for (int ct = 0; ct < NCT; ++ct) acc[ct] = f32x16{};
   const int row = me.i0 + li;
+  // The statistics of row i, a half in each of its lanes; zero past the length.
+  const auto put_stats = [&](float e, float s) __attribute__((always_inline)) {
+    if (me.i0 < a.T)
+      reinterpret_cast<bf16x8*>(a.ws)[(((size_t)b * Hq + me.h) * win_tp(a.T) + row) * 2 + hh] =
+          win_pieces(row < len ? (hh == 0 ? e : s) : 0.0f);
+  };
+  if (first >= len) put_stats(0.0f, 0.0f);
   if (first < len) {  // uniform
     const WinTiles tl(a, len, first, last, kTile);
     const int ntiles = tl.n;
@@ -716,6 +690,7 @@ __global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_dq_ring_kernel(Wi
     const WinRow mine(a, len, i), r0(a, len, min(me.i0, len - 1)), r1(a, len, min(me.i0 + kTile, len) - 1);
     const WT wt(lane);
     op_t qop[KD], dop[KD];
+    float delta = 0.0f;
     {
       const size_t at = ((size_t)b * a.T * Hq + me.h) * D + i * qs + hh * E;
 #pragma unroll
@@ -723,11 +698,17 @@ __global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_dq_ring_kernel(Wi
         qop[ks] = load_op<bf16>((const bf16*)a.q + at + ks * KW);
         dop[ks] = load_op<bf16>((const bf16*)a.dout + at + ks * KW);
       }
+#pragma unroll
+      for (int ks = 0; ks < KD; ++ks) {
+        const op_t o = load_op<bf16>((const bf16*)a.out + at + ks * KW);
+#pragma unroll
+        for (int e = 0; e < E; ++e) delta += (float)o[e] * (float)dop[ks][e];
+      }
+      delta += xor32(delta);
     }
     const float scale = kLog2e / sqrtf((float)D);
-    const float lse = a.lse[((size_t)b * Hq + me.h) * a.T + i] * kLog2e;
-    const float delta =
-        win_value(reinterpret_cast<const bf16x8*>(a.ws)[(((size_t)b * Hq + me.h) * win_tp(a.T) + i) * 2 + 1]);
+    const float nat = a.lse[((size_t)b * Hq + me.h) * a.T + i], lse = nat * kLog2e;
+    put_stats(nat * sqrtf((float)D), delta);
 
     int trow[IPW], tcol[IPW];
 #pragma unroll
@@ -829,9 +810,21 @@ __global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_dq_ring_kernel(Wi
 // from LDS.)
 constexpr int kWinKeyWaves = 8;
 
+// How the workgroups' lists of query tiles (of all heads) are cut into parts
+// that are summed in the workspace: those of the keys among the sinks, which
+// every later query sees (the first `ns` workgroups of a (request, KV head)), into
+// ps, the others into p.
+struct WinParts {
+  int wgs, ns, ps, p;
+  __host__ __device__ int items() const { return ns * ps + (wgs - ns) * p; }
+  // Rows of partial sums of dK and dV: ps for the first ns workgroups' keys
+  // (padded), then p of every key, each where there is more than one.
+  __host__ __device__ long sink_rows() const { return ps > 1 ? (long)ps * ns * 4 * kTile : 0; }
+  __host__ __device__ long rows(int T) const { return sink_rows() + (p > 1 ? (long)p * T : 0); }
+};
+
 template <int D>
-__global__ __launch_bounds__(kWave* kWinKeyWaves, 2) void hyb_win_dkv_ring_kernel(WindowArgs a, int wgs,
-                                                                                           int parts) {
+__global__ __launch_bounds__(kWave* kWinKeyWaves, 2) void hyb_win_dkv_ring_kernel(WindowArgs a, WinParts cut) {
   typedef Mma<bf16> M;
   typedef M::op_t op_t;
   typedef WinTile<D> WT;
@@ -860,11 +853,13 @@ __global__ __launch_bounds__(kWave* kWinKeyWaves, 2) void hyb_win_dkv_ring_kerne
   const int li = lane & 31, hh = lane >> 5;
   const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv, Tp = win_tp(a.T);
   int bg, x;
-  win_place(blockIdx.x, a.s.B * Hkv, wgs * parts, bg, x);
+  win_place(blockIdx.x, a.s.B * Hkv, bg, x);  // the longest (first keys) first
+  const bool sink = x < cut.ns * cut.ps;
+  const int parts = sink ? cut.ps : cut.p;
+  if (!sink) x -= cut.ns * cut.ps;
   const int part = x % parts;
-  x /= parts;  // the longest (first keys) first
+  x = x / parts + (sink ? 0 : cut.ns);
   const int b = bg / Hkv, g = bg % Hkv;
-  const int h0 = g * G + part * G / parts, h1 = g * G + (part + 1) * G / parts;  // this part's heads
   const int len = win_len(a, b);
   const int w0 = x * 4 * kTile, j0 = w0 + w * kTile, j = j0 + li;
   f32x16 acc[2][NCT];  // dK, dV
@@ -872,9 +867,11 @@ __global__ __launch_bounds__(kWave* kWinKeyWaves, 2) void hyb_win_dkv_ring_kerne
   for (int ct = 0; ct < NCT; ++ct) acc[0][ct] = acc[1][ct] = f32x16{};
   if (w0 < len) {  // uniform
     const size_t qs = (size_t)Hq * D, ks_ = (size_t)Hkv * D;
-    // query tiles t0 .. t0 + nq - 1 of every head; a half takes every second
+    // query tiles t0 .. t0 + nq - 1 of every head, of which this part takes
+    // ntiles from first on, a half every second
     const WinQueries all(a, len, w0, min(w0 + 4 * kTile, len));
-    const int t0 = all.q0 / kTile, nq = (all.q1 + kTile - 1) / kTile - t0, ntiles = nq * (h1 - h0);
+    const int t0 = all.q0 / kTile, nq = (all.q1 + kTile - 1) / kTile - t0;
+    const int first = (int)((long)nq * G * part / parts), ntiles = (int)((long)nq * G * (part + 1) / parts) - first;
     const int nsteps = (ntiles + 1) / 2, mysteps = (ntiles + 1 - half) / 2;
     const WinKey mine(a, len, min(j, len - 1));
     // query tiles that every key of the wave is seen by: f0 <= i0 and i0 + 32 <= f1
@@ -912,9 +909,7 @@ __global__ __launch_bounds__(kWave* kWinKeyWaves, 2) void hyb_win_dkv_ring_kerne
       tcol[u] = (lane % WT::CPR ^ WT::swz(trow[u])) * WT::EPC;
     }
     // Head and query tile of this half's next copies and next products.
-    int inh = h0, inq = half, cq = half;
-    if (inq >= nq) inq -= nq, ++inh;
-    if (cq >= nq) cq -= nq;
+    int inh = g * G + (first + half) / nq, inq = (first + half) % nq, cq = inq;
     auto issue = [&](int n, Slot& s) __attribute__((always_inline)) {
       if (n >= mysteps) return;
       const int i0 = (t0 + inq) * kTile, left = len - 1 - i0;
@@ -1011,7 +1006,10 @@ __global__ __launch_bounds__(kWave* kWinKeyWaves, 2) void hyb_win_dkv_ring_kerne
           }
   }
   if (j >= a.T) return;
-  const size_t row = ((size_t)b * a.T + j) * Hkv + g, rows = (size_t)a.s.B * a.T * Hkv;
+  // this part's rows of sums: [part][dK, dV][B][rows][Hkv][D]
+  const int span = sink ? cut.ns * 4 * kTile : a.T;
+  const size_t row = ((size_t)b * a.T + j) * Hkv + g, rows = (size_t)a.s.B * span * Hkv;
+  float* const sums = a.sums + (sink ? 0 : cut.sink_rows() * 2 * a.s.B * Hkv * D);
   const float f = j >= len ? 0.0f : half == 0 ? 1.0f / sqrtf((float)D) : 1.0f;
 #pragma unroll
   for (int o = 0; o < 2; ++o)
@@ -1019,19 +1017,25 @@ __global__ __launch_bounds__(kWave* kWinKeyWaves, 2) void hyb_win_dkv_ring_kerne
       if (parts == 1)
         win_store<bf16, D>(o == 0 ? a.dk : a.dv, row, acc[o], f, hh, a.s.out_f32);
       else
-        win_store<bf16, D>(a.sums, (part * 2 + o) * rows + row, acc[o], f, hh, true);
+        win_store<bf16, D>(sums, (part * 2 + o) * rows + ((size_t)b * span + j) * Hkv + g, acc[o], f, hh, true);
     }
 }
 
-// dK and dV from the parts' sums, in order; four entries per thread.
+// dK and dV from the parts' sums, in order, of the keys j0 .. j1 - 1; four
+// entries per thread.
 template <int D>
-__global__ __launch_bounds__(256) void hyb_win_sum_kernel(WindowArgs a, int parts) {
-  const size_t n = (size_t)a.s.B * a.T * a.s.Hkv * D / 4;
+__global__ __launch_bounds__(256) void hyb_win_sum_kernel(WindowArgs a, const float* sums, int parts, int span, int j0,
+                                                          int j1) {
+  const size_t per = (size_t)a.s.Hkv * D / 4, n = (size_t)a.s.B * (j1 - j0) * per, all = (size_t)a.s.B * span * per;
   for (size_t x = (size_t)blockIdx.x * 256 + threadIdx.x; x < 2 * n; x += (size_t)gridDim.x * 256) {
+    const int o = x >= n;
+    const size_t y = x - o * n, bj = y / per, c = y % per;
+    const size_t b = bj / (j1 - j0), j = j0 + bj % (j1 - j0);
+    const f32x4* src = reinterpret_cast<const f32x4*>(sums) + o * all + (b * span + j) * per + c;
     f32x4 s = {};
-    for (int p = 0; p < parts; ++p) s += reinterpret_cast<const f32x4*>(a.sums)[p * 2 * n + x];
-    const float o[4] = {s[0], s[1], s[2], s[3]};
-    store_out4<bf16>(x < n ? a.dk : a.dv, 4 * (x < n ? x : x - n), o, a.s.out_f32);
+    for (int p = 0; p < parts; ++p) s += src[2 * all * p];
+    const float v[4] = {s[0], s[1], s[2], s[3]};
+    store_out4<bf16>(o ? a.dv : a.dk, 4 * ((b * a.T + j) * per + c), v, a.s.out_f32);
   }
 }
 
@@ -1070,34 +1074,51 @@ static hipError_t win_backward_go(const WindowArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-// Parts that a KV head's query heads are cut into where its keys alone make few
-// workgroups: each sums its heads' dK and dV in the workspace.
-static int win_parts(const Shape& s, int T) {
-  const long wgs = (long)s.B * s.Hkv * ((T + kWinWaves * kTile - 1) / (kWinWaves * kTile));
-  const int G = s.Hq / s.Hkv;
-  int p = 1;
-  while (p < G && wgs * p < 512) ++p;
-  return p;
+// The cut: about two workgroups per CU (512, one at a time), each of 16 query
+// tiles or more; the sinks' keys in parts as long as the others', at most 16 of them
+// all together.
+static WinParts win_cut(const Shape& s, int T, int window, int n_sinks) {
+  const int wk = 4 * kTile, G = s.Hq / s.Hkv;
+  WinParts c;
+  c.wgs = (T + wk - 1) / wk;
+  c.ns = std::min(c.wgs, (std::min(n_sinks, T) + wk - 1) / wk);
+  const long all = (long)s.B * s.Hkv * c.wgs, every = ((long)T + kTile - 1) / kTile * G;
+  const long seen = std::min<long>(every, (((long)window + s.L + wk + kTile - 1) / kTile + 1) * G);  // tiles of a list
+  c.p = (int)std::max<long>(1, std::min<long>((512 + all - 1) / all, seen / 16));
+  const long each = (seen + c.p - 1) / c.p;
+  c.ps = c.p;
+  if (c.ns > 0 && every >= 2 * each)
+    c.ps = (int)std::max<long>(c.p, std::min<long>((every + each - 1) / each, 16 / c.ns));
+  return c;
 }
 static size_t win_stats_bytes(const Shape& s, int T) { return (size_t)s.B * s.Hq * win_tp(T) * 32; }
+// Partial sums at most, for any window and number of sinks (whose workgroups
+// times parts are 16, or every workgroup p times).
+static size_t win_sums_bytes(const Shape& s, int T) {
+  const WinParts c = win_cut(s, T, T, 0);
+  const long sinks = c.wgs > 1 ? 16 : std::min(16, (T + kTile - 1) / kTile * (s.Hq / s.Hkv));
+  const long most = std::max((long)c.wgs * c.p, sinks);
+  return (size_t)(most * 4 * kTile + (c.p > 1 ? (long)c.p * T : 0)) * 2 * s.B * s.Hkv * s.D * sizeof(float);
+}
 
 template <int D>
 static hipError_t win_backward_ring_go(WindowArgs a, hipStream_t st) {
-  const int parts = win_parts(a.s, a.T);
+  const WinParts cut = win_cut(a.s, a.T, a.window, a.n_sinks);
   a.sums = (float*)((char*)a.ws + win_stats_bytes(a.s, a.T));
-  const long rows = (long)a.s.B * win_tp(a.T) * a.s.Hq;
-  hipLaunchKernelGGL(hyb_win_stats_kernel<D>, dim3((unsigned)std::min<long>((rows * D / 8 + 255) / 256, 4096)),
-                     dim3(256), 0, st, a);
-  const int wgs = win_wgs(a), kwgs = (a.T + kWinWaves * kTile - 1) / (kWinWaves * kTile);
+  const int wgs = win_wgs(a);
   hipLaunchKernelGGL(hyb_win_dq_ring_kernel<D>, dim3((unsigned)(a.s.B * a.s.Hkv * wgs)), dim3(kWave * kWinWaves), 0, st,
                      a, wgs);
-  hipLaunchKernelGGL(hyb_win_dkv_ring_kernel<D>, dim3((unsigned)(a.s.B * a.s.Hkv * kwgs * parts)),
-                     dim3(kWave * kWinKeyWaves), 0, st, a, kwgs, parts);
-  if (parts > 1) {
-    const long n = (long)a.s.B * a.T * a.s.Hkv * D / 2;
+  hipLaunchKernelGGL(hyb_win_dkv_ring_kernel<D>, dim3((unsigned)(a.s.B * a.s.Hkv * cut.items())),
+                     dim3(kWave * kWinKeyWaves), 0, st, a, cut);
+  const int sinks = std::min(cut.ns * 4 * kTile, a.T);  // keys of the sinks' workgroups
+  auto sum = [&](const float* sums, int parts, int span, int j0, int j1) {
+    if (parts == 1 || j0 >= j1) return;
+    const long n = (long)a.s.B * (j1 - j0) * a.s.Hkv * D / 2;
     hipLaunchKernelGGL(hyb_win_sum_kernel<D>, dim3((unsigned)std::min<long>((n + 255) / 256, 4096)), dim3(256), 0, st, a,
-                       parts);
-  }
+                       sums, parts, span, j0, j1);
+  };
+  sum(a.sums, cut.ps, cut.ns * 4 * kTile, 0, sinks);
+  sum(a.sums + cut.sink_rows() * 2 * a.s.B * a.s.Hkv * D, cut.p, a.T, sinks, a.T);
   return hipGetLastError();
 }
 
@@ -1119,8 +1140,7 @@ long window_workgroups(const Shape& s, int T) {
 
 size_t window_backward_ws_bytes(const Shape& s, int T) {
   if (s.dtype != 1) return (size_t)s.B * s.Hq * T * sizeof(float);  // delta
-  const int parts = win_parts(s, T);
-  return win_stats_bytes(s, T) + (parts > 1 ? (size_t)parts * 2 * s.B * T * s.Hkv * s.D * sizeof(float) : 0);
+  return win_stats_bytes(s, T) + win_sums_bytes(s, T);
 }
 
 }  // namespace hyb
