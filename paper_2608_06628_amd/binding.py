@@ -8,7 +8,9 @@ library has not been built, loading it raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
+import functools
 import os
 
 import torch
@@ -399,278 +401,280 @@ def hybrid_attn_backward_full(q, k, v, W, alpha, block, dout=None, target=None, 
 # current one is, and allocate on the stream they run on, so that a buffer
 # made here is neither written before earlier work has left it nor reused
 # while the call still runs.
-class _On:
-    """The device and stream of a call: `with _On(tensor, stream) as st`."""
-
-    def __init__(self, t, stream):
-        if not isinstance(t, torch.Tensor) or not t.is_cuda:
-            raise TypeError("expected CUDA (HIP) tensors")
-        self.dev = t.get_device()
-        self.ctx = []
-        if self.dev != torch._C._cuda_getDevice():
-            self.ctx.append(torch.cuda.device(self.dev))
-        if stream is not None:
-            if not isinstance(stream, torch.cuda.Stream):
-                stream = torch.cuda.ExternalStream(stream, device=t.device)
-            if stream.device != t.device:
-                raise ValueError(f"a stream of {stream.device} for tensors of {t.device}")
-            self.ctx.append(torch.cuda.stream(stream))
-
-    def __enter__(self):
-        for c in self.ctx:
-            c.__enter__()
-        return torch._C._cuda_getCurrentRawStream(self.dev)
-
-    def __exit__(self, *exc):
-        for c in reversed(self.ctx):
-            c.__exit__(*exc)
-
-    def ptr(self, t, name, dtype=None, shape=None):
-        """The address of a contiguous tensor of this device (None for None)."""
-        p = _ptr(t, name, dtype)
-        if t is not None:
-            self.check(t, name, shape)
-        return p
-
-    def check(self, t, name, shape):
-        if t.get_device() != self.dev:
-            raise ValueError(f"{name} is on device {t.get_device()}, the call runs on {self.dev}")
-        if shape is not None and t.shape != shape:
-            raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-
-    def rows(self, t, name, dtype, shape):
-        """The address and row stride of [N][H][d] whose rows [H][d] are contiguous."""
-        if t is None:
-            return None, 0
-        if not isinstance(t, torch.Tensor) or not t.is_cuda:
-            raise TypeError(f"{name} must be a CUDA (HIP) tensor")
-        if t.dtype is not dtype:
-            raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-        self.check(t, name, shape)
-        if t.stride(2) != 1 or t.stride(1) != shape[2]:
-            raise ValueError(f"{name}: the heads of a token must be contiguous")
-        # (a stride says nothing where there is at most one row)
-        return t.data_ptr(), t.stride(0) if shape[0] > 1 else 0
+def _placed(f):
+    @functools.wraps(f)
+    def call(first, *args, stream=None, **kw):
+        try:
+            dev = first.get_device()
+        except AttributeError:
+            dev = -1
+        if dev < 0:
+            raise TypeError(f"{f.__name__} takes CUDA (HIP) tensors")
+        if stream is None and dev == torch._C._cuda_getDevice():
+            return f(dev, first, *args, **kw)
+        with contextlib.ExitStack() as on:
+            on.enter_context(torch.cuda.device(dev))
+            if stream is not None:
+                if not isinstance(stream, torch.cuda.Stream):
+                    stream = torch.cuda.ExternalStream(stream, device=dev)
+                if stream.device.index != dev:
+                    raise ValueError(f"a stream of {stream.device} for tensors of device {dev}")
+                on.enter_context(torch.cuda.stream(stream))
+            return f(dev, first, *args, **kw)
+    return call
 
 
-def _rope_call(on, q, k, wq, wk, inv_freq, positions, eps, rot_scale, layout, q_out, k_out, odt,
-               v=None, grad_dtype=HYB_BF16):
-    """Dims and the addresses of what the rope entry points share."""
-    N, Hq, d = q.shape
-    Hkv = k.shape[1]
-    act = q.dtype
-    (pq, sq), (pk, sk) = on.rows(q, "q", act, (N, Hq, d)), on.rows(k, "k", act, (N, Hkv, d))
-    pv, sv = on.rows(v, "v", act, (N, Hkv, d))
-    (oq, soq), (ok, sok) = (on.rows(q_out, "q_out", odt, (N, Hq, d)),
-                            on.rows(k_out, "k_out", odt, (N, Hkv, d)))
-    flags = HYB_OUT_F32 if odt == torch.float32 and act != torch.float32 else 0
-    dims = RopeDims(N, Hq, Hkv, d, 2 * inv_freq.shape[0] if inv_freq is not None else 0,
-                    _ROPE_LAYOUT[layout], _dt(q), grad_dtype, flags, eps, rot_scale, sq, sk, sv,
-                    soq, sok)
-    small = (on.ptr(wq, "wq", act, (d,)), on.ptr(wk, "wk", act, (d,)),
-             on.ptr(positions, "positions", torch.int32, (N,)),
-             on.ptr(inv_freq, "inv_freq", torch.float64))
-    return dims, (pq, pk, pv, oq, ok), small
+def _dptr(dev, t, name, dtype, shape=None):
+    """The address of a contiguous tensor of the device (None for None)."""
+    if t is None:
+        return None
+    try:
+        if (t.get_device() == dev and t.dtype is dtype and t.is_contiguous()
+                and (shape is None or t.shape == shape)):
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _ptr(t, name, dtype)
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on device {t.get_device()}, the call runs on {dev}")
+    raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
 
 
-def hybrid_qk_norm_rope(q, k, inv_freq, positions, wq=None, wk=None, eps=1e-6, rot_scale=1.0,
-                        layout="half", q_out=None, k_out=None, out_f32=False, stream=None):
-    """Norm (weights wq, wk [d], None: no norm) and rotation of q [N][Hq][d] and
-    k [N][Hkv][d], which may be views of one packed projection, by positions [N]
-    int32 and inv_freq [rot_dim / 2] float64 (None: no rotation); layout "half"
-    or "interleaved".  Returns (q_out, k_out)."""
-    lib = load()
-    on = _On(q, stream)
-    with on as st:
-        odt = torch.float32 if out_f32 or (q_out is not None and q_out.dtype == torch.float32) else q.dtype
-        if q_out is None:
-            q_out = torch.empty(q.shape, dtype=odt, device=q.device)
-        if k_out is None:
-            k_out = torch.empty(k.shape, dtype=odt, device=q.device)
-        dims, (pq, pk, _, oq, ok), (pwq, pwk, pos, freq) = _rope_call(
-            on, q, k, wq, wk, inv_freq, positions, eps, rot_scale, layout, q_out, k_out, odt)
-        _check(lib.hybrid_qk_norm_rope(ctypes.byref(dims), pq, pk, pwq, pwk, pos, freq, oq, ok, st))
-    return q_out, k_out
-
-
-def hybrid_qk_norm_rope_paged(q, k, v, inv_freq, positions, slots, k_pages, v_pages, wq=None,
-                              wk=None, eps=1e-6, rot_scale=1.0, layout="half", q_out=None,
-                              k_out=None, want_k=False, out_f32=False, stream=None):
-    """hybrid_qk_norm_rope with k's result and v [N][Hkv][d] written to rows slots
-    [N] (int32; -1: nowhere) of the pools k_pages, v_pages [n_pages][page_size][Hkv][d].
-    Returns (q_out, k_out), k_out None unless given or asked for with want_k."""
-    lib = load()
-    on = _On(q, stream)
-    with on as st:
-        odt = torch.float32 if out_f32 or (q_out is not None and q_out.dtype == torch.float32) else q.dtype
-        if q_out is None:
-            q_out = torch.empty(q.shape, dtype=odt, device=q.device)
-        if k_out is None and want_k:
-            k_out = torch.empty(k.shape, dtype=odt, device=q.device)
-        dims, (pq, pk, pv, oq, ok), (pwq, pwk, pos, freq) = _rope_call(
-            on, q, k, wq, wk, inv_freq, positions, eps, rot_scale, layout, q_out, k_out, odt, v=v)
-        pool = (k_pages.shape[0], k_pages.shape[1], k.shape[1], k.shape[2])
-        _check(lib.hybrid_qk_norm_rope_paged(
-            ctypes.byref(dims), pq, pk, pv, pwq, pwk, pos, freq,
-            on.ptr(slots, "slots", torch.int32, (q.shape[0],)), oq, ok,
-            on.ptr(k_pages, "k_pages", q.dtype, pool), on.ptr(v_pages, "v_pages", q.dtype, pool),
-            pool[0], pool[1], st))
-    return q_out, k_out
-
-
-def hybrid_qk_norm_rope_backward(q, k, dq_out, dk_out, inv_freq, positions, wq=None, wk=None,
-                                 eps=1e-6, rot_scale=1.0, layout="half", dq=None, dk=None,
-                                 out_f32=False, ws=None, stream=None):
-    """Gradient of hybrid_qk_norm_rope for dq_out [N][Hq][d], dk_out [N][Hkv][d]
-    (both fp32 or both bf16).  Returns (dq, dk in q's dtype or fp32 with out_f32,
-    dwq, dwk fp32 [d] or None where there is no weight)."""
-    lib = load()
-    on = _On(q, stream)
-    with on as st:
-        odt = torch.float32 if out_f32 or (dq is not None and dq.dtype == torch.float32) else q.dtype
-        dev, f32 = q.device, torch.float32
-        if dq is None:
-            dq = torch.empty(q.shape, dtype=odt, device=dev)
-        if dk is None:
-            dk = torch.empty(k.shape, dtype=odt, device=dev)
-        dwq = torch.empty(q.shape[2], dtype=f32, device=dev) if wq is not None else None
-        dwk = torch.empty(q.shape[2], dtype=f32, device=dev) if wk is not None else None
-        dims, (pq, pk, _, oq, ok), (pwq, pwk, pos, freq) = _rope_call(
-            on, q, k, wq, wk, inv_freq, positions, eps, rot_scale, layout, dq, dk, odt,
-            grad_dtype=_dt(dq_out))
-        if ws is None and (wq is not None or wk is not None):
-            ws = torch.empty(int(lib.hybrid_rope_workspace_bytes(ctypes.byref(dims))),
-                             dtype=torch.uint8, device=dev)
-        _check(lib.hybrid_qk_norm_rope_backward(
-            ctypes.byref(dims), pq, pk, pwq, pwk, pos, freq,
-            on.ptr(dq_out, "dq_out", dq_out.dtype, q.shape),
-            on.ptr(dk_out, "dk_out", dq_out.dtype, k.shape), oq, ok, on.ptr(dwq, "dwq"),
-            on.ptr(dwk, "dwk"), on.ptr(ws, "ws"), _bytes(ws), st))
-    return dq, dk, dwq, dwk
+def _rows(dev, t, name, dtype, shape):
+    """The address and row stride of [N][H][d] whose rows [H][d] are contiguous."""
+    if t is None:
+        return None, 0
+    try:
+        if t.get_device() == dev and t.dtype is dtype and t.shape == shape:
+            s = t.stride()
+            if s[2] == 1 and (s[1] == shape[2] or shape[1] == 1):
+                # (a stride says nothing where there is at most one row)
+                return t.data_ptr(), s[0] if shape[0] > 1 else 0
+    except AttributeError:
+        pass
+    _dptr(dev, t.contiguous() if isinstance(t, torch.Tensor) else t, name, dtype, shape)
+    raise ValueError(f"{name}: the heads of a token must be contiguous")
 
 
 def _bytes(t):
     return t.numel() * t.element_size() if t is not None else 0
 
 
-def kv_pages_plan(prefix_len, new_len, page_table, free_pages, page_size, max_tokens,
-                  stream=None):
+# (a ctypes structure costs more to fill than to find; nothing writes to them)
+_rope_dims = functools.lru_cache(maxsize=256)(RopeDims)
+_dims = functools.lru_cache(maxsize=256)(make_dims)
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _odt(act, out, out_f32):
+    if out is not None:
+        out_f32 = out.dtype == torch.float32
+    return torch.float32 if out_f32 else act
+
+
+def _rope_args(dev, q, k, wq, wk, inv_freq, positions, eps, rot_scale, layout, q_out, k_out, odt,
+               v=None, grad=HYB_BF16):
+    """Dims and the addresses that the rope entry points share."""
+    N, Hq, d = qs = q.shape
+    ks = k.shape
+    act = q.dtype
+    if len(ks) != 3 or ks[0] != N or ks[2] != d:
+        raise ValueError(f"k must have shape [{N}][heads][{d}], got {tuple(ks)}")
+    pq, sq = _rows(dev, q, "q", act, qs)
+    pk, sk = _rows(dev, k, "k", act, ks)
+    pv, sv = _rows(dev, v, "v", act, ks)
+    oq, soq = _rows(dev, q_out, "q_out", odt, qs)
+    ok, sok = _rows(dev, k_out, "k_out", odt, ks)
+    dims = _rope_dims(N, Hq, ks[1], d, 2 * inv_freq.shape[0] if inv_freq is not None else 0,
+                      _ROPE_LAYOUT[layout], _dt(q), grad,
+                      HYB_OUT_F32 if odt is not act else 0, eps, rot_scale, sq, sk, sv, soq, sok)
+    return (dims, pq, pk, pv, oq, ok, _dptr(dev, wq, "wq", act, (d,)),
+            _dptr(dev, wk, "wk", act, (d,)), _dptr(dev, positions, "positions", torch.int32, (N,)),
+            _dptr(dev, inv_freq, "inv_freq", torch.float64))
+
+
+@_placed
+def hybrid_qk_norm_rope(dev, q, k, inv_freq, positions, wq=None, wk=None, eps=1e-6, rot_scale=1.0,
+                        layout="half", q_out=None, k_out=None, out_f32=False):
+    """Norm (weights wq, wk [d], None: no norm) and rotation of q [N][Hq][d] and
+    k [N][Hkv][d], which may be views of one packed projection, by positions [N]
+    int32 and inv_freq [rot_dim / 2] float64 (None: no rotation); layout "half"
+    or "interleaved".  Returns (q_out, k_out)."""
+    odt = _odt(q.dtype, q_out, out_f32)
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=odt, device=q.device)
+    if k_out is None:
+        k_out = torch.empty(k.shape, dtype=odt, device=q.device)
+    dims, pq, pk, _, oq, ok, pwq, pwk, pos, freq = _rope_args(
+        dev, q, k, wq, wk, inv_freq, positions, eps, rot_scale, layout, q_out, k_out, odt)
+    _check(load().hybrid_qk_norm_rope(dims, pq, pk, pwq, pwk, pos, freq, oq, ok, _raw_stream(dev)))
+    return q_out, k_out
+
+
+@_placed
+def hybrid_qk_norm_rope_paged(dev, q, k, v, inv_freq, positions, slots, k_pages, v_pages, wq=None,
+                              wk=None, eps=1e-6, rot_scale=1.0, layout="half", q_out=None,
+                              k_out=None, want_k=False, out_f32=False):
+    """hybrid_qk_norm_rope with k's result and v [N][Hkv][d] written to rows slots
+    [N] (int32; -1: nowhere) of the pools k_pages, v_pages [n_pages][page_size][Hkv][d].
+    Returns (q_out, k_out), k_out None unless given or asked for with want_k."""
+    odt = _odt(q.dtype, q_out, out_f32)
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=odt, device=q.device)
+    if k_out is None and want_k:
+        k_out = torch.empty(k.shape, dtype=odt, device=q.device)
+    dims, pq, pk, pv, oq, ok, pwq, pwk, pos, freq = _rope_args(
+        dev, q, k, wq, wk, inv_freq, positions, eps, rot_scale, layout, q_out, k_out, odt, v=v)
+    n_pages, page_size = k_pages.shape[:2]
+    pool = (n_pages, page_size) + tuple(k.shape[1:])
+    _check(load().hybrid_qk_norm_rope_paged(
+        dims, pq, pk, pv, pwq, pwk, pos, freq,
+        _dptr(dev, slots, "slots", torch.int32, (q.shape[0],)), oq, ok,
+        _dptr(dev, k_pages, "k_pages", q.dtype, pool),
+        _dptr(dev, v_pages, "v_pages", q.dtype, pool), n_pages, page_size, _raw_stream(dev)))
+    return q_out, k_out
+
+
+@_placed
+def hybrid_qk_norm_rope_backward(dev, q, k, dq_out, dk_out, inv_freq, positions, wq=None, wk=None,
+                                 eps=1e-6, rot_scale=1.0, layout="half", dq=None, dk=None,
+                                 out_f32=False, ws=None):
+    """Gradient of hybrid_qk_norm_rope for dq_out [N][Hq][d], dk_out [N][Hkv][d]
+    (both fp32 or both bf16).  Returns (dq, dk in q's dtype or fp32 with out_f32,
+    dwq, dwk fp32 [d] or None where there is no weight)."""
+    lib = load()
+    odt = _odt(q.dtype, dq, out_f32)
+    at, f32, d = q.device, torch.float32, q.shape[2]
+    if dq is None:
+        dq = torch.empty(q.shape, dtype=odt, device=at)
+    if dk is None:
+        dk = torch.empty(k.shape, dtype=odt, device=at)
+    dwq = torch.empty(d, dtype=f32, device=at) if wq is not None else None
+    dwk = torch.empty(d, dtype=f32, device=at) if wk is not None else None
+    dims, pq, pk, _, oq, ok, pwq, pwk, pos, freq = _rope_args(
+        dev, q, k, wq, wk, inv_freq, positions, eps, rot_scale, layout, dq, dk, odt,
+        grad=_dt(dq_out))
+    if ws is None and (wq is not None or wk is not None):
+        ws = torch.empty(lib.hybrid_rope_workspace_bytes(dims), dtype=torch.uint8, device=at)
+    _check(lib.hybrid_qk_norm_rope_backward(
+        dims, pq, pk, pwq, pwk, pos, freq, _dptr(dev, dq_out, "dq_out", dq_out.dtype, q.shape),
+        _dptr(dev, dk_out, "dk_out", dq_out.dtype, k.shape), oq, ok,
+        None if dwq is None else dwq.data_ptr(), None if dwk is None else dwk.data_ptr(),
+        _dptr(dev, ws, "ws", torch.uint8), _bytes(ws), _raw_stream(dev)))
+    return dq, dk, dwq, dwk
+
+
+@_placed
+def kv_pages_plan(dev, prefix_len, new_len, page_table, free_pages, page_size, max_tokens):
     """Pages (written into page_table [B][max_pages] int32 from free_pages) and
     rows of the new_len [B] tokens that follow prefix_len [B] cached ones, all
     int32 on the device.  Returns (slots [max_tokens], positions [max_tokens],
     token_start [B + 1], counts [2]: pages taken and missing)."""
-    lib = load()
-    on = _On(prefix_len, stream)
-    with on as st:
-        B, max_pages = page_table.shape
-        i32, dev = torch.int32, prefix_len.device
-        slots = torch.empty(max_tokens, dtype=i32, device=dev)
-        positions = torch.empty(max_tokens, dtype=i32, device=dev)
-        start = torch.empty(B + 1, dtype=i32, device=dev)
-        counts = torch.empty(2, dtype=i32, device=dev)
-        if B == 0:
-            slots.fill_(-1), positions.zero_(), start.zero_(), counts.zero_()
-        _check(lib.kv_pages_plan(
-            B, max_pages, page_size, free_pages.numel() if free_pages is not None else 0,
-            max_tokens, on.ptr(prefix_len, "prefix_len", i32, (B,)),
-            on.ptr(new_len, "new_len", i32, (B,)), on.ptr(free_pages, "free_pages", i32),
-            on.ptr(page_table, "page_table", i32), on.ptr(slots, "slots"),
-            on.ptr(positions, "positions"), on.ptr(start, "token_start"),
-            on.ptr(counts, "counts"), st))
+    B, max_pages = page_table.shape
+    i32, at = torch.int32, prefix_len.device
+    if B == 0:
+        return (torch.full((max_tokens,), -1, dtype=i32, device=at),
+                *(torch.zeros(n, dtype=i32, device=at) for n in (max_tokens, 1, 2)))
+    slots, positions, start, counts = (torch.empty(n, dtype=i32, device=at)
+                                       for n in (max_tokens, max_tokens, B + 1, 2))
+    _check(load().kv_pages_plan(
+        B, max_pages, page_size, free_pages.numel() if free_pages is not None else 0, max_tokens,
+        _dptr(dev, prefix_len, "prefix_len", i32, (B,)), _dptr(dev, new_len, "new_len", i32, (B,)),
+        _dptr(dev, free_pages, "free_pages", i32), _dptr(dev, page_table, "page_table", i32),
+        slots.data_ptr(), positions.data_ptr(), start.data_ptr(), counts.data_ptr(),
+        _raw_stream(dev)))
     return slots, positions, start, counts
 
 
-def softmax_window_step_paged(q, k, v, k_pages, v_pages, page_table, prefix_len, window,
-                              n_sinks=0, block_len=None, out=None, ws=None, out_f32=False,
-                              stream=None):
+def _window_dims(q, k, block, odt):
+    B, n, Hq, d = q.shape
+    kv = (B, n, k.shape[2], d)
+    return _dims(B, Hq, kv[2], d, block, 64, _dt(q), 1, HYB_OUT_F32 if odt is not q.dtype else 0), kv
+
+
+@_placed
+def softmax_window_step_paged(dev, q, k, v, k_pages, v_pages, page_table, prefix_len, window,
+                              n_sinks=0, block_len=None, out=None, ws=None, out_f32=False):
     """softmax_prefix_step_paged over the last `window` cached tokens and the
     first n_sinks, plus the block (the first block_len[b] rows of request b;
     rows past it of out are left as they were, zero if out is made here)."""
     lib = load()
-    on = _On(q, stream)
-    with on as st:
-        B, L, Hq, d = q.shape
-        Hkv = k.shape[2]
-        act = q.dtype
-        flags, odt = _out_flags(out, act, out_f32)
-        dims = make_dims(B, Hq, Hkv, d, L, 64, _dt(q), 1, flags)
-        if out is None:
-            out = (torch.empty if block_len is None else torch.zeros)(q.shape, dtype=odt,
-                                                                      device=q.device)
-        pool = (k_pages.shape[0], k_pages.shape[1], Hkv, d)
-        max_pages = page_table.shape[1]
-        if ws is None:
-            need = workspace_bytes(dims, OP_WINDOW_STEP,
-                                   min(max_pages * pool[1], window + n_sinks + 64))
-            ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-        kv = (B, L, Hkv, d)
-        _check(lib.softmax_window_step_paged(
-            ctypes.byref(dims), on.ptr(q, "q"), on.ptr(k, "k", act, kv), on.ptr(v, "v", act, kv),
-            on.ptr(k_pages, "k_pages", act, pool), on.ptr(v_pages, "v_pages", act, pool),
-            pool[0], pool[1], on.ptr(page_table, "page_table", torch.int32, (B, max_pages)),
-            max_pages, on.ptr(prefix_len, "prefix_len", torch.int32, (B,)), window, n_sinks,
-            on.ptr(block_len, "block_len", torch.int32, (B,)), on.ptr(out, "out", odt, q.shape),
-            on.ptr(ws, "ws"), _bytes(ws), st))
+    B, L, Hq, d = q.shape
+    act, i32 = q.dtype, torch.int32
+    odt = _odt(act, out, out_f32)
+    dims, kv = _window_dims(q, k, L, odt)
+    if out is None:
+        new = torch.empty if block_len is None else torch.zeros
+        out = new(q.shape, dtype=odt, device=q.device)
+    n_pages, page_size = k_pages.shape[:2]
+    pool = (n_pages, page_size, kv[2], d)
+    max_pages = page_table.shape[1]
+    if ws is None:
+        need = lib.hybrid_workspace_bytes(dims, OP_WINDOW_STEP,
+                                          min(max_pages * page_size, window + n_sinks + 64))
+        ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    _check(lib.softmax_window_step_paged(
+        dims, _dptr(dev, q, "q", act), _dptr(dev, k, "k", act, kv), _dptr(dev, v, "v", act, kv),
+        _dptr(dev, k_pages, "k_pages", act, pool), _dptr(dev, v_pages, "v_pages", act, pool),
+        n_pages, page_size, _dptr(dev, page_table, "page_table", i32, (B, max_pages)), max_pages,
+        _dptr(dev, prefix_len, "prefix_len", i32, (B,)), window, n_sinks,
+        _dptr(dev, block_len, "block_len", i32, (B,)), _dptr(dev, out, "out", odt, q.shape),
+        _dptr(dev, ws, "ws", torch.uint8), _bytes(ws), _raw_stream(dev)))
     return out
 
 
-def softmax_window_prefill(q, k, v, block, window, n_sinks=0, seq_lens=None, out=None, lse=None,
-                           want_lse=True, ws=None, out_f32=False, stream=None):
+@_placed
+def softmax_window_prefill(dev, q, k, v, block, window, n_sinks=0, seq_lens=None, out=None,
+                           lse=None, want_lse=True, ws=None, out_f32=False):
     """Softmax of q [B][T][Hq][d] over k, v [B][T][Hkv][d], block-causal in blocks
     of `block` tokens, over the block, the `window` tokens before it and the
     first n_sinks.  seq_lens [B] int32 (device): rows past them of out and lse
     are left as they were (zero if made here).  Returns (out, lse fp32
     [B][Hq][T] or None)."""
     lib = load()
-    on = _On(q, stream)
-    with on as st:
-        B, T, Hq, d = q.shape
-        Hkv = k.shape[2]
-        act = q.dtype
-        flags, odt = _out_flags(out, act, out_f32)
-        dims = make_dims(B, Hq, Hkv, d, block, 64, _dt(q), 1, flags)
-        new = torch.empty if seq_lens is None else torch.zeros
-        if out is None:
-            out = new(q.shape, dtype=odt, device=q.device)
-        if lse is None and want_lse:
-            lse = new((B, Hq, T), dtype=torch.float32, device=q.device)
-        if ws is None:
-            need = workspace_bytes(dims, OP_WINDOW_PREFILL, T)
-            ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-        kv = (B, T, Hkv, d)
-        _check(lib.softmax_window_prefill(
-            ctypes.byref(dims), T, window, n_sinks, on.ptr(q, "q"), on.ptr(k, "k", act, kv),
-            on.ptr(v, "v", act, kv), on.ptr(seq_lens, "seq_lens", torch.int32, (B,)),
-            on.ptr(out, "out", odt, q.shape), on.ptr(lse, "lse", torch.float32, (B, Hq, T)),
-            on.ptr(ws, "ws"), _bytes(ws), st))
+    B, T, Hq, d = q.shape
+    act, f32 = q.dtype, torch.float32
+    odt = _odt(act, out, out_f32)
+    dims, kv = _window_dims(q, k, block, odt)
+    new = torch.empty if seq_lens is None else torch.zeros
+    if out is None:
+        out = new(q.shape, dtype=odt, device=q.device)
+    if lse is None and want_lse:
+        lse = new((B, Hq, T), dtype=f32, device=q.device)
+    if ws is None:
+        need = lib.hybrid_workspace_bytes(dims, OP_WINDOW_PREFILL, T)
+        ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    _check(lib.softmax_window_prefill(
+        dims, T, window, n_sinks, _dptr(dev, q, "q", act), _dptr(dev, k, "k", act, kv),
+        _dptr(dev, v, "v", act, kv), _dptr(dev, seq_lens, "seq_lens", torch.int32, (B,)),
+        _dptr(dev, out, "out", odt, q.shape), _dptr(dev, lse, "lse", f32, (B, Hq, T)),
+        _dptr(dev, ws, "ws", torch.uint8), _bytes(ws), _raw_stream(dev)))
     return out, lse
 
 
-def softmax_window_backward(q, k, v, out, lse, dout, block, window, n_sinks=0, seq_lens=None,
-                            dq=None, dk=None, dv=None, ws=None, out_f32=False, stream=None):
+@_placed
+def softmax_window_backward(dev, q, k, v, out, lse, dout, block, window, n_sinks=0, seq_lens=None,
+                            dq=None, dk=None, dv=None, ws=None, out_f32=False):
     """Gradient of softmax_window_prefill for the upstream gradient dout; out (in
     q's dtype) and lse as the forward call left them.  Returns (dq, dk, dv) in
     q's dtype (fp32 with out_f32); rows past seq_lens are zero."""
     lib = load()
-    on = _On(q, stream)
-    with on as st:
-        B, T, Hq, d = q.shape
-        Hkv = k.shape[2]
-        act = q.dtype
-        flags, odt = _out_flags(dq, act, out_f32)
-        dims = make_dims(B, Hq, Hkv, d, block, 64, _dt(q), 1, flags)
-        kv = (B, T, Hkv, d)
-        dq = torch.empty(q.shape, dtype=odt, device=q.device) if dq is None else dq
-        dk = torch.empty(kv, dtype=odt, device=q.device) if dk is None else dk
-        dv = torch.empty(kv, dtype=odt, device=q.device) if dv is None else dv
-        if ws is None:
-            need = workspace_bytes(dims, OP_WINDOW_BACKWARD, T)
-            ws = torch.empty(need, dtype=torch.uint8, device=q.device)
-        _check(lib.softmax_window_backward(
-            ctypes.byref(dims), T, window, n_sinks, on.ptr(q, "q"), on.ptr(k, "k", act, kv),
-            on.ptr(v, "v", act, kv), on.ptr(seq_lens, "seq_lens", torch.int32, (B,)),
-            on.ptr(out, "out", act, q.shape), on.ptr(lse, "lse", torch.float32, (B, Hq, T)),
-            on.ptr(dout, "dout", act, q.shape), on.ptr(dq, "dq", odt, q.shape),
-            on.ptr(dk, "dk", odt, kv), on.ptr(dv, "dv", odt, kv), on.ptr(ws, "ws"), _bytes(ws),
-            st))
+    B, T, Hq, d = q.shape
+    act, at = q.dtype, q.device
+    odt = _odt(act, dq, out_f32)
+    dims, kv = _window_dims(q, k, block, odt)
+    dq = torch.empty(q.shape, dtype=odt, device=at) if dq is None else dq
+    dk = torch.empty(kv, dtype=odt, device=at) if dk is None else dk
+    dv = torch.empty(kv, dtype=odt, device=at) if dv is None else dv
+    if ws is None:
+        need = lib.hybrid_workspace_bytes(dims, OP_WINDOW_BACKWARD, T)
+        ws = torch.empty(need, dtype=torch.uint8, device=at)
+    _check(lib.softmax_window_backward(
+        dims, T, window, n_sinks, _dptr(dev, q, "q", act), _dptr(dev, k, "k", act, kv),
+        _dptr(dev, v, "v", act, kv), _dptr(dev, seq_lens, "seq_lens", torch.int32, (B,)),
+        _dptr(dev, out, "out", act, q.shape),
+        _dptr(dev, lse, "lse", torch.float32, (B, Hq, T)),
+        _dptr(dev, dout, "dout", act, q.shape), _dptr(dev, dq, "dq", odt, q.shape),
+        _dptr(dev, dk, "dk", odt, kv), _dptr(dev, dv, "dv", odt, kv),
+        _dptr(dev, ws, "ws", torch.uint8), _bytes(ws), _raw_stream(dev)))
     return dq, dk, dv

@@ -25,7 +25,7 @@
 namespace hyb {
 
 constexpr int kPlanThreads = 256;
-constexpr int kPlanTokens = 4;  // tokens of a thread and round
+constexpr int kPlanTokens = 4;  // neighbouring tokens of a thread, found by one search
 
 // Index of the last of sums[0 .. n] (not falling, sums[0] = 0) that is <= x,
 // below n.
@@ -41,51 +41,70 @@ __device__ inline int plan_find(const int* sums, int n, int x) {
   return lo;
 }
 
+// Sums that stay at 2^31 - 1 (of terms that are not negative, so the order of
+// the additions does not matter).
+__device__ inline int plan_add(int a, int b) { return __builtin_elementwise_add_sat(a, b); }
+// Sum over the lanes up to this one, by shifts within and broadcasts between the
+// rows of 16 lanes.
+__device__ inline int plan_scan(int x) {
+  x = plan_add(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true));   // row_shr:1
+  x = plan_add(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true));
+  x = plan_add(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true));
+  x = plan_add(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true));
+  x = plan_add(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));  // row_bcast:15 into rows 1, 3
+  return plan_add(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));  // row_bcast:31 into rows 2, 3
+}
+
 __global__ __launch_bounds__(kPlanThreads) void hyb_pages_plan_kernel(PagesArgs a) {
-  extern __shared__ int sums[];  // token starts [B + 1], then page starts [B + 1]
-  __shared__ long carry[2][kPlanThreads / kWave];
-  const int B = a.B, tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+  // per request the first of its tokens and of its new pages (B + 1 entries:
+  // the totals last), then its cached tokens
+  extern __shared__ int sums[];
+  __shared__ int carry[2][kPlanThreads / kWave];
+  const int B = a.B, tid = threadIdx.x, wave = tid / kWave;
   const int page = 1 << a.page_shift;
   const long cap = (long)a.max_pages << a.page_shift;
   int* const start = sums;
   int* const first = sums + B + 1;
-  auto prefix = [&](int b) { return (int)min((long)max(a.prefix_len[b], 0), cap); };
+  int* const cached = first + B + 1;
   auto held = [&](int p) { return (int)(((long)p + page - 1) >> a.page_shift); };
-  auto saturated = [](long x) { return (int)min(x, 0x7fffffffL); };
 
-  // Running sums: a thread takes `each` neighbouring requests.
+  // Running sums: a thread takes `each` neighbouring requests (one where they fit).
   const int each = (B + kPlanThreads - 1) / kPlanThreads;
   const int b0 = min(tid * each, B), b1 = min(b0 + each, B);
-  long nt = 0, np = 0;
+  int nt = 0, np = 0;
   for (int b = b0; b < b1; ++b) {
-    const int p = prefix(b), n = max(a.new_len[b], 0);
-    nt += n;
-    np += ((min((long)p + n, cap) + page - 1) >> a.page_shift) - held(p);
+    const int p = min(max(a.prefix_len[b], 0), (int)cap), n = max(a.new_len[b], 0);
+    const int need = (int)((min((long)p + n, cap) + page - 1) >> a.page_shift) - held(p);
+    // (the thread's own sums for now)
+    cached[b] = p;
+    start[b] = nt;
+    first[b] = np;
+    nt = plan_add(nt, n);
+    np = plan_add(np, need);
   }
-  long it = nt, ip = np;  // inclusive over the wave
-  for (int o = 1; o < kWave; o <<= 1) {
-    const long x = __shfl_up(it, o), y = __shfl_up(ip, o);
-    if (lane >= o) it += x, ip += y;
-  }
-  if (lane == kWave - 1) carry[0][wave] = it, carry[1][wave] = ip;
+  const int it = plan_scan(nt), ip = plan_scan(np);
+  if (tid % kWave == kWave - 1) carry[0][wave] = it, carry[1][wave] = ip;
+  // what the lanes before hold (a saturated sum cannot be taken back by its
+  // last term)
+  int et = __builtin_amdgcn_update_dpp(0, it, 0x138, 0xf, 0xf, false);  // wave_shr:1
+  int ep = __builtin_amdgcn_update_dpp(0, ip, 0x138, 0xf, 0xf, false);
   __syncthreads();
-  long et = it - nt, ep = ip - np;
-  for (int w = 0; w < wave; ++w) et += carry[0][w], ep += carry[1][w];
-  for (int b = b0; b < b1; ++b) {
-    const int p = prefix(b), n = max(a.new_len[b], 0);
-    start[b] = saturated(et);
-    first[b] = saturated(ep);
-    et += n;
-    ep += ((min((long)p + n, cap) + page - 1) >> a.page_shift) - held(p);
+  int tokens = 0, pages = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanThreads / kWave; ++w) {
+    if (w < wave) et = plan_add(et, carry[0][w]), ep = plan_add(ep, carry[1][w]);
+    tokens = plan_add(tokens, carry[0][w]);
+    pages = plan_add(pages, carry[1][w]);
   }
-  long all_t = 0, all_p = 0;
-  for (int w = 0; w < kPlanThreads / kWave; ++w) all_t += carry[0][w], all_p += carry[1][w];
+  for (int b = b0; b < b1; ++b) {
+    start[b] = plan_add(start[b], et);
+    first[b] = plan_add(first[b], ep);
+  }
   if (tid == 0) {
-    start[B] = saturated(all_t);
-    first[B] = saturated(all_p);
+    start[B] = tokens;
+    first[B] = pages;
   }
   __syncthreads();
-  const int tokens = start[B], pages = first[B];
   if (blockIdx.x == 0) {
     for (int b = tid; b <= B; b += kPlanThreads) a.token_start[b] = start[b];
     if (tid == 0) {
@@ -96,46 +115,53 @@ __global__ __launch_bounds__(kPlanThreads) void hyb_pages_plan_kernel(PagesArgs 
   // The table's new entries.
   for (long i = (long)blockIdx.x * kPlanThreads + tid; i < pages; i += (long)gridDim.x * kPlanThreads) {
     const int b = plan_find(first, B, (int)i);
-    const int e = held(prefix(b)) + ((int)i - first[b]);
+    const int e = held(cached[b]) + ((int)i - first[b]);
     a.page_table[(size_t)b * a.max_pages + e] = i < a.n_free ? a.free_pages[i] : -1;
   }
   // The tokens' slots and positions.
-  for (long t0 = (long)blockIdx.x * kPlanThreads * kPlanTokens; t0 < a.max_tokens;
+  for (long t0 = ((long)blockIdx.x * kPlanThreads + tid) * kPlanTokens; t0 < a.max_tokens;
        t0 += (long)gridDim.x * kPlanThreads * kPlanTokens) {
+    int slot[kPlanTokens], pos[kPlanTokens];
+    int b = t0 < tokens ? plan_find(start, B, (int)t0) : B - 1;
 #pragma unroll
     for (int u = 0; u < kPlanTokens; ++u) {
-      const long t = t0 + u * kPlanThreads + tid;
-      if (t >= a.max_tokens) break;
-      long slot = -1, pos = 0;
-      if (t < tokens) {
-        const int b = plan_find(start, B, (int)t);
-        const int p = prefix(b);
-        pos = (long)p + (t - start[b]);
-        if (pos < cap) {
-          const int e = (int)(pos >> a.page_shift), h = held(p);
-          long pg;
-          if (e < h) {
-            pg = a.page_table[(size_t)b * a.max_pages + e];
-          } else {
-            const long i = (long)first[b] + (e - h);
-            pg = i < a.n_free ? a.free_pages[i] : -1;
-          }
-          slot = pg < 0 ? -1 : (pg << a.page_shift) + (pos & (page - 1));
-          if (slot > 0x7fffffffL) slot = -1;
-        }
+      const long t = t0 + u;
+      slot[u] = -1;
+      pos[u] = 0;
+      if (t >= tokens) continue;
+      while (b + 1 < B && start[b + 1] <= t) ++b;
+      const int p = cached[b];
+      const long x = (long)p + (t - start[b]);
+      pos[u] = (int)min(x, 0x7fffffffL);
+      if (x >= cap) continue;
+      const int e = (int)(x >> a.page_shift), h = held(p);
+      const long i = (long)first[b] + (e - h);
+      long pg = -1;
+      if (e < h)
+        pg = a.page_table[(size_t)b * a.max_pages + e];
+      else if (i < a.n_free)
+        pg = a.free_pages[i];
+      const long row = (pg << a.page_shift) + (x & (page - 1));
+      slot[u] = pg < 0 || row > 0x7fffffffL ? -1 : (int)row;
+    }
+    if (t0 + kPlanTokens <= a.max_tokens) {
+      *reinterpret_cast<int4*>(a.slots + t0) = int4{slot[0], slot[1], slot[2], slot[3]};
+      *reinterpret_cast<int4*>(a.positions + t0) = int4{pos[0], pos[1], pos[2], pos[3]};
+    } else {
+      for (int u = 0; u < (int)(a.max_tokens - t0); ++u) {
+        a.slots[t0 + u] = slot[u];
+        a.positions[t0 + u] = pos[u];
       }
-      a.slots[t] = (int)slot;
-      a.positions[t] = saturated(pos);
     }
   }
 }
 
 hipError_t launch_pages_plan(const PagesArgs& a, hipStream_t st) {
-  // Workgroups for the tokens; the table's entries are fewer (a page of 16
-  // rows and more), and taken by the same ones.
+  // Workgroups for the tokens; the table's entries are fewer, and taken by the
+  // same ones.
   const long per = kPlanThreads * kPlanTokens;
   const unsigned grid = (unsigned)std::min<long>(std::max<long>(1, (a.max_tokens + per - 1) / per), 2048);
-  hipLaunchKernelGGL(hyb_pages_plan_kernel, dim3(grid), dim3(kPlanThreads), 2 * (a.B + 1) * sizeof(int), st, a);
+  hipLaunchKernelGGL(hyb_pages_plan_kernel, dim3(grid), dim3(kPlanThreads), (3 * a.B + 2) * sizeof(int), st, a);
   return hipGetLastError();
 }
 

@@ -1075,8 +1075,9 @@ static hipError_t win_backward_go(const WindowArgs& a, hipStream_t st) {
 }
 
 // The cut: about two workgroups per CU (512, one at a time), each of 16 query
-// tiles or more; the sinks' keys in parts as long as the others', at most 16 of them
-// all together.
+// tiles or more; the sinks' keys in parts as long as the others', as long as those
+// are at most 16 per (request, KV head) and 512 in all.
+static int win_sink_parts(const Shape& s) { return (int)std::min<long>(16, 512 / std::max<long>(1, (long)s.B * s.Hkv)); }
 static WinParts win_cut(const Shape& s, int T, int window, int n_sinks) {
   const int wk = 4 * kTile, G = s.Hq / s.Hkv;
   WinParts c;
@@ -1088,23 +1089,28 @@ static WinParts win_cut(const Shape& s, int T, int window, int n_sinks) {
   const long each = (seen + c.p - 1) / c.p;
   c.ps = c.p;
   if (c.ns > 0 && every >= 2 * each)
-    c.ps = (int)std::max<long>(c.p, std::min<long>((every + each - 1) / each, 16 / c.ns));
+    c.ps = (int)std::max<long>(c.p, std::min<long>((every + each - 1) / each, win_sink_parts(s) / c.ns));
   return c;
 }
 static size_t win_stats_bytes(const Shape& s, int T) { return (size_t)s.B * s.Hq * win_tp(T) * 32; }
-// Partial sums at most, for any window and number of sinks (whose workgroups
-// times parts are 16, or every workgroup p times).
+// Partial sums at most, for any window and number of sinks: p is largest for a
+// full window; the sinks' workgroups times their parts are within
+// win_sink_parts, or have p parts as every workgroup (one workgroup's keys see
+// one list, with or without sinks).
 static size_t win_sums_bytes(const Shape& s, int T) {
   const WinParts c = win_cut(s, T, T, 0);
-  const long sinks = c.wgs > 1 ? 16 : std::min(16, (T + kTile - 1) / kTile * (s.Hq / s.Hkv));
-  const long most = std::max((long)c.wgs * c.p, sinks);
-  return (size_t)(most * 4 * kTile + (c.p > 1 ? (long)c.p * T : 0)) * 2 * s.B * s.Hkv * s.D * sizeof(float);
+  const long sinks = c.wgs > 1 && win_sink_parts(s) > 1 ? win_sink_parts(s) : 0;
+  const long tiles = c.p > 1 ? std::max((long)c.wgs * c.p, sinks) : sinks;
+  return (size_t)(tiles * 4 * kTile + (c.p > 1 ? (long)c.p * T : 0)) * 2 * s.B * s.Hkv * s.D * sizeof(float);
 }
 
 template <int D>
 static hipError_t win_backward_ring_go(WindowArgs a, hipStream_t st) {
   const WinParts cut = win_cut(a.s, a.T, a.window, a.n_sinks);
   a.sums = (float*)((char*)a.ws + win_stats_bytes(a.s, a.T));
+  // (what the workspace was sized for, whatever window and n_sinks are)
+  if ((size_t)cut.rows(a.T) * 2 * a.s.B * a.s.Hkv * D * sizeof(float) > win_sums_bytes(a.s, a.T))
+    return hipErrorInvalidValue;
   const int wgs = win_wgs(a);
   hipLaunchKernelGGL(hyb_win_dq_ring_kernel<D>, dim3((unsigned)(a.s.B * a.s.Hkv * wgs)), dim3(kWave * kWinWaves), 0, st,
                      a, wgs);

@@ -190,7 +190,7 @@ def prefill(d=None, T=100, window=64, sinks=4):
 
 def backward(d=None, T=100, window=64, sinks=4):
     # q k v seq_lens out lse dout dq dk dv ws
-    return Call("softmax_window_backward", [d or dims(), T, window, sinks] + [A(i) for i in range(11)] + [1 << 24, None],
+    return Call("softmax_window_backward", [d or dims(), T, window, sinks] + [A(i) for i in range(11)] + [1 << 30, None],
                 range(4, 14), (7,))
 
 
