@@ -381,7 +381,7 @@ int softmax_prefix_impl(const hyb_dims_t* dims, const void* q, const void* k,
   const int max_seen =
       win ? (int)std::min<long long>(max_prefix, (long long)window + n_sinks + 64) : max_prefix;
   const size_t need =
-      hybrid_workspace_bytes(dims, HYB_OP_SOFTMAX_PREFIX, max_seen);
+      hybrid_workspace_bytes(dims, win ? HYB_OP_WINDOW_STEP : HYB_OP_SOFTMAX_PREFIX, max_seen);
   if (need > 0 && (!ws || ws_bytes < need))
     return fail(HYB_EWORKSPACE, "%s needs %zu workspace bytes, got %zu", name,
                 need, ws ? ws_bytes : (size_t)0);
@@ -410,7 +410,8 @@ int softmax_prefix_impl(const hyb_dims_t* dims, const void* q, const void* k,
     return fail(HYB_EINVAL, "the workspace overlaps an input");
   hyb::SoftmaxPrefixArgs a{s,         q,   k,  v,
                            k_cache,   v_cache, prefix_len, max_prefix,
-                           out,       ws,  hyb::softmax_prefix_splits(s, max_seen),
+                           out,       ws,
+                           win ? hyb::softmax_window_splits(s, max_seen) : hyb::softmax_prefix_splits(s, max_seen),
                            paged && max_prefix > 0 ? page_table : nullptr,
                            page_shift, max_pages, n_pages, max_seen,
                            window,    n_sinks, block_len};
@@ -948,8 +949,9 @@ size_t hybrid_workspace_bytes(const hyb_dims_t* dims, int32_t op,
     case HYB_OP_PREFILL:
       if (extent == 0 || extent % s.L != 0) return 0;
       return hyb::prefill_ws_bytes(s, extent);
-    case HYB_OP_SOFTMAX_PREFIX:
     case HYB_OP_WINDOW_STEP:
+      return hyb::softmax_prefix_ws_bytes(s, hyb::softmax_window_splits(s, extent));
+    case HYB_OP_SOFTMAX_PREFIX:
       return hyb::softmax_prefix_ws_bytes(
           s, hyb::softmax_prefix_splits(s, extent));
     case HYB_OP_BACKWARD:

@@ -427,6 +427,51 @@ __device__ inline void buf_to_lds16(__amdgpu_buffer_rsrc_t r, void* lds, int vof
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)lds, 16, voff, soff, 0, 0);
 }
 
+// The wait states between a 32x32 product and a read of its result, for
+// places where a branch stands between the two: the compiler (ROCm 7.2) counts
+// them along one path only, and a read six states after a bf16 product (which
+// needs 11) found its last registers from before the product.
+template <typename T>
+__device__ inline void mma_settle() {
+  __builtin_amdgcn_sched_barrier(0);
+  if constexpr (sizeof(T) == 2)
+    asm volatile("s_nop 10");
+  else
+    asm volatile("s_nop 15\n\ts_nop 1");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// A tile of 32 rows of D bf16 entries in LDS, put there by 16-byte copies, that
+// is read by rows and, by transposing reads, by columns.
+template <int D>
+struct RowColTile {
+  static constexpr int EPC = 8, CPR = D / EPC;
+  static constexpr int RPI = kWave / CPR, IK = kTile / RPI;
+  static constexpr int kBytes = kTile * D * 2;
+  // Chunk c of row t sits at c ^ swz(t): the 16 rows that fill the banks have
+  // 16 places for one chunk (row reads), and four rows from a multiple of four on
+  // fall in different groups of four chunks (transposing reads).
+  __device__ static constexpr int swz(int t) {
+    return D == 128 ? ((t & 3) << 2) | ((t >> 2) & 3) : ((t & 2) << 1) | ((t >> 2) & 3);
+  }
+  int row, col;  // byte offsets of this lane's row and column operands
+  __device__ inline explicit RowColTile(int lane) {
+    const int li = lane & 31, hh = lane >> 5, qi = lane & 15, b = (lane >> 4) & 1;
+    row = li * 2 * D + 16 * (hh ^ swz(li));
+    const int r = 4 * hh + qi / 4;
+    col = r * 2 * D + 16 * ((2 * b + (qi & 3) / 2) ^ swz(r)) + 8 * (qi & 1);
+  }
+  // entries 16 ks + 8 hh .. + 7 of row li
+  __device__ inline bf16x8 row_op(const bf16* t, int ks) const {
+    return *reinterpret_cast<const bf16x8*>(reinterpret_cast<const char*>(t) + (row ^ (32 * ks)));
+  }
+  // column 32 ct + li at the rows row_of(8 ks + e, hh)
+  __device__ inline bf16x8 col_op(const bf16* t, int ct, int ks) const {
+    const char* p = reinterpret_cast<const char*>(t) + 16 * ks * 2 * D;
+    return lds_tr_op(p + (col ^ (64 * ct)), p + (col ^ (64 * ct) ^ 32) + 8 * 2 * D);
+  }
+};
+
 // Workgroup barrier that orders LDS accesses only.  __syncthreads() carries a
 // workgroup fence over every address space, which makes each wave wait for
 // all of its outstanding global loads before the barrier; restricting the

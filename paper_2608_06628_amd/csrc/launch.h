@@ -204,5 +204,6 @@ size_t backward_ws_bytes(const Shape& s, int T, bool inputs = false);
 // Workspace of softmax_prefix_step for n_split splits.
 size_t softmax_prefix_ws_bytes(const Shape& s, int n_split);
 int softmax_prefix_splits(const Shape& s, int max_prefix);
+int softmax_window_splits(const Shape& s, int max_seen);
 
 }  // namespace hyb

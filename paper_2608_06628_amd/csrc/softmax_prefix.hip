@@ -509,6 +509,7 @@ __global__ __launch_bounds__(kWave* NG) void hyb_sp_partial_kernel(
 #pragma unroll
     for (int ks = 0; ks < C::KD; ++ks)
       sc = M::mma(load_op<T>(&sh.k[buf][li][ks * KW + hh * E]), qop[ks], sc);
+    if constexpr (WIN) mma_settle<T>();
     // Scaled scores; keys past the range only in the range's last tile
     // (a wave-uniform test, so full tiles carry no masks).
     const bool full = j0 + kTile <= hi && !(WIN && seen.cuts(j0));
@@ -554,6 +555,7 @@ __global__ __launch_bounds__(kWave* NG) void hyb_sp_partial_kernel(
 #pragma unroll
       for (int ks = 0; ks < C::KL; ++ks)
         acc[ct] = M::mma(vt_op(buf, ct, ks), cvt_op<T>(&p[ks * E]), acc[ct]);
+    if constexpr (WIN) mma_settle<T>();
     if (after(j0, n, 1) < hi) put(nx, buf ^ 1);  // next tile into the free buffer
     nx = af;
     __syncthreads();
@@ -834,6 +836,7 @@ __global__ __launch_bounds__(kWave* NG, D == 64 && NG == 8 ? 4 : 2) void hyb_sp_
   auto take_scores = [&](auto check, int n, const f32x16& s) __attribute__((always_inline)) {
     sc = s;
     if constexpr (decltype(check)::value || WIN) {
+      if constexpr (WIN) mma_settle<bf16>();
       const int j0 = first_key(n);
       if (j0 + kTile > hi || (WIN && seen.cuts(j0))) {  // uniform
 #pragma unroll
@@ -849,6 +852,7 @@ __global__ __launch_bounds__(kWave* NG, D == 64 && NG == 8 ? 4 : 2) void hyb_sp_
     mt = fmaxf(mt, xor32(mt));
     float mn;
     if (rf.take(mt * scale, SpRef::restarts<1>(n), mn)) {
+      if constexpr (WIN) mma_settle<bf16>();
       const float corr = __builtin_amdgcn_exp2f(m - mn);
       lsum[0] *= corr;
 #pragma unroll
@@ -984,6 +988,7 @@ __global__ __launch_bounds__(kWave* NG, D == 64 && NG == 8 ? 4 : 2) void hyb_sp_
   lds_barrier_nodrain();
   const int rest = ntiles - n;  // 1 .. R
   compute(yes, ntiles - 1, nullptr, rest == 2 ? s1.v : rest == 3 ? s2.v : rest == 4 ? s3.v : s0.v);
+  if constexpr (WIN) mma_settle<bf16>();
 
   if (li >= Lb) return;
   const float l = lsum[0];
@@ -1013,6 +1018,227 @@ __global__ __launch_bounds__(kWave* NG, D == 64 && NG == 8 ? 4 : 2) void hyb_sp_
   if (hh == 0) {
     wml[0] = m * 0.6931471805599453f;  // back to the natural log
     wml[1] = l;
+  }
+}
+
+// A window's few queries (bf16, the G heads' L queries within 32: decoding):
+// they are the columns of one tile of scores, so a wave answers all of them
+// and the four waves of a workgroup take the range's tiles in turn, each with
+// copies of its own (two slots of K and V, no barrier in the loop) and sums of its
+// own, joined in LDS at the end.  With a wave per head, as above, each has one or
+// a few columns of its tile filled, and the loop is four times as many dependent
+// steps.
+template <int D>
+__global__ __launch_bounds__(kWave * 4) void hyb_sp_token_kernel(SoftmaxPrefixArgs a, SpCut cut) {
+  typedef Mma<bf16> M;
+  typedef M::op_t op_t;
+  typedef RowColTile<D> RT;
+  constexpr int E = M::E, KW = M::KW, KD = D / KW, KL = kTile / KW, NCT = D / kTile, NW = 4;
+  struct alignas(16) Slot {
+    bf16 k[kTile * D], v[kTile * D];
+  };
+  __shared__ Slot ring[NW][2];
+  __shared__ float refs[NW][kTile], sums[NW][kTile];
+  __shared__ int pages[kMaxRangePages];
+
+  const int tid = threadIdx.x, lane = tid & (kWave - 1);
+  const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int li = lane & 31, hh = lane >> 5;
+  const int Hq = a.s.Hq, Hkv = a.s.Hkv, L = a.s.L, G = Hq / Hkv;
+  const int g = blockIdx.x % Hkv, r = blockIdx.x / Hkv;
+  static_assert(sizeof(ring) >= kPlanInts * sizeof(int), "the plan's scratch fits the slots");
+  const SpRange rg = sp_range<true>(a, sp_plan<true>(a, cut, reinterpret_cast<int*>(&ring)), r, lane);
+  if (rg.b < 0) return;  // uniform: past the plan's last range
+  const int b = rg.b, lo = rg.lo, hi = rg.hi;
+  const int Lb = sp_block<true>(a, b), P = sp_keys<true>(a, b) - Lb;
+  const SpSeen seen = sp_seen<true>(a, b);
+  const size_t kstride = (size_t)Hkv * D;
+  // this lane's column: query i of head h
+  const int i = li % L, h = g * G + li / L;
+  const bool col = li < G * L && i < Lb;
+  op_t qop[KD];
+  {
+    const bf16* row = (const bf16*)a.q + (((size_t)b * L + (col ? i : 0)) * Hq + (col ? h : g * G)) * D + hh * E;
+#pragma unroll
+    for (int ks = 0; ks < KD; ++ks) qop[ks] = keep_if<bf16>(col, load_op<bf16>(row + ks * KW));
+  }
+  const bf16* kc = (const bf16*)a.k_cache + g * D;
+  const bf16* vc = (const bf16*)a.v_cache + g * D;
+  const bf16* kb = (const bf16*)a.k + ((size_t)b * L * Hkv + g) * D;
+  const bf16* vb = (const bf16*)a.v + ((size_t)b * L * Hkv + g) * D;
+  // The pages of the range's cached keys, as in the ring kernel.
+  const int p0 = lo >> a.page_shift;
+  int pa = 0x7fffffff, pskip = 0;
+  if (seen.skip > 0 && rg.t0 < seen.st && rg.t0 + rg.nt > seen.st) {
+    pa = (seen.st * kTile - 1) >> a.page_shift;
+    pskip = max(0, ((seen.st + seen.skip) * kTile >> a.page_shift) - pa - 1);
+  }
+  {
+    const int32_t* ptab = a.page_table + (size_t)b * a.max_pages;
+    const int chi = min(hi, P);
+    const int np = chi > lo ? ((chi - 1) >> a.page_shift) - p0 + 1 - pskip : 0;
+    for (int e = tid; e < np; e += kWave * NW)
+      pages[e] = sp_page(a, ptab, (p0 + e + (p0 + e > pa ? pskip : 0)) << a.page_shift);
+    __syncthreads();
+  }
+
+  const RT rt(lane);
+  int trow[RT::IK], tcol[RT::IK];
+#pragma unroll
+  for (int u = 0; u < RT::IK; ++u) {
+    trow[u] = u * RT::RPI + lane / RT::CPR;
+    tcol[u] = (lane % RT::CPR ^ RT::swz(trow[u])) * RT::EPC;
+  }
+  const int mine = (rg.nt - w + NW - 1) / NW;  // this wave's tiles
+  auto first_key = [&](int n) __attribute__((always_inline)) { return seen.tile(rg.t0 + w + NW * n) * kTile; };
+  auto issue = [&](int n, Slot& s) __attribute__((always_inline)) {
+    if (n >= mine) return;
+    const int j0 = first_key(n);
+    ptrdiff_t shift = 0;  // from a row's place in its request to its place in the pools
+    if (j0 < P) {
+      const int pi = j0 >> a.page_shift;
+      shift = ((ptrdiff_t)__builtin_amdgcn_readfirstlane(pages[pi - p0 - (pi > pa ? pskip : 0)]) - pi) << a.page_shift;
+    }
+    if (j0 + kTile <= min(hi, P) && !seen.cuts(j0)) {
+      const ptrdiff_t at = (shift + j0) * (ptrdiff_t)kstride;
+      const int span = (int)(kTile * kstride * sizeof(bf16));
+      const __amdgpu_buffer_rsrc_t rk =
+          __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(kc + at), 0, span, kBufferWord3);
+      const __amdgpu_buffer_rsrc_t rv =
+          __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(vc + at), 0, span, kBufferWord3);
+#pragma unroll
+      for (int u = 0; u < RT::IK; ++u)
+        buf_to_lds16(rk, s.k + u * RT::RPI * D, (int)((trow[u] * (int)kstride + tcol[u]) * sizeof(bf16)), 0);
+#pragma unroll
+      for (int u = 0; u < RT::IK; ++u)
+        buf_to_lds16(rv, s.v + u * RT::RPI * D, (int)((trow[u] * (int)kstride + tcol[u]) * sizeof(bf16)), 0);
+    } else {
+      // keys past the range and hidden ones read a visible row of the tile
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+        for (int u = 0; u < RT::IK; ++u) {
+          int j = min(j0 + trow[u], hi - 1);
+          j = seen.hides(j) ? seen.stand_in(j0) : j;
+          const bf16* base = sp_pick(j < P, kv == 0 ? kc : vc, kv == 0 ? kb : vb);
+          const bf16* row = base + (ptrdiff_t)(j < P ? shift + j : j - P) * (ptrdiff_t)kstride + tcol[u];
+          __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)row,
+                                           (__attribute__((address_space(3))) void*)((kv == 0 ? s.k : s.v) + u * RT::RPI * D),
+                                           16, 0, 0);
+        }
+    }
+  };
+  // The weights' reference, in the log2 domain; finite, so that a wave without
+  // tiles weighs nothing.
+  const float scale = kLog2e / sqrtf((float)D);
+  float m = -1e30f, l = 0.0f;
+  f32x16 acc[NCT];
+#pragma unroll
+  for (int ct = 0; ct < NCT; ++ct) acc[ct] = f32x16{};
+  auto compute = [&](int n, const Slot& s) __attribute__((always_inline)) {
+    f32x16 sc = {};
+#pragma unroll
+    for (int ks = 0; ks < KD; ++ks) sc = M::mma(rt.row_op(s.k, ks), qop[ks], sc);
+    mma_settle<bf16>();
+    const int j0 = first_key(n);
+    if (j0 + kTile > hi || seen.cuts(j0)) {  // uniform
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int j = j0 + row_of(e, hh);
+        sc[e] = j < hi && !seen.hides(j) ? sc[e] : -INFINITY;
+      }
+    }
+    float mt = sc[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) mt = fmaxf(mt, sc[e]);
+    mt = fmaxf(mt, xor32(mt)) * scale;
+    // (the reference moves only when a maximum passes it by 2^8)
+    if (__any(mt > m + 8.0f)) {
+      mma_settle<bf16>();
+      const float mn = mt > m + 8.0f ? mt : m;
+      const float corr = __builtin_amdgcn_exp2f(m - mn);
+      l *= corr;
+#pragma unroll
+      for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[ct][e] *= corr;
+      m = mn;
+    }
+    float p[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale, -m));
+      l += p[e];
+    }
+    op_t pop[KL];
+#pragma unroll
+    for (int ks = 0; ks < KL; ++ks) pop[ks] = cvt_op<bf16>(&p[ks * E]);
+#pragma unroll
+    for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+      for (int ks = 0; ks < KL; ++ks) acc[ct] = M::mma(rt.col_op(s.v, ct, ks), pop[ks], acc[ct]);
+  };
+  auto step = [&](int n, Slot& s) __attribute__((always_inline)) {
+    if (n + 1 < mine) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * RT::IK) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    compute(n, s);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot is read
+    issue(n + 2, s);
+  };
+  issue(0, ring[w][0]);
+  issue(1, ring[w][1]);
+  for (int n = 0; n < mine; n += 2) {
+    step(n, ring[w][0]);
+    if (n + 1 < mine) step(n + 1, ring[w][1]);
+  }
+
+  // The waves' sums over one reference: wave w scales its own and leaves them in
+  // its slots, then joins the columns 32 ct .. + 31 of the heads' entries for
+  // ct = w (and w + 4 ..: D is at most 4 such groups).
+  l += xor32(l);
+  if (hh == 0) refs[w][li] = m;
+  lds_barrier();
+  float mm = refs[0][li];
+#pragma unroll
+  for (int x = 1; x < NW; ++x) mm = fmaxf(mm, refs[x][li]);
+  const float f = __builtin_amdgcn_exp2f(m - mm);
+  if (hh == 0) sums[w][li] = l * f;
+  f32x4* const parts = reinterpret_cast<f32x4*>(&ring);  // [wave][ct * 4 + e][lane]
+  static_assert(sizeof(Slot) * 2 >= NCT * 4 * kWave * sizeof(f32x4), "a wave's sums fit its slots");
+#pragma unroll
+  for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      parts[(w * NCT * 4 + ct * 4 + e) * kWave + lane] =
+          f32x4{acc[ct][4 * e] * f, acc[ct][4 * e + 1] * f, acc[ct][4 * e + 2] * f, acc[ct][4 * e + 3] * f};
+  lds_barrier();
+  if (w >= NCT || !col) return;
+  float den = 0.0f;
+#pragma unroll
+  for (int x = 0; x < NW; ++x) den += sums[x][li];
+  const bool whole = rg.n == 1;
+  const float inv = whole ? 1.0f / den : 1.0f;
+  const size_t row = sp_row(a, r, h, i);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    f32x4 o = {};
+#pragma unroll
+    for (int x = 0; x < NW; ++x) {
+      const f32x4 y = parts[(x * NCT * 4 + w * 4 + e) * kWave + lane];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[k] += y[k];
+    }
+    const float v[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+    const size_t at = w * kTile + row_of(4 * e, hh);
+    if (whole)
+      store_out4<bf16>(a.out, (((size_t)b * L + i) * Hq + h) * D + at, v, a.s.out_f32);
+    else
+      *reinterpret_cast<f32x4*>((float*)a.ws + row * D + at) = f32x4{v[0], v[1], v[2], v[3]};
+  }
+  if (!whole && w == 0 && hh == 0) {
+    float* wml = sp_ml<D>(a) + row * 2;
+    wml[0] = mm * 0.6931471805599453f;  // back to the natural log
+    wml[1] = den;
   }
 }
 
@@ -1104,6 +1330,15 @@ int softmax_prefix_splits(const Shape& s, int max_prefix) {
   return (int)want;
 }
 
+// Of a window.  Few queries take the token kernel (sp_tokens): one workgroup per
+// (request, KV head) fills the chip from 256 on, and then a merge costs more than an
+// even cut saves.
+static bool sp_tokens(const Shape& s) { return s.dtype == 1 && s.Hq / s.Hkv * s.L <= kTile; }
+int softmax_window_splits(const Shape& s, int max_seen) {
+  if (sp_tokens(s) && (long)s.B * s.Hkv >= 256 && max_seen + s.L <= kMaxRange) return 1;
+  return softmax_prefix_splits(s, max_seen);
+}
+
 // A single KV range per (request, KV head) writes the normalised output
 // directly and needs no workspace.
 size_t softmax_prefix_ws_bytes(const Shape& s, int n_split) {
@@ -1174,7 +1409,10 @@ static hipError_t sp_go(const SoftmaxPrefixArgs& a, hipStream_t st) {
   }
   // bf16 with 1, 2, 4 or 8 query heads per KV head: the copy ring; else the
   // register-staged kernel.
-  if constexpr (sizeof(T) == 2) {
+  if (WIN && sp_tokens(a.s)) {
+    static const int resident = sp_resident(hyb_sp_token_kernel<D>, 4);
+    e = sp_launch(hyb_sp_token_kernel<D>, resident, 4, true, a, st, &cut);
+  } else if constexpr (sizeof(T) == 2) {
     switch (a.s.Hq / a.s.Hkv) {
       HYB_SP_CASE(1, true, hyb_sp_ring_kernel<D, 1)
       HYB_SP_CASE(2, true, hyb_sp_ring_kernel<D, 2)

@@ -596,35 +596,7 @@ __global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_ring_kernel(Windo
 // Two kernels: dQ with delta and the rows' statistics (a wave owns 32 queries and
 // loops over key tiles), then dK with dV (a wave owns 32 keys and loops over the
 // query tiles of its KV head's heads).  Tiles come through rings as in the forward;
-// here a tile is read both by rows and, by transposing reads, by columns.
-template <int D>
-struct WinTile {
-  static constexpr int EPC = 8, CPR = D / EPC;
-  static constexpr int RPI = kWave / CPR, IK = kTile / RPI;
-  static constexpr int kBytes = kTile * D * 2;
-  // Chunk c of row t sits at c ^ swz(t): the 16 rows that fill the banks have
-  // 16 places for one chunk (row reads), and four rows from a multiple of four on
-  // fall in different groups of four chunks (transposing reads).
-  __device__ static constexpr int swz(int t) {
-    return D == 128 ? ((t & 3) << 2) | ((t >> 2) & 3) : ((t & 2) << 1) | ((t >> 2) & 3);
-  }
-  int row, col;  // byte offsets of this lane's row and column operands
-  __device__ inline explicit WinTile(int lane) {
-    const int li = lane & 31, hh = lane >> 5, qi = lane & 15, b = (lane >> 4) & 1;
-    row = li * 2 * D + 16 * (hh ^ swz(li));
-    const int r = 4 * hh + qi / 4;
-    col = r * 2 * D + 16 * ((2 * b + (qi & 3) / 2) ^ swz(r)) + 8 * (qi & 1);
-  }
-  // entries 16 ks + 8 hh .. + 7 of row li
-  __device__ inline bf16x8 row_op(const bf16* t, int ks) const {
-    return *reinterpret_cast<const bf16x8*>(reinterpret_cast<const char*>(t) + (row ^ (32 * ks)));
-  }
-  // column 32 ct + li at the rows row_of(8 ks + e, hh)
-  __device__ inline bf16x8 col_op(const bf16* t, int ct, int ks) const {
-    const char* p = reinterpret_cast<const char*>(t) + 16 * ks * 2 * D;
-    return lds_tr_op(p + (col ^ (64 * ct)), p + (col ^ (64 * ct) ^ 32) + 8 * 2 * D);
-  }
-};
+// here a tile is read both by rows and by columns (RowColTile).
 
 // The keys' side of WinRow: key j is seen by the queries q0 .. q1 - 1.
 struct WinKey {
@@ -654,7 +626,7 @@ template <int D>
 __global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_dq_ring_kernel(WindowArgs a, int wgs) {
   typedef Mma<bf16> M;
   typedef M::op_t op_t;
-  typedef WinTile<D> WT;
+  typedef RowColTile<D> WT;
   constexpr int E = M::E, KW = M::KW, KD = D / KW, KL = kTile / KW, NCT = D / kTile, R = 4;
   constexpr int IPW = 2 * WT::IK / kWinWaves;  // copies per wave and step: waves 0, 1 K's, waves 2, 3 V's
   __shared__ alignas(16) bf16 kr[R][kTile * D], vr[R][kTile * D];
@@ -827,7 +799,7 @@ template <int D>
 __global__ __launch_bounds__(kWave* kWinKeyWaves, 2) void hyb_win_dkv_ring_kernel(WindowArgs a, WinParts cut) {
   typedef Mma<bf16> M;
   typedef M::op_t op_t;
-  typedef WinTile<D> WT;
+  typedef RowColTile<D> WT;
   constexpr int E = M::E, KW = M::KW, KD = D / KW, KL = kTile / KW, NCT = D / kTile, R = 3;
   constexpr int IPQ = 2 * WT::IK / 4;  // a half's copies per wave and step: two waves Q's, two dO's
   constexpr int IPW = IPQ + 1;         // and a quarter of the statistics each
