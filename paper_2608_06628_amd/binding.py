@@ -456,6 +456,10 @@ def _rows(dev, t, name, dtype, shape):
     raise ValueError(f"{name}: the heads of a token must be contiguous")
 
 
+def _new(t, shape, dtype):
+    return t.new_empty(shape) if dtype is t.dtype else t.new_empty(shape, dtype=dtype)
+
+
 def _bytes(t):
     return t.numel() * t.element_size() if t is not None else 0
 
@@ -502,9 +506,9 @@ def hybrid_qk_norm_rope(dev, q, k, inv_freq, positions, wq=None, wk=None, eps=1e
     or "interleaved".  Returns (q_out, k_out)."""
     odt = _odt(q.dtype, q_out, out_f32)
     if q_out is None:
-        q_out = torch.empty(q.shape, dtype=odt, device=q.device)
+        q_out = _new(q, q.shape, odt)
     if k_out is None:
-        k_out = torch.empty(k.shape, dtype=odt, device=q.device)
+        k_out = _new(q, k.shape, odt)
     dims, pq, pk, _, oq, ok, pwq, pwk, pos, freq = _rope_args(
         dev, q, k, wq, wk, inv_freq, positions, eps, rot_scale, layout, q_out, k_out, odt)
     _check(load().hybrid_qk_norm_rope(dims, pq, pk, pwq, pwk, pos, freq, oq, ok, _raw_stream(dev)))
@@ -520,9 +524,9 @@ def hybrid_qk_norm_rope_paged(dev, q, k, v, inv_freq, positions, slots, k_pages,
     Returns (q_out, k_out), k_out None unless given or asked for with want_k."""
     odt = _odt(q.dtype, q_out, out_f32)
     if q_out is None:
-        q_out = torch.empty(q.shape, dtype=odt, device=q.device)
+        q_out = _new(q, q.shape, odt)
     if k_out is None and want_k:
-        k_out = torch.empty(k.shape, dtype=odt, device=q.device)
+        k_out = _new(q, k.shape, odt)
     dims, pq, pk, pv, oq, ok, pwq, pwk, pos, freq = _rope_args(
         dev, q, k, wq, wk, inv_freq, positions, eps, rot_scale, layout, q_out, k_out, odt, v=v)
     n_pages, page_size = k_pages.shape[:2]
@@ -546,9 +550,9 @@ def hybrid_qk_norm_rope_backward(dev, q, k, dq_out, dk_out, inv_freq, positions,
     odt = _odt(q.dtype, dq, out_f32)
     at, f32, d = q.device, torch.float32, q.shape[2]
     if dq is None:
-        dq = torch.empty(q.shape, dtype=odt, device=at)
+        dq = _new(q, q.shape, odt)
     if dk is None:
-        dk = torch.empty(k.shape, dtype=odt, device=at)
+        dk = _new(q, k.shape, odt)
     dwq = torch.empty(d, dtype=f32, device=at) if wq is not None else None
     dwk = torch.empty(d, dtype=f32, device=at) if wk is not None else None
     dims, pq, pk, _, oq, ok, pwq, pwk, pos, freq = _rope_args(
@@ -575,11 +579,11 @@ def kv_pages_plan(dev, prefix_len, new_len, page_table, free_pages, page_size, m
     if B == 0:
         return (torch.full((max_tokens,), -1, dtype=i32, device=at),
                 *(torch.zeros(n, dtype=i32, device=at) for n in (max_tokens, 1, 2)))
-    slots, positions, start, counts = (torch.empty(n, dtype=i32, device=at)
-                                       for n in (max_tokens, max_tokens, B + 1, 2))
+    lens = _dptr(dev, prefix_len, "prefix_len", i32, (B,))
+    slots, positions, start, counts = map(prefix_len.new_empty, (max_tokens, max_tokens, B + 1, 2))
     _check(load().kv_pages_plan(
         B, max_pages, page_size, free_pages.numel() if free_pages is not None else 0, max_tokens,
-        _dptr(dev, prefix_len, "prefix_len", i32, (B,)), _dptr(dev, new_len, "new_len", i32, (B,)),
+        lens, _dptr(dev, new_len, "new_len", i32, (B,)),
         _dptr(dev, free_pages, "free_pages", i32), _dptr(dev, page_table, "page_table", i32),
         slots.data_ptr(), positions.data_ptr(), start.data_ptr(), counts.data_ptr(),
         _raw_stream(dev)))
@@ -663,9 +667,9 @@ def softmax_window_backward(dev, q, k, v, out, lse, dout, block, window, n_sinks
     act, at = q.dtype, q.device
     odt = _odt(act, dq, out_f32)
     dims, kv = _window_dims(q, k, block, odt)
-    dq = torch.empty(q.shape, dtype=odt, device=at) if dq is None else dq
-    dk = torch.empty(kv, dtype=odt, device=at) if dk is None else dk
-    dv = torch.empty(kv, dtype=odt, device=at) if dv is None else dv
+    dq = _new(q, q.shape, odt) if dq is None else dq
+    dk = _new(q, kv, odt) if dk is None else dk
+    dv = _new(q, kv, odt) if dv is None else dv
     if ws is None:
         need = lib.hybrid_workspace_bytes(dims, OP_WINDOW_BACKWARD, T)
         ws = torch.empty(need, dtype=torch.uint8, device=at)

@@ -69,81 +69,120 @@ __device__ inline bool win_none(const WinRow& r0, const WinRow& r1, int sinks, i
   return j0 >= r1.end || (j0 + n <= r0.lo && j0 >= sinks);
 }
 
-// ---- plain kernels (fp32) ---------------------------------------------------
+// The keys' side of WinRow: key j is seen by the queries q0 .. q1 - 1.
+struct WinKey {
+  int q0, q1;
+  __device__ inline WinKey(const WindowArgs& a, int len, int j) {
+    const int L = a.s.L;
+    q0 = j / L * L;
+    const long end = ((long)j + a.window) / L * L + L;
+    q1 = j < a.n_sinks ? len : (int)min(end, (long)len);
+  }
+};
+
+// The workgroups' order: the x-th workgroups of all (request, KV head)s one after
+// the other, so that with the longest first the chip ends with short ones; a
+// (request, KV head) stays on one XCD where their number is a multiple of 8
+// (workgroups go to the XCDs in turn), which keeps what it reads in that XCD's L2.
+// (One (request, KV head) after the other left the last one's long workgroups
+// to the end: gradient of 8 x 2048 tokens 618 us, now 503.)
+__device__ inline void win_place(int bid, int nbg, int& bg, int& x) {
+  bg = bid % nbg;
+  x = bid / nbg;
+}
+
+// ---- fp32 kernels -------------------------------------------------------------
 //
 // One wave per 32 rows (queries of a head; keys of a KV head in the dK, dV
-// kernel), four waves per workgroup sharing the tiles they loop over through
-// LDS.  fp32 products run at 1/16 of the bf16 rate, so the loop waits for its
-// MFMAs whatever the staging does.
+// kernel), four waves per workgroup sharing the pairs of tiles they loop over
+// through LDS: the next pair is in registers on its way from memory while this
+// one is used, and moves to the other buffer at the end of the step, so a step has
+// one barrier.  fp32 products run at 1/16 of the bf16 rate and bound the loop (a
+// pair of tiles at d = 64 is 128 products of 64 cycles for the four waves' SIMDs).
 
 constexpr int kWinWaves = 4;
 
-template <typename T, int D>
-struct WinCfg {
-  typedef Mma<T> M;
-  static constexpr int KD = D / M::KW, KL = kTile / M::KW, NCT = D / kTile;
-  static constexpr int EPC = 16 / (int)sizeof(T), CPR = D / EPC;
-  static constexpr int LD = D + 2 * EPC;  // row pitch in LDS
-  typedef T Tile[kTile][LD];
-  typedef typename M::op_t Ops[KD];
+template <int D>
+struct WinF32 {
+  typedef Mma<float> M;
+  static constexpr int KD = D / M::KW, NCT = D / kTile;
+  static constexpr int LD = D + 4;             // row pitch in LDS
+  static constexpr int NCH = kTile * D / 4 / (kWave * kWinWaves);  // 16-byte pieces of a tile per thread
+  typedef float Tile[kTile][LD];
+  typedef float Ops[KD];
   typedef f32x16 Acc[NCT];
+  struct Regs {
+    float4 a[NCH], b[NCH];
+  };
 };
 
-// Rows row0 .. row0 + 31 of src (row stride in elements), zero from row `rows`
-// on, into a tile; all threads of the workgroup.
-template <typename T, int D>
-__device__ inline void win_stage(typename WinCfg<T, D>::Tile& dst, const T* src, size_t stride, int row0, int rows) {
-  typedef WinCfg<T, D> C;
-  for (int x = threadIdx.x; x < kTile * C::CPR; x += kWave * kWinWaves) {
-    const int r = x / C::CPR, c = x % C::CPR * C::EPC;
-    uint4 v = {0, 0, 0, 0};
-    if (row0 + r < rows) v = *reinterpret_cast<const uint4*>(src + (size_t)(row0 + r) * stride + c);
-    *reinterpret_cast<uint4*>(&dst[r][c]) = v;
+// Rows row0 .. row0 + 31 of two arrays (row stride in elements), zero from row
+// `rows` on: into registers, and from there into two tiles; all threads of the
+// workgroup.
+template <int D>
+__device__ inline void win_fetch(typename WinF32<D>::Regs& r, const float* a, const float* b, size_t stride, int row0,
+                                 int rows) {
+#pragma unroll
+  for (int u = 0; u < WinF32<D>::NCH; ++u) {
+    const int x = threadIdx.x + u * kWave * kWinWaves, i = row0 + x / (D / 4);
+    const size_t at = (size_t)min(i, rows - 1) * stride + x % (D / 4) * 4;
+    const float4 va = *reinterpret_cast<const float4*>(a + at), vb = *reinterpret_cast<const float4*>(b + at);
+    const float4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+    r.a[u] = i < rows ? va : zero;
+    r.b[u] = i < rows ? vb : zero;
   }
 }
-// A row as an operand (zero past the last row).
-template <typename T, int D>
-__device__ inline void win_row_ops(typename WinCfg<T, D>::Ops& op, const T* row, bool ok, int hh) {
-  typedef Mma<T> M;
+template <int D>
+__device__ inline void win_put(const typename WinF32<D>::Regs& r, typename WinF32<D>::Tile& a,
+                               typename WinF32<D>::Tile& b) {
 #pragma unroll
-  for (int ks = 0; ks < WinCfg<T, D>::KD; ++ks) op[ks] = ok ? load_op<T>(row + ks * M::KW + hh * M::E) : M::zero();
+  for (int u = 0; u < WinF32<D>::NCH; ++u) {
+    const int x = threadIdx.x + u * kWave * kWinWaves;
+    *reinterpret_cast<float4*>(&a[x / (D / 4)][x % (D / 4) * 4]) = r.a[u];
+    *reinterpret_cast<float4*>(&b[x / (D / 4)][x % (D / 4) * 4]) = r.b[u];
+  }
+}
+// The entry of a row that step ks of a product over d contracts in lane half
+// hh: any order will do that both operands share, and this one makes four steps
+// one 16-byte piece.
+__device__ constexpr int win_entry(int ks, int hh) { return ks / 4 * 8 + 4 * hh + ks % 4; }
+// A row as an operand (zero past the last row).
+template <int D>
+__device__ inline void win_row_ops(typename WinF32<D>::Ops& op, const float* row, bool ok, int hh) {
+#pragma unroll
+  for (int ks = 0; ks < WinF32<D>::KD; ks += 4) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(row + win_entry(ks, hh));
+#pragma unroll
+    for (int k = 0; k < 4; ++k) op[ks + k] = ok ? v[k] : 0.0f;
+  }
 }
 // tile rows times the operands of 32 columns: rows in accumulator order.
-template <typename T, int D>
-__device__ inline f32x16 win_rows_mma(const typename WinCfg<T, D>::Tile& t, const typename Mma<T>::op_t* op, int li,
-                                      int hh) {
-  typedef Mma<T> M;
+template <int D>
+__device__ inline f32x16 win_rows_mma(const typename WinF32<D>::Tile& t, const float* op, int li, int hh) {
   f32x16 s = {};
 #pragma unroll
-  for (int ks = 0; ks < WinCfg<T, D>::KD; ++ks) s = M::mma(load_op<T>(&t[li][ks * M::KW + hh * M::E]), op[ks], s);
+  for (int ks = 0; ks < WinF32<D>::KD; ks += 4) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(&t[li][win_entry(ks, hh)]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s = Mma<float>::mma(v[k], op[ks + k], s);
+  }
+  mma_settle<float>();
   return s;
 }
 // acc[D][32] += tile^T x, x in accumulator order over the tile's rows.
-template <typename T, int D>
-__device__ inline void win_cols_mma(typename WinCfg<T, D>::Acc& acc, const typename WinCfg<T, D>::Tile& t,
-                                    const float (&x)[16], int li, int hh) {
-  typedef WinCfg<T, D> C;
-  typedef Mma<T> M;
+template <int D>
+__device__ inline void win_cols_mma(typename WinF32<D>::Acc& acc, const typename WinF32<D>::Tile& t, const float (&x)[16],
+                                    int li, int hh) {
 #pragma unroll
-  for (int ct = 0; ct < C::NCT; ++ct)
+  for (int ct = 0; ct < WinF32<D>::NCT; ++ct)
 #pragma unroll
-    for (int ks = 0; ks < C::KL; ++ks) {
-      typename M::op_t a;
-      if constexpr (M::E == 1) {
-        a = t[row_of(ks, hh)][ct * kTile + li];
-      } else {
-#pragma unroll
-        for (int e = 0; e < M::E; ++e) a[e] = t[row_of(ks * M::E + e, hh)][ct * kTile + li];
-      }
-      acc[ct] = M::mma(a, cvt_op<T>(&x[ks * M::E]), acc[ct]);
-    }
+    for (int ks = 0; ks < 16; ++ks) acc[ct] = Mma<float>::mma(t[row_of(ks, hh)][ct * kTile + li], x[ks], acc[ct]);
 }
 // acc^T (times f) to row `row` of out.
 template <typename T, int D>
-__device__ inline void win_store(void* out, size_t row, const typename WinCfg<T, D>::Acc& acc, float f, int hh,
-                                 bool f32) {
+__device__ inline void win_store(void* out, size_t row, const f32x16 (&acc)[D / kTile], float f, int hh, bool f32) {
 #pragma unroll
-  for (int ct = 0; ct < WinCfg<T, D>::NCT; ++ct)
+  for (int ct = 0; ct < D / kTile; ++ct)
 #pragma unroll
     for (int i = 0; i < 16; i += 4) {
       const float o[4] = {acc[ct][i] * f, acc[ct][i + 1] * f, acc[ct][i + 2] * f, acc[ct][i + 3] * f};
@@ -163,146 +202,146 @@ __device__ inline WinUnit win_unit(const WindowArgs& a, int len, int b, int g, i
   return WinUnit{b, g, g * G + u % G, i0, i0 < len};
 }
 
-template <typename T, int D>
+template <int D>
 __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_fwd_kernel(WindowArgs a, int wgs) {
-  typedef WinCfg<T, D> C;
-  typedef Mma<T> M;
-  __shared__ alignas(16) typename C::Tile kt, vt;
+  typedef WinF32<D> C;
+  __shared__ alignas(16) typename C::Tile kt[2], vt[2];
   const int lane = threadIdx.x & (kWave - 1), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int li = lane & 31, hh = lane >> 5;
   const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv;
-  const int bg = blockIdx.x / wgs, x = wgs - 1 - blockIdx.x % wgs, b = bg / Hkv, g = bg % Hkv;  // longest first
+  int bg, x;
+  win_place(blockIdx.x, a.s.B * Hkv, bg, x);
+  x = wgs - 1 - x;  // the longest first
+  const int b = bg / Hkv, g = bg % Hkv;
   const int len = win_len(a, b);
   const WinUnit me = win_unit(a, len, b, g, x * kWinWaves + w);
   const int first = x * kWinWaves / G * kTile, last = min(((x + 1) * kWinWaves - 1) / G * kTile + kTile, len);
   if (first >= len) return;  // uniform
   const WinTiles tl(a, len, first, last, kTile);
   const size_t qs = (size_t)Hq * D, ks_ = (size_t)Hkv * D;
-  const T* K = (const T*)a.k + ((size_t)b * a.T * Hkv + g) * D;
-  const T* V = (const T*)a.v + ((size_t)b * a.T * Hkv + g) * D;
+  const float* K = (const float*)a.k + ((size_t)b * a.T * Hkv + g) * D;
+  const float* V = (const float*)a.v + ((size_t)b * a.T * Hkv + g) * D;
   const int i = min(me.i0 + li, len - 1);
   const WinRow row(a, len, i), r0(a, len, min(me.i0, len - 1)), r1(a, len, min(me.i0 + kTile, len) - 1);
-  typename M::op_t qop[C::KD];
-  win_row_ops<T, D>(qop, (const T*)a.q + ((size_t)b * a.T * Hq + me.h) * D + i * qs, true, hh);
+  typename C::Regs next;
+  win_fetch<D>(next, K, V, ks_, tl.first(0, kTile), len);
+  typename C::Ops qop;
+  win_row_ops<D>(qop, (const float*)a.q + ((size_t)b * a.T * Hq + me.h) * D + i * qs, true, hh);
   const float scale = kLog2e / sqrtf((float)D);
   float m = kNoRef, l = 0.0f;
-  f32x16 acc[C::NCT];
+  typename C::Acc acc;
 #pragma unroll
   for (int ct = 0; ct < C::NCT; ++ct) acc[ct] = f32x16{};
+  win_put<D>(next, kt[0], vt[0]);
+  __syncthreads();
   for (int n = 0; n < tl.n; ++n) {
-    const int j0 = tl.first(n, kTile);
+    const int j0 = tl.first(n, kTile), buf = n & 1;
+    if (n + 1 < tl.n) win_fetch<D>(next, K, V, ks_, tl.first(n + 1, kTile), len);
+    if (me.any && !win_none(r0, r1, a.n_sinks, j0, kTile)) {  // uniform over the wave
+      const f32x16 sc = win_rows_mma<D>(kt[buf], qop, li, hh);
+      const bool full = win_full(r0, r1, a.n_sinks, j0, kTile);
+      float p[16], mt = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        p[e] = full || row.sees(j0 + row_of(e, hh), a.n_sinks) ? sc[e] * scale : -INFINITY;
+        mt = fmaxf(mt, p[e]);
+      }
+      mt = fmaxf(mt, xor32(mt));
+      const float mn = fmaxf(m, mt);
+      if (__any(mn > m)) {
+        mma_settle<float>();
+        const float corr = __builtin_amdgcn_exp2f(m - mn);
+        l *= corr;
+#pragma unroll
+        for (int ct = 0; ct < C::NCT; ++ct)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[ct][e] *= corr;
+        m = mn;
+      }
+      float ps = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        p[e] = __builtin_amdgcn_exp2f(p[e] - m);
+        ps += p[e];
+      }
+      l += ps + xor32(ps);
+      win_cols_mma<D>(acc, vt[buf], p, li, hh);
+      mma_settle<float>();
+    }
+    if (n + 1 < tl.n) win_put<D>(next, kt[buf ^ 1], vt[buf ^ 1]);
     __syncthreads();
-    win_stage<T, D>(kt, K, ks_, j0, len);
-    win_stage<T, D>(vt, V, ks_, j0, len);
-    __syncthreads();
-    if (!me.any || win_none(r0, r1, a.n_sinks, j0, kTile)) continue;  // uniform over the wave
-    const f32x16 sc = win_rows_mma<T, D>(kt, qop, li, hh);
-    const bool full = win_full(r0, r1, a.n_sinks, j0, kTile);
-    float p[16], mt = -INFINITY;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      p[e] = full || row.sees(j0 + row_of(e, hh), a.n_sinks) ? sc[e] * scale : -INFINITY;
-      mt = fmaxf(mt, p[e]);
-    }
-    mt = fmaxf(mt, xor32(mt));
-    const float mn = fmaxf(m, mt);
-    if (__any(mn > m)) {
-      const float corr = __builtin_amdgcn_exp2f(m - mn);
-      l *= corr;
-#pragma unroll
-      for (int ct = 0; ct < C::NCT; ++ct) acc[ct] *= corr;
-      m = mn;
-    }
-    float ps = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      p[e] = __builtin_amdgcn_exp2f(p[e] - m);
-      ps += p[e];
-    }
-    l += ps + xor32(ps);
-    win_cols_mma<T, D>(acc, vt, p, li, hh);
   }
   if (!me.any || me.i0 + li >= len) return;
-  win_store<T, D>(a.out, ((size_t)b * a.T + i) * Hq + me.h, acc, 1.0f / l, hh, a.s.out_f32);
+  win_store<float, D>(a.out, ((size_t)b * a.T + i) * Hq + me.h, acc, 1.0f / l, hh, true);
   if (a.lse && hh == 0) a.lse[((size_t)b * Hq + me.h) * a.T + i] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
-// delta_i = dout_i out_i of every row, [B][Hq][T] (zero past a length); D / 8
-// lanes per row.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void hyb_win_delta_kernel(WindowArgs a) {
-  constexpr int LPR = D / 8;
-  const long rows = (long)a.s.B * a.T * a.s.Hq;
-  for (long r = (long)blockIdx.x * (256 / LPR) + threadIdx.x / LPR; r < rows; r += (long)gridDim.x * (256 / LPR)) {
-    const int h = (int)(r % a.s.Hq);
-    const long bi = r / a.s.Hq;
-    const int b = (int)(bi / a.T), i = (int)(bi % a.T);
-    float s = 0.0f;
-    if (i < win_len(a, b)) {
-      const T* x = (const T*)a.out + r * D + threadIdx.x % LPR * 8;
-      const T* y = (const T*)a.dout + r * D + threadIdx.x % LPR * 8;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s += (float)x[e] * (float)y[e];
-    }
-#pragma unroll
-    for (int o = 1; o < LPR; o <<= 1) s += __shfl_xor(s, o);
-    if (threadIdx.x % LPR == 0) a.ws[((size_t)b * a.s.Hq + h) * a.T + i] = s;
-  }
-}
-
-template <typename T, int D>
+// dQ, and delta of the rows for the dK, dV kernel.
+template <int D>
 __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dq_kernel(WindowArgs a, int wgs) {
-  typedef WinCfg<T, D> C;
-  typedef Mma<T> M;
-  __shared__ alignas(16) typename C::Tile kt, vt;
+  typedef WinF32<D> C;
+  __shared__ alignas(16) typename C::Tile kt[2], vt[2];
   const int lane = threadIdx.x & (kWave - 1), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int li = lane & 31, hh = lane >> 5;
   const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv;
-  const int bg = blockIdx.x / wgs, x = wgs - 1 - blockIdx.x % wgs, b = bg / Hkv, g = bg % Hkv;
+  int bg, x;
+  win_place(blockIdx.x, a.s.B * Hkv, bg, x);
+  x = wgs - 1 - x;
+  const int b = bg / Hkv, g = bg % Hkv;
   const int len = win_len(a, b);
   const WinUnit me = win_unit(a, len, b, g, x * kWinWaves + w);
   const int first = x * kWinWaves / G * kTile, last = min(((x + 1) * kWinWaves - 1) / G * kTile + kTile, len);
   const size_t qs = (size_t)Hq * D, ks_ = (size_t)Hkv * D;
-  f32x16 acc[C::NCT];
+  typename C::Acc acc;
 #pragma unroll
   for (int ct = 0; ct < C::NCT; ++ct) acc[ct] = f32x16{};
   if (first < len) {  // uniform
     const WinTiles tl(a, len, first, last, kTile);
-    const T* K = (const T*)a.k + ((size_t)b * a.T * Hkv + g) * D;
-    const T* V = (const T*)a.v + ((size_t)b * a.T * Hkv + g) * D;
+    const float* K = (const float*)a.k + ((size_t)b * a.T * Hkv + g) * D;
+    const float* V = (const float*)a.v + ((size_t)b * a.T * Hkv + g) * D;
     const int i = min(me.i0 + li, len - 1);
     const WinRow row(a, len, i), r0(a, len, min(me.i0, len - 1)), r1(a, len, min(me.i0 + kTile, len) - 1);
-    typename M::op_t qop[C::KD], dop[C::KD];
+    typename C::Regs next;
+    win_fetch<D>(next, K, V, ks_, tl.first(0, kTile), len);
+    typename C::Ops qop, dop;
     const size_t at = ((size_t)b * a.T * Hq + me.h) * D + i * qs;
-    win_row_ops<T, D>(qop, (const T*)a.q + at, true, hh);
-    win_row_ops<T, D>(dop, (const T*)a.dout + at, true, hh);
+    win_row_ops<D>(qop, (const float*)a.q + at, true, hh);
+    win_row_ops<D>(dop, (const float*)a.dout + at, true, hh);
+    float delta = 0.0f;
+#pragma unroll
+    for (int ks = 0; ks < C::KD; ++ks) delta += dop[ks] * ((const float*)a.out)[at + win_entry(ks, hh)];
+    delta += xor32(delta);
     const float scale = kLog2e / sqrtf((float)D);
     const size_t st = ((size_t)b * Hq + me.h) * a.T + i;
-    const float lse = a.lse[st] * kLog2e, delta = a.ws[st];
+    const float lse = a.lse[st] * kLog2e;
+    if (hh == 0 && me.i0 + li < len) a.ws[st] = delta;
+    win_put<D>(next, kt[0], vt[0]);
+    __syncthreads();
     for (int n = 0; n < tl.n; ++n) {
-      const int j0 = tl.first(n, kTile);
-      __syncthreads();
-      win_stage<T, D>(kt, K, ks_, j0, len);
-      win_stage<T, D>(vt, V, ks_, j0, len);
-      __syncthreads();
-      if (!me.any || win_none(r0, r1, a.n_sinks, j0, kTile)) continue;
-      const f32x16 sc = win_rows_mma<T, D>(kt, qop, li, hh);
-      const f32x16 dp = win_rows_mma<T, D>(vt, dop, li, hh);
-      const bool full = win_full(r0, r1, a.n_sinks, j0, kTile);
-      float ds[16];
+      const int j0 = tl.first(n, kTile), buf = n & 1;
+      if (n + 1 < tl.n) win_fetch<D>(next, K, V, ks_, tl.first(n + 1, kTile), len);
+      if (me.any && !win_none(r0, r1, a.n_sinks, j0, kTile)) {
+        const f32x16 sc = win_rows_mma<D>(kt[buf], qop, li, hh);
+        const f32x16 dp = win_rows_mma<D>(vt[buf], dop, li, hh);
+        const bool full = win_full(r0, r1, a.n_sinks, j0, kTile);
+        float ds[16];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float p = full || row.sees(j0 + row_of(e, hh), a.n_sinks)
-                            ? __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale, -lse))
-                            : 0.0f;
-        ds[e] = p * (dp[e] - delta);
+        for (int e = 0; e < 16; ++e) {
+          const float p = full || row.sees(j0 + row_of(e, hh), a.n_sinks)
+                              ? __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale, -lse))
+                              : 0.0f;
+          ds[e] = p * (dp[e] - delta);
+        }
+        win_cols_mma<D>(acc, kt[buf], ds, li, hh);
+        mma_settle<float>();
       }
-      win_cols_mma<T, D>(acc, kt, ds, li, hh);
+      if (n + 1 < tl.n) win_put<D>(next, kt[buf ^ 1], vt[buf ^ 1]);
+      __syncthreads();
     }
   }
   if (me.i0 + li >= a.T) return;  // rows past the length: zero
-  win_store<T, D>(a.dq, ((size_t)b * a.T + me.i0 + li) * Hq + me.h, acc,
-                  me.i0 + li < len ? 1.0f / sqrtf((float)D) : 0.0f, hh, a.s.out_f32);
+  win_store<float, D>(a.dq, ((size_t)b * a.T + me.i0 + li) * Hq + me.h, acc,
+                      me.i0 + li < len ? 1.0f / sqrtf((float)D) : 0.0f, hh, true);
 }
 
 // The queries that see some of the keys j0 .. j1 - 1 (j1 <= len): from q0 to q1 - 1.
@@ -318,63 +357,77 @@ struct WinQueries {
 
 // dK, dV: a wave owns 32 keys, and loops over the queries of all heads of
 // its KV head.
-template <typename T, int D>
-__global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dkv_kernel(WindowArgs a, int wgs) {
-  typedef WinCfg<T, D> C;
-  typedef Mma<T> M;
-  __shared__ alignas(16) typename C::Tile qt, dt;
-  __shared__ alignas(16) float lse[kTile], delta[kTile];
+template <int D>
+__global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dkv_kernel(WindowArgs a) {
+  typedef WinF32<D> C;
+  __shared__ alignas(16) typename C::Tile qt[2], dt[2];
+  __shared__ alignas(16) float stats[2][2][kTile];  // lse (log2) and delta
   const int lane = threadIdx.x & (kWave - 1), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int li = lane & 31, hh = lane >> 5;
   const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv;
-  const int bg = blockIdx.x / wgs, x = blockIdx.x % wgs, b = bg / Hkv, g = bg % Hkv;
+  int bg, x;
+  win_place(blockIdx.x, a.s.B * Hkv, bg, x);
+  const int b = bg / Hkv, g = bg % Hkv;
   const int len = win_len(a, b);
   const int w0 = x * kWinWaves * kTile, j0 = w0 + w * kTile, j = j0 + li;  // first key of the workgroup, of the wave
   const size_t qs = (size_t)Hq * D, ks_ = (size_t)Hkv * D;
-  f32x16 dk[C::NCT], dv[C::NCT];
+  typename C::Acc dk, dv;
 #pragma unroll
   for (int ct = 0; ct < C::NCT; ++ct) dk[ct] = dv[ct] = f32x16{};
   if (w0 < len) {  // uniform
     const WinQueries all(a, len, w0, min(w0 + kWinWaves * kTile, len));
-    typename M::op_t kop[C::KD], vop[C::KD];
+    const int t0 = all.q0 / kTile, nq = (all.q1 + kTile - 1) / kTile - t0, nsteps = nq * G;
+    const WinKey mine(a, len, min(j, len - 1));
+    typename C::Regs next;
+    float nst = 0.0f;
+    // Step n: query tile t0 + n % nq of the group's head n / nq.
+    auto fetch = [&](int n) __attribute__((always_inline)) {
+      const int h = g * G + n / nq, i0 = (t0 + n % nq) * kTile;
+      const size_t head = ((size_t)b * a.T * Hq + h) * D;
+      win_fetch<D>(next, (const float*)a.q + head, (const float*)a.dout + head, qs, i0, len);
+      if (threadIdx.x < 2 * kTile) {
+        const size_t at = ((size_t)b * Hq + h) * a.T + min(i0 + (int)threadIdx.x % kTile, len - 1);
+        nst = threadIdx.x < kTile ? a.lse[at] * kLog2e : a.ws[at];
+      }
+    };
+    auto put = [&](int buf) __attribute__((always_inline)) {
+      win_put<D>(next, qt[buf], dt[buf]);
+      if (threadIdx.x < 2 * kTile) (&stats[buf][0][0])[threadIdx.x] = nst;
+    };
+    fetch(0);
+    typename C::Ops kop, vop;
     const size_t at = ((size_t)b * a.T * Hkv + g) * D + (size_t)min(j, len - 1) * ks_;
-    win_row_ops<T, D>(kop, (const T*)a.k + at, j < len, hh);
-    win_row_ops<T, D>(vop, (const T*)a.v + at, j < len, hh);
+    win_row_ops<D>(kop, (const float*)a.k + at, j < len, hh);
+    win_row_ops<D>(vop, (const float*)a.v + at, j < len, hh);
     const float scale = kLog2e / sqrtf((float)D);
-    for (int h = g * G; h < g * G + G; ++h) {
-      const size_t head = ((size_t)b * a.T * Hq + h) * D, st = ((size_t)b * Hq + h) * a.T;
-      for (int i0 = all.q0 / kTile * kTile; i0 < all.q1; i0 += kTile) {
-        __syncthreads();
-        win_stage<T, D>(qt, (const T*)a.q + head, qs, i0, len);
-        win_stage<T, D>(dt, (const T*)a.dout + head, qs, i0, len);
-        if (threadIdx.x < kTile) {
-          const int i = min(i0 + (int)threadIdx.x, len - 1);
-          lse[threadIdx.x] = a.lse[st + i] * kLog2e;
-          delta[threadIdx.x] = a.ws[st + i];
-        }
-        __syncthreads();
-        const WinRow r0(a, len, i0), r1(a, len, min(i0 + kTile, len) - 1);
-        if (j0 >= len || win_none(r0, r1, a.n_sinks, j0, kTile)) continue;
-        const f32x16 sc = win_rows_mma<T, D>(qt, kop, li, hh);
-        const f32x16 dp = win_rows_mma<T, D>(dt, vop, li, hh);
-        const bool full = i0 + kTile <= len && win_full(r0, r1, a.n_sinks, j0, kTile);
+    put(0);
+    __syncthreads();
+    for (int n = 0; n < nsteps; ++n) {
+      const int i0 = (t0 + n % nq) * kTile, buf = n & 1;
+      if (n + 1 < nsteps) fetch(n + 1);
+      const WinRow r0(a, len, i0), r1(a, len, min(i0 + kTile, len) - 1);
+      if (j0 < len && !win_none(r0, r1, a.n_sinks, j0, kTile)) {
+        const f32x16 sc = win_rows_mma<D>(qt[buf], kop, li, hh);
+        const f32x16 dp = win_rows_mma<D>(dt[buf], vop, li, hh);
         float p[16], ds[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int r = row_of(e, hh), i = i0 + r;
-          const bool sees = full || (i < len && WinRow(a, len, min(i, len - 1)).sees(j, a.n_sinks));
-          p[e] = sees ? __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale, -lse[r])) : 0.0f;
-          ds[e] = p[e] * (dp[e] - delta[r]);
+          p[e] = i >= mine.q0 && i < mine.q1 ? __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale, -stats[buf][0][r])) : 0.0f;
+          ds[e] = p[e] * (dp[e] - stats[buf][1][r]);
         }
-        win_cols_mma<T, D>(dv, dt, p, li, hh);
-        win_cols_mma<T, D>(dk, qt, ds, li, hh);
+        win_cols_mma<D>(dv, dt[buf], p, li, hh);
+        win_cols_mma<D>(dk, qt[buf], ds, li, hh);
+        mma_settle<float>();
       }
+      if (n + 1 < nsteps) put(buf ^ 1);
+      __syncthreads();
     }
   }
   if (j >= a.T) return;
   const size_t row = ((size_t)b * a.T + j) * Hkv + g;
-  win_store<T, D>(a.dk, row, dk, j < len ? 1.0f / sqrtf((float)D) : 0.0f, hh, a.s.out_f32);
-  win_store<T, D>(a.dv, row, dv, j < len ? 1.0f : 0.0f, hh, a.s.out_f32);
+  win_store<float, D>(a.dk, row, dk, j < len ? 1.0f / sqrtf((float)D) : 0.0f, hh, true);
+  win_store<float, D>(a.dv, row, dv, j < len ? 1.0f : 0.0f, hh, true);
 }
 
 // ---- bf16 forward -----------------------------------------------------------
@@ -398,17 +451,6 @@ struct WinRing {
   __device__ static constexpr int swz(int t) { return (t / RP256) % CPR; }
   __device__ static constexpr int vswz(int t) { return 4 * ((t / RP256) % (CPR / 4)); }
 };
-
-// The workgroups' order: the x-th workgroups of all (request, KV head)s one after
-// the other, so that with the longest first the chip ends with short ones; a
-// (request, KV head) stays on one XCD where their number is a multiple of 8
-// (workgroups go to the XCDs in turn), which keeps what it reads in that XCD's L2.
-// (One (request, KV head) after the other left the last one's long workgroups
-// to the end: gradient of 8 x 2048 tokens 618 us, now 503.)
-__device__ inline void win_place(int bid, int nbg, int& bg, int& x) {
-  bg = bid % nbg;
-  x = bid / nbg;
-}
 
 // The reference of a query's weights moves only when a tile's maximum passes it
 // by 2^8: until then weights are up to 2^8, which neither type minds, and the
@@ -597,17 +639,6 @@ __global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_ring_kernel(Windo
 // loops over key tiles), then dK with dV (a wave owns 32 keys and loops over the
 // query tiles of its KV head's heads).  Tiles come through rings as in the forward;
 // here a tile is read both by rows and by columns (RowColTile).
-
-// The keys' side of WinRow: key j is seen by the queries q0 .. q1 - 1.
-struct WinKey {
-  int q0, q1;
-  __device__ inline WinKey(const WindowArgs& a, int len, int j) {
-    const int L = a.s.L;
-    q0 = j / L * L;
-    const long end = ((long)j + a.window) / L * L + L;
-    q1 = j < a.n_sinks ? len : (int)min(end, (long)len);
-  }
-};
 
 // Statistics of a row for the dK, dV kernel, as operands of one more step of its
 // products: lse sqrt(d) and delta, each as three bf16 pieces (24 bits), which
@@ -1025,24 +1056,20 @@ static hipError_t win_ring_go(const WindowArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <typename T, int D>
-static hipError_t win_prefill_go(const WindowArgs& a, hipStream_t st) {
+template <int D>
+static hipError_t win_prefill_f32_go(const WindowArgs& a, hipStream_t st) {
   const int wgs = win_wgs(a);
-  hipLaunchKernelGGL((hyb_win_fwd_kernel<T, D>), dim3((unsigned)(a.s.B * a.s.Hkv * wgs)), dim3(kWave * kWinWaves), 0,
-                     st, a, wgs);
+  hipLaunchKernelGGL(hyb_win_fwd_kernel<D>, dim3((unsigned)(a.s.B * a.s.Hkv * wgs)), dim3(kWave * kWinWaves), 0, st, a,
+                     wgs);
   return hipGetLastError();
 }
 
-template <typename T, int D>
-static hipError_t win_backward_go(const WindowArgs& a, hipStream_t st) {
-  const long rows = (long)a.s.B * a.T * a.s.Hq;
-  hipLaunchKernelGGL((hyb_win_delta_kernel<T, D>), dim3((unsigned)std::min<long>((rows * D / 8 + 255) / 256, 4096)),
-                     dim3(256), 0, st, a);
+template <int D>
+static hipError_t win_backward_f32_go(const WindowArgs& a, hipStream_t st) {
   const int wgs = win_wgs(a), kwgs = (a.T + kWinWaves * kTile - 1) / (kWinWaves * kTile);
-  hipLaunchKernelGGL((hyb_win_dq_kernel<T, D>), dim3((unsigned)(a.s.B * a.s.Hkv * wgs)), dim3(kWave * kWinWaves), 0,
-                     st, a, wgs);
-  hipLaunchKernelGGL((hyb_win_dkv_kernel<T, D>), dim3((unsigned)(a.s.B * a.s.Hkv * kwgs)), dim3(kWave * kWinWaves), 0,
-                     st, a, kwgs);
+  hipLaunchKernelGGL(hyb_win_dq_kernel<D>, dim3((unsigned)(a.s.B * a.s.Hkv * wgs)), dim3(kWave * kWinWaves), 0, st, a,
+                     wgs);
+  hipLaunchKernelGGL(hyb_win_dkv_kernel<D>, dim3((unsigned)(a.s.B * a.s.Hkv * kwgs)), dim3(kWave * kWinWaves), 0, st, a);
   return hipGetLastError();
 }
 
@@ -1102,12 +1129,12 @@ static hipError_t win_backward_ring_go(WindowArgs a, hipStream_t st) {
 
 hipError_t launch_window_prefill(const WindowArgs& a, hipStream_t st) {
   if (a.s.dtype == 1) return a.s.D == 64 ? win_ring_go<64>(a, st) : win_ring_go<128>(a, st);
-  return a.s.D == 64 ? win_prefill_go<float, 64>(a, st) : win_prefill_go<float, 128>(a, st);
+  return a.s.D == 64 ? win_prefill_f32_go<64>(a, st) : win_prefill_f32_go<128>(a, st);
 }
 
 hipError_t launch_window_backward(const WindowArgs& a, hipStream_t st) {
   if (a.s.dtype == 1) return a.s.D == 64 ? win_backward_ring_go<64>(a, st) : win_backward_ring_go<128>(a, st);
-  return a.s.D == 64 ? win_backward_go<float, 64>(a, st) : win_backward_go<float, 128>(a, st);
+  return a.s.D == 64 ? win_backward_f32_go<64>(a, st) : win_backward_f32_go<128>(a, st);
 }
 
 // Workgroups of the largest launch (the grid's limit is checked by the caller).
