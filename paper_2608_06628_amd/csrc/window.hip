@@ -44,7 +44,7 @@ struct WinRow {
     lo = max(0, s0 - a.window);
     end = min(s0 + min(a.s.L, len - s0), len);
   }
-  __device__ inline bool sees(int j, int sinks) const { return j < end && (j >= lo || j < sinks); }
+  __device__ inline bool sees(int j, int sinks) const { return (j < end) & ((j >= lo) | (j < sinks)); }
 };
 
 // The key tiles that the queries i0 .. i1 - 1 see some of: tiles 0 .. st - 1
@@ -112,13 +112,13 @@ struct WinF32 {
   typedef float Ops[KD];
   typedef f32x16 Acc[NCT];
   struct Regs {
-    float4 a[NCH], b[NCH];
+    f32x4 a[NCH], b[NCH];
   };
 };
 
-// Rows row0 .. row0 + 31 of two arrays (row stride in elements), zero from row
-// `rows` on: into registers, and from there into two tiles; all threads of the
-// workgroup.
+// Rows row0 .. row0 + 31 of two arrays (row stride in elements) into registers,
+// and from there, zero from row `rows` on, into two tiles; all threads of the
+// workgroup.  (The zeros are put in last: a select at the load would wait for it.)
 template <int D>
 __device__ inline void win_fetch(typename WinF32<D>::Regs& r, const float* a, const float* b, size_t stride, int row0,
                                  int rows) {
@@ -126,20 +126,19 @@ __device__ inline void win_fetch(typename WinF32<D>::Regs& r, const float* a, co
   for (int u = 0; u < WinF32<D>::NCH; ++u) {
     const int x = threadIdx.x + u * kWave * kWinWaves, i = row0 + x / (D / 4);
     const size_t at = (size_t)min(i, rows - 1) * stride + x % (D / 4) * 4;
-    const float4 va = *reinterpret_cast<const float4*>(a + at), vb = *reinterpret_cast<const float4*>(b + at);
-    const float4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-    r.a[u] = i < rows ? va : zero;
-    r.b[u] = i < rows ? vb : zero;
+    r.a[u] = *reinterpret_cast<const f32x4*>(a + at);
+    r.b[u] = *reinterpret_cast<const f32x4*>(b + at);
   }
 }
 template <int D>
 __device__ inline void win_put(const typename WinF32<D>::Regs& r, typename WinF32<D>::Tile& a,
-                               typename WinF32<D>::Tile& b) {
+                               typename WinF32<D>::Tile& b, int row0, int rows) {
 #pragma unroll
   for (int u = 0; u < WinF32<D>::NCH; ++u) {
-    const int x = threadIdx.x + u * kWave * kWinWaves;
-    *reinterpret_cast<float4*>(&a[x / (D / 4)][x % (D / 4) * 4]) = r.a[u];
-    *reinterpret_cast<float4*>(&b[x / (D / 4)][x % (D / 4) * 4]) = r.b[u];
+    const int x = threadIdx.x + u * kWave * kWinWaves, i = x / (D / 4);
+    const bool ok = row0 + i < rows;
+    *reinterpret_cast<f32x4*>(&a[i][x % (D / 4) * 4]) = ok ? r.a[u] : f32x4{};
+    *reinterpret_cast<f32x4*>(&b[i][x % (D / 4) * 4]) = ok ? r.b[u] : f32x4{};
   }
 }
 // The entry of a row that step ks of a product over d contracts in lane half
@@ -232,21 +231,21 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_fwd_kernel(WindowArg
   typename C::Acc acc;
 #pragma unroll
   for (int ct = 0; ct < C::NCT; ++ct) acc[ct] = f32x16{};
-  win_put<D>(next, kt[0], vt[0]);
+  win_put<D>(next, kt[0], vt[0], tl.first(0, kTile), len);
   __syncthreads();
   for (int n = 0; n < tl.n; ++n) {
     const int j0 = tl.first(n, kTile), buf = n & 1;
     if (n + 1 < tl.n) win_fetch<D>(next, K, V, ks_, tl.first(n + 1, kTile), len);
     if (me.any && !win_none(r0, r1, a.n_sinks, j0, kTile)) {  // uniform over the wave
-      const f32x16 sc = win_rows_mma<D>(kt[buf], qop, li, hh);
-      const bool full = win_full(r0, r1, a.n_sinks, j0, kTile);
-      float p[16], mt = -INFINITY;
+      f32x16 sc = win_rows_mma<D>(kt[buf], qop, li, hh);
+      if (!win_full(r0, r1, a.n_sinks, j0, kTile)) {  // uniform
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        p[e] = full || row.sees(j0 + row_of(e, hh), a.n_sinks) ? sc[e] * scale : -INFINITY;
-        mt = fmaxf(mt, p[e]);
+        for (int e = 0; e < 16; ++e) sc[e] = row.sees(j0 + row_of(e, hh), a.n_sinks) ? sc[e] : -INFINITY;
       }
-      mt = fmaxf(mt, xor32(mt));
+      float p[16], mt = sc[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) mt = fmaxf(mt, sc[e]);
+      mt = fmaxf(mt, xor32(mt)) * scale;
       const float mn = fmaxf(m, mt);
       if (__any(mn > m)) {
         mma_settle<float>();
@@ -261,14 +260,14 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_fwd_kernel(WindowArg
       float ps = 0.0f;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(p[e] - m);
+        p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale, -m));
         ps += p[e];
       }
       l += ps + xor32(ps);
       win_cols_mma<D>(acc, vt[buf], p, li, hh);
       mma_settle<float>();
     }
-    if (n + 1 < tl.n) win_put<D>(next, kt[buf ^ 1], vt[buf ^ 1]);
+    if (n + 1 < tl.n) win_put<D>(next, kt[buf ^ 1], vt[buf ^ 1], tl.first(n + 1, kTile), len);
     __syncthreads();
   }
   if (!me.any || me.i0 + li >= len) return;
@@ -315,27 +314,26 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dq_kernel(WindowArgs
     const size_t st = ((size_t)b * Hq + me.h) * a.T + i;
     const float lse = a.lse[st] * kLog2e;
     if (hh == 0 && me.i0 + li < len) a.ws[st] = delta;
-    win_put<D>(next, kt[0], vt[0]);
+    win_put<D>(next, kt[0], vt[0], tl.first(0, kTile), len);
     __syncthreads();
     for (int n = 0; n < tl.n; ++n) {
       const int j0 = tl.first(n, kTile), buf = n & 1;
       if (n + 1 < tl.n) win_fetch<D>(next, K, V, ks_, tl.first(n + 1, kTile), len);
       if (me.any && !win_none(r0, r1, a.n_sinks, j0, kTile)) {
-        const f32x16 sc = win_rows_mma<D>(kt[buf], qop, li, hh);
+        f32x16 sc = win_rows_mma<D>(kt[buf], qop, li, hh);
         const f32x16 dp = win_rows_mma<D>(vt[buf], dop, li, hh);
-        const bool full = win_full(r0, r1, a.n_sinks, j0, kTile);
+        if (!win_full(r0, r1, a.n_sinks, j0, kTile)) {  // uniform
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sc[e] = row.sees(j0 + row_of(e, hh), a.n_sinks) ? sc[e] : -INFINITY;
+        }
         float ds[16];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float p = full || row.sees(j0 + row_of(e, hh), a.n_sinks)
-                              ? __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale, -lse))
-                              : 0.0f;
-          ds[e] = p * (dp[e] - delta);
-        }
+        for (int e = 0; e < 16; ++e)
+          ds[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale, -lse)) * (dp[e] - delta);
         win_cols_mma<D>(acc, kt[buf], ds, li, hh);
         mma_settle<float>();
       }
-      if (n + 1 < tl.n) win_put<D>(next, kt[buf ^ 1], vt[buf ^ 1]);
+      if (n + 1 < tl.n) win_put<D>(next, kt[buf ^ 1], vt[buf ^ 1], tl.first(n + 1, kTile), len);
       __syncthreads();
     }
   }
@@ -390,8 +388,9 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dkv_kernel(WindowArg
         nst = threadIdx.x < kTile ? a.lse[at] * kLog2e : a.ws[at];
       }
     };
-    auto put = [&](int buf) __attribute__((always_inline)) {
-      win_put<D>(next, qt[buf], dt[buf]);
+    auto put = [&](int n) __attribute__((always_inline)) {
+      const int buf = n & 1;
+      win_put<D>(next, qt[buf], dt[buf], (t0 + n % nq) * kTile, len);
       if (threadIdx.x < 2 * kTile) (&stats[buf][0][0])[threadIdx.x] = nst;
     };
     fetch(0);
@@ -413,14 +412,15 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dkv_kernel(WindowArg
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int r = row_of(e, hh), i = i0 + r;
-          p[e] = i >= mine.q0 && i < mine.q1 ? __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale, -stats[buf][0][r])) : 0.0f;
+          const float x = __builtin_fmaf(sc[e], scale, -stats[buf][0][r]);
+          p[e] = __builtin_amdgcn_exp2f((i >= mine.q0) & (i < mine.q1) ? x : -INFINITY);
           ds[e] = p[e] * (dp[e] - stats[buf][1][r]);
         }
         win_cols_mma<D>(dv, dt[buf], p, li, hh);
         win_cols_mma<D>(dk, qt[buf], ds, li, hh);
         mma_settle<float>();
       }
-      if (n + 1 < nsteps) put(buf ^ 1);
+      if (n + 1 < nsteps) put(n + 1);
       __syncthreads();
     }
   }
