@@ -21,6 +21,7 @@
 // each accumulator tile is the next product's operand without leaving its
 // registers (device.h).
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "device.h"
@@ -90,6 +91,43 @@ __device__ inline void win_place(int bid, int nbg, int& bg, int& x) {
   bg = bid % nbg;
   x = bid / nbg;
 }
+
+// The dK, dV kernels: a workgroup owns 128 keys and goes through the query
+// tiles that see them, of all heads of the KV head.  These lists are cut into
+// parts that are summed in the workspace: those of the keys among the sinks, which
+// every later query sees (the first `ns` workgroups of a (request, KV head)), into
+// ps, the others into p.
+constexpr int kWinKeys = 4 * kTile;
+struct WinParts {
+  int wgs, ns, ps, p;
+  __host__ __device__ int items() const { return ns * ps + (wgs - ns) * p; }
+  // Rows of partial sums of dK and dV: ps for the first ns workgroups' keys
+  // (padded), then p of every key, each where there is more than one.
+  __host__ __device__ long sink_rows() const { return ps > 1 ? (long)ps * ns * kWinKeys : 0; }
+  __host__ __device__ long rows(int T) const { return sink_rows() + (p > 1 ? (long)p * T : 0); }
+};
+// Item y of a (request, KV head): its keys' workgroup x and part; and where its
+// results go: key j's row of dK (o = 0) or dV (o = 1) in the sums
+// [part][o][B][span][Hkv][D] of its region.
+struct WinItem {
+  int x, part, parts, span;
+  bool sink;
+  __device__ inline WinItem(const WindowArgs& a, const WinParts& c, int y) {
+    sink = y < c.ns * c.ps;
+    parts = sink ? c.ps : c.p;
+    if (!sink) y -= c.ns * c.ps;
+    part = y % parts;
+    x = y / parts + (sink ? 0 : c.ns);
+    span = sink ? c.ns * kWinKeys : a.T;
+  }
+  template <int D>
+  __device__ inline float* sums(const WindowArgs& a, const WinParts& c) const {
+    return a.sums + (sink ? 0 : c.sink_rows() * 2 * a.s.B * a.s.Hkv * D);
+  }
+  __device__ inline size_t row(const WindowArgs& a, int o, int b, int j, int g) const {
+    return (((size_t)(part * 2 + o) * a.s.B + b) * span + j) * a.s.Hkv + g;
+  }
+};
 
 // ---- fp32 kernels -------------------------------------------------------------
 //
@@ -356,7 +394,7 @@ struct WinQueries {
 // dK, dV: a wave owns 32 keys, and loops over the queries of all heads of
 // its KV head.
 template <int D>
-__global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dkv_kernel(WindowArgs a) {
+__global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dkv_kernel(WindowArgs a, WinParts cut) {
   typedef WinF32<D> C;
   __shared__ alignas(16) typename C::Tile qt[2], dt[2];
   __shared__ alignas(16) float stats[2][2][kTile];  // lse (log2) and delta
@@ -365,22 +403,26 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dkv_kernel(WindowArg
   const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv;
   int bg, x;
   win_place(blockIdx.x, a.s.B * Hkv, bg, x);
+  const WinItem it(a, cut, x);
   const int b = bg / Hkv, g = bg % Hkv;
   const int len = win_len(a, b);
-  const int w0 = x * kWinWaves * kTile, j0 = w0 + w * kTile, j = j0 + li;  // first key of the workgroup, of the wave
+  const int w0 = it.x * kWinKeys, j0 = w0 + w * kTile, j = j0 + li;  // first key of the workgroup, of the wave
   const size_t qs = (size_t)Hq * D, ks_ = (size_t)Hkv * D;
   typename C::Acc dk, dv;
 #pragma unroll
   for (int ct = 0; ct < C::NCT; ++ct) dk[ct] = dv[ct] = f32x16{};
   if (w0 < len) {  // uniform
-    const WinQueries all(a, len, w0, min(w0 + kWinWaves * kTile, len));
-    const int t0 = all.q0 / kTile, nq = (all.q1 + kTile - 1) / kTile - t0, nsteps = nq * G;
+    const WinQueries all(a, len, w0, min(w0 + kWinKeys, len));
+    const int t0 = all.q0 / kTile, nq = (all.q1 + kTile - 1) / kTile - t0;
+    const int first = (int)((long)nq * G * it.part / it.parts);
+    const int nsteps = (int)((long)nq * G * (it.part + 1) / it.parts) - first;
     const WinKey mine(a, len, min(j, len - 1));
     typename C::Regs next;
     float nst = 0.0f;
-    // Step n: query tile t0 + n % nq of the group's head n / nq.
+    // Step n: the list's query tile first + n, of the group's heads in turn.
+    auto tile = [&](int n) __attribute__((always_inline)) { return (t0 + (first + n) % nq) * kTile; };
     auto fetch = [&](int n) __attribute__((always_inline)) {
-      const int h = g * G + n / nq, i0 = (t0 + n % nq) * kTile;
+      const int h = g * G + (first + n) / nq, i0 = tile(n);
       const size_t head = ((size_t)b * a.T * Hq + h) * D;
       win_fetch<D>(next, (const float*)a.q + head, (const float*)a.dout + head, qs, i0, len);
       if (threadIdx.x < 2 * kTile) {
@@ -390,19 +432,19 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dkv_kernel(WindowArg
     };
     auto put = [&](int n) __attribute__((always_inline)) {
       const int buf = n & 1;
-      win_put<D>(next, qt[buf], dt[buf], (t0 + n % nq) * kTile, len);
+      win_put<D>(next, qt[buf], dt[buf], tile(n), len);
       if (threadIdx.x < 2 * kTile) (&stats[buf][0][0])[threadIdx.x] = nst;
     };
-    fetch(0);
+    if (nsteps > 0) fetch(0);
     typename C::Ops kop, vop;
     const size_t at = ((size_t)b * a.T * Hkv + g) * D + (size_t)min(j, len - 1) * ks_;
     win_row_ops<D>(kop, (const float*)a.k + at, j < len, hh);
     win_row_ops<D>(vop, (const float*)a.v + at, j < len, hh);
     const float scale = kLog2e / sqrtf((float)D);
-    put(0);
+    if (nsteps > 0) put(0);
     __syncthreads();
     for (int n = 0; n < nsteps; ++n) {
-      const int i0 = (t0 + n % nq) * kTile, buf = n & 1;
+      const int i0 = tile(n), buf = n & 1;
       if (n + 1 < nsteps) fetch(n + 1);
       const WinRow r0(a, len, i0), r1(a, len, min(i0 + kTile, len) - 1);
       if (j0 < len && !win_none(r0, r1, a.n_sinks, j0, kTile)) {
@@ -413,7 +455,7 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dkv_kernel(WindowArg
         for (int e = 0; e < 16; ++e) {
           const int r = row_of(e, hh), i = i0 + r;
           const float x = __builtin_fmaf(sc[e], scale, -stats[buf][0][r]);
-          p[e] = __builtin_amdgcn_exp2f((i >= mine.q0) & (i < mine.q1) ? x : -INFINITY);
+          p[e] = __builtin_amdgcn_exp2f(i >= mine.q0 && i < mine.q1 ? x : -INFINITY);
           ds[e] = p[e] * (dp[e] - stats[buf][1][r]);
         }
         win_cols_mma<D>(dv, dt[buf], p, li, hh);
@@ -426,8 +468,14 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dkv_kernel(WindowArg
   }
   if (j >= a.T) return;
   const size_t row = ((size_t)b * a.T + j) * Hkv + g;
-  win_store<float, D>(a.dk, row, dk, j < len ? 1.0f / sqrtf((float)D) : 0.0f, hh, true);
-  win_store<float, D>(a.dv, row, dv, j < len ? 1.0f : 0.0f, hh, true);
+  const float fk = j < len ? 1.0f / sqrtf((float)D) : 0.0f, fv = j < len ? 1.0f : 0.0f;
+  if (it.parts == 1) {
+    win_store<float, D>(a.dk, row, dk, fk, hh, true);
+    win_store<float, D>(a.dv, row, dv, fv, hh, true);
+  } else {
+    win_store<float, D>(it.sums<D>(a, cut), it.row(a, 0, b, j, g), dk, fk, hh, true);
+    win_store<float, D>(it.sums<D>(a, cut), it.row(a, 1, b, j, g), dv, fv, hh, true);
+  }
 }
 
 // ---- bf16 forward -----------------------------------------------------------
@@ -813,19 +861,6 @@ __global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_dq_ring_kernel(Wi
 // from LDS.)
 constexpr int kWinKeyWaves = 8;
 
-// How the workgroups' lists of query tiles (of all heads) are cut into parts
-// that are summed in the workspace: those of the keys among the sinks, which
-// every later query sees (the first `ns` workgroups of a (request, KV head)), into
-// ps, the others into p.
-struct WinParts {
-  int wgs, ns, ps, p;
-  __host__ __device__ int items() const { return ns * ps + (wgs - ns) * p; }
-  // Rows of partial sums of dK and dV: ps for the first ns workgroups' keys
-  // (padded), then p of every key, each where there is more than one.
-  __host__ __device__ long sink_rows() const { return ps > 1 ? (long)ps * ns * 4 * kTile : 0; }
-  __host__ __device__ long rows(int T) const { return sink_rows() + (p > 1 ? (long)p * T : 0); }
-};
-
 template <int D>
 __global__ __launch_bounds__(kWave* kWinKeyWaves, 2) void hyb_win_dkv_ring_kernel(WindowArgs a, WinParts cut) {
   typedef Mma<bf16> M;
@@ -857,14 +892,10 @@ __global__ __launch_bounds__(kWave* kWinKeyWaves, 2) void hyb_win_dkv_ring_kerne
   const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv, Tp = win_tp(a.T);
   int bg, x;
   win_place(blockIdx.x, a.s.B * Hkv, bg, x);  // the longest (first keys) first
-  const bool sink = x < cut.ns * cut.ps;
-  const int parts = sink ? cut.ps : cut.p;
-  if (!sink) x -= cut.ns * cut.ps;
-  const int part = x % parts;
-  x = x / parts + (sink ? 0 : cut.ns);
+  const WinItem it(a, cut, x);
   const int b = bg / Hkv, g = bg % Hkv;
   const int len = win_len(a, b);
-  const int w0 = x * 4 * kTile, j0 = w0 + w * kTile, j = j0 + li;
+  const int w0 = it.x * kWinKeys, j0 = w0 + w * kTile, j = j0 + li;
   f32x16 acc[2][NCT];  // dK, dV
 #pragma unroll
   for (int ct = 0; ct < NCT; ++ct) acc[0][ct] = acc[1][ct] = f32x16{};
@@ -872,9 +903,10 @@ __global__ __launch_bounds__(kWave* kWinKeyWaves, 2) void hyb_win_dkv_ring_kerne
     const size_t qs = (size_t)Hq * D, ks_ = (size_t)Hkv * D;
     // query tiles t0 .. t0 + nq - 1 of every head, of which this part takes
     // ntiles from first on, a half every second
-    const WinQueries all(a, len, w0, min(w0 + 4 * kTile, len));
+    const WinQueries all(a, len, w0, min(w0 + kWinKeys, len));
     const int t0 = all.q0 / kTile, nq = (all.q1 + kTile - 1) / kTile - t0;
-    const int first = (int)((long)nq * G * part / parts), ntiles = (int)((long)nq * G * (part + 1) / parts) - first;
+    const int first = (int)((long)nq * G * it.part / it.parts);
+    const int ntiles = (int)((long)nq * G * (it.part + 1) / it.parts) - first;
     const int nsteps = (ntiles + 1) / 2, mysteps = (ntiles + 1 - half) / 2;
     const WinKey mine(a, len, min(j, len - 1));
     // query tiles that every key of the wave is seen by: f0 <= i0 and i0 + 32 <= f1
@@ -1009,36 +1041,36 @@ __global__ __launch_bounds__(kWave* kWinKeyWaves, 2) void hyb_win_dkv_ring_kerne
           }
   }
   if (j >= a.T) return;
-  // this part's rows of sums: [part][dK, dV][B][rows][Hkv][D]
-  const int span = sink ? cut.ns * 4 * kTile : a.T;
-  const size_t row = ((size_t)b * a.T + j) * Hkv + g, rows = (size_t)a.s.B * span * Hkv;
-  float* const sums = a.sums + (sink ? 0 : cut.sink_rows() * 2 * a.s.B * Hkv * D);
+  const size_t row = ((size_t)b * a.T + j) * Hkv + g;
   const float f = j >= len ? 0.0f : half == 0 ? 1.0f / sqrtf((float)D) : 1.0f;
 #pragma unroll
   for (int o = 0; o < 2; ++o)
     if (o == half) {
-      if (parts == 1)
+      if (it.parts == 1)
         win_store<bf16, D>(o == 0 ? a.dk : a.dv, row, acc[o], f, hh, a.s.out_f32);
       else
-        win_store<bf16, D>(sums, (part * 2 + o) * rows + ((size_t)b * span + j) * Hkv + g, acc[o], f, hh, true);
+        win_store<bf16, D>(it.sums<D>(a, cut), it.row(a, o, b, j, g), acc[o], f, hh, true);
     }
 }
 
-// dK and dV from the parts' sums, in order, of the keys j0 .. j1 - 1; four
-// entries per thread.
-template <int D>
-__global__ __launch_bounds__(256) void hyb_win_sum_kernel(WindowArgs a, const float* sums, int parts, int span, int j0,
-                                                          int j1) {
-  const size_t per = (size_t)a.s.Hkv * D / 4, n = (size_t)a.s.B * (j1 - j0) * per, all = (size_t)a.s.B * span * per;
+// dK and dV from the parts' sums, in order; four entries per thread.  Keys from
+// `end` on have one part, written in place.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void hyb_win_sum_kernel(WindowArgs a, WinParts cut, int end) {
+  const size_t per = (size_t)a.s.Hkv * D / 4, n = (size_t)a.s.B * end * per;
   for (size_t x = (size_t)blockIdx.x * 256 + threadIdx.x; x < 2 * n; x += (size_t)gridDim.x * 256) {
     const int o = x >= n;
     const size_t y = x - o * n, bj = y / per, c = y % per;
-    const size_t b = bj / (j1 - j0), j = j0 + bj % (j1 - j0);
-    const f32x4* src = reinterpret_cast<const f32x4*>(sums) + o * all + (b * span + j) * per + c;
+    const int b = (int)(bj / end), j = (int)(bj % end);
+    const bool sink = j < cut.ns * kWinKeys;
+    const int parts = sink ? cut.ps : cut.p, span = sink ? cut.ns * kWinKeys : a.T;
+    const f32x4* src = reinterpret_cast<const f32x4*>(a.sums) + (sink ? 0 : cut.sink_rows() * 2 * a.s.B * per) +
+                       (((size_t)o * a.s.B + b) * span + j) * per + c;
     f32x4 s = {};
-    for (int p = 0; p < parts; ++p) s += src[2 * all * p];
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p) s += src[(size_t)2 * a.s.B * span * per * p];
     const float v[4] = {s[0], s[1], s[2], s[3]};
-    store_out4<bf16>(o ? a.dv : a.dk, 4 * ((b * a.T + j) * per + c), v, a.s.out_f32);
+    store_out4<T>(o ? a.dv : a.dk, 4 * (((size_t)b * a.T + j) * per + c), v, a.s.out_f32);
   }
 }
 
@@ -1064,66 +1096,78 @@ static hipError_t win_prefill_f32_go(const WindowArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <int D>
-static hipError_t win_backward_f32_go(const WindowArgs& a, hipStream_t st) {
-  const int wgs = win_wgs(a), kwgs = (a.T + kWinWaves * kTile - 1) / (kWinWaves * kTile);
-  hipLaunchKernelGGL(hyb_win_dq_kernel<D>, dim3((unsigned)(a.s.B * a.s.Hkv * wgs)), dim3(kWave * kWinWaves), 0, st, a,
-                     wgs);
-  hipLaunchKernelGGL(hyb_win_dkv_kernel<D>, dim3((unsigned)(a.s.B * a.s.Hkv * kwgs)), dim3(kWave * kWinWaves), 0, st, a);
-  return hipGetLastError();
-}
-
-// The cut: about two workgroups per CU (512, one at a time), each of 16 query
-// tiles or more; the sinks' keys in parts as long as the others', as long as those
+// The cut.  A part costs its start and end (`fixed` query tiles' time) besides its
+// tiles, the chip takes 256 workgroups at a time, and more parts than one cost
+// the sums' traffic and a launch; p is the number with the least estimated time,
+// in units of a query tile (bf16: 0.35 us a tile, two at a time in a workgroup).
+// The sinks' keys are cut into parts as long as the others', as long as those
 // are at most 16 per (request, KV head) and 512 in all.
 static int win_sink_parts(const Shape& s) { return (int)std::min<long>(16, 512 / std::max<long>(1, (long)s.B * s.Hkv)); }
+static int win_most_parts(const Shape& s, int T) {
+  const long all = (long)s.B * s.Hkv * ((T + kWinKeys - 1) / kWinKeys);
+  const long every = ((long)T + kTile - 1) / kTile * (s.Hq / s.Hkv);
+  return (int)std::max<long>(1, std::min<long>({16, 1024 / all, every / 8}));
+}
 static WinParts win_cut(const Shape& s, int T, int window, int n_sinks) {
-  const int wk = 4 * kTile, G = s.Hq / s.Hkv;
+  const int G = s.Hq / s.Hkv;
   WinParts c;
-  c.wgs = (T + wk - 1) / wk;
-  c.ns = std::min(c.wgs, (std::min(n_sinks, T) + wk - 1) / wk);
-  const long all = (long)s.B * s.Hkv * c.wgs, every = ((long)T + kTile - 1) / kTile * G;
-  const long seen = std::min<long>(every, (((long)window + s.L + wk + kTile - 1) / kTile + 1) * G);  // tiles of a list
-  c.p = (int)std::max<long>(1, std::min<long>((512 + all - 1) / all, seen / 16));
-  const long each = (seen + c.p - 1) / c.p;
+  c.wgs = (T + kWinKeys - 1) / kWinKeys;
+  c.ns = std::min(c.wgs, (std::min(n_sinks, T) + kWinKeys - 1) / kWinKeys);
+  const double all = (double)s.B * s.Hkv * c.wgs, every = std::ceil(T / 32.0);
+  const double seen = std::min(every, std::ceil(((double)window + s.L + kWinKeys) / kTile) + 1);  // tiles of a head
+  const double mean = seen - seen * seen / (2 * every);  // (the last keys' lists end early)
+  const bool f32 = s.dtype != 1;
+  const double fixed = f32 ? 2 : 16, sum = (double)s.B * T * s.Hkv * s.D * (f32 ? 1e-6 : 1e-5), launch = f32 ? 2 : 14;
+  double best = 0;
+  for (int p = 1; p <= win_most_parts(s, T); ++p) {
+    const double t = std::max(fixed + seen * G / p, all * (p * fixed + mean * G) / 256) + (p > 1 ? launch + p * sum : 0);
+    if (p == 1 || t < best) {
+      best = t;
+      c.p = p;
+    }
+  }
+  const int each = (int)std::ceil(seen * G / c.p);
   c.ps = c.p;
-  if (c.ns > 0 && every >= 2 * each)
-    c.ps = (int)std::max<long>(c.p, std::min<long>((every + each - 1) / each, win_sink_parts(s) / c.ns));
+  if (c.ns > 0 && every * G >= 2 * each)
+    c.ps = (int)std::max<long>(c.p, std::min<long>((long)((every * G + each - 1) / each), win_sink_parts(s) / c.ns));
   return c;
 }
-static size_t win_stats_bytes(const Shape& s, int T) { return (size_t)s.B * s.Hq * win_tp(T) * 32; }
-// Partial sums at most, for any window and number of sinks: p is largest for a
-// full window; the sinks' workgroups times their parts are within
-// win_sink_parts, or have p parts as every workgroup (one workgroup's keys see
-// one list, with or without sinks).
+// bf16: the rows' statistics; fp32: delta.
+static size_t win_stats_bytes(const Shape& s, int T) {
+  return s.dtype == 1 ? (size_t)s.B * s.Hq * win_tp(T) * 32 : ((size_t)s.B * s.Hq * T * sizeof(float) + 255) / 256 * 256;
+}
+// Partial sums at most, for any window and number of sinks: the sinks'
+// workgroups times their parts are within win_sink_parts, or have p parts as every
+// workgroup (one workgroup's keys see one list, with or without sinks).
 static size_t win_sums_bytes(const Shape& s, int T) {
-  const WinParts c = win_cut(s, T, T, 0);
-  const long sinks = c.wgs > 1 && win_sink_parts(s) > 1 ? win_sink_parts(s) : 0;
-  const long tiles = c.p > 1 ? std::max((long)c.wgs * c.p, sinks) : sinks;
-  return (size_t)(tiles * 4 * kTile + (c.p > 1 ? (long)c.p * T : 0)) * 2 * s.B * s.Hkv * s.D * sizeof(float);
+  const int wgs = (T + kWinKeys - 1) / kWinKeys, p = win_most_parts(s, T), sp = win_sink_parts(s);
+  const long sinks = wgs > 1 && sp > 1 ? sp : 0;
+  const long tiles = p > 1 ? std::max((long)wgs * p, sinks) : sinks;
+  return (size_t)(tiles * kWinKeys + (p > 1 ? (long)p * T : 0)) * 2 * s.B * s.Hkv * s.D * sizeof(float);
 }
 
-template <int D>
-static hipError_t win_backward_ring_go(WindowArgs a, hipStream_t st) {
+template <typename T, int D>
+static hipError_t win_backward_go(WindowArgs a, hipStream_t st) {
   const WinParts cut = win_cut(a.s, a.T, a.window, a.n_sinks);
   a.sums = (float*)((char*)a.ws + win_stats_bytes(a.s, a.T));
   // (what the workspace was sized for, whatever window and n_sinks are)
   if ((size_t)cut.rows(a.T) * 2 * a.s.B * a.s.Hkv * D * sizeof(float) > win_sums_bytes(a.s, a.T))
     return hipErrorInvalidValue;
   const int wgs = win_wgs(a);
-  hipLaunchKernelGGL(hyb_win_dq_ring_kernel<D>, dim3((unsigned)(a.s.B * a.s.Hkv * wgs)), dim3(kWave * kWinWaves), 0, st,
-                     a, wgs);
-  hipLaunchKernelGGL(hyb_win_dkv_ring_kernel<D>, dim3((unsigned)(a.s.B * a.s.Hkv * cut.items())),
-                     dim3(kWave * kWinKeyWaves), 0, st, a, cut);
-  const int sinks = std::min(cut.ns * 4 * kTile, a.T);  // keys of the sinks' workgroups
-  auto sum = [&](const float* sums, int parts, int span, int j0, int j1) {
-    if (parts == 1 || j0 >= j1) return;
-    const long n = (long)a.s.B * (j1 - j0) * a.s.Hkv * D / 2;
-    hipLaunchKernelGGL(hyb_win_sum_kernel<D>, dim3((unsigned)std::min<long>((n + 255) / 256, 4096)), dim3(256), 0, st, a,
-                       sums, parts, span, j0, j1);
-  };
-  sum(a.sums, cut.ps, cut.ns * 4 * kTile, 0, sinks);
-  sum(a.sums + cut.sink_rows() * 2 * a.s.B * a.s.Hkv * D, cut.p, a.T, sinks, a.T);
+  const dim3 gq((unsigned)(a.s.B * a.s.Hkv * wgs)), gk((unsigned)(a.s.B * a.s.Hkv * cut.items()));
+  if constexpr (sizeof(T) == 2) {
+    hipLaunchKernelGGL(hyb_win_dq_ring_kernel<D>, gq, dim3(kWave * kWinWaves), 0, st, a, wgs);
+    hipLaunchKernelGGL(hyb_win_dkv_ring_kernel<D>, gk, dim3(kWave * kWinKeyWaves), 0, st, a, cut);
+  } else {
+    hipLaunchKernelGGL(hyb_win_dq_kernel<D>, gq, dim3(kWave * kWinWaves), 0, st, a, wgs);
+    hipLaunchKernelGGL(hyb_win_dkv_kernel<D>, gk, dim3(kWave * kWinWaves), 0, st, a, cut);
+  }
+  const int end = cut.p > 1 ? a.T : cut.ps > 1 ? std::min(cut.ns * kWinKeys, a.T) : 0;
+  if (end > 0) {
+    const long n = (long)a.s.B * end * a.s.Hkv * D / 2;
+    hipLaunchKernelGGL((hyb_win_sum_kernel<T, D>), dim3((unsigned)std::min<long>((n + 255) / 256, 4096)), dim3(256), 0,
+                       st, a, cut, end);
+  }
   return hipGetLastError();
 }
 
@@ -1133,8 +1177,8 @@ hipError_t launch_window_prefill(const WindowArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_window_backward(const WindowArgs& a, hipStream_t st) {
-  if (a.s.dtype == 1) return a.s.D == 64 ? win_backward_ring_go<64>(a, st) : win_backward_ring_go<128>(a, st);
-  return a.s.D == 64 ? win_backward_f32_go<64>(a, st) : win_backward_f32_go<128>(a, st);
+  if (a.s.dtype == 1) return a.s.D == 64 ? win_backward_go<bf16, 64>(a, st) : win_backward_go<bf16, 128>(a, st);
+  return a.s.D == 64 ? win_backward_go<float, 64>(a, st) : win_backward_go<float, 128>(a, st);
 }
 
 // Workgroups of the largest launch (the grid's limit is checked by the caller).
@@ -1144,7 +1188,6 @@ long window_workgroups(const Shape& s, int T) {
 }
 
 size_t window_backward_ws_bytes(const Shape& s, int T) {
-  if (s.dtype != 1) return (size_t)s.B * s.Hq * T * sizeof(float);  // delta
   return win_stats_bytes(s, T) + win_sums_bytes(s, T);
 }
 

@@ -190,3 +190,13 @@ def test_streams_and_replays():
         wb = back(*w)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(o + g, w + wb)), lens
+
+
+@pytest.mark.parametrize("B,T,Hq,Hkv,d,L,window,sinks,dtype,lens", [
+    (1, 1500, 4, 1, 64, 1, 100, 3, BF, [1400]), (1, 1000, 8, 2, 128, 32, 1000, 0, BF, None),
+    (2, 700, 2, 2, 64, 16, 64, 300, BF, [700, 130]), (1, 900, 6, 1, 128, 8, 31, 150, FL, [890]),
+    (1, 1300, 3, 1, 64, 32, 1300, 0, FL, None)])
+def test_backward_in_parts(B, T, Hq, Hkv, d, L, window, sinks, dtype, lens):
+    """Few keys and many queries: the lists of queries are cut into parts, the
+    sinks' into more of them."""
+    test_backward(B, T, Hq, Hkv, d, L, window, sinks, dtype, lens)
