@@ -854,15 +854,17 @@ __global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_dq_ring_kernel(Wi
                      a.s.out_f32);
 }
 
-// A workgroup owns 128 keys and has two halves of four waves, a wave 32 keys of
-// its half: the halves take the query tiles in turn and their sums are joined
-// in LDS at the end.  (So that two waves share a SIMD with the LDS of one
-// workgroup: dK and dV take 128 registers, K 32, the scores and dP 32; V is read
-// from LDS.)
-constexpr int kWinKeyWaves = 8;
+// A workgroup owns 128 keys, a wave 32 of them.  At d = 128 it has two halves of
+// four waves, which take the query tiles in turn and join their sums in LDS at
+// the end, so that two waves share a SIMD with the LDS of one workgroup (dK and dV
+// take 128 registers, K 32, the scores and dP 32; V is read from LDS).  At d = 64
+// three workgroups of four waves fit a CU.
+template <int D>
+constexpr int kWinHalves = D == 128 ? 2 : 1;
 
 template <int D>
-__global__ __launch_bounds__(kWave* kWinKeyWaves, 2) void hyb_win_dkv_ring_kernel(WindowArgs a, WinParts cut) {
+__global__ __launch_bounds__(kWave * 4 * kWinHalves<D>, 2) void hyb_win_dkv_ring_kernel(WindowArgs a, WinParts cut) {
+  constexpr int H = kWinHalves<D>;
   typedef Mma<bf16> M;
   typedef M::op_t op_t;
   typedef RowColTile<D> WT;
@@ -873,11 +875,11 @@ __global__ __launch_bounds__(kWave* kWinKeyWaves, 2) void hyb_win_dkv_ring_kerne
     bf16 q[kTile * D], d[kTile * D], st[kTile * 16];
   };
   struct Loop {
-    Slot ring[2][R];
+    Slot ring[H][R];
     bf16 v[4][kTile * D];
   };
-  struct Join {
-    f32x4 x[2][4][NCT * 4][kWave];
+  struct Join {  // (the other half's dK or dV)
+    f32x4 x[H == 2 ? 2 : 0][4][NCT * 4][kWave];
   };
   union Smem {
     Loop loop;
@@ -902,21 +904,21 @@ __global__ __launch_bounds__(kWave* kWinKeyWaves, 2) void hyb_win_dkv_ring_kerne
   if (w0 < len) {  // uniform
     const size_t qs = (size_t)Hq * D, ks_ = (size_t)Hkv * D;
     // query tiles t0 .. t0 + nq - 1 of every head, of which this part takes
-    // ntiles from first on, a half every second
+    // ntiles from first on, a half every H-th
     const WinQueries all(a, len, w0, min(w0 + kWinKeys, len));
     const int t0 = all.q0 / kTile, nq = (all.q1 + kTile - 1) / kTile - t0;
     const int first = (int)((long)nq * G * it.part / it.parts);
     const int ntiles = (int)((long)nq * G * (it.part + 1) / it.parts) - first;
-    const int nsteps = (ntiles + 1) / 2, mysteps = (ntiles + 1 - half) / 2;
+    const int nsteps = (ntiles + H - 1) / H, mysteps = (ntiles + H - 1 - half) / H;
     const WinKey mine(a, len, min(j, len - 1));
     // query tiles that every key of the wave is seen by: f0 <= i0 and i0 + 32 <= f1
     const int jl = max(min(j0 + kTile, len) - 1, 0);
     const int f0 = WinKey(a, len, jl).q0, f1 = WinKey(a, len, min(max(j0, a.n_sinks), jl)).q1;
     const WT wt(lane);
-    // this half's share of V: tiles 2 half and 2 half + 1 of the keys, a copy per wave and round
+    // this half's share of V: 4 / H of the keys' tiles, a copy per wave and round
 #pragma unroll
-    for (int u = 0; u < 2 * WT::IK / 4; ++u) {
-      const int c = u * 4 + w, t = 2 * half + c / WT::IK, r = c % WT::IK * WT::RPI + lane / WT::CPR;
+    for (int u = 0; u < WT::IK / H; ++u) {
+      const int c = u * 4 + w, t = 4 / H * half + c / WT::IK, r = c % WT::IK * WT::RPI + lane / WT::CPR;
       const bf16* src = (const bf16*)a.v + ((size_t)b * a.T * Hkv + g) * D + min(w0 + t * kTile + r, len - 1) * ks_ +
                         (lane % WT::CPR ^ WT::swz(r)) * WT::EPC;
       __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
@@ -960,7 +962,7 @@ __global__ __launch_bounds__(kWave* kWinKeyWaves, 2) void hyb_win_dkv_ring_kerne
       const float* st = (const float*)a.ws + (((size_t)b * Hq + inh) * Tp + i0) * 8 + w * kWave + lane;
       __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)st,
                                        (__attribute__((address_space(3))) void*)((float*)s.st + w * kWave), 4, 0, 0);
-      inq += 2;
+      inq += H;
       while (inq >= nq) inq -= nq, ++inh;
     };
     auto compute = [&](const Slot& s) __attribute__((always_inline)) {
@@ -978,7 +980,7 @@ __global__ __launch_bounds__(kWave* kWinKeyWaves, 2) void hyb_win_dkv_ring_kerne
           sc[e] = i >= mine.q0 && i < mine.q1 ? sc[e] : -INFINITY;
         }
       }
-      cq += 2;
+      cq += H;
       while (cq >= nq) cq -= nq;
       op_t pop[KL], sop[KL];
 #pragma unroll
@@ -1016,36 +1018,38 @@ __global__ __launch_bounds__(kWave* kWinKeyWaves, 2) void hyb_win_dkv_ring_kerne
       if (n + 1 < nsteps) step(n + 1, std::integral_constant<int, 1>{});
       if (n + 2 < nsteps) step(n + 2, std::integral_constant<int, 2>{});
     }
-    // The halves' sums: each hands over one of dK and dV and keeps the other.
-    lds_barrier_nodrain();
+    if constexpr (H == 2) {
+      // The halves' sums: each hands over one of dK and dV and keeps the other.
+      lds_barrier_nodrain();
 #pragma unroll
-    for (int o = 0; o < 2; ++o)
-      if (o != half)
+      for (int o = 0; o < 2; ++o)
+        if (o != half)
 #pragma unroll
-        for (int ct = 0; ct < NCT; ++ct)
+          for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            sh.join.x[o][w][ct * 4 + e][lane] = f32x4{acc[o][ct][4 * e], acc[o][ct][4 * e + 1], acc[o][ct][4 * e + 2],
-                                                      acc[o][ct][4 * e + 3]};
-    lds_barrier_nodrain();
+            for (int e = 0; e < 4; ++e)
+              sh.join.x[o][w][ct * 4 + e][lane] = f32x4{acc[o][ct][4 * e], acc[o][ct][4 * e + 1], acc[o][ct][4 * e + 2],
+                                                        acc[o][ct][4 * e + 3]};
+      lds_barrier_nodrain();
 #pragma unroll
-    for (int o = 0; o < 2; ++o)
-      if (o == half)
+      for (int o = 0; o < 2; ++o)
+        if (o == half)
 #pragma unroll
-        for (int ct = 0; ct < NCT; ++ct)
+          for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const f32x4 y = sh.join.x[o][w][ct * 4 + e][lane];
+            for (int e = 0; e < 4; ++e) {
+              const f32x4 y = sh.join.x[o][w][ct * 4 + e][lane];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) acc[o][ct][4 * e + k] += y[k];
-          }
+              for (int k = 0; k < 4; ++k) acc[o][ct][4 * e + k] += y[k];
+            }
+    }
   }
   if (j >= a.T) return;
   const size_t row = ((size_t)b * a.T + j) * Hkv + g;
-  const float f = j >= len ? 0.0f : half == 0 ? 1.0f / sqrtf((float)D) : 1.0f;
 #pragma unroll
   for (int o = 0; o < 2; ++o)
-    if (o == half) {
+    if (H == 1 || o == half) {
+      const float f = j >= len ? 0.0f : o == 0 ? 1.0f / sqrtf((float)D) : 1.0f;
       if (it.parts == 1)
         win_store<bf16, D>(o == 0 ? a.dk : a.dv, row, acc[o], f, hh, a.s.out_f32);
       else
@@ -1097,9 +1101,10 @@ static hipError_t win_prefill_f32_go(const WindowArgs& a, hipStream_t st) {
 }
 
 // The cut.  A part costs its start and end (`fixed` query tiles' time) besides its
-// tiles, the chip takes 256 workgroups at a time, and more parts than one cost
-// the sums' traffic and a launch; p is the number with the least estimated time,
-// in units of a query tile (bf16: 0.35 us a tile, two at a time in a workgroup).
+// tiles, the chip works through 256 lists at full speed (bf16 at d = 64: 512), and
+// more parts than one cost the sums' traffic and a launch; p is the number
+// with the least estimated time, in units of a query tile (bf16: 0.35 us, or 0.7
+// for the workgroups of d = 64, which take one tile at a time).
 // The sinks' keys are cut into parts as long as the others', as long as those
 // are at most 16 per (request, KV head) and 512 in all.
 static int win_sink_parts(const Shape& s) { return (int)std::min<long>(16, 512 / std::max<long>(1, (long)s.B * s.Hkv)); }
@@ -1117,10 +1122,11 @@ static WinParts win_cut(const Shape& s, int T, int window, int n_sinks) {
   const double seen = std::min(every, std::ceil(((double)window + s.L + kWinKeys) / kTile) + 1);  // tiles of a head
   const double mean = seen - seen * seen / (2 * every);  // (the last keys' lists end early)
   const bool f32 = s.dtype != 1;
-  const double fixed = f32 ? 2 : 16, sum = (double)s.B * T * s.Hkv * s.D * (f32 ? 1e-6 : 1e-5), launch = f32 ? 2 : 14;
+  const double unit = f32 ? 3.5 : s.D == 64 ? 0.7 : 0.35, lists = !f32 && s.D == 64 ? 512 : 256;
+  const double fixed = 5.5 / unit, launch = 5 / unit, sum = (double)s.B * T * s.Hkv * s.D * 3.5e-6 / unit;
   double best = 0;
   for (int p = 1; p <= win_most_parts(s, T); ++p) {
-    const double t = std::max(fixed + seen * G / p, all * (p * fixed + mean * G) / 256) + (p > 1 ? launch + p * sum : 0);
+    const double t = std::max(fixed + seen * G / p, all * (p * fixed + mean * G) / lists) + (p > 1 ? launch + p * sum : 0);
     if (p == 1 || t < best) {
       best = t;
       c.p = p;
@@ -1157,7 +1163,7 @@ static hipError_t win_backward_go(WindowArgs a, hipStream_t st) {
   const dim3 gq((unsigned)(a.s.B * a.s.Hkv * wgs)), gk((unsigned)(a.s.B * a.s.Hkv * cut.items()));
   if constexpr (sizeof(T) == 2) {
     hipLaunchKernelGGL(hyb_win_dq_ring_kernel<D>, gq, dim3(kWave * kWinWaves), 0, st, a, wgs);
-    hipLaunchKernelGGL(hyb_win_dkv_ring_kernel<D>, gk, dim3(kWave * kWinKeyWaves), 0, st, a, cut);
+    hipLaunchKernelGGL(hyb_win_dkv_ring_kernel<D>, gk, dim3(kWave * 4 * kWinHalves<D>), 0, st, a, cut);
   } else {
     hipLaunchKernelGGL(hyb_win_dq_kernel<D>, gq, dim3(kWave * kWinWaves), 0, st, a, wgs);
     hipLaunchKernelGGL(hyb_win_dkv_kernel<D>, gk, dim3(kWave * kWinWaves), 0, st, a, cut);
