@@ -45,18 +45,26 @@ __device__ inline float row_sum(float x) {
   return x;
 }
 
-// 8 entries of a row as two pieces of four, at p0 and p1.
+// 8 entries of a row as two pieces of four, at p0 and p1: as loaded (so that a
+// load can be on its way while others are used), and as fp32.
 template <typename T>
-__device__ inline void load_pieces(const T* p0, const T* p1, float (&x)[8]) {
-  if constexpr (sizeof(T) == 4) {
-    const f32x4 a = *reinterpret_cast<const f32x4*>(p0), b = *reinterpret_cast<const f32x4*>(p1);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
-  } else {
-    const bf16x4 a = *reinterpret_cast<const bf16x4*>(p0), b = *reinterpret_cast<const bf16x4*>(p1);
+struct Pieces {
+  typedef T piece_t __attribute__((ext_vector_type(4)));
+  piece_t a = {}, b = {};
+  __device__ inline void load(const T* p0, const T* p1) {
+    a = *reinterpret_cast<const piece_t*>(p0);
+    b = *reinterpret_cast<const piece_t*>(p1);
+  }
+  __device__ inline void get(float (&x)[8]) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = (float)a[i], x[4 + i] = (float)b[i];
   }
+};
+template <typename T>
+__device__ inline void load_pieces(const T* p0, const T* p1, float (&x)[8]) {
+  Pieces<T> p;
+  p.load(p0, p1);
+  p.get(x);
 }
 template <typename T>
 __device__ inline void store_pieces(T* p0, T* p1, const float (&x)[8]) {
@@ -155,20 +163,24 @@ __global__ __launch_bounds__(kWave* kRopeWaves) void hyb_rope_kernel(RopeArgs a,
       if (slot >= a.n_rows) slot = -1;
     }
     const int pos = a.positions[tok];
-    bool ready = false;
+    Pieces<T> next;
+    auto load = [&](int gr) __attribute__((always_inline)) {
+      const int h = gr * HPG + lane / LPR;
+      const bool isq = h < a.Hq, isv = PAGED && h >= a.Hq + a.Hkv;
+      const T* row = isq   ? (const T*)a.q + tok * a.q_stride + h * D
+                     : isv ? (const T*)a.v + tok * a.v_stride + (h - a.Hq - a.Hkv) * D
+                           : (const T*)a.k + tok * a.k_stride + (h - a.Hq) * D;
+      if (h < heads) next.load(row + t.e0, row + t.e1);
+    };
+    load(g0);
+    t.at(pos, a.rot_scale);
     for (int gr = g0; gr < g1; ++gr) {
       const int h = gr * HPG + lane / LPR;
       const bool live = h < heads, isq = h < a.Hq, isv = PAGED && h >= a.Hq + a.Hkv;
       const int hk = isv ? h - a.Hq - a.Hkv : h - a.Hq;
-      float x[8] = {};
-      if (live) {
-        const T* row = isq   ? (const T*)a.q + tok * a.q_stride + h * D
-                       : isv ? (const T*)a.v + tok * a.v_stride + hk * D
-                             : (const T*)a.k + tok * a.k_stride + hk * D;
-        load_pieces(row + t.e0, row + t.e1, x);
-      }
-      if (!ready) t.at(pos, a.rot_scale);  // behind the first loads
-      ready = true;
+      float x[8];
+      next.get(x);
+      if (gr + 1 < g1) load(gr + 1);
       float ss = 0.0f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) ss += x[i] * x[i];
@@ -215,24 +227,29 @@ __global__ __launch_bounds__(kWave* kRopeWaves) void hyb_rope_backward_kernel(Ro
     const long tok = un / u.parts;
     const int g0 = (int)(un - tok * u.parts) * u.per, g1 = min(g0 + u.per, u.groups);
     const int pos = a.positions[tok];
-    bool ready = false;
+    Pieces<T> nx;
+    Pieces<G> ng;
+    auto load = [&](int gr) __attribute__((always_inline)) {
+      const int h = gr * HPG + lane / LPR, hk = h - a.Hq;
+      const bool isq = h < a.Hq;
+      if (h >= heads) return;
+      const G* gp = isq ? (const G*)a.dq_out + ((size_t)tok * a.Hq + h) * D
+                        : (const G*)a.dk_out + ((size_t)tok * a.Hkv + hk) * D;
+      ng.load(gp + t.e0, gp + t.e1);
+      const T* row = isq ? (const T*)a.q + tok * a.q_stride + h * D : (const T*)a.k + tok * a.k_stride + hk * D;
+      if (isq ? a.wq != nullptr : a.wk != nullptr) nx.load(row + t.e0, row + t.e1);
+    };
+    load(g0);
+    t.at(pos, a.rot_scale);
     for (int gr = g0; gr < g1; ++gr) {
       const int h = gr * HPG + lane / LPR;
       const bool live = h < heads, isq = h < a.Hq;
       const int hk = h - a.Hq;
       const bool norm = isq ? a.wq != nullptr : a.wk != nullptr;
-      float x[8] = {}, g[8] = {};
-      if (live) {
-        const G* gp = isq ? (const G*)a.dq_out + ((size_t)tok * a.Hq + h) * D
-                          : (const G*)a.dk_out + ((size_t)tok * a.Hkv + hk) * D;
-        load_pieces(gp + t.e0, gp + t.e1, g);
-        if (norm) {
-          const T* row = isq ? (const T*)a.q + tok * a.q_stride + h * D : (const T*)a.k + tok * a.k_stride + hk * D;
-          load_pieces(row + t.e0, row + t.e1, x);
-        }
-      }
-      if (!ready) t.at(pos, a.rot_scale);
-      ready = true;
+      float x[8], g[8];
+      nx.get(x);
+      ng.get(g);
+      if (gr + 1 < g1) load(gr + 1);
       t.template apply<true>(g);
       float ss = 0.0f, dot = 0.0f;
 #pragma unroll
