@@ -1021,138 +1021,115 @@ __global__ __launch_bounds__(kWave* NG, D == 64 && NG == 8 ? 4 : 2) void hyb_sp_
   }
 }
 
-// A window's few queries (bf16, the G heads' L queries within 32: decoding):
-// they are the columns of one tile of scores, so a wave answers all of them
-// and the four waves of a workgroup take the range's tiles in turn, each with
-// copies of its own (two slots of K and V, no barrier in the loop) and sums of its
-// own, joined in LDS at the end.  With a wave per head, as above, each has one or
-// a few columns of its tile filled, and the loop is four times as many dependent
-// steps.
+// ---- kernels of a window ------------------------------------------------------
+//
+// A range's tiles for a workgroup of the kernels below: where they are and how a
+// wave copies rows of one.  `pages` is LDS for kMaxRangePages numbers.
 template <int D>
-__global__ __launch_bounds__(kWave * 4) void hyb_sp_token_kernel(SoftmaxPrefixArgs a, SpCut cut) {
-  typedef Mma<bf16> M;
-  typedef M::op_t op_t;
+struct SpTiles {
   typedef RowColTile<D> RT;
-  constexpr int E = M::E, KW = M::KW, KD = D / KW, KL = kTile / KW, NCT = D / kTile, NW = 4;
-  struct alignas(16) Slot {
-    bf16 k[kTile * D], v[kTile * D];
-  };
-  __shared__ Slot ring[NW][2];
-  __shared__ float refs[NW][kTile], sums[NW][kTile];
-  __shared__ int pages[kMaxRangePages];
+  const bf16 *kc, *vc, *kb, *vb;  // cache pools and block at the KV head
+  SpSeen seen;
+  int t0, nt, hi, P, page_shift, p0, pa, pskip;
+  int kstride;  // elements from a token to the next
+  const int* pages;
 
-  const int tid = threadIdx.x, lane = tid & (kWave - 1);
-  const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const int li = lane & 31, hh = lane >> 5;
-  const int Hq = a.s.Hq, Hkv = a.s.Hkv, L = a.s.L, G = Hq / Hkv;
-  const int g = blockIdx.x % Hkv, r = blockIdx.x / Hkv;
-  static_assert(sizeof(ring) >= kPlanInts * sizeof(int), "the plan's scratch fits the slots");
-  const SpRange rg = sp_range<true>(a, sp_plan<true>(a, cut, reinterpret_cast<int*>(&ring)), r, lane);
-  if (rg.b < 0) return;  // uniform: past the plan's last range
-  const int b = rg.b, lo = rg.lo, hi = rg.hi;
-  const int Lb = sp_block<true>(a, b), P = sp_keys<true>(a, b) - Lb;
-  const SpSeen seen = sp_seen<true>(a, b);
-  const size_t kstride = (size_t)Hkv * D;
-  // this lane's column: query i of head h
-  const int i = li % L, h = g * G + li / L;
-  const bool col = li < G * L && i < Lb;
-  op_t qop[KD];
-  {
-    const bf16* row = (const bf16*)a.q + (((size_t)b * L + (col ? i : 0)) * Hq + (col ? h : g * G)) * D + hh * E;
-#pragma unroll
-    for (int ks = 0; ks < KD; ++ks) qop[ks] = keep_if<bf16>(col, load_op<bf16>(row + ks * KW));
-  }
-  const bf16* kc = (const bf16*)a.k_cache + g * D;
-  const bf16* vc = (const bf16*)a.v_cache + g * D;
-  const bf16* kb = (const bf16*)a.k + ((size_t)b * L * Hkv + g) * D;
-  const bf16* vb = (const bf16*)a.v + ((size_t)b * L * Hkv + g) * D;
-  // The pages of the range's cached keys, as in the ring kernel.
-  const int p0 = lo >> a.page_shift;
-  int pa = 0x7fffffff, pskip = 0;
-  if (seen.skip > 0 && rg.t0 < seen.st && rg.t0 + rg.nt > seen.st) {
-    pa = (seen.st * kTile - 1) >> a.page_shift;
-    pskip = max(0, ((seen.st + seen.skip) * kTile >> a.page_shift) - pa - 1);
-  }
-  {
-    const int32_t* ptab = a.page_table + (size_t)b * a.max_pages;
+  // All threads of the workgroup; ends with a barrier.
+  __device__ inline SpTiles(const SoftmaxPrefixArgs& a, const SpRange& rg, int g, int P_, int* lds) {
+    kc = (const bf16*)a.k_cache + g * D;
+    vc = (const bf16*)a.v_cache + g * D;
+    kb = (const bf16*)a.k + ((size_t)rg.b * a.s.L * a.s.Hkv + g) * D;
+    vb = (const bf16*)a.v + ((size_t)rg.b * a.s.L * a.s.Hkv + g) * D;
+    seen = sp_seen<true>(a, rg.b);
+    t0 = rg.t0, nt = rg.nt, hi = rg.hi, P = P_;
+    page_shift = a.page_shift;
+    kstride = a.s.Hkv * D;
+    pages = lds;
+    // the pages of the range's cached keys, as in the ring kernel
+    p0 = rg.lo >> page_shift;
+    pa = 0x7fffffff;
+    pskip = 0;
+    if (seen.skip > 0 && t0 < seen.st && t0 + nt > seen.st) {
+      pa = (seen.st * kTile - 1) >> page_shift;
+      pskip = max(0, ((seen.st + seen.skip) * kTile >> page_shift) - pa - 1);
+    }
+    const int32_t* ptab = a.page_table + (size_t)rg.b * a.max_pages;
     const int chi = min(hi, P);
-    const int np = chi > lo ? ((chi - 1) >> a.page_shift) - p0 + 1 - pskip : 0;
-    for (int e = tid; e < np; e += kWave * NW)
-      pages[e] = sp_page(a, ptab, (p0 + e + (p0 + e > pa ? pskip : 0)) << a.page_shift);
+    const int np = chi > rg.lo ? ((chi - 1) >> page_shift) - p0 + 1 - pskip : 0;
+    for (int e = threadIdx.x; e < np; e += blockDim.x)
+      lds[e] = sp_page(a, ptab, (p0 + e + (p0 + e > pa ? pskip : 0)) << page_shift);
     __syncthreads();
   }
-
-  const RT rt(lane);
-  int trow[RT::IK], tcol[RT::IK];
-#pragma unroll
-  for (int u = 0; u < RT::IK; ++u) {
-    trow[u] = u * RT::RPI + lane / RT::CPR;
-    tcol[u] = (lane % RT::CPR ^ RT::swz(trow[u])) * RT::EPC;
+  // First key of the range's tile i.
+  __device__ inline int first_key(int i) const { return seen.tile(t0 + i) * kTile; }
+  // This lane's row and entry in copy u of a tile.
+  __device__ static inline int copy_row(int u, int lane) { return u * RT::RPI + lane / RT::CPR; }
+  __device__ static inline int copy_col(int u, int lane) {
+    return (lane % RT::CPR ^ RT::swz(copy_row(u, lane))) * RT::EPC;
   }
-  const int mine = (rg.nt - w + NW - 1) / NW;  // this wave's tiles
-  auto first_key = [&](int n) __attribute__((always_inline)) { return seen.tile(rg.t0 + w + NW * n) * kTile; };
-  auto issue = [&](int n, Slot& s) __attribute__((always_inline)) {
-    if (n >= mine) return;
-    const int j0 = first_key(n);
+  // Copies u0 .. u0 + N - 1 of K (kv = 0) or V of the tile at j0 into dst.
+  template <int N>
+  __device__ inline void copy(int kv, int j0, int u0, bf16* dst, int lane) const {
     ptrdiff_t shift = 0;  // from a row's place in its request to its place in the pools
     if (j0 < P) {
-      const int pi = j0 >> a.page_shift;
-      shift = ((ptrdiff_t)__builtin_amdgcn_readfirstlane(pages[pi - p0 - (pi > pa ? pskip : 0)]) - pi) << a.page_shift;
+      const int pi = j0 >> page_shift;
+      shift = ((ptrdiff_t)__builtin_amdgcn_readfirstlane(pages[pi - p0 - (pi > pa ? pskip : 0)]) - pi) << page_shift;
     }
-    if (j0 + kTile <= min(hi, P) && !seen.cuts(j0)) {
-      const ptrdiff_t at = (shift + j0) * (ptrdiff_t)kstride;
-      const int span = (int)(kTile * kstride * sizeof(bf16));
-      const __amdgpu_buffer_rsrc_t rk =
-          __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(kc + at), 0, span, kBufferWord3);
-      const __amdgpu_buffer_rsrc_t rv =
-          __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(vc + at), 0, span, kBufferWord3);
+    if (j0 + kTile <= min(hi, P) && !seen.cuts(j0)) {  // uniform: wholly in the cache and seen
+      const bf16* base = sp_pick(kv == 0, kc, vc) + (shift + j0) * (ptrdiff_t)kstride;
+      const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+          const_cast<bf16*>(base), 0, (int)(kTile * kstride * sizeof(bf16)), kBufferWord3);
 #pragma unroll
-      for (int u = 0; u < RT::IK; ++u)
-        buf_to_lds16(rk, s.k + u * RT::RPI * D, (int)((trow[u] * (int)kstride + tcol[u]) * sizeof(bf16)), 0);
-#pragma unroll
-      for (int u = 0; u < RT::IK; ++u)
-        buf_to_lds16(rv, s.v + u * RT::RPI * D, (int)((trow[u] * (int)kstride + tcol[u]) * sizeof(bf16)), 0);
+      for (int u = 0; u < N; ++u)
+        buf_to_lds16(rs, dst + (u0 + u) * RT::RPI * D,
+                     (int)((copy_row(u0 + u, lane) * kstride + copy_col(u0 + u, lane)) * sizeof(bf16)), 0);
     } else {
       // keys past the range and hidden ones read a visible row of the tile
 #pragma unroll
-      for (int kv = 0; kv < 2; ++kv)
-#pragma unroll
-        for (int u = 0; u < RT::IK; ++u) {
-          int j = min(j0 + trow[u], hi - 1);
-          j = seen.hides(j) ? seen.stand_in(j0) : j;
-          const bf16* base = sp_pick(j < P, kv == 0 ? kc : vc, kv == 0 ? kb : vb);
-          const bf16* row = base + (ptrdiff_t)(j < P ? shift + j : j - P) * (ptrdiff_t)kstride + tcol[u];
-          __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)row,
-                                           (__attribute__((address_space(3))) void*)((kv == 0 ? s.k : s.v) + u * RT::RPI * D),
-                                           16, 0, 0);
-        }
+      for (int u = 0; u < N; ++u) {
+        int j = min(j0 + copy_row(u0 + u, lane), hi - 1);
+        j = seen.hides(j) ? seen.stand_in(j0) : j;
+        const bf16* base = sp_pick(j < P, sp_pick(kv == 0, kc, vc), sp_pick(kv == 0, kb, vb));
+        const bf16* row = base + (ptrdiff_t)(j < P ? shift + j : j - P) * kstride + copy_col(u0 + u, lane);
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)row,
+                                         (__attribute__((address_space(3))) void*)(dst + (u0 + u) * RT::RPI * D), 16, 0, 0);
+      }
     }
-  };
-  // The weights' reference, in the log2 domain; finite, so that a wave without
-  // tiles weighs nothing.
-  const float scale = kLog2e / sqrtf((float)D);
+  }
+};
+
+// What a wave keeps of its 32 columns (queries): the weights' reference in the
+// log2 domain (finite, so that a wave without tiles weighs nothing; it moves only
+// when a maximum passes it by 2^8), their sum over the lane's rows, and the
+// weighted sums of V^T.
+template <int D>
+struct SpAcc {
+  typedef Mma<bf16> M;
+  static constexpr int KD = D / M::KW, KL = kTile / M::KW, NCT = D / kTile;
   float m = -1e30f, l = 0.0f;
   f32x16 acc[NCT];
+  __device__ inline SpAcc() {
 #pragma unroll
-  for (int ct = 0; ct < NCT; ++ct) acc[ct] = f32x16{};
-  auto compute = [&](int n, const Slot& s) __attribute__((always_inline)) {
+    for (int ct = 0; ct < NCT; ++ct) acc[ct] = f32x16{};
+  }
+  // Adds the tile at j0 (K, V in LDS); scale = log2(e) / sqrt(d).
+  __device__ inline void add(const SpTiles<D>& t, const RowColTile<D>& rt, int j0, const bf16* kt, const bf16* vt,
+                             const bf16x8 (&qop)[KD], float scale, int hh) {
     f32x16 sc = {};
 #pragma unroll
-    for (int ks = 0; ks < KD; ++ks) sc = M::mma(rt.row_op(s.k, ks), qop[ks], sc);
+    for (int ks = 0; ks < KD; ++ks) sc = M::mma(rt.row_op(kt, ks), qop[ks], sc);
     mma_settle<bf16>();
-    const int j0 = first_key(n);
-    if (j0 + kTile > hi || seen.cuts(j0)) {  // uniform
+    if (j0 + kTile > t.hi || t.seen.cuts(j0)) {  // uniform
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const int j = j0 + row_of(e, hh);
-        sc[e] = j < hi && !seen.hides(j) ? sc[e] : -INFINITY;
+        sc[e] = j < t.hi && !t.seen.hides(j) ? sc[e] : -INFINITY;
       }
     }
     float mt = sc[0];
 #pragma unroll
     for (int e = 1; e < 16; ++e) mt = fmaxf(mt, sc[e]);
     mt = fmaxf(mt, xor32(mt)) * scale;
-    // (the reference moves only when a maximum passes it by 2^8)
     if (__any(mt > m + 8.0f)) {
       mma_settle<bf16>();
       const float mn = mt > m + 8.0f ? mt : m;
@@ -1164,24 +1141,121 @@ __global__ __launch_bounds__(kWave * 4) void hyb_sp_token_kernel(SoftmaxPrefixAr
         for (int e = 0; e < 16; ++e) acc[ct][e] *= corr;
       m = mn;
     }
-    float p[16];
+    bf16x8 pop[KL];
+    float sum[4] = {};
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale, -m));
-      l += p[e];
+    for (int ks = 0; ks < KL; ++ks) {
+      float p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[ks * 8 + e], scale, -m));
+        sum[e % 4] += p[e];
+      }
+      pop[ks] = cvt_op<bf16>(p);
     }
-    op_t pop[KL];
-#pragma unroll
-    for (int ks = 0; ks < KL; ++ks) pop[ks] = cvt_op<bf16>(&p[ks * E]);
+    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 #pragma unroll
     for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
-      for (int ks = 0; ks < KL; ++ks) acc[ct] = M::mma(rt.col_op(s.v, ct, ks), pop[ks], acc[ct]);
+      for (int ks = 0; ks < KL; ++ks) acc[ct] = M::mma(rt.col_op(vt, ct, ks), pop[ks], acc[ct]);
+  }
+};
+
+// Four entries of a query's result: normalised into out, or as they are into
+// the workspace where the request has more ranges.
+template <int D>
+__device__ inline void sp_put(const SoftmaxPrefixArgs& a, const SpRange& rg, int r, int h, int i, int at, const f32x4& o,
+                              float den) {
+  if (rg.n == 1) {
+    const float inv = 1.0f / den;
+    const float v[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+    store_out4<bf16>(a.out, (((size_t)rg.b * a.s.L + i) * a.s.Hq + h) * D + at, v, a.s.out_f32);
+  } else {
+    *reinterpret_cast<f32x4*>((float*)a.ws + sp_row(a, r, h, i) * D + at) = o;
+  }
+}
+template <int D>
+__device__ inline void sp_put_sum(const SoftmaxPrefixArgs& a, const SpRange& rg, int r, int h, int i, float m, float den) {
+  if (rg.n == 1) return;
+  float* wml = sp_ml<D>(a) + sp_row(a, r, h, i) * 2;
+  wml[0] = m * 0.6931471805599453f;  // back to the natural log
+  wml[1] = den;
+}
+
+// Where a range and KV head have several workgroups, for groups of heads: workgroup
+// blockIdx.x is group hg of range and KV head `at`.  They read the same tiles, so
+// they are eight workgroups apart, on one XCD (the last ranges, fewer than eight,
+// as many apart as they are).
+__device__ inline void sp_place(int groups, int& at, int& hg) {
+  const int ats = gridDim.x / groups, at8 = blockIdx.x / (kNumXcd * groups) * kNumXcd, step = min(kNumXcd, ats - at8);
+  const int in8 = blockIdx.x - at8 * groups;
+  at = at8 + in8 % step;
+  hg = in8 / step;
+}
+
+// Few queries (bf16; decoding, and small batches of blocks): as many of a KV
+// head's query heads as have their L queries within the 32 columns of one tile of
+// scores share a workgroup (all of them in decoding), a wave answers all columns,
+// and the four waves take the range's tiles in turn, each with copies of its own
+// (two slots of K and V, no barrier in the loop) and sums of its own, joined in
+// LDS at the end.  With a wave per head, as above, each has one or a few columns of
+// its tile filled, and the loop is four times as many dependent steps (one token
+// of 64 requests over a window of 4096 117 us, now 98; of one request 25 and 17).
+__host__ __device__ inline int sp_pack(const Shape& s) {  // heads of a workgroup
+  const int G = s.Hq / s.Hkv, fit = kTile / s.L;
+  return fit < G ? fit : G;
+}
+__host__ __device__ inline int sp_groups(const Shape& s) {  // workgroups of a range and KV head
+  const int G = s.Hq / s.Hkv;
+  return (G + sp_pack(s) - 1) / sp_pack(s);
+}
+template <int D>
+__global__ __launch_bounds__(kWave * 4) void hyb_sp_token_kernel(SoftmaxPrefixArgs a, SpCut cut) {
+  typedef SpAcc<D> A;
+  typedef RowColTile<D> RT;
+  constexpr int NCT = A::NCT, NW = 4;
+  struct alignas(16) Slot {
+    bf16 k[kTile * D], v[kTile * D];
   };
+  __shared__ Slot ring[NW][2];
+  __shared__ float refs[NW][kTile], sums[NW][kTile];
+  __shared__ int pages[kMaxRangePages];
+
+  const int lane = threadIdx.x & (kWave - 1);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int li = lane & 31, hh = lane >> 5;
+  const int Hq = a.s.Hq, Hkv = a.s.Hkv, L = a.s.L, G = Hq / Hkv, pack = sp_pack(a.s), groups = sp_groups(a.s);
+  int at, hg;
+  sp_place(groups, at, hg);
+  const int g = at % Hkv, r = at / Hkv;
+  static_assert(sizeof(ring) >= kPlanInts * sizeof(int), "the plan's scratch fits the slots");
+  const SpRange rg = sp_range<true>(a, sp_plan<true>(a, cut, reinterpret_cast<int*>(&ring)), r, lane);
+  if (rg.b < 0) return;  // uniform: past the plan's last range
+  const int Lb = sp_block<true>(a, rg.b);
+  // this lane's column: query i of head h
+  const int i = li % L, hl = hg * pack + li / L, h = g * G + hl;
+  const bool col = li < pack * L && hl < G && i < Lb;
+  bf16x8 qop[A::KD];
+  {
+    const bf16* row = (const bf16*)a.q + (((size_t)rg.b * L + (col ? i : 0)) * Hq + (col ? h : g * G)) * D + hh * 8;
+#pragma unroll
+    for (int ks = 0; ks < A::KD; ++ks) qop[ks] = keep_if<bf16>(col, load_op<bf16>(row + ks * 16));
+  }
+  const SpTiles<D> t(a, rg, g, sp_keys<true>(a, rg.b) - Lb, pages);
+  const RT rt(lane);
+  const int mine = (rg.nt - w + NW - 1) / NW;  // this wave's tiles
+  auto issue = [&](int n, Slot& s) __attribute__((always_inline)) {
+    if (n >= mine) return;
+    const int j0 = t.first_key(w + NW * n);
+    t.template copy<RT::IK>(0, j0, 0, s.k, lane);
+    t.template copy<RT::IK>(1, j0, 0, s.v, lane);
+  };
+  const float scale = kLog2e / sqrtf((float)D);
+  A acc;
   auto step = [&](int n, Slot& s) __attribute__((always_inline)) {
     if (n + 1 < mine) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * RT::IK) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    compute(n, s);
+    acc.add(t, rt, t.first_key(w + NW * n), s.k, s.v, qop, scale, hh);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot is read
     issue(n + 2, s);
   };
@@ -1193,32 +1267,29 @@ __global__ __launch_bounds__(kWave * 4) void hyb_sp_token_kernel(SoftmaxPrefixAr
   }
 
   // The waves' sums over one reference: wave w scales its own and leaves them in
-  // its slots, then joins the columns 32 ct .. + 31 of the heads' entries for
-  // ct = w (and w + 4 ..: D is at most 4 such groups).
-  l += xor32(l);
-  if (hh == 0) refs[w][li] = m;
-  lds_barrier();
+  // LDS, then joins entries 32 w .. + 31 of every query.
+  mma_settle<bf16>();
+  const float l = acc.l + xor32(acc.l);
+  if (hh == 0) refs[w][li] = acc.m;
+  lds_barrier();  // (and the slots are free)
   float mm = refs[0][li];
 #pragma unroll
   for (int x = 1; x < NW; ++x) mm = fmaxf(mm, refs[x][li]);
-  const float f = __builtin_amdgcn_exp2f(m - mm);
+  const float f = __builtin_amdgcn_exp2f(acc.m - mm);
   if (hh == 0) sums[w][li] = l * f;
   f32x4* const parts = reinterpret_cast<f32x4*>(&ring);  // [wave][ct * 4 + e][lane]
-  static_assert(sizeof(Slot) * 2 >= NCT * 4 * kWave * sizeof(f32x4), "a wave's sums fit its slots");
+  static_assert(sizeof(ring) >= NW * NCT * 4 * kWave * sizeof(f32x4), "the sums fit the slots");
 #pragma unroll
   for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      parts[(w * NCT * 4 + ct * 4 + e) * kWave + lane] =
-          f32x4{acc[ct][4 * e] * f, acc[ct][4 * e + 1] * f, acc[ct][4 * e + 2] * f, acc[ct][4 * e + 3] * f};
+      parts[(w * NCT * 4 + ct * 4 + e) * kWave + lane] = f32x4{acc.acc[ct][4 * e] * f, acc.acc[ct][4 * e + 1] * f,
+                                                                acc.acc[ct][4 * e + 2] * f, acc.acc[ct][4 * e + 3] * f};
   lds_barrier();
   if (w >= NCT || !col) return;
   float den = 0.0f;
 #pragma unroll
   for (int x = 0; x < NW; ++x) den += sums[x][li];
-  const bool whole = rg.n == 1;
-  const float inv = whole ? 1.0f / den : 1.0f;
-  const size_t row = sp_row(a, r, h, i);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     f32x4 o = {};
@@ -1228,18 +1299,112 @@ __global__ __launch_bounds__(kWave * 4) void hyb_sp_token_kernel(SoftmaxPrefixAr
 #pragma unroll
       for (int k = 0; k < 4; ++k) o[k] += y[k];
     }
-    const float v[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
-    const size_t at = w * kTile + row_of(4 * e, hh);
-    if (whole)
-      store_out4<bf16>(a.out, (((size_t)b * L + i) * Hq + h) * D + at, v, a.s.out_f32);
-    else
-      *reinterpret_cast<f32x4*>((float*)a.ws + row * D + at) = f32x4{v[0], v[1], v[2], v[3]};
+    sp_put<D>(a, rg, r, h, i, w * kTile + row_of(4 * e, hh), o, den);
   }
-  if (!whole && w == 0 && hh == 0) {
-    float* wml = sp_ml<D>(a) + row * 2;
-    wml[0] = mm * 0.6931471805599453f;  // back to the natural log
-    wml[1] = den;
+  if (w == 0 && hh == 0) sp_put_sum<D>(a, rg, r, h, i, mm, den);
+}
+
+// Blocks (2 or 4 query heads per KV head): a wave per head, as in the ring kernel,
+// in two halves that take the range's tiles in turn and join their sums in LDS.
+// A window's ranges are short, so what a call waits for is the steps of one, and
+// the partial results of several per request cost as much as they save; so a
+// workgroup takes a range in half the steps instead of a range half as long:
+// 32 requests of 32 queries, window 512, 28.5 us by the ring kernel in ranges of 512
+// keys, 22 so; 24 of a window of 1024 33 and 30.  What bounds it is the copies in
+// flight (96 KiB per workgroup, about 3 us), where the workgroups are few.
+template <int D, int NG>
+__global__ __launch_bounds__(kWave * 2 * NG, 2) void hyb_sp_block_kernel(SoftmaxPrefixArgs a, SpCut cut) {
+  typedef SpAcc<D> A;
+  typedef RowColTile<D> RT;
+  constexpr int NCT = A::NCT, R = 4;
+  constexpr int IPW = 2 * RT::IK / NG;  // copies per wave and step: the half's first waves K's, the others V's
+  static_assert(IPW * NG == 2 * RT::IK && 3 * IPW <= 63, "copies split evenly, and those in flight fit vmcnt");
+  struct alignas(16) Slot {
+    bf16 k[kTile * D], v[kTile * D];
+  };
+  __shared__ Slot ring[2][R];
+  __shared__ float refs[2][NG][kTile], sums[2][NG][kTile];
+  __shared__ int pages[kMaxRangePages];
+
+  const int lane = threadIdx.x & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), half = wave / NG, w = wave % NG;
+  const int li = lane & 31, hh = lane >> 5;
+  const int Hq = a.s.Hq, Hkv = a.s.Hkv, L = a.s.L;
+  const int g = blockIdx.x % Hkv, r = blockIdx.x / Hkv, h = g * NG + w;
+  static_assert(sizeof(ring) >= kPlanInts * sizeof(int), "the plan's scratch fits the slots");
+  const SpRange rg = sp_range<true>(a, sp_plan<true>(a, cut, reinterpret_cast<int*>(&ring)), r, lane);
+  if (rg.b < 0) return;  // uniform: past the plan's last range
+  const int Lb = sp_block<true>(a, rg.b);
+  bf16x8 qop[A::KD];
+  {
+    const bf16* row = (const bf16*)a.q + (((size_t)rg.b * L + min(li, Lb - 1)) * Hq + h) * D + hh * 8;
+#pragma unroll
+    for (int ks = 0; ks < A::KD; ++ks) qop[ks] = keep_if<bf16>(li < Lb, load_op<bf16>(row + ks * 16));
   }
+  const SpTiles<D> t(a, rg, g, sp_keys<true>(a, rg.b) - Lb, pages);
+  const RT rt(lane);
+  const int nsteps = (rg.nt + 1) / 2, mine = (rg.nt + 1 - half) / 2;
+  const int kv = w * IPW / RT::IK, u0 = w * IPW % RT::IK;
+  auto issue = [&](int n, Slot& s) __attribute__((always_inline)) {
+    if (n < mine) t.template copy<IPW>(kv, t.first_key(half + 2 * n), u0, kv == 0 ? s.k : s.v, lane);
+  };
+  const float scale = kLog2e / sqrtf((float)D);
+  A acc;
+  // Tile n + 3 of the half goes to the slot of tile n - 1.
+  auto step = [&](int n, auto S) __attribute__((always_inline)) {
+    constexpr int SV = decltype(S)::value;
+    const int later = mine - 1 - n;
+    if (later >= 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * IPW) : "memory");
+    else if (later == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(IPW) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    lds_barrier_nodrain();
+    issue(n + 3, ring[half][(SV + 3) % R]);
+    if (n < mine) acc.add(t, rt, t.first_key(half + 2 * n), ring[half][SV].k, ring[half][SV].v, qop, scale, hh);
+  };
+  issue(0, ring[half][0]);
+  issue(1, ring[half][1]);
+  issue(2, ring[half][2]);
+  for (int n = 0; n < nsteps; n += R) {
+    step(n, std::integral_constant<int, 0>{});
+    if (n + 1 < nsteps) step(n + 1, std::integral_constant<int, 1>{});
+    if (n + 2 < nsteps) step(n + 2, std::integral_constant<int, 2>{});
+    if (n + 3 < nsteps) step(n + 3, std::integral_constant<int, 3>{});
+  }
+
+  // The halves' sums over one reference: each hands over half of the entries
+  // and joins the others.
+  mma_settle<bf16>();
+  const float l = acc.l + xor32(acc.l);
+  if (hh == 0) refs[half][w][li] = acc.m;
+  lds_barrier_nodrain();  // (and the slots are free)
+  const float mm = fmaxf(refs[0][w][li], refs[1][w][li]);
+  const float f = __builtin_amdgcn_exp2f(acc.m - mm);
+  if (hh == 0) sums[half][w][li] = l * f;
+  constexpr int NH = NCT / 2;  // groups of 32 entries per half
+  f32x4* const parts = reinterpret_cast<f32x4*>(&ring);  // [for half][w][ct * 4 + e][lane]
+  static_assert(sizeof(ring) >= 2 * NG * NH * 4 * kWave * sizeof(f32x4), "the sums fit the slots");
+#pragma unroll
+  for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const f32x4 y = {acc.acc[ct][4 * e] * f, acc.acc[ct][4 * e + 1] * f, acc.acc[ct][4 * e + 2] * f,
+                       acc.acc[ct][4 * e + 3] * f};
+      if (ct / NH != half) parts[((ct / NH * NG + w) * NH * 4 + ct % NH * 4 + e) * kWave + lane] = y;
+    }
+  lds_barrier_nodrain();
+  if (li >= Lb) return;
+  const float den = sums[0][w][li] + sums[1][w][li];
+#pragma unroll
+  for (int ct = 0; ct < NCT; ++ct)
+    if (ct / NH == half)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        f32x4 o = parts[((half * NG + w) * NH * 4 + ct % NH * 4 + e) * kWave + lane];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[k] += acc.acc[ct][4 * e + k] * f;
+        sp_put<D>(a, rg, r, h, li, ct * kTile + row_of(4 * e, hh), o, den);
+      }
+  if (half == 0 && hh == 0) sp_put_sum<D>(a, rg, r, h, li, mm, den);
 }
 
 // Merge of the partial results of the requests that have several ranges.  A
@@ -1330,13 +1495,27 @@ int softmax_prefix_splits(const Shape& s, int max_prefix) {
   return (int)want;
 }
 
-// Of a window.  Few queries take the token kernel (sp_tokens): one workgroup per
-// (request, KV head) fills the chip from 256 on, and then a merge costs more than an
-// even cut saves.
-static bool sp_tokens(const Shape& s) { return s.dtype == 1 && s.Hq / s.Hkv * s.L <= kTile; }
+// A window's kernels (bf16).  The token kernel where all heads of a KV head share a
+// workgroup, or where its workgroups, one per group of heads, are at most 256 (a
+// group reads every tile again; 8 requests of 32 queries, window 1024, 28 us by
+// the block kernel); the block kernel while a request is one range of it.
+static bool sp_tokens(const Shape& s) {
+  return s.dtype == 1 && (sp_groups(s) == 1 || (long)s.B * s.Hkv * sp_groups(s) <= 256);
+}
+static bool sp_blocks(const Shape& s, int max_seen) {
+  const int G = s.Hq / s.Hkv;
+  return s.dtype == 1 && !sp_tokens(s) && (G == 2 || G == 4) && max_seen + s.L <= 2048;
+}
+// Ranges per request: one by the block kernel, and by the token kernel where
+// its workgroups fill the chip anyway (a merge costs more than an even cut
+// saves).
 int softmax_window_splits(const Shape& s, int max_seen) {
-  if (sp_tokens(s) && (long)s.B * s.Hkv >= 256 && max_seen + s.L <= kMaxRange) return 1;
-  return softmax_prefix_splits(s, max_seen);
+  if (sp_blocks(s, max_seen)) return 1;
+  const int n = softmax_prefix_splits(s, max_seen);
+  if (!sp_tokens(s) || (long)max_seen + s.L > kMaxRange) return n;
+  if ((long)s.B * s.Hkv * sp_groups(s) >= 256) return 1;
+  // (ranges of 1024 keys and more where the heads have workgroups of their own)
+  return sp_groups(s) == 1 ? n : std::max(1, std::min(n, (int)(((long)max_seen + s.L) / 1024)));
 }
 
 // A single KV range per (request, KV head) writes the normalised output
@@ -1359,8 +1538,8 @@ static int sp_resident(K kernel, int waves) {
 
 template <typename K>
 static hipError_t sp_launch(K kernel, int resident, int waves, bool ring, const SoftmaxPrefixArgs& a, hipStream_t st,
-                            SpCut* out) {
-  const int ns = a.n_split;
+                            SpCut* out, int groups = 1) {
+  const int ns = a.n_split, per = a.s.Hkv * groups;  // workgroups of a range
   SpCut cut;
   // Of the ring's workgroups two per CU, one with more than four waves, keep
   // the memory as busy as more do, three tiles of each in flight; the
@@ -1369,13 +1548,13 @@ static hipError_t sp_launch(K kernel, int resident, int waves, bool ring, const 
   // d = 64 up to five of the ring's workgroups fit: 32 requests of 1024 keys, 8
   // KV heads of one head, 26.7 us, now 19.2; 32 of 1 to 4096 keys at 16 KV heads,
   // paged, 115 and 77.)
-  cut.slots = max(1, (waves > 4 ? min(resident, 256) : resident) / a.s.Hkv);
-  cut.sat = ring ? max(1, min(cut.slots, (waves > 4 ? 256 : 512) / a.s.Hkv)) : cut.slots;
+  cut.slots = max(1, (waves > 4 ? min(resident, 256) : resident) / per);
+  cut.sat = ring ? max(1, min(cut.slots, (waves > 4 ? 256 : 512) / per)) : cut.slots;
   // Ranges of a plan at most: three rounds, within the workspace, and at
   // least what the longest range allows.
   const int need = (int)(((long)a.max_seen + a.s.L + kMaxRange - 1) / kMaxRange);
   cut.limit = min(a.s.B * ns, max(a.s.B * need, 3 * cut.sat));
-  cut.layer = max(1, 256 / a.s.Hkv);
+  cut.layer = max(1, 256 / per);
   // Where ranges of at most 512 keys of full-length requests fit one round,
   // the host cuts every request into those: there is little to gain from the
   // lengths, and working a plan out costs each kernel a few us (32 requests of
@@ -1389,7 +1568,7 @@ static hipError_t sp_launch(K kernel, int resident, int waves, bool ring, const 
     cut.limit = a.s.B * ns;  // (full-length requests' ranges)
   }
   *out = cut;
-  hipLaunchKernelGGL(kernel, dim3(a.s.Hkv * cut.limit), dim3(kWave * waves), 0, st, a, cut);
+  hipLaunchKernelGGL(kernel, dim3(per * cut.limit), dim3(kWave * waves), 0, st, a, cut);
   return hipGetLastError();
 }
 
@@ -1411,10 +1590,15 @@ static hipError_t sp_go(const SoftmaxPrefixArgs& a, hipStream_t st) {
   // register-staged kernel.
   if (WIN && sp_tokens(a.s)) {
     static const int resident = sp_resident(hyb_sp_token_kernel<D>, 4);
-    e = sp_launch(hyb_sp_token_kernel<D>, resident, 4, true, a, st, &cut);
+    e = sp_launch(hyb_sp_token_kernel<D>, resident, 4, true, a, st, &cut, sp_groups(a.s));
+  } else if (WIN && sp_blocks(a.s, a.max_seen) && a.s.Hq / a.s.Hkv == 2) {
+    static const int resident = sp_resident(hyb_sp_block_kernel<D, 2>, 4);
+    e = sp_launch(hyb_sp_block_kernel<D, 2>, resident, 4, true, a, st, &cut);
+  } else if (WIN && sp_blocks(a.s, a.max_seen)) {
+    static const int resident = sp_resident(hyb_sp_block_kernel<D, 4>, 8);
+    e = sp_launch(hyb_sp_block_kernel<D, 4>, resident, 8, true, a, st, &cut);
   } else if constexpr (sizeof(T) == 2) {
     switch (a.s.Hq / a.s.Hkv) {
-      HYB_SP_CASE(1, true, hyb_sp_ring_kernel<D, 1)
       HYB_SP_CASE(2, true, hyb_sp_ring_kernel<D, 2)
       HYB_SP_CASE(3, false, hyb_sp_partial_kernel<T, D, 3)
       HYB_SP_CASE(4, true, hyb_sp_ring_kernel<D, 4)
@@ -1422,7 +1606,15 @@ static hipError_t sp_go(const SoftmaxPrefixArgs& a, hipStream_t st) {
       HYB_SP_CASE(6, false, hyb_sp_partial_kernel<T, D, 6)
       HYB_SP_CASE(7, false, hyb_sp_partial_kernel<T, D, 7)
       HYB_SP_CASE(8, true, hyb_sp_ring_kernel<D, 8)
-      default: return hipErrorInvalidValue;
+      default:
+        if constexpr (!WIN) {  // (a window's single head takes the token kernel)
+          switch (a.s.Hq / a.s.Hkv) {
+            HYB_SP_CASE(1, true, hyb_sp_ring_kernel<D, 1)
+            default: return hipErrorInvalidValue;
+          }
+          break;
+        }
+        return hipErrorInvalidValue;
     }
   } else {
     switch (a.s.Hq / a.s.Hkv) {

@@ -177,3 +177,16 @@ def test_streams_and_replays():
         want = hb.softmax_window_step_paged(*args())
         torch.cuda.synchronize()
         assert all(torch.equal(o, want) for _, o in graphs), lens
+
+
+@pytest.mark.parametrize("B,L,Hq,Hkv,d,window,sinks", [
+    (70, 32, 16, 4, 128, 90, 4), (70, 20, 8, 4, 64, 300, 33), (40, 32, 32, 8, 128, 64, 0), (33, 32, 16, 8, 128, 500, 1),
+    (9, 24, 12, 4, 128, 200, 4), (40, 9, 32, 4, 64, 100, 2), (3, 11, 16, 4, 128, 1500, 7), (130, 3, 10, 2, 128, 40, 5)])
+def test_batches(B, L, Hq, Hkv, d, window, sinks):
+    """Batches that fill the chip, and few requests whose heads are spread over
+    it, with requests of every length and one that is empty."""
+    announce(f"window step batch {B} {L} {Hq} {Hkv} {d}")
+    lens = [i * 37 % 700 for i in range(B)]
+    c = make(B, L, Hq, Hkv, d, 32, lens, BF, B + L)
+    hide(c, window, sinks)
+    check(c, window, sinks, [(i * 7) % (L + 1) for i in range(B)], what="batch")
