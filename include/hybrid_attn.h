@@ -466,8 +466,9 @@ size_t hybrid_rope_workspace_bytes(const hyb_rope_dims_t* dims);
  * int32 [2]: pages taken, pages that were missing.  Sums past 2^31 - 1 stay there.
  * batch is 1 .. 4096 (0: nothing to do); page_size a power of two from 1 to 65536;
  * max_pages * page_size < 2^31 - 64; n_free >= 0 (free_pages may be NULL when
- * 0); max_tokens >= 0 (slots and positions may be NULL when 0).  Outputs must not overlap
- * each other, the table or an input. */
+ * 0, and needs 4-byte alignment only: a caller goes on in its list where the
+ * last call's pages ended); max_tokens >= 0 (slots and positions may be NULL
+ * when 0).  Outputs must not overlap each other, the table or an input. */
 int kv_pages_plan(int32_t batch, int32_t max_pages, int32_t page_size,
                   int32_t n_free, int32_t max_tokens,
                   const int32_t* prefix_len, const int32_t* new_len,

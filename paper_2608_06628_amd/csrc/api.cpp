@@ -806,7 +806,8 @@ int kv_pages_plan(int32_t batch, int32_t max_pages, int32_t page_size,
   if (batch == 0) return ok();
   TRY(check_ptr(prefix_len, "prefix_len"));
   TRY(check_ptr(new_len, "new_len"));
-  TRY(check_ptr(free_pages, "free_pages", n_free > 0));
+  if (!free_pages && n_free > 0) return fail(HYB_ENULL, "free_pages is NULL");
+  if (reinterpret_cast<uintptr_t>(free_pages) & 3) return fail(HYB_EALIGN, "free_pages is not 4-byte aligned");
   TRY(check_ptr(page_table, "page_table", max_pages > 0));
   TRY(check_ptr(slots, "slots", max_tokens > 0));
   TRY(check_ptr(positions, "positions", max_tokens > 0));
