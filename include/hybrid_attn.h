@@ -317,8 +317,10 @@ int hybrid_attn_backward_full(const hyb_dims_t* dims, int32_t seq_len,
  * table row only entries 0 .. ceil(min(n_sinks, prefix) / page_size) - 1 and
  * (prefix - window) / page_size (rounded down) .. ceil(prefix / page_size) - 1
  * are read, so pages that left the window may be freed and reused.
- * ws/ws_bytes: at least hybrid_workspace_bytes(dims, HYB_OP_WINDOW_STEP, min(max_pages *
- * page_size, n_sinks + window + 64)) bytes. */
+ * Up to 65536 query heads.  ws/ws_bytes: at least hybrid_workspace_bytes(dims,
+ * HYB_OP_WINDOW_STEP, min(max_pages * page_size, n_sinks + window + 64)) bytes.
+ * Calls whose executions may overlap (two streams, two captured graphs) need
+ * workspaces of their own, here and below. */
 int softmax_window_step_paged(const hyb_dims_t* dims, const void* q,
                               const void* k, const void* v,
                               const void* k_pages, const void* v_pages,
@@ -338,8 +340,9 @@ int softmax_window_step_paged(const hyb_dims_t* dims, const void* q,
  * 2^30; the last block may be partial).  seq_lens (device [B] or NULL): tokens
  * of each sequence, clamped to [0, T]; later rows of q, k, v play no part
  * (their values may be anything) and later rows of out and lse are not
- * written.  The values of a sequence's own tokens must be finite.  lse (fp32
- * [B][Hq][T], or NULL): log of the sum of exp(q.k / sqrt(d)) over the tokens
+ * written.  The values of a sequence's own tokens must be finite, also where a
+ * query does not see them, and their scores within fp32.  lse (fp32
+ * [B][Hq][T], or NULL; up to 65536 query heads): log of the sum of exp(q.k / sqrt(d)) over the tokens
  * seen, which the gradient takes.  feat_dim and n_slots are not used (feat_dim
  * must still be valid).  ws/ws_bytes: at least hybrid_workspace_bytes(dims,
  * HYB_OP_WINDOW_PREFILL, seq_len) bytes (NULL when that is 0).  out and lse must not
@@ -405,7 +408,8 @@ typedef struct {
  * positions int32 [N] (any value); inv_freq double [rot_dim / 2], radians per
  * position: angles are formed in 64 bits, so far positions keep their phase, and
  * every scaling of positions for long contexts is a table (may be NULL
- * when rot_dim is 0).  Arithmetic is fp32, rounded once.  q_out and k_out may
+ * when rot_dim is 0).  Arithmetic is fp32, rounded once; an x whose squares
+ * leave fp32 (about 1e19) gives zeros.  q_out and k_out may
  * be interleaved in one buffer, and must not overlap each other or an input. */
 int hybrid_qk_norm_rope(const hyb_rope_dims_t* dims, const void* q,
                         const void* k, const void* wq, const void* wk,
@@ -436,7 +440,8 @@ int hybrid_qk_norm_rope_paged(const hyb_rope_dims_t* dims, const void* q,
  * fp32 dq, dk of hybrid_attn_backward_full and the dq, dk of
  * softmax_window_backward fit as they are).  ws/ws_bytes: at least
  * hybrid_rope_workspace_bytes(dims) bytes when a weight is given (else may be
- * NULL).  Outputs and the workspace must not overlap each other or an input.
+ * NULL).  Every token counts for dwq and dwk, so those of a padded batch need
+ * finite q and k and gradients of zero.  Outputs and the workspace must not overlap each other or an input.
  * Deterministic. */
 int hybrid_qk_norm_rope_backward(const hyb_rope_dims_t* dims, const void* q,
                                  const void* k, const void* wq, const void* wk,

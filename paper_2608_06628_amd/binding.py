@@ -11,6 +11,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import functools
+import inspect
 import os
 
 import torch
@@ -402,25 +403,31 @@ def hybrid_attn_backward_full(q, k, v, W, alpha, block, dout=None, target=None, 
 # made here is neither written before earlier work has left it nor reused
 # while the call still runs.
 def _placed(f):
+    name = list(inspect.signature(f).parameters)[1]
+
     @functools.wraps(f)
-    def call(first, *args, stream=None, **kw):
+    def call(*args, stream=None, **kw):
         try:
-            dev = first.get_device()
-        except AttributeError:
+            dev = (args[0] if args else kw[name]).get_device()
+        except (AttributeError, KeyError):
             dev = -1
         if dev < 0:
-            raise TypeError(f"{f.__name__} takes CUDA (HIP) tensors")
+            raise TypeError(f"{f.__name__} takes CUDA (HIP) tensors, {name} first")
         if stream is None and dev == torch._C._cuda_getDevice():
-            return f(dev, first, *args, **kw)
+            return f(dev, *args, **kw)
         with contextlib.ExitStack() as on:
             on.enter_context(torch.cuda.device(dev))
             if stream is not None:
-                if not isinstance(stream, torch.cuda.Stream):
-                    stream = torch.cuda.ExternalStream(stream, device=dev)
+                if not isinstance(stream, torch.cuda.Stream):  # a raw handle; 0 is the null stream
+                    stream = (torch.cuda.ExternalStream(stream, device=dev) if stream
+                              else torch.cuda.default_stream(dev))
                 if stream.device.index != dev:
                     raise ValueError(f"a stream of {stream.device} for tensors of device {dev}")
                 on.enter_context(torch.cuda.stream(stream))
-            return f(dev, first, *args, **kw)
+            return f(dev, *args, **kw)
+    call.__signature__ = inspect.Signature(
+        [p for p in inspect.signature(f).parameters.values() if p.name != "dev"]
+        + [inspect.Parameter("stream", inspect.Parameter.KEYWORD_ONLY, default=None)])
     return call
 
 
@@ -460,8 +467,9 @@ def _new(t, shape, dtype):
     return t.new_empty(shape) if dtype is t.dtype else t.new_empty(shape, dtype=dtype)
 
 
-def _bytes(t):
-    return t.numel() * t.element_size() if t is not None else 0
+def _ws(dev, t):
+    """A workspace's address and size, whatever its type."""
+    return (None, 0) if t is None else (_dptr(dev, t, "ws", t.dtype), t.numel() * t.element_size())
 
 
 # (a ctypes structure costs more to fill than to find; nothing writes to them)
@@ -494,7 +502,7 @@ def _rope_args(dev, q, k, wq, wk, inv_freq, positions, eps, rot_scale, layout, q
                       HYB_OUT_F32 if odt is not act else 0, eps, rot_scale, sq, sk, sv, soq, sok)
     return (dims, pq, pk, pv, oq, ok, _dptr(dev, wq, "wq", act, (d,)),
             _dptr(dev, wk, "wk", act, (d,)), _dptr(dev, positions, "positions", torch.int32, (N,)),
-            _dptr(dev, inv_freq, "inv_freq", torch.float64))
+            _dptr(dev, inv_freq, "inv_freq", torch.float64, (dims.rot_dim // 2,)))
 
 
 @_placed
@@ -564,7 +572,7 @@ def hybrid_qk_norm_rope_backward(dev, q, k, dq_out, dk_out, inv_freq, positions,
         dims, pq, pk, pwq, pwk, pos, freq, _dptr(dev, dq_out, "dq_out", dq_out.dtype, q.shape),
         _dptr(dev, dk_out, "dk_out", dq_out.dtype, k.shape), oq, ok,
         None if dwq is None else dwq.data_ptr(), None if dwk is None else dwk.data_ptr(),
-        _dptr(dev, ws, "ws", torch.uint8), _bytes(ws), _raw_stream(dev)))
+        *_ws(dev, ws), _raw_stream(dev)))
     return dq, dk, dwq, dwk
 
 
@@ -623,7 +631,7 @@ def softmax_window_step_paged(dev, q, k, v, k_pages, v_pages, page_table, prefix
         n_pages, page_size, _dptr(dev, page_table, "page_table", i32, (B, max_pages)), max_pages,
         _dptr(dev, prefix_len, "prefix_len", i32, (B,)), window, n_sinks,
         _dptr(dev, block_len, "block_len", i32, (B,)), _dptr(dev, out, "out", odt, q.shape),
-        _dptr(dev, ws, "ws", torch.uint8), _bytes(ws), _raw_stream(dev)))
+        *_ws(dev, ws), _raw_stream(dev)))
     return out
 
 
@@ -652,7 +660,7 @@ def softmax_window_prefill(dev, q, k, v, block, window, n_sinks=0, seq_lens=None
         dims, T, window, n_sinks, _dptr(dev, q, "q", act), _dptr(dev, k, "k", act, kv),
         _dptr(dev, v, "v", act, kv), _dptr(dev, seq_lens, "seq_lens", torch.int32, (B,)),
         _dptr(dev, out, "out", odt, q.shape), _dptr(dev, lse, "lse", f32, (B, Hq, T)),
-        _dptr(dev, ws, "ws", torch.uint8), _bytes(ws), _raw_stream(dev)))
+        *_ws(dev, ws), _raw_stream(dev)))
     return out, lse
 
 
@@ -680,5 +688,5 @@ def softmax_window_backward(dev, q, k, v, out, lse, dout, block, window, n_sinks
         _dptr(dev, lse, "lse", torch.float32, (B, Hq, T)),
         _dptr(dev, dout, "dout", act, q.shape), _dptr(dev, dq, "dq", odt, q.shape),
         _dptr(dev, dk, "dk", odt, kv), _dptr(dev, dv, "dv", odt, kv),
-        _dptr(dev, ws, "ws", torch.uint8), _bytes(ws), _raw_stream(dev)))
+        *_ws(dev, ws), _raw_stream(dev)))
     return dq, dk, dv

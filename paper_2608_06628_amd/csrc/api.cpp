@@ -456,6 +456,8 @@ int softmax_window_step_paged(const hyb_dims_t* dims, const void* q,
                               void* stream) {
   if (window < 0 || n_sinks < 0)
     return fail(HYB_EINVAL, "window %d and n_sinks %d must be >= 0", window, n_sinks);
+  if (dims && dims->n_q_heads > 65536)
+    return fail(HYB_EUNSUPPORTED, "n_q_heads %d not supported (at most 65536)", dims->n_q_heads);
   return softmax_prefix_impl(dims, q, k, v, k_pages, v_pages, prefix_len, 0,
                              true, page_table, n_pages, page_size, max_pages,
                              out, ws, ws_bytes, stream, window, n_sinks, block_len);
@@ -492,6 +494,7 @@ int check_window(const hyb_dims_t* dims, int32_t seq_len, int32_t window,
     return fail(HYB_EINVAL, "seq_len %d is not in 1 .. 2^30", seq_len);
   if (window < 0 || n_sinks < 0)
     return fail(HYB_EINVAL, "window %d and n_sinks %d must be >= 0", window, n_sinks);
+  if (s->Hq > 65536) return fail(HYB_EUNSUPPORTED, "n_q_heads %d not supported (at most 65536)", s->Hq);
   if (hyb::window_workgroups(*s, seq_len) > 0x7fffffffL)
     return fail(HYB_EINVAL, "batch * heads * seq_len exceeds the grid limit");
   return HYB_OK;
@@ -962,7 +965,7 @@ size_t hybrid_workspace_bytes(const hyb_dims_t* dims, int32_t op,
     case HYB_OP_WINDOW_PREFILL:
       return 0;
     case HYB_OP_WINDOW_BACKWARD:
-      return hyb::window_backward_ws_bytes(s, extent);
+      return s.B > 0 && extent > 0 && extent <= (1 << 30) ? hyb::window_backward_ws_bytes(s, extent) : 0;
   }
   return 0;
 }

@@ -230,3 +230,21 @@ def test_binding_takes_device_tensors_only():
                  lambda: hb.softmax_window_prefill(t[None], t[None], t[None], 1, 1)):
         with pytest.raises(TypeError):
             call()
+
+
+def test_workspace_of_nothing():
+    """Sizes of empty calls are 0, for every op, and no query ends the process."""
+    lib = hb.load()
+    for op in (hb.OP_WINDOW_STEP, hb.OP_WINDOW_PREFILL, hb.OP_WINDOW_BACKWARD):
+        for d, extent in ((dims(batch=0), 100), (dims(), -1), (dims(head_dim=7), 10), (dims(batch=0), 0)):
+            assert lib.hybrid_workspace_bytes(ctypes.byref(d), op, extent) == 0
+        lib.hybrid_workspace_bytes(ctypes.byref(dims()), op, 2 ** 31 - 1)
+    assert lib.hybrid_workspace_bytes(ctypes.byref(dims()), hb.OP_WINDOW_BACKWARD, 0) == 0
+    assert lib.hybrid_rope_workspace_bytes(ctypes.byref(rope(tokens=0))) == 0
+    assert lib.hybrid_rope_workspace_bytes(None) == 0
+
+
+def test_too_many_heads():
+    d = dims(n_q_heads=1 << 17, n_kv_heads=1 << 17, batch=1)
+    for make in (prefill, backward, step):
+        assert make(d)() == 5 and "heads" in hb.last_error()
