@@ -1018,6 +1018,9 @@ __global__ __launch_bounds__(kWave * 4 * kWinHalves<D>, 2) void hyb_win_dkv_ring
       if (n + 1 < nsteps) step(n + 1, std::integral_constant<int, 1>{});
       if (n + 2 < nsteps) step(n + 2, std::integral_constant<int, 2>{});
     }
+    // (a part without query tiles, where keys have fewer than parts, has taken no
+    // step, and its copies of V may be on their way into what the sums take over)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     if constexpr (H == 2) {
       // The halves' sums: each hands over one of dK and dV and keeps the other.
       lds_barrier_nodrain();

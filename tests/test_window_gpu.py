@@ -200,3 +200,13 @@ def test_backward_in_parts(B, T, Hq, Hkv, d, L, window, sinks, dtype, lens):
     """Few keys and many queries: the lists of queries are cut into parts, the
     sinks' into more of them."""
     test_backward(B, T, Hq, Hkv, d, L, window, sinks, dtype, lens)
+
+
+@pytest.mark.parametrize("B,T,Hq,Hkv,d,L,window,sinks,dtype,lens", [
+    (1, 1300, 1, 1, 128, 32, 1300, 0, BF, None), (2, 1300, 1, 1, 128, 32, 1300, 200, BF, [1300, 1153]),
+    (1, 1290, 1, 1, 64, 1, 1290, 0, BF, None), (1, 1300, 1, 1, 128, 32, 1300, 0, FL, None)])
+def test_backward_parts_without_tiles(B, T, Hq, Hkv, d, L, window, sinks, dtype, lens):
+    """The last keys are seen by fewer tiles of queries than their list has
+    parts: a part that adds nothing leaves zeros."""
+    for _ in range(3):
+        test_backward(B, T, Hq, Hkv, d, L, window, sinks, dtype, lens)
