@@ -312,7 +312,8 @@ int hybrid_attn_backward_full(const hyb_dims_t* dims, int32_t seq_len,
  * window and n_sinks are >= 0; a window of at least the prefix gives
  * softmax_prefix_step_paged.  block_len (device [B] or NULL): active tokens of
  * each block, as for hybrid_attn_step.
- * Arguments otherwise as for softmax_prefix_step_paged.  Tokens that are not
+ * Arguments otherwise as for softmax_prefix_step_paged, rows past block_len[b]
+ * are not written, and scores q.k must be below 1e29 in magnitude.  Tokens that are not
  * seen play no part, whatever their rows hold (NaN included), and of a page
  * table row only entries 0 .. ceil(min(n_sinks, prefix) / page_size) - 1 and
  * (prefix - window) / page_size (rounded down) .. ceil(prefix / page_size) - 1
@@ -341,12 +342,12 @@ int softmax_window_step_paged(const hyb_dims_t* dims, const void* q,
  * of each sequence, clamped to [0, T]; later rows of q, k, v play no part
  * (their values may be anything) and later rows of out and lse are not
  * written.  The values of a sequence's own tokens must be finite, also where a
- * query does not see them, and their scores within fp32.  lse (fp32
- * [B][Hq][T], or NULL; up to 65536 query heads): log of the sum of exp(q.k / sqrt(d)) over the tokens
- * seen, which the gradient takes.  feat_dim and n_slots are not used (feat_dim
- * must still be valid).  ws/ws_bytes: at least hybrid_workspace_bytes(dims,
- * HYB_OP_WINDOW_PREFILL, seq_len) bytes (NULL when that is 0).  out and lse must not
- * overlap each other, an input or the workspace.
+ * query does not see them, and scores q.k below 1e29 in magnitude.  lse (fp32
+ * [B][Hq][T], or NULL): log of the sum of exp(q.k / sqrt(d)) over the tokens
+ * seen, which the gradient takes.  Up to 65536 query heads; feat_dim and n_slots
+ * are not used (feat_dim must still be valid).  ws/ws_bytes: at least
+ * hybrid_workspace_bytes(dims, HYB_OP_WINDOW_PREFILL, seq_len) bytes (NULL when
+ * that is 0).  out and lse must not overlap each other, an input or the workspace.
  * bf16: the weights enter P V rounded to bf16, lse sums them unrounded. */
 int softmax_window_prefill(const hyb_dims_t* dims, int32_t seq_len,
                            int32_t window, int32_t n_sinks, const void* q,
@@ -441,8 +442,8 @@ int hybrid_qk_norm_rope_paged(const hyb_rope_dims_t* dims, const void* q,
  * softmax_window_backward fit as they are).  ws/ws_bytes: at least
  * hybrid_rope_workspace_bytes(dims) bytes when a weight is given (else may be
  * NULL).  Every token counts for dwq and dwk, so those of a padded batch need
- * finite q and k and gradients of zero.  Outputs and the workspace must not overlap each other or an input.
- * Deterministic. */
+ * finite q and k and gradients of zero.  Outputs and the workspace must not
+ * overlap each other or an input.  Deterministic. */
 int hybrid_qk_norm_rope_backward(const hyb_rope_dims_t* dims, const void* q,
                                  const void* k, const void* wq, const void* wk,
                                  const int32_t* positions,

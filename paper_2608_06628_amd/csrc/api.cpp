@@ -495,7 +495,7 @@ int check_window(const hyb_dims_t* dims, int32_t seq_len, int32_t window,
   if (window < 0 || n_sinks < 0)
     return fail(HYB_EINVAL, "window %d and n_sinks %d must be >= 0", window, n_sinks);
   if (s->Hq > 65536) return fail(HYB_EUNSUPPORTED, "n_q_heads %d not supported (at most 65536)", s->Hq);
-  if (hyb::window_workgroups(*s, seq_len) > 0x7fffffffL)
+  if (hyb::window_threads(*s, seq_len) > 0xffffffffL)
     return fail(HYB_EINVAL, "batch * heads * seq_len exceeds the grid limit");
   return HYB_OK;
 }

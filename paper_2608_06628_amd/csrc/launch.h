@@ -140,7 +140,7 @@ size_t rope_backward_ws_bytes(const RopeArgs& a);
 hipError_t launch_pages_plan(const PagesArgs& a, hipStream_t st);
 hipError_t launch_window_prefill(const WindowArgs& a, hipStream_t st);
 hipError_t launch_window_backward(const WindowArgs& a, hipStream_t st);
-long window_workgroups(const Shape& s, int T);
+double window_threads(const Shape& s, int T);
 size_t window_backward_ws_bytes(const Shape& s, int T);
 // The step for small batches: one wave per (request, head, 32-column slice).
 hipError_t launch_step_small(const StepArgs& a, hipStream_t st);

@@ -1190,10 +1190,14 @@ hipError_t launch_window_backward(const WindowArgs& a, hipStream_t st) {
   return a.s.D == 64 ? win_backward_go<float, 64>(a, st) : win_backward_go<float, 128>(a, st);
 }
 
-// Workgroups of the largest launch (the grid's limit is checked by the caller).
-long window_workgroups(const Shape& s, int T) {
+// Threads of the largest launch (the grid's limit is checked by the caller): a
+// workgroup per four units of queries, or one of up to 512 threads per 128 keys and
+// part, of which there are more than one in small grids only.
+double window_threads(const Shape& s, int T) {
   const long units = ((long)T + kTile - 1) / kTile * (s.Hq / s.Hkv);
-  return (long)s.B * s.Hkv * ((units + kWinWaves - 1) / kWinWaves);
+  const double queries = kWave * kWinWaves * (double)((units + kWinWaves - 1) / kWinWaves);
+  const double keys = kWave * 4 * kWinHalves<128> * std::ceil((double)T / kWinKeys);
+  return (double)s.B * s.Hkv * std::max(queries, keys);
 }
 
 size_t window_backward_ws_bytes(const Shape& s, int T) {

@@ -248,3 +248,12 @@ def test_too_many_heads():
     d = dims(n_q_heads=1 << 17, n_kv_heads=1 << 17, batch=1)
     for make in (prefill, backward, step):
         assert make(d)() == 5 and "heads" in hb.last_error()
+
+
+def test_more_workgroups_than_a_grid_holds():
+    d = dims(batch=1 << 24, n_q_heads=1, n_kv_heads=1)
+    for make in (prefill, backward):
+        assert make(d, T=1)() != 0 and "grid limit" in hb.last_error()
+    d = dims(batch=2 ** 31 - 1, n_q_heads=65536, n_kv_heads=65536)
+    for make in (prefill, backward):
+        assert make(d, T=1 << 30)() != 0 and "grid limit" in hb.last_error()
