@@ -155,14 +155,14 @@ struct WinF32 {
 };
 
 // Rows row0 .. row0 + 31 of two arrays (row stride in elements) into registers,
-// and from there, zero from row `rows` on, into two tiles; all threads of the
-// workgroup.  (The zeros are put in last: a select at the load would wait for it.)
+// and from there, zero from row `rows` on, into two tiles; by four waves, whose
+// thread number t is.  (The zeros are put in last: a select at the load would wait for it.)
 template <int D>
 __device__ inline void win_fetch(typename WinF32<D>::Regs& r, const float* a, const float* b, size_t stride, int row0,
-                                 int rows) {
+                                 int rows, int t) {
 #pragma unroll
   for (int u = 0; u < WinF32<D>::NCH; ++u) {
-    const int x = threadIdx.x + u * kWave * kWinWaves, i = row0 + x / (D / 4);
+    const int x = t + u * kWave * kWinWaves, i = row0 + x / (D / 4);
     const size_t at = (size_t)min(i, rows - 1) * stride + x % (D / 4) * 4;
     r.a[u] = *reinterpret_cast<const f32x4*>(a + at);
     r.b[u] = *reinterpret_cast<const f32x4*>(b + at);
@@ -170,10 +170,10 @@ __device__ inline void win_fetch(typename WinF32<D>::Regs& r, const float* a, co
 }
 template <int D>
 __device__ inline void win_put(const typename WinF32<D>::Regs& r, typename WinF32<D>::Tile& a,
-                               typename WinF32<D>::Tile& b, int row0, int rows) {
+                               typename WinF32<D>::Tile& b, int row0, int rows, int t) {
 #pragma unroll
   for (int u = 0; u < WinF32<D>::NCH; ++u) {
-    const int x = threadIdx.x + u * kWave * kWinWaves, i = x / (D / 4);
+    const int x = t + u * kWave * kWinWaves, i = x / (D / 4);
     const bool ok = row0 + i < rows;
     *reinterpret_cast<f32x4*>(&a[i][x % (D / 4) * 4]) = ok ? r.a[u] : f32x4{};
     *reinterpret_cast<f32x4*>(&b[i][x % (D / 4) * 4]) = ok ? r.b[u] : f32x4{};
@@ -239,11 +239,28 @@ __device__ inline WinUnit win_unit(const WindowArgs& a, int len, int b, int g, i
   return WinUnit{b, g, g * G + u % G, i0, i0 < len};
 }
 
-template <int D>
-__global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_fwd_kernel(WindowArgs a, int wgs) {
+// Forward.  With H = 2 two halves of four waves take a unit's tiles in turn, each
+// through buffers of its own, and join their sums in LDS: a CU that holds one
+// workgroup has two waves per SIMD then, and one's products run beside the other's
+// weights (3 x 1197 tokens, 8 heads of d = 64, window 300: 47 us with one half, now 40).
+template <int D, int H>
+__global__ __launch_bounds__(kWave* kWinWaves* H) void hyb_win_fwd_kernel(WindowArgs a, int wgs) {
   typedef WinF32<D> C;
-  __shared__ alignas(16) typename C::Tile kt[2], vt[2];
-  const int lane = threadIdx.x & (kWave - 1), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  struct Tiles {
+    typename C::Tile k[H][2], v[H][2];
+  };
+  struct Join {  // the second half's sums and weighted sums
+    float m[kWinWaves][kTile], l[kWinWaves][kTile];
+    f32x4 x[kWinWaves][C::NCT * 4][kWave];
+  };
+  union Smem {
+    Tiles tiles;
+    Join join;
+    __device__ Smem() {}
+  };
+  __shared__ alignas(16) Smem sh;
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int half = wave / kWinWaves, w = wave % kWinWaves, t = threadIdx.x % (kWave * kWinWaves);
   const int li = lane & 31, hh = lane >> 5;
   const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv;
   int bg, x;
@@ -260,8 +277,13 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_fwd_kernel(WindowArg
   const float* V = (const float*)a.v + ((size_t)b * a.T * Hkv + g) * D;
   const int i = min(me.i0 + li, len - 1);
   const WinRow row(a, len, i), r0(a, len, min(me.i0, len - 1)), r1(a, len, min(me.i0 + kTile, len) - 1);
+  // This half's step n takes tile H n + half.
+  typename C::Tile(&kt)[2] = sh.tiles.k[half];
+  typename C::Tile(&vt)[2] = sh.tiles.v[half];
+  const int nsteps = (tl.n + H - 1) / H, mine = (tl.n + H - 1 - half) / H;
+  auto key = [&](int n) __attribute__((always_inline)) { return tl.first(H * n + half, kTile); };
   typename C::Regs next;
-  win_fetch<D>(next, K, V, ks_, tl.first(0, kTile), len);
+  if (mine > 0) win_fetch<D>(next, K, V, ks_, key(0), len, t);
   typename C::Ops qop;
   win_row_ops<D>(qop, (const float*)a.q + ((size_t)b * a.T * Hq + me.h) * D + i * qs, true, hh);
   const float scale = kLog2e / sqrtf((float)D);
@@ -269,12 +291,12 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_fwd_kernel(WindowArg
   typename C::Acc acc;
 #pragma unroll
   for (int ct = 0; ct < C::NCT; ++ct) acc[ct] = f32x16{};
-  win_put<D>(next, kt[0], vt[0], tl.first(0, kTile), len);
+  if (mine > 0) win_put<D>(next, kt[0], vt[0], key(0), len, t);
   __syncthreads();
-  for (int n = 0; n < tl.n; ++n) {
-    const int j0 = tl.first(n, kTile), buf = n & 1;
-    if (n + 1 < tl.n) win_fetch<D>(next, K, V, ks_, tl.first(n + 1, kTile), len);
-    if (me.any && !win_none(r0, r1, a.n_sinks, j0, kTile)) {  // uniform over the wave
+  for (int n = 0; n < nsteps; ++n) {
+    const int buf = n & 1, j0 = n < mine ? key(n) : 0;
+    if (n + 1 < mine) win_fetch<D>(next, K, V, ks_, key(n + 1), len, t);
+    if (me.any && n < mine && !win_none(r0, r1, a.n_sinks, j0, kTile)) {  // uniform over the wave
       f32x16 sc = win_rows_mma<D>(kt[buf], qop, li, hh);
       if (!win_full(r0, r1, a.n_sinks, j0, kTile)) {  // uniform
 #pragma unroll
@@ -305,8 +327,36 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_fwd_kernel(WindowArg
       win_cols_mma<D>(acc, vt[buf], p, li, hh);
       mma_settle<float>();
     }
-    if (n + 1 < tl.n) win_put<D>(next, kt[buf ^ 1], vt[buf ^ 1], tl.first(n + 1, kTile), len);
+    if (n + 1 < mine) win_put<D>(next, kt[buf ^ 1], vt[buf ^ 1], key(n + 1), len, t);
     __syncthreads();
+  }
+  if constexpr (H == 2) {
+    if (half == 1) {
+      if (hh == 0) {
+        sh.join.m[w][li] = m;
+        sh.join.l[w][li] = l;
+      }
+#pragma unroll
+      for (int ct = 0; ct < C::NCT; ++ct)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          sh.join.x[w][ct * 4 + e][lane] =
+              f32x4{acc[ct][4 * e], acc[ct][4 * e + 1], acc[ct][4 * e + 2], acc[ct][4 * e + 3]};
+    }
+    __syncthreads();
+    if (half == 1) return;
+    const float mo = sh.join.m[w][li], mm = fmaxf(m, mo);
+    const float f = __builtin_amdgcn_exp2f(m - mm), fo = __builtin_amdgcn_exp2f(mo - mm);
+    l = l * f + sh.join.l[w][li] * fo;
+    m = mm;
+#pragma unroll
+    for (int ct = 0; ct < C::NCT; ++ct)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const f32x4 y = sh.join.x[w][ct * 4 + e][lane];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[ct][4 * e + k] = acc[ct][4 * e + k] * f + y[k] * fo;
+      }
   }
   if (!me.any || me.i0 + li >= len) return;
   win_store<float, D>(a.out, ((size_t)b * a.T + i) * Hq + me.h, acc, 1.0f / l, hh, true);
@@ -339,7 +389,7 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dq_kernel(WindowArgs
     const int i = min(me.i0 + li, len - 1);
     const WinRow row(a, len, i), r0(a, len, min(me.i0, len - 1)), r1(a, len, min(me.i0 + kTile, len) - 1);
     typename C::Regs next;
-    win_fetch<D>(next, K, V, ks_, tl.first(0, kTile), len);
+    win_fetch<D>(next, K, V, ks_, tl.first(0, kTile), len, threadIdx.x);
     typename C::Ops qop, dop;
     const size_t at = ((size_t)b * a.T * Hq + me.h) * D + i * qs;
     win_row_ops<D>(qop, (const float*)a.q + at, true, hh);
@@ -352,11 +402,11 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dq_kernel(WindowArgs
     const size_t st = ((size_t)b * Hq + me.h) * a.T + i;
     const float lse = a.lse[st] * kLog2e;
     if (hh == 0 && me.i0 + li < len) a.ws[st] = delta;
-    win_put<D>(next, kt[0], vt[0], tl.first(0, kTile), len);
+    win_put<D>(next, kt[0], vt[0], tl.first(0, kTile), len, threadIdx.x);
     __syncthreads();
     for (int n = 0; n < tl.n; ++n) {
       const int j0 = tl.first(n, kTile), buf = n & 1;
-      if (n + 1 < tl.n) win_fetch<D>(next, K, V, ks_, tl.first(n + 1, kTile), len);
+      if (n + 1 < tl.n) win_fetch<D>(next, K, V, ks_, tl.first(n + 1, kTile), len, threadIdx.x);
       if (me.any && !win_none(r0, r1, a.n_sinks, j0, kTile)) {
         f32x16 sc = win_rows_mma<D>(kt[buf], qop, li, hh);
         const f32x16 dp = win_rows_mma<D>(vt[buf], dop, li, hh);
@@ -371,7 +421,7 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dq_kernel(WindowArgs
         win_cols_mma<D>(acc, kt[buf], ds, li, hh);
         mma_settle<float>();
       }
-      if (n + 1 < tl.n) win_put<D>(next, kt[buf ^ 1], vt[buf ^ 1], tl.first(n + 1, kTile), len);
+      if (n + 1 < tl.n) win_put<D>(next, kt[buf ^ 1], vt[buf ^ 1], tl.first(n + 1, kTile), len, threadIdx.x);
       __syncthreads();
     }
   }
@@ -424,7 +474,7 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dkv_kernel(WindowArg
     auto fetch = [&](int n) __attribute__((always_inline)) {
       const int h = g * G + (first + n) / nq, i0 = tile(n);
       const size_t head = ((size_t)b * a.T * Hq + h) * D;
-      win_fetch<D>(next, (const float*)a.q + head, (const float*)a.dout + head, qs, i0, len);
+      win_fetch<D>(next, (const float*)a.q + head, (const float*)a.dout + head, qs, i0, len, threadIdx.x);
       if (threadIdx.x < 2 * kTile) {
         const size_t at = ((size_t)b * Hq + h) * a.T + min(i0 + (int)threadIdx.x % kTile, len - 1);
         nst = threadIdx.x < kTile ? a.lse[at] * kLog2e : a.ws[at];
@@ -432,7 +482,7 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dkv_kernel(WindowArg
     };
     auto put = [&](int n) __attribute__((always_inline)) {
       const int buf = n & 1;
-      win_put<D>(next, qt[buf], dt[buf], tile(n), len);
+      win_put<D>(next, qt[buf], dt[buf], tile(n), len, threadIdx.x);
       if (threadIdx.x < 2 * kTile) (&stats[buf][0][0])[threadIdx.x] = nst;
     };
     if (nsteps > 0) fetch(0);
@@ -1097,9 +1147,18 @@ static hipError_t win_ring_go(const WindowArgs& a, hipStream_t st) {
 
 template <int D>
 static hipError_t win_prefill_f32_go(const WindowArgs& a, hipStream_t st) {
-  const int wgs = win_wgs(a);
-  hipLaunchKernelGGL(hyb_win_fwd_kernel<D>, dim3((unsigned)(a.s.B * a.s.Hkv * wgs)), dim3(kWave * kWinWaves), 0, st, a,
-                     wgs);
+  const int wgs = win_wgs(a), n = a.s.B * a.s.Hkv * wgs;
+  // Two halves at d = 128, where one workgroup fits a CU either way (8 x 4096 tokens,
+  // 16 heads, window 500, 1404 us with one, now 1300; 1 x 1024, 159 and 144), and at
+  // d = 64, where three of one half fit, while workgroups are few (1 x 3000 tokens, 192
+  // of them, 260 and 215; 2 x 2048, 512, 231 and 165; of 4096 616, and 684 in halves).
+  bool halves = true;
+  if constexpr (D == 64) {
+    halves = n <= 512;
+    if (!halves) hipLaunchKernelGGL((hyb_win_fwd_kernel<D, 1>), dim3((unsigned)n), dim3(kWave * kWinWaves), 0, st, a, wgs);
+  }
+  if (halves)
+    hipLaunchKernelGGL((hyb_win_fwd_kernel<D, 2>), dim3((unsigned)n), dim3(kWave * kWinWaves * 2), 0, st, a, wgs);
   return hipGetLastError();
 }
 
@@ -1191,11 +1250,11 @@ hipError_t launch_window_backward(const WindowArgs& a, hipStream_t st) {
 }
 
 // Threads of the largest launch (the grid's limit is checked by the caller): a
-// workgroup per four units of queries, or one of up to 512 threads per 128 keys and
-// part, of which there are more than one in small grids only.
+// workgroup of up to 512 threads per four units of queries, or per 128 keys and part,
+// of which there are more than one in small grids only.
 double window_threads(const Shape& s, int T) {
   const long units = ((long)T + kTile - 1) / kTile * (s.Hq / s.Hkv);
-  const double queries = kWave * kWinWaves * (double)((units + kWinWaves - 1) / kWinWaves);
+  const double queries = kWave * kWinWaves * 2 * (double)((units + kWinWaves - 1) / kWinWaves);
   const double keys = kWave * 4 * kWinHalves<128> * std::ceil((double)T / kWinKeys);
   return (double)s.B * s.Hkv * std::max(queries, keys);
 }

@@ -210,3 +210,10 @@ def test_backward_parts_without_tiles(B, T, Hq, Hkv, d, L, window, sinks, dtype,
     parts: a part that adds nothing leaves zeros."""
     for _ in range(3):
         test_backward(B, T, Hq, Hkv, d, L, window, sinks, dtype, lens)
+
+
+@pytest.mark.parametrize("B,T,Hq,Hkv,d,L,window,sinks", [
+    (1, 40, 4, 4, 64, 1, 3, 0), (2, 1100, 32, 8, 64, 32, 64, 40), (1, 90, 2, 1, 128, 7, 20, 9)])
+def test_prefill_f32_halves(B, T, Hq, Hkv, d, L, window, sinks):
+    """fp32 with a half of the waves without tiles, and grids past the halves."""
+    test_prefill(B, T, Hq, Hkv, d, L, window, sinks, FL, [T - 3 * b for b in range(B)])
