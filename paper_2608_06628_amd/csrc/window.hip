@@ -215,11 +215,11 @@ __device__ inline void win_cols_mma(typename WinF32<D>::Acc& acc, const typename
 #pragma unroll
     for (int ks = 0; ks < 16; ++ks) acc[ct] = Mma<float>::mma(t[row_of(ks, hh)][ct * kTile + li], x[ks], acc[ct]);
 }
-// acc^T (times f) to row `row` of out.
-template <typename T, int D>
+// acc^T (times f) to row `row` of out; entries CT0 * 32 .. CT1 * 32 - 1.
+template <typename T, int D, int CT0 = 0, int CT1 = D / kTile>
 __device__ inline void win_store(void* out, size_t row, const f32x16 (&acc)[D / kTile], float f, int hh, bool f32) {
 #pragma unroll
-  for (int ct = 0; ct < D / kTile; ++ct)
+  for (int ct = CT0; ct < CT1; ++ct)
 #pragma unroll
     for (int i = 0; i < 16; i += 4) {
       const float o[4] = {acc[ct][i] * f, acc[ct][i + 1] * f, acc[ct][i + 2] * f, acc[ct][i + 3] * f};
@@ -555,16 +555,77 @@ struct WinRing {
 // accumulators need no rescale.
 constexpr float kRefSlack = 8.0f;
 
+// Where workgroups are few and lists long, H = 2 halves of four waves take a unit's
+// tiles in turn, each through rings of its own, and join their sums in LDS.  The halves
+// have the same number of steps: one that is past the list's end copies the last tile
+// again and hides it.
 template <int D>
-__global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_ring_kernel(WindowArgs a, int wgs) {
+struct WinJoin {  // each half hands over the other's half of the entries
+  static constexpr int NH = D / kTile / 2;
+  float m[2][kWinWaves][kTile], l[2][kWinWaves][kTile];
+  f32x4 x[2][kWinWaves][NH * 4][kWave];
+
+  // Columns 32 NH O .. of a row's sums, for half O.
+  template <int O>
+  __device__ __attribute__((always_inline)) inline void give(int w, int lane, const f32x16 (&acc)[2 * NH]) {
+#pragma unroll
+    for (int ct = 0; ct < NH; ++ct)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        x[O][w][ct * 4 + e][lane] = f32x4{acc[O * NH + ct][4 * e], acc[O * NH + ct][4 * e + 1],
+                                          acc[O * NH + ct][4 * e + 2], acc[O * NH + ct][4 * e + 3]};
+  }
+  // Half O's own columns times f, plus the other's times fo.
+  template <int O>
+  __device__ __attribute__((always_inline)) inline void take(int w, int lane, f32x16 (&acc)[2 * NH], float f, float fo) const {
+#pragma unroll
+    for (int ct = 0; ct < NH; ++ct)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const f32x4 y = x[O][w][ct * 4 + e][lane];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[O * NH + ct][4 * e + k] = acc[O * NH + ct][4 * e + k] * f + y[k] * fo;
+      }
+  }
+};
+template <int D, int H, int R>
+struct WinSmem {
+  struct Rings {
+    bf16 k[H][R][kTile * D], v[H][R][kTile * D];
+  };
+  struct None {};
+  union {
+    Rings rings;
+    std::conditional_t<H == 2, WinJoin<D>, None> join;
+  };
+  __device__ WinSmem() {}
+};
+// A half's columns of a row.
+template <int D, int H>
+__device__ inline void win_store_half(void* out, size_t row, const f32x16 (&acc)[D / kTile], float f, int hh, bool f32,
+                                      int half) {
+  if constexpr (H == 1) {
+    win_store<bf16, D>(out, row, acc, f, hh, f32);
+  } else if (half == 0) {
+    win_store<bf16, D, 0, D / kTile / 2>(out, row, acc, f, hh, f32);
+  } else {
+    win_store<bf16, D, D / kTile / 2, D / kTile>(out, row, acc, f, hh, f32);
+  }
+}
+
+template <int D, int H>
+__global__ __launch_bounds__(kWave* kWinWaves* H, 2) void hyb_win_ring_kernel(WindowArgs a, int wgs) {
   typedef Mma<bf16> M;
   typedef M::op_t op_t;
   typedef WinRing<D> RG;
   constexpr int E = M::E, KW = M::KW, KD = D / KW, KL = kTile / KW, NCT = D / kTile, R = RG::R;
   constexpr int IPW = 2 * RG::IK / kWinWaves;  // copies per wave and step: waves 0, 1 K's, waves 2, 3 V's
-  __shared__ alignas(16) bf16 kr[R][kTile * D], vr[R][kTile * D];
+  __shared__ alignas(16) WinSmem<D, H, R> sh;
 
-  const int lane = threadIdx.x & (kWave - 1), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int half = wave / kWinWaves, w = wave % kWinWaves;
+  auto& kr = sh.rings.k[half];
+  auto& vr = sh.rings.v[half];
   const int li = lane & 31, hh = lane >> 5;
   const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv;
   int bg, x;
@@ -576,7 +637,8 @@ __global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_ring_kernel(Windo
   const int first = x * kWinWaves / G * kTile, last = min(((x + 1) * kWinWaves - 1) / G * kTile + kTile, len);
   if (first >= len) return;  // uniform
   const WinTiles tl(a, len, first, last, kTile);
-  const int ntiles = tl.n;
+  const int ntiles = (tl.n + H - 1) / H;  // of each half: the list's every H-th
+  auto key = [&](int n) __attribute__((always_inline)) { return tl.first(min(H * n + half, tl.n - 1), kTile); };
   const size_t qs = (size_t)Hq * D, ks_ = (size_t)Hkv * D;
   const bf16* K = (const bf16*)a.k + ((size_t)b * a.T * Hkv + g) * D;
   const bf16* V = (const bf16*)a.v + ((size_t)b * a.T * Hkv + g) * D;
@@ -606,7 +668,7 @@ __global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_ring_kernel(Windo
   }
   auto issue = [&](int n, bf16* dst) __attribute__((always_inline)) {
     if (n >= ntiles) return;
-    const int j0 = tl.first(n, kTile), left = len - 1 - j0;
+    const int j0 = key(n), left = len - 1 - j0;
     const bf16* base = (w < kWinWaves / 2 ? K : V) + (size_t)j0 * ks_;
     const __amdgpu_buffer_rsrc_t rs =
         __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(base), 0, (int)(kTile * ks_ * sizeof(bf16)), kBufferWord3);
@@ -628,10 +690,11 @@ __global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_ring_kernel(Windo
   // Takes the scores of tile n: masks, maximum, reference.
   auto take = [&](int n, const f32x16& s) __attribute__((always_inline)) {
     sc = s;
-    const int j0 = tl.first(n, kTile);
-    if (!win_full(r0, r1, a.n_sinks, j0, kTile)) {  // uniform
+    const int j0 = key(n);
+    const bool over = H > 1 && H * n + half >= tl.n;
+    if (over || !win_full(r0, r1, a.n_sinks, j0, kTile)) {  // uniform
 #pragma unroll
-      for (int e = 0; e < 16; ++e) sc[e] = row.sees(j0 + row_of(e, hh), a.n_sinks) ? sc[e] : -INFINITY;
+      for (int e = 0; e < 16; ++e) sc[e] = (!over & row.sees(j0 + row_of(e, hh), a.n_sinks)) ? sc[e] : -INFINITY;
     }
     float mt = sc[0];
 #pragma unroll
@@ -725,10 +788,31 @@ __global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_ring_kernel(Windo
   compute(std::true_type{}, ntiles - 1, nullptr, vr[ntiles - 1 - n]);
 
   l += xor32(l);
+  if constexpr (H == 2) {
+    mma_settle<bf16>();
+    lds_barrier_nodrain();  // the rings are read
+    if (hh == 0) {
+      sh.join.m[half][w][li] = m;
+      sh.join.l[half][w][li] = l;
+    }
+    if (half == 0)
+      sh.join.template give<1>(w, lane, acc);
+    else
+      sh.join.template give<0>(w, lane, acc);
+    lds_barrier_nodrain();
+    const float mo = sh.join.m[1 - half][w][li], mm = fmaxf(m, mo);
+    const float f = __builtin_amdgcn_exp2f(m - mm), fo = __builtin_amdgcn_exp2f(mo - mm);
+    if (half == 0)
+      sh.join.template take<0>(w, lane, acc, f, fo);
+    else
+      sh.join.template take<1>(w, lane, acc, f, fo);
+    l = l * f + sh.join.l[1 - half][w][li] * fo;
+    m = mm;
+  }
   const int i = me.i0 + li;
   if (i >= len) return;
-  win_store<bf16, D>(a.out, ((size_t)b * a.T + i) * Hq + me.h, acc, 1.0f / l, hh, a.s.out_f32);
-  if (a.lse && hh == 0) a.lse[((size_t)b * Hq + me.h) * a.T + i] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+  win_store_half<D, H>(a.out, ((size_t)b * a.T + i) * Hq + me.h, acc, 1.0f / l, hh, a.s.out_f32, half);
+  if (a.lse && hh == 0 && half == 0) a.lse[((size_t)b * Hq + me.h) * a.T + i] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
 // ---- bf16 gradient ----------------------------------------------------------
@@ -751,16 +835,19 @@ __device__ inline bf16x8 win_pieces(float x) {
   }
   return o;
 }
-template <int D>
-__global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_dq_ring_kernel(WindowArgs a, int wgs) {
+template <int D, int H>
+__global__ __launch_bounds__(kWave* kWinWaves* H, 2) void hyb_win_dq_ring_kernel(WindowArgs a, int wgs) {
   typedef Mma<bf16> M;
   typedef M::op_t op_t;
   typedef RowColTile<D> WT;
   constexpr int E = M::E, KW = M::KW, KD = D / KW, KL = kTile / KW, NCT = D / kTile, R = 4;
   constexpr int IPW = 2 * WT::IK / kWinWaves;  // copies per wave and step: waves 0, 1 K's, waves 2, 3 V's
-  __shared__ alignas(16) bf16 kr[R][kTile * D], vr[R][kTile * D];
+  __shared__ alignas(16) WinSmem<D, H, R> sh;
 
-  const int lane = threadIdx.x & (kWave - 1), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int half = wave / kWinWaves, w = wave % kWinWaves;
+  auto& kr = sh.rings.k[half];
+  auto& vr = sh.rings.v[half];
   const int li = lane & 31, hh = lane >> 5;
   const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv;
   int bg, x;
@@ -776,14 +863,15 @@ __global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_dq_ring_kernel(Wi
   const int row = me.i0 + li;
   // The statistics of row i, a half in each of its lanes; zero past the length.
   const auto put_stats = [&](float e, float s) __attribute__((always_inline)) {
-    if (me.i0 < a.T)
+    if (me.i0 < a.T && half == 0)
       reinterpret_cast<bf16x8*>(a.ws)[(((size_t)b * Hq + me.h) * win_tp(a.T) + row) * 2 + hh] =
           win_pieces(row < len ? (hh == 0 ? e : s) : 0.0f);
   };
   if (first >= len) put_stats(0.0f, 0.0f);
   if (first < len) {  // uniform
     const WinTiles tl(a, len, first, last, kTile);
-    const int ntiles = tl.n;
+    const int ntiles = (tl.n + H - 1) / H;
+    auto key = [&](int n) __attribute__((always_inline)) { return tl.first(min(H * n + half, tl.n - 1), kTile); };
     const size_t qs = (size_t)Hq * D, ks_ = (size_t)Hkv * D;
     const bf16* K = (const bf16*)a.k + ((size_t)b * a.T * Hkv + g) * D;
     const bf16* V = (const bf16*)a.v + ((size_t)b * a.T * Hkv + g) * D;
@@ -821,7 +909,7 @@ __global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_dq_ring_kernel(Wi
       if (n >= ntiles) return;
       const bool isk = w < kWinWaves / 2;
       bf16* dst = isk ? dk : dv;
-      const int j0 = tl.first(n, kTile), left = len - 1 - j0;
+      const int j0 = key(n), left = len - 1 - j0;
       const bf16* base = (isk ? K : V) + (size_t)j0 * ks_;
       const __amdgpu_buffer_rsrc_t rs =
           __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(base), 0, (int)(kTile * ks_ * sizeof(bf16)), kBufferWord3);
@@ -843,10 +931,11 @@ __global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_dq_ring_kernel(Wi
     auto take = [&](int n, const f32x16& s, const f32x16& d) __attribute__((always_inline)) {
       sc = s;
       dp = d;
-      const int j0 = tl.first(n, kTile);
-      if (!win_full(r0, r1, a.n_sinks, j0, kTile)) {  // uniform
+      const int j0 = key(n);
+      const bool over = H > 1 && H * n + half >= tl.n;
+      if (over || !win_full(r0, r1, a.n_sinks, j0, kTile)) {  // uniform
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sc[e] = mine.sees(j0 + row_of(e, hh), a.n_sinks) ? sc[e] : -INFINITY;
+        for (int e = 0; e < 16; ++e) sc[e] = (!over & mine.sees(j0 + row_of(e, hh), a.n_sinks)) ? sc[e] : -INFINITY;
       }
     };
     auto compute = [&](auto lastc, int n, const bf16* kn, const bf16* vn, const bf16* kt) __attribute__((always_inline)) {
@@ -898,10 +987,23 @@ __global__ __launch_bounds__(kWave* kWinWaves, 2) void hyb_win_dq_ring_kernel(Wi
     if (n + 2 < ntiles) step(n + 1, std::integral_constant<int, 1>{});
     if (n + 3 < ntiles) step(n + 2, std::integral_constant<int, 2>{});
     compute(std::true_type{}, ntiles - 1, nullptr, nullptr, kr[ntiles - 1 - n]);
+    if constexpr (H == 2) {
+      mma_settle<bf16>();
+      lds_barrier_nodrain();  // the rings are read
+      if (half == 0)
+      sh.join.template give<1>(w, lane, acc);
+    else
+      sh.join.template give<0>(w, lane, acc);
+      lds_barrier_nodrain();
+      if (half == 0)
+        sh.join.template take<0>(w, lane, acc, 1.0f, 1.0f);
+      else
+        sh.join.template take<1>(w, lane, acc, 1.0f, 1.0f);
+    }
   }
   if (row >= a.T) return;  // rows past the length: zero
-  win_store<bf16, D>(a.dq, ((size_t)b * a.T + row) * Hq + me.h, acc, row < len ? 1.0f / sqrtf((float)D) : 0.0f, hh,
-                     a.s.out_f32);
+  win_store_half<D, H>(a.dq, ((size_t)b * a.T + row) * Hq + me.h, acc, row < len ? 1.0f / sqrtf((float)D) : 0.0f, hh,
+                       a.s.out_f32, half);
 }
 
 // A workgroup owns 128 keys, a wave 32 of them.  At d = 128 it has two halves of
@@ -1137,11 +1239,24 @@ static int win_wgs(const WindowArgs& a) {
   return (int)((units + kWinWaves - 1) / kWinWaves);
 }
 
+// Whether n workgroups' units are taken in two halves (bf16): where at most two
+// workgroups of one half would share a CU and the longest lists have 32 tiles and
+// more (1 x 2048 tokens, 16 heads of d = 128, every earlier block: 256 workgroups, 51 us
+// in one half, now 41; 2 x 2048, 512 workgroups, 58 and 51; 1 x 4096, 8 heads of d = 64, 67
+// and 54; but a window of 512 for 1 x 4096, 8 heads, 17.5 and 18.2, and 1024 workgroups of
+// 1 x 8192, window 4096, 245 both).
+static bool win_halves(const WindowArgs& a, int n) {
+  const long seen = std::min<long>(a.T, (long)a.window + std::min(a.n_sinks, a.T) + a.s.L);
+  return n <= 512 && seen >= 32 * kTile;
+}
+
 template <int D>
 static hipError_t win_ring_go(const WindowArgs& a, hipStream_t st) {
-  const int wgs = win_wgs(a);
-  hipLaunchKernelGGL(hyb_win_ring_kernel<D>, dim3((unsigned)(a.s.B * a.s.Hkv * wgs)), dim3(kWave * kWinWaves), 0,
-                     st, a, wgs);
+  const int wgs = win_wgs(a), n = a.s.B * a.s.Hkv * wgs;
+  if (win_halves(a, n))
+    hipLaunchKernelGGL((hyb_win_ring_kernel<D, 2>), dim3((unsigned)n), dim3(kWave * kWinWaves * 2), 0, st, a, wgs);
+  else
+    hipLaunchKernelGGL((hyb_win_ring_kernel<D, 1>), dim3((unsigned)n), dim3(kWave * kWinWaves), 0, st, a, wgs);
   return hipGetLastError();
 }
 
@@ -1224,7 +1339,14 @@ static hipError_t win_backward_go(WindowArgs a, hipStream_t st) {
   const int wgs = win_wgs(a);
   const dim3 gq((unsigned)(a.s.B * a.s.Hkv * wgs)), gk((unsigned)(a.s.B * a.s.Hkv * cut.items()));
   if constexpr (sizeof(T) == 2) {
-    hipLaunchKernelGGL(hyb_win_dq_ring_kernel<D>, gq, dim3(kWave * kWinWaves), 0, st, a, wgs);
+    // (dQ in halves at d = 64 only, 1 x 4096 tokens as above 139 and 114 us with dK, dV;
+    // at d = 128 two halves need more registers than there are, and were no faster)
+    bool halves = false;
+    if constexpr (D == 64) {
+      halves = win_halves(a, a.s.B * a.s.Hkv * wgs);
+      if (halves) hipLaunchKernelGGL((hyb_win_dq_ring_kernel<D, 2>), gq, dim3(kWave * kWinWaves * 2), 0, st, a, wgs);
+    }
+    if (!halves) hipLaunchKernelGGL((hyb_win_dq_ring_kernel<D, 1>), gq, dim3(kWave * kWinWaves), 0, st, a, wgs);
     hipLaunchKernelGGL(hyb_win_dkv_ring_kernel<D>, gk, dim3(kWave * 4 * kWinHalves<D>), 0, st, a, cut);
   } else {
     hipLaunchKernelGGL(hyb_win_dq_kernel<D>, gq, dim3(kWave * kWinWaves), 0, st, a, wgs);

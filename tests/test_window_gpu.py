@@ -217,3 +217,13 @@ def test_backward_parts_without_tiles(B, T, Hq, Hkv, d, L, window, sinks, dtype,
 def test_prefill_f32_halves(B, T, Hq, Hkv, d, L, window, sinks):
     """fp32 with a half of the waves without tiles, and grids past the halves."""
     test_prefill(B, T, Hq, Hkv, d, L, window, sinks, FL, [T - 3 * b for b in range(B)])
+
+
+@pytest.mark.parametrize("B,T,Hq,Hkv,d,L,window,sinks,lens", [
+    (1, 1100, 4, 1, 128, 32, 1100, 0, None), (2, 1057, 2, 1, 64, 1, 1024, 3, [1057, 31]),
+    (1, 1090, 3, 3, 64, 32, 64, 1000, [1025]), (2, 1024, 2, 2, 128, 8, 1020, 0, [1, 1024])])
+def test_halves(B, T, Hq, Hkv, d, L, window, sinks, lens):
+    """Long lists and few workgroups: two halves take a list's tiles in turn,
+    one of them without any for the first queries."""
+    test_prefill(B, T, Hq, Hkv, d, L, window, sinks, BF, lens)
+    test_backward(B, T, Hq, Hkv, d, L, window, sinks, BF, lens)
