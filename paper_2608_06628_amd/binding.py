@@ -448,19 +448,22 @@ def _dptr(dev, t, name, dtype, shape=None):
 
 
 def _rows(dev, t, name, dtype, shape):
-    """The address and row stride of [N][H][d] whose rows [H][d] are contiguous."""
+    """The address and row stride of [N][H][d] whose rows [H][d] are contiguous.
+    (A stride of 0, of an expanded tensor, would mean contiguous rows to the library.)"""
     if t is None:
         return None, 0
     try:
         if t.get_device() == dev and t.dtype is dtype and t.shape == shape:
             s = t.stride()
             if s[2] == 1 and (s[1] == shape[2] or shape[1] == 1):
-                # (a stride says nothing where there is at most one row)
-                return t.data_ptr(), s[0] if shape[0] > 1 else 0
+                if shape[0] < 2:  # (a stride says nothing)
+                    return t.data_ptr(), 0
+                if s[0]:
+                    return t.data_ptr(), s[0]
     except AttributeError:
         pass
     _dptr(dev, t.contiguous() if isinstance(t, torch.Tensor) else t, name, dtype, shape)
-    raise ValueError(f"{name}: the heads of a token must be contiguous")
+    raise ValueError(f"{name}: the heads of a token must be contiguous, and the tokens apart")
 
 
 def _new(t, shape, dtype):

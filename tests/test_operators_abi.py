@@ -257,3 +257,14 @@ def test_more_workgroups_than_a_grid_holds():
     d = dims(batch=2 ** 31 - 1, n_q_heads=65536, n_kv_heads=65536)
     for make in (prefill, backward):
         assert make(d, T=1 << 30)() != 0 and "grid limit" in hb.last_error()
+
+
+def test_rows_of_a_tensor():
+    """Row strides as the library takes them: an expanded tensor has none."""
+    t = torch.zeros(6, 4, 64)
+    rows = lambda x: hb._rows(-1, x, "q", torch.float32, x.shape)[1]
+    assert rows(t) == 256 and rows(t[::2]) == 512 and rows(t[:1]) == 0 and rows(t[:0]) == 0
+    assert rows(t[:, :1]) == 256 and rows(t[:1].expand(1, 4, 64)) == 0
+    for bad in (t[:1].expand(6, 4, 64), t[:, :, ::2], t[:, ::2], t[:, :1].expand(6, 4, 64), t.transpose(0, 1)):
+        with pytest.raises((ValueError, TypeError)):
+            rows(bad)
