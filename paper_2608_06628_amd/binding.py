@@ -466,8 +466,14 @@ def _rows(dev, t, name, dtype, shape):
     raise ValueError(f"{name}: the heads of a token must be contiguous, and the tokens apart")
 
 
-def _new(t, shape, dtype):
-    return t.new_empty(shape) if dtype is t.dtype else t.new_empty(shape, dtype=dtype)
+_CONTIGUOUS = torch.contiguous_format
+
+
+def _new(t, dtype):
+    """A contiguous tensor like t, of dtype."""
+    if dtype is t.dtype:
+        return torch.empty_like(t, memory_format=_CONTIGUOUS)
+    return torch.empty_like(t, dtype=dtype, memory_format=_CONTIGUOUS)
 
 
 def _ws(dev, t):
@@ -517,9 +523,9 @@ def hybrid_qk_norm_rope(dev, q, k, inv_freq, positions, wq=None, wk=None, eps=1e
     or "interleaved".  Returns (q_out, k_out)."""
     odt = _odt(q.dtype, q_out, out_f32)
     if q_out is None:
-        q_out = _new(q, q.shape, odt)
+        q_out = _new(q, odt)
     if k_out is None:
-        k_out = _new(q, k.shape, odt)
+        k_out = _new(k, odt)
     dims, pq, pk, _, oq, ok, pwq, pwk, pos, freq = _rope_args(
         dev, q, k, wq, wk, inv_freq, positions, eps, rot_scale, layout, q_out, k_out, odt)
     _check(load().hybrid_qk_norm_rope(dims, pq, pk, pwq, pwk, pos, freq, oq, ok, _raw_stream(dev)))
@@ -535,9 +541,9 @@ def hybrid_qk_norm_rope_paged(dev, q, k, v, inv_freq, positions, slots, k_pages,
     Returns (q_out, k_out), k_out None unless given or asked for with want_k."""
     odt = _odt(q.dtype, q_out, out_f32)
     if q_out is None:
-        q_out = _new(q, q.shape, odt)
+        q_out = _new(q, odt)
     if k_out is None and want_k:
-        k_out = _new(q, k.shape, odt)
+        k_out = _new(k, odt)
     dims, pq, pk, pv, oq, ok, pwq, pwk, pos, freq = _rope_args(
         dev, q, k, wq, wk, inv_freq, positions, eps, rot_scale, layout, q_out, k_out, odt, v=v)
     n_pages, page_size = k_pages.shape[:2]
@@ -561,9 +567,9 @@ def hybrid_qk_norm_rope_backward(dev, q, k, dq_out, dk_out, inv_freq, positions,
     odt = _odt(q.dtype, dq, out_f32)
     at, f32, d = q.device, torch.float32, q.shape[2]
     if dq is None:
-        dq = _new(q, q.shape, odt)
+        dq = _new(q, odt)
     if dk is None:
-        dk = _new(q, k.shape, odt)
+        dk = _new(k, odt)
     dwq = torch.empty(d, dtype=f32, device=at) if wq is not None else None
     dwk = torch.empty(d, dtype=f32, device=at) if wk is not None else None
     dims, pq, pk, _, oq, ok, pwq, pwk, pos, freq = _rope_args(
@@ -678,9 +684,9 @@ def softmax_window_backward(dev, q, k, v, out, lse, dout, block, window, n_sinks
     act, at = q.dtype, q.device
     odt = _odt(act, dq, out_f32)
     dims, kv = _window_dims(q, k, block, odt)
-    dq = _new(q, q.shape, odt) if dq is None else dq
-    dk = _new(q, kv, odt) if dk is None else dk
-    dv = _new(q, kv, odt) if dv is None else dv
+    dq = _new(q, odt) if dq is None else dq
+    dk = _new(k, odt) if dk is None else dk
+    dv = _new(v, odt) if dv is None else dv
     if ws is None:
         need = lib.hybrid_workspace_bytes(dims, OP_WINDOW_BACKWARD, T)
         ws = torch.empty(need, dtype=torch.uint8, device=at)
