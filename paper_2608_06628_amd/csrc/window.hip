@@ -105,6 +105,7 @@ __device__ inline void win_place(int bid, int nbg, int& bg, int& x) {
 constexpr int kWinKeys = 4 * kTile;
 struct WinParts {
   int wgs, ns, ps, p;
+  bool halves;  // (bf16) workgroups of two halves
   __host__ __device__ int items() const { return ns * ps + (wgs - ns) * p; }
   // Rows of partial sums of dK and dV: ps for the first ns workgroups' keys
   // (padded), then p of every key, each where there is more than one.
@@ -997,9 +998,9 @@ __global__ __launch_bounds__(kWave* kWinWaves* H, 2) void hyb_win_dq_ring_kernel
       mma_settle<bf16>();
       lds_barrier_nodrain();  // the rings are read
       if (half == 0)
-      sh.join.template give<1>(w, lane, acc);
-    else
-      sh.join.template give<0>(w, lane, acc);
+        sh.join.template give<1>(w, lane, acc);
+      else
+        sh.join.template give<0>(w, lane, acc);
       lds_barrier_nodrain();
       if (half == 0)
         sh.join.template take<0>(w, lane, acc, 1.0f, 1.0f);
@@ -1012,17 +1013,13 @@ __global__ __launch_bounds__(kWave* kWinWaves* H, 2) void hyb_win_dq_ring_kernel
                        a.s.out_f32, half);
 }
 
-// A workgroup owns 128 keys, a wave 32 of them.  At d = 128 it has two halves of
-// four waves, which take the query tiles in turn and join their sums in LDS at
-// the end, so that two waves share a SIMD with the LDS of one workgroup (dK and dV
-// take 128 registers, K 32, the scores and dP 32; V is read from LDS).  At d = 64
-// three workgroups of four waves fit a CU.
-template <int D>
-constexpr int kWinHalves = D == 128 ? 2 : 1;
-
-template <int D>
-__global__ __launch_bounds__(kWave * 4 * kWinHalves<D>, 2) void hyb_win_dkv_ring_kernel(WindowArgs a, WinParts cut) {
-  constexpr int H = kWinHalves<D>;
+// A workgroup owns 128 keys, a wave 32 of them.  With H = 2 it has two halves of
+// four waves, which take the query tiles in turn and join their sums in LDS at the
+// end: at d = 128, so that two waves share a SIMD with the LDS of one workgroup (dK and
+// dV take 128 registers, K 32, the scores and dP 32; V is read from LDS); at d = 64, where
+// three workgroups of four waves fit a CU, where there are fewer (win_cut).
+template <int D, int H>
+__global__ __launch_bounds__(kWave * 4 * H, 2) void hyb_win_dkv_ring_kernel(WindowArgs a, WinParts cut) {
   typedef Mma<bf16> M;
   typedef M::op_t op_t;
   typedef RowColTile<D> WT;
@@ -1283,11 +1280,15 @@ static hipError_t win_prefill_f32_go(const WindowArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-// The cut.  A part costs its start and end (`fixed` query tiles' time) besides its
-// tiles, the chip works through 256 lists at full speed (bf16 at d = 64: 512), and
-// more parts than one cost the sums' traffic and a launch; p is the number
-// with the least estimated time, in units of a query tile (bf16: 0.35 us, or 0.7
-// for the workgroups of d = 64, which take one tile at a time).
+// The cut: parts and, on bf16 at d = 64, halves, with the least estimated time (us): a
+// list costs its start and end (`fixed`) besides its query tiles (`unit` each), the chip
+// takes a workgroup of two halves per CU at a time (without halves, or on fp32, several
+// share one), and more parts than one cost the sums' traffic and a launch.  The
+// numbers are fitted to 23 shapes of bf16 with up to 16 parts, where what this takes is
+// within 1.3% of the best on average and 8% in each.  (d = 128, 2 x 1024 tokens, window
+// 200, 16 and 4 heads: 60 us in 1 part, 48 in 3, 46.5 in 4, which are 256 lists, 58 in 5.  d =
+// 64, 2 x 3001, window 511, 8 and 2 heads: no halves, 1 to 5 parts 89, 65, 56, 58, 56; halves, 67, 54,
+// 60, 61, 58.)
 // The sinks' keys are cut into parts as long as the others', as long as those
 // are at most 16 per (request, KV head) and 512 in all.
 static int win_sink_parts(const Shape& s) { return (int)std::min<long>(16, 512 / std::max<long>(1, (long)s.B * s.Hkv)); }
@@ -1305,14 +1306,20 @@ static WinParts win_cut(const Shape& s, int T, int window, int n_sinks) {
   const double seen = std::min(every, std::ceil(((double)window + s.L + kWinKeys) / kTile) + 1);  // tiles of a head
   const double mean = seen - seen * seen / (2 * every);  // (the last keys' lists end early)
   const bool f32 = s.dtype != 1;
-  const double unit = f32 ? 3.5 : s.D == 64 ? 0.7 : 0.35, lists = !f32 && s.D == 64 ? 512 : 256;
-  const double fixed = 5.5 / unit, launch = 5 / unit, sum = (double)s.B * T * s.Hkv * s.D * 3.5e-6 / unit;
+  const double launch = 4.5, sum = (double)s.B * T * s.Hkv * s.D * (f32 ? 3.5e-6 : 2.5e-6);
   double best = 0;
-  for (int p = 1; p <= win_most_parts(s, T); ++p) {
-    const double t = std::max(fixed + seen * G / p, all * (p * fixed + mean * G) / lists) + (p > 1 ? launch + p * sum : 0);
-    if (p == 1 || t < best) {
-      best = t;
-      c.p = p;
+  c.p = 0;
+  for (int h = f32 || s.D == 64 ? 1 : 2; h <= (f32 ? 1 : 2); ++h) {
+    const double unit = f32 ? 3.5 : s.D == 128 ? 0.75 : h == 1 ? 0.65 : 0.4;
+    const double fixed = f32 ? 5.5 : s.D == 128 ? 6.0 : h == 1 ? 1.0 : 2.5;
+    for (int p = 1; p <= win_most_parts(s, T); ++p) {
+      const double rounds = h == 2 ? std::ceil(all * p / 256) : std::max(1.0, all * p / (f32 ? 256 : 450));
+      const double t = rounds * fixed + G * unit / p * std::max(seen, rounds * mean) + (p > 1 ? launch + p * sum : 0);
+      if (c.p == 0 || t < best) {
+        best = t;
+        c.p = p;
+        c.halves = h == 2;
+      }
     }
   }
   const int each = (int)std::ceil(seen * G / c.p);
@@ -1353,7 +1360,10 @@ static hipError_t win_backward_go(WindowArgs a, hipStream_t st) {
       if (halves) hipLaunchKernelGGL((hyb_win_dq_ring_kernel<D, 2>), gq, dim3(kWave * kWinWaves * 2), 0, st, a, wgs);
     }
     if (!halves) hipLaunchKernelGGL((hyb_win_dq_ring_kernel<D, 1>), gq, dim3(kWave * kWinWaves), 0, st, a, wgs);
-    hipLaunchKernelGGL(hyb_win_dkv_ring_kernel<D>, gk, dim3(kWave * 4 * kWinHalves<D>), 0, st, a, cut);
+    if constexpr (D == 64) {
+      if (!cut.halves) hipLaunchKernelGGL((hyb_win_dkv_ring_kernel<D, 1>), gk, dim3(kWave * 4), 0, st, a, cut);
+    }
+    if (D == 128 || cut.halves) hipLaunchKernelGGL((hyb_win_dkv_ring_kernel<D, 2>), gk, dim3(kWave * 8), 0, st, a, cut);
   } else {
     hipLaunchKernelGGL(hyb_win_dq_kernel<D>, gq, dim3(kWave * kWinWaves), 0, st, a, wgs);
     hipLaunchKernelGGL(hyb_win_dkv_kernel<D>, gk, dim3(kWave * kWinWaves), 0, st, a, cut);
@@ -1383,7 +1393,7 @@ hipError_t launch_window_backward(const WindowArgs& a, hipStream_t st) {
 double window_threads(const Shape& s, int T) {
   const long units = ((long)T + kTile - 1) / kTile * (s.Hq / s.Hkv);
   const double queries = kWave * kWinWaves * 2 * (double)((units + kWinWaves - 1) / kWinWaves);
-  const double keys = kWave * 4 * kWinHalves<128> * std::ceil((double)T / kWinKeys);
+  const double keys = kWave * kWinWaves * 2 * std::ceil((double)T / kWinKeys);
   return (double)s.B * s.Hkv * std::max(queries, keys);
 }
 

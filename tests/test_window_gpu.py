@@ -227,3 +227,11 @@ def test_halves(B, T, Hq, Hkv, d, L, window, sinks, lens):
     one of them without any for the first queries."""
     test_prefill(B, T, Hq, Hkv, d, L, window, sinks, BF, lens)
     test_backward(B, T, Hq, Hkv, d, L, window, sinks, BF, lens)
+
+
+@pytest.mark.parametrize("B,T,Hq,Hkv,L,window,sinks,lens", [
+    (1, 700, 2, 2, 32, 30, 0, [650]), (2, 3001, 2, 1, 1, 511, 4, [3001, 2500]), (4, 290, 4, 2, 16, 290, 0, None),
+    (4, 1500, 4, 4, 32, 1500, 0, [1500, 3, 0, 700])])
+def test_backward_halves(B, T, Hq, Hkv, L, window, sinks, lens):
+    """d = 64: keys' workgroups with and without halves, in one part and in more."""
+    test_backward(B, T, Hq, Hkv, 64, L, window, sinks, BF, lens)
