@@ -1282,11 +1282,11 @@ static hipError_t win_prefill_f32_go(const WindowArgs& a, hipStream_t st) {
 
 // The cut: parts and, on bf16 at d = 64, halves, with the least estimated time (us): a
 // list costs its start and end (`fixed`) besides its query tiles (`unit` each), the chip
-// takes a workgroup of two halves per CU at a time (without halves, or on fp32, several
-// share one), and more parts than one cost the sums' traffic and a launch.  The
-// numbers are fitted to 23 shapes of bf16 with up to 16 parts, where what this takes is
-// within 1.3% of the best on average and 8% in each.  (d = 128, 2 x 1024 tokens, window
-// 200, 16 and 4 heads: 60 us in 1 part, 48 in 3, 46.5 in 4, which are 256 lists, 58 in 5.  d =
+// takes a workgroup per CU at a time (on bf16 at d = 64 without halves several share one),
+// and more parts than one cost the sums' traffic and a launch.  The numbers are fitted to 23
+// shapes of bf16 and 16 of fp32 with up to 16 parts, where what this takes is within 2%
+// of the best on average and 11% in each.  (d = 128, 2 x 1024 tokens, window 200, 16 and 4 heads:
+// 60 us in 1 part, 48 in 3, 46.5 in 4, which are 256 lists, 58 in 5; fp32 538, 245, 208, 258.  d =
 // 64, 2 x 3001, window 511, 8 and 2 heads: no halves, 1 to 5 parts 89, 65, 56, 58, 56; halves, 67, 54,
 // 60, 61, 58.)
 // The sinks' keys are cut into parts as long as the others', as long as those
@@ -1310,10 +1310,10 @@ static WinParts win_cut(const Shape& s, int T, int window, int n_sinks) {
   double best = 0;
   c.p = 0;
   for (int h = f32 || s.D == 64 ? 1 : 2; h <= (f32 ? 1 : 2); ++h) {
-    const double unit = f32 ? 3.5 : s.D == 128 ? 0.75 : h == 1 ? 0.65 : 0.4;
-    const double fixed = f32 ? 5.5 : s.D == 128 ? 6.0 : h == 1 ? 1.0 : 2.5;
+    const double unit = f32 ? 6.0 * s.D / 64 : s.D == 128 ? 0.75 : h == 1 ? 0.65 : 0.4;
+    const double fixed = f32 || s.D == 128 ? 6.0 : h == 1 ? 1.0 : 2.5;
     for (int p = 1; p <= win_most_parts(s, T); ++p) {
-      const double rounds = h == 2 ? std::ceil(all * p / 256) : std::max(1.0, all * p / (f32 ? 256 : 450));
+      const double rounds = f32 || h == 2 ? std::ceil(all * p / 256) : std::max(1.0, all * p / 450);
       const double t = rounds * fixed + G * unit / p * std::max(seen, rounds * mean) + (p > 1 ? launch + p * sum : 0);
       if (c.p == 0 || t < best) {
         best = t;
