@@ -214,3 +214,21 @@ def test_other_stream_and_graph():
         b = hb.hybrid_qk_norm_rope_backward(q, k, *o, freq, pos, wq, wk)
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(out + back, o + b)), i
+
+
+def test_ways_to_call():
+    """By name, and on a stream given as an object, a raw handle or the null stream."""
+    q, k, _, pos, freq, wq, wk = make(70, 8, 2, 64, 64, BF, 3, packed=False)
+    want = hb.hybrid_qk_norm_rope(q, k, freq, pos, wq, wk)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    for stream in (s, s.cuda_stream, 0, torch.cuda.default_stream()):
+        got = hb.hybrid_qk_norm_rope(q=q, k=k, inv_freq=freq, positions=pos, wq=wq, wk=wk, stream=stream)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), stream
+    with pytest.raises(ValueError):
+        hb.hybrid_qk_norm_rope(q[:1].expand(70, 8, 64), k, freq, pos, wq, wk)
+    with pytest.raises((TypeError, ValueError)):
+        hb.hybrid_qk_norm_rope(q, k, freq.float(), pos, wq, wk)
+    with pytest.raises((TypeError, ValueError)):
+        hb.hybrid_qk_norm_rope(q, k, freq, pos.long(), wq, wk)
