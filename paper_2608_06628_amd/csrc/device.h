@@ -429,13 +429,14 @@ __device__ inline void buf_to_lds16(__amdgpu_buffer_rsrc_t r, void* lds, int vof
 
 // The wait states between a 32x32 product and a read of its result, for
 // places where a branch stands between the two: the compiler (ROCm 7.2) counts
-// them along one path only, and a read six states after a bf16 product (which
-// needs 11) found its last registers from before the product.
+// them along one path only, and a read six states after a bf16 product found
+// its last registers from before the product.  It needs 12 (fp32 18; a 16x16
+// product 8 and 10), which is what the compiler leaves in straight code.
 template <typename T>
 __device__ inline void mma_settle() {
   __builtin_amdgcn_sched_barrier(0);
   if constexpr (sizeof(T) == 2)
-    asm volatile("s_nop 10");
+    asm volatile("s_nop 11");
   else
     asm volatile("s_nop 15\n\ts_nop 1");
   __builtin_amdgcn_sched_barrier(0);

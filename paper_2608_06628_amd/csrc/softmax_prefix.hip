@@ -359,12 +359,11 @@ struct SpRef {
   // (what it was is left in ref for the rescale, and set by the caller).
   __device__ inline bool take(float mt, bool restart, float& next) {
     most = fmaxf(most, mt);
-    if (restart) {  // uniform
-      const float w = fmaxf(mt, most - 100.0f);  // (finite after a finite tile)
-      next = w + fmaxf(0.0f, ceilf(most - w));
-    } else {
-      next = fmaxf(ref, mt);
-    }
+    const float w = fmaxf(mt, most - 100.0f);  // (finite after a finite tile)
+    const float anew = w + fmaxf(0.0f, ceilf(most - w)), on = fmaxf(ref, mt);
+    // A select although restart is uniform: with a branch, the wait states between
+    // P V and the rescale were counted along the longer way (mma_settle).
+    next = restart ? anew : on;
     return __any(next != ref);
   }
 };
@@ -557,11 +556,14 @@ __global__ __launch_bounds__(kWave* NG) void hyb_sp_partial_kernel(
         acc[ct] = M::mma(vt_op(buf, ct, ks), cvt_op<T>(&p[ks * E]), acc[ct]);
     if constexpr (WIN) mma_settle<T>();
     if (after(j0, n, 1) < hi) put(nx, buf ^ 1);  // next tile into the free buffer
+    // (the next step may move the sums between registers before it branches)
+    if constexpr (!WIN && sizeof(T) == 4) mma_settle<T>();
     nx = af;
     __syncthreads();
   }
 
   // Partial result of this range: unnormalised O, running max and sum.
+  mma_settle<T>();
   if (li >= Lb) return;
   if (rg.n == 1) {
     // one range: the result is final, normalised here
@@ -988,7 +990,7 @@ __global__ __launch_bounds__(kWave* NG, D == 64 && NG == 8 ? 4 : 2) void hyb_sp_
   lds_barrier_nodrain();
   const int rest = ntiles - n;  // 1 .. R
   compute(yes, ntiles - 1, nullptr, rest == 2 ? s1.v : rest == 3 ? s2.v : rest == 4 ? s3.v : s0.v);
-  if constexpr (WIN) mma_settle<bf16>();
+  mma_settle<bf16>();
 
   if (li >= Lb) return;
   const float l = lsum[0];

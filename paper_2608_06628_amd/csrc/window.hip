@@ -707,6 +707,7 @@ __global__ __launch_bounds__(kWave* kWinWaves* H, 2) void hyb_win_ring_kernel(Wi
     for (int e = 1; e < 16; ++e) mt = fmaxf(mt, sc[e]);
     mt = fmaxf(mt, xor32(mt)) * scale;
     if (__any(mt > m + kRefSlack)) {
+      mma_settle<bf16>();
       const float mn = mt > m + kRefSlack ? mt : m;
       const float corr = __builtin_amdgcn_exp2f(m - mn);
       l *= corr;
