@@ -12,6 +12,7 @@ import contextlib
 import ctypes
 import functools
 import inspect
+import operator
 import os
 
 import torch
@@ -151,7 +152,14 @@ def _stream(stream):
     return getattr(stream, "cuda_stream", stream)
 
 
+# (ctypes keeps the low 32 bits of a larger number and says nothing: what a caller
+# gives as a number is compared with this, not what a tensor's memory bounds)
+_I32 = 2 ** 31 - 1
+
+
 def make_dims(B, Hq, Hkv, d, L, f, dtype, n_slots, flags=0) -> Dims:
+    if not -_I32 <= L <= _I32:
+        raise ValueError(f"a block of {L} tokens is not supported")
     return Dims(B, Hq, Hkv, d, L, f, dtype, n_slots, flags)
 
 
@@ -312,13 +320,13 @@ def softmax_prefix_step_paged(q, k, v, k_pages, v_pages, page_table, prefix_len,
     B, L, Hq, d = q.shape
     Hkv = k.shape[2]
     n_pages, page_size = k_pages.shape[0], k_pages.shape[1]
-    max_pages = page_table.shape[1]
+    max_pages = min(page_table.shape[1], _I32)
     act = q.dtype
     flags, odt = _out_flags(out, act, out_f32)
     dims = make_dims(B, Hq, Hkv, d, L, 64, _dt(q), 1, flags)
     if out is None:
         out = torch.empty(q.shape, dtype=odt, device=q.device)
-    need = workspace_bytes(dims, OP_SOFTMAX_PREFIX, max_pages * page_size)
+    need = workspace_bytes(dims, OP_SOFTMAX_PREFIX, min(max_pages * page_size, _I32))
     if need and ws is None:
         ws = torch.empty(need, dtype=torch.uint8, device=q.device)
     _check(lib.softmax_prefix_step_paged(
@@ -593,18 +601,28 @@ def kv_pages_plan(dev, prefix_len, new_len, page_table, free_pages, page_size, m
     token_start [B + 1], counts [2]: pages taken and missing)."""
     B, max_pages = page_table.shape
     i32, at = torch.int32, prefix_len.device
+    if not (0 <= max_tokens <= _I32 and -_I32 <= page_size <= _I32 and max_pages <= _I32):
+        raise ValueError(f"max_tokens {max_tokens}, page_size {page_size} and a table of {max_pages} "
+                         "pages per request must be 0 .. 2^31 - 1")
     if B == 0:
         return (torch.full((max_tokens,), -1, dtype=i32, device=at),
                 *(torch.zeros(n, dtype=i32, device=at) for n in (max_tokens, 1, 2)))
     lens = _dptr(dev, prefix_len, "prefix_len", i32, (B,))
     slots, positions, start, counts = map(prefix_len.new_empty, (max_tokens, max_tokens, B + 1, 2))
     _check(load().kv_pages_plan(
-        B, max_pages, page_size, free_pages.numel() if free_pages is not None else 0, max_tokens,
+        B, max_pages, page_size, min(free_pages.numel(), _I32) if free_pages is not None else 0,
+        max_tokens,
         lens, _dptr(dev, new_len, "new_len", i32, (B,)),
         _dptr(dev, free_pages, "free_pages", i32), _dptr(dev, page_table, "page_table", i32),
         slots.data_ptr(), positions.data_ptr(), start.data_ptr(), counts.data_ptr(),
         _raw_stream(dev)))
     return slots, positions, start, counts
+
+
+def _reach(n):
+    """A window or a number of sinks: one past 2^31 - 1 sees what that one sees (the
+    library refuses those below 0)."""
+    return max(min(operator.index(n), _I32), -1)
 
 
 def _window_dims(q, k, block, odt):
@@ -629,10 +647,11 @@ def softmax_window_step_paged(dev, q, k, v, k_pages, v_pages, page_table, prefix
         out = new(q.shape, dtype=odt, device=q.device)
     n_pages, page_size = k_pages.shape[:2]
     pool = (n_pages, page_size, kv[2], d)
-    max_pages = page_table.shape[1]
+    max_pages = min(page_table.shape[1], _I32)
+    window, n_sinks = _reach(window), _reach(n_sinks)
     if ws is None:
         need = lib.hybrid_workspace_bytes(dims, OP_WINDOW_STEP,
-                                          min(max_pages * page_size, window + n_sinks + 64))
+                                          min(max_pages * page_size, window + n_sinks + 64, _I32))
         ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
     _check(lib.softmax_window_step_paged(
         dims, _dptr(dev, q, "q", act), _dptr(dev, k, "k", act, kv), _dptr(dev, v, "v", act, kv),
@@ -649,14 +668,15 @@ def softmax_window_prefill(dev, q, k, v, block, window, n_sinks=0, seq_lens=None
                            lse=None, want_lse=True, ws=None, out_f32=False):
     """Softmax of q [B][T][Hq][d] over k, v [B][T][Hkv][d], block-causal in blocks
     of `block` tokens, over the block, the `window` tokens before it and the
-    first n_sinks.  seq_lens [B] int32 (device): rows past them of out and lse
-    are left as they were (zero if made here).  Returns (out, lse fp32
-    [B][Hq][T] or None)."""
+    first n_sinks (a window of T or more: every earlier block).  seq_lens [B]
+    int32 (device): rows past them of out and lse are left as they were (zero if
+    made here).  Returns (out, lse fp32 [B][Hq][T] or None)."""
     lib = load()
     B, T, Hq, d = q.shape
     act, f32 = q.dtype, torch.float32
     odt = _odt(act, out, out_f32)
     dims, kv = _window_dims(q, k, block, odt)
+    window, n_sinks = _reach(window), _reach(n_sinks)
     new = torch.empty if seq_lens is None else torch.zeros
     if out is None:
         out = new(q.shape, dtype=odt, device=q.device)
@@ -684,6 +704,7 @@ def softmax_window_backward(dev, q, k, v, out, lse, dout, block, window, n_sinks
     act, at = q.dtype, q.device
     odt = _odt(act, dq, out_f32)
     dims, kv = _window_dims(q, k, block, odt)
+    window, n_sinks = _reach(window), _reach(n_sinks)
     dq = _new(q, odt) if dq is None else dq
     dk = _new(k, odt) if dk is None else dk
     dv = _new(v, odt) if dv is None else dv

@@ -235,3 +235,10 @@ def test_halves(B, T, Hq, Hkv, d, L, window, sinks, lens):
 def test_backward_halves(B, T, Hq, Hkv, L, window, sinks, lens):
     """d = 64: keys' workgroups with and without halves, in one part and in more."""
     test_backward(B, T, Hq, Hkv, 64, L, window, sinks, BF, lens)
+
+
+@pytest.mark.parametrize("window,sinks", [(1 << 32, 0), ((1 << 40) + 5, 1 << 32), (0, 1 << 31), (16, (1 << 32) + 3)])
+def test_windows_past_32_bits(window, sinks):
+    """A window or a number of sinks past 2^31 - 1 sees all there is."""
+    test_prefill(1, 130, 4, 2, 64, 16, window, sinks, BF, [120])
+    test_backward(1, 130, 4, 2, 64, 16, window, sinks, BF, [120])

@@ -190,3 +190,11 @@ def test_batches(B, L, Hq, Hkv, d, window, sinks):
     c = make(B, L, Hq, Hkv, d, 32, lens, BF, B + L)
     hide(c, window, sinks)
     check(c, window, sinks, [(i * 7) % (L + 1) for i in range(B)], what="batch")
+
+
+@pytest.mark.parametrize("window,sinks", [(1 << 32, 0), ((1 << 40) + 5, 1 << 32), (3, (1 << 32) + 1)])
+def test_windows_past_32_bits(window, sinks):
+    """A window or a number of sinks past 2^31 - 1 sees all there is."""
+    c = make(2, 5, 8, 2, 64, 32, [200, 33], BF, 8)
+    hide(c, window, sinks)
+    check(c, window, sinks, what="past 32 bits")
