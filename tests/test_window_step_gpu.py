@@ -7,7 +7,7 @@ import torch
 from paper_2608_06628_amd import binding as hb
 
 from _helpers import announce
-from _window_ref import assert_within, attend, rows64
+from _window_ref import add_scores, assert_within, attend, climb, rows64
 
 pytestmark = pytest.mark.gpu
 BF, FL = torch.bfloat16, torch.float32
@@ -198,3 +198,30 @@ def test_windows_past_32_bits(window, sinks):
     c = make(2, 5, 8, 2, 64, 32, [200, 33], BF, 8)
     hide(c, window, sinks)
     check(c, window, sinks, what="past 32 bits")
+
+
+@pytest.mark.parametrize("shape", ["grow", "fall", "late", "spike"])
+@pytest.mark.parametrize("B,L,Hq,Hkv,d,page,lens,window,sinks,dtype", [
+    (3, 1, 16, 4, 128, 64, [1500, 700, 90], 1200, 40, BF),   # one token: four waves take the tiles in turn
+    (2, 5, 8, 8, 64, 32, [900, 390], 800, 0, BF),            # a head per KV head
+    (1, 1, 16, 4, 128, 64, [9000], 8000, 70, BF),            # ranges that are merged
+    (70, 32, 8, 2, 64, 32, [i * 17 % 900 for i in range(70)], 700, 33, BF),  # blocks, in two halves
+    (70, 32, 4, 2, 128, 32, [i * 17 % 900 for i in range(70)], 700, 33, BF),
+    (40, 32, 32, 4, 128, 64, [i * 31 % 900 for i in range(40)], 700, 33, BF),  # eight heads: the copy ring
+    (60, 32, 24, 8, 64, 32, [i * 31 % 700 for i in range(60)], 500, 40, BF),   # three: staged in registers
+    (3, 21, 8, 4, 64, 32, [700, 390, 64], 600, 5, FL),
+    (2, 1, 4, 1, 128, 64, [5000, 900], 4500, 64, FL)])
+def test_references_that_move(shape, B, L, Hq, Hkv, d, page, lens, window, sinks, dtype):
+    """Scores that climb or fall along the cache by far more than the slack of a
+    query's reference: waves, halves and ranges end on different ones."""
+    c = make(B, L, Hq, Hkv, d, page, lens, dtype, B + L)
+    for b, n in enumerate(lens):
+        j = np.arange(n)
+        at = c["table"][b].cpu().numpy()[j // page].astype(np.int64) * page + j % page
+        rows = torch.from_numpy(at).cuda()
+        pool = c["kp"].view(-1, Hkv, d)
+        keys = torch.cat([pool[rows], c["k"][b]])
+        c["q"][b], keys = add_scores(c["q"][b], keys, climb(shape, n + L))
+        pool[rows], c["k"][b] = keys[:n], keys[n:]
+    hide(c, window, sinks)
+    check(c, window, sinks, what=shape)
