@@ -225,3 +225,23 @@ def test_references_that_move(shape, B, L, Hq, Hkv, d, page, lens, window, sinks
         pool[rows], c["k"][b] = keys[:n], keys[n:]
     hide(c, window, sinks)
     check(c, window, sinks, what=shape)
+
+
+@pytest.mark.parametrize("B,L,Hq,Hkv,d,lens", [
+    (3, 32, 16, 4, 128, [700, 64, 2000]), (40, 32, 16, 4, 64, [i * 53 % 2000 for i in range(40)]),
+    (2, 1, 8, 2, 128, [1990, 333]), (24, 32, 16, 2, 128, [i * 83 % 2000 for i in range(24)])])
+def test_all_of_the_cache_by_row(B, L, Hq, Hkv, d, lens):
+    """A window of the whole prefix and softmax_prefix_step_paged, both within what
+    the weights' roundings allow of each row."""
+    c = make(B, L, Hq, Hkv, d, 64, lens, BF, 5)
+    check(c, 2048, 0, what="window")
+    out = hb.softmax_prefix_step_paged(c["q"], c["k"], c["v"], c["kp"], c["vp"], c["table"], c["lens"], out_f32=True)
+    torch.cuda.synchronize()
+    for b, n in enumerate(lens):
+        row = c["table"][b].cpu().numpy()[np.arange(n) // 64].astype(np.int64) * 64 + np.arange(n) % 64
+        kc, vc = (rows64(p.view(-1, Hkv, d)[torch.from_numpy(row).cuda()]) for p in (c["kp"], c["vp"]))
+        kb, vb = np.concatenate([kc, rows64(c["k"][b])]), np.concatenate([vc, rows64(c["v"][b])])
+        for h in range(0, Hq, 3):
+            g = h * Hkv // Hq
+            o, _, err, _ = attend(rows64(c["q"][b, :, h]), kb[:, g], vb[:, g], np.ones((L, len(kb)), bool), True)
+            assert_within(out[b, :, h], o, err * 1.001 + 2.0 ** -8 * 1.01 * np.abs(o), FL, f"prefix b={b} h={h}")
