@@ -409,9 +409,10 @@ typedef struct {
  * positions int32 [N] (any value); inv_freq double [rot_dim / 2], radians per
  * position: angles are formed in 64 bits, so far positions keep their phase, and
  * every scaling of positions for long contexts is a table (may be NULL
- * when rot_dim is 0).  Arithmetic is fp32, rounded once; an x whose squares
- * leave fp32 (about 1e19) gives zeros.  q_out and k_out may
- * be interleaved in one buffer, and must not overlap each other or an input. */
+ * when rot_dim is 0).  Arithmetic is fp32, rounded once; a row whose sum of
+ * squares leaves fp32 (about 3e38) gives zeros where it is normalised.  q_out
+ * and k_out may be interleaved in one buffer, and must not overlap each other
+ * or an input. */
 int hybrid_qk_norm_rope(const hyb_rope_dims_t* dims, const void* q,
                         const void* k, const void* wq, const void* wk,
                         const int32_t* positions, const double* inv_freq,

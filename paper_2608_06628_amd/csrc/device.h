@@ -448,7 +448,6 @@ template <int D>
 struct RowColTile {
   static constexpr int EPC = 8, CPR = D / EPC;
   static constexpr int RPI = kWave / CPR, IK = kTile / RPI;
-  static constexpr int kBytes = kTile * D * 2;
   // Chunk c of row t sits at c ^ swz(t): the 16 rows that fill the banks have
   // 16 places for one chunk (row reads), and four rows from a multiple of four on
   // fall in different groups of four chunks (transposing reads).

@@ -100,7 +100,8 @@ struct Turn {
     for (int i = 0; i < 4; ++i) freq[i] = rot ? a.inv_freq[4 * r + i] * 0.15915494309189535 : 0.0;
   }
   // The angles in turns, reduced to half a turn in 64 bits; their sines and
-  // cosines in 32.
+  // cosines in 32 (the reduced angle's rounding moves it by at most 2^-26 of a turn,
+  // 9e-8 rad, an fp32 rounding).
   __device__ inline void at(int pos, float scale) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {

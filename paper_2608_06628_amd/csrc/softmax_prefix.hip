@@ -1143,6 +1143,8 @@ struct SpAcc {
         for (int e = 0; e < 16; ++e) acc[ct][e] *= corr;
       m = mn;
     }
+    // The weights enter P V rounded to bf16 (each off by at most 2^-8 of itself;
+    // products of fp32 run at 1/16 of the rate); their sum is over the unrounded ones.
     bf16x8 pop[KL];
     float sum[4] = {};
 #pragma unroll

@@ -743,6 +743,9 @@ __global__ __launch_bounds__(kWave* kWinWaves* H, 2) void hyb_win_ring_kernel(Wi
       s1 += p[e + 1];
     }
     l += s0 + s1;
+    // The weights enter P V rounded to bf16 (each off by at most 2^-8 of itself, half
+    // a step as any bf16 value; products of fp32 run at 1/16 of the rate); their sum
+    // is over the unrounded ones, so lse carries none of it.
     op_t pop[KL];
 #pragma unroll
     for (int ks = 0; ks < KL; ++ks) pop[ks] = cvt_op<bf16>(&p[ks * E]);
@@ -954,7 +957,7 @@ __global__ __launch_bounds__(kWave* kWinWaves* H, 2) void hyb_win_dq_ring_kernel
 #pragma unroll
       for (int e = 0; e < 16; ++e)
         ds[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale, -lse)) * (dp[e] - delta);
-      op_t sop[KL];
+      op_t sop[KL];  // (dS rounded to bf16 for its product, as the weights of the forward)
 #pragma unroll
       for (int ks = 0; ks < KL; ++ks) sop[ks] = cvt_op<bf16>(&ds[ks * E]);
 #pragma unroll
@@ -1138,7 +1141,7 @@ __global__ __launch_bounds__(kWave * 4 * H, 2) void hyb_win_dkv_ring_kernel(Wind
       }
       cq += H;
       while (cq >= nq) cq -= nq;
-      op_t pop[KL], sop[KL];
+      op_t pop[KL], sop[KL];  // (P and dS rounded to bf16 for their products, as in the forward)
 #pragma unroll
       for (int ks = 0; ks < KL; ++ks) {
         float p[E], ds[E];

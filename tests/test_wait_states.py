@@ -20,7 +20,7 @@ from paper_2608_06628_amd import binding as hb
 
 STATES = {"v_mfma_f32_32x32x16_bf16": 12, "v_mfma_f32_16x16x32_bf16": 8, "v_mfma_f32_32x32x2_f32": 18,
           "v_mfma_f32_16x16x4_f32": 10}
-OBJDUMP = shutil.which("llvm-objdump") or "/opt/rocm/llvm/bin/llvm-objdump"
+OBJDUMP = next((p for p in ("/opt/rocm/llvm/bin/llvm-objdump", shutil.which("llvm-objdump")) if p and os.path.exists(p)), None)
 REG = re.compile(r"\b([va])(?:(\d+)\b|\[(\d+):(\d+)\])")
 BRANCH = re.compile(r"<[^>]*\+0x([0-9a-f]+)>|<([^>+]*)>")
 
@@ -114,7 +114,7 @@ def shortest(code):
 
 
 def test_results_are_read_when_they_are_there(tmp_path):
-    if not os.path.exists(OBJDUMP):
+    if OBJDUMP is None:
         pytest.skip("no llvm-objdump")
     assert os.path.exists(hb.LIB_PATH), "the library is not built"
     early, products = {}, 0
