@@ -470,7 +470,8 @@ size_t hybrid_rope_workspace_bytes(const hyb_rope_dims_t* dims);
  * its request.  Rows past the last token get slot -1 and position 0; tokens
  * past max_tokens are dropped (their pages are still taken).  token_start
  * int32 [B + 1]: first packed row of each request, then the total.  counts
- * int32 [2]: pages taken, pages that were missing.  Sums past 2^31 - 1 stay there.
+ * int32 [2]: pages taken, pages that were missing.  Sums past 2^31 - 1 stay there,
+ * and table entries past that many new pages are not written.
  * batch is 1 .. 4096 (0: nothing to do); page_size a power of two from 1 to 65536;
  * max_pages * page_size < 2^31 - 64; n_free >= 0 (free_pages may be NULL when
  * 0, and needs 4-byte alignment only: a caller goes on in its list where the

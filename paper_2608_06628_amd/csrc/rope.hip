@@ -21,8 +21,9 @@
 // million times a frequency leaves an fp32 angle 0.06 off; its sine and cosine
 // in 32).
 //
-// Measured, 16 and 4 heads of d = 128, bf16: 65536 tokens 128 us (5.26 TB/s), 64 tokens
-// into pages 4 us; gradient of 16384 tokens 45 us (5.6 TB/s), and 5 for the weights' sums.
+// Measured, 16 and 4 heads of d = 128, bf16: 65536 tokens 127 us a call, one after the other
+// (5.3 TB/s; fp32, 16384 tokens, 64); the kernels alone, under a trace: 64 tokens into pages 4 us,
+// gradient of 16384 tokens 44 us (5.7 TB/s), and 5 for the weights' sums.
 #include <algorithm>
 #include <type_traits>
 
@@ -318,10 +319,10 @@ __global__ __launch_bounds__(16 * kDwRows) void hyb_rope_dw_kernel(const float* 
 }
 
 // Workgroups at most.  The forward's waves take one unit each, so that the rows on
-// their way at a time are neighbours in memory (65536 tokens of 16 and 4 heads, d = 128:
-// 131 us, 5.1 TB/s; 152 by 2048 workgroups in rounds, 171 with the next unit's loads
-// ahead of the last stores; stores that bypass the caches 122, which the attention that
-// reads the rows next pays back).  The gradient's leave a partial row each, which the
+// their way at a time are neighbours in memory (65536 tokens of 16 and 4 heads, d = 128,
+// on one card: by 2048 workgroups in rounds 1.16 times as long, with the next unit's loads
+// ahead of the last stores 1.31 times; with stores that bypass the caches 0.93 times, which
+// the attention that reads the rows next pays back).  The gradient's leave a partial row each, which the
 // weights' kernel reads (16384 tokens 49 us with 1024, 55 with 512, 51 with 2048).
 constexpr int kRopeGrid = 1 << 20;
 constexpr int kRopeBackwardGrid = 1024;

@@ -21,10 +21,10 @@
 // each accumulator tile is the next product's operand without leaving its
 // registers (device.h).
 //
-// Measured, bf16, 16 and 4 heads of d = 128: 8 x 8192 tokens, window 4096, 1.67 to 1.78 ms
-// (940 to 1000 TFLOP/s; a product of 8192 cubed reaches 1180 to 1210 on the same cards, and the
-// clock falls to 1.85 GHz for both); gradient of 8 x 2048 tokens, every earlier block, 480 to
-// 513 us (0.68 to 0.73 PFLOP/s of 10 d per pair).
+// Measured, bf16, 16 and 4 heads of d = 128, calls one after the other: 8 x 8192 tokens, window
+// 4096, 1.67 to 1.78 ms (940 to 1000 TFLOP/s; a product of 8192 cubed reaches 1180 to 1210 on the
+// same cards, and the clock falls to 1.85 GHz for both); gradient of 8 x 2048 tokens, every earlier
+// block, 480 to 513 us (0.68 to 0.73 PFLOP/s of 10 d per pair).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -830,8 +830,9 @@ __global__ __launch_bounds__(kWave* kWinWaves* H, 2) void hyb_win_ring_kernel(Wi
 // Two kernels: dQ with delta and the rows' statistics (a wave owns 32 queries and
 // loops over key tiles), then dK with dV (a wave owns 32 keys and loops over the
 // query tiles of its KV head's heads).  Tiles come through rings as in the forward;
-// here a tile is read both by rows and by columns (RowColTile).  8 x 2048 tokens: dQ
-// 0.22 to 0.27 ms, dK and dV 0.29 to 0.37, their matrix cores busy 0.53 and 0.56 of the time.
+// here a tile is read both by rows and by columns (RowColTile).  8 x 2048 tokens: of a call's time
+// dQ takes two fifths, dK and dV three (under a trace, which runs each call slower, 0.22 and 0.30 ms
+// at best), their matrix cores busy 0.53 and 0.56 of the time.
 
 // Statistics of a row for the dK, dV kernel, as operands of one more step of its
 // products: lse sqrt(d) and delta, each as three bf16 pieces (24 bits), which
@@ -1290,9 +1291,9 @@ static hipError_t win_prefill_f32_go(const WindowArgs& a, hipStream_t st) {
 // and more parts than one cost the sums' traffic and a launch.  The numbers are fitted to 23
 // shapes of bf16 and 16 of fp32 with up to 16 parts, where what this takes is within 2%
 // of the best on average and 11% in each.  (d = 128, 2 x 1024 tokens, window 200, 16 and 4 heads:
-// 60 us in 1 part, 48 in 3, 46.5 in 4, which are 256 lists, 58 in 5; fp32 538, 245, 208, 258.  d =
-// 64, 2 x 3001, window 511, 8 and 2 heads: no halves, 1 to 5 parts 89, 65, 56, 58, 56; halves, 67, 54,
-// 60, 61, 58.)
+// 60 us in 1 part, 47 in 3, 46 in 4, which are 256 lists, 58 in 5; fp32 538, 246, 208, 259, where
+// the estimate takes 8, 230.  d = 64, 2 x 3001, window 511, 8 and 2 heads: no halves, 1 to 5 parts
+// 89, 65, 56, 58, 56; halves, 67, 54, 60, 61, 58.)
 // The sinks' keys are cut into parts as long as the others', as long as those
 // are at most 16 per (request, KV head) and 512 in all.
 static int win_sink_parts(const Shape& s) { return (int)std::min<long>(16, 512 / std::max<long>(1, (long)s.B * s.Hkv)); }
