@@ -106,23 +106,3 @@ def norm_rope_gradient(x, w, g, pos, inv_freq, layout, eps, scale):
     rows = x.shape[0] * x.shape[1]
     dw_err = (64 + min(rows, 512)) * F32 * (mag * np.abs(xh)).sum((0, 1))
     return dx, (u * xh).sum((0, 1)), dx_err, dw_err
-
-
-def climb(shape, n):
-    """Score added to key j of n: in steps that pass what a reference of the
-    weights puts up with (2^8, a score of 5.55), early or late in the sequence,
-    down again, and by single keys that leave the others their share."""
-    j, top = np.arange(n), (n - 1) // 32
-    return {"grow": 6.5 * np.minimum(j // 32, 8), "fall": 6.5 * np.maximum(8 - j // 32, 0),
-            "late": 6.5 * np.maximum(j // 32 - (top - 8), 0),
-            "spike": np.where(j % 97 == 45, 5.8, 0.0) + np.where(j == n * 3 // 4, 11.0, 0.0)}[shape]
-
-
-def add_scores(q, k, extra):
-    """q [.., d] and k [n, .., d] such that key j's scaled scores rise by extra[j]."""
-    d = q.shape[-1]
-    up = torch.full((d,), d ** -0.25, dtype=torch.float64)
-    up[::3] *= -1.0
-    extra = torch.from_numpy(np.asarray(extra, dtype=np.float64)).view(-1, *[1] * (k.dim() - 1))
-    return ((q.double().cpu() + up).to(q.dtype).to(q.device),
-            (k.double().cpu() + extra * up).to(k.dtype).to(k.device))
