@@ -103,7 +103,8 @@ typedef enum {
   HYB_OP_BACKWARD_FULL = 5,
   HYB_OP_WINDOW_STEP = 6,
   HYB_OP_WINDOW_PREFILL = 7,
-  HYB_OP_WINDOW_BACKWARD = 8
+  HYB_OP_WINDOW_BACKWARD = 8,
+  HYB_OP_WINDOW_STEP_Q8 = 9
 } hyb_op_t;
 
 typedef struct {
@@ -484,10 +485,84 @@ int kv_pages_plan(int32_t batch, int32_t max_pages, int32_t page_size,
                   int32_t* slots, int32_t* positions, int32_t* token_start,
                   int32_t* counts, void* stream);
 
+/* A paged KV cache in 8 bits: half the bytes of a bf16 one, for the softmax layers
+ * that keep a cache beside the hybrid ones.  k_pages, v_pages: pools of codes
+ * [n_pages][page_size][Hkv][d], e4m3 (the OCP type without infinities); k_scales,
+ * v_scales: [n_pages][page_size / scale_block][Hkv] bytes, the scale 2^(byte - 127)
+ * of scale_block consecutive rows of a page at one KV head.  A cached value is its code
+ * times its scale, exactly in bf16 and fp32.  page_size is a power of two from 32 to
+ * 65536, scale_block one from 32 to page_size. */
+typedef struct {
+  int32_t tokens;      /* N >= 0, rows of k and v (0: nothing to do)         */
+  int32_t batch;       /* B >= 0, requests                                   */
+  int32_t n_kv_heads;  /* Hkv, 1 .. 65536                                    */
+  int32_t head_dim;    /* d: 64 or 128                                       */
+  int32_t dtype;       /* hyb_dtype_t of k and v                             */
+  int32_t max_pages;   /* entries of a request's page table row, >= 0        */
+  int32_t n_pages;     /* pages of the pools, >= 1 when max_pages > 0        */
+  int32_t page_size;   /* tokens per page                                    */
+  int32_t scale_block; /* tokens per scale                                   */
+  /* elements from a token's row to the next; 0: contiguous.  A multiple of 8,
+   * at least the row's length. */
+  int64_t k_stride, v_stride;
+} hyb_kv_q8_dims_t;
+
+/* Quantises new keys and values as it writes them into the cache.  Request b brings
+ * the packed rows token_start[b] .. token_start[b + 1] - 1 of k and v [N][Hkv][d] (as
+ * kv_pages_plan packs and counts them) as tokens first[b], first[b] + 1, .. of its
+ * cache, through its row of page_table [B][max_pages].  Device values are clamped:
+ * first [B] to [0, max_pages * page_size], token_start [B + 1] (not falling) to [0, N]
+ * with token_start[0] read as 0; tokens past the page table, and those whose page
+ * number lies outside [0, n_pages), are not written.
+ * Per scale block and head: with m the largest finite magnitude of the block's new
+ * entries, the scale is the least power of two 2^e with m <= 448 2^e, at least 2^-117;
+ * where the call's first token in the block is not the block's first row, the block goes
+ * on: it keeps at least its old scale, and where that grows the rows before, tokens
+ * below first[b], are rounded again to the new one (exactly but for codes that become
+ * subnormal).  Codes are rounded to nearest even; an entry that is not finite becomes
+ * NaN.  A block's rows behind the call's last token hold nothing after a call (their
+ * codes stay, their scale may not).  Requests of one call must not share a page that
+ * they write to.  The pools must not overlap each other or an input. */
+int kv_pages_q8_write(const hyb_kv_q8_dims_t* dims, const void* k,
+                      const void* v, void* k_pages, void* v_pages,
+                      uint8_t* k_scales, uint8_t* v_scales,
+                      const int32_t* page_table, const int32_t* first,
+                      const int32_t* token_start, void* stream);
+
+/* The reverse: the values of cached tokens first[b], first[b] + 1, .. of request b into
+ * the packed rows token_start[b] .. token_start[b + 1] - 1 of k and v, in dims->dtype.
+ * Device values are clamped as above; rows of k and v without a cached token (behind the
+ * last request's, past the page table, of a page number out of range) are left as they
+ * were.  k and v must not overlap each other or an input (their rows may be interleaved
+ * in one buffer). */
+int kv_pages_q8_read(const hyb_kv_q8_dims_t* dims, const void* k_pages,
+                     const void* v_pages, const uint8_t* k_scales,
+                     const uint8_t* v_scales, const int32_t* page_table,
+                     const int32_t* first, const int32_t* token_start, void* k,
+                     void* v, void* stream);
+
+/* softmax_window_step_paged over an 8-bit cache: q, k, v, out and the block are
+ * dims->dtype, the cached tokens e4m3 with their scales.  Arguments and meaning otherwise
+ * as there (a window of at least the prefix sees the whole cache), with any number of
+ * query heads per KV head up to 65536 heads in all; a page number outside [0, n_pages) is
+ * clamped into it.  bf16: the weights enter P V rounded to bf16, their sum takes them
+ * unrounded.  ws/ws_bytes: at least hybrid_workspace_bytes(dims,
+ * HYB_OP_WINDOW_STEP_Q8, min(max_pages * page_size, n_sinks + window + 64)) bytes.  out and
+ * the workspace must not overlap each other or an input. */
+int softmax_window_step_paged_q8(
+    const hyb_dims_t* dims, const void* q, const void* k, const void* v,
+    const void* k_pages, const void* v_pages, const uint8_t* k_scales,
+    const uint8_t* v_scales, int32_t n_pages, int32_t page_size,
+    int32_t scale_block, const int32_t* page_table, int32_t max_pages,
+    const int32_t* prefix_len, int32_t window, int32_t n_sinks,
+    const int32_t* block_len, void* out, void* ws, size_t ws_bytes,
+    void* stream);
+
 /* Workspace bytes the given op needs for these dims; `extent` is seq_len for
  * HYB_OP_PREFILL, HYB_OP_BACKWARD, HYB_OP_BACKWARD_FULL, HYB_OP_WINDOW_PREFILL
  * and HYB_OP_WINDOW_BACKWARD, max_prefix for HYB_OP_SOFTMAX_PREFIX, the cached
- * tokens a request sees at most for HYB_OP_WINDOW_STEP, ignored otherwise.
+ * tokens a request sees at most for HYB_OP_WINDOW_STEP and
+ * HYB_OP_WINDOW_STEP_Q8, ignored otherwise.
  * Returns 0 for invalid dims. */
 size_t hybrid_workspace_bytes(const hyb_dims_t* dims, int32_t op,
                               int32_t extent);

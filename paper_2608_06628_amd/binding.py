@@ -26,7 +26,7 @@ HYB_STEP_SPLIT, HYB_STEP_WHOLE, HYB_STEP_HALVES = 2, 4, 8
 _STEP_KERNEL = {None: 0, "auto": 0, "split": HYB_STEP_SPLIT, "whole": HYB_STEP_WHOLE,
                 "halves": HYB_STEP_HALVES}
 OP_STEP, OP_COMMIT, OP_PREFILL, OP_SOFTMAX_PREFIX, OP_BACKWARD, OP_BACKWARD_FULL = 0, 1, 2, 3, 4, 5
-OP_WINDOW_STEP, OP_WINDOW_PREFILL, OP_WINDOW_BACKWARD = 6, 7, 8
+OP_WINDOW_STEP, OP_WINDOW_PREFILL, OP_WINDOW_BACKWARD, OP_WINDOW_STEP_Q8 = 6, 7, 8, 9
 _ROPE_LAYOUT = {"half": 0, "interleaved": 1}
 STATUS = {0: "HYB_OK", 1: "HYB_ENULL", 2: "HYB_EINVAL", 3: "HYB_EALIGN",
           4: "HYB_EDTYPE", 5: "HYB_EUNSUPPORTED", 6: "HYB_EWORKSPACE",
@@ -37,7 +37,8 @@ EXPORTS = ("hybrid_attn_step", "hybrid_attn_step_commit", "hybrid_state_commit",
            "hybrid_attn_backward", "hybrid_attn_backward_full", "hybrid_workspace_bytes",
            "hybrid_last_error", "softmax_window_step_paged", "softmax_window_prefill",
            "softmax_window_backward", "hybrid_qk_norm_rope", "hybrid_qk_norm_rope_paged",
-           "hybrid_qk_norm_rope_backward", "hybrid_rope_workspace_bytes", "kv_pages_plan")
+           "hybrid_qk_norm_rope_backward", "hybrid_rope_workspace_bytes", "kv_pages_plan",
+           "kv_pages_q8_write", "kv_pages_q8_read", "softmax_window_step_paged_q8")
 NOALLOC_SCRATCH_BYTES = 64 << 20
 
 
@@ -59,6 +60,12 @@ class RopeDims(ctypes.Structure):
         "grad_dtype", "flags")] + [(n, ctypes.c_float) for n in ("eps", "rot_scale")] + [
         (n, ctypes.c_int64) for n in ("q_stride", "k_stride", "v_stride", "q_out_stride",
                                       "k_out_stride")]
+
+
+class KvQ8Dims(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "tokens", "batch", "n_kv_heads", "head_dim", "dtype", "max_pages", "n_pages", "page_size",
+        "scale_block")] + [(n, ctypes.c_int64) for n in ("k_stride", "v_stride")]
 
 
 _lib = None
@@ -97,6 +104,11 @@ def load():
     lib.hybrid_rope_workspace_bytes.argtypes = [R]
     lib.hybrid_rope_workspace_bytes.restype = sz
     lib.kv_pages_plan.argtypes = [i32] * 5 + [vp] * 9
+    Q = ctypes.POINTER(KvQ8Dims)
+    lib.kv_pages_q8_write.argtypes = [Q] + [vp] * 10
+    lib.kv_pages_q8_read.argtypes = [Q] + [vp] * 10
+    lib.softmax_window_step_paged_q8.argtypes = [P] + [vp] * 7 + [i32] * 3 + [vp, i32, vp, i32, i32,
+                                                                              vp, vp, vp, sz, vp]
     lib.hybrid_workspace_bytes.argtypes = [P, i32, i32]
     lib.hybrid_workspace_bytes.restype = sz
     lib.hybrid_last_error.argtypes = []
@@ -106,7 +118,8 @@ def load():
               "hybrid_state_prefill_noalloc", "softmax_prefix_step", "softmax_prefix_step_paged",
               "softmax_window_step_paged", "softmax_window_prefill", "softmax_window_backward",
               "hybrid_qk_norm_rope", "hybrid_qk_norm_rope_paged", "hybrid_qk_norm_rope_backward",
-              "kv_pages_plan"):
+              "kv_pages_plan", "kv_pages_q8_write", "kv_pages_q8_read",
+              "softmax_window_step_paged_q8"):
         getattr(lib, n).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -720,3 +733,101 @@ def softmax_window_backward(dev, q, k, v, out, lse, dout, block, window, n_sinks
         _dptr(dev, dk, "dk", odt, kv), _dptr(dev, dv, "dv", odt, kv),
         *_ws(dev, ws), _raw_stream(dev)))
     return dq, dk, dv
+
+
+_E4M3, _E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+
+
+def _q8_pools(dev, k_pages, v_pages, k_scales, v_scales, Hkv, d):
+    """The addresses of an 8-bit cache's pools, its pages, their size and the scale block."""
+    pool = k_pages.shape
+    if len(pool) != 4 or pool[2] != Hkv or pool[3] != d:
+        raise ValueError(f"k_pages must have shape [pages][page_size][{Hkv}][{d}], got {tuple(pool)}")
+    n_pages, page = pool[0], pool[1]
+    blocks = k_scales.shape[1] if k_scales.dim() == 3 else 0
+    if blocks < 1 or page % blocks:
+        raise ValueError(f"k_scales must have shape [{n_pages}][page_size / scale_block][{Hkv}], got "
+                         f"{tuple(k_scales.shape)} for pages of {page}")
+    scale = (n_pages, blocks, Hkv)
+    return (_dptr(dev, k_pages, "k_pages", _E4M3), _dptr(dev, v_pages, "v_pages", _E4M3, pool),
+            _dptr(dev, k_scales, "k_scales", _E8M0, scale),
+            _dptr(dev, v_scales, "v_scales", _E8M0, scale)), n_pages, page, page // blocks
+
+
+_q8_dims = functools.lru_cache(maxsize=256)(KvQ8Dims)
+
+
+def _q8_args(dev, k, v, k_pages, v_pages, k_scales, v_scales, page_table, first, token_start):
+    N, Hkv, d = shape = k.shape
+    B, max_pages = page_table.shape
+    i32 = torch.int32
+    pools, n_pages, page, sb = _q8_pools(dev, k_pages, v_pages, k_scales, v_scales, Hkv, d)
+    pk, sk = _rows(dev, k, "k", k.dtype, shape)
+    pv, sv = _rows(dev, v, "v", k.dtype, shape)
+    dims = _q8_dims(min(N, _I32), B, Hkv, d, _dt(k), min(max_pages, _I32), n_pages, page, sb, sk, sv)
+    return dims, pk, pv, pools, (_dptr(dev, page_table, "page_table", i32), _dptr(dev, first, "first", i32, (B,)),
+                                 _dptr(dev, token_start, "token_start", i32, (B + 1,)))
+
+
+@_placed
+def kv_pages_q8_write(dev, k, v, k_pages, v_pages, k_scales, v_scales, page_table, first, token_start):
+    """Quantises k, v [N][Hkv][d] (views of one packed projection or not) into an
+    8-bit cache: k_pages, v_pages [n_pages][page_size][Hkv][d] float8_e4m3fn, k_scales, v_scales
+    [n_pages][page_size / scale_block][Hkv] float8_e8m0fnu.  Rows token_start[b] ..
+    token_start[b + 1] - 1 (token_start [B + 1] as kv_pages_plan gives it) become tokens
+    first[b] .. of request b, whose pages page_table [B][max_pages] names; all int32."""
+    dims, pk, pv, pools, where = _q8_args(dev, k, v, k_pages, v_pages, k_scales, v_scales, page_table, first,
+                                          token_start)
+    _check(load().kv_pages_q8_write(dims, pk, pv, *pools, *where, _raw_stream(dev)))
+
+
+@_placed
+def kv_pages_q8_read(dev, k_pages, v_pages, k_scales, v_scales, page_table, first, token_start, tokens=None,
+                     k=None, v=None, dtype=torch.bfloat16):
+    """The values of cached tokens first[b] .. of every request as rows token_start[b] ..
+    token_start[b + 1] - 1 of k, v [tokens][Hkv][d]; rows without a token are left as they
+    were (zero where k or v is made here, in dtype).  Returns (k, v)."""
+    given = k if k is not None else v
+    if given is None:
+        if tokens is None:
+            raise TypeError("kv_pages_q8_read needs tokens, the number of rows, or k and v")
+        shape, act = (tokens, *k_pages.shape[2:]), dtype
+    else:
+        shape, act = given.shape, given.dtype
+    if k is None:
+        k = torch.zeros(shape, dtype=act, device=k_pages.device)
+    if v is None:
+        v = torch.zeros(shape, dtype=act, device=k_pages.device)
+    dims, pk, pv, pools, where = _q8_args(dev, k, v, k_pages, v_pages, k_scales, v_scales, page_table, first,
+                                          token_start)
+    _check(load().kv_pages_q8_read(dims, *pools, *where, pk, pv, _raw_stream(dev)))
+    return k, v
+
+
+@_placed
+def softmax_window_step_paged_q8(dev, q, k, v, k_pages, v_pages, k_scales, v_scales, page_table, prefix_len,
+                                 window, n_sinks=0, block_len=None, out=None, ws=None, out_f32=False):
+    """softmax_window_step_paged over an 8-bit cache (kv_pages_q8_write); a window of the
+    whole prefix or more sees all of it."""
+    lib = load()
+    B, L, Hq, d = q.shape
+    act, i32 = q.dtype, torch.int32
+    odt = _odt(act, out, out_f32)
+    dims, kv = _window_dims(q, k, L, odt)
+    if out is None:
+        new = torch.empty if block_len is None else torch.zeros
+        out = new(q.shape, dtype=odt, device=q.device)
+    pools, n_pages, page, sb = _q8_pools(dev, k_pages, v_pages, k_scales, v_scales, kv[2], d)
+    max_pages = min(page_table.shape[1], _I32)
+    window, n_sinks = _reach(window), _reach(n_sinks)
+    if ws is None:
+        need = lib.hybrid_workspace_bytes(dims, OP_WINDOW_STEP_Q8,
+                                          min(max_pages * page, window + n_sinks + 64, _I32))
+        ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    _check(lib.softmax_window_step_paged_q8(
+        dims, _dptr(dev, q, "q", act), _dptr(dev, k, "k", act, kv), _dptr(dev, v, "v", act, kv), *pools,
+        n_pages, page, sb, _dptr(dev, page_table, "page_table", i32, (B, max_pages)), max_pages,
+        _dptr(dev, prefix_len, "prefix_len", i32, (B,)), window, n_sinks,
+        _dptr(dev, block_len, "block_len", i32, (B,)), _dptr(dev, out, "out", odt, q.shape),
+        *_ws(dev, ws), _raw_stream(dev)))
+    return out

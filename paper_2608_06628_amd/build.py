@@ -18,7 +18,7 @@ OUT = os.path.join(PKG, "libhybattn.so")
 BUILD = os.path.join(ROOT, "_build")
 SOURCES = ["api.cpp", "step.hip", "commit.hip", "prefill.hip", "softmax_prefix.hip", "backward.hip",
            "scratch.hip", "step_small.hip", "rope.hip", "pages.hip",
-           "window.hip"]
+           "window.hip", "kv_q8.hip", "softmax_q8.hip"]
 ARCH = "gfx950"
 FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC",

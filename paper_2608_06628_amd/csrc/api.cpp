@@ -11,6 +11,7 @@
 
 #include "../../include/hybrid_attn.h"
 #include "launch.h"
+#include "launch_cache.h"
 
 namespace {
 
@@ -833,6 +834,151 @@ int kv_pages_plan(int32_t batch, int32_t max_pages, int32_t page_size,
 
 namespace {
 
+int check_page(int32_t page_size, int32_t scale_block, int32_t max_pages, int32_t n_pages, int* page_shift, int* sb_shift) {
+  if (max_pages < 0) return fail(HYB_EINVAL, "max_pages %d < 0", max_pages);
+  if (page_size < 32 || page_size > (1 << 16) || (page_size & (page_size - 1)))
+    return fail(HYB_EUNSUPPORTED, "page_size %d not supported (a power of two, 32 .. 65536)", page_size);
+  if (scale_block < 32 || scale_block > page_size || (scale_block & (scale_block - 1)))
+    return fail(HYB_EUNSUPPORTED, "scale_block %d not supported (a power of two, 32 .. page_size)", scale_block);
+  if ((long long)max_pages * page_size > 0x7fffffffLL - 64)
+    return fail(HYB_EINVAL, "max_pages * page_size exceeds the index range");
+  if (max_pages > 0 && n_pages < 1) return fail(HYB_EINVAL, "n_pages %d < 1", n_pages);
+  for (*page_shift = 0; (1 << *page_shift) < page_size;) ++*page_shift;
+  for (*sb_shift = 0; (1 << *sb_shift) < scale_block;) ++*sb_shift;
+  return HYB_OK;
+}
+
+// Validation and dispatch of the 8-bit cache's write, and (read) of its reverse.
+int kv_q8_impl(const hyb_kv_q8_dims_t* d, const void* k, const void* v, const void* k_pages, const void* v_pages,
+               const uint8_t* k_scales, const uint8_t* v_scales, const int32_t* page_table, const int32_t* first,
+               const int32_t* token_start, bool read, void* stream) {
+  const char* name = read ? "kv_pages_q8_read" : "kv_pages_q8_write";
+  if (!d) return fail(HYB_ENULL, "dims is NULL");
+  if (d->dtype != HYB_F32 && d->dtype != HYB_BF16)
+    return fail(HYB_EDTYPE, "dtype %d is neither HYB_F32 nor HYB_BF16", d->dtype);
+  if (d->tokens < 0 || d->batch < 0) return fail(HYB_EINVAL, "tokens %d and batch %d must be >= 0", d->tokens, d->batch);
+  if (d->n_kv_heads < 1 || d->n_kv_heads > 65536)
+    return fail(HYB_EINVAL, "n_kv_heads %d is not in 1 .. 65536", d->n_kv_heads);
+  if (d->head_dim != 64 && d->head_dim != 128)
+    return fail(HYB_EUNSUPPORTED, "head_dim %d not supported (64 or 128)", d->head_dim);
+  hyb::KvQ8Args a{};
+  TRY(check_page(d->page_size, d->scale_block, d->max_pages, d->n_pages, &a.page_shift, &a.sb_shift));
+  const long n = (long)d->n_kv_heads * d->head_dim;
+  for (const int64_t s : {d->k_stride, d->v_stride}) {
+    if (s != 0 && (s < n || s > (1L << 31)))
+      return fail(HYB_EINVAL, "a row stride of %ld is shorter than the row, or longer than 2^31", (long)s);
+    if (s % 8) return fail(HYB_EALIGN, "a row stride of %ld is not a multiple of 8 elements", (long)s);
+  }
+  a.k_stride = d->k_stride ? d->k_stride : n;
+  a.v_stride = d->v_stride ? d->v_stride : n;
+  a.N = d->tokens, a.B = d->batch, a.Hkv = d->n_kv_heads, a.D = d->head_dim, a.dtype = d->dtype;
+  a.max_pages = d->max_pages, a.n_pages = d->n_pages;
+  if (hyb::kv_q8_threads(a) > 0xffffffffL) return fail(HYB_EINVAL, "tokens * heads exceeds the grid limit");
+  if (a.N == 0 || a.B == 0 || a.max_pages == 0) return ok();
+  TRY(check_ptr(k, "k"));
+  TRY(check_ptr(v, "v"));
+  TRY(check_ptr(k_pages, "k_pages"));
+  TRY(check_ptr(v_pages, "v_pages"));
+  TRY(check_ptr(k_scales, "k_scales"));
+  TRY(check_ptr(v_scales, "v_scales"));
+  TRY(check_ptr(page_table, "page_table"));
+  TRY(check_ptr(first, "first"));
+  TRY(check_ptr(token_start, "token_start"));
+  const size_t es = elem_bytes(a.dtype), rows = (size_t)a.n_pages << a.page_shift;
+  const size_t nc = rows * n, ns = (rows >> a.sb_shift) * a.Hkv;
+  const Rows tok[2] = {{k, n * es, a.k_stride * es}, {v, n * es, a.v_stride * es}};
+  const Buf pools[4] = {{k_pages, nc}, {v_pages, nc}, {k_scales, ns}, {v_scales, ns}};
+  const Buf small[3] = {{page_table, (size_t)a.B * a.max_pages * 4}, {first, (size_t)a.B * 4},
+                        {token_start, ((size_t)a.B + 1) * 4}};
+  if (read) {
+    TRY(check_rows(tok, 2, nullptr, 0, a.N));
+    TRY(check_buffers(pools, 4, false, tok, 2, a.N));
+    TRY(check_buffers(small, 3, false, tok, 2, a.N));
+  } else {
+    TRY(check_buffers(pools, 4, true, tok, 2, a.N));
+    TRY(check_overlaps(pools, 4, small, 3));
+  }
+  a.k = const_cast<void*>(k), a.v = const_cast<void*>(v);  // (read by the write)
+  a.page_table = page_table, a.first = first, a.token_start = token_start;
+  a.k_pages = (uint8_t*)const_cast<void*>(k_pages), a.v_pages = (uint8_t*)const_cast<void*>(v_pages);
+  a.k_scales = const_cast<uint8_t*>(k_scales), a.v_scales = const_cast<uint8_t*>(v_scales);
+  (void)hipGetLastError();
+  return launched(read ? hyb::launch_kv_q8_read(a, (hipStream_t)stream) : hyb::launch_kv_q8_write(a, (hipStream_t)stream),
+                  name);
+}
+
+}  // namespace
+
+extern "C" {
+
+int kv_pages_q8_write(const hyb_kv_q8_dims_t* dims, const void* k, const void* v, void* k_pages, void* v_pages,
+                      uint8_t* k_scales, uint8_t* v_scales, const int32_t* page_table, const int32_t* first,
+                      const int32_t* token_start, void* stream) {
+  return kv_q8_impl(dims, k, v, k_pages, v_pages, k_scales, v_scales, page_table, first, token_start, false, stream);
+}
+
+int kv_pages_q8_read(const hyb_kv_q8_dims_t* dims, const void* k_pages, const void* v_pages, const uint8_t* k_scales,
+                     const uint8_t* v_scales, const int32_t* page_table, const int32_t* first,
+                     const int32_t* token_start, void* k, void* v, void* stream) {
+  return kv_q8_impl(dims, k, v, k_pages, v_pages, k_scales, v_scales, page_table, first, token_start, true, stream);
+}
+
+int softmax_window_step_paged_q8(const hyb_dims_t* dims, const void* q, const void* k, const void* v,
+                                 const void* k_pages, const void* v_pages, const uint8_t* k_scales,
+                                 const uint8_t* v_scales, int32_t n_pages, int32_t page_size, int32_t scale_block,
+                                 const int32_t* page_table, int32_t max_pages, const int32_t* prefix_len,
+                                 int32_t window, int32_t n_sinks, const int32_t* block_len, void* out, void* ws,
+                                 size_t ws_bytes, void* stream) {
+  hyb::Shape s;
+  TRY(check_dims(dims, false, &s));
+  TRY(no_step_flags(dims));
+  if (window < 0 || n_sinks < 0)
+    return fail(HYB_EINVAL, "window %d and n_sinks %d must be >= 0", window, n_sinks);
+  if (s.Hq > 65536) return fail(HYB_EUNSUPPORTED, "n_q_heads %d not supported (at most 65536)", s.Hq);
+  int page_shift, sb_shift;
+  TRY(check_page(page_size, scale_block, max_pages, n_pages, &page_shift, &sb_shift));
+  if (s.B == 0) return ok();
+  const int max_prefix = max_pages * page_size;
+  TRY(check_ptr(q, "q"));
+  TRY(check_ptr(k, "k"));
+  TRY(check_ptr(v, "v"));
+  TRY(check_ptr(out, "out"));
+  TRY(check_ptr(prefix_len, "prefix_len"));
+  TRY(check_ptr(k_pages, "k_pages", max_prefix > 0));
+  TRY(check_ptr(v_pages, "v_pages", max_prefix > 0));
+  TRY(check_ptr(k_scales, "k_scales", max_prefix > 0));
+  TRY(check_ptr(v_scales, "v_scales", max_prefix > 0));
+  TRY(check_ptr(page_table, "page_table", max_prefix > 0));
+  TRY(check_ptr(block_len, "block_len", false));
+  // cached tokens that a query sees, at most (a window's ends share tiles with hidden tokens)
+  const int max_seen = (int)std::min<long long>(max_prefix, (long long)window + n_sinks + 64);
+  const size_t need = hybrid_workspace_bytes(dims, HYB_OP_WINDOW_STEP_Q8, max_seen);
+  if (need > 0 && (!ws || ws_bytes < need))
+    return fail(HYB_EWORKSPACE, "softmax_window_step_paged_q8 needs %zu workspace bytes, got %zu", need,
+                ws ? ws_bytes : (size_t)0);
+  TRY(check_ptr(ws, "ws", false));
+  const hyb::SoftmaxQ8Args a{{s, q, k, v, k_pages, v_pages, prefix_len, max_prefix, out, ws,
+                              hyb::softmax_q8_splits(s, max_seen + 32), page_table, page_shift, max_pages, n_pages,
+                              max_seen + 32, window, n_sinks, block_len},
+                             k_scales, v_scales, sb_shift};
+  if (hyb::softmax_q8_threads(a) > 0xffffffffL)
+    return fail(HYB_EINVAL, "batch * heads * block exceeds the grid limit");
+  const size_t es = elem_bytes(s.dtype), nq = (size_t)s.B * s.L * s.Hq * s.D, nkv = (size_t)s.B * s.L * s.Hkv * s.D;
+  const size_t rows = max_prefix > 0 ? (size_t)n_pages << page_shift : 0;
+  const size_t nc = rows * s.Hkv * s.D, ns = (rows >> sb_shift) * s.Hkv;
+  const Buf written[] = {{out, nq * out_bytes(s)}, {ws, need}};
+  const Buf read_only[] = {{q, nq * es}, {k, nkv * es}, {v, nkv * es}, {k_pages, nc}, {v_pages, nc}, {k_scales, ns},
+                           {v_scales, ns}, {page_table, (size_t)s.B * max_pages * 4}, {prefix_len, (size_t)s.B * 4},
+                           {block_len, (size_t)s.B * 4}};
+  TRY(check_overlaps(written, 2, read_only, 10));
+  (void)hipGetLastError();
+  return launched(hyb::launch_softmax_q8(a, (hipStream_t)stream), "softmax_window_step_paged_q8");
+}
+
+}  // extern "C"
+
+namespace {
+
 // Validation and dispatch of the backward; dq, dk, dv all null (the Stage-1
 // gradient only) or all set (the input gradients as well).
 int backward_impl(const hyb_dims_t* dims, int32_t seq_len, const void* q,
@@ -955,6 +1101,9 @@ size_t hybrid_workspace_bytes(const hyb_dims_t* dims, int32_t op,
       return hyb::prefill_ws_bytes(s, extent);
     case HYB_OP_WINDOW_STEP:
       return hyb::softmax_prefix_ws_bytes(s, hyb::softmax_window_splits(s, extent));
+    case HYB_OP_WINDOW_STEP_Q8:
+      if (extent > 0x7fffffff - 64) return 0;
+      return hyb::softmax_prefix_ws_bytes(s, hyb::softmax_q8_splits(s, extent + 32));
     case HYB_OP_SOFTMAX_PREFIX:
       return hyb::softmax_prefix_ws_bytes(
           s, hyb::softmax_prefix_splits(s, extent));

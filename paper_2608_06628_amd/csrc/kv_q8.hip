@@ -1,0 +1,242 @@
+// kv_q8.hip -- a paged KV cache in 8 bits: packed rows of new keys and values are
+// quantised as they are written into its pages, and rows are read back.
+//
+// A scale block is scale_block consecutive rows of a page at one KV head.  For the
+// block's new entries x, with m the largest finite |x|:
+//   e    = the least whole number with m <= 448 2^e (448: the largest e4m3), >= -117
+//   code = e4m3(x 2^-e), rounded to nearest even;  value = code 2^e
+// Where the block goes on (its first rows hold earlier tokens), e is at least what it
+// was, and where it grows the earlier codes c become e4m3(c 2^(old - e)).  A power of
+// two as the scale keeps that exact but for codes that fall below 2^-6, costs e4m3 no
+// precision (its step is relative) and makes every value exact in bf16.
+//
+// Bound: memory; each row is read once and its codes written once.  A job is a scale
+// block's new rows at one head, of K or V: one wave holds 64 rows in registers between
+// the maximum and the codes (blocks of more rows take a wave per 64, up to four, and
+// past 256 rows a second look at memory).  Jobs are numbered so that request b's start
+// at start_b / block + 2 b, which leaves every request room for the blocks it touches
+// (its rows need not begin with a block) and needs no sums: a job finds its request by
+// one look at the starts of 64 requests (two of 4096).
+#include <algorithm>
+
+#include "fp8.h"
+#include "launch_cache.h"
+
+namespace hyb {
+
+constexpr int kQ8Rows = 64;   // rows that a wave holds
+constexpr int kQ8Waves = 4;   // of a workgroup
+
+// First row of request b (clamped to the rows there are; request 0 starts at row 0).
+__device__ inline int q8_start(const KvQ8Args& a, int b) { return b == 0 ? 0 : min(max(a.token_start[b], 0), a.N); }
+__host__ __device__ inline long q8_first_job(int start, int b, int shift) { return (long)(start >> shift) + 2L * b; }
+
+// The rows lo .. lo + n - 1 (of k and v) that job `x` of blocks of 2^shift tokens
+// covers, and where they are in the pools.
+struct Q8Rows {
+  int n = 0;    // none: nothing to do
+  int src;      // first row of k and v
+  int at;       // its place in the block
+  size_t dst;   // row of the pools where the block starts
+  __device__ inline Q8Rows(const KvQ8Args& a, long x, int shift, int lane) {
+    int lo = 0, hi = a.B;  // the last request in lo .. hi - 1 that starts by job x
+    while (hi - lo > 1) {
+      const int step = (hi - lo + kWave - 1) / kWave, b = lo + lane * step;
+      const bool by = b < hi && q8_first_job(q8_start(a, b), b, shift) <= x;
+      lo += step * max(0, __builtin_popcountll(__ballot(by)) - 1);
+      hi = min(hi, lo + step);
+    }
+    const int s = q8_start(a, lo), e = q8_start(a, lo + 1), cap = a.max_pages << a.page_shift;
+    const long p0 = min(max(a.first[lo], 0), cap), p1 = min(p0 + max(e - s, 0), (long)cap);
+    const long j0 = ((p0 >> shift) + x - q8_first_job(s, lo, shift)) << shift;
+    const long from = max(p0, j0), to = min(p1, j0 + (1L << shift));
+    if (from >= to) return;
+    const int page = a.page_table[(size_t)lo * a.max_pages + (j0 >> a.page_shift)];
+    if (page < 0 || page >= a.n_pages) return;
+    n = (int)(to - from);
+    src = s + (int)(from - p0);
+    at = (int)(from - j0);
+    dst = ((size_t)page << a.page_shift) + (j0 & ((1L << a.page_shift) - 1));
+  }
+};
+
+// Eight entries of a row.
+template <typename T>
+struct Q8Piece;
+template <>
+struct Q8Piece<bf16> {
+  bf16x8 x;
+  __device__ inline void load(const bf16* p) { x = *reinterpret_cast<const bf16x8*>(p); }
+  __device__ inline float operator[](int e) const { return (float)x[e]; }
+};
+template <>
+struct Q8Piece<float> {
+  f32x4 a, b;
+  __device__ inline void load(const float* p) {
+    a = *reinterpret_cast<const f32x4*>(p);
+    b = *reinterpret_cast<const f32x4*>(p + 4);
+  }
+  __device__ inline float operator[](int e) const { return e < 4 ? a[e] : b[e - 4]; }
+};
+
+// Largest of x over the wave, in every lane.
+__device__ inline int q8_wave_max(int x) {
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x128, 0xf, 0xf, false));  // row_ror:8
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x124, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x122, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x121, 0xf, 0xf, false));
+  auto f = [](int v) { return __builtin_bit_cast(float, v); };
+  x = max(x, __builtin_bit_cast(int, xor16(f(x))));
+  return max(x, __builtin_bit_cast(int, xor32(f(x))));
+}
+
+// W waves share a job (1 or all of a workgroup's).
+template <typename T, int D, int W>
+__global__ __launch_bounds__(kWave* kQ8Waves) void hyb_kv_q8_write_kernel(KvQ8Args a, long jobs) {
+  constexpr int LPR = D / 8;           // lanes per row
+  constexpr int RPI = kWave / LPR;     // rows per load
+  constexpr int NL = kQ8Rows / RPI;    // loads that a wave holds
+  __shared__ int most[kQ8Waves];
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int w = W == 1 ? 0 : wave;
+  const long job = W == 1 ? (long)blockIdx.x * kQ8Waves + wave : (long)blockIdx.x;
+  if (job >= jobs) return;  // (one wave of its own, or the whole workgroup)
+  const int g = (int)(job % a.Hkv), kv = (int)(job / a.Hkv & 1);
+  const Q8Rows r(a, job / a.Hkv >> 1, a.sb_shift, lane);
+  if (r.n == 0) return;
+  const long stride = kv ? a.v_stride : a.k_stride;
+  const T* src = (const T*)(kv ? a.v : a.k) + r.src * stride + (long)g * D + lane % LPR * 8;
+  uint8_t* const pool = kv ? a.v_pages : a.k_pages;
+  uint8_t* const scale = (kv ? a.v_scales : a.k_scales) + (r.dst >> a.sb_shift) * a.Hkv + g;
+  const int old = r.at > 0 ? min((int)*scale, 254) : 0;
+  Q8Piece<T> x[NL];
+  int m = 0;
+  // This wave's rows, 64 at a time: w, w + W, ..; those past the last are the last again.
+  auto load = [&](int c0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < NL; ++u)
+      if (c0 + u * RPI < r.n) x[u].load(src + min(c0 + u * RPI + lane / LPR, r.n - 1) * stride);
+  };
+  int last = -1;
+  for (int c0 = w * kQ8Rows; c0 < r.n; c0 += W * kQ8Rows) {
+    load(c0);
+    last = c0;
+#pragma unroll
+    for (int u = 0; u < NL; ++u)
+      if (c0 + u * RPI < r.n) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int bits = __builtin_bit_cast(int, x[u][e]) & 0x7fffffff;
+          m = max(m, bits < 0x7f800000 ? bits : 0);
+        }
+      }
+  }
+  m = q8_wave_max(m);
+  if constexpr (W > 1) {
+    if (lane == 0) most[wave] = m;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < W; ++i) m = max(m, most[i]);
+  }
+  const int byte = max(scale_byte(__builtin_amdgcn_readfirstlane(m)), old);
+  if (w == 0 && lane == 0) *scale = (uint8_t)byte;
+  if (old != 0 && old < byte) {  // the block grows: its earlier rows (16 codes per lane)
+    constexpr int LPC = D / 16;
+    const float f = scale_of(max(old - byte + 127, 0));
+    for (int i = (w * kWave + lane) / LPC; i < r.at; i += W * kWave / LPC) {
+      uint4* const p = reinterpret_cast<uint4*>(pool + ((r.dst + i) * a.Hkv + g) * D + lane % LPC * 16);
+      const uint4 c = *p;
+      auto fewer = [f](uint32_t c4) {
+        const f32x4 y = fp8_f32(c4, 1.0f);
+        return fp8_codes(y[0], y[1], y[2], y[3], f);
+      };
+      *p = uint4{fewer(c.x), fewer(c.y), fewer(c.z), fewer(c.w)};
+    }
+  }
+  const float f = scale_of(254 - byte);
+  for (int c0 = w * kQ8Rows; c0 < r.n; c0 += W * kQ8Rows) {
+    if (c0 != last || c0 != w * kQ8Rows) load(c0);  // (held where the wave has no more)
+#pragma unroll
+    for (int u = 0; u < NL; ++u) {
+      const int i = c0 + u * RPI + lane / LPR;
+      if (c0 + u * RPI < r.n && i < r.n) {
+        const uint2 c = {fp8_codes(x[u][0], x[u][1], x[u][2], x[u][3], f),
+                         fp8_codes(x[u][4], x[u][5], x[u][6], x[u][7], f)};
+        *reinterpret_cast<uint2*>(pool + ((r.dst + r.at + i) * a.Hkv + g) * D + lane % LPR * 8) = c;
+      }
+    }
+  }
+}
+
+// Reading: a job is at most 64 rows of a scale block at one head, of K or V.
+template <typename T, int D>
+__global__ __launch_bounds__(kWave* kQ8Waves) void hyb_kv_q8_read_kernel(KvQ8Args a, long jobs, int shift) {
+  constexpr int LPR = D / 8, RPI = kWave / LPR, NL = kQ8Rows / RPI;
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const long job = (long)blockIdx.x * kQ8Waves + wave;
+  if (job >= jobs) return;
+  const int g = (int)(job % a.Hkv), kv = (int)(job / a.Hkv & 1);
+  const Q8Rows r(a, job / a.Hkv >> 1, shift, lane);
+  if (r.n == 0) return;
+  const long stride = kv ? a.v_stride : a.k_stride;
+  T* dst = (T*)(kv ? a.v : a.k) + r.src * stride + (long)g * D + lane % LPR * 8;
+  const uint8_t* pool = (kv ? a.v_pages : a.k_pages) + ((r.dst + r.at) * a.Hkv + g) * D + lane % LPR * 8;
+  const float f = scale_of((kv ? a.v_scales : a.k_scales)[(r.dst >> a.sb_shift) * a.Hkv + g]);
+  uint2 c[NL];
+#pragma unroll
+  for (int u = 0; u < NL; ++u)
+    if (u * RPI < r.n)
+      c[u] = *reinterpret_cast<const uint2*>(pool + (size_t)min(u * RPI + lane / LPR, r.n - 1) * a.Hkv * D);
+#pragma unroll
+  for (int u = 0; u < NL; ++u) {
+    const int i = u * RPI + lane / LPR;
+    if (u * RPI < r.n && i < r.n) {
+      if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<bf16x8*>(dst + i * stride) = fp8_bf16(c[u].x, c[u].y, f);
+      } else {
+        *reinterpret_cast<f32x4*>(dst + i * stride) = fp8_f32(c[u].x, f);
+        *reinterpret_cast<f32x4*>(dst + i * stride + 4) = fp8_f32(c[u].y, f);
+      }
+    }
+  }
+}
+
+// Jobs for blocks of 2^shift tokens.
+static long q8_jobs(const KvQ8Args& a, int shift) { return q8_first_job(a.N, a.B, shift) * 2 * a.Hkv; }
+static int q8_read_shift(const KvQ8Args& a) { return std::min(a.sb_shift, 6); }
+
+double kv_q8_threads(const KvQ8Args& a) {
+  return kWave * (kQ8Waves + std::max((double)q8_jobs(a, q8_read_shift(a)),
+                                      a.sb_shift > 6 ? (double)q8_jobs(a, a.sb_shift) * kQ8Waves : 0.0));
+}
+
+template <typename T, int D>
+static hipError_t q8_write_go(const KvQ8Args& a, hipStream_t st) {
+  const long jobs = q8_jobs(a, a.sb_shift);
+  const dim3 block(kWave * kQ8Waves);
+  if (a.sb_shift <= 6)
+    hipLaunchKernelGGL((hyb_kv_q8_write_kernel<T, D, 1>), dim3((unsigned)((jobs + kQ8Waves - 1) / kQ8Waves)), block, 0,
+                       st, a, jobs);
+  else
+    hipLaunchKernelGGL((hyb_kv_q8_write_kernel<T, D, kQ8Waves>), dim3((unsigned)jobs), block, 0, st, a, jobs);
+  return hipGetLastError();
+}
+template <typename T, int D>
+static hipError_t q8_read_go(const KvQ8Args& a, hipStream_t st) {
+  const int shift = q8_read_shift(a);
+  const long jobs = q8_jobs(a, shift);
+  hipLaunchKernelGGL((hyb_kv_q8_read_kernel<T, D>), dim3((unsigned)((jobs + kQ8Waves - 1) / kQ8Waves)),
+                     dim3(kWave * kQ8Waves), 0, st, a, jobs, shift);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv_q8_write(const KvQ8Args& a, hipStream_t st) {
+  if (a.dtype == 1) return a.D == 64 ? q8_write_go<bf16, 64>(a, st) : q8_write_go<bf16, 128>(a, st);
+  return a.D == 64 ? q8_write_go<float, 64>(a, st) : q8_write_go<float, 128>(a, st);
+}
+hipError_t launch_kv_q8_read(const KvQ8Args& a, hipStream_t st) {
+  if (a.dtype == 1) return a.D == 64 ? q8_read_go<bf16, 64>(a, st) : q8_read_go<bf16, 128>(a, st);
+  return a.D == 64 ? q8_read_go<float, 64>(a, st) : q8_read_go<float, 128>(a, st);
+}
+
+}  // namespace hyb

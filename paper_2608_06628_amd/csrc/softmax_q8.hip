@@ -1,0 +1,418 @@
+// softmax_q8.hip -- softmax attention of the active block over a paged KV cache in 8
+// bits (e4m3 codes, a power-of-two scale per block of tokens and KV head) and the block
+// itself, over the whole prefix or its window and first tokens.
+//
+//   out_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = exp(q_i k_j / sqrt(d)),
+//   k_j = 2^ek c_j, v_j = 2^ev c'_j for the codes c, c' of cached tokens,
+//   over the cached tokens seen and the block's (unquantised) own
+//
+// The keys are cut into ranges and the ranges' results merged as over an unquantised
+// cache (softmax_prefix.h); a tile is 32 cached tokens, which share a page and a scale,
+// and the block is the last tile.
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "fp8.h"
+#include "launch_cache.h"
+#include "softmax_prefix.h"
+
+namespace hyb {
+
+// A tile of 32 rows of D codes in LDS, put there by 16-byte copies: chunk c of K's row t
+// sits at c ^ kswz(t), so that the 16 rows which fill the banks have 16 places for
+// one chunk, and of V's at c ^ vswz(t), so that the rows r .. r + 3 and r + 8 .. r + 11 of
+// two neighbouring chunks, which a transposing read takes, fall in distinct banks.
+template <int D>
+struct Q8Tile {
+  static constexpr int CPR = D / 16;           // chunks per row
+  static constexpr int RPI = kWave / CPR;      // rows per copy instruction
+  static constexpr int IK = kTile / RPI;       // copies per tile
+  static constexpr int kBytes = kTile * D;
+  __device__ static constexpr int kswz(int t) { return D == 128 ? (t >> 1) & 7 : (t >> 2) & 3; }
+  __device__ static constexpr int vswz(int t) {
+    return D == 128 ? 2 * ((t >> 1) & 1) + 4 * ((t >> 3) & 1) : 2 * ((t >> 3) & 1);
+  }
+  int krow, kx, vrow, vx;  // this lane's row operand, and its transposing read
+  __device__ inline explicit Q8Tile(int lane) {
+    const int li = lane & 31, hh = lane >> 5, i = lane & 15, b = (lane >> 4) & 1;
+    krow = li * D;
+    kx = 16 * (hh ^ kswz(li));
+    // lane pair i / 2 addresses row 4 hh + (0 .. 3, 8 .. 11)[i / 2], 16 columns of it
+    const int r = 4 * hh + (i / 2 & 3) + 8 * (i / 8);
+    vrow = r * D + 8 * (i & 1);
+    vx = 16 * (b ^ vswz(r));
+  }
+  // codes 32 i + 16 hh .. + 15 of row li
+  __device__ inline uint4 row(const uint8_t* t, int i) const {
+    return *reinterpret_cast<const uint4*>(t + krow + (kx ^ (32 * i)));
+  }
+  // column 32 ct + li at the rows row_of(8 ks + e, hh), e = 0 .. 7.  In each 16-lane
+  // quarter the read gives lane i byte i % 8 of the 8-byte pieces addressed by
+  // lanes i / 8 + 2 e.
+  __device__ inline uint2 column(const uint8_t* t, int ct, int ks) const {
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    const i32x2 x = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+        (__attribute__((address_space(3))) i32x2*)(t + 16 * ks * D + vrow + (vx ^ (32 * ct))));
+    return uint2{(uint32_t)x[0], (uint32_t)x[1]};
+  }
+};
+
+// A range's tiles: where they are and how a wave copies one.
+template <int D>
+struct Q8Tiles {
+  typedef Q8Tile<D> QT;
+  const uint8_t *kc, *vc;  // pools at the KV head
+  SpSeen seen;
+  int t0, nt, P, page_shift, p0, pa, pskip;
+  int stride;  // codes from a token to the next
+  const int* pages;
+
+  // All threads of the workgroup; ends with a barrier.  `lds` holds kMaxRangePages numbers.
+  __device__ inline Q8Tiles(const SoftmaxQ8Args& a, const SpRange& rg, int g, int P_, int* lds) {
+    kc = (const uint8_t*)a.k_cache + g * D;
+    vc = (const uint8_t*)a.v_cache + g * D;
+    seen = sp_seen<2>(a, rg.b);
+    t0 = rg.t0, nt = rg.nt, P = P_;
+    page_shift = a.page_shift;
+    stride = a.s.Hkv * D;
+    pages = lds;
+    // the range's pages (page index p0 + e at e; behind page pa, the last before the
+    // skipped tiles, p0 + e + pskip), clamped to the pool
+    p0 = rg.lo >> page_shift;
+    pa = 0x7fffffff;
+    pskip = 0;
+    if (seen.skip > 0 && t0 < seen.st && t0 + nt > seen.st) {
+      pa = (seen.st * kTile - 1) >> page_shift;
+      pskip = max(0, ((seen.st + seen.skip) * kTile >> page_shift) - pa - 1);
+    }
+    const int32_t* ptab = a.page_table + (size_t)rg.b * a.max_pages;
+    const int chi = min(rg.hi, P);
+    const int np = chi > rg.lo ? ((chi - 1) >> page_shift) - p0 + 1 - pskip : 0;
+    for (int e = threadIdx.x; e < np; e += blockDim.x)
+      lds[e] = sp_page(a, ptab, (p0 + e + (p0 + e > pa ? pskip : 0)) << page_shift);
+    __syncthreads();
+  }
+  __device__ inline int first_key(int i) const { return seen.tile(t0 + i) * kTile; }
+  // Page of the tile at j0 (cached).
+  __device__ inline int page(int j0) const {
+    const int pi = j0 >> page_shift;
+    return pages[pi - p0 - (pi > pa ? pskip : 0)];
+  }
+  // Bytes of the K and V scales of the tile at j0: K's low.
+  __device__ inline int scales(const SoftmaxQ8Args& a, int g, int j0) const {
+    const size_t row = ((size_t)page(j0) << page_shift) + (j0 & ((1 << page_shift) - 1));
+    const size_t at = (row >> a.sb_shift) * a.s.Hkv + g;
+    return a.k_scales[at] | a.v_scales[at] << 8;
+  }
+  // Whether keys j0 .. j0 + 31 are all cached and seen.
+  __device__ inline bool whole(int j0) const { return j0 + kTile <= P && !seen.cuts(j0); }
+  __device__ inline bool sees(int j) const { return j < P && !seen.hides(j); }
+  // K (kv = 0) or V of the tile at j0 into dst; 16 bytes per lane and copy.  Rows that
+  // are not seen read one of the tile that is: their weights are zero, and what they
+  // hold may be anything.
+  __device__ inline void copy(int kv, int j0, uint8_t* dst, int lane) const {
+    const size_t row0 = ((size_t)__builtin_amdgcn_readfirstlane(page(j0)) << page_shift) + (j0 & ((1 << page_shift) - 1));
+    const uint8_t* base = (kv == 0 ? kc : vc) + row0 * stride;
+    const __amdgpu_buffer_rsrc_t rs =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, kTile * stride, kBufferWord3);
+    const bool all = whole(j0);  // uniform
+#pragma unroll
+    for (int u = 0; u < QT::IK; ++u) {
+      const int t = u * QT::RPI + lane / QT::CPR;
+      const int c = lane % QT::CPR ^ (kv == 0 ? QT::kswz(t) : QT::vswz(t));
+      int r = t;
+      if (!all) {
+        r = min(j0 + t, P - 1);
+        if (seen.hides(r)) r = seen.he < min(j0 + kTile, P) ? seen.he : seen.hs - 1;
+        r -= j0;
+      }
+      buf_to_lds16(rs, dst + u * QT::RPI * D, r * stride + c * 16, 0);
+    }
+  }
+};
+
+// What a wave keeps of its 32 columns: the weights' reference in the log2 domain
+// (finite, so that a wave without tiles weighs nothing; it moves only when a
+// maximum passes it by 2^8), their sum over the lane's rows, and the weighted sums of V^T.
+template <typename T, int D>
+struct Q8Acc {
+  typedef Mma<T> M;
+  typedef typename M::op_t op_t;
+  static constexpr int KD = D / M::KW, KL = kTile / M::KW, NCT = D / kTile;
+  // Entry of a row that lane half hh contracts at step ks, element e: any order will do
+  // that both operands share, and here 16 codes of a row are one read.
+  static constexpr int SPR = 16 / M::E;  // steps of a read
+  __device__ static constexpr int entry(int ks, int hh) { return ks / SPR * 32 + 16 * hh + ks % SPR * M::E; }
+  float m = -1e30f, l = 0.0f;
+  f32x16 acc[NCT];
+  __device__ inline Q8Acc() {
+#pragma unroll
+    for (int ct = 0; ct < NCT; ++ct) acc[ct] = f32x16{};
+  }
+  // Scores (K Q^T) of a tile of codes, without their scale.
+  __device__ static inline f32x16 scores(const Q8Tile<D>& qt, const uint8_t* kt, const op_t (&qop)[KD]) {
+    f32x16 sc = {};
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+      const uint4 c = qt.row(kt, i);
+      if constexpr (sizeof(T) == 2) {
+        sc = M::mma(fp8_bf16(c.x, c.y, 1.0f), qop[2 * i], sc);
+        sc = M::mma(fp8_bf16(c.z, c.w, 1.0f), qop[2 * i + 1], sc);
+      } else {
+        const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const f32x4 k = fp8_f32(w[x], 1.0f);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc = M::mma(k[e], qop[16 * i + 4 * x + e], sc);
+        }
+      }
+    }
+    return sc;
+  }
+  // Weights of a tile's masked scores (in p), for a scale into the log2 domain.
+  __device__ inline void weights(const f32x16& sc, float scale, float (&p)[16]) {
+    float mt = sc[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) mt = fmaxf(mt, sc[e]);
+    mt = fmaxf(mt, xor32(mt)) * scale;
+    if (__any(mt > m + 8.0f)) {
+      mma_settle<T>();
+      const float mn = mt > m + 8.0f ? mt : m;
+      const float corr = __builtin_amdgcn_exp2f(m - mn);
+      l *= corr;
+#pragma unroll
+      for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[ct][e] *= corr;
+      m = mn;
+    }
+    float sum[4] = {};
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale, -m));
+      sum[e % 4] += p[e];
+    }
+    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  }
+  // A tile of cached tokens at j0 with its scales' bytes.
+  __device__ inline void add(const Q8Tiles<D>& t, const Q8Tile<D>& qt, int j0, const uint8_t* kt, const uint8_t* vt,
+                             int bytes, const op_t (&qop)[KD], float scale, int hh) {
+    f32x16 sc = scores(qt, kt, qop);
+    mma_settle<T>();
+    if (!t.whole(j0)) {  // uniform
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sc[e] = t.sees(j0 + row_of(e, hh)) ? sc[e] : -INFINITY;
+    }
+    float p[16];
+    weights(sc, scale * scale_of(bytes & 255), p);
+    const float fv = scale_of(bytes >> 8);
+    if constexpr (sizeof(T) == 2) {
+      // The weights enter P V rounded to bf16 (each off by at most 2^-8 of itself;
+      // products of fp32 run at 1/16 of the rate); their sum is over the unrounded ones.
+      op_t pop[KL];
+#pragma unroll
+      for (int ks = 0; ks < KL; ++ks) pop[ks] = cvt_op<bf16>(&p[ks * 8]);
+#pragma unroll
+      for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+        for (int ks = 0; ks < KL; ++ks) {
+          const uint2 c = qt.column(vt, ct, ks);
+          acc[ct] = M::mma(fp8_bf16(c.x, c.y, fv), pop[ks], acc[ct]);
+        }
+    } else {
+#pragma unroll
+      for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+          const uint2 c = qt.column(vt, ct, ks);
+          const f32x4 lo = fp8_f32(c.x, fv), hi = fp8_f32(c.y, fv);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) acc[ct] = M::mma(e < 4 ? lo[e] : hi[e - 4], p[8 * ks + e], acc[ct]);
+        }
+    }
+  }
+  // The block's tile: n rows of T in LDS, D entries each and 16 bytes apart from the next.
+  static constexpr int LD = D + 16 / (int)sizeof(T);
+  __device__ inline void add_block(const T* kb, const T* vb, int n, const op_t (&qop)[KD], float scale, int li, int hh) {
+    f32x16 sc = {};
+#pragma unroll
+    for (int ks = 0; ks < KD; ++ks) sc = M::mma(load_op<T>(kb + li * LD + entry(ks, hh)), qop[ks], sc);
+    mma_settle<T>();
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sc[e] = row_of(e, hh) < n ? sc[e] : -INFINITY;
+    float p[16];
+    weights(sc, scale, p);
+#pragma unroll
+    for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+      for (int ks = 0; ks < KL; ++ks)
+        acc[ct] = M::mma(load_rows_op<T>(vb + ct * kTile + li, LD, ks, hh, kTile, false), cvt_op<T>(&p[ks * M::E]), acc[ct]);
+  }
+};
+
+// Where the L queries of a KV head's query heads are, one head after the other, in
+// tiles of 32 columns: `groups` of them.
+__host__ __device__ inline int q8_groups(const Shape& s) { return (s.Hq / s.Hkv * s.L + kTile - 1) / kTile; }
+
+// A workgroup answers 32 columns over a range of keys: the four waves take the
+// range's tiles in turn, each through copies of its own (R slots, no barrier in the loop)
+// and sums of its own, joined in LDS at the end.  The codes are converted as they become
+// operands, once each.
+template <typename T, int D>
+__global__ __launch_bounds__(kWave * 4) void hyb_q8_token_kernel(SoftmaxQ8Args a, SpCut cut) {
+  typedef Q8Acc<T, D> A;
+  typedef Q8Tile<D> QT;
+  constexpr int NCT = A::NCT, NW = 4, R = sizeof(T) == 2 ? 4 : 2;  // (fp32: the block's rows take the room)
+  struct alignas(16) Slot {
+    uint8_t k[QT::kBytes], v[QT::kBytes];
+  };
+  struct Block {
+    T k[kTile * A::LD], v[kTile * A::LD];
+  };
+  union Smem {
+    struct {
+      Slot ring[NW][R];
+    } loop;
+    f32x4 parts[NW][NCT * 4][kWave];
+    int plan[kPlanInts];
+    __device__ Smem() {}
+  };
+  __shared__ alignas(16) Smem sh;
+  __shared__ alignas(16) Block blk;
+  __shared__ float refs[NW][kTile], sums[NW][kTile];
+  __shared__ int pages[kMaxRangePages];
+  __shared__ uint16_t bytes[kMaxRange / kTile + 2];
+
+  const int lane = threadIdx.x & (kWave - 1);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int li = lane & 31, hh = lane >> 5;
+  const int Hq = a.s.Hq, Hkv = a.s.Hkv, L = a.s.L, G = Hq / Hkv;
+  int at, hg;
+  sp_place(q8_groups(a.s), at, hg);
+  const int g = at % Hkv, r = at / Hkv;
+  const SpRange rg = sp_range<2>(a, sp_plan<2>(a, cut, sh.plan), r, lane);
+  if (rg.b < 0) return;  // uniform: past the plan's last range
+  const int Lb = sp_block<2>(a, rg.b), P = min(max(a.prefix_len[rg.b], 0), a.max_prefix);
+  // this lane's column: query i of head h
+  const int col = hg * kTile + li, hl = col / L, i = col - hl * L, h = g * G + hl;
+  const bool mine = hl < G && i < Lb;
+  typename A::op_t qop[A::KD];
+  {
+    const T* row = (const T*)a.q + (((size_t)rg.b * L + (mine ? i : 0)) * Hq + (mine ? h : g * G)) * D;
+#pragma unroll
+    for (int ks = 0; ks < A::KD; ++ks) qop[ks] = keep_if<T>(mine, load_op<T>(row + A::entry(ks, hh)));
+  }
+  const Q8Tiles<D> t(a, rg, g, P, pages);
+  const QT qt(lane);
+  const bool block = rg.hi > (P + kTile - 1) / kTile * kTile;  // the range's last tile is the block's
+  const int nt = rg.nt - (block ? 1 : 0), my = (nt - w + NW - 1) / NW;  // cached tiles, this wave's
+  for (int e = threadIdx.x; e < nt; e += NW * kWave) bytes[e] = (uint16_t)t.scales(a, g, t.first_key(e));
+  auto issue = [&](int n, Slot& s) __attribute__((always_inline)) {
+    if (n >= my) return;
+    const int j0 = t.first_key(w + NW * n);
+    t.copy(0, j0, s.k, lane);
+    t.copy(1, j0, s.v, lane);
+  };
+  if (block) {  // rows past the block's are the last again
+    constexpr int EPC = 16 / (int)sizeof(T), CPR = D / EPC;
+    const size_t row0 = (size_t)rg.b * L;
+    for (int x = threadIdx.x; x < kTile * CPR; x += NW * kWave) {
+      const size_t src = ((row0 + min(x / CPR, Lb - 1)) * Hkv + g) * D + x % CPR * EPC;
+      const int dst = x / CPR * A::LD + x % CPR * EPC;
+      *reinterpret_cast<uint4*>(&blk.k[dst]) = *reinterpret_cast<const uint4*>((const T*)a.k + src);
+      *reinterpret_cast<uint4*>(&blk.v[dst]) = *reinterpret_cast<const uint4*>((const T*)a.v + src);
+    }
+  }
+  __syncthreads();  // (the plan's scratch has been read)
+  const float scale = kLog2e / sqrtf((float)D);
+  A acc;
+#pragma unroll
+  for (int n = 0; n < R - 1; ++n) issue(n, sh.loop.ring[w][n]);
+  auto step = [&](int n, auto S) __attribute__((always_inline)) {
+    constexpr int SV = decltype(S)::value;
+    if (n >= my) return;
+    issue(n + R - 1, sh.loop.ring[w][(SV + R - 1) % R]);
+    const int later = min(my - 1 - n, R - 1);
+    if (later == 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(6 * QT::IK) : "memory");
+    else if (later == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * QT::IK) : "memory");
+    else if (later == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * QT::IK) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    const Slot& s = sh.loop.ring[w][SV];
+    acc.add(t, qt, t.first_key(w + NW * n), s.k, s.v, bytes[w + NW * n], qop, scale, hh);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot is read
+  };
+  for (int n = 0; n < my; n += R) {
+    step(n, std::integral_constant<int, 0>{});
+    step(n + 1, std::integral_constant<int, 1>{});
+    if constexpr (R == 4) {
+      step(n + 2, std::integral_constant<int, 2>{});
+      step(n + 3, std::integral_constant<int, 3>{});
+    }
+  }
+  if (block && w == nt % NW) acc.add_block(blk.k, blk.v, Lb, qop, scale, li, hh);
+
+  // The waves' sums over one reference: wave w scales its own and leaves them in
+  // LDS, then joins entries 32 w .. + 31 of every column.
+  mma_settle<T>();
+  const float l = acc.l + xor32(acc.l);
+  if (hh == 0) refs[w][li] = acc.m;
+  lds_barrier();  // (and the slots are free)
+  float mm = refs[0][li];
+#pragma unroll
+  for (int x = 1; x < NW; ++x) mm = fmaxf(mm, refs[x][li]);
+  const float f = __builtin_amdgcn_exp2f(acc.m - mm);
+  if (hh == 0) sums[w][li] = l * f;
+#pragma unroll
+  for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      sh.parts[w][ct * 4 + e][lane] = f32x4{acc.acc[ct][4 * e] * f, acc.acc[ct][4 * e + 1] * f, acc.acc[ct][4 * e + 2] * f,
+                                            acc.acc[ct][4 * e + 3] * f};
+  lds_barrier();
+  if (w >= NCT || !mine) return;
+  float den = 0.0f;
+#pragma unroll
+  for (int x = 0; x < NW; ++x) den += sums[x][li];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    f32x4 o = {};
+#pragma unroll
+    for (int x = 0; x < NW; ++x) {
+      const f32x4 y = sh.parts[x][w * 4 + e][lane];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[k] += y[k];
+    }
+    sp_put<T, D>(a, rg, r, h, i, w * kTile + row_of(4 * e, hh), o, den);
+  }
+  if (w == 0 && hh == 0) sp_put_sum<D>(a, rg, r, h, i, mm, den);
+}
+
+int softmax_q8_splits(const Shape& s, int max_seen) { return softmax_prefix_splits(s, max_seen); }
+
+template <typename T, int D>
+static hipError_t q8_go(const SoftmaxQ8Args& a, hipStream_t st) {
+  SpCut cut;
+  static const int resident = sp_resident(hyb_q8_token_kernel<T, D>, 4);
+  const hipError_t e = sp_launch(hyb_q8_token_kernel<T, D>, resident, 4, true, a, st, &cut, q8_groups(a.s));
+  if (e != hipSuccess || a.n_split == 1) return e;  // one range: already written out
+  const long units = (long)a.s.B * a.s.Hq * ((a.s.L + 1024 / D - 1) / (1024 / D));
+  hipLaunchKernelGGL((hyb_sp_combine_kernel<T, D, 2>), dim3((unsigned)std::min<long>(units, 2048)), dim3(256), 0, st, a,
+                     cut);
+  return hipGetLastError();
+}
+
+// Threads of the largest launch.
+double softmax_q8_threads(const SoftmaxQ8Args& a) {
+  // (a plan's ranges: at most n_split per request, or what kMaxRange asks for)
+  const double need = std::ceil(((double)a.max_seen + a.s.L) / kMaxRange);
+  return 256.0 * a.s.B * a.s.Hkv * q8_groups(a.s) * std::max((double)a.n_split, need);
+}
+
+hipError_t launch_softmax_q8(const SoftmaxQ8Args& a, hipStream_t st) {
+  if (a.s.dtype == 1) return a.s.D == 64 ? q8_go<bf16, 64>(a, st) : q8_go<bf16, 128>(a, st);
+  return a.s.D == 64 ? q8_go<float, 64>(a, st) : q8_go<float, 128>(a, st);
+}
+
+}  // namespace hyb
