@@ -104,7 +104,8 @@ typedef enum {
   HYB_OP_WINDOW_STEP = 6,
   HYB_OP_WINDOW_PREFILL = 7,
   HYB_OP_WINDOW_BACKWARD = 8,
-  HYB_OP_WINDOW_STEP_Q8 = 9
+  HYB_OP_WINDOW_STEP_Q8 = 9,
+  HYB_OP_PACKED_BACKWARD = 10
 } hyb_op_t;
 
 typedef struct {
@@ -558,9 +559,46 @@ int softmax_window_step_paged_q8(
     const int32_t* block_len, void* out, void* ws, size_t ws_bytes,
     void* stream);
 
+/* softmax_window_prefill over packed sequences: dims->batch sequences of any lengths,
+ * one after the other in `tokens` rows (N, 0 .. 2^30), as kv_pages_plan packs a batch's
+ * prompts and a trainer its documents.  Sequence b is rows token_start[b] ..
+ * token_start[b + 1] - 1 (device [B + 1], not falling; clamped to [0, N], and
+ * token_start[0] read as 0); a token sees tokens of its own sequence only, as there: blocks of
+ * L = dims->block count from the sequence's first token, L = 1 is causal attention, a
+ * window of N or more full (block-)causal.  q [N][Hq][d], k, v [N][Hkv][d] may be views
+ * of one packed projection: strides in elements from a row to the next, 0 for
+ * contiguous, a multiple of 8, at most 2^24.  out [N][Hq][d] is contiguous; lse (fp32
+ * [Hq][N], or NULL) as there.  Rows behind the last sequence play no part and are not
+ * written.  The values of a sequence's own tokens must be finite, scores q.k below 1e29
+ * in magnitude.  Up to 65536 query heads; feat_dim and n_slots are not used (feat_dim
+ * must still be valid).  No workspace.  out and lse must not overlap each other or an input. */
+int softmax_packed_prefill(const hyb_dims_t* dims, int32_t tokens,
+                           int32_t window, int32_t n_sinks, const void* q,
+                           const void* k, const void* v, int64_t q_stride,
+                           int64_t k_stride, int64_t v_stride,
+                           const int32_t* token_start, void* out, float* lse,
+                           void* stream);
+
+/* Gradient of softmax_packed_prefill with respect to q, k and v for the upstream
+ * gradient dout [N][Hq][d] (dims->dtype); out (dims->dtype) and lse as the forward call
+ * left them.  dq [N][Hq][d], dk, dv [N][Hkv][d], contiguous, in dims->dtype or fp32 with
+ * HYB_OUT_F32, all required and overwritten: zero in the rows behind the last sequence
+ * (a call of no sequences writes nothing).
+ * ws/ws_bytes: at least hybrid_workspace_bytes(dims, HYB_OP_PACKED_BACKWARD, tokens) bytes.
+ * No output may overlap another output, an input or the workspace.  Deterministic (no
+ * atomics). */
+int softmax_packed_backward(const hyb_dims_t* dims, int32_t tokens,
+                            int32_t window, int32_t n_sinks, const void* q,
+                            const void* k, const void* v, int64_t q_stride,
+                            int64_t k_stride, int64_t v_stride,
+                            const int32_t* token_start, const void* out,
+                            const float* lse, const void* dout, void* dq,
+                            void* dk, void* dv, void* ws, size_t ws_bytes,
+                            void* stream);
+
 /* Workspace bytes the given op needs for these dims; `extent` is seq_len for
  * HYB_OP_PREFILL, HYB_OP_BACKWARD, HYB_OP_BACKWARD_FULL, HYB_OP_WINDOW_PREFILL
- * and HYB_OP_WINDOW_BACKWARD, max_prefix for HYB_OP_SOFTMAX_PREFIX, the cached
+ * and HYB_OP_WINDOW_BACKWARD, tokens for HYB_OP_PACKED_BACKWARD, max_prefix for HYB_OP_SOFTMAX_PREFIX, the cached
  * tokens a request sees at most for HYB_OP_WINDOW_STEP and
  * HYB_OP_WINDOW_STEP_Q8, ignored otherwise.
  * Returns 0 for invalid dims. */

@@ -26,7 +26,8 @@ HYB_STEP_SPLIT, HYB_STEP_WHOLE, HYB_STEP_HALVES = 2, 4, 8
 _STEP_KERNEL = {None: 0, "auto": 0, "split": HYB_STEP_SPLIT, "whole": HYB_STEP_WHOLE,
                 "halves": HYB_STEP_HALVES}
 OP_STEP, OP_COMMIT, OP_PREFILL, OP_SOFTMAX_PREFIX, OP_BACKWARD, OP_BACKWARD_FULL = 0, 1, 2, 3, 4, 5
-OP_WINDOW_STEP, OP_WINDOW_PREFILL, OP_WINDOW_BACKWARD, OP_WINDOW_STEP_Q8 = 6, 7, 8, 9
+OP_WINDOW_STEP, OP_WINDOW_PREFILL, OP_WINDOW_BACKWARD = 6, 7, 8
+OP_WINDOW_STEP_Q8, OP_PACKED_BACKWARD = 9, 10
 _ROPE_LAYOUT = {"half": 0, "interleaved": 1}
 STATUS = {0: "HYB_OK", 1: "HYB_ENULL", 2: "HYB_EINVAL", 3: "HYB_EALIGN",
           4: "HYB_EDTYPE", 5: "HYB_EUNSUPPORTED", 6: "HYB_EWORKSPACE",
@@ -38,7 +39,8 @@ EXPORTS = ("hybrid_attn_step", "hybrid_attn_step_commit", "hybrid_state_commit",
            "hybrid_last_error", "softmax_window_step_paged", "softmax_window_prefill",
            "softmax_window_backward", "hybrid_qk_norm_rope", "hybrid_qk_norm_rope_paged",
            "hybrid_qk_norm_rope_backward", "hybrid_rope_workspace_bytes", "kv_pages_plan",
-           "kv_pages_q8_write", "kv_pages_q8_read", "softmax_window_step_paged_q8")
+           "kv_pages_q8_write", "kv_pages_q8_read", "softmax_window_step_paged_q8",
+           "softmax_packed_prefill", "softmax_packed_backward")
 NOALLOC_SCRATCH_BYTES = 64 << 20
 
 
@@ -109,6 +111,9 @@ def load():
     lib.kv_pages_q8_read.argtypes = [Q] + [vp] * 10
     lib.softmax_window_step_paged_q8.argtypes = [P] + [vp] * 7 + [i32] * 3 + [vp, i32, vp, i32, i32,
                                                                               vp, vp, vp, sz, vp]
+    i64 = ctypes.c_int64
+    lib.softmax_packed_prefill.argtypes = [P, i32, i32, i32, vp, vp, vp, i64, i64, i64] + [vp] * 4
+    lib.softmax_packed_backward.argtypes = [P, i32, i32, i32, vp, vp, vp, i64, i64, i64] + [vp] * 8 + [sz, vp]
     lib.hybrid_workspace_bytes.argtypes = [P, i32, i32]
     lib.hybrid_workspace_bytes.restype = sz
     lib.hybrid_last_error.argtypes = []
@@ -119,7 +124,7 @@ def load():
               "softmax_window_step_paged", "softmax_window_prefill", "softmax_window_backward",
               "hybrid_qk_norm_rope", "hybrid_qk_norm_rope_paged", "hybrid_qk_norm_rope_backward",
               "kv_pages_plan", "kv_pages_q8_write", "kv_pages_q8_read",
-              "softmax_window_step_paged_q8"):
+              "softmax_window_step_paged_q8", "softmax_packed_prefill", "softmax_packed_backward"):
         getattr(lib, n).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -831,3 +836,62 @@ def softmax_window_step_paged_q8(dev, q, k, v, k_pages, v_pages, k_scales, v_sca
         _dptr(dev, block_len, "block_len", i32, (B,)), _dptr(dev, out, "out", odt, q.shape),
         *_ws(dev, ws), _raw_stream(dev)))
     return out
+
+
+def _packed_args(dev, q, k, v, token_start, block, odt):
+    """Dims and the addresses and strides of packed q, k, v, and where the sequences start."""
+    N, Hq, d = q.shape
+    kv = (N, k.shape[1], d)
+    pq, sq = _rows(dev, q, "q", q.dtype, q.shape)
+    pk, sk = _rows(dev, k, "k", q.dtype, kv)
+    pv, sv = _rows(dev, v, "v", q.dtype, kv)
+    dims = _dims(token_start.numel() - 1, Hq, kv[1], d, block, 64, _dt(q), 1,
+                 HYB_OUT_F32 if odt is not q.dtype else 0)
+    return dims, kv, (pq, pk, pv, sq, sk, sv, _dptr(dev, token_start, "token_start", torch.int32))
+
+
+@_placed
+def softmax_packed_prefill(dev, q, k, v, token_start, block, window, n_sinks=0, out=None, lse=None,
+                           want_lse=True, out_f32=False):
+    """softmax_window_prefill over packed sequences: rows token_start[b] .. token_start[b + 1]
+    - 1 ([B + 1] int32 on the device) of q [N][Hq][d] and k, v [N][Hkv][d], which may be views of
+    one packed projection.  block 1 is causal attention, a window of N or more sees every
+    earlier block.  Rows behind the last sequence of out and lse are left as they were (zero if
+    made here).  Returns (out, lse fp32 [Hq][N] or None)."""
+    odt, f32 = _odt(q.dtype, out, out_f32), torch.float32
+    N, Hq, _ = q.shape
+    dims, _, at = _packed_args(dev, q, k, v, token_start, block, odt)
+    if out is None:
+        out = torch.zeros(q.shape, dtype=odt, device=q.device)
+    if lse is None and want_lse:
+        lse = torch.zeros((Hq, N), dtype=f32, device=q.device)
+    _check(load().softmax_packed_prefill(
+        dims, min(N, _I32), _reach(window), _reach(n_sinks), *at, _dptr(dev, out, "out", odt, q.shape),
+        _dptr(dev, lse, "lse", f32, (Hq, N)), _raw_stream(dev)))
+    return out, lse
+
+
+@_placed
+def softmax_packed_backward(dev, q, k, v, token_start, out, lse, dout, block, window, n_sinks=0, dq=None,
+                            dk=None, dv=None, ws=None, out_f32=False):
+    """Gradient of softmax_packed_prefill for the upstream gradient dout; out (in q's dtype)
+    and lse as the forward call left them.  Returns (dq, dk, dv) in q's dtype (fp32 with
+    out_f32); rows behind the last sequence are zero."""
+    lib = load()
+    act, odt = q.dtype, _odt(q.dtype, dq, out_f32)
+    N, Hq, _ = q.shape
+    dims, kv, at = _packed_args(dev, q, k, v, token_start, block, odt)
+    dq = torch.empty(q.shape, dtype=odt, device=q.device) if dq is None else dq
+    dk = torch.empty(kv, dtype=odt, device=q.device) if dk is None else dk
+    dv = torch.empty(kv, dtype=odt, device=q.device) if dv is None else dv
+    if dims.batch == 0:  # no sequence: every row is behind the last
+        return dq.zero_(), dk.zero_(), dv.zero_()
+    if ws is None and N > 0:
+        need = lib.hybrid_workspace_bytes(dims, OP_PACKED_BACKWARD, min(N, _I32))
+        ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _check(lib.softmax_packed_backward(
+        dims, min(N, _I32), _reach(window), _reach(n_sinks), *at, _dptr(dev, out, "out", act, q.shape),
+        _dptr(dev, lse, "lse", torch.float32, (Hq, N)), _dptr(dev, dout, "dout", act, q.shape),
+        _dptr(dev, dq, "dq", odt, q.shape), _dptr(dev, dk, "dk", odt, kv), _dptr(dev, dv, "dv", odt, kv),
+        *_ws(dev, ws), _raw_stream(dev)))
+    return dq, dk, dv

@@ -12,6 +12,7 @@
 #include "../../include/hybrid_attn.h"
 #include "launch.h"
 #include "launch_cache.h"
+#include "launch_packed.h"
 
 namespace {
 
@@ -979,6 +980,105 @@ int softmax_window_step_paged_q8(const hyb_dims_t* dims, const void* q, const vo
 
 namespace {
 
+// What softmax_packed_prefill and its gradient check alike.
+int check_packed(const hyb_dims_t* dims, int32_t tokens, int32_t window, int32_t n_sinks, int64_t q_stride,
+                 int64_t k_stride, int64_t v_stride, hyb::PackedArgs* a) {
+  hyb::Shape& s = a->s;
+  TRY(check_dims(dims, false, &s));
+  TRY(no_step_flags(dims));
+  if (tokens < 0 || tokens > (1 << 30)) return fail(HYB_EINVAL, "tokens %d is not in 0 .. 2^30", tokens);
+  if (window < 0 || n_sinks < 0)
+    return fail(HYB_EINVAL, "window %d and n_sinks %d must be >= 0", window, n_sinks);
+  if (s.Hq > 65536) return fail(HYB_EUNSUPPORTED, "n_q_heads %d not supported (at most 65536)", s.Hq);
+  const long nq = (long)s.Hq * s.D, nk = (long)s.Hkv * s.D;
+  const int64_t given[3] = {q_stride, k_stride, v_stride};
+  const long least[3] = {nq, nk, nk};
+  long* set[3] = {&a->q_stride, &a->k_stride, &a->v_stride};
+  for (int i = 0; i < 3; ++i) {
+    // (a tile of 32 rows is addressed with 32 bits)
+    if (given[i] != 0 && (given[i] < least[i] || given[i] > (1L << 24)))
+      return fail(HYB_EINVAL, "a row stride of %ld is shorter than the row, or longer than 2^24", (long)given[i]);
+    if (given[i] % 8) return fail(HYB_EALIGN, "a row stride of %ld is not a multiple of 8 elements", (long)given[i]);
+    *set[i] = given[i] ? given[i] : least[i];
+  }
+  if (s.B > 0 && tokens > 0 && hyb::packed_threads(s, tokens) > 0xffffffffL)
+    return fail(HYB_EINVAL, "tokens * heads exceeds the grid limit");
+  a->N = tokens, a->window = window, a->n_sinks = n_sinks;
+  return HYB_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int softmax_packed_prefill(const hyb_dims_t* dims, int32_t tokens, int32_t window, int32_t n_sinks, const void* q,
+                           const void* k, const void* v, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                           const int32_t* token_start, void* out, float* lse, void* stream) {
+  hyb::PackedArgs a{};
+  TRY(check_packed(dims, tokens, window, n_sinks, q_stride, k_stride, v_stride, &a));
+  const hyb::Shape& s = a.s;
+  if (s.B == 0 || tokens == 0) return ok();
+  TRY(check_ptr(q, "q"));
+  TRY(check_ptr(k, "k"));
+  TRY(check_ptr(v, "v"));
+  TRY(check_ptr(token_start, "token_start"));
+  TRY(check_ptr(out, "out"));
+  TRY(check_ptr(lse, "lse", false));
+  const size_t es = elem_bytes(s.dtype), n = tokens;
+  const size_t nq = (size_t)s.Hq * s.D, nk = (size_t)s.Hkv * s.D;
+  const Rows in[3] = {{q, nq * es, a.q_stride * es}, {k, nk * es, a.k_stride * es}, {v, nk * es, a.v_stride * es}};
+  const Buf written[2] = {{out, n * nq * out_bytes(s)}, {lse, n * s.Hq * 4}};
+  const Buf small[1] = {{token_start, ((size_t)s.B + 1) * 4}};
+  TRY(check_buffers(written, 2, true, in, 3, tokens));
+  TRY(check_overlaps(written, 2, small, 1));
+  a.q = q, a.k = k, a.v = v, a.token_start = token_start;
+  a.out = out, a.lse = lse;
+  (void)hipGetLastError();
+  return launched(hyb::launch_packed_prefill(a, (hipStream_t)stream), "softmax_packed_prefill");
+}
+
+int softmax_packed_backward(const hyb_dims_t* dims, int32_t tokens, int32_t window, int32_t n_sinks, const void* q,
+                            const void* k, const void* v, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                            const int32_t* token_start, const void* out, const float* lse, const void* dout, void* dq,
+                            void* dk, void* dv, void* ws, size_t ws_bytes, void* stream) {
+  hyb::PackedArgs a{};
+  TRY(check_packed(dims, tokens, window, n_sinks, q_stride, k_stride, v_stride, &a));
+  const hyb::Shape& s = a.s;
+  if (s.B == 0 || tokens == 0) return ok();
+  TRY(check_ptr(q, "q"));
+  TRY(check_ptr(k, "k"));
+  TRY(check_ptr(v, "v"));
+  TRY(check_ptr(token_start, "token_start"));
+  TRY(check_ptr(out, "out"));
+  TRY(check_ptr(lse, "lse"));
+  TRY(check_ptr(dout, "dout"));
+  TRY(check_ptr(dq, "dq"));
+  TRY(check_ptr(dk, "dk"));
+  TRY(check_ptr(dv, "dv"));
+  const size_t need = hybrid_workspace_bytes(dims, HYB_OP_PACKED_BACKWARD, tokens);
+  if (!ws || ws_bytes < need)
+    return fail(HYB_EWORKSPACE, "softmax_packed_backward needs %zu workspace bytes, got %zu", need,
+                ws ? ws_bytes : (size_t)0);
+  TRY(check_ptr(ws, "ws"));
+  const size_t es = elem_bytes(s.dtype), eo = out_bytes(s), n = tokens;
+  const size_t nq = (size_t)s.Hq * s.D, nk = (size_t)s.Hkv * s.D;
+  const Rows in[3] = {{q, nq * es, a.q_stride * es}, {k, nk * es, a.k_stride * es}, {v, nk * es, a.v_stride * es}};
+  const Buf written[4] = {{dq, n * nq * eo}, {dk, n * nk * eo}, {dv, n * nk * eo}, {ws, need}};
+  const Buf read_only[4] = {{out, n * nq * es}, {dout, n * nq * es}, {lse, n * s.Hq * 4},
+                            {token_start, ((size_t)s.B + 1) * 4}};
+  TRY(check_buffers(written, 4, true, in, 3, tokens));
+  TRY(check_overlaps(written, 4, read_only, 4));
+  a.q = q, a.k = k, a.v = v, a.token_start = token_start;
+  a.out = const_cast<void*>(out), a.lse = const_cast<float*>(lse);  // (only read)
+  a.dout = dout, a.dq = dq, a.dk = dk, a.dv = dv, a.ws = (float*)ws;
+  (void)hipGetLastError();
+  return launched(hyb::launch_packed_backward(a, (hipStream_t)stream), "softmax_packed_backward");
+}
+
+}  // extern "C"
+
+namespace {
+
 // Validation and dispatch of the backward; dq, dk, dv all null (the Stage-1
 // gradient only) or all set (the input gradients as well).
 int backward_impl(const hyb_dims_t* dims, int32_t seq_len, const void* q,
@@ -1101,6 +1201,8 @@ size_t hybrid_workspace_bytes(const hyb_dims_t* dims, int32_t op,
       return hyb::prefill_ws_bytes(s, extent);
     case HYB_OP_WINDOW_STEP:
       return hyb::softmax_prefix_ws_bytes(s, hyb::softmax_window_splits(s, extent));
+    case HYB_OP_PACKED_BACKWARD:
+      return s.B > 0 && extent > 0 && extent <= (1 << 30) ? hyb::packed_backward_ws_bytes(s, extent) : 0;
     case HYB_OP_WINDOW_STEP_Q8:
       if (extent > 0x7fffffff - 64) return 0;
       return hyb::softmax_prefix_ws_bytes(s, hyb::softmax_q8_splits(s, extent + 32));

@@ -21,14 +21,13 @@
 
 #include "fp8.h"
 #include "launch_cache.h"
+#include "ragged.h"
 
 namespace hyb {
 
 constexpr int kQ8Rows = 64;   // rows that a wave holds
 constexpr int kQ8Waves = 4;   // of a workgroup
 
-// First row of request b (clamped to the rows there are; request 0 starts at row 0).
-__device__ inline int q8_start(const KvQ8Args& a, int b) { return b == 0 ? 0 : min(max(a.token_start[b], 0), a.N); }
 __host__ __device__ inline long q8_first_job(int start, int b, int shift) { return (long)(start >> shift) + 2L * b; }
 
 // The rows lo .. lo + n - 1 (of k and v) that job `x` of blocks of 2^shift tokens
@@ -39,19 +38,14 @@ struct Q8Rows {
   int at;       // its place in the block
   size_t dst;   // row of the pools where the block starts
   __device__ inline Q8Rows(const KvQ8Args& a, long x, int shift, int lane) {
-    int lo = 0, hi = a.B;  // the last request in lo .. hi - 1 that starts by job x
-    while (hi - lo > 1) {
-      const int step = (hi - lo + kWave - 1) / kWave, b = lo + lane * step;
-      const bool by = b < hi && q8_first_job(q8_start(a, b), b, shift) <= x;
-      lo += step * max(0, __builtin_popcountll(__ballot(by)) - 1);
-      hi = min(hi, lo + step);
-    }
-    const int s = q8_start(a, lo), e = q8_start(a, lo + 1), cap = a.max_pages << a.page_shift;
-    const long p0 = min(max(a.first[lo], 0), cap), p1 = min(p0 + max(e - s, 0), (long)cap);
-    const long j0 = ((p0 >> shift) + x - q8_first_job(s, lo, shift)) << shift;
+    auto start = [&](int b) { return ragged_start(a.token_start, b, a.N); };
+    const int b = ragged_find(a.B, x, lane, [&](int i) { return q8_first_job(start(i), i, shift); });
+    const int s = start(b), e = start(b + 1), cap = a.max_pages << a.page_shift;
+    const long p0 = min(max(a.first[b], 0), cap), p1 = min(p0 + max(e - s, 0), (long)cap);
+    const long j0 = ((p0 >> shift) + x - q8_first_job(s, b, shift)) << shift;
     const long from = max(p0, j0), to = min(p1, j0 + (1L << shift));
     if (from >= to) return;
-    const int page = a.page_table[(size_t)lo * a.max_pages + (j0 >> a.page_shift)];
+    const int page = a.page_table[(size_t)b * a.max_pages + (j0 >> a.page_shift)];
     if (page < 0 || page >= a.n_pages) return;
     n = (int)(to - from);
     src = s + (int)(from - p0);

@@ -31,6 +31,8 @@
 
 #include "device.h"
 #include "launch.h"
+#include "launch_packed.h"
+#include "ragged.h"
 
 namespace hyb {
 
@@ -38,9 +40,6 @@ namespace hyb {
 // which it sees none leaves weights of exactly zero.
 constexpr float kNoRef = -1e30f;
 
-__device__ inline int win_len(const WindowArgs& a, int b) {
-  return a.seq_lens ? min(max(a.seq_lens[b], 0), a.T) : a.T;
-}
 
 // What query i (below len) sees: keys lo .. end - 1, and those below sinks.
 struct WinRow {
@@ -97,12 +96,93 @@ __device__ inline void win_place(int bid, int nbg, int& bg, int& x) {
   x = bid / nbg;
 }
 
+// Units of the query kernels (32 queries of a head) per workgroup; keys of a
+// workgroup of the dK, dV kernels.
+constexpr int kWinWaves = 4;
+constexpr int kWinKeys = 4 * kTile;
+
+// A sequence: its tokens, the rows that are its own (those past its tokens get gradients
+// of zero), and where they are.  Offsets are of a head's entries of its first row.
+template <typename A>
+struct WinSeq;
+template <>
+struct WinSeq<WindowArgs> {
+  const WindowArgs& a;
+  int b, len, cap;
+  __device__ inline WinSeq(const WindowArgs& a_, int b_)
+      : a(a_), b(b_), len(a_.seq_lens ? min(max(a_.seq_lens[b_], 0), a_.T) : a_.T), cap(a_.T) {}
+  __device__ inline size_t q(int h, int D) const { return ((size_t)b * a.T * a.s.Hq + h) * D; }
+  __device__ inline size_t k(int g, int D) const { return ((size_t)b * a.T * a.s.Hkv + g) * D; }
+  __device__ inline size_t v(int g, int D) const { return k(g, D); }
+  __device__ inline size_t dout(int h, int D) const { return q(h, D); }
+  // from a row to the next
+  __device__ inline size_t qs(int D) const { return (size_t)a.s.Hq * D; }
+  __device__ inline size_t ks(int D) const { return (size_t)a.s.Hkv * D; }
+  __device__ inline size_t vs(int D) const { return ks(D); }
+  __device__ inline size_t row(int i) const { return (size_t)b * a.T + i; }         // of out, the gradients
+  __device__ inline size_t lse(int h, int i) const { return ((size_t)b * a.s.Hq + h) * a.T + i; }
+  // of the bf16 gradient's statistics: [B][Hq][Tp], Tp = T rounded up to a tile
+  __device__ inline size_t stats(int h, int i) const { return ((size_t)b * a.s.Hq + h) * ((a.T + kTile - 1) / kTile * kTile) + i; }
+};
+// Packed: one sequence more than there are, of no tokens, has the rows behind the last.
+__host__ __device__ inline long win_packed_tiles(int start, int b) { return (long)(start / kTile) + b; }
+template <>
+struct WinSeq<PackedArgs> {
+  const PackedArgs& a;
+  int b, len, cap, start;
+  __device__ inline WinSeq(const PackedArgs& a_, int b_) : a(a_), b(b_) {
+    start = ragged_start(a.token_start, b, a.N);
+    len = b < a.s.B ? max(ragged_start(a.token_start, b + 1, a.N) - start, 0) : 0;
+    cap = b < a.s.B ? len : a.N - start;
+  }
+  __device__ inline size_t q(int h, int D) const { return (size_t)start * a.q_stride + (size_t)h * D; }
+  __device__ inline size_t k(int g, int D) const { return (size_t)start * a.k_stride + (size_t)g * D; }
+  __device__ inline size_t v(int g, int D) const { return (size_t)start * a.v_stride + (size_t)g * D; }
+  __device__ inline size_t dout(int h, int D) const { return ((size_t)start * a.s.Hq + h) * D; }
+  __device__ inline size_t qs(int) const { return a.q_stride; }
+  __device__ inline size_t ks(int) const { return a.k_stride; }
+  __device__ inline size_t vs(int) const { return a.v_stride; }
+  __device__ inline size_t row(int i) const { return (size_t)start + i; }
+  __device__ inline size_t lse(int h, int i) const { return (size_t)h * a.N + start + i; }
+  // [Hq][tiles of all sequences][32]
+  __device__ inline size_t stats(int h, int i) const {
+    return ((size_t)h * win_packed_tiles(a.N, a.s.B + 1) + win_packed_tiles(start, b)) * kTile + i;
+  }
+};
+
+// Packed: the first workgroup of the queries of sequence b, and of its keys, so that
+// every sequence has room for its own: of 4 units, G per tile of queries, and of 128 keys.
+__host__ __device__ inline long win_packed_queries(int start, int b, int G) {
+  return (long)start * G / (kWinWaves * kTile) + (long)b * ((G + kWinWaves - 1) / kWinWaves + 2);
+}
+__host__ __device__ inline long win_packed_keys(int start, int b) { return (long)(start / kWinKeys) + b; }
+
+// This workgroup's sequence, KV head, and its place x among the sequence's
+// workgroups of queries, of `wgs` (per sequence and head, or packed per head); those of the
+// last queries, which see most, come first.
+__device__ inline WinSeq<WindowArgs> win_of_queries(const WindowArgs& a, int wgs, int, int& g, int& x) {
+  int bg;
+  win_place(blockIdx.x, a.s.B * a.s.Hkv, bg, x);
+  x = wgs - 1 - x;
+  g = bg % a.s.Hkv;
+  return WinSeq<WindowArgs>(a, bg / a.s.Hkv);
+}
+__device__ inline WinSeq<PackedArgs> win_of_queries(const PackedArgs& a, int wgs, int lane, int& g, int& x) {
+  const int G = a.s.Hq / a.s.Hkv;
+  win_place(blockIdx.x, a.s.Hkv, g, x);
+  x = wgs - 1 - x;
+  const int b = ragged_find(a.s.B + 1, x, lane,
+                            [&](int i) { return win_packed_queries(ragged_start(a.token_start, i, a.N), i, G); });
+  const WinSeq<PackedArgs> s(a, b);
+  x = max(0, x - (int)win_packed_queries(s.start, b, G));
+  return s;
+}
+
 // The dK, dV kernels: a workgroup owns 128 keys and goes through the query
 // tiles that see them, of all heads of the KV head.  These lists are cut into
 // parts that are summed in the workspace: those of the keys among the sinks, which
 // every later query sees (the first `ns` workgroups of a (request, KV head)), into
 // ps, the others into p.
-constexpr int kWinKeys = 4 * kTile;
 struct WinParts {
   int wgs, ns, ps, p;
   bool halves;  // (bf16) workgroups of two halves
@@ -118,6 +198,7 @@ struct WinParts {
 struct WinItem {
   int x, part, parts, span;
   bool sink;
+  __device__ inline WinItem() {}
   __device__ inline WinItem(const WindowArgs& a, const WinParts& c, int y) {
     sink = y < c.ns * c.ps;
     parts = sink ? c.ps : c.p;
@@ -130,10 +211,36 @@ struct WinItem {
   __device__ inline float* sums(const WindowArgs& a, const WinParts& c) const {
     return a.sums + (sink ? 0 : c.sink_rows() * 2 * a.s.B * a.s.Hkv * D);
   }
-  __device__ inline size_t row(const WindowArgs& a, int o, int b, int j, int g) const {
-    return (((size_t)(part * 2 + o) * a.s.B + b) * span + j) * a.s.Hkv + g;
+  __device__ inline size_t row(const WinSeq<WindowArgs>& s, int o, int j, int g) const {
+    return (((size_t)(part * 2 + o) * s.a.s.B + s.b) * span + j) * s.a.s.Hkv + g;
+  }
+  __device__ inline size_t row(const WinSeq<PackedArgs>& s, int o, int j, int g) const {
+    return ((size_t)(part * 2 + o) * s.a.N + s.row(j)) * s.a.s.Hkv + g;
   }
 };
+// This workgroup's sequence, KV head and item; those of the first keys, which most queries
+// see, come first.  Packed: every list has p parts, also the sinks', with the sums
+// [part][o][N][Hkv][D].
+__device__ inline WinSeq<WindowArgs> win_of_keys(const WindowArgs& a, const WinParts& cut, int, int& g, WinItem& it) {
+  int bg, y;
+  win_place(blockIdx.x, a.s.B * a.s.Hkv, bg, y);
+  it = WinItem(a, cut, y);
+  g = bg % a.s.Hkv;
+  return WinSeq<WindowArgs>(a, bg / a.s.Hkv);
+}
+__device__ inline WinSeq<PackedArgs> win_of_keys(const PackedArgs& a, const WinParts& cut, int lane, int& g, WinItem& it) {
+  int y;
+  win_place(blockIdx.x, a.s.Hkv, g, y);
+  it.sink = false;
+  it.parts = cut.p;
+  it.part = y % cut.p;
+  const int x = y / cut.p;
+  const int b = ragged_find(a.s.B + 1, x, lane,
+                            [&](int i) { return win_packed_keys(ragged_start(a.token_start, i, a.N), i); });
+  const WinSeq<PackedArgs> s(a, b);
+  it.x = max(0, x - (int)win_packed_keys(s.start, b));
+  return s;
+}
 
 // ---- fp32 kernels -------------------------------------------------------------
 //
@@ -143,8 +250,6 @@ struct WinItem {
 // one is used, and moves to the other buffer at the end of the step, so a step has
 // one barrier.  fp32 products run at 1/16 of the bf16 rate and bound the loop (a
 // pair of tiles at d = 64 is 128 products of 64 cycles for the four waves' SIMDs).
-
-constexpr int kWinWaves = 4;
 
 template <int D>
 struct WinF32 {
@@ -160,18 +265,18 @@ struct WinF32 {
   };
 };
 
-// Rows row0 .. row0 + 31 of two arrays (row stride in elements) into registers,
+// Rows row0 .. row0 + 31 of two arrays (row strides in elements) into registers,
 // and from there, zero from row `rows` on, into two tiles; by four waves, whose
 // thread number t is.  (The zeros are put in last: a select at the load would wait for it.)
 template <int D>
-__device__ inline void win_fetch(typename WinF32<D>::Regs& r, const float* a, const float* b, size_t stride, int row0,
-                                 int rows, int t) {
+__device__ inline void win_fetch(typename WinF32<D>::Regs& r, const float* a, const float* b, size_t as,
+                                 size_t bs, int row0, int rows, int t) {
 #pragma unroll
   for (int u = 0; u < WinF32<D>::NCH; ++u) {
     const int x = t + u * kWave * kWinWaves, i = row0 + x / (D / 4);
-    const size_t at = (size_t)min(i, rows - 1) * stride + x % (D / 4) * 4;
-    r.a[u] = *reinterpret_cast<const f32x4*>(a + at);
-    r.b[u] = *reinterpret_cast<const f32x4*>(b + at);
+    const int row = min(i, rows - 1), c = x % (D / 4) * 4;
+    r.a[u] = *reinterpret_cast<const f32x4*>(a + row * as + c);
+    r.b[u] = *reinterpret_cast<const f32x4*>(b + row * bs + c);
   }
 }
 template <int D>
@@ -236,21 +341,21 @@ __device__ inline void win_store(void* out, size_t row, const f32x16 (&acc)[D / 
 // Units of the query kernels: 32 queries of one head; the heads of a KV head
 // vary fastest, so that a workgroup's waves share their keys.
 struct WinUnit {
-  int b, g, h, i0;  // request, KV head, query head, first query
+  int h, i0;  // query head, first query
   bool any;
 };
-__device__ inline WinUnit win_unit(const WindowArgs& a, int len, int b, int g, int u) {
+__device__ inline WinUnit win_unit(const WindowArgs& a, int len, int g, int u) {
   const int G = a.s.Hq / a.s.Hkv;
   const int i0 = u / G * kTile;
-  return WinUnit{b, g, g * G + u % G, i0, i0 < len};
+  return WinUnit{g * G + u % G, i0, i0 < len};
 }
 
 // Forward.  With H = 2 two halves of four waves take a unit's tiles in turn, each
 // through buffers of its own, and join their sums in LDS: a CU that holds one
 // workgroup has two waves per SIMD then, and one's products run beside the other's
 // weights (3 x 1197 tokens, 8 heads of d = 64, window 300: 47 us with one half, now 40).
-template <int D, int H>
-__global__ __launch_bounds__(kWave* kWinWaves* H) void hyb_win_fwd_kernel(WindowArgs a, int wgs) {
+template <int D, int H, typename A>
+__global__ __launch_bounds__(kWave* kWinWaves* H) void hyb_win_fwd_kernel(A a, int wgs) {
   typedef WinF32<D> C;
   struct Tiles {
     typename C::Tile k[H][2], v[H][2];
@@ -269,18 +374,16 @@ __global__ __launch_bounds__(kWave* kWinWaves* H) void hyb_win_fwd_kernel(Window
   const int half = wave / kWinWaves, w = wave % kWinWaves, t = threadIdx.x % (kWave * kWinWaves);
   const int li = lane & 31, hh = lane >> 5;
   const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv;
-  int bg, x;
-  win_place(blockIdx.x, a.s.B * Hkv, bg, x);
-  x = wgs - 1 - x;  // the longest first
-  const int b = bg / Hkv, g = bg % Hkv;
-  const int len = win_len(a, b);
-  const WinUnit me = win_unit(a, len, b, g, x * kWinWaves + w);
+  int g, x;
+  const WinSeq<A> sq = win_of_queries(a, wgs, lane, g, x);
+  const int len = sq.len;
+  const WinUnit me = win_unit(a, len, g, x * kWinWaves + w);
   const int first = x * kWinWaves / G * kTile, last = min(((x + 1) * kWinWaves - 1) / G * kTile + kTile, len);
   if (first >= len) return;  // uniform
   const WinTiles tl(a, len, first, last, kTile);
-  const size_t qs = (size_t)Hq * D, ks_ = (size_t)Hkv * D;
-  const float* K = (const float*)a.k + ((size_t)b * a.T * Hkv + g) * D;
-  const float* V = (const float*)a.v + ((size_t)b * a.T * Hkv + g) * D;
+  const size_t qs = sq.qs(D), ks_ = sq.ks(D), vs_ = sq.vs(D);
+  const float* K = (const float*)a.k + sq.k(g, D);
+  const float* V = (const float*)a.v + sq.v(g, D);
   const int i = min(me.i0 + li, len - 1);
   const WinRow row(a, len, i), r0(a, len, min(me.i0, len - 1)), r1(a, len, min(me.i0 + kTile, len) - 1);
   // This half's step n takes tile H n + half.
@@ -289,9 +392,9 @@ __global__ __launch_bounds__(kWave* kWinWaves* H) void hyb_win_fwd_kernel(Window
   const int nsteps = (tl.n + H - 1) / H, mine = (tl.n + H - 1 - half) / H;
   auto key = [&](int n) __attribute__((always_inline)) { return tl.first(H * n + half, kTile); };
   typename C::Regs next;
-  if (mine > 0) win_fetch<D>(next, K, V, ks_, key(0), len, t);
+  if (mine > 0) win_fetch<D>(next, K, V, ks_, vs_, key(0), len, t);
   typename C::Ops qop;
-  win_row_ops<D>(qop, (const float*)a.q + ((size_t)b * a.T * Hq + me.h) * D + i * qs, true, hh);
+  win_row_ops<D>(qop, (const float*)a.q + sq.q(me.h, D) + i * qs, true, hh);
   const float scale = kLog2e / sqrtf((float)D);
   float m = kNoRef, l = 0.0f;
   typename C::Acc acc;
@@ -301,7 +404,7 @@ __global__ __launch_bounds__(kWave* kWinWaves* H) void hyb_win_fwd_kernel(Window
   __syncthreads();
   for (int n = 0; n < nsteps; ++n) {
     const int buf = n & 1, j0 = n < mine ? key(n) : 0;
-    if (n + 1 < mine) win_fetch<D>(next, K, V, ks_, key(n + 1), len, t);
+    if (n + 1 < mine) win_fetch<D>(next, K, V, ks_, vs_, key(n + 1), len, t);
     if (me.any && n < mine && !win_none(r0, r1, a.n_sinks, j0, kTile)) {  // uniform over the wave
       f32x16 sc = win_rows_mma<D>(kt[buf], qop, li, hh);
       if (!win_full(r0, r1, a.n_sinks, j0, kTile)) {  // uniform
@@ -365,54 +468,52 @@ __global__ __launch_bounds__(kWave* kWinWaves* H) void hyb_win_fwd_kernel(Window
       }
   }
   if (!me.any || me.i0 + li >= len) return;
-  win_store<float, D>(a.out, ((size_t)b * a.T + i) * Hq + me.h, acc, 1.0f / l, hh, true);
-  if (a.lse && hh == 0) a.lse[((size_t)b * Hq + me.h) * a.T + i] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+  win_store<float, D>(a.out, sq.row(i) * Hq + me.h, acc, 1.0f / l, hh, true);
+  if (a.lse && hh == 0) a.lse[sq.lse(me.h, i)] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
 // dQ, and delta of the rows for the dK, dV kernel.
-template <int D>
-__global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dq_kernel(WindowArgs a, int wgs) {
+template <int D, typename A>
+__global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dq_kernel(A a, int wgs) {
   typedef WinF32<D> C;
   __shared__ alignas(16) typename C::Tile kt[2], vt[2];
   const int lane = threadIdx.x & (kWave - 1), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int li = lane & 31, hh = lane >> 5;
   const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv;
-  int bg, x;
-  win_place(blockIdx.x, a.s.B * Hkv, bg, x);
-  x = wgs - 1 - x;
-  const int b = bg / Hkv, g = bg % Hkv;
-  const int len = win_len(a, b);
-  const WinUnit me = win_unit(a, len, b, g, x * kWinWaves + w);
+  int g, x;
+  const WinSeq<A> sq = win_of_queries(a, wgs, lane, g, x);
+  const int len = sq.len;
+  const WinUnit me = win_unit(a, len, g, x * kWinWaves + w);
   const int first = x * kWinWaves / G * kTile, last = min(((x + 1) * kWinWaves - 1) / G * kTile + kTile, len);
-  const size_t qs = (size_t)Hq * D, ks_ = (size_t)Hkv * D;
+  const size_t qs = sq.qs(D), ks_ = sq.ks(D), vs_ = sq.vs(D);
   typename C::Acc acc;
 #pragma unroll
   for (int ct = 0; ct < C::NCT; ++ct) acc[ct] = f32x16{};
   if (first < len) {  // uniform
     const WinTiles tl(a, len, first, last, kTile);
-    const float* K = (const float*)a.k + ((size_t)b * a.T * Hkv + g) * D;
-    const float* V = (const float*)a.v + ((size_t)b * a.T * Hkv + g) * D;
+    const float* K = (const float*)a.k + sq.k(g, D);
+    const float* V = (const float*)a.v + sq.v(g, D);
     const int i = min(me.i0 + li, len - 1);
     const WinRow row(a, len, i), r0(a, len, min(me.i0, len - 1)), r1(a, len, min(me.i0 + kTile, len) - 1);
     typename C::Regs next;
-    win_fetch<D>(next, K, V, ks_, tl.first(0, kTile), len, threadIdx.x);
+    win_fetch<D>(next, K, V, ks_, vs_, tl.first(0, kTile), len, threadIdx.x);
     typename C::Ops qop, dop;
-    const size_t at = ((size_t)b * a.T * Hq + me.h) * D + i * qs;
-    win_row_ops<D>(qop, (const float*)a.q + at, true, hh);
+    const size_t at = sq.dout(me.h, D) + (size_t)i * Hq * D;
+    win_row_ops<D>(qop, (const float*)a.q + sq.q(me.h, D) + i * qs, true, hh);
     win_row_ops<D>(dop, (const float*)a.dout + at, true, hh);
     float delta = 0.0f;
 #pragma unroll
     for (int ks = 0; ks < C::KD; ++ks) delta += dop[ks] * ((const float*)a.out)[at + win_entry(ks, hh)];
     delta += xor32(delta);
     const float scale = kLog2e / sqrtf((float)D);
-    const size_t st = ((size_t)b * Hq + me.h) * a.T + i;
+    const size_t st = sq.lse(me.h, i);
     const float lse = a.lse[st] * kLog2e;
     if (hh == 0 && me.i0 + li < len) a.ws[st] = delta;
     win_put<D>(next, kt[0], vt[0], tl.first(0, kTile), len, threadIdx.x);
     __syncthreads();
     for (int n = 0; n < tl.n; ++n) {
       const int j0 = tl.first(n, kTile), buf = n & 1;
-      if (n + 1 < tl.n) win_fetch<D>(next, K, V, ks_, tl.first(n + 1, kTile), len, threadIdx.x);
+      if (n + 1 < tl.n) win_fetch<D>(next, K, V, ks_, vs_, tl.first(n + 1, kTile), len, threadIdx.x);
       if (me.any && !win_none(r0, r1, a.n_sinks, j0, kTile)) {
         f32x16 sc = win_rows_mma<D>(kt[buf], qop, li, hh);
         const f32x16 dp = win_rows_mma<D>(vt[buf], dop, li, hh);
@@ -431,8 +532,8 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dq_kernel(WindowArgs
       __syncthreads();
     }
   }
-  if (me.i0 + li >= a.T) return;  // rows past the length: zero
-  win_store<float, D>(a.dq, ((size_t)b * a.T + me.i0 + li) * Hq + me.h, acc,
+  if (me.i0 + li >= sq.cap) return;  // rows past the length: zero
+  win_store<float, D>(a.dq, sq.row(me.i0 + li) * Hq + me.h, acc,
                       me.i0 + li < len ? 1.0f / sqrtf((float)D) : 0.0f, hh, true);
 }
 
@@ -449,21 +550,20 @@ struct WinQueries {
 
 // dK, dV: a wave owns 32 keys, and loops over the queries of all heads of
 // its KV head.
-template <int D>
-__global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dkv_kernel(WindowArgs a, WinParts cut) {
+template <int D, typename A>
+__global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dkv_kernel(A a, WinParts cut) {
   typedef WinF32<D> C;
   __shared__ alignas(16) typename C::Tile qt[2], dt[2];
   __shared__ alignas(16) float stats[2][2][kTile];  // lse (log2) and delta
   const int lane = threadIdx.x & (kWave - 1), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int li = lane & 31, hh = lane >> 5;
   const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv;
-  int bg, x;
-  win_place(blockIdx.x, a.s.B * Hkv, bg, x);
-  const WinItem it(a, cut, x);
-  const int b = bg / Hkv, g = bg % Hkv;
-  const int len = win_len(a, b);
+  int g;
+  WinItem it;
+  const WinSeq<A> sq = win_of_keys(a, cut, lane, g, it);
+  const int len = sq.len;
   const int w0 = it.x * kWinKeys, j0 = w0 + w * kTile, j = j0 + li;  // first key of the workgroup, of the wave
-  const size_t qs = (size_t)Hq * D, ks_ = (size_t)Hkv * D;
+  const size_t qs = sq.qs(D), ks_ = sq.ks(D), vs_ = sq.vs(D);
   typename C::Acc dk, dv;
 #pragma unroll
   for (int ct = 0; ct < C::NCT; ++ct) dk[ct] = dv[ct] = f32x16{};
@@ -479,10 +579,10 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dkv_kernel(WindowArg
     auto tile = [&](int n) __attribute__((always_inline)) { return (t0 + (first + n) % nq) * kTile; };
     auto fetch = [&](int n) __attribute__((always_inline)) {
       const int h = g * G + (first + n) / nq, i0 = tile(n);
-      const size_t head = ((size_t)b * a.T * Hq + h) * D;
-      win_fetch<D>(next, (const float*)a.q + head, (const float*)a.dout + head, qs, i0, len, threadIdx.x);
+      win_fetch<D>(next, (const float*)a.q + sq.q(h, D), (const float*)a.dout + sq.dout(h, D), qs, (size_t)Hq * D, i0, len,
+                   threadIdx.x);
       if (threadIdx.x < 2 * kTile) {
-        const size_t at = ((size_t)b * Hq + h) * a.T + min(i0 + (int)threadIdx.x % kTile, len - 1);
+        const size_t at = sq.lse(h, min(i0 + (int)threadIdx.x % kTile, len - 1));
         nst = threadIdx.x < kTile ? a.lse[at] * kLog2e : a.ws[at];
       }
     };
@@ -493,9 +593,9 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dkv_kernel(WindowArg
     };
     if (nsteps > 0) fetch(0);
     typename C::Ops kop, vop;
-    const size_t at = ((size_t)b * a.T * Hkv + g) * D + (size_t)min(j, len - 1) * ks_;
-    win_row_ops<D>(kop, (const float*)a.k + at, j < len, hh);
-    win_row_ops<D>(vop, (const float*)a.v + at, j < len, hh);
+    const size_t j1 = min(j, len - 1);
+    win_row_ops<D>(kop, (const float*)a.k + sq.k(g, D) + j1 * ks_, j < len, hh);
+    win_row_ops<D>(vop, (const float*)a.v + sq.v(g, D) + j1 * vs_, j < len, hh);
     const float scale = kLog2e / sqrtf((float)D);
     if (nsteps > 0) put(0);
     __syncthreads();
@@ -522,15 +622,15 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dkv_kernel(WindowArg
       __syncthreads();
     }
   }
-  if (j >= a.T) return;
-  const size_t row = ((size_t)b * a.T + j) * Hkv + g;
+  if (j >= sq.cap) return;
+  const size_t row = sq.row(j) * Hkv + g;
   const float fk = j < len ? 1.0f / sqrtf((float)D) : 0.0f, fv = j < len ? 1.0f : 0.0f;
   if (it.parts == 1) {
     win_store<float, D>(a.dk, row, dk, fk, hh, true);
     win_store<float, D>(a.dv, row, dv, fv, hh, true);
   } else {
-    win_store<float, D>(it.sums<D>(a, cut), it.row(a, 0, b, j, g), dk, fk, hh, true);
-    win_store<float, D>(it.sums<D>(a, cut), it.row(a, 1, b, j, g), dv, fv, hh, true);
+    win_store<float, D>(it.sums<D>(a, cut), it.row(sq, 0, j, g), dk, fk, hh, true);
+    win_store<float, D>(it.sums<D>(a, cut), it.row(sq, 1, j, g), dv, fv, hh, true);
   }
 }
 
@@ -619,8 +719,8 @@ __device__ inline void win_store_half(void* out, size_t row, const f32x16 (&acc)
   }
 }
 
-template <int D, int H>
-__global__ __launch_bounds__(kWave* kWinWaves* H, 2) void hyb_win_ring_kernel(WindowArgs a, int wgs) {
+template <int D, int H, typename A>
+__global__ __launch_bounds__(kWave* kWinWaves* H, 2) void hyb_win_ring_kernel(A a, int wgs) {
   typedef Mma<bf16> M;
   typedef M::op_t op_t;
   typedef WinRing<D> RG;
@@ -634,24 +734,22 @@ __global__ __launch_bounds__(kWave* kWinWaves* H, 2) void hyb_win_ring_kernel(Wi
   auto& vr = sh.rings.v[half];
   const int li = lane & 31, hh = lane >> 5;
   const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv;
-  int bg, x;
-  win_place(blockIdx.x, a.s.B * Hkv, bg, x);
-  x = wgs - 1 - x;  // the longest first
-  const int b = bg / Hkv, g = bg % Hkv;
-  const int len = win_len(a, b);
-  const WinUnit me = win_unit(a, len, b, g, x * kWinWaves + w);
+  int g, x;
+  const WinSeq<A> sq = win_of_queries(a, wgs, lane, g, x);
+  const int len = sq.len;
+  const WinUnit me = win_unit(a, len, g, x * kWinWaves + w);
   const int first = x * kWinWaves / G * kTile, last = min(((x + 1) * kWinWaves - 1) / G * kTile + kTile, len);
   if (first >= len) return;  // uniform
   const WinTiles tl(a, len, first, last, kTile);
   const int ntiles = (tl.n + H - 1) / H;  // of each half: the list's every H-th
   auto key = [&](int n) __attribute__((always_inline)) { return tl.first(min(H * n + half, tl.n - 1), kTile); };
-  const size_t qs = (size_t)Hq * D, ks_ = (size_t)Hkv * D;
-  const bf16* K = (const bf16*)a.k + ((size_t)b * a.T * Hkv + g) * D;
-  const bf16* V = (const bf16*)a.v + ((size_t)b * a.T * Hkv + g) * D;
+  const size_t qs = sq.qs(D), ks_ = sq.ks(D), vs_ = sq.vs(D);
+  const bf16* K = (const bf16*)a.k + sq.k(g, D);
+  const bf16* V = (const bf16*)a.v + sq.v(g, D);
 
   op_t qop[KD];
   {
-    const bf16* row = (const bf16*)a.q + ((size_t)b * a.T * Hq + me.h) * D + min(me.i0 + li, len - 1) * qs + hh * E;
+    const bf16* row = (const bf16*)a.q + sq.q(me.h, D) + min(me.i0 + li, len - 1) * qs + hh * E;
 #pragma unroll
     for (int ks = 0; ks < KD; ++ks) qop[ks] = load_op<bf16>(row + ks * KW);
   }
@@ -675,13 +773,14 @@ __global__ __launch_bounds__(kWave* kWinWaves* H, 2) void hyb_win_ring_kernel(Wi
   auto issue = [&](int n, bf16* dst) __attribute__((always_inline)) {
     if (n >= ntiles) return;
     const int j0 = key(n), left = len - 1 - j0;
-    const bf16* base = (w < kWinWaves / 2 ? K : V) + (size_t)j0 * ks_;
+    const size_t rs_ = w < kWinWaves / 2 ? ks_ : vs_;
+    const bf16* base = (w < kWinWaves / 2 ? K : V) + (size_t)j0 * rs_;
     const __amdgpu_buffer_rsrc_t rs =
-        __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(base), 0, (int)(kTile * ks_ * sizeof(bf16)), kBufferWord3);
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(base), 0, (int)(kTile * rs_ * sizeof(bf16)), kBufferWord3);
 #pragma unroll
     for (int u = 0; u < IPW; ++u)
       buf_to_lds16(rs, dst + (w * IPW + u) % RG::IK * RG::RPI * D,
-                   (int)((min(trow[u], left) * (int)ks_ + tcol[u]) * sizeof(bf16)), 0);
+                   (int)((min(trow[u], left) * (int)rs_ + tcol[u]) * sizeof(bf16)), 0);
   };
   // K of tile nk or V of tile nv, whichever this wave copies.
   auto issue_step = [&](int nk, bf16* dk, int nv, bf16* dv) __attribute__((always_inline)) {
@@ -821,8 +920,8 @@ __global__ __launch_bounds__(kWave* kWinWaves* H, 2) void hyb_win_ring_kernel(Wi
   }
   const int i = me.i0 + li;
   if (i >= len) return;
-  win_store_half<D, H>(a.out, ((size_t)b * a.T + i) * Hq + me.h, acc, 1.0f / l, hh, a.s.out_f32, half);
-  if (a.lse && hh == 0 && half == 0) a.lse[((size_t)b * Hq + me.h) * a.T + i] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+  win_store_half<D, H>(a.out, sq.row(i) * Hq + me.h, acc, 1.0f / l, hh, a.s.out_f32, half);
+  if (a.lse && hh == 0 && half == 0) a.lse[sq.lse(me.h, i)] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
 // ---- bf16 gradient ----------------------------------------------------------
@@ -847,8 +946,8 @@ __device__ inline bf16x8 win_pieces(float x) {
   }
   return o;
 }
-template <int D, int H>
-__global__ __launch_bounds__(kWave* kWinWaves* H, 2) void hyb_win_dq_ring_kernel(WindowArgs a, int wgs) {
+template <int D, int H, typename A>
+__global__ __launch_bounds__(kWave* kWinWaves* H, 2) void hyb_win_dq_ring_kernel(A a, int wgs) {
   typedef Mma<bf16> M;
   typedef M::op_t op_t;
   typedef RowColTile<D> WT;
@@ -862,12 +961,10 @@ __global__ __launch_bounds__(kWave* kWinWaves* H, 2) void hyb_win_dq_ring_kernel
   auto& vr = sh.rings.v[half];
   const int li = lane & 31, hh = lane >> 5;
   const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv;
-  int bg, x;
-  win_place(blockIdx.x, a.s.B * Hkv, bg, x);
-  x = wgs - 1 - x;  // the longest first
-  const int b = bg / Hkv, g = bg % Hkv;
-  const int len = win_len(a, b);
-  const WinUnit me = win_unit(a, len, b, g, x * kWinWaves + w);
+  int g, x;
+  const WinSeq<A> sq = win_of_queries(a, wgs, lane, g, x);
+  const int len = sq.len;
+  const WinUnit me = win_unit(a, len, g, x * kWinWaves + w);
   const int first = x * kWinWaves / G * kTile, last = min(((x + 1) * kWinWaves - 1) / G * kTile + kTile, len);
   f32x16 acc[NCT];
 #pragma unroll
@@ -875,8 +972,8 @@ __global__ __launch_bounds__(kWave* kWinWaves* H, 2) void hyb_win_dq_ring_kernel
   const int row = me.i0 + li;
   // The statistics of row i, a half in each of its lanes; zero past the length.
   const auto put_stats = [&](float e, float s) __attribute__((always_inline)) {
-    if (me.i0 < a.T && half == 0)
-      reinterpret_cast<bf16x8*>(a.ws)[(((size_t)b * Hq + me.h) * win_tp(a.T) + row) * 2 + hh] =
+    if (me.i0 < sq.cap && half == 0)
+      reinterpret_cast<bf16x8*>(a.ws)[sq.stats(me.h, row) * 2 + hh] =
           win_pieces(row < len ? (hh == 0 ? e : s) : 0.0f);
   };
   if (first >= len) put_stats(0.0f, 0.0f);
@@ -884,19 +981,20 @@ __global__ __launch_bounds__(kWave* kWinWaves* H, 2) void hyb_win_dq_ring_kernel
     const WinTiles tl(a, len, first, last, kTile);
     const int ntiles = (tl.n + H - 1) / H;
     auto key = [&](int n) __attribute__((always_inline)) { return tl.first(min(H * n + half, tl.n - 1), kTile); };
-    const size_t qs = (size_t)Hq * D, ks_ = (size_t)Hkv * D;
-    const bf16* K = (const bf16*)a.k + ((size_t)b * a.T * Hkv + g) * D;
-    const bf16* V = (const bf16*)a.v + ((size_t)b * a.T * Hkv + g) * D;
+    const size_t qs = sq.qs(D), ks_ = sq.ks(D), vs_ = sq.vs(D);
+    const bf16* K = (const bf16*)a.k + sq.k(g, D);
+    const bf16* V = (const bf16*)a.v + sq.v(g, D);
     const int i = min(row, len - 1);
     const WinRow mine(a, len, i), r0(a, len, min(me.i0, len - 1)), r1(a, len, min(me.i0 + kTile, len) - 1);
     const WT wt(lane);
     op_t qop[KD], dop[KD];
     float delta = 0.0f;
     {
-      const size_t at = ((size_t)b * a.T * Hq + me.h) * D + i * qs + hh * E;
+      const size_t at = sq.dout(me.h, D) + (size_t)i * Hq * D + hh * E;
+      const bf16* qrow = (const bf16*)a.q + sq.q(me.h, D) + i * qs + hh * E;
 #pragma unroll
       for (int ks = 0; ks < KD; ++ks) {
-        qop[ks] = load_op<bf16>((const bf16*)a.q + at + ks * KW);
+        qop[ks] = load_op<bf16>(qrow + ks * KW);
         dop[ks] = load_op<bf16>((const bf16*)a.dout + at + ks * KW);
       }
 #pragma unroll
@@ -908,7 +1006,7 @@ __global__ __launch_bounds__(kWave* kWinWaves* H, 2) void hyb_win_dq_ring_kernel
       delta += xor32(delta);
     }
     const float scale = kLog2e / sqrtf((float)D);
-    const float nat = a.lse[((size_t)b * Hq + me.h) * a.T + i], lse = nat * kLog2e;
+    const float nat = a.lse[sq.lse(me.h, i)], lse = nat * kLog2e;
     put_stats(nat * sqrtf((float)D), delta);
 
     int trow[IPW], tcol[IPW];
@@ -922,13 +1020,14 @@ __global__ __launch_bounds__(kWave* kWinWaves* H, 2) void hyb_win_dq_ring_kernel
       const bool isk = w < kWinWaves / 2;
       bf16* dst = isk ? dk : dv;
       const int j0 = key(n), left = len - 1 - j0;
-      const bf16* base = (isk ? K : V) + (size_t)j0 * ks_;
+      const size_t rs_ = isk ? ks_ : vs_;
+      const bf16* base = (isk ? K : V) + (size_t)j0 * rs_;
       const __amdgpu_buffer_rsrc_t rs =
-          __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(base), 0, (int)(kTile * ks_ * sizeof(bf16)), kBufferWord3);
+          __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(base), 0, (int)(kTile * rs_ * sizeof(bf16)), kBufferWord3);
 #pragma unroll
       for (int u = 0; u < IPW; ++u)
         buf_to_lds16(rs, dst + (w * IPW + u) % WT::IK * WT::RPI * D,
-                     (int)((min(trow[u], left) * (int)ks_ + tcol[u]) * sizeof(bf16)), 0);
+                     (int)((min(trow[u], left) * (int)rs_ + tcol[u]) * sizeof(bf16)), 0);
     };
     f32x16 sc, dp;
     // Scores and dP of tile n, masked.
@@ -1013,8 +1112,8 @@ __global__ __launch_bounds__(kWave* kWinWaves* H, 2) void hyb_win_dq_ring_kernel
         sh.join.template take<1>(w, lane, acc, 1.0f, 1.0f);
     }
   }
-  if (row >= a.T) return;  // rows past the length: zero
-  win_store_half<D, H>(a.dq, ((size_t)b * a.T + row) * Hq + me.h, acc, row < len ? 1.0f / sqrtf((float)D) : 0.0f, hh,
+  if (row >= sq.cap) return;  // rows past the length: zero
+  win_store_half<D, H>(a.dq, sq.row(row) * Hq + me.h, acc, row < len ? 1.0f / sqrtf((float)D) : 0.0f, hh,
                        a.s.out_f32, half);
 }
 
@@ -1023,8 +1122,8 @@ __global__ __launch_bounds__(kWave* kWinWaves* H, 2) void hyb_win_dq_ring_kernel
 // end: at d = 128, so that two waves share a SIMD with the LDS of one workgroup (dK and
 // dV take 128 registers, K 32, the scores and dP 32; V is read from LDS); at d = 64, where
 // three workgroups of four waves fit a CU, where there are fewer (win_cut).
-template <int D, int H>
-__global__ __launch_bounds__(kWave * 4 * H, 2) void hyb_win_dkv_ring_kernel(WindowArgs a, WinParts cut) {
+template <int D, int H, typename A>
+__global__ __launch_bounds__(kWave * 4 * H, 2) void hyb_win_dkv_ring_kernel(A a, WinParts cut) {
   typedef Mma<bf16> M;
   typedef M::op_t op_t;
   typedef RowColTile<D> WT;
@@ -1051,18 +1150,17 @@ __global__ __launch_bounds__(kWave * 4 * H, 2) void hyb_win_dkv_ring_kernel(Wind
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int half = wave >> 2, w = wave & 3;
   const int li = lane & 31, hh = lane >> 5;
-  const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv, Tp = win_tp(a.T);
-  int bg, x;
-  win_place(blockIdx.x, a.s.B * Hkv, bg, x);  // the longest (first keys) first
-  const WinItem it(a, cut, x);
-  const int b = bg / Hkv, g = bg % Hkv;
-  const int len = win_len(a, b);
+  const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv;
+  int g;
+  WinItem it;
+  const WinSeq<A> sq = win_of_keys(a, cut, lane, g, it);
+  const int len = sq.len;
   const int w0 = it.x * kWinKeys, j0 = w0 + w * kTile, j = j0 + li;
   f32x16 acc[2][NCT];  // dK, dV
 #pragma unroll
   for (int ct = 0; ct < NCT; ++ct) acc[0][ct] = acc[1][ct] = f32x16{};
   if (w0 < len) {  // uniform
-    const size_t qs = (size_t)Hq * D, ks_ = (size_t)Hkv * D;
+    const size_t qs = sq.qs(D), ks_ = sq.ks(D), vs_ = sq.vs(D);
     // query tiles t0 .. t0 + nq - 1 of every head, of which this part takes
     // ntiles from first on, a half every H-th
     const WinQueries all(a, len, w0, min(w0 + kWinKeys, len));
@@ -1079,7 +1177,7 @@ __global__ __launch_bounds__(kWave * 4 * H, 2) void hyb_win_dkv_ring_kernel(Wind
 #pragma unroll
     for (int u = 0; u < WT::IK / H; ++u) {
       const int c = u * 4 + w, t = 4 / H * half + c / WT::IK, r = c % WT::IK * WT::RPI + lane / WT::CPR;
-      const bf16* src = (const bf16*)a.v + ((size_t)b * a.T * Hkv + g) * D + min(w0 + t * kTile + r, len - 1) * ks_ +
+      const bf16* src = (const bf16*)a.v + sq.v(g, D) + min(w0 + t * kTile + r, len - 1) * vs_ +
                         (lane % WT::CPR ^ WT::swz(r)) * WT::EPC;
       __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
                                        (__attribute__((address_space(3))) void*)(sh.loop.v[t] + c % WT::IK * WT::RPI * D),
@@ -1087,7 +1185,7 @@ __global__ __launch_bounds__(kWave * 4 * H, 2) void hyb_win_dkv_ring_kernel(Wind
     }
     op_t kop[KD];
     {
-      const size_t at = ((size_t)b * a.T * Hkv + g) * D + min(j, len - 1) * ks_ + hh * E;
+      const size_t at = sq.k(g, D) + min(j, len - 1) * ks_ + hh * E;
 #pragma unroll
       for (int ks = 0; ks < KD; ++ks) kop[ks] = load_op<bf16>((const bf16*)a.k + at + ks * KW);
     }
@@ -1111,15 +1209,16 @@ __global__ __launch_bounds__(kWave * 4 * H, 2) void hyb_win_dkv_ring_kernel(Wind
       if (n >= mysteps) return;
       const int i0 = (t0 + inq) * kTile, left = len - 1 - i0;
       const bool isq = w < 2;
-      const bf16* base = (const bf16*)(isq ? a.q : a.dout) + ((size_t)b * a.T * Hq + inh) * D + (size_t)i0 * qs;
+      const size_t rs_ = isq ? qs : (size_t)Hq * D;
+      const bf16* base = (const bf16*)(isq ? a.q : a.dout) + (isq ? sq.q(inh, D) : sq.dout(inh, D)) + (size_t)i0 * rs_;
       const __amdgpu_buffer_rsrc_t rs =
-          __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(base), 0, (int)(kTile * qs * sizeof(bf16)), kBufferWord3);
+          __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(base), 0, (int)(kTile * rs_ * sizeof(bf16)), kBufferWord3);
       bf16* dst = isq ? s.q : s.d;
 #pragma unroll
       for (int u = 0; u < IPQ; ++u)
         buf_to_lds16(rs, dst + (w * IPQ + u) % WT::IK * WT::RPI * D,
-                     (int)((min(trow[u], left) * (int)qs + tcol[u]) * sizeof(bf16)), 0);
-      const float* st = (const float*)a.ws + (((size_t)b * Hq + inh) * Tp + i0) * 8 + w * kWave + lane;
+                     (int)((min(trow[u], left) * (int)rs_ + tcol[u]) * sizeof(bf16)), 0);
+      const float* st = (const float*)a.ws + sq.stats(inh, i0) * 8 + w * kWave + lane;
       __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)st,
                                        (__attribute__((address_space(3))) void*)((float*)s.st + w * kWave), 4, 0, 0);
       inq += H;
@@ -1207,8 +1306,8 @@ __global__ __launch_bounds__(kWave * 4 * H, 2) void hyb_win_dkv_ring_kernel(Wind
             }
     }
   }
-  if (j >= a.T) return;
-  const size_t row = ((size_t)b * a.T + j) * Hkv + g;
+  if (j >= sq.cap) return;
+  const size_t row = sq.row(j) * Hkv + g;
 #pragma unroll
   for (int o = 0; o < 2; ++o)
     if (H == 1 || o == half) {
@@ -1216,7 +1315,7 @@ __global__ __launch_bounds__(kWave * 4 * H, 2) void hyb_win_dkv_ring_kernel(Wind
       if (it.parts == 1)
         win_store<bf16, D>(o == 0 ? a.dk : a.dv, row, acc[o], f, hh, a.s.out_f32);
       else
-        win_store<bf16, D>(it.sums<D>(a, cut), it.row(a, o, b, j, g), acc[o], f, hh, true);
+        win_store<bf16, D>(it.sums<D>(a, cut), it.row(sq, o, j, g), acc[o], f, hh, true);
     }
 }
 
@@ -1258,30 +1357,53 @@ static bool win_halves(const WindowArgs& a, int n) {
   return n <= 512 && seen >= 32 * kTile;
 }
 
-template <int D>
-static hipError_t win_ring_go(const WindowArgs& a, hipStream_t st) {
-  const int wgs = win_wgs(a), n = a.s.B * a.s.Hkv * wgs;
-  if (win_halves(a, n))
-    hipLaunchKernelGGL((hyb_win_ring_kernel<D, 2>), dim3((unsigned)n), dim3(kWave * kWinWaves * 2), 0, st, a, wgs);
+// The grids of the queries' and keys' workgroups: `wgs` and `keys` per (request, KV head), or
+// packed per KV head; `busy` of the queries' are at work.
+template <typename A>
+struct WinGrid;
+template <>
+struct WinGrid<WindowArgs> {
+  int wgs, n, busy, heads;
+  explicit WinGrid(const WindowArgs& a) : wgs(win_wgs(a)), n(a.s.B * a.s.Hkv * wgs), busy(n), heads(a.s.B * a.s.Hkv) {}
+  int items(const WindowArgs&, const WinParts& cut) const { return cut.items(); }
+};
+template <>
+struct WinGrid<PackedArgs> {
+  int wgs, n, busy, heads;
+  explicit WinGrid(const PackedArgs& a) : heads(a.s.Hkv) {
+    wgs = (int)win_packed_queries(a.N, a.s.B + 1, a.s.Hq / a.s.Hkv);
+    n = wgs * heads;
+    busy = (int)std::min<long>(n, (long)a.N * a.s.Hq / (kWinWaves * kTile));
+  }
+  int items(const PackedArgs& a, const WinParts& cut) const { return (int)win_packed_keys(a.N, a.s.B + 1) * cut.p; }
+};
+
+template <int D, typename A>
+static hipError_t win_ring_go(const A& a, hipStream_t st) {
+  const WinGrid<A> gr(a);
+  const dim3 grid((unsigned)gr.n);
+  if (win_halves(a, gr.busy))
+    hipLaunchKernelGGL((hyb_win_ring_kernel<D, 2, A>), grid, dim3(kWave * kWinWaves * 2), 0, st, a, gr.wgs);
   else
-    hipLaunchKernelGGL((hyb_win_ring_kernel<D, 1>), dim3((unsigned)n), dim3(kWave * kWinWaves), 0, st, a, wgs);
+    hipLaunchKernelGGL((hyb_win_ring_kernel<D, 1, A>), grid, dim3(kWave * kWinWaves), 0, st, a, gr.wgs);
   return hipGetLastError();
 }
 
-template <int D>
-static hipError_t win_prefill_f32_go(const WindowArgs& a, hipStream_t st) {
-  const int wgs = win_wgs(a), n = a.s.B * a.s.Hkv * wgs;
+template <int D, typename A>
+static hipError_t win_prefill_f32_go(const A& a, hipStream_t st) {
+  const WinGrid<A> gr(a);
+  const dim3 grid((unsigned)gr.n);
   // Two halves at d = 128, where one workgroup fits a CU either way (8 x 4096 tokens,
   // 16 heads, window 500, 1404 us with one, now 1300; 1 x 1024, 159 and 144), and at
   // d = 64, where three of one half fit, while workgroups are few (1 x 3000 tokens, 192
   // of them, 260 and 215; 2 x 2048, 512, 231 and 165; of 4096 616, and 684 in halves).
   bool halves = true;
   if constexpr (D == 64) {
-    halves = n <= 512;
-    if (!halves) hipLaunchKernelGGL((hyb_win_fwd_kernel<D, 1>), dim3((unsigned)n), dim3(kWave * kWinWaves), 0, st, a, wgs);
+    halves = gr.busy <= 512;
+    if (!halves) hipLaunchKernelGGL((hyb_win_fwd_kernel<D, 1, A>), grid, dim3(kWave * kWinWaves), 0, st, a, gr.wgs);
   }
   if (halves)
-    hipLaunchKernelGGL((hyb_win_fwd_kernel<D, 2>), dim3((unsigned)n), dim3(kWave * kWinWaves * 2), 0, st, a, wgs);
+    hipLaunchKernelGGL((hyb_win_fwd_kernel<D, 2, A>), grid, dim3(kWave * kWinWaves * 2), 0, st, a, gr.wgs);
   return hipGetLastError();
 }
 
@@ -1347,6 +1469,40 @@ static size_t win_sums_bytes(const Shape& s, int T) {
   return (size_t)(tiles * kWinKeys + (p > 1 ? (long)p * T : 0)) * 2 * s.B * s.Hkv * s.D * sizeof(float);
 }
 
+// The gradient's kernels but the last.
+template <typename T, int D, typename A>
+static void win_backward_kernels(const A& a, const WinParts& cut, hipStream_t st) {
+  const WinGrid<A> gr(a);
+  const dim3 gq((unsigned)gr.n), gk((unsigned)(gr.heads * gr.items(a, cut)));
+  if constexpr (sizeof(T) == 2) {
+    // (dQ in halves at d = 64 only, 1 x 4096 tokens as above 139 and 114 us with dK, dV;
+    // at d = 128 two halves need more registers than there are, and were no faster)
+    bool halves = false;
+    if constexpr (D == 64) {
+      halves = win_halves(a, gr.busy);
+      if (halves) hipLaunchKernelGGL((hyb_win_dq_ring_kernel<D, 2, A>), gq, dim3(kWave * kWinWaves * 2), 0, st, a, gr.wgs);
+    }
+    if (!halves) hipLaunchKernelGGL((hyb_win_dq_ring_kernel<D, 1, A>), gq, dim3(kWave * kWinWaves), 0, st, a, gr.wgs);
+    if constexpr (D == 64) {
+      if (!cut.halves) hipLaunchKernelGGL((hyb_win_dkv_ring_kernel<D, 1, A>), gk, dim3(kWave * 4), 0, st, a, cut);
+    }
+    if (D == 128 || cut.halves) hipLaunchKernelGGL((hyb_win_dkv_ring_kernel<D, 2, A>), gk, dim3(kWave * 8), 0, st, a, cut);
+  } else {
+    hipLaunchKernelGGL((hyb_win_dq_kernel<D, A>), gq, dim3(kWave * kWinWaves), 0, st, a, gr.wgs);
+    hipLaunchKernelGGL((hyb_win_dkv_kernel<D, A>), gk, dim3(kWave * kWinWaves), 0, st, a, cut);
+  }
+}
+// The sums of the parts of keys 0 .. end - 1 of every sequence.
+template <typename T, int D>
+static hipError_t win_backward_sums(const WindowArgs& a, const WinParts& cut, int end, hipStream_t st) {
+  if (end > 0) {
+    const long n = (long)a.s.B * end * a.s.Hkv * D / 2;
+    hipLaunchKernelGGL((hyb_win_sum_kernel<T, D>), dim3((unsigned)std::min<long>((n + 255) / 256, 4096)), dim3(256), 0,
+                       st, a, cut, end);
+  }
+  return hipGetLastError();
+}
+
 template <typename T, int D>
 static hipError_t win_backward_go(WindowArgs a, hipStream_t st) {
   const WinParts cut = win_cut(a.s, a.T, a.window, a.n_sinks);
@@ -1354,32 +1510,8 @@ static hipError_t win_backward_go(WindowArgs a, hipStream_t st) {
   // (what the workspace was sized for, whatever window and n_sinks are)
   if ((size_t)cut.rows(a.T) * 2 * a.s.B * a.s.Hkv * D * sizeof(float) > win_sums_bytes(a.s, a.T))
     return hipErrorInvalidValue;
-  const int wgs = win_wgs(a);
-  const dim3 gq((unsigned)(a.s.B * a.s.Hkv * wgs)), gk((unsigned)(a.s.B * a.s.Hkv * cut.items()));
-  if constexpr (sizeof(T) == 2) {
-    // (dQ in halves at d = 64 only, 1 x 4096 tokens as above 139 and 114 us with dK, dV;
-    // at d = 128 two halves need more registers than there are, and were no faster)
-    bool halves = false;
-    if constexpr (D == 64) {
-      halves = win_halves(a, a.s.B * a.s.Hkv * wgs);
-      if (halves) hipLaunchKernelGGL((hyb_win_dq_ring_kernel<D, 2>), gq, dim3(kWave * kWinWaves * 2), 0, st, a, wgs);
-    }
-    if (!halves) hipLaunchKernelGGL((hyb_win_dq_ring_kernel<D, 1>), gq, dim3(kWave * kWinWaves), 0, st, a, wgs);
-    if constexpr (D == 64) {
-      if (!cut.halves) hipLaunchKernelGGL((hyb_win_dkv_ring_kernel<D, 1>), gk, dim3(kWave * 4), 0, st, a, cut);
-    }
-    if (D == 128 || cut.halves) hipLaunchKernelGGL((hyb_win_dkv_ring_kernel<D, 2>), gk, dim3(kWave * 8), 0, st, a, cut);
-  } else {
-    hipLaunchKernelGGL(hyb_win_dq_kernel<D>, gq, dim3(kWave * kWinWaves), 0, st, a, wgs);
-    hipLaunchKernelGGL(hyb_win_dkv_kernel<D>, gk, dim3(kWave * kWinWaves), 0, st, a, cut);
-  }
-  const int end = cut.p > 1 ? a.T : cut.ps > 1 ? std::min(cut.ns * kWinKeys, a.T) : 0;
-  if (end > 0) {
-    const long n = (long)a.s.B * end * a.s.Hkv * D / 2;
-    hipLaunchKernelGGL((hyb_win_sum_kernel<T, D>), dim3((unsigned)std::min<long>((n + 255) / 256, 4096)), dim3(256), 0,
-                       st, a, cut, end);
-  }
-  return hipGetLastError();
+  win_backward_kernels<T, D>(a, cut, st);
+  return win_backward_sums<T, D>(a, cut, cut.p > 1 ? a.T : cut.ps > 1 ? std::min(cut.ns * kWinKeys, a.T) : 0, st);
 }
 
 hipError_t launch_window_prefill(const WindowArgs& a, hipStream_t st) {
@@ -1390,6 +1522,56 @@ hipError_t launch_window_prefill(const WindowArgs& a, hipStream_t st) {
 hipError_t launch_window_backward(const WindowArgs& a, hipStream_t st) {
   if (a.s.dtype == 1) return a.s.D == 64 ? win_backward_go<bf16, 64>(a, st) : win_backward_go<bf16, 128>(a, st);
   return a.s.D == 64 ? win_backward_go<float, 64>(a, st) : win_backward_go<float, 128>(a, st);
+}
+
+// ---- packed sequences ---------------------------------------------------------
+
+// Mean length, for the choices that the host makes.
+static int packed_mean(const Shape& s, int N) { return std::max(1, (N + s.B - 1) / s.B); }
+static size_t packed_stats_bytes(const Shape& s, int N) {
+  if (s.dtype != 1) return ((size_t)s.Hq * N * sizeof(float) + 255) / 256 * 256;
+  return (size_t)s.Hq * win_packed_tiles(N, s.B + 1) * kTile * 32;
+}
+static size_t packed_sums_bytes(const Shape& s, int N, int parts) {
+  return parts > 1 ? (size_t)parts * N * 2 * s.Hkv * s.D * sizeof(float) : 0;
+}
+
+template <typename T, int D>
+static hipError_t packed_backward_go(PackedArgs a, hipStream_t st) {
+  const int most = win_most_parts(a.s, a.T);
+  WinParts cut = win_cut(a.s, a.T, a.window, 0);
+  cut.p = std::min(cut.p, most);
+  cut.ns = 0;
+  a.sums = (float*)((char*)a.ws + packed_stats_bytes(a.s, a.N));
+  win_backward_kernels<T, D>(a, cut, st);
+  WindowArgs rows = a;  // as one sequence of all rows
+  rows.s.B = 1;
+  rows.T = a.N;
+  return win_backward_sums<T, D>(rows, cut, cut.p > 1 ? a.N : 0, st);
+}
+
+hipError_t launch_packed_prefill(const PackedArgs& a_, hipStream_t st) {
+  PackedArgs a = a_;
+  a.T = packed_mean(a.s, a.N);
+  if (a.s.dtype == 1) return a.s.D == 64 ? win_ring_go<64>(a, st) : win_ring_go<128>(a, st);
+  return a.s.D == 64 ? win_prefill_f32_go<64>(a, st) : win_prefill_f32_go<128>(a, st);
+}
+
+hipError_t launch_packed_backward(const PackedArgs& a_, hipStream_t st) {
+  PackedArgs a = a_;
+  a.T = packed_mean(a.s, a.N);
+  if (a.s.dtype == 1) return a.s.D == 64 ? packed_backward_go<bf16, 64>(a, st) : packed_backward_go<bf16, 128>(a, st);
+  return a.s.D == 64 ? packed_backward_go<float, 64>(a, st) : packed_backward_go<float, 128>(a, st);
+}
+
+double packed_threads(const Shape& s, int N) {
+  const double queries = (double)win_packed_queries(N, s.B + 1, s.Hq / s.Hkv);
+  const double keys = (double)win_packed_keys(N, s.B + 1) * win_most_parts(s, packed_mean(s, N));
+  return kWave * kWinWaves * 2.0 * s.Hkv * std::max(queries, keys);
+}
+
+size_t packed_backward_ws_bytes(const Shape& s, int N) {
+  return packed_stats_bytes(s, N) + packed_sums_bytes(s, N, win_most_parts(s, packed_mean(s, N)));
 }
 
 // Threads of the largest launch (the grid's limit is checked by the caller): a

@@ -113,3 +113,44 @@ def test_binding_takes_device_tensors():
         hb.kv_pages_q8_read(p, p, s, s, i[None], i, i, tokens=4)
     with pytest.raises(TypeError):
         hb.softmax_window_step_paged_q8(k[None], k[None], k[None], p, p, s, s, i[None], i, 5)
+
+
+def packed(d=None, tokens=40, window=10, sinks=2, strides=(0, 0, 0)):
+    # dims tokens window sinks q k v qs ks vs token_start out lse
+    return Call("softmax_packed_prefill", [d or dims(), tokens, window, sinks] + [A(i) for i in range(3)] + list(strides)
+                + [A(3), A(4), A(5), None], [4, 5, 6, 10, 11, 12], (12,))
+
+
+def packed_gradient(d=None, tokens=40, window=10, sinks=2, strides=(0, 0, 0)):
+    # dims tokens window sinks q k v qs ks vs token_start out lse dout dq dk dv ws bytes
+    return Call("softmax_packed_backward", [d or dims(), tokens, window, sinks] + [A(i) for i in range(3)] + list(strides)
+                + [A(3), A(4), A(5), A(6), A(7), A(8), A(9), A(10), 1 << 26, None],
+                [4, 5, 6, 10, 11, 12, 13, 14, 15, 16])
+
+
+@pytest.mark.parametrize("make", [packed, packed_gradient])
+def test_packed_refusals(make):
+    for kw, code in ((dict(tokens=-1), 2), (dict(tokens=(1 << 30) + 1), 2), (dict(window=-1), 2), (dict(sinks=-1), 2),
+                     (dict(strides=(2040, 0, 0)), 2), (dict(strides=(0, 8, 0)), 2), (dict(strides=(0, 0, -512)), 2),
+                     (dict(strides=(2052, 0, 0)), 3), (dict(strides=(0, 0, 1 << 25)), 2)):
+        assert make(**kw)() == code and hb.last_error(), kw
+    for kw, code in ((dict(batch=-1), 2), (dict(head_dim=32), 5), (dict(block=33), 5), (dict(dtype=7), 4), (dict(flags=2), 2),
+                     (dict(n_q_heads=15), 2), (dict(n_q_heads=1 << 17, n_kv_heads=1 << 17), 5)):
+        assert make(dims(**kw))() == code and hb.last_error(), kw
+    assert make(dims(n_q_heads=65536, n_kv_heads=65536), tokens=1 << 30)() == 2  # the grid's limit
+    c = make()
+    assert c.fn(None, *c.args[1:]) == 1
+    c.check_pointers()
+    nothing = make(dims(batch=0))
+    assert nothing() == 0 and make(tokens=0)() == 0
+
+
+def test_packed_overlaps():
+    packed().check_overlaps([11, 12], [4, 5, 6, 10])
+    c = packed_gradient()
+    c.check_overlaps([14, 15, 16, 17], [4, 5, 6, 10, 11, 12, 13])
+    need = hb.workspace_bytes(dims(), hb.OP_PACKED_BACKWARD, 40)
+    assert need > 0 and c(17, None) == 6 and c(18, need - 1) == 6 and c(17, ODD) == 3
+    for bad in (dims(head_dim=5), dims(batch=0)):
+        assert hb.workspace_bytes(bad, hb.OP_PACKED_BACKWARD, 100) == 0
+    assert hb.workspace_bytes(dims(), hb.OP_PACKED_BACKWARD, 0) == 0
