@@ -171,6 +171,24 @@ template <int WIN>
 __device__ inline SpPlan sp_plan(const SoftmaxPrefixArgs& a, const SpCut& cut, int* tiles) {
   const int B = a.s.B, tid = threadIdx.x;
   if (a.n_split == 1) return SpPlan{1 << 24, true};
+  if constexpr (WIN == 2) {
+    // An even share of all tiles for B (n_split - 1) ranges, so that the requests'
+    // ranges, each rounded up, are at most B n_split; every wave works it out.
+    long sum = 0;
+    int most = 0;
+    for (int b = tid % kWave; b < B; b += kWave) {
+      const int nt = sp_tiles<WIN>(a, b);
+      sum += nt;
+      most = max(most, nt);
+    }
+    // (in two pieces: 2^31 tokens of each of many requests)
+    const long total = ((long)__builtin_amdgcn_readfirstlane(wave_all((int)(sum >> 24), AddOp{})) << 24) +
+                       __builtin_amdgcn_readfirstlane(wave_all((int)(sum & 0xffffff), AddOp{}));
+    most = __builtin_amdgcn_readfirstlane(wave_all(most, MaxOp{}));
+    const int share = cut.limit - B;
+    const int c = (int)min(max((total + share - 1) / share, 1L), (long)kMaxRange / kTile);
+    return SpPlan{c, most <= c};
+  }
   if (cut.c > 0) return SpPlan{cut.c, false};
   if (tid < kWave) {
     int total = 0, most = 0;

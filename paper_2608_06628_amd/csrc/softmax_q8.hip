@@ -108,9 +108,15 @@ struct Q8Tiles {
   // Whether keys j0 .. j0 + 31 are all cached and seen.
   __device__ inline bool whole(int j0) const { return j0 + kTile <= P && !seen.cuts(j0); }
   __device__ inline bool sees(int j) const { return j < P && !seen.hides(j); }
-  // K (kv = 0) or V of the tile at j0 into dst; 16 bytes per lane and copy.  Rows that
-  // are not seen read one of the tile that is: their weights are zero, and what they
-  // hold may be anything.
+  // Row t of the tile at j0, or, where that is not seen, one of the tile that is: its
+  // weight is zero, and what the row holds may be anything.
+  __device__ inline int row(int j0, int t, bool all) const {
+    if (all) return t;  // uniform
+    int j = min(j0 + t, P - 1);
+    if (seen.hides(j)) j = seen.he < min(j0 + kTile, P) ? seen.he : seen.hs - 1;
+    return j - j0;
+  }
+  // K (kv = 0) or V of the tile at j0 into dst; 16 bytes per lane and copy.
   __device__ inline void copy(int kv, int j0, uint8_t* dst, int lane) const {
     const size_t row0 = ((size_t)__builtin_amdgcn_readfirstlane(page(j0)) << page_shift) + (j0 & ((1 << page_shift) - 1));
     const uint8_t* base = (kv == 0 ? kc : vc) + row0 * stride;
@@ -121,13 +127,7 @@ struct Q8Tiles {
     for (int u = 0; u < QT::IK; ++u) {
       const int t = u * QT::RPI + lane / QT::CPR;
       const int c = lane % QT::CPR ^ (kv == 0 ? QT::kswz(t) : QT::vswz(t));
-      int r = t;
-      if (!all) {
-        r = min(j0 + t, P - 1);
-        if (seen.hides(r)) r = seen.he < min(j0 + kTile, P) ? seen.he : seen.hs - 1;
-        r -= j0;
-      }
-      buf_to_lds16(rs, dst + u * QT::RPI * D, r * stride + c * 16, 0);
+      buf_to_lds16(rs, dst + u * QT::RPI * D, row(j0, t, all) * stride + c * 16, 0);
     }
   }
 };
@@ -150,26 +150,33 @@ struct Q8Acc {
 #pragma unroll
     for (int ct = 0; ct < NCT; ++ct) acc[ct] = f32x16{};
   }
-  // Scores (K Q^T) of a tile of codes, without their scale.
-  __device__ static inline f32x16 scores(const Q8Tile<D>& qt, const uint8_t* kt, const op_t (&qop)[KD]) {
-    f32x16 sc = {};
+  // Scores (K Q^T) of a tile of codes, without their scale, for C tiles of columns.
+  template <int C>
+  __device__ static inline void scores(f32x16 (&sc)[C], const Q8Tile<D>& qt, const uint8_t* kt, const op_t (&qop)[C][KD]) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) sc[c] = f32x16{};
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
-      const uint4 c = qt.row(kt, i);
+      const uint4 x = qt.row(kt, i);
       if constexpr (sizeof(T) == 2) {
-        sc = M::mma(fp8_bf16(c.x, c.y, 1.0f), qop[2 * i], sc);
-        sc = M::mma(fp8_bf16(c.z, c.w, 1.0f), qop[2 * i + 1], sc);
+        const op_t k0 = fp8_bf16(x.x, x.y, 1.0f), k1 = fp8_bf16(x.z, x.w, 1.0f);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          sc[c] = M::mma(k0, qop[c][2 * i], sc[c]);
+          sc[c] = M::mma(k1, qop[c][2 * i + 1], sc[c]);
+        }
       } else {
-        const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const f32x4 k = fp8_f32(w[x], 1.0f);
+        for (int y = 0; y < 4; ++y) {
+          const f32x4 k = fp8_f32(w[y], 1.0f);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sc = M::mma(k[e], qop[16 * i + 4 * x + e], sc);
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int c = 0; c < C; ++c) sc[c] = M::mma(k[e], qop[c][16 * i + 4 * y + e], sc[c]);
         }
       }
     }
-    return sc;
   }
   // Weights of a tile's masked scores (in p), for a scale into the log2 domain.
   __device__ inline void weights(const f32x16& sc, float scale, float (&p)[16]) {
@@ -196,40 +203,54 @@ struct Q8Acc {
     }
     l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
   }
-  // A tile of cached tokens at j0 with its scales' bytes.
-  __device__ inline void add(const Q8Tiles<D>& t, const Q8Tile<D>& qt, int j0, const uint8_t* kt, const uint8_t* vt,
-                             int bytes, const op_t (&qop)[KD], float scale, int hh) {
-    f32x16 sc = scores(qt, kt, qop);
+  // A tile of cached tokens at j0 with its scales' bytes, to C tiles of columns.
+  template <int C>
+  __device__ static inline void add(Q8Acc (&me)[C], const Q8Tiles<D>& t, const Q8Tile<D>& qt, int j0, const uint8_t* kt,
+                                    const uint8_t* vt, int bytes, const op_t (&qop)[C][KD], float scale, int hh) {
+    f32x16 sc[C];
+    scores<C>(sc, qt, kt, qop);
     mma_settle<T>();
     if (!t.whole(j0)) {  // uniform
 #pragma unroll
-      for (int e = 0; e < 16; ++e) sc[e] = t.sees(j0 + row_of(e, hh)) ? sc[e] : -INFINITY;
+      for (int e = 0; e < 16; ++e) {
+        const bool ok = t.sees(j0 + row_of(e, hh));
+#pragma unroll
+        for (int c = 0; c < C; ++c) sc[c][e] = ok ? sc[c][e] : -INFINITY;
+      }
     }
-    float p[16];
-    weights(sc, scale * scale_of(bytes & 255), p);
-    const float fv = scale_of(bytes >> 8);
+    const float fk = scale * scale_of(bytes & 255), fv = scale_of(bytes >> 8);
+    float p[C][16];
+#pragma unroll
+    for (int c = 0; c < C; ++c) me[c].weights(sc[c], fk, p[c]);
     if constexpr (sizeof(T) == 2) {
       // The weights enter P V rounded to bf16 (each off by at most 2^-8 of itself;
       // products of fp32 run at 1/16 of the rate); their sum is over the unrounded ones.
-      op_t pop[KL];
+      op_t pop[C][KL];
 #pragma unroll
-      for (int ks = 0; ks < KL; ++ks) pop[ks] = cvt_op<bf16>(&p[ks * 8]);
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int ks = 0; ks < KL; ++ks) pop[c][ks] = cvt_op<bf16>(&p[c][ks * 8]);
 #pragma unroll
       for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
         for (int ks = 0; ks < KL; ++ks) {
-          const uint2 c = qt.column(vt, ct, ks);
-          acc[ct] = M::mma(fp8_bf16(c.x, c.y, fv), pop[ks], acc[ct]);
+          const uint2 x = qt.column(vt, ct, ks);
+          const op_t v = fp8_bf16(x.x, x.y, fv);
+#pragma unroll
+          for (int c = 0; c < C; ++c) me[c].acc[ct] = M::mma(v, pop[c][ks], me[c].acc[ct]);
         }
     } else {
 #pragma unroll
       for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
-          const uint2 c = qt.column(vt, ct, ks);
-          const f32x4 lo = fp8_f32(c.x, fv), hi = fp8_f32(c.y, fv);
+          const uint2 x = qt.column(vt, ct, ks);
+          const f32x4 lo = fp8_f32(x.x, fv), hi = fp8_f32(x.y, fv);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) acc[ct] = M::mma(e < 4 ? lo[e] : hi[e - 4], p[8 * ks + e], acc[ct]);
+          for (int e = 0; e < 8; ++e)
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+              me[c].acc[ct] = M::mma(e < 4 ? lo[e] : hi[e - 4], p[c][8 * ks + e], me[c].acc[ct]);
         }
     }
   }
@@ -256,11 +277,11 @@ struct Q8Acc {
 // tiles of 32 columns: `groups` of them.
 __host__ __device__ inline int q8_groups(const Shape& s) { return (s.Hq / s.Hkv * s.L + kTile - 1) / kTile; }
 
-// A workgroup answers 32 columns over a range of keys: the four waves take the
+// A workgroup answers C tiles of 32 columns over a range of keys: the four waves take the
 // range's tiles in turn, each through copies of its own (R slots, no barrier in the loop)
 // and sums of its own, joined in LDS at the end.  The codes are converted as they become
-// operands, once each.
-template <typename T, int D>
+// operands, once each for all columns.
+template <typename T, int D, int C>
 __global__ __launch_bounds__(kWave * 4) void hyb_q8_token_kernel(SoftmaxQ8Args a, SpCut cut) {
   typedef Q8Acc<T, D> A;
   typedef Q8Tile<D> QT;
@@ -275,13 +296,13 @@ __global__ __launch_bounds__(kWave * 4) void hyb_q8_token_kernel(SoftmaxQ8Args a
     struct {
       Slot ring[NW][R];
     } loop;
-    f32x4 parts[NW][NCT * 4][kWave];
+    f32x4 parts[NW][C][NCT * 4][kWave];
     int plan[kPlanInts];
     __device__ Smem() {}
   };
   __shared__ alignas(16) Smem sh;
   __shared__ alignas(16) Block blk;
-  __shared__ float refs[NW][kTile], sums[NW][kTile];
+  __shared__ float refs[NW][C][kTile], sums[NW][C][kTile];
   __shared__ int pages[kMaxRangePages];
   __shared__ uint16_t bytes[kMaxRange / kTile + 2];
 
@@ -290,19 +311,24 @@ __global__ __launch_bounds__(kWave * 4) void hyb_q8_token_kernel(SoftmaxQ8Args a
   const int li = lane & 31, hh = lane >> 5;
   const int Hq = a.s.Hq, Hkv = a.s.Hkv, L = a.s.L, G = Hq / Hkv;
   int at, hg;
-  sp_place(q8_groups(a.s), at, hg);
+  sp_place((q8_groups(a.s) + C - 1) / C, at, hg);
   const int g = at % Hkv, r = at / Hkv;
   const SpRange rg = sp_range<2>(a, sp_plan<2>(a, cut, sh.plan), r, lane);
   if (rg.b < 0) return;  // uniform: past the plan's last range
   const int Lb = sp_block<2>(a, rg.b), P = min(max(a.prefix_len[rg.b], 0), a.max_prefix);
-  // this lane's column: query i of head h
-  const int col = hg * kTile + li, hl = col / L, i = col - hl * L, h = g * G + hl;
-  const bool mine = hl < G && i < Lb;
-  typename A::op_t qop[A::KD];
-  {
-    const T* row = (const T*)a.q + (((size_t)rg.b * L + (mine ? i : 0)) * Hq + (mine ? h : g * G)) * D;
+  // this lane's columns: query i of head h
+  int i[C], h[C];
+  bool mine[C];
+  typename A::op_t qop[C][A::KD];
 #pragma unroll
-    for (int ks = 0; ks < A::KD; ++ks) qop[ks] = keep_if<T>(mine, load_op<T>(row + A::entry(ks, hh)));
+  for (int c = 0; c < C; ++c) {
+    const int col = (hg * C + c) * kTile + li, hl = col / L;
+    i[c] = col - hl * L;
+    h[c] = g * G + hl;
+    mine[c] = hl < G && i[c] < Lb;
+    const T* row = (const T*)a.q + (((size_t)rg.b * L + (mine[c] ? i[c] : 0)) * Hq + (mine[c] ? h[c] : g * G)) * D;
+#pragma unroll
+    for (int ks = 0; ks < A::KD; ++ks) qop[c][ks] = keep_if<T>(mine[c], load_op<T>(row + A::entry(ks, hh)));
   }
   const Q8Tiles<D> t(a, rg, g, P, pages);
   const QT qt(lane);
@@ -327,7 +353,7 @@ __global__ __launch_bounds__(kWave * 4) void hyb_q8_token_kernel(SoftmaxQ8Args a
   }
   __syncthreads();  // (the plan's scratch has been read)
   const float scale = kLog2e / sqrtf((float)D);
-  A acc;
+  A acc[C];
 #pragma unroll
   for (int n = 0; n < R - 1; ++n) issue(n, sh.loop.ring[w][n]);
   auto step = [&](int n, auto S) __attribute__((always_inline)) {
@@ -340,7 +366,7 @@ __global__ __launch_bounds__(kWave * 4) void hyb_q8_token_kernel(SoftmaxQ8Args a
     else if (later == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * QT::IK) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     const Slot& s = sh.loop.ring[w][SV];
-    acc.add(t, qt, t.first_key(w + NW * n), s.k, s.v, bytes[w + NW * n], qop, scale, hh);
+    A::template add<C>(acc, t, qt, t.first_key(w + NW * n), s.k, s.v, bytes[w + NW * n], qop, scale, hh);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot is read
   };
   for (int n = 0; n < my; n += R) {
@@ -351,64 +377,440 @@ __global__ __launch_bounds__(kWave * 4) void hyb_q8_token_kernel(SoftmaxQ8Args a
       step(n + 3, std::integral_constant<int, 3>{});
     }
   }
-  if (block && w == nt % NW) acc.add_block(blk.k, blk.v, Lb, qop, scale, li, hh);
+  if (block && w == nt % NW) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) acc[c].add_block(blk.k, blk.v, Lb, qop[c], scale, li, hh);
+  }
 
   // The waves' sums over one reference: wave w scales its own and leaves them in
   // LDS, then joins entries 32 w .. + 31 of every column.
   mma_settle<T>();
-  const float l = acc.l + xor32(acc.l);
-  if (hh == 0) refs[w][li] = acc.m;
-  lds_barrier();  // (and the slots are free)
-  float mm = refs[0][li];
+  float l[C], mm[C], f[C];
 #pragma unroll
-  for (int x = 1; x < NW; ++x) mm = fmaxf(mm, refs[x][li]);
-  const float f = __builtin_amdgcn_exp2f(acc.m - mm);
-  if (hh == 0) sums[w][li] = l * f;
+  for (int c = 0; c < C; ++c) {
+    l[c] = acc[c].l + xor32(acc[c].l);
+    if (hh == 0) refs[w][c][li] = acc[c].m;
+  }
+  lds_barrier();  // (and the slots are free)
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    mm[c] = refs[0][c][li];
+#pragma unroll
+    for (int x = 1; x < NW; ++x) mm[c] = fmaxf(mm[c], refs[x][c][li]);
+    f[c] = __builtin_amdgcn_exp2f(acc[c].m - mm[c]);
+    if (hh == 0) sums[w][c][li] = l[c] * f[c];
+#pragma unroll
+    for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const f32x16& y = acc[c].acc[ct];
+        sh.parts[w][c][ct * 4 + e][lane] = f32x4{y[4 * e] * f[c], y[4 * e + 1] * f[c], y[4 * e + 2] * f[c], y[4 * e + 3] * f[c]};
+      }
+  }
+  lds_barrier();
+  if (w >= NCT) return;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    if (!mine[c]) continue;
+    float den = 0.0f;
+#pragma unroll
+    for (int x = 0; x < NW; ++x) den += sums[x][c][li];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      f32x4 o = {};
+#pragma unroll
+      for (int x = 0; x < NW; ++x) {
+        const f32x4 y = sh.parts[x][c][w * 4 + e][lane];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[k] += y[k];
+      }
+      sp_put<T, D>(a, rg, r, h[c], i[c], w * kTile + row_of(4 * e, hh), o, den);
+    }
+    if (w == 0 && hh == 0) sp_put_sum<D>(a, rg, r, h[c], i[c], mm[c], den);
+  }
+}
+
+// Blocks (bf16; more than 64 columns): a wave answers 32 columns, and the four waves of a
+// half share its tiles; the two halves of a workgroup take the range's tiles in turn and join
+// their sums in LDS.  A tile's codes go through registers, A tiles ahead, and into LDS as
+// bf16 values, scales included, so that each is converted once for four tiles of
+// columns; the tiles are then read as those of a bf16 cache.  Step n forms the scores of tile n + 1 while it
+// takes the weights of tile n (two independent chains, whose MFMAs and VALU instructions
+// interleave), and puts tile n + 2 into the slot of tile n - 1.
+template <int D>
+__global__ __launch_bounds__(kWave * 8, 2) void hyb_q8_block_kernel(SoftmaxQ8Args a, SpCut cut) {
+  typedef Mma<bf16> M;
+  typedef M::op_t op_t;
+  typedef RowColTile<D> RT;
+  constexpr int KD = D / M::KW, KL = kTile / M::KW, NCT = D / kTile, NW = 4, R = 3, A = 3;
+  constexpr int CPR = D / 16, PK = kTile * CPR;          // 16-code pieces of a row, of a tile of K or V
+  constexpr int PT = 2 * PK / (kWave * NW);              // pieces of a thread of the half and tile
+  static_assert(PT >= 1 && PK % kWave == 0, "a wave's pieces are all of K or of V");
+  struct alignas(16) Slot {
+    bf16 x[2][kTile * D];
+  };
+  constexpr int NH = NCT / 2;  // groups of 32 entries that a half joins
+  union Smem {
+    Slot ring[2][R];
+    f32x4 parts[2][NW][NH * 4][kWave];  // [for half]
+    int plan[kPlanInts];
+    __device__ Smem() {}
+  };
+  __shared__ alignas(16) Smem sh;
+  __shared__ float refs[2][NW][kTile], sums[2][NW][kTile];
+  __shared__ int pages[kMaxRangePages];
+  // Of the range's cached tiles, and of one more, hidden whole, behind them: the offset of
+  // their first row in the pools (kPartial in the high word: not all of its rows are seen),
+  // and the bytes of their scales.
+  constexpr uint32_t kPartial = 1u << 31;
+  __shared__ uint2 places[kMaxRange / kTile + 3];
+  __shared__ uint16_t bytes[kMaxRange / kTile + 3];
+
+  const int lane = threadIdx.x & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), half = wave / NW, w = wave % NW;
+  Slot(&ring)[R] = sh.ring[half];
+  const int li = lane & 31, hh = lane >> 5;
+  const int Hq = a.s.Hq, Hkv = a.s.Hkv, L = a.s.L, G = Hq / Hkv;
+  int at, hg;
+  sp_place((q8_groups(a.s) + NW - 1) / NW, at, hg);
+  const int g = at % Hkv, r = at / Hkv;
+  const SpRange rg = sp_range<2>(a, sp_plan<2>(a, cut, sh.plan), r, lane);
+  if (rg.b < 0) return;  // uniform: past the plan's last range
+  const int Lb = sp_block<2>(a, rg.b), P = min(max(a.prefix_len[rg.b], 0), a.max_prefix);
+  const int col = (hg * NW + w) * kTile + li, hl = col / L, i = col - hl * L, h = g * G + hl;
+  const bool mine = hl < G && i < Lb;
+  op_t qop[KD];
+  {
+    const bf16* row = (const bf16*)a.q + (((size_t)rg.b * L + (mine ? i : 0)) * Hq + (mine ? h : g * G)) * D + hh * 8;
+#pragma unroll
+    for (int ks = 0; ks < KD; ++ks) qop[ks] = keep_if<bf16>(mine, load_op<bf16>(row + ks * M::KW));
+  }
+  const Q8Tiles<D> t(a, rg, g, P, pages);
+  const RT rt(lane);
+  // The list: the block's tile first, if it is the range's, then the cached ones, nc of
+  // them; this half's tile n is the list's 2 n + half.  The halves have the same number:
+  // one that is past the list's end takes the hidden one.
+  const int nb = rg.hi > (P + kTile - 1) / kTile * kTile ? 1 : 0, nc = rg.nt - nb, ntiles = (rg.nt + 1) / 2;
+  const bool first_is_block = half < nb;
+  for (int e = threadIdx.x; e <= nc; e += blockDim.x) {
+    const int j0 = t.first_key(max(0, min(e, nc - 1)));
+    const size_t row = ((size_t)t.page(j0) << t.page_shift) + (j0 & ((1 << t.page_shift) - 1));
+    const size_t off = nc > 0 ? row * t.stride : 0;
+    places[e] = uint2{(uint32_t)off, (uint32_t)(off >> 32) | (e == nc || !t.whole(j0) ? kPartial : 0u)};
+    bytes[e] = nc > 0 ? (uint16_t)t.scales(a, g, j0) : 0;
+  }
+  auto entry = [&](int n) __attribute__((always_inline)) { return max(0, min(2 * n + half - nb, nc)); };
+  __syncthreads();  // (the plan's scratch is read, the places are there)
+
+  uint4 next[A][PT];  // codes of tiles on their way
+  int voff[PT], dst0[PT], dst1[PT];  // this thread's pieces: their offsets in a tile in the pools, and in a slot
+  const int kvs = PT > 1 ? 0 : w * kWave / PK;
+#pragma unroll
+  for (int u = 0; u < PT; ++u) {
+    const int y = (u * kWave * NW + w * kWave + lane) % PK, row = y / CPR, c16 = y % CPR;
+    voff[u] = row * t.stride + c16 * 16;
+    dst0[u] = row * D + ((2 * c16) ^ RT::swz(row)) * 8;
+    dst1[u] = row * D + ((2 * c16 + 1) ^ RT::swz(row)) * 8;
+  }
+  auto kind = [&](int u) __attribute__((always_inline)) { return PT > 1 ? u * kWave * NW / PK : kvs; };  // K's or V's
+  // Always as many loads, whatever n is: where some were left out, the compiler, which
+  // counts what is in flight, would wait for all of them.  (Without cached tiles the buffer is
+  // empty, and nothing is loaded.)
+  const int span = nc > 0 ? kTile * t.stride : 0;
+  auto fetch = [&](int n, uint2 place, uint4 (&c)[PT]) __attribute__((always_inline)) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane(place.x), hi = __builtin_amdgcn_readfirstlane(place.y);
+    const size_t off = (size_t)(hi & ~kPartial) << 32 | lo;
+    int at[PT];
+#pragma unroll
+    for (int u = 0; u < PT; ++u) at[u] = voff[u];
+    if (hi & kPartial) {  // uniform; (any row will do for the hidden tile)
+      const int j0 = t.first_key(max(0, min(entry(n), nc - 1)));
+#pragma unroll
+      for (int u = 0; u < PT; ++u) {
+        const int y = (u * kWave * NW + w * kWave + lane) % PK;
+        at[u] = t.row(j0, y / CPR, t.whole(j0)) * t.stride + y % CPR * 16;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < PT; ++u) {
+      const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+          const_cast<uint8_t*>((kind(u) == 0 ? t.kc : t.vc) + off), 0, span, kBufferWord3);
+      c[u] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rs, at[u], 0, 0));
+    }
+  };
+  auto put = [&](int by, const uint4 (&c)[PT], Slot& s) __attribute__((always_inline)) {
+    const int two = __builtin_amdgcn_readfirstlane(by);
+#pragma unroll
+    for (int u = 0; u < PT; ++u) {
+      const float f = scale_of(kind(u) == 0 ? two & 255 : two >> 8);
+      *reinterpret_cast<bf16x8*>(s.x[kind(u)] + dst0[u]) = fp8_bf16(c[u].x, c[u].y, f);
+      *reinterpret_cast<bf16x8*>(s.x[kind(u)] + dst1[u]) = fp8_bf16(c[u].z, c[u].w, f);
+    }
+  };
+  // The block's rows as they are; those past its last are the last again.
+  auto put_block = [&](Slot& s) __attribute__((always_inline)) {
+    for (int x = w * kWave + lane; x < 2 * kTile * D / 8; x += kWave * NW) {
+      const int kv = x / (kTile * D / 8), row = x / (D / 8) % kTile, c8 = x % (D / 8);
+      const bf16* src = (const bf16*)(kv == 0 ? a.k : a.v) + (((size_t)rg.b * L + min(row, Lb - 1)) * Hkv + g) * D + c8 * 8;
+      *reinterpret_cast<bf16x8*>(&s.x[kv][row * D + (c8 ^ RT::swz(row)) * 8]) = load_op<bf16>(src);
+    }
+  };
+
+  const float scale = kLog2e / sqrtf((float)D);
+  float m = -1e30f, l = 0.0f;
+  f32x16 acc[NCT], sc;
+#pragma unroll
+  for (int ct = 0; ct < NCT; ++ct) acc[ct] = f32x16{};
+  auto scores = [&](const Slot& s) __attribute__((always_inline)) {
+    f32x16 x = {};
+#pragma unroll
+    for (int ks = 0; ks < KD; ++ks) x = M::mma(rt.row_op(s.x[0], ks), qop[ks], x);
+    return x;
+  };
+  // Takes the scores of tile n: masks, maximum, reference (which moves only when a
+  // maximum passes it by 2^8).
+  auto take = [&](int n, const f32x16& s, bool partial) __attribute__((always_inline)) {
+    sc = s;
+    if (partial) {  // uniform
+      const bool block = n == 0 && first_is_block, past = !block && entry(n) == nc;
+      const int j0 = block || past ? 0 : t.first_key(entry(n));
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int j = j0 + row_of(e, hh);
+        sc[e] = !past && (block ? j < Lb : t.sees(j)) ? sc[e] : -INFINITY;
+      }
+    }
+    float mt = sc[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) mt = fmaxf(mt, sc[e]);
+    mt = fmaxf(mt, xor32(mt)) * scale;
+    if (__any(mt > m + 8.0f)) {
+      mma_settle<bf16>();
+      const float mn = mt > m + 8.0f ? mt : m;
+      const float corr = __builtin_amdgcn_exp2f(m - mn);
+      l *= corr;
+#pragma unroll
+      for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[ct][e] *= corr;
+      m = mn;
+    }
+  };
+  auto compute = [&](auto lastc, int n, const Slot& sn, const Slot& sv, bool partial, auto stage) __attribute__((always_inline)) {
+    constexpr bool LAST = decltype(lastc)::value;
+    f32x16 x;
+    if constexpr (!LAST) x = scores(sn);
+    stage();
+    float p[16], s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale, -m));
+#pragma unroll
+    for (int e = 0; e < 16; e += 2) {
+      s0 += p[e];
+      s1 += p[e + 1];
+    }
+    l += s0 + s1;
+    op_t pop[KL];  // (the weights rounded to bf16 for P V, their sum over the unrounded ones)
+#pragma unroll
+    for (int ks = 0; ks < KL; ++ks) pop[ks] = cvt_op<bf16>(&p[ks * 8]);
+#pragma unroll
+    for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+      for (int ks = 0; ks < KL; ++ks) acc[ct] = M::mma(rt.col_op(sv.x[1], ct, ks), pop[ks], acc[ct]);
+    if constexpr (!LAST) take(n + 1, x, partial);
+  };
+#pragma unroll
+  for (int n = 0; n < A; ++n) fetch(n, places[entry(n)], next[n]);
+  if (first_is_block)
+    put_block(ring[0]);
+  else
+    put(bytes[entry(0)], next[0], ring[0]);
+  fetch(A, places[entry(A)], next[0]);
+  put(bytes[entry(1)], next[1], ring[1]);
+  fetch(A + 1, places[entry(A + 1)], next[1]);
+  // (what a step takes of a tile as numbers is read a step ahead)
+  uint2 place = places[entry(A + 2)];
+  int by = bytes[entry(2)];
+  uint32_t how = places[entry(1)].y;
+  lds_barrier();
+  {
+    const f32x16 x = scores(ring[0]);
+    mma_settle<bf16>();
+    take(0, x, first_is_block || (__builtin_amdgcn_readfirstlane(places[entry(0)].y) & kPartial));
+  }
+  // (R = A: a tile's registers and slot have the same number)
+  static_assert(R == A, "one index for both");
+  auto step = [&](int n, auto S) __attribute__((always_inline)) {
+    constexpr int SV = decltype(S)::value;
+    const bool partial = __builtin_amdgcn_readfirstlane(how) & kPartial;
+    compute(std::false_type{}, n, ring[(SV + 1) % R], ring[SV], partial, [&]() __attribute__((always_inline)) {
+      // every wave has read tile n - 1, whose slot tile n + 2 takes
+      put(by, next[(SV + 2) % A], ring[(SV + 2) % R]);
+      fetch(n + 2 + A, place, next[(SV + 2) % A]);
+      place = places[entry(n + 3 + A)];
+      by = bytes[entry(n + 3)];
+      how = places[entry(n + 2)].y;
+    });
+    lds_barrier();
+  };
+  int n = 0;
+  for (; n + R < ntiles; n += R) {
+    step(n, std::integral_constant<int, 0>{});
+    step(n + 1, std::integral_constant<int, 1>{});
+    step(n + 2, std::integral_constant<int, 2>{});
+  }
+  if (n + 1 < ntiles) step(n, std::integral_constant<int, 0>{});
+  if (n + 2 < ntiles) step(n + 1, std::integral_constant<int, 1>{});
+  compute(std::true_type{}, ntiles - 1, ring[0], ring[ntiles - 1 - n], false, [] {});
+  // The halves' sums over one reference: each hands over half of the entries and joins
+  // the others.
+  mma_settle<bf16>();
+  l += xor32(l);
+  if (hh == 0) refs[half][w][li] = m;
+  lds_barrier();  // (and the slots are free)
+  const float mm = fmaxf(refs[0][w][li], refs[1][w][li]), f = __builtin_amdgcn_exp2f(m - mm);
+  if (hh == 0) sums[half][w][li] = l * f;
 #pragma unroll
   for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      sh.parts[w][ct * 4 + e][lane] = f32x4{acc.acc[ct][4 * e] * f, acc.acc[ct][4 * e + 1] * f, acc.acc[ct][4 * e + 2] * f,
-                                            acc.acc[ct][4 * e + 3] * f};
+      if (ct / NH != half)
+        sh.parts[ct / NH][w][ct % NH * 4 + e][lane] =
+            f32x4{acc[ct][4 * e] * f, acc[ct][4 * e + 1] * f, acc[ct][4 * e + 2] * f, acc[ct][4 * e + 3] * f};
   lds_barrier();
-  if (w >= NCT || !mine) return;
-  float den = 0.0f;
+  if (!mine) return;
+  const float den = sums[0][w][li] + sums[1][w][li];
 #pragma unroll
-  for (int x = 0; x < NW; ++x) den += sums[x][li];
+  for (int ct = 0; ct < NCT; ++ct)
+    if (ct / NH == half)
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    f32x4 o = {};
+      for (int e = 0; e < 4; ++e) {
+        f32x4 o = sh.parts[half][w][ct % NH * 4 + e][lane];
 #pragma unroll
-    for (int x = 0; x < NW; ++x) {
-      const f32x4 y = sh.parts[x][w * 4 + e][lane];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) o[k] += y[k];
-    }
-    sp_put<T, D>(a, rg, r, h, i, w * kTile + row_of(4 * e, hh), o, den);
-  }
-  if (w == 0 && hh == 0) sp_put_sum<D>(a, rg, r, h, i, mm, den);
+        for (int k = 0; k < 4; ++k) o[k] += acc[ct][4 * e + k] * f;
+        sp_put<bf16, D>(a, rg, r, h, i, ct * kTile + row_of(4 * e, hh), o, den);
+      }
+  if (half == 0 && hh == 0) sp_put_sum<D>(a, rg, r, h, i, mm, den);
 }
 
-int softmax_q8_splits(const Shape& s, int max_seen) { return softmax_prefix_splits(s, max_seen); }
+// Merge of few rows' ranges: a workgroup per row, D / 4 threads per range, as many
+// ranges at once as it has threads for.  (16 rows of 64 ranges: 27.5 us by eight rows per
+// workgroup, one after the other, 4 us so.)
+template <typename T, int D>
+__global__ __launch_bounds__(256) void hyb_q8_combine_kernel(SoftmaxPrefixArgs a, SpCut cut) {
+  constexpr int TPR = D / 4, NG = 256 / TPR;
+  __shared__ alignas(16) int plan[kPlanInts];
+  __shared__ float most[NG], sums[NG];
+  __shared__ f32x4 parts[NG][TPR];
+  const SpPlan p = sp_plan<2>(a, cut, plan);
+  if (p.whole) return;  // every row is already written out
+  const int Hq = a.s.Hq, L = a.s.L, lane = threadIdx.x & (kWave - 1);
+  const int b = blockIdx.x / (Hq * L), h = blockIdx.x / L % Hq, i = blockIdx.x % L;
+  const int n = sp_ranges(p, sp_tiles<2>(a, b));
+  if (n <= 1 || i >= sp_block<2>(a, b)) return;  // uniform
+  int base = 0;
+  for (int b0 = lane; b0 < b; b0 += kWave) base += sp_ranges(p, sp_tiles<2>(a, b0));
+  base = wave_all(base, AddOp{});
+  const int grp = threadIdx.x / TPR, c = threadIdx.x % TPR;
+  const size_t row0 = sp_row(a, base, h, i), step = (size_t)Hq * L;
+  const float* wml = sp_ml<D>(a);
+  float m = -1e30f, den = 0.0f;
+  f32x4 num = {};
+#pragma unroll 4
+  for (int s = grp; s < n; s += NG) {
+    const size_t rr = row0 + s * step;
+    const float2 ml = *reinterpret_cast<const float2*>(wml + rr * 2);
+    const f32x4 x = *reinterpret_cast<const f32x4*>((const float*)a.ws + rr * D + c * 4);
+    const float mn = fmaxf(m, ml.x), f = fast_exp(m - mn), g = fast_exp(ml.x - mn);
+    m = mn;
+    den = den * f + ml.y * g;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) num[e] = num[e] * f + x[e] * g;
+  }
+  if (c == 0) {
+    most[grp] = m;
+    sums[grp] = den;
+  }
+  parts[grp][c] = num;
+  __syncthreads();
+  if (threadIdx.x >= TPR) return;
+  float mm = most[0];
+#pragma unroll
+  for (int x = 1; x < NG; ++x) mm = fmaxf(mm, most[x]);
+  float o[4] = {}, d = 0.0f;
+#pragma unroll
+  for (int x = 0; x < NG; ++x) {
+    const float f = fast_exp(most[x] - mm);
+    d += sums[x] * f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += parts[x][c][e] * f;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] /= d;
+  store_out4<T>(a.out, (((size_t)b * L + i) * Hq + h) * D + c * 4, o, a.s.out_f32);
+}
+
+// Tiles of columns that a workgroup answers (32 columns each), as the kernels above.
+static int q8_columns(const Shape& s) { return s.dtype != 1 ? 1 : q8_groups(s) <= 2 ? q8_groups(s) : 4; }
+// Workgroups of a range and KV head.
+static int q8_wgs(const Shape& s) { return (q8_groups(s) + q8_columns(s) - 1) / q8_columns(s); }
+
+// Into how many ranges requests of max_seen cached tokens are cut: the least estimated
+// time (us).  The chip takes a workgroup per CU at a time; one costs its start and end
+// besides its tiles, and more ranges than one cost a merge.
+static int q8_parts(const Shape& s, int max_seen) {
+  const double tiles = std::ceil(max_seen / 32.0) + 1, wgs = (double)s.B * s.Hkv * q8_wgs(s);
+  const bool block = q8_columns(s) == 4;
+  const double tile = s.dtype != 1 ? 2.0 * s.D / 64 : block ? 0.34 : 0.4, fixed = 6.0;
+  const double rows = (double)s.B * s.Hq * s.L, row = (s.D + 2) * 8 / 4e6;  // a partial row's write and read
+  int best = 1;
+  double least = 0;
+  const int most = (int)std::max(1.0, std::min(tiles / 4, std::ceil(2048.0 / wgs)));
+  for (int k = 1; k <= most; ++k) {
+    const double t = std::ceil(wgs * k / 256) * (tiles / k * tile + fixed) + (k > 1 ? 4.0 + rows * k * row : 0.0);
+    if (k == 1 || t < least * 0.98) {
+      least = t;
+      best = k;
+    }
+  }
+  return best;
+}
+// Ranges per request at most: a plan's ranges are c tiles, an even share of all
+// tiles, so that requests of different lengths have one more than that on average.
+int softmax_q8_splits(const Shape& s, int max_seen) {
+  if (s.B == 0) return 1;
+  const int need = (int)(((long)max_seen + s.L + kMaxRange - 1) / kMaxRange);
+  const int k = q8_parts(s, max_seen);
+  return k == 1 && need <= 1 ? 1 : std::max(k, need) + 1;
+}
 
 template <typename T, int D>
 static hipError_t q8_go(const SoftmaxQ8Args& a, hipStream_t st) {
-  SpCut cut;
-  static const int resident = sp_resident(hyb_q8_token_kernel<T, D>, 4);
-  const hipError_t e = sp_launch(hyb_q8_token_kernel<T, D>, resident, 4, true, a, st, &cut, q8_groups(a.s));
-  if (e != hipSuccess || a.n_split == 1) return e;  // one range: already written out
-  const long units = (long)a.s.B * a.s.Hq * ((a.s.L + 1024 / D - 1) / (1024 / D));
-  hipLaunchKernelGGL((hyb_sp_combine_kernel<T, D, 2>), dim3((unsigned)std::min<long>(units, 2048)), dim3(256), 0, st, a,
-                     cut);
+  const int wgs = q8_wgs(a.s);
+  SpCut cut = {};
+  cut.limit = a.s.B * a.n_split;
+  const dim3 grid((unsigned)(a.s.Hkv * wgs * cut.limit));
+  if constexpr (sizeof(T) == 2) {
+    switch (q8_columns(a.s)) {
+      case 1: hipLaunchKernelGGL((hyb_q8_token_kernel<T, D, 1>), grid, dim3(kWave * 4), 0, st, a, cut); break;
+      case 2: hipLaunchKernelGGL((hyb_q8_token_kernel<T, D, 2>), grid, dim3(kWave * 4), 0, st, a, cut); break;
+      default: hipLaunchKernelGGL((hyb_q8_block_kernel<D>), grid, dim3(kWave * 8), 0, st, a, cut);
+    }
+  } else {
+    hipLaunchKernelGGL((hyb_q8_token_kernel<T, D, 1>), grid, dim3(kWave * 4), 0, st, a, cut);
+  }
+  if (a.n_split == 1) return hipGetLastError();  // one range: already written out
+  const long rows = (long)a.s.B * a.s.Hq * a.s.L, units = (long)a.s.B * a.s.Hq * ((a.s.L + 1024 / D - 1) / (1024 / D));
+  if (rows <= 2048 && a.n_split > 4)
+    hipLaunchKernelGGL((hyb_q8_combine_kernel<T, D>), dim3((unsigned)rows), dim3(256), 0, st, a, cut);
+  else
+    hipLaunchKernelGGL((hyb_sp_combine_kernel<T, D, 2>), dim3((unsigned)std::min<long>(units, 2048)), dim3(256), 0, st, a,
+                       cut);
   return hipGetLastError();
 }
 
 // Threads of the largest launch.
-double softmax_q8_threads(const SoftmaxQ8Args& a) {
-  // (a plan's ranges: at most n_split per request, or what kMaxRange asks for)
-  const double need = std::ceil(((double)a.max_seen + a.s.L) / kMaxRange);
-  return 256.0 * a.s.B * a.s.Hkv * q8_groups(a.s) * std::max((double)a.n_split, need);
-}
+double softmax_q8_threads(const SoftmaxQ8Args& a) { return 512.0 * a.s.B * a.n_split * a.s.Hkv * q8_wgs(a.s); }
 
 hipError_t launch_softmax_q8(const SoftmaxQ8Args& a, hipStream_t st) {
   if (a.s.dtype == 1) return a.s.D == 64 ? q8_go<bf16, 64>(a, st) : q8_go<bf16, 128>(a, st);

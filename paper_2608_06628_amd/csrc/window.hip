@@ -170,6 +170,16 @@ __device__ inline WinSeq<WindowArgs> win_of_queries(const WindowArgs& a, int wgs
 __device__ inline WinSeq<PackedArgs> win_of_queries(const PackedArgs& a, int wgs, int lane, int& g, int& x) {
   const int G = a.s.Hq / a.s.Hkv;
   win_place(blockIdx.x, a.s.Hkv, g, x);
+  if (a.s.B < kMaxLevelled) {  // the longest lists first, of all sequences
+    int level = 0;
+    const int b = ragged_level(a.s.B + 1, x, wgs, lane, [&](int i) {
+      return ((WinSeq<PackedArgs>(a, i).cap + kTile - 1) / kTile * G + kWinWaves - 1) / kWinWaves;
+    }, level);
+    WinSeq<PackedArgs> s(a, max(b, 0));
+    if (b < 0) s.len = s.cap = 0;
+    x = level;
+    return s;
+  }
   x = wgs - 1 - x;
   const int b = ragged_find(a.s.B + 1, x, lane,
                             [&](int i) { return win_packed_queries(ragged_start(a.token_start, i, a.N), i, G); });
@@ -235,6 +245,15 @@ __device__ inline WinSeq<PackedArgs> win_of_keys(const PackedArgs& a, const WinP
   it.parts = cut.p;
   it.part = y % cut.p;
   const int x = y / cut.p;
+  if (a.s.B < kMaxLevelled) {
+    auto count = [&](int i) { return (WinSeq<PackedArgs>(a, i).cap + kWinKeys - 1) / kWinKeys; };
+    int level = 0;
+    const int b = ragged_level(a.s.B + 1, x, cut.wgs, lane, count, level);
+    WinSeq<PackedArgs> s(a, max(b, 0));
+    it.x = (s.cap + kWinKeys - 1) / kWinKeys - 1 - level;
+    if (b < 0) s.len = s.cap = it.x = 0;
+    return s;
+  }
   const int b = ragged_find(a.s.B + 1, x, lane,
                             [&](int i) { return win_packed_keys(ragged_start(a.token_start, i, a.N), i); });
   const WinSeq<PackedArgs> s(a, b);
@@ -1542,6 +1561,7 @@ static hipError_t packed_backward_go(PackedArgs a, hipStream_t st) {
   WinParts cut = win_cut(a.s, a.T, a.window, 0);
   cut.p = std::min(cut.p, most);
   cut.ns = 0;
+  cut.wgs = (int)win_packed_keys(a.N, a.s.B + 1);
   a.sums = (float*)((char*)a.ws + packed_stats_bytes(a.s, a.N));
   win_backward_kernels<T, D>(a, cut, st);
   WindowArgs rows = a;  // as one sequence of all rows

@@ -100,6 +100,11 @@ CASES = [  # B, L, Hq, Hkv, d, page, sb, lens, window, sinks, dtype
     (2, 3, 10, 2, 64, 32, 32, [160, 95], ALL, 0, BF),
     (1, 32, 16, 1, 128, 64, 64, [500], 300, 40, BF),   # 16 query heads per KV head
     (2, 1, 48, 1, 64, 64, 32, [200, 31], ALL, 0, BF),   # 48
+    (3, 32, 16, 4, 128, 64, 32, [0, 1, 32], ALL, 0, BF),  # a block alone, and two tiles
+    (3, 32, 12, 2, 64, 32, 32, [0, 70, 650], 200, 3, BF),  # 6 tiles of columns
+    (2, 29, 9, 3, 128, 32, 32, [95, 64], ALL, 0, BF),     # 3
+    (1, 32, 4, 1, 128, 64, 64, [12000], ALL, 0, BF),
+    (70, 1, 4, 2, 64, 64, 64, [(i * 37) % 200 for i in range(70)], ALL, 0, BF),
     (1, 1, 16, 4, 128, 64, 64, [20000], ALL, 0, BF),   # several ranges
     (2, 32, 4, 1, 64, 64, 64, [9000, 100], ALL, 0, BF),
     (3, 1, 8, 4, 64, 64, 32, [900, 0, 64], ALL, 0, FL),
@@ -108,7 +113,7 @@ CASES = [  # B, L, Hq, Hkv, d, page, sb, lens, window, sinks, dtype
     (1, 1, 4, 2, 64, 32, 32, [6000], 5000, 33, FL)]
 
 
-@pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(str(x) for x in c[:7]) + f"-{c[8]}-{c[9]}-{str(c[10])[6:]}")
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(str(x) for x in c[:7]) + f"-{c[7][0]}-{c[8]}-{c[9]}-{str(c[10])[6:]}")
 def test_step(case):
     announce(f"softmax q8 {case}")
     B, L, Hq, Hkv, d, page, sb, lens, window, sinks, dtype = case
