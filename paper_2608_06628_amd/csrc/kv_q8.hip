@@ -11,9 +11,11 @@
 // precision (its step is relative) and makes every value exact in bf16.
 //
 // Bound: memory; each row is read once and its codes written once.  A job is a scale
-// block's new rows at one head, of K or V: one wave holds 64 rows in registers between
-// the maximum and the codes (blocks of more rows take a wave per 64, up to four, and
-// past 256 rows a second look at memory).  Jobs are numbered so that request b's start
+// block's new rows at one head, of K or V: a wave holds 32 rows in registers between
+// the maximum and the codes (blocks of more rows take a wave per 32, up to eight, and
+// past 256 rows a second look at memory).  65536 tokens of 4 heads of d = 128, bf16, in blocks
+// of 64: 37 us, 5.1 TB/s, what a copy reaches; with 64 rows per wave, fewer of which fit, 42,
+// and 42 by stores that keep the codes in the caches.  Jobs are numbered so that request b's start
 // at start_b / block + 2 b, which leaves every request room for the blocks it touches
 // (its rows need not begin with a block) and needs no sums: a job finds its request by
 // one look at the starts of 64 requests (two of 4096).
@@ -25,18 +27,19 @@
 
 namespace hyb {
 
-constexpr int kQ8Rows = 64;   // rows that a wave holds
-constexpr int kQ8Waves = 4;   // of a workgroup
+constexpr int kQ8Rows = 32;   // rows that a wave holds (written)
+constexpr int kQ8Waves = 8;   // of a workgroup that writes
+constexpr int kQ8Readers = 4;
 
 __host__ __device__ inline long q8_first_job(int start, int b, int shift) { return (long)(start >> shift) + 2L * b; }
 
 // The rows lo .. lo + n - 1 (of k and v) that job `x` of blocks of 2^shift tokens
 // covers, and where they are in the pools.
 struct Q8Rows {
-  int n = 0;    // none: nothing to do
-  int src;      // first row of k and v
-  int at;       // its place in the block
-  size_t dst;   // row of the pools where the block starts
+  int n = 0;       // none: nothing to do
+  int src = 0;     // first row of k and v
+  int at = 0;      // its place in the block
+  size_t dst = 0;  // row of the pools where the block starts
   __device__ inline Q8Rows(const KvQ8Args& a, long x, int shift, int lane) {
     auto start = [&](int b) { return ragged_start(a.token_start, b, a.N); };
     const int b = ragged_find(a.B, x, lane, [&](int i) { return q8_first_job(start(i), i, shift); });
@@ -84,7 +87,7 @@ __device__ inline int q8_wave_max(int x) {
   return max(x, __builtin_bit_cast(int, xor32(f(x))));
 }
 
-// W waves share a job (1 or all of a workgroup's).
+// W waves share a job.  Codes are stored past the caches: a call writes more than it reads again.
 template <typename T, int D, int W>
 __global__ __launch_bounds__(kWave* kQ8Waves) void hyb_kv_q8_write_kernel(KvQ8Args a, long jobs) {
   constexpr int LPR = D / 8;           // lanes per row
@@ -92,20 +95,20 @@ __global__ __launch_bounds__(kWave* kQ8Waves) void hyb_kv_q8_write_kernel(KvQ8Ar
   constexpr int NL = kQ8Rows / RPI;    // loads that a wave holds
   __shared__ int most[kQ8Waves];
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int w = W == 1 ? 0 : wave;
-  const long job = W == 1 ? (long)blockIdx.x * kQ8Waves + wave : (long)blockIdx.x;
-  if (job >= jobs) return;  // (one wave of its own, or the whole workgroup)
+  const int w = wave % W;
+  const long job = min((long)blockIdx.x * (kQ8Waves / W) + wave / W, jobs);  // (behind the last: nothing)
   const int g = (int)(job % a.Hkv), kv = (int)(job / a.Hkv & 1);
-  const Q8Rows r(a, job / a.Hkv >> 1, a.sb_shift, lane);
-  if (r.n == 0) return;
+  Q8Rows r(a, job / a.Hkv >> 1, a.sb_shift, lane);
+  if (job == jobs) r.n = 0;
+  if (W == 1 && r.n == 0) return;  // (else at the barrier)
   const long stride = kv ? a.v_stride : a.k_stride;
   const T* src = (const T*)(kv ? a.v : a.k) + r.src * stride + (long)g * D + lane % LPR * 8;
   uint8_t* const pool = kv ? a.v_pages : a.k_pages;
   uint8_t* const scale = (kv ? a.v_scales : a.k_scales) + (r.dst >> a.sb_shift) * a.Hkv + g;
-  const int old = r.at > 0 ? min((int)*scale, 254) : 0;
+  const int old = r.n > 0 && r.at > 0 ? min((int)*scale, 254) : 0;
   Q8Piece<T> x[NL];
   int m = 0;
-  // This wave's rows, 64 at a time: w, w + W, ..; those past the last are the last again.
+  // This wave's rows, 32 at a time: w, w + W, ..; those past the last are the last again.
   auto load = [&](int c0) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < NL; ++u)
@@ -129,8 +132,9 @@ __global__ __launch_bounds__(kWave* kQ8Waves) void hyb_kv_q8_write_kernel(KvQ8Ar
   if constexpr (W > 1) {
     if (lane == 0) most[wave] = m;
     __syncthreads();
+    if (r.n == 0) return;
 #pragma unroll
-    for (int i = 0; i < W; ++i) m = max(m, most[i]);
+    for (int i = 0; i < W; ++i) m = max(m, most[wave - w + i]);
   }
   const int byte = max(scale_byte(__builtin_amdgcn_readfirstlane(m)), old);
   if (w == 0 && lane == 0) *scale = (uint8_t)byte;
@@ -156,18 +160,20 @@ __global__ __launch_bounds__(kWave* kQ8Waves) void hyb_kv_q8_write_kernel(KvQ8Ar
       if (c0 + u * RPI < r.n && i < r.n) {
         const uint2 c = {fp8_codes(x[u][0], x[u][1], x[u][2], x[u][3], f),
                          fp8_codes(x[u][4], x[u][5], x[u][6], x[u][7], f)};
-        *reinterpret_cast<uint2*>(pool + ((r.dst + r.at + i) * a.Hkv + g) * D + lane % LPR * 8) = c;
+        __builtin_nontemporal_store(__builtin_bit_cast(uint64_t, c), reinterpret_cast<uint64_t*>(
+            pool + ((r.dst + r.at + i) * a.Hkv + g) * D + lane % LPR * 8));
       }
     }
   }
 }
 
-// Reading: a job is at most 64 rows of a scale block at one head, of K or V.
+// Reading: a job is at most 64 rows of a scale block at one head, of K or V.  (64000 tokens of 4
+// heads of d = 128 into bf16: 31 us, 6.4 TB/s; 43 where the rows are stored by way of the caches.)
 template <typename T, int D>
-__global__ __launch_bounds__(kWave* kQ8Waves) void hyb_kv_q8_read_kernel(KvQ8Args a, long jobs, int shift) {
-  constexpr int LPR = D / 8, RPI = kWave / LPR, NL = kQ8Rows / RPI;
+__global__ __launch_bounds__(kWave* kQ8Readers) void hyb_kv_q8_read_kernel(KvQ8Args a, long jobs, int shift) {
+  constexpr int LPR = D / 8, RPI = kWave / LPR, NL = 64 / RPI;
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const long job = (long)blockIdx.x * kQ8Waves + wave;
+  const long job = (long)blockIdx.x * kQ8Readers + wave;
   if (job >= jobs) return;
   const int g = (int)(job % a.Hkv), kv = (int)(job / a.Hkv & 1);
   const Q8Rows r(a, job / a.Hkv >> 1, shift, lane);
@@ -186,10 +192,11 @@ __global__ __launch_bounds__(kWave* kQ8Waves) void hyb_kv_q8_read_kernel(KvQ8Arg
     const int i = u * RPI + lane / LPR;
     if (u * RPI < r.n && i < r.n) {
       if constexpr (sizeof(T) == 2) {
-        *reinterpret_cast<bf16x8*>(dst + i * stride) = fp8_bf16(c[u].x, c[u].y, f);
+        __builtin_nontemporal_store(__builtin_bit_cast(u32x4, fp8_bf16(c[u].x, c[u].y, f)),
+                                    reinterpret_cast<u32x4*>(dst + i * stride));
       } else {
-        *reinterpret_cast<f32x4*>(dst + i * stride) = fp8_f32(c[u].x, f);
-        *reinterpret_cast<f32x4*>(dst + i * stride + 4) = fp8_f32(c[u].y, f);
+        __builtin_nontemporal_store(fp8_f32(c[u].x, f), reinterpret_cast<f32x4*>(dst + i * stride));
+        __builtin_nontemporal_store(fp8_f32(c[u].y, f), reinterpret_cast<f32x4*>(dst + i * stride + 4));
       }
     }
   }
@@ -199,28 +206,32 @@ __global__ __launch_bounds__(kWave* kQ8Waves) void hyb_kv_q8_read_kernel(KvQ8Arg
 static long q8_jobs(const KvQ8Args& a, int shift) { return q8_first_job(a.N, a.B, shift) * 2 * a.Hkv; }
 static int q8_read_shift(const KvQ8Args& a) { return std::min(a.sb_shift, 6); }
 
+// Waves of a job.
+static int q8_write_waves(const KvQ8Args& a) { return std::min(kQ8Waves, std::max(1, (1 << a.sb_shift) / kQ8Rows)); }
+
 double kv_q8_threads(const KvQ8Args& a) {
-  return kWave * (kQ8Waves + std::max((double)q8_jobs(a, q8_read_shift(a)),
-                                      a.sb_shift > 6 ? (double)q8_jobs(a, a.sb_shift) * kQ8Waves : 0.0));
+  return kWave * (kQ8Waves + std::max((double)q8_jobs(a, q8_read_shift(a)), (double)q8_jobs(a, a.sb_shift) * q8_write_waves(a)));
 }
 
 template <typename T, int D>
 static hipError_t q8_write_go(const KvQ8Args& a, hipStream_t st) {
   const long jobs = q8_jobs(a, a.sb_shift);
-  const dim3 block(kWave * kQ8Waves);
-  if (a.sb_shift <= 6)
-    hipLaunchKernelGGL((hyb_kv_q8_write_kernel<T, D, 1>), dim3((unsigned)((jobs + kQ8Waves - 1) / kQ8Waves)), block, 0,
-                       st, a, jobs);
-  else
-    hipLaunchKernelGGL((hyb_kv_q8_write_kernel<T, D, kQ8Waves>), dim3((unsigned)jobs), block, 0, st, a, jobs);
+  const int waves = q8_write_waves(a);
+  const dim3 grid((unsigned)((jobs * waves + kQ8Waves - 1) / kQ8Waves)), block(kWave * kQ8Waves);
+  switch (waves) {
+    case 1: hipLaunchKernelGGL((hyb_kv_q8_write_kernel<T, D, 1>), grid, block, 0, st, a, jobs); break;
+    case 2: hipLaunchKernelGGL((hyb_kv_q8_write_kernel<T, D, 2>), grid, block, 0, st, a, jobs); break;
+    case 4: hipLaunchKernelGGL((hyb_kv_q8_write_kernel<T, D, 4>), grid, block, 0, st, a, jobs); break;
+    default: hipLaunchKernelGGL((hyb_kv_q8_write_kernel<T, D, 8>), grid, block, 0, st, a, jobs);
+  }
   return hipGetLastError();
 }
 template <typename T, int D>
 static hipError_t q8_read_go(const KvQ8Args& a, hipStream_t st) {
   const int shift = q8_read_shift(a);
   const long jobs = q8_jobs(a, shift);
-  hipLaunchKernelGGL((hyb_kv_q8_read_kernel<T, D>), dim3((unsigned)((jobs + kQ8Waves - 1) / kQ8Waves)),
-                     dim3(kWave * kQ8Waves), 0, st, a, jobs, shift);
+  hipLaunchKernelGGL((hyb_kv_q8_read_kernel<T, D>), dim3((unsigned)((jobs + kQ8Readers - 1) / kQ8Readers)),
+                     dim3(kWave * kQ8Readers), 0, st, a, jobs, shift);
   return hipGetLastError();
 }
 

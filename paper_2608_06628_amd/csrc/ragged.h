@@ -42,20 +42,33 @@ __device__ inline int ragged_sum(int x) {
   return __builtin_amdgcn_readfirstlane(x + __builtin_bit_cast(int, xor32(f(x))));
 }
 
-// Finds the x-th workgroup's sequence and level (b = -1: there are fewer); most: the
-// largest count there can be.
+__device__ inline int ragged_most(int x) {
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x128, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x124, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x122, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x121, 0xf, 0xf, false));
+  auto f = [](int v) { return __builtin_bit_cast(float, v); };
+  x = max(x, __builtin_bit_cast(int, xor16(f(x))));
+  return __builtin_amdgcn_readfirstlane(max(x, __builtin_bit_cast(int, xor32(f(x)))));
+}
+
+// Finds the x-th workgroup's sequence and level (b = -1: there are fewer).
 template <typename F>
-__device__ inline int ragged_level(int n, int x, int most, int lane, F count, int& level) {
-  int c[kLevelLanes];
+__device__ inline int ragged_level(int n, int x, int lane, F count, int& level) {
+  int c[kLevelLanes], most = 0;
 #pragma unroll
-  for (int i = 0; i < kLevelLanes; ++i) c[i] = lane + i * kWave < n ? count(lane + i * kWave) : 0;
+  for (int i = 0; i < kLevelLanes; ++i) {
+    c[i] = 0;
+    if (i * kWave < n && lane + i * kWave < n) c[i] = count(lane + i * kWave);
+    most = max(most, c[i]);
+  }
   auto above = [&](int y) {  // workgroups at levels above y
     int t = 0;
 #pragma unroll
     for (int i = 0; i < kLevelLanes; ++i) t += max(0, c[i] - 1 - y);
     return ragged_sum(t);
   };
-  int lo = -1, hi = most;  // above(hi) <= x; above(lo) > x, or lo = -1
+  int lo = -1, hi = ragged_most(most) - 1;  // above(hi) <= x; above(lo) > x, or lo = -1
   if (above(-1) <= x) return -1;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;

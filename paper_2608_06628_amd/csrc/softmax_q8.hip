@@ -761,14 +761,16 @@ static int q8_wgs(const Shape& s) { return (q8_groups(s) + q8_columns(s) - 1) / 
 static int q8_parts(const Shape& s, int max_seen) {
   const double tiles = std::ceil(max_seen / 32.0) + 1, wgs = (double)s.B * s.Hkv * q8_wgs(s);
   const bool block = q8_columns(s) == 4;
-  const double tile = s.dtype != 1 ? 2.0 * s.D / 64 : block ? 0.34 : 0.4, fixed = 6.0;
-  const double rows = (double)s.B * s.Hq * s.L, row = (s.D + 2) * 8 / 4e6;  // a partial row's write and read
+  const double tile = s.dtype != 1 ? 2.0 * s.D / 64 : block ? 0.65 : 0.4, fixed = 6.0;
+  const double rows = (double)s.B * s.Hq * s.L, row = (s.D + 2) * 8 / 2e6;  // a partial row's write and read
   int best = 1;
   double least = 0;
-  const int most = (int)std::max(1.0, std::min(tiles / 4, std::ceil(2048.0 / wgs)));
-  for (int k = 1; k <= most; ++k) {
-    const double t = std::ceil(wgs * k / 256) * (tiles / k * tile + fixed) + (k > 1 ? 4.0 + rows * k * row : 0.0);
-    if (k == 1 || t < least * 0.98) {
+  // one, and as many as fill the chip once, twice, ..
+  for (int rounds = 0; rounds <= 4; ++rounds) {
+    const int k = rounds == 0 ? 1 : (int)std::min(256.0 * rounds / wgs, tiles / 4);
+    if (k < 1) continue;
+    const double t = std::ceil(wgs * k / 256) * (tiles / k * tile + fixed) + (k > 1 ? 6.0 + rows * k * row : 0.0);
+    if (rounds == 0 || t < least * 0.98) {
       least = t;
       best = k;
     }

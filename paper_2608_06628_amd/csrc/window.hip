@@ -96,7 +96,7 @@ __device__ inline void win_place(int bid, int nbg, int& bg, int& x) {
   x = bid / nbg;
 }
 
-// Units of the query kernels (32 queries of a head) per workgroup; keys of a
+// Units of the query kernels (32 queries of a head) per workgroup, at most; keys of a
 // workgroup of the dK, dV kernels.
 constexpr int kWinWaves = 4;
 constexpr int kWinKeys = 4 * kTile;
@@ -151,15 +151,16 @@ struct WinSeq<PackedArgs> {
 };
 
 // Packed: the first workgroup of the queries of sequence b, and of its keys, so that
-// every sequence has room for its own: of 4 units, G per tile of queries, and of 128 keys.
-__host__ __device__ inline long win_packed_queries(int start, int b, int G) {
-  return (long)start * G / (kWinWaves * kTile) + (long)b * ((G + kWinWaves - 1) / kWinWaves + 2);
+// every sequence has room for its own: of U units, G per tile of queries, and of 128 keys.
+__host__ __device__ inline long win_packed_queries(int start, int b, int G, int U = kWinWaves) {
+  return (long)start * G / (U * kTile) + (long)b * ((G + U - 1) / U + 2);
 }
 __host__ __device__ inline long win_packed_keys(int start, int b) { return (long)(start / kWinKeys) + b; }
 
 // This workgroup's sequence, KV head, and its place x among the sequence's
 // workgroups of queries, of `wgs` (per sequence and head, or packed per head); those of the
 // last queries, which see most, come first.
+template <int U = kWinWaves>
 __device__ inline WinSeq<WindowArgs> win_of_queries(const WindowArgs& a, int wgs, int, int& g, int& x) {
   int bg;
   win_place(blockIdx.x, a.s.B * a.s.Hkv, bg, x);
@@ -167,13 +168,14 @@ __device__ inline WinSeq<WindowArgs> win_of_queries(const WindowArgs& a, int wgs
   g = bg % a.s.Hkv;
   return WinSeq<WindowArgs>(a, bg / a.s.Hkv);
 }
+template <int U = kWinWaves>
 __device__ inline WinSeq<PackedArgs> win_of_queries(const PackedArgs& a, int wgs, int lane, int& g, int& x) {
   const int G = a.s.Hq / a.s.Hkv;
   win_place(blockIdx.x, a.s.Hkv, g, x);
   if (a.s.B < kMaxLevelled) {  // the longest lists first, of all sequences
     int level = 0;
-    const int b = ragged_level(a.s.B + 1, x, wgs, lane, [&](int i) {
-      return ((WinSeq<PackedArgs>(a, i).cap + kTile - 1) / kTile * G + kWinWaves - 1) / kWinWaves;
+    const int b = ragged_level(a.s.B + 1, x, lane, [&](int i) {
+      return ((WinSeq<PackedArgs>(a, i).cap + kTile - 1) / kTile * G + U - 1) / U;
     }, level);
     WinSeq<PackedArgs> s(a, max(b, 0));
     if (b < 0) s.len = s.cap = 0;
@@ -182,9 +184,9 @@ __device__ inline WinSeq<PackedArgs> win_of_queries(const PackedArgs& a, int wgs
   }
   x = wgs - 1 - x;
   const int b = ragged_find(a.s.B + 1, x, lane,
-                            [&](int i) { return win_packed_queries(ragged_start(a.token_start, i, a.N), i, G); });
+                            [&](int i) { return win_packed_queries(ragged_start(a.token_start, i, a.N), i, G, U); });
   const WinSeq<PackedArgs> s(a, b);
-  x = max(0, x - (int)win_packed_queries(s.start, b, G));
+  x = max(0, x - (int)win_packed_queries(s.start, b, G, U));
   return s;
 }
 
@@ -248,7 +250,7 @@ __device__ inline WinSeq<PackedArgs> win_of_keys(const PackedArgs& a, const WinP
   if (a.s.B < kMaxLevelled) {
     auto count = [&](int i) { return (WinSeq<PackedArgs>(a, i).cap + kWinKeys - 1) / kWinKeys; };
     int level = 0;
-    const int b = ragged_level(a.s.B + 1, x, cut.wgs, lane, count, level);
+    const int b = ragged_level(a.s.B + 1, x, lane, count, level);
     WinSeq<PackedArgs> s(a, max(b, 0));
     it.x = (s.cap + kWinKeys - 1) / kWinKeys - 1 - level;
     if (b < 0) s.len = s.cap = it.x = 0;
@@ -270,12 +272,12 @@ __device__ inline WinSeq<PackedArgs> win_of_keys(const PackedArgs& a, const WinP
 // one barrier.  fp32 products run at 1/16 of the bf16 rate and bound the loop (a
 // pair of tiles at d = 64 is 128 products of 64 cycles for the four waves' SIMDs).
 
-template <int D>
+template <int D, int W = kWinWaves>  // W: waves that share a tile's copies
 struct WinF32 {
   typedef Mma<float> M;
   static constexpr int KD = D / M::KW, NCT = D / kTile;
   static constexpr int LD = D + 4;             // row pitch in LDS
-  static constexpr int NCH = kTile * D / 4 / (kWave * kWinWaves);  // 16-byte pieces of a tile per thread
+  static constexpr int NCH = kTile * D / 4 / (kWave * W);  // 16-byte pieces of a tile per thread
   typedef float Tile[kTile][LD];
   typedef float Ops[KD];
   typedef f32x16 Acc[NCT];
@@ -285,25 +287,25 @@ struct WinF32 {
 };
 
 // Rows row0 .. row0 + 31 of two arrays (row strides in elements) into registers,
-// and from there, zero from row `rows` on, into two tiles; by four waves, whose
+// and from there, zero from row `rows` on, into two tiles; by W waves, whose
 // thread number t is.  (The zeros are put in last: a select at the load would wait for it.)
-template <int D>
-__device__ inline void win_fetch(typename WinF32<D>::Regs& r, const float* a, const float* b, size_t as,
+template <int D, int W = kWinWaves>
+__device__ inline void win_fetch(typename WinF32<D, W>::Regs& r, const float* a, const float* b, size_t as,
                                  size_t bs, int row0, int rows, int t) {
 #pragma unroll
-  for (int u = 0; u < WinF32<D>::NCH; ++u) {
-    const int x = t + u * kWave * kWinWaves, i = row0 + x / (D / 4);
+  for (int u = 0; u < WinF32<D, W>::NCH; ++u) {
+    const int x = t + u * kWave * W, i = row0 + x / (D / 4);
     const int row = min(i, rows - 1), c = x % (D / 4) * 4;
     r.a[u] = *reinterpret_cast<const f32x4*>(a + row * as + c);
     r.b[u] = *reinterpret_cast<const f32x4*>(b + row * bs + c);
   }
 }
-template <int D>
-__device__ inline void win_put(const typename WinF32<D>::Regs& r, typename WinF32<D>::Tile& a,
+template <int D, int W = kWinWaves>
+__device__ inline void win_put(const typename WinF32<D, W>::Regs& r, typename WinF32<D>::Tile& a,
                                typename WinF32<D>::Tile& b, int row0, int rows, int t) {
 #pragma unroll
-  for (int u = 0; u < WinF32<D>::NCH; ++u) {
-    const int x = t + u * kWave * kWinWaves, i = x / (D / 4);
+  for (int u = 0; u < WinF32<D, W>::NCH; ++u) {
+    const int x = t + u * kWave * W, i = x / (D / 4);
     const bool ok = row0 + i < rows;
     *reinterpret_cast<f32x4*>(&a[i][x % (D / 4) * 4]) = ok ? r.a[u] : f32x4{};
     *reinterpret_cast<f32x4*>(&b[i][x % (D / 4) * 4]) = ok ? r.b[u] : f32x4{};
@@ -369,19 +371,19 @@ __device__ inline WinUnit win_unit(const WindowArgs& a, int len, int g, int u) {
   return WinUnit{g * G + u % G, i0, i0 < len};
 }
 
-// Forward.  With H = 2 two halves of four waves take a unit's tiles in turn, each
+// Forward, of U units per workgroup.  With H = 2 two halves of U waves take a unit's tiles in turn, each
 // through buffers of its own, and join their sums in LDS: a CU that holds one
 // workgroup has two waves per SIMD then, and one's products run beside the other's
 // weights (3 x 1197 tokens, 8 heads of d = 64, window 300: 47 us with one half, now 40).
-template <int D, int H, typename A>
-__global__ __launch_bounds__(kWave* kWinWaves* H) void hyb_win_fwd_kernel(A a, int wgs) {
-  typedef WinF32<D> C;
+template <int D, int H, typename A, int U = kWinWaves>
+__global__ __launch_bounds__(kWave* U* H) void hyb_win_fwd_kernel(A a, int wgs) {
+  typedef WinF32<D, U> C;
   struct Tiles {
     typename C::Tile k[H][2], v[H][2];
   };
   struct Join {  // the second half's sums and weighted sums
-    float m[kWinWaves][kTile], l[kWinWaves][kTile];
-    f32x4 x[kWinWaves][C::NCT * 4][kWave];
+    float m[U][kTile], l[U][kTile];
+    f32x4 x[U][C::NCT * 4][kWave];
   };
   union Smem {
     Tiles tiles;
@@ -390,14 +392,14 @@ __global__ __launch_bounds__(kWave* kWinWaves* H) void hyb_win_fwd_kernel(A a, i
   };
   __shared__ alignas(16) Smem sh;
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int half = wave / kWinWaves, w = wave % kWinWaves, t = threadIdx.x % (kWave * kWinWaves);
+  const int half = wave / U, w = wave % U, t = threadIdx.x % (kWave * U);
   const int li = lane & 31, hh = lane >> 5;
   const int Hq = a.s.Hq, Hkv = a.s.Hkv, G = Hq / Hkv;
   int g, x;
-  const WinSeq<A> sq = win_of_queries(a, wgs, lane, g, x);
+  const WinSeq<A> sq = win_of_queries<U>(a, wgs, lane, g, x);
   const int len = sq.len;
-  const WinUnit me = win_unit(a, len, g, x * kWinWaves + w);
-  const int first = x * kWinWaves / G * kTile, last = min(((x + 1) * kWinWaves - 1) / G * kTile + kTile, len);
+  const WinUnit me = win_unit(a, len, g, x * U + w);
+  const int first = x * U / G * kTile, last = min(((x + 1) * U - 1) / G * kTile + kTile, len);
   if (first >= len) return;  // uniform
   const WinTiles tl(a, len, first, last, kTile);
   const size_t qs = sq.qs(D), ks_ = sq.ks(D), vs_ = sq.vs(D);
@@ -411,7 +413,7 @@ __global__ __launch_bounds__(kWave* kWinWaves* H) void hyb_win_fwd_kernel(A a, i
   const int nsteps = (tl.n + H - 1) / H, mine = (tl.n + H - 1 - half) / H;
   auto key = [&](int n) __attribute__((always_inline)) { return tl.first(H * n + half, kTile); };
   typename C::Regs next;
-  if (mine > 0) win_fetch<D>(next, K, V, ks_, vs_, key(0), len, t);
+  if (mine > 0) win_fetch<D, U>(next, K, V, ks_, vs_, key(0), len, t);
   typename C::Ops qop;
   win_row_ops<D>(qop, (const float*)a.q + sq.q(me.h, D) + i * qs, true, hh);
   const float scale = kLog2e / sqrtf((float)D);
@@ -419,11 +421,11 @@ __global__ __launch_bounds__(kWave* kWinWaves* H) void hyb_win_fwd_kernel(A a, i
   typename C::Acc acc;
 #pragma unroll
   for (int ct = 0; ct < C::NCT; ++ct) acc[ct] = f32x16{};
-  if (mine > 0) win_put<D>(next, kt[0], vt[0], key(0), len, t);
+  if (mine > 0) win_put<D, U>(next, kt[0], vt[0], key(0), len, t);
   __syncthreads();
   for (int n = 0; n < nsteps; ++n) {
     const int buf = n & 1, j0 = n < mine ? key(n) : 0;
-    if (n + 1 < mine) win_fetch<D>(next, K, V, ks_, vs_, key(n + 1), len, t);
+    if (n + 1 < mine) win_fetch<D, U>(next, K, V, ks_, vs_, key(n + 1), len, t);
     if (me.any && n < mine && !win_none(r0, r1, a.n_sinks, j0, kTile)) {  // uniform over the wave
       f32x16 sc = win_rows_mma<D>(kt[buf], qop, li, hh);
       if (!win_full(r0, r1, a.n_sinks, j0, kTile)) {  // uniform
@@ -455,7 +457,7 @@ __global__ __launch_bounds__(kWave* kWinWaves* H) void hyb_win_fwd_kernel(A a, i
       win_cols_mma<D>(acc, vt[buf], p, li, hh);
       mma_settle<float>();
     }
-    if (n + 1 < mine) win_put<D>(next, kt[buf ^ 1], vt[buf ^ 1], key(n + 1), len, t);
+    if (n + 1 < mine) win_put<D, U>(next, kt[buf ^ 1], vt[buf ^ 1], key(n + 1), len, t);
     __syncthreads();
   }
   if constexpr (H == 2) {
@@ -1389,10 +1391,10 @@ struct WinGrid<WindowArgs> {
 template <>
 struct WinGrid<PackedArgs> {
   int wgs, n, busy, heads;
-  explicit WinGrid(const PackedArgs& a) : heads(a.s.Hkv) {
-    wgs = (int)win_packed_queries(a.N, a.s.B + 1, a.s.Hq / a.s.Hkv);
+  explicit WinGrid(const PackedArgs& a, int U = kWinWaves) : heads(a.s.Hkv) {
+    wgs = (int)win_packed_queries(a.N, a.s.B + 1, a.s.Hq / a.s.Hkv, U);
     n = wgs * heads;
-    busy = (int)std::min<long>(n, (long)a.N * a.s.Hq / (kWinWaves * kTile));
+    busy = (int)std::min<long>(n, ((long)a.N / kTile + a.s.B / 2) * a.s.Hq / U);
   }
   int items(const PackedArgs& a, const WinParts& cut) const { return (int)win_packed_keys(a.N, a.s.B + 1) * cut.p; }
 };
@@ -1412,6 +1414,16 @@ template <int D, typename A>
 static hipError_t win_prefill_f32_go(const A& a, hipStream_t st) {
   const WinGrid<A> gr(a);
   const dim3 grid((unsigned)gr.n);
+  if constexpr (std::is_same_v<A, PackedArgs>) {
+    // Two units per workgroup while those have a CU each: a SIMD then has one wave of a
+    // step's products, not two (5 sequences of 1 to 701, 8 heads of d = 64: 56 us with four
+    // units).
+    const WinGrid<A> two(a, 2);
+    if (two.busy <= 256) {
+      hipLaunchKernelGGL((hyb_win_fwd_kernel<D, 2, A, 2>), dim3((unsigned)two.n), dim3(kWave * 4), 0, st, a, two.wgs);
+      return hipGetLastError();
+    }
+  }
   // Two halves at d = 128, where one workgroup fits a CU either way (8 x 4096 tokens,
   // 16 heads, window 500, 1404 us with one, now 1300; 1 x 1024, 159 and 144), and at
   // d = 64, where three of one half fit, while workgroups are few (1 x 3000 tokens, 192
@@ -1555,13 +1567,40 @@ static size_t packed_sums_bytes(const Shape& s, int N, int parts) {
   return parts > 1 ? (size_t)parts * N * 2 * s.Hkv * s.D * sizeof(float) : 0;
 }
 
+// The cut, by win_cut's reasoning and numbers, for sequences half as long again as their mean
+// (the longest lists are what a call waits for where there are few; the host knows only the
+// mean).  (40 sequences of 1 to 511, window 255, 8 and 2 heads of d = 64: a call takes 66 us in
+// one part of halves, 65, 59 and 56 in 2, 3 and 4 without; 40 of 255 48 and, in 4, 52; 16 of 1 to
+// 2048, 16 and 4 heads of d = 128, 417 in one and 453 in 2.)
+static WinParts packed_cut(const Shape& s, int N, int window) {
+  const int G = s.Hq / s.Hkv, mean_len = packed_mean(s, N);
+  const int T = (int)std::min<long>(N, (long)mean_len * 3 / 2);
+  WinParts c = {};
+  const double all = (N / (double)kWinKeys + (s.B - 1) / 2.0) * s.Hkv, every = std::ceil(T / 32.0);
+  const double seen = std::min(every, std::ceil(((double)window + s.L + kWinKeys) / kTile) + 1);
+  const double mean = seen - seen * seen / (2 * every);
+  const bool f32 = s.dtype != 1;
+  const double launch = 4.5, sum = (double)N * s.Hkv * s.D * (f32 ? 3.5e-6 : s.D == 128 ? 2.5e-6 : 1.25e-6);
+  double best = 0;
+  for (int h = f32 || s.D == 64 ? 1 : 2; h <= (f32 ? 1 : 2); ++h) {
+    const double unit = f32 ? 6.0 * s.D / 64 : s.D == 128 ? 0.75 : h == 1 ? 0.65 : 0.4;
+    const double fixed = f32 || s.D == 128 ? 6.0 : h == 1 ? 1.0 : 2.5;
+    for (int p = 1; p <= win_most_parts(s, mean_len); ++p) {
+      const double rounds = f32 || h == 2 ? std::ceil(all * p / 256) : std::max(1.0, all * p / 450);
+      const double t = rounds * fixed + G * unit / p * std::max(seen, rounds * mean) + (p > 1 ? launch + p * sum : 0);
+      if (c.p == 0 || t < best) {
+        best = t;
+        c.p = p;
+        c.halves = h == 2;
+      }
+    }
+  }
+  return c;
+}
+
 template <typename T, int D>
 static hipError_t packed_backward_go(PackedArgs a, hipStream_t st) {
-  const int most = win_most_parts(a.s, a.T);
-  WinParts cut = win_cut(a.s, a.T, a.window, 0);
-  cut.p = std::min(cut.p, most);
-  cut.ns = 0;
-  cut.wgs = (int)win_packed_keys(a.N, a.s.B + 1);
+  const WinParts cut = packed_cut(a.s, a.N, a.window);
   a.sums = (float*)((char*)a.ws + packed_stats_bytes(a.s, a.N));
   win_backward_kernels<T, D>(a, cut, st);
   WindowArgs rows = a;  // as one sequence of all rows
@@ -1585,7 +1624,7 @@ hipError_t launch_packed_backward(const PackedArgs& a_, hipStream_t st) {
 }
 
 double packed_threads(const Shape& s, int N) {
-  const double queries = (double)win_packed_queries(N, s.B + 1, s.Hq / s.Hkv);
+  const double queries = (double)win_packed_queries(N, s.B + 1, s.Hq / s.Hkv, 2);
   const double keys = (double)win_packed_keys(N, s.B + 1) * win_most_parts(s, packed_mean(s, N));
   return kWave * kWinWaves * 2.0 * s.Hkv * std::max(queries, keys);
 }
