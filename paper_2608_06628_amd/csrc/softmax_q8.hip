@@ -150,33 +150,26 @@ struct Q8Acc {
 #pragma unroll
     for (int ct = 0; ct < NCT; ++ct) acc[ct] = f32x16{};
   }
-  // Scores (K Q^T) of a tile of codes, without their scale, for C tiles of columns.
-  template <int C>
-  __device__ static inline void scores(f32x16 (&sc)[C], const Q8Tile<D>& qt, const uint8_t* kt, const op_t (&qop)[C][KD]) {
-#pragma unroll
-    for (int c = 0; c < C; ++c) sc[c] = f32x16{};
+  // Scores (K Q^T) of a tile of codes, without their scale.
+  __device__ static inline f32x16 scores(const Q8Tile<D>& qt, const uint8_t* kt, const op_t (&qop)[KD]) {
+    f32x16 sc = {};
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
       const uint4 x = qt.row(kt, i);
       if constexpr (sizeof(T) == 2) {
-        const op_t k0 = fp8_bf16(x.x, x.y, 1.0f), k1 = fp8_bf16(x.z, x.w, 1.0f);
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          sc[c] = M::mma(k0, qop[c][2 * i], sc[c]);
-          sc[c] = M::mma(k1, qop[c][2 * i + 1], sc[c]);
-        }
+        sc = M::mma(fp8_bf16(x.x, x.y, 1.0f), qop[2 * i], sc);
+        sc = M::mma(fp8_bf16(x.z, x.w, 1.0f), qop[2 * i + 1], sc);
       } else {
         const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
           const f32x4 k = fp8_f32(w[y], 1.0f);
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int c = 0; c < C; ++c) sc[c] = M::mma(k[e], qop[c][16 * i + 4 * y + e], sc[c]);
+          for (int e = 0; e < 4; ++e) sc = M::mma(k[e], qop[16 * i + 4 * y + e], sc);
         }
       }
     }
+    return sc;
   }
   // Weights of a tile's masked scores (in p), for a scale into the log2 domain.
   __device__ inline void weights(const f32x16& sc, float scale, float (&p)[16]) {
@@ -203,41 +196,30 @@ struct Q8Acc {
     }
     l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
   }
-  // A tile of cached tokens at j0 with its scales' bytes, to C tiles of columns.
-  template <int C>
-  __device__ static inline void add(Q8Acc (&me)[C], const Q8Tiles<D>& t, const Q8Tile<D>& qt, int j0, const uint8_t* kt,
-                                    const uint8_t* vt, int bytes, const op_t (&qop)[C][KD], float scale, int hh) {
-    f32x16 sc[C];
-    scores<C>(sc, qt, kt, qop);
+  // A tile of cached tokens at j0 with its scales' bytes.
+  __device__ inline void add(const Q8Tiles<D>& t, const Q8Tile<D>& qt, int j0, const uint8_t* kt, const uint8_t* vt,
+                             int bytes, const op_t (&qop)[KD], float scale, int hh) {
+    f32x16 sc = scores(qt, kt, qop);
     mma_settle<T>();
     if (!t.whole(j0)) {  // uniform
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const bool ok = t.sees(j0 + row_of(e, hh));
-#pragma unroll
-        for (int c = 0; c < C; ++c) sc[c][e] = ok ? sc[c][e] : -INFINITY;
-      }
+      for (int e = 0; e < 16; ++e) sc[e] = t.sees(j0 + row_of(e, hh)) ? sc[e] : -INFINITY;
     }
     const float fk = scale * scale_of(bytes & 255), fv = scale_of(bytes >> 8);
-    float p[C][16];
-#pragma unroll
-    for (int c = 0; c < C; ++c) me[c].weights(sc[c], fk, p[c]);
+    float p[16];
+    weights(sc, fk, p);
     if constexpr (sizeof(T) == 2) {
       // The weights enter P V rounded to bf16 (each off by at most 2^-8 of itself;
       // products of fp32 run at 1/16 of the rate); their sum is over the unrounded ones.
-      op_t pop[C][KL];
+      op_t pop[KL];
 #pragma unroll
-      for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int ks = 0; ks < KL; ++ks) pop[c][ks] = cvt_op<bf16>(&p[c][ks * 8]);
+      for (int ks = 0; ks < KL; ++ks) pop[ks] = cvt_op<bf16>(&p[ks * 8]);
 #pragma unroll
       for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
         for (int ks = 0; ks < KL; ++ks) {
           const uint2 x = qt.column(vt, ct, ks);
-          const op_t v = fp8_bf16(x.x, x.y, fv);
-#pragma unroll
-          for (int c = 0; c < C; ++c) me[c].acc[ct] = M::mma(v, pop[c][ks], me[c].acc[ct]);
+          acc[ct] = M::mma(fp8_bf16(x.x, x.y, fv), pop[ks], acc[ct]);
         }
     } else {
 #pragma unroll
@@ -247,10 +229,7 @@ struct Q8Acc {
           const uint2 x = qt.column(vt, ct, ks);
           const f32x4 lo = fp8_f32(x.x, fv), hi = fp8_f32(x.y, fv);
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-              me[c].acc[ct] = M::mma(e < 4 ? lo[e] : hi[e - 4], p[c][8 * ks + e], me[c].acc[ct]);
+          for (int e = 0; e < 8; ++e) acc[ct] = M::mma(e < 4 ? lo[e] : hi[e - 4], p[8 * ks + e], acc[ct]);
         }
     }
   }
@@ -277,11 +256,11 @@ struct Q8Acc {
 // tiles of 32 columns: `groups` of them.
 __host__ __device__ inline int q8_groups(const Shape& s) { return (s.Hq / s.Hkv * s.L + kTile - 1) / kTile; }
 
-// A workgroup answers C tiles of 32 columns over a range of keys: the four waves take the
+// A workgroup answers 32 columns over a range of keys: the four waves take the
 // range's tiles in turn, each through copies of its own (R slots, no barrier in the loop)
 // and sums of its own, joined in LDS at the end.  The codes are converted as they become
-// operands, once each for all columns.
-template <typename T, int D, int C>
+// operands.
+template <typename T, int D>
 __global__ __launch_bounds__(kWave * 4) void hyb_q8_token_kernel(SoftmaxQ8Args a, SpCut cut) {
   typedef Q8Acc<T, D> A;
   typedef Q8Tile<D> QT;
@@ -296,13 +275,13 @@ __global__ __launch_bounds__(kWave * 4) void hyb_q8_token_kernel(SoftmaxQ8Args a
     struct {
       Slot ring[NW][R];
     } loop;
-    f32x4 parts[NW][C][NCT * 4][kWave];
+    f32x4 parts[NW][NCT * 4][kWave];
     int plan[kPlanInts];
     __device__ Smem() {}
   };
   __shared__ alignas(16) Smem sh;
   __shared__ alignas(16) Block blk;
-  __shared__ float refs[NW][C][kTile], sums[NW][C][kTile];
+  __shared__ float refs[NW][kTile], sums[NW][kTile];
   __shared__ int pages[kMaxRangePages];
   __shared__ uint16_t bytes[kMaxRange / kTile + 2];
 
@@ -311,24 +290,19 @@ __global__ __launch_bounds__(kWave * 4) void hyb_q8_token_kernel(SoftmaxQ8Args a
   const int li = lane & 31, hh = lane >> 5;
   const int Hq = a.s.Hq, Hkv = a.s.Hkv, L = a.s.L, G = Hq / Hkv;
   int at, hg;
-  sp_place((q8_groups(a.s) + C - 1) / C, at, hg);
+  sp_place(q8_groups(a.s), at, hg);
   const int g = at % Hkv, r = at / Hkv;
   const SpRange rg = sp_range<2>(a, sp_plan<2>(a, cut, sh.plan), r, lane);
   if (rg.b < 0) return;  // uniform: past the plan's last range
   const int Lb = sp_block<2>(a, rg.b), P = min(max(a.prefix_len[rg.b], 0), a.max_prefix);
-  // this lane's columns: query i of head h
-  int i[C], h[C];
-  bool mine[C];
-  typename A::op_t qop[C][A::KD];
+  // this lane's column: query i of head h
+  const int col = hg * kTile + li, hl = col / L, i = col - hl * L, h = g * G + hl;
+  const bool mine = hl < G && i < Lb;
+  typename A::op_t qop[A::KD];
+  {
+    const T* row = (const T*)a.q + (((size_t)rg.b * L + (mine ? i : 0)) * Hq + (mine ? h : g * G)) * D;
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
-    const int col = (hg * C + c) * kTile + li, hl = col / L;
-    i[c] = col - hl * L;
-    h[c] = g * G + hl;
-    mine[c] = hl < G && i[c] < Lb;
-    const T* row = (const T*)a.q + (((size_t)rg.b * L + (mine[c] ? i[c] : 0)) * Hq + (mine[c] ? h[c] : g * G)) * D;
-#pragma unroll
-    for (int ks = 0; ks < A::KD; ++ks) qop[c][ks] = keep_if<T>(mine[c], load_op<T>(row + A::entry(ks, hh)));
+    for (int ks = 0; ks < A::KD; ++ks) qop[ks] = keep_if<T>(mine, load_op<T>(row + A::entry(ks, hh)));
   }
   const Q8Tiles<D> t(a, rg, g, P, pages);
   const QT qt(lane);
@@ -353,7 +327,7 @@ __global__ __launch_bounds__(kWave * 4) void hyb_q8_token_kernel(SoftmaxQ8Args a
   }
   __syncthreads();  // (the plan's scratch has been read)
   const float scale = kLog2e / sqrtf((float)D);
-  A acc[C];
+  A acc;
 #pragma unroll
   for (int n = 0; n < R - 1; ++n) issue(n, sh.loop.ring[w][n]);
   auto step = [&](int n, auto S) __attribute__((always_inline)) {
@@ -366,7 +340,7 @@ __global__ __launch_bounds__(kWave * 4) void hyb_q8_token_kernel(SoftmaxQ8Args a
     else if (later == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * QT::IK) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     const Slot& s = sh.loop.ring[w][SV];
-    A::template add<C>(acc, t, qt, t.first_key(w + NW * n), s.k, s.v, bytes[w + NW * n], qop, scale, hh);
+    acc.add(t, qt, t.first_key(w + NW * n), s.k, s.v, bytes[w + NW * n], qop, scale, hh);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot is read
   };
   for (int n = 0; n < my; n += R) {
@@ -377,60 +351,46 @@ __global__ __launch_bounds__(kWave * 4) void hyb_q8_token_kernel(SoftmaxQ8Args a
       step(n + 3, std::integral_constant<int, 3>{});
     }
   }
-  if (block && w == nt % NW) {
-#pragma unroll
-    for (int c = 0; c < C; ++c) acc[c].add_block(blk.k, blk.v, Lb, qop[c], scale, li, hh);
-  }
+  if (block && w == nt % NW) acc.add_block(blk.k, blk.v, Lb, qop, scale, li, hh);
 
   // The waves' sums over one reference: wave w scales its own and leaves them in
   // LDS, then joins entries 32 w .. + 31 of every column.
   mma_settle<T>();
-  float l[C], mm[C], f[C];
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    l[c] = acc[c].l + xor32(acc[c].l);
-    if (hh == 0) refs[w][c][li] = acc[c].m;
-  }
+  const float l = acc.l + xor32(acc.l);
+  if (hh == 0) refs[w][li] = acc.m;
   lds_barrier();  // (and the slots are free)
+  float mm = refs[0][li];
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
-    mm[c] = refs[0][c][li];
+  for (int x = 1; x < NW; ++x) mm = fmaxf(mm, refs[x][li]);
+  const float f = __builtin_amdgcn_exp2f(acc.m - mm);
+  if (hh == 0) sums[w][li] = l * f;
 #pragma unroll
-    for (int x = 1; x < NW; ++x) mm[c] = fmaxf(mm[c], refs[x][c][li]);
-    f[c] = __builtin_amdgcn_exp2f(acc[c].m - mm[c]);
-    if (hh == 0) sums[w][c][li] = l[c] * f[c];
-#pragma unroll
-    for (int ct = 0; ct < NCT; ++ct)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const f32x16& y = acc[c].acc[ct];
-        sh.parts[w][c][ct * 4 + e][lane] = f32x4{y[4 * e] * f[c], y[4 * e + 1] * f[c], y[4 * e + 2] * f[c], y[4 * e + 3] * f[c]};
-      }
-  }
-  lds_barrier();
-  if (w >= NCT) return;
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    if (!mine[c]) continue;
-    float den = 0.0f;
-#pragma unroll
-    for (int x = 0; x < NW; ++x) den += sums[x][c][li];
+  for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      f32x4 o = {};
-#pragma unroll
-      for (int x = 0; x < NW; ++x) {
-        const f32x4 y = sh.parts[x][c][w * 4 + e][lane];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) o[k] += y[k];
-      }
-      sp_put<T, D>(a, rg, r, h[c], i[c], w * kTile + row_of(4 * e, hh), o, den);
+      const f32x16& y = acc.acc[ct];
+      sh.parts[w][ct * 4 + e][lane] = f32x4{y[4 * e] * f, y[4 * e + 1] * f, y[4 * e + 2] * f, y[4 * e + 3] * f};
     }
-    if (w == 0 && hh == 0) sp_put_sum<D>(a, rg, r, h[c], i[c], mm[c], den);
+  lds_barrier();
+  if (w >= NCT || !mine) return;
+  float den = 0.0f;
+#pragma unroll
+  for (int x = 0; x < NW; ++x) den += sums[x][li];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    f32x4 o = {};
+#pragma unroll
+    for (int x = 0; x < NW; ++x) {
+      const f32x4 y = sh.parts[x][w * 4 + e][lane];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[k] += y[k];
+    }
+    sp_put<T, D>(a, rg, r, h, i, w * kTile + row_of(4 * e, hh), o, den);
   }
+  if (w == 0 && hh == 0) sp_put_sum<D>(a, rg, r, h, i, mm, den);
 }
 
-// Blocks (bf16; more than 64 columns): a wave answers 32 columns, and the four waves of a
+// Blocks (bf16; more than 32 columns): a wave answers 32 columns, and the four waves of a
 // half share its tiles; the two halves of a workgroup take the range's tiles in turn and join
 // their sums in LDS.  A tile's codes go through registers, A tiles ahead, and into LDS as
 // bf16 values, scales included, so that each is converted once for four tiles of
@@ -750,29 +710,38 @@ __global__ __launch_bounds__(256) void hyb_q8_combine_kernel(SoftmaxPrefixArgs a
   store_out4<T>(a.out, (((size_t)b * L + i) * Hq + h) * D + c * 4, o, a.s.out_f32);
 }
 
-// Tiles of columns that a workgroup answers (32 columns each), as the kernels above.
-static int q8_columns(const Shape& s) { return s.dtype != 1 ? 1 : q8_groups(s) <= 2 ? q8_groups(s) : 4; }
-// Workgroups of a range and KV head.
-static int q8_wgs(const Shape& s) { return (q8_groups(s) + q8_columns(s) - 1) / q8_columns(s); }
-
-// Into how many ranges requests of max_seen cached tokens are cut: the least estimated
-// time (us).  The chip takes a workgroup per CU at a time; one costs its start and end
-// besides its tiles, and more ranges than one cost a merge.
-static int q8_parts(const Shape& s, int max_seen) {
-  const double tiles = std::ceil(max_seen / 32.0) + 1, wgs = (double)s.B * s.Hkv * q8_wgs(s);
-  const bool block = q8_columns(s) == 4;
-  const double tile = s.dtype != 1 ? 2.0 * s.D / 64 : block ? 0.65 : 0.4, fixed = 6.0;
-  const double rows = (double)s.B * s.Hq * s.L, row = (s.D + 2) * 8 / 2e6;  // a partial row's write and read
-  int best = 1;
+// Which kernel, its workgroups for a range and KV head, and into how many ranges requests of
+// max_seen cached tokens are cut: the least estimated time (us).  The chip takes a
+// workgroup per CU at a time; one costs its start and end besides its tiles (0.32 us of 32
+// columns and 0.53 of 128 at D = 128, 0.23 and 0.38 at 64), and more ranges than one cost a
+// merge and the partial rows.  (Measured, 4 KV heads of 4 query heads, D = 128, blocks of
+// 32, the kernel of 32 columns against that of 128 at each one's best ranges: a window of 1024
+// of 16 requests 19 and 29 us, of 24 36 and 30; of 4096 of 4 requests 28 and 29, of 16 51
+// and 42.)
+struct Q8Way {
+  bool block;
+  int wgs, ranges;
+};
+static Q8Way q8_way(const Shape& s, int max_seen) {
+  const int groups = q8_groups(s);
+  const double tiles = std::ceil(max_seen / 32.0) + 1, width = s.D == 64 ? 0.72 : 1.0;
+  const double rows = (double)s.B * s.Hq * s.L, row = (s.D + 2) * 8 / 6e6;  // a partial row's write and read
+  Q8Way best = {};
   double least = 0;
-  // one, and as many as fill the chip once, twice, ..
-  for (int rounds = 0; rounds <= 4; ++rounds) {
-    const int k = rounds == 0 ? 1 : (int)std::min(256.0 * rounds / wgs, tiles / 4);
-    if (k < 1) continue;
-    const double t = std::ceil(wgs * k / 256) * (tiles / k * tile + fixed) + (k > 1 ? 6.0 + rows * k * row : 0.0);
-    if (rounds == 0 || t < least * 0.98) {
-      least = t;
-      best = k;
+  for (int block = 0; block <= (s.dtype == 1 && groups > 1 ? 1 : 0); ++block) {
+    const int per = block ? (groups + 3) / 4 : groups;
+    const double wgs = (double)s.B * s.Hkv * per;
+    const double tile = s.dtype != 1 ? s.D / 32.0 : (block ? 0.53 : 0.32) * width, fixed = block ? 11.0 : 9.0;
+    // one, and as many as fill the chip once, twice, ..
+    for (int rounds = 0; rounds <= 4; ++rounds) {
+      const int k = rounds == 0 ? 1 : (int)std::min(256.0 * rounds / wgs, tiles / 4);
+      if (k < 1) continue;
+      const double t =
+          std::ceil(wgs * k / 256) * (std::ceil(tiles / k) * tile + fixed) + (k > 1 ? 7.0 + rows * k * row : 0.0);
+      if (least == 0 || t < least * 0.98) {
+        least = t;
+        best = {block != 0, per, k};
+      }
     }
   }
   return best;
@@ -782,24 +751,23 @@ static int q8_parts(const Shape& s, int max_seen) {
 int softmax_q8_splits(const Shape& s, int max_seen) {
   if (s.B == 0) return 1;
   const int need = (int)(((long)max_seen + s.L + kMaxRange - 1) / kMaxRange);
-  const int k = q8_parts(s, max_seen);
+  const int k = q8_way(s, max_seen).ranges;
   return k == 1 && need <= 1 ? 1 : std::max(k, need) + 1;
 }
 
 template <typename T, int D>
 static hipError_t q8_go(const SoftmaxQ8Args& a, hipStream_t st) {
-  const int wgs = q8_wgs(a.s);
+  const Q8Way way = q8_way(a.s, a.max_seen);
   SpCut cut = {};
   cut.limit = a.s.B * a.n_split;
-  const dim3 grid((unsigned)(a.s.Hkv * wgs * cut.limit));
+  const dim3 grid((unsigned)(a.s.Hkv * way.wgs * cut.limit));
   if constexpr (sizeof(T) == 2) {
-    switch (q8_columns(a.s)) {
-      case 1: hipLaunchKernelGGL((hyb_q8_token_kernel<T, D, 1>), grid, dim3(kWave * 4), 0, st, a, cut); break;
-      case 2: hipLaunchKernelGGL((hyb_q8_token_kernel<T, D, 2>), grid, dim3(kWave * 4), 0, st, a, cut); break;
-      default: hipLaunchKernelGGL((hyb_q8_block_kernel<D>), grid, dim3(kWave * 8), 0, st, a, cut);
-    }
+    if (way.block)
+      hipLaunchKernelGGL((hyb_q8_block_kernel<D>), grid, dim3(kWave * 8), 0, st, a, cut);
+    else
+      hipLaunchKernelGGL((hyb_q8_token_kernel<T, D>), grid, dim3(kWave * 4), 0, st, a, cut);
   } else {
-    hipLaunchKernelGGL((hyb_q8_token_kernel<T, D, 1>), grid, dim3(kWave * 4), 0, st, a, cut);
+    hipLaunchKernelGGL((hyb_q8_token_kernel<T, D>), grid, dim3(kWave * 4), 0, st, a, cut);
   }
   if (a.n_split == 1) return hipGetLastError();  // one range: already written out
   const long rows = (long)a.s.B * a.s.Hq * a.s.L, units = (long)a.s.B * a.s.Hq * ((a.s.L + 1024 / D - 1) / (1024 / D));
@@ -812,7 +780,10 @@ static hipError_t q8_go(const SoftmaxQ8Args& a, hipStream_t st) {
 }
 
 // Threads of the largest launch.
-double softmax_q8_threads(const SoftmaxQ8Args& a) { return 512.0 * a.s.B * a.n_split * a.s.Hkv * q8_wgs(a.s); }
+double softmax_q8_threads(const SoftmaxQ8Args& a) {
+  const Q8Way way = q8_way(a.s, a.max_seen);
+  return (way.block ? 8.0 : 4.0) * kWave * a.s.B * a.n_split * a.s.Hkv * way.wgs;
+}
 
 hipError_t launch_softmax_q8(const SoftmaxQ8Args& a, hipStream_t st) {
   if (a.s.dtype == 1) return a.s.D == 64 ? q8_go<bf16, 64>(a, st) : q8_go<bf16, 128>(a, st);
