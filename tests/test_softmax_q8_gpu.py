@@ -30,9 +30,12 @@ def make(B, L, Hq, Hkv, d, page, sb, lens, dtype, seed, window, sinks):
     g = torch.Generator().manual_seed(seed)
     r = np.random.RandomState(seed)
     per = -(-max(list(lens) + [1]) // page) + 1
-    n = B * per + 2
+    own = [-(-m // page) for m in lens]
+    n = sum(own) + 2
     rnd = lambda *s: torch.randn(*s, generator=g).to(dtype).cuda()
-    table = r.permutation(n)[:B * per].reshape(B, per)
+    table, free = np.zeros((B, per), int), r.permutation(n)
+    for b, m in enumerate(own):
+        table[b, :m], free = free[:m], free[m:]
     cache = ref.Cache(n, page, sb, Hkv, d, seed)
     keep = np.zeros((n, page), bool)
     read = np.zeros((B, per), bool)
@@ -57,6 +60,8 @@ def make(B, L, Hq, Hkv, d, page, sb, lens, dtype, seed, window, sinks):
 def expect(c, b, m):
     """(out, bound) [m, Hq, d] of request b's first m queries."""
     Hq, Hkv = c["q"].shape[2], c["k"].shape[2]
+    if m == 0:
+        return None
     j = seen(c["lens"][b], c["window"], c["sinks"])
     at = c["host"][b, j // c["page"]], j % c["page"]
     kb, vb = (np.concatenate([ref.values(*c["cache"].host[x])[at], rows64(c[x][b, :m])]) for x in "kv")
@@ -73,6 +78,7 @@ def run(c, block, **kw):
 def check(c, block=None, what=""):
     B, L = c["q"].shape[:2]
     dtype = c["q"].dtype
+    want = [expect(c, b, L if block is None else min(max(block[b], 0), L)) for b in range(B)]
     for f32 in ([False, True] if dtype == BF else [False]):
         out = torch.full_like(c["q"], 9.0, dtype=FL if f32 else dtype)
         run(c, block, out=out)
@@ -81,7 +87,7 @@ def check(c, block=None, what=""):
             m = L if block is None else min(max(block[b], 0), L)
             assert bool((out[b, m:] == 9.0).all()), f"{what}: rows past the block were written"
             if m:
-                assert_within(out[b, :m], *expect(c, b, m), out.dtype, f"{what} b={b}")
+                assert_within(out[b, :m], *want[b], out.dtype, f"{what} b={b}")
 
 
 CASES = [  # B, L, Hq, Hkv, d, page, sb, lens, window, sinks, dtype
@@ -113,6 +119,24 @@ CASES = [  # B, L, Hq, Hkv, d, page, sb, lens, window, sinks, dtype
     (1, 1, 4, 2, 64, 32, 32, [6000], 5000, 33, FL)]
 
 
+# Blocks of more workgroups of 32 columns than the chip has CUs, or long caches of several
+# requests: the kernel of 128 columns.
+BLOCKS = [
+    (6, 32, 64, 16, 128, 64, 64, [1000, 33, 640, 2048, 0, 31], 96, 32, BF),
+    (6, 32, 64, 16, 128, 64, 32, [1000, 33, 640, 2048, 0, 31], 0, 0, BF),
+    (6, 32, 64, 16, 64, 32, 32, [1000, 33, 640, 2048, 0, 31], 0, 5, BF),
+    (6, 32, 64, 16, 64, 64, 32, [1000, 33, 640, 2048, 1, 32], ALL, 0, BF),
+    (8, 29, 36, 12, 128, 32, 32, [95, 64, 0, 1, 32, 33, 300, 128], ALL, 0, BF),  # 3 tiles of columns
+    (5, 32, 72, 12, 64, 32, 32, [0, 70, 650, 31, 96], 200, 3, BF),               # 6
+    (9, 16, 64, 16, 128, 64, 64, [0, 70, 650, 31, 96, 5, 64, 63, 200], 100, 0, BF),  # 2
+    (5, 32, 64, 4, 128, 64, 64, [500, 0, 33, 64, 1], 300, 40, BF),               # 16
+    (16, 32, 16, 4, 128, 64, 64, [4000] + [(i * 97) % 300 for i in range(15)], ALL, 0, BF),  # several ranges
+    (4, 32, 16, 4, 128, 64, 32, [12000, 1, 5000, 0], ALL, 0, BF),
+    (4, 32, 16, 4, 64, 32, 32, [16000, 31, 3000, 64], ALL, 0, BF),
+    (8, 32, 16, 4, 128, 128, 64, [9000] + [(i * 53) % 200 for i in range(7)], 8500, 70, BF)]
+CASES += BLOCKS
+
+
 @pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(str(x) for x in c[:7]) + f"-{c[7][0]}-{c[8]}-{c[9]}-{str(c[10])[6:]}")
 def test_step(case):
     announce(f"softmax q8 {case}")
@@ -133,49 +157,54 @@ def test_no_cache_at_all():
 
 @pytest.mark.parametrize("window,sinks", [(1, 0), (31, 1), (32, 32), (33, 31), (64, 33), (100, 64), (5, 200), (0, 64),
                                           (0, 31), (127, 0)])
-@pytest.mark.parametrize("L", [1, 32])
-def test_edges_of_the_window(window, sinks, L):
-    announce(f"softmax q8 window {window} {sinks} {L}")
+@pytest.mark.parametrize("L,Hq,Hkv", [(1, 4, 2), (32, 4, 2), (32, 20, 10)])
+def test_edges_of_the_window(window, sinks, L, Hq, Hkv):
+    announce(f"softmax q8 window {window} {sinks} {L} {Hq}")
     lens = [0, 1, 31, 32, 33, 63, 64, 65, 96, 127, 128, 129, 160, 257]
-    check(make(len(lens), L, 4, 2, 64, 32, 32, lens, BF, window + sinks, window, sinks), what=f"{window} {sinks}")
+    check(make(len(lens), L, Hq, Hkv, 64, 32, 32, lens, BF, window + sinks, window, sinks), what=f"{window} {sinks}")
 
 
-def test_scores_that_climb_and_fall():
+@pytest.mark.parametrize("L,Hq,Hkv", [(4, 4, 1), (32, 258, 129)])
+def test_scores_that_climb_and_fall(L, Hq, Hkv):
     """Keys whose scores rise or fall along the prefix by hundreds: the reference moves
     every tile, or never."""
     announce("softmax q8 climbing")
     for sign in (1.0, -1.0):
-        c = make(1, 4, 4, 1, 64, 32, 32, [700], BF, 21, ALL, 0)
+        c = make(1, L, Hq, Hkv, 64, 32, 32, [700], BF, 21, ALL, 0)
         codes, scales = c["cache"].host["k"]
         scales[:] = 127
         codes[:] = 0
         j = np.arange(700)
-        codes[c["host"][0, j // 32], j % 32, 0, 0] = ref.encode(sign * np.minimum(448, j * 0.6))
+        codes[c["host"][0, j // 32], j % 32, :, 0] = ref.encode(sign * np.minimum(448, j * 0.6))[:, None]
         c["cache"].send()
         c["q"][..., 0] = 5.0
         check(c, what=f"climbing {sign}")
 
 
-def test_nan_where_it_is_seen():
+@pytest.mark.parametrize("L,G,Hkv", [(2, 2, 2), (32, 2, 65)])
+def test_nan_where_it_is_seen(L, G, Hkv):
     """A token whose key was not finite makes its requests' rows NaN, and no other's."""
-    announce("softmax q8 NaN")
-    c = make(2, 2, 4, 2, 64, 32, 32, [50, 50], BF, 22, ALL, 0)
+    announce(f"softmax q8 NaN {L} {Hkv}")
+    c = make(2, L, G * Hkv, Hkv, 64, 32, 32, [50, 50], BF, 22, ALL, 0)
     codes, _ = c["cache"].host["k"]
     codes[c["host"][0, 1], 3, 1, 5] = 127
     c["cache"].send()
     out = run(c, None, out_f32=True)
-    assert bool(out[0, :, 2:].isnan().all())
-    assert_within(out[0, :, :2], expect(c, 0, 2)[0][:, :2], expect(c, 0, 2)[1][:, :2], FL, "other heads")
-    assert_within(out[1], *expect(c, 1, 2), FL, "the other request")
+    assert bool(out[0, :, 2:4].isnan().all())
+    (o, e), keep = expect(c, 0, L), [h for h in range(G * Hkv) if h // G != 1]
+    assert_within(out[0][:, keep], o[:, keep], e[:, keep], FL, "other heads")
+    assert_within(out[1], *expect(c, 1, L), FL, "the other request")
 
 
-def test_same_bits_and_captured():
+@pytest.mark.parametrize("B,L,Hq,Hkv", [(3, 4, 8, 2), (20, 32, 16, 4)])
+def test_same_bits_and_captured(B, L, Hq, Hkv):
     """Twice the same bits; a captured call takes the lengths of each replay."""
-    announce("softmax q8 captured")
-    c = make(3, 4, 8, 2, 128, 64, 64, [3000, 500, 0], BF, 23, ALL, 0)
+    announce(f"softmax q8 captured {B} {L}")
+    more = [0] * (B - 3)
+    c = make(B, L, Hq, Hkv, 128, 64, 64, [3000, 500, 0] + more, BF, 23, ALL, 0)
     lens, out = i32(c["lens"]), torch.zeros_like(c["q"])
     args = (c["q"], c["k"], c["v"], *c["cache"].args, c["table"], lens, ALL)
-    need = hb.workspace_bytes(hb.make_dims(3, 8, 2, 128, 4, 64, hb.HYB_BF16, 1), hb.OP_WINDOW_STEP_Q8,
+    need = hb.workspace_bytes(hb.make_dims(B, Hq, Hkv, 128, L, 64, hb.HYB_BF16, 1), hb.OP_WINDOW_STEP_Q8,
                               c["table"].shape[1] * 64)
     ws = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
     s = torch.cuda.Stream()
@@ -187,6 +216,7 @@ def test_same_bits_and_captured():
     with torch.cuda.graph(g):
         hb.softmax_window_step_paged_q8(*args, out=out, ws=ws)
     for now in ([3000, 500, 0], [100, 499, 0], [2999, 1, 0], [3000, 500, 0]):
+        now = now + more
         lens.copy_(i32(now))
         out.zero_()
         g.replay()
@@ -195,4 +225,4 @@ def test_same_bits_and_captured():
         assert torch.equal(out, eager)
         c["lens"] = now
         for b in range(3):
-            assert_within(out[b], *expect(c, b, 4), BF, f"replay {now} {b}")
+            assert_within(out[b], *expect(c, b, L), BF, f"replay {now} {b}")
