@@ -371,6 +371,60 @@ __device__ inline WinUnit win_unit(const WindowArgs& a, int len, int g, int u) {
   return WinUnit{g * G + u % G, i0, i0 < len};
 }
 
+// A wave's 32 queries take the keys j0 .. j0 + 31 (`full`, uniform: every query sees every one): m is the
+// reference of the weights in the log2 domain, l their sum, acc the weighted sums of V^T.
+template <int D>
+__device__ inline void win_take(typename WinF32<D>::Acc& acc, float& m, float& l, const typename WinF32<D>::Tile& kt,
+                                const typename WinF32<D>::Tile& vt, const float* qop, const WinRow& row, bool full,
+                                int sinks, int j0, float scale, int li, int hh) {
+  f32x16 sc = win_rows_mma<D>(kt, qop, li, hh);
+  if (!full) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sc[e] = row.sees(j0 + row_of(e, hh), sinks) ? sc[e] : -INFINITY;
+  }
+  float p[16], mt = sc[0];
+#pragma unroll
+  for (int e = 1; e < 16; ++e) mt = fmaxf(mt, sc[e]);
+  mt = fmaxf(mt, xor32(mt)) * scale;
+  const float mn = fmaxf(m, mt);
+  if (__any(mn > m)) {
+    mma_settle<float>();
+    const float corr = __builtin_amdgcn_exp2f(m - mn);
+    l *= corr;
+#pragma unroll
+    for (int ct = 0; ct < WinF32<D>::NCT; ++ct)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[ct][e] *= corr;
+    m = mn;
+  }
+  float ps = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale, -m));
+    ps += p[e];
+  }
+  l += ps + xor32(ps);
+  win_cols_mma<D>(acc, vt, p, li, hh);
+  mma_settle<float>();
+}
+// The same for dQ: weights from the rows' lse (log2), times dP - delta.
+template <int D>
+__device__ inline void win_take_dq(typename WinF32<D>::Acc& acc, const typename WinF32<D>::Tile& kt,
+                                   const typename WinF32<D>::Tile& vt, const float* qop, const float* dop, const WinRow& row,
+                                   bool full, int sinks, int j0, float scale, float lse, float delta, int li, int hh) {
+  f32x16 sc = win_rows_mma<D>(kt, qop, li, hh);
+  const f32x16 dp = win_rows_mma<D>(vt, dop, li, hh);
+  if (!full) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sc[e] = row.sees(j0 + row_of(e, hh), sinks) ? sc[e] : -INFINITY;
+  }
+  float ds[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) ds[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale, -lse)) * (dp[e] - delta);
+  win_cols_mma<D>(acc, kt, ds, li, hh);
+  mma_settle<float>();
+}
+
 // Forward, of U units per workgroup.  With H = 2 two halves of U waves take a unit's tiles in turn, each
 // through buffers of its own, and join their sums in LDS: a CU that holds one
 // workgroup has two waves per SIMD then, and one's products run beside the other's
@@ -426,37 +480,8 @@ __global__ __launch_bounds__(kWave* U* H) void hyb_win_fwd_kernel(A a, int wgs) 
   for (int n = 0; n < nsteps; ++n) {
     const int buf = n & 1, j0 = n < mine ? key(n) : 0;
     if (n + 1 < mine) win_fetch<D, U>(next, K, V, ks_, vs_, key(n + 1), len, t);
-    if (me.any && n < mine && !win_none(r0, r1, a.n_sinks, j0, kTile)) {  // uniform over the wave
-      f32x16 sc = win_rows_mma<D>(kt[buf], qop, li, hh);
-      if (!win_full(r0, r1, a.n_sinks, j0, kTile)) {  // uniform
-#pragma unroll
-        for (int e = 0; e < 16; ++e) sc[e] = row.sees(j0 + row_of(e, hh), a.n_sinks) ? sc[e] : -INFINITY;
-      }
-      float p[16], mt = sc[0];
-#pragma unroll
-      for (int e = 1; e < 16; ++e) mt = fmaxf(mt, sc[e]);
-      mt = fmaxf(mt, xor32(mt)) * scale;
-      const float mn = fmaxf(m, mt);
-      if (__any(mn > m)) {
-        mma_settle<float>();
-        const float corr = __builtin_amdgcn_exp2f(m - mn);
-        l *= corr;
-#pragma unroll
-        for (int ct = 0; ct < C::NCT; ++ct)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) acc[ct][e] *= corr;
-        m = mn;
-      }
-      float ps = 0.0f;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale, -m));
-        ps += p[e];
-      }
-      l += ps + xor32(ps);
-      win_cols_mma<D>(acc, vt[buf], p, li, hh);
-      mma_settle<float>();
-    }
+    if (me.any && n < mine && !win_none(r0, r1, a.n_sinks, j0, kTile))  // uniform over the wave
+      win_take<D>(acc, m, l, kt[buf], vt[buf], qop, row, win_full(r0, r1, a.n_sinks, j0, kTile), a.n_sinks, j0, scale, li, hh);
     if (n + 1 < mine) win_put<D, U>(next, kt[buf ^ 1], vt[buf ^ 1], key(n + 1), len, t);
     __syncthreads();
   }
@@ -535,20 +560,9 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dq_kernel(A a, int w
     for (int n = 0; n < tl.n; ++n) {
       const int j0 = tl.first(n, kTile), buf = n & 1;
       if (n + 1 < tl.n) win_fetch<D>(next, K, V, ks_, vs_, tl.first(n + 1, kTile), len, threadIdx.x);
-      if (me.any && !win_none(r0, r1, a.n_sinks, j0, kTile)) {
-        f32x16 sc = win_rows_mma<D>(kt[buf], qop, li, hh);
-        const f32x16 dp = win_rows_mma<D>(vt[buf], dop, li, hh);
-        if (!win_full(r0, r1, a.n_sinks, j0, kTile)) {  // uniform
-#pragma unroll
-          for (int e = 0; e < 16; ++e) sc[e] = row.sees(j0 + row_of(e, hh), a.n_sinks) ? sc[e] : -INFINITY;
-        }
-        float ds[16];
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          ds[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale, -lse)) * (dp[e] - delta);
-        win_cols_mma<D>(acc, kt[buf], ds, li, hh);
-        mma_settle<float>();
-      }
+      if (me.any && !win_none(r0, r1, a.n_sinks, j0, kTile))
+        win_take_dq<D>(acc, kt[buf], vt[buf], qop, dop, row, win_full(r0, r1, a.n_sinks, j0, kTile), a.n_sinks, j0, scale,
+                       lse, delta, li, hh);
       if (n + 1 < tl.n) win_put<D>(next, kt[buf ^ 1], vt[buf ^ 1], tl.first(n + 1, kTile), len, threadIdx.x);
       __syncthreads();
     }
@@ -556,6 +570,151 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dq_kernel(A a, int w
   if (me.i0 + li >= sq.cap) return;  // rows past the length: zero
   win_store<float, D>(a.dq, sq.row(me.i0 + li) * Hq + me.h, acc,
                       me.i0 + li < len ? 1.0f / sqrtf((float)D) : 0.0f, hh, true);
+}
+
+// Few units: a workgroup per unit, whose waves take the unit's tiles in turn, each through a pair
+// of tiles of its own (no barrier in the loop), and join their sums in LDS.
+template <int D>
+struct WinFew {
+  typedef WinF32<D, 1> C;
+  static constexpr int NW = kWinWaves, NCT = C::NCT;
+  union {
+    struct {
+      typename C::Tile k[NW], v[NW];
+    } tiles;
+    f32x4 parts[NW][NCT * 4][kWave];
+  };
+  float m[NW][kTile], l[NW][kTile];
+  __device__ WinFew() {}
+  // This wave's tiles: number w, w + 4, .. of the list, each handed to f(j0) in LDS.
+  template <typename F>
+  __device__ __attribute__((always_inline)) inline void each(const WinTiles& tl, const float* K, const float* V, size_t ks,
+                                                             size_t vs, int len, int w, int lane, F f) {
+    if (w >= tl.n) return;
+    typename C::Regs next;
+    win_fetch<D, 1>(next, K, V, ks, vs, tl.first(w, kTile), len, lane);
+    for (int n = w; n < tl.n; n += NW) {
+      const int j0 = tl.first(n, kTile);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the tiles have been read
+      win_put<D, 1>(next, tiles.k[w], tiles.v[w], j0, len, lane);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // and are there
+      if (n + NW < tl.n) win_fetch<D, 1>(next, K, V, ks, vs, tl.first(n + NW, kTile), len, lane);
+      f(j0);
+    }
+  }
+  // The waves' sums, times f each, joined: wave w stores NCT of the row's 4 NCT pieces.  The tiles are free.
+  __device__ __attribute__((always_inline)) inline void join(const typename C::Acc& acc, float f, int w, int lane) {
+#pragma unroll
+    for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        parts[w][ct * 4 + e][lane] =
+            f32x4{acc[ct][4 * e] * f, acc[ct][4 * e + 1] * f, acc[ct][4 * e + 2] * f, acc[ct][4 * e + 3] * f};
+    __syncthreads();
+  }
+  __device__ __attribute__((always_inline)) inline void store(void* out, size_t row, float f, int w, int lane) const {
+#pragma unroll
+    for (int u = 0; u < NCT; ++u) {
+      const int x = w * NCT + u;
+      float o[4] = {};
+#pragma unroll
+      for (int y = 0; y < NW; ++y) {
+        const f32x4 z = parts[y][x][lane];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[k] += z[k];
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[k] *= f;
+      store_out4<float>(out, row * D + x / 4 * kTile + row_of(x % 4 * 4, lane >> 5), o, true);
+    }
+  }
+};
+
+template <typename A>
+__global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_fwd_few_kernel(A a, int wgs) {
+  constexpr int D = 64;
+  typedef WinF32<D, 1> C;
+  __shared__ alignas(16) WinFew<D> sh;
+  const int lane = threadIdx.x & (kWave - 1), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int li = lane & 31, hh = lane >> 5;
+  int g, x;
+  const WinSeq<A> sq = win_of_queries<1>(a, wgs, lane, g, x);
+  const int len = sq.len;
+  const WinUnit me = win_unit(a, len, g, x);
+  if (!me.any) return;  // uniform
+  const int i = min(me.i0 + li, len - 1), end = min(me.i0 + kTile, len);
+  const WinTiles tl(a, len, me.i0, end, kTile);
+  const WinRow row(a, len, i), r0(a, len, me.i0), r1(a, len, end - 1);
+  typename C::Ops qop;
+  win_row_ops<D>(qop, (const float*)a.q + sq.q(me.h, D) + i * sq.qs(D), true, hh);
+  const float scale = kLog2e / sqrtf((float)D);
+  float m = kNoRef, l = 0.0f;
+  typename C::Acc acc;
+#pragma unroll
+  for (int ct = 0; ct < C::NCT; ++ct) acc[ct] = f32x16{};
+  sh.each(tl, (const float*)a.k + sq.k(g, D), (const float*)a.v + sq.v(g, D), sq.ks(D), sq.vs(D), len, w, lane,
+          [&](int j0) __attribute__((always_inline)) {
+            win_take<D>(acc, m, l, sh.tiles.k[w], sh.tiles.v[w], qop, row, win_full(r0, r1, a.n_sinks, j0, kTile),
+                        a.n_sinks, j0, scale, li, hh);
+          });
+  mma_settle<float>();
+  if (hh == 0) sh.m[w][li] = m;
+  __syncthreads();  // (and the tiles are free)
+  float mm = sh.m[0][li];
+#pragma unroll
+  for (int y = 1; y < kWinWaves; ++y) mm = fmaxf(mm, sh.m[y][li]);
+  const float f = __builtin_amdgcn_exp2f(m - mm);
+  if (hh == 0) sh.l[w][li] = l * f;
+  sh.join(acc, f, w, lane);
+  l = 0.0f;
+#pragma unroll
+  for (int y = 0; y < kWinWaves; ++y) l += sh.l[y][li];
+  if (me.i0 + li >= len) return;
+  sh.store(a.out, sq.row(i) * a.s.Hq + me.h, 1.0f / l, w, lane);
+  if (a.lse && w == 0 && hh == 0) a.lse[sq.lse(me.h, i)] = (mm + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
+template <typename A>
+__global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dq_few_kernel(A a, int wgs) {
+  constexpr int D = 64;
+  typedef WinF32<D, 1> C;
+  __shared__ alignas(16) WinFew<D> sh;
+  const int lane = threadIdx.x & (kWave - 1), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int li = lane & 31, hh = lane >> 5, Hq = a.s.Hq;
+  int g, x;
+  const WinSeq<A> sq = win_of_queries<1>(a, wgs, lane, g, x);
+  const int len = sq.len;
+  const WinUnit me = win_unit(a, len, g, x);
+  typename C::Acc acc;
+#pragma unroll
+  for (int ct = 0; ct < C::NCT; ++ct) acc[ct] = f32x16{};
+  if (me.any) {  // uniform
+    const int i = min(me.i0 + li, len - 1), end = min(me.i0 + kTile, len);
+    const WinTiles tl(a, len, me.i0, end, kTile);
+    const WinRow row(a, len, i), r0(a, len, me.i0), r1(a, len, end - 1);
+    typename C::Ops qop, dop;
+    const size_t at = sq.dout(me.h, D) + (size_t)i * Hq * D;
+    win_row_ops<D>(qop, (const float*)a.q + sq.q(me.h, D) + i * sq.qs(D), true, hh);
+    win_row_ops<D>(dop, (const float*)a.dout + at, true, hh);
+    float delta = 0.0f;
+#pragma unroll
+    for (int ks = 0; ks < C::KD; ++ks) delta += dop[ks] * ((const float*)a.out)[at + win_entry(ks, hh)];
+    delta += xor32(delta);
+    const float scale = kLog2e / sqrtf((float)D);
+    const size_t st = sq.lse(me.h, i);
+    const float lse = a.lse[st] * kLog2e;
+    if (w == 0 && hh == 0 && me.i0 + li < len) a.ws[st] = delta;
+    sh.each(tl, (const float*)a.k + sq.k(g, D), (const float*)a.v + sq.v(g, D), sq.ks(D), sq.vs(D), len, w, lane,
+            [&](int j0) __attribute__((always_inline)) {
+              win_take_dq<D>(acc, sh.tiles.k[w], sh.tiles.v[w], qop, dop, row, win_full(r0, r1, a.n_sinks, j0, kTile),
+                             a.n_sinks, j0, scale, lse, delta, li, hh);
+            });
+    mma_settle<float>();
+  }
+  __syncthreads();  // (the tiles are free)
+  sh.join(acc, 1.0f, w, lane);
+  if (me.i0 + li >= sq.cap) return;  // rows past the length: zero
+  sh.store(a.dq, sq.row(me.i0 + li) * Hq + me.h, me.i0 + li < len ? 1.0f / sqrtf((float)D) : 0.0f, w, lane);
 }
 
 // The queries that see some of the keys j0 .. j1 - 1 (j1 <= len): from q0 to q1 - 1.
@@ -1410,14 +1569,31 @@ static hipError_t win_ring_go(const A& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+// Whether n units of packed sequences (fp32, d = 64) have a workgroup each: where lists are long
+// and units few.  (us of a forward and a gradient so and otherwise: 5 sequences of 140 to 701, 8
+// heads, 545 units, 32 and 58, 141 and 189; 1 of 2048, 516, 74 and 103, 219 and 363; 16 of 64 to 1024,
+// 2240, 99 and 117, 351 and 377; but 16 of 128 to 2048, 4416, 295 and 273, and 20 of 5 to 100, 18.7
+// and 15.7.  At d = 128 a wave's tiles on their way need more registers than there are.)
+static bool win_few(const PackedArgs& a, int n) {
+  const long seen = std::min<long>(a.T, (long)a.window + std::min(a.n_sinks, a.T) + a.s.L);
+  return n <= 2560 && seen >= 8 * kTile;
+}
+
 template <int D, typename A>
 static hipError_t win_prefill_f32_go(const A& a, hipStream_t st) {
   const WinGrid<A> gr(a);
   const dim3 grid((unsigned)gr.n);
   if constexpr (std::is_same_v<A, PackedArgs>) {
+    if constexpr (D == 64) {
+      const WinGrid<A> one(a, 1);
+      if (win_few(a, one.busy)) {
+        hipLaunchKernelGGL((hyb_win_fwd_few_kernel<A>), dim3((unsigned)one.n), dim3(kWave * kWinWaves), 0, st, a, one.wgs);
+        return hipGetLastError();
+      }
+    }
     // Two units per workgroup while those have a CU each: a SIMD then has one wave of a
-    // step's products, not two (5 sequences of 1 to 701, 8 heads of d = 64: 56 us with four
-    // units).
+    // step's products, not two (16 heads of d = 128, 1 sequence of 1024: 146 us with four
+    // units, 95 with two; of 125 26 and 18).
     const WinGrid<A> two(a, 2);
     if (two.busy <= 256) {
       hipLaunchKernelGGL((hyb_win_fwd_kernel<D, 2, A, 2>), dim3((unsigned)two.n), dim3(kWave * 4), 0, st, a, two.wgs);
@@ -1519,7 +1695,14 @@ static void win_backward_kernels(const A& a, const WinParts& cut, hipStream_t st
     }
     if (D == 128 || cut.halves) hipLaunchKernelGGL((hyb_win_dkv_ring_kernel<D, 2, A>), gk, dim3(kWave * 8), 0, st, a, cut);
   } else {
-    hipLaunchKernelGGL((hyb_win_dq_kernel<D, A>), gq, dim3(kWave * kWinWaves), 0, st, a, gr.wgs);
+    bool few = false;
+    if constexpr (D == 64 && std::is_same_v<A, PackedArgs>) {
+      const WinGrid<A> one(a, 1);
+      few = win_few(a, one.busy);
+      if (few)
+        hipLaunchKernelGGL((hyb_win_dq_few_kernel<A>), dim3((unsigned)one.n), dim3(kWave * kWinWaves), 0, st, a, one.wgs);
+    }
+    if (!few) hipLaunchKernelGGL((hyb_win_dq_kernel<D, A>), gq, dim3(kWave * kWinWaves), 0, st, a, gr.wgs);
     hipLaunchKernelGGL((hyb_win_dkv_kernel<D, A>), gk, dim3(kWave * kWinWaves), 0, st, a, cut);
   }
 }
@@ -1563,6 +1746,17 @@ static size_t packed_stats_bytes(const Shape& s, int N) {
   if (s.dtype != 1) return ((size_t)s.Hq * N * sizeof(float) + 255) / 256 * 256;
   return (size_t)s.Hq * win_packed_tiles(N, s.B + 1) * kTile * 32;
 }
+// Parts at most: as win_most_parts, but in fp32, where a query tile takes 6 us at d = 64 and 12 at
+// 128, down to one each while the lists have a CU each or little more (a call for 1 sequence of
+// 125, 32 heads of d = 128, 135 us with 8 tiles at least, 72 so; 20 of 5 to 100, 16 heads of d = 64,
+// 121 and 66).
+static int packed_most_parts(const Shape& s, int N) {
+  const int T = packed_mean(s, N);
+  const long all = (long)s.B * s.Hkv * ((T + kWinKeys - 1) / kWinKeys);
+  const long every = ((long)T + kTile - 1) / kTile * (s.Hq / s.Hkv);
+  const long least = s.dtype == 1 ? every / 8 : std::max(every / 8, std::min(every, 768 / all));
+  return (int)std::max<long>(1, std::min<long>({16, 1024 / all, least}));
+}
 static size_t packed_sums_bytes(const Shape& s, int N, int parts) {
   return parts > 1 ? (size_t)parts * N * 2 * s.Hkv * s.D * sizeof(float) : 0;
 }
@@ -1585,9 +1779,10 @@ static WinParts packed_cut(const Shape& s, int N, int window) {
   for (int h = f32 || s.D == 64 ? 1 : 2; h <= (f32 ? 1 : 2); ++h) {
     const double unit = f32 ? 6.0 * s.D / 64 : s.D == 128 ? 0.75 : h == 1 ? 0.65 : 0.4;
     const double fixed = f32 || s.D == 128 ? 6.0 : h == 1 ? 1.0 : 2.5;
-    for (int p = 1; p <= win_most_parts(s, mean_len); ++p) {
+    for (int p = 1; p <= packed_most_parts(s, N); ++p) {
       const double rounds = f32 || h == 2 ? std::ceil(all * p / 256) : std::max(1.0, all * p / 450);
-      const double t = rounds * fixed + G * unit / p * std::max(seen, rounds * mean) + (p > 1 ? launch + p * sum : 0);
+      const double steps = f32 ? std::ceil(G * seen / p) : G * seen / p;  // (a step of fp32 is long)
+      const double t = rounds * fixed + unit * steps * std::max(1.0, rounds * mean / seen) + (p > 1 ? launch + p * sum : 0);
       if (c.p == 0 || t < best) {
         best = t;
         c.p = p;
@@ -1625,12 +1820,12 @@ hipError_t launch_packed_backward(const PackedArgs& a_, hipStream_t st) {
 
 double packed_threads(const Shape& s, int N) {
   const double queries = (double)win_packed_queries(N, s.B + 1, s.Hq / s.Hkv, 2);
-  const double keys = (double)win_packed_keys(N, s.B + 1) * win_most_parts(s, packed_mean(s, N));
+  const double keys = (double)win_packed_keys(N, s.B + 1) * packed_most_parts(s, N);
   return kWave * kWinWaves * 2.0 * s.Hkv * std::max(queries, keys);
 }
 
 size_t packed_backward_ws_bytes(const Shape& s, int N) {
-  return packed_stats_bytes(s, N) + packed_sums_bytes(s, N, win_most_parts(s, packed_mean(s, N)));
+  return packed_stats_bytes(s, N) + packed_sums_bytes(s, N, packed_most_parts(s, N));
 }
 
 // Threads of the largest launch (the grid's limit is checked by the caller): a

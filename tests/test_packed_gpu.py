@@ -92,7 +92,11 @@ LONG = [
     ([3, 1300, 2, 1100], 2, 1, 128, 1, 300, 200, BF, 0),
     ([20] * 60 + [900], 8, 2, 64, 1, ALL, 0, BF, 0),
     ([900, 5], 4, 1, 128, 1, ALL, 0, FL, 0),
-    ([700, 600], 4, 4, 64, 32, 200, 64, FL, 3)]
+    ([700, 600], 4, 4, 64, 32, 200, 64, FL, 3),
+    ([701, 1, 300, 33, 257], 8, 4, 64, 1, ALL, 0, FL, 13),  # few units: a workgroup each
+    ([600], 12, 4, 64, 7, ALL, 0, FL, 0),
+    ([500, 480], 3, 1, 64, 1, 100, 170, FL, 2),
+    ([125], 16, 2, 128, 1, ALL, 4, FL, 0)]                   # 16 parts
 
 
 @pytest.mark.parametrize("case", CASES + LONG, ids=str)
