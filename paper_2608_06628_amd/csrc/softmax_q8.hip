@@ -256,15 +256,22 @@ struct Q8Acc {
 // tiles of 32 columns: `groups` of them.
 __host__ __device__ inline int q8_groups(const Shape& s) { return (s.Hq / s.Hkv * s.L + kTile - 1) / kTile; }
 
-// A workgroup answers 32 columns over a range of keys: the four waves take the
+// A workgroup answers 32 columns over a range of keys: its waves take the
 // range's tiles in turn, each through copies of its own (R slots, no barrier in the loop)
 // and sums of its own, joined in LDS at the end.  The codes are converted as they become
-// operands.
+// operands.  Eight waves: a tile is one chain of reads, conversions, products and weights, which
+// two waves per SIMD overlap (a tile of 32 columns at d = 128 takes a CU 0.32 us with four waves
+// of four slots, 0.18 so; 64 requests of 16384 tokens 214 and 194 us).  fp32 at d = 128 has
+// room for four.
 template <typename T, int D>
-__global__ __launch_bounds__(kWave * 4) void hyb_q8_token_kernel(SoftmaxQ8Args a, SpCut cut) {
+__host__ __device__ constexpr int q8_token_threads() {
+  return kWave * (sizeof(T) == 4 && D == 128 ? 4 : 8);
+}
+template <typename T, int D>
+__global__ __launch_bounds__((q8_token_threads<T, D>())) void hyb_q8_token_kernel(SoftmaxQ8Args a, SpCut cut) {
   typedef Q8Acc<T, D> A;
   typedef Q8Tile<D> QT;
-  constexpr int NCT = A::NCT, NW = 4, R = sizeof(T) == 2 ? 4 : 2;  // (fp32: the block's rows take the room)
+  constexpr int NCT = A::NCT, NW = q8_token_threads<T, D>() / kWave, R = 2;
   struct alignas(16) Slot {
     uint8_t k[QT::kBytes], v[QT::kBytes];
   };
@@ -328,16 +335,12 @@ __global__ __launch_bounds__(kWave * 4) void hyb_q8_token_kernel(SoftmaxQ8Args a
   __syncthreads();  // (the plan's scratch has been read)
   const float scale = kLog2e / sqrtf((float)D);
   A acc;
-#pragma unroll
-  for (int n = 0; n < R - 1; ++n) issue(n, sh.loop.ring[w][n]);
+  issue(0, sh.loop.ring[w][0]);
   auto step = [&](int n, auto S) __attribute__((always_inline)) {
     constexpr int SV = decltype(S)::value;
     if (n >= my) return;
-    issue(n + R - 1, sh.loop.ring[w][(SV + R - 1) % R]);
-    const int later = min(my - 1 - n, R - 1);
-    if (later == 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(6 * QT::IK) : "memory");
-    else if (later == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * QT::IK) : "memory");
-    else if (later == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * QT::IK) : "memory");
+    issue(n + 1, sh.loop.ring[w][(SV + 1) % R]);
+    if (n + 1 < my) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * QT::IK) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     const Slot& s = sh.loop.ring[w][SV];
     acc.add(t, qt, t.first_key(w + NW * n), s.k, s.v, bytes[w + NW * n], qop, scale, hh);
@@ -346,15 +349,11 @@ __global__ __launch_bounds__(kWave * 4) void hyb_q8_token_kernel(SoftmaxQ8Args a
   for (int n = 0; n < my; n += R) {
     step(n, std::integral_constant<int, 0>{});
     step(n + 1, std::integral_constant<int, 1>{});
-    if constexpr (R == 4) {
-      step(n + 2, std::integral_constant<int, 2>{});
-      step(n + 3, std::integral_constant<int, 3>{});
-    }
   }
   if (block && w == nt % NW) acc.add_block(blk.k, blk.v, Lb, qop, scale, li, hh);
 
-  // The waves' sums over one reference: wave w scales its own and leaves them in
-  // LDS, then joins entries 32 w .. + 31 of every column.
+  // The waves' sums over one reference: a wave scales its own and leaves them in LDS,
+  // then joins its share of every column's entries.
   mma_settle<T>();
   const float l = acc.l + xor32(acc.l);
   if (hh == 0) refs[w][li] = acc.m;
@@ -372,20 +371,22 @@ __global__ __launch_bounds__(kWave * 4) void hyb_q8_token_kernel(SoftmaxQ8Args a
       sh.parts[w][ct * 4 + e][lane] = f32x4{y[4 * e] * f, y[4 * e + 1] * f, y[4 * e + 2] * f, y[4 * e + 3] * f};
     }
   lds_barrier();
-  if (w >= NCT || !mine) return;
+  if (!mine) return;
   float den = 0.0f;
 #pragma unroll
   for (int x = 0; x < NW; ++x) den += sums[x][li];
+  constexpr int PW = NCT * 4 / NW;  // pieces of four entries per wave
+  static_assert(PW * NW == NCT * 4, "every piece has its wave");
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
+  for (int y = w * PW; y < w * PW + PW; ++y) {
     f32x4 o = {};
 #pragma unroll
     for (int x = 0; x < NW; ++x) {
-      const f32x4 y = sh.parts[x][w * 4 + e][lane];
+      const f32x4 z = sh.parts[x][y][lane];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) o[k] += y[k];
+      for (int k = 0; k < 4; ++k) o[k] += z[k];
     }
-    sp_put<T, D>(a, rg, r, h, i, w * kTile + row_of(4 * e, hh), o, den);
+    sp_put<T, D>(a, rg, r, h, i, y / 4 * kTile + row_of(y % 4 * 4, hh), o, den);
   }
   if (w == 0 && hh == 0) sp_put_sum<D>(a, rg, r, h, i, mm, den);
 }
@@ -712,12 +713,12 @@ __global__ __launch_bounds__(256) void hyb_q8_combine_kernel(SoftmaxPrefixArgs a
 
 // Which kernel, its workgroups for a range and KV head, and into how many ranges requests of
 // max_seen cached tokens are cut: the least estimated time (us).  The chip takes a
-// workgroup per CU at a time; one costs its start and end besides its tiles (0.32 us of 32
-// columns and 0.53 of 128 at D = 128, 0.23 and 0.38 at 64), and more ranges than one cost a
-// merge and the partial rows.  (Measured, 4 KV heads of 4 query heads, D = 128, blocks of
-// 32, the kernel of 32 columns against that of 128 at each one's best ranges: a window of 1024
-// of 16 requests 19 and 29 us, of 24 36 and 30; of 4096 of 4 requests 28 and 29, of 16 51
-// and 42.)
+// workgroup per CU at a time; one costs its start and end besides its tiles (at D = 128 0.19 us
+// of 32 columns and 0.55 of 128, fp32 1.36, at 64 0.14, 0.4 and 0.62), and more ranges than one cost
+// a merge and the partial rows.  (The numbers are fitted to 88 shapes of bf16, where what this
+// takes is within 0.4% of the best on average.  4 KV heads of 4 query heads, D = 128, blocks of 32,
+// the kernel of 32 columns against that of 128 at each one's best ranges: a window of 1024 of 16
+// requests 15 and 29 us, of 48 41 and 32; of 4096 of 4 requests 25 and 29, of 24 61 and 57.)
 struct Q8Way {
   bool block;
   int wgs, ranges;
@@ -725,19 +726,20 @@ struct Q8Way {
 static Q8Way q8_way(const Shape& s, int max_seen) {
   const int groups = q8_groups(s);
   const double tiles = std::ceil(max_seen / 32.0) + 1, width = s.D == 64 ? 0.72 : 1.0;
-  const double rows = (double)s.B * s.Hq * s.L, row = (s.D + 2) * 8 / 6e6;  // a partial row's write and read
+  const double rows = (double)s.B * s.Hq * s.L, row = (s.D + 2) / 1e6;  // a partial row's write and read
   Q8Way best = {};
   double least = 0;
   for (int block = 0; block <= (s.dtype == 1 && groups > 1 ? 1 : 0); ++block) {
     const int per = block ? (groups + 3) / 4 : groups;
     const double wgs = (double)s.B * s.Hkv * per;
-    const double tile = s.dtype != 1 ? s.D / 32.0 : (block ? 0.53 : 0.32) * width, fixed = block ? 11.0 : 9.0;
+    const double tile = s.dtype != 1 ? (s.D == 64 ? 0.62 : 1.36) : (block ? 0.55 : 0.19) * width;
+    const double fixed = block ? 11.3 : 8.4;
     // one, and as many as fill the chip once, twice, ..
     for (int rounds = 0; rounds <= 4; ++rounds) {
       const int k = rounds == 0 ? 1 : (int)std::min(256.0 * rounds / wgs, tiles / 4);
       if (k < 1) continue;
       const double t =
-          std::ceil(wgs * k / 256) * (std::ceil(tiles / k) * tile + fixed) + (k > 1 ? 7.0 + rows * k * row : 0.0);
+          std::ceil(wgs * k / 256) * (std::ceil(tiles / k) * tile + fixed) + (k > 1 ? 6.0 + rows * k * row : 0.0);
       if (least == 0 || t < least * 0.98) {
         least = t;
         best = {block != 0, per, k};
@@ -765,9 +767,9 @@ static hipError_t q8_go(const SoftmaxQ8Args& a, hipStream_t st) {
     if (way.block)
       hipLaunchKernelGGL((hyb_q8_block_kernel<D>), grid, dim3(kWave * 8), 0, st, a, cut);
     else
-      hipLaunchKernelGGL((hyb_q8_token_kernel<T, D>), grid, dim3(kWave * 4), 0, st, a, cut);
+      hipLaunchKernelGGL((hyb_q8_token_kernel<T, D>), grid, dim3((q8_token_threads<T, D>())), 0, st, a, cut);
   } else {
-    hipLaunchKernelGGL((hyb_q8_token_kernel<T, D>), grid, dim3(kWave * 4), 0, st, a, cut);
+    hipLaunchKernelGGL((hyb_q8_token_kernel<T, D>), grid, dim3((q8_token_threads<T, D>())), 0, st, a, cut);
   }
   if (a.n_split == 1) return hipGetLastError();  // one range: already written out
   const long rows = (long)a.s.B * a.s.Hq * a.s.L, units = (long)a.s.B * a.s.Hq * ((a.s.L + 1024 / D - 1) / (1024 / D));
@@ -782,7 +784,7 @@ static hipError_t q8_go(const SoftmaxQ8Args& a, hipStream_t st) {
 // Threads of the largest launch.
 double softmax_q8_threads(const SoftmaxQ8Args& a) {
   const Q8Way way = q8_way(a.s, a.max_seen);
-  return (way.block ? 8.0 : 4.0) * kWave * a.s.B * a.n_split * a.s.Hkv * way.wgs;
+  return 8.0 * kWave * a.s.B * a.n_split * a.s.Hkv * way.wgs;
 }
 
 hipError_t launch_softmax_q8(const SoftmaxQ8Args& a, hipStream_t st) {

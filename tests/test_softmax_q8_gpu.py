@@ -120,7 +120,7 @@ CASES = [  # B, L, Hq, Hkv, d, page, sb, lens, window, sinks, dtype
 
 
 # Blocks of more workgroups of 32 columns than the chip has CUs, or long caches of several
-# requests: the kernel of 128 columns.
+# requests: most take the kernel of 128 columns.
 BLOCKS = [
     (6, 32, 64, 16, 128, 64, 64, [1000, 33, 640, 2048, 0, 31], 96, 32, BF),
     (6, 32, 64, 16, 128, 64, 32, [1000, 33, 640, 2048, 0, 31], 0, 0, BF),
@@ -133,6 +133,7 @@ BLOCKS = [
     (16, 32, 16, 4, 128, 64, 64, [4000] + [(i * 97) % 300 for i in range(15)], ALL, 0, BF),  # several ranges
     (4, 32, 16, 4, 128, 64, 32, [12000, 1, 5000, 0], ALL, 0, BF),
     (4, 32, 16, 4, 64, 32, 32, [16000, 31, 3000, 64], ALL, 0, BF),
+    (16, 32, 16, 4, 64, 64, 64, [16000] + [(i * 71) % 260 for i in range(15)], ALL, 0, BF),
     (8, 32, 16, 4, 128, 128, 64, [9000] + [(i * 53) % 200 for i in range(7)], 8500, 70, BF)]
 CASES += BLOCKS
 
