@@ -58,6 +58,11 @@ struct Q8Tile {
   }
 };
 
+// As buf_to_lds16, past the caches: for what no one else reads.
+__device__ inline void buf_to_lds16_once(__amdgpu_buffer_rsrc_t r, void* lds, int voff) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)lds, 16, voff, 0, 0, 2);
+}
+
 // A range's tiles: where they are and how a wave copies one.
 template <int D>
 struct Q8Tiles {
@@ -117,6 +122,7 @@ struct Q8Tiles {
     return j - j0;
   }
   // K (kv = 0) or V of the tile at j0 into dst; 16 bytes per lane and copy.
+  template <bool ONCE>
   __device__ inline void copy(int kv, int j0, uint8_t* dst, int lane) const {
     const size_t row0 = ((size_t)__builtin_amdgcn_readfirstlane(page(j0)) << page_shift) + (j0 & ((1 << page_shift) - 1));
     const uint8_t* base = (kv == 0 ? kc : vc) + row0 * stride;
@@ -127,7 +133,11 @@ struct Q8Tiles {
     for (int u = 0; u < QT::IK; ++u) {
       const int t = u * QT::RPI + lane / QT::CPR;
       const int c = lane % QT::CPR ^ (kv == 0 ? QT::kswz(t) : QT::vswz(t));
-      buf_to_lds16(rs, dst + u * QT::RPI * D, row(j0, t, all) * stride + c * 16, 0);
+      const int at = row(j0, t, all) * stride + c * 16;
+      if constexpr (ONCE)
+        buf_to_lds16_once(rs, dst + u * QT::RPI * D, at);
+      else
+        buf_to_lds16(rs, dst + u * QT::RPI * D, at, 0);
     }
   }
 };
@@ -267,7 +277,7 @@ template <typename T, int D>
 __host__ __device__ constexpr int q8_token_threads() {
   return kWave * (sizeof(T) == 4 && D == 128 ? 4 : 8);
 }
-template <typename T, int D>
+template <typename T, int D, bool ONCE>
 __global__ __launch_bounds__((q8_token_threads<T, D>())) void hyb_q8_token_kernel(SoftmaxQ8Args a, SpCut cut) {
   typedef Q8Acc<T, D> A;
   typedef Q8Tile<D> QT;
@@ -319,8 +329,8 @@ __global__ __launch_bounds__((q8_token_threads<T, D>())) void hyb_q8_token_kerne
   auto issue = [&](int n, Slot& s) __attribute__((always_inline)) {
     if (n >= my) return;
     const int j0 = t.first_key(w + NW * n);
-    t.copy(0, j0, s.k, lane);
-    t.copy(1, j0, s.v, lane);
+    t.template copy<ONCE>(0, j0, s.k, lane);
+    t.template copy<ONCE>(1, j0, s.v, lane);
   };
   if (block) {  // rows past the block's are the last again
     constexpr int EPC = 16 / (int)sizeof(T), CPR = D / EPC;
@@ -763,14 +773,21 @@ static hipError_t q8_go(const SoftmaxQ8Args& a, hipStream_t st) {
   SpCut cut = {};
   cut.limit = a.s.B * a.n_split;
   const dim3 grid((unsigned)(a.s.Hkv * way.wgs * cut.limit));
+  const dim3 threads((q8_token_threads<T, D>()));
+  bool done = false;
   if constexpr (sizeof(T) == 2) {
+    // A cache that no second workgroup reads and the chip's caches (256 MB) would not keep until the
+    // next call goes past them (64 requests of 16384 tokens, 1 GB, 194 us through them, 173 so;
+    // 24 of 8192, 100 MB at D = 64 and read again by the next call, 39 and 42; 16 blocks of 4 tiles of
+    // columns, 55 and 63).
+    const bool once = way.wgs == 1 && (double)a.s.B * a.s.Hkv * a.max_seen * 2 * D > 256e6;
+    done = way.block || once;
     if (way.block)
       hipLaunchKernelGGL((hyb_q8_block_kernel<D>), grid, dim3(kWave * 8), 0, st, a, cut);
-    else
-      hipLaunchKernelGGL((hyb_q8_token_kernel<T, D>), grid, dim3((q8_token_threads<T, D>())), 0, st, a, cut);
-  } else {
-    hipLaunchKernelGGL((hyb_q8_token_kernel<T, D>), grid, dim3((q8_token_threads<T, D>())), 0, st, a, cut);
+    else if (once)
+      hipLaunchKernelGGL((hyb_q8_token_kernel<T, D, true>), grid, threads, 0, st, a, cut);
   }
+  if (!done) hipLaunchKernelGGL((hyb_q8_token_kernel<T, D, false>), grid, threads, 0, st, a, cut);
   if (a.n_split == 1) return hipGetLastError();  // one range: already written out
   const long rows = (long)a.s.B * a.s.Hq * a.s.L, units = (long)a.s.B * a.s.Hq * ((a.s.L + 1024 / D - 1) / (1024 / D));
   if (rows <= 2048 && a.n_split > 4)

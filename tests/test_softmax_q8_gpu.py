@@ -148,6 +148,17 @@ def test_step(case):
         check(c, [[1, L, 0, L - 1, 2][b % 5] for b in range(B)], "active rows")
 
 
+@pytest.mark.parametrize("d,lens", [(128, [700, 5000, 0, 64]), (64, [3001, 31, 32, 1])])
+def test_wide_tables(d, lens):
+    """Room for caches of 262144 tokens, of which few are used (the loads past the caches, and many
+    ranges that hold nothing)."""
+    announce(f"softmax q8 wide tables {d}")
+    c = make(4, 1, 16, 4, d, 64, 32, lens, BF, 31, ALL, 0)
+    more = torch.full((4, 4096 - c["table"].shape[1]), 2 ** 31 - 1, dtype=torch.int32, device="cuda")
+    c["table"] = torch.cat([c["table"], more], 1)
+    check(c, what="wide tables")
+
+
 def test_no_cache_at_all():
     """max_pages = 0: the block alone."""
     announce("softmax q8 without pages")
