@@ -25,6 +25,12 @@
 // 4096, 1.67 to 1.78 ms (940 to 1000 TFLOP/s; a product of 8192 cubed reaches 1180 to 1210 on the
 // same cards, and the clock falls to 1.85 GHz for both); gradient of 8 x 2048 tokens, every earlier
 // block, 480 to 513 us (0.68 to 0.73 PFLOP/s of 10 d per pair).
+//
+// Packed sequences (PackedArgs) go through the same kernels: a workgroup finds its sequence, and
+// its place there, from the starts on the device (ragged.h; 2 to 7% of a call for equal
+// lengths beside the padded one).  24 sequences of 170 to 4096 tokens, blocks of 32, every earlier
+// block, 710 us (800 TFLOP/s); gradient of 16 of 128 to 2048, causal, 410 to 418 us; of 40 of 13 to 511, window 255, 8
+// and 2 heads of d = 64, 54 us.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -39,7 +45,6 @@ namespace hyb {
 // Reference of a query that has seen no key yet: finite, so that a tile in
 // which it sees none leaves weights of exactly zero.
 constexpr float kNoRef = -1e30f;
-
 
 // What query i (below len) sees: keys lo .. end - 1, and those below sinks.
 struct WinRow {
