@@ -411,14 +411,14 @@ __global__ __launch_bounds__((q8_token_threads<T, D>())) void hyb_q8_token_kerne
 }
 
 // Blocks (bf16; more than 32 columns): a wave answers 32 columns, and the four waves of a
-// half share its tiles; the two halves of a workgroup take the range's tiles in turn and join
-// their sums in LDS.  A tile's codes go through registers, A tiles ahead, and into LDS as
+// half share its tiles; with H = 2 the two halves of a workgroup take the range's tiles in turn and join
+// their sums in LDS, with H = 1, where workgroups are many, two of them share a CU.  A tile's codes go through registers, A tiles ahead, and into LDS as
 // bf16 values, scales included, so that each is converted once for four tiles of
 // columns; the tiles are then read as those of a bf16 cache.  Step n forms the scores of tile n + 1 while it
 // takes the weights of tile n (two independent chains, whose MFMAs and VALU instructions
 // interleave), and puts tile n + 2 into the slot of tile n - 1.
-template <int D>
-__global__ __launch_bounds__(kWave * 8, 2) void hyb_q8_block_kernel(SoftmaxQ8Args a, SpCut cut) {
+template <int D, int H>
+__global__ __launch_bounds__(kWave * 4 * H, 2) void hyb_q8_block_kernel(SoftmaxQ8Args a, SpCut cut) {
   typedef Mma<bf16> M;
   typedef M::op_t op_t;
   typedef RowColTile<D> RT;
@@ -431,13 +431,13 @@ __global__ __launch_bounds__(kWave * 8, 2) void hyb_q8_block_kernel(SoftmaxQ8Arg
   };
   constexpr int NH = NCT / 2;  // groups of 32 entries that a half joins
   union Smem {
-    Slot ring[2][R];
-    f32x4 parts[2][NW][NH * 4][kWave];  // [for half]
+    Slot ring[H][R];
+    f32x4 parts[H][NW][NH * 4][kWave];  // [for half]
     int plan[kPlanInts];
     __device__ Smem() {}
   };
   __shared__ alignas(16) Smem sh;
-  __shared__ float refs[2][NW][kTile], sums[2][NW][kTile];
+  __shared__ float refs[H][NW][kTile], sums[H][NW][kTile];
   __shared__ int pages[kMaxRangePages];
   // Of the range's cached tiles, and of one more, hidden whole, behind them: the offset of
   // their first row in the pools (kPartial in the high word: not all of its rows are seen),
@@ -470,7 +470,7 @@ __global__ __launch_bounds__(kWave * 8, 2) void hyb_q8_block_kernel(SoftmaxQ8Arg
   // The list: the block's tile first, if it is the range's, then the cached ones, nc of
   // them; this half's tile n is the list's 2 n + half.  The halves have the same number:
   // one that is past the list's end takes the hidden one.
-  const int nb = rg.hi > (P + kTile - 1) / kTile * kTile ? 1 : 0, nc = rg.nt - nb, ntiles = (rg.nt + 1) / 2;
+  const int nb = rg.hi > (P + kTile - 1) / kTile * kTile ? 1 : 0, nc = rg.nt - nb, ntiles = (rg.nt + H - 1) / H;
   const bool first_is_block = half < nb;
   for (int e = threadIdx.x; e <= nc; e += blockDim.x) {
     const int j0 = t.first_key(max(0, min(e, nc - 1)));
@@ -479,7 +479,7 @@ __global__ __launch_bounds__(kWave * 8, 2) void hyb_q8_block_kernel(SoftmaxQ8Arg
     places[e] = uint2{(uint32_t)off, (uint32_t)(off >> 32) | (e == nc || !t.whole(j0) ? kPartial : 0u)};
     bytes[e] = nc > 0 ? (uint16_t)t.scales(a, g, j0) : 0;
   }
-  auto entry = [&](int n) __attribute__((always_inline)) { return max(0, min(2 * n + half - nb, nc)); };
+  auto entry = [&](int n) __attribute__((always_inline)) { return max(0, min(H * n + half - nb, nc)); };
   __syncthreads();  // (the plan's scratch is read, the places are there)
 
   // The row of 16-code piece y: the rows whose pieces a write puts down at once (two, at
@@ -649,35 +649,46 @@ __global__ __launch_bounds__(kWave * 8, 2) void hyb_q8_block_kernel(SoftmaxQ8Arg
   if (n + 1 < ntiles) step(n, std::integral_constant<int, 0>{});
   if (n + 2 < ntiles) step(n + 1, std::integral_constant<int, 1>{});
   compute(std::true_type{}, ntiles - 1, ring[0], ring[ntiles - 1 - n], false, [] {});
-  // The halves' sums over one reference: each hands over half of the entries and joins
-  // the others.
   mma_settle<bf16>();
   l += xor32(l);
-  if (hh == 0) refs[half][w][li] = m;
-  lds_barrier();  // (and the slots are free)
-  const float mm = fmaxf(refs[0][w][li], refs[1][w][li]), f = __builtin_amdgcn_exp2f(m - mm);
-  if (hh == 0) sums[half][w][li] = l * f;
+  if constexpr (H == 1) {
+    if (!mine) return;
 #pragma unroll
-  for (int ct = 0; ct < NCT; ++ct)
+    for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (ct / NH != half)
-        sh.parts[ct / NH][w][ct % NH * 4 + e][lane] =
-            f32x4{acc[ct][4 * e] * f, acc[ct][4 * e + 1] * f, acc[ct][4 * e + 2] * f, acc[ct][4 * e + 3] * f};
-  lds_barrier();
-  if (!mine) return;
-  const float den = sums[0][w][li] + sums[1][w][li];
+      for (int e = 0; e < 4; ++e)
+        sp_put<bf16, D>(a, rg, r, h, i, ct * kTile + row_of(4 * e, hh),
+                        f32x4{acc[ct][4 * e], acc[ct][4 * e + 1], acc[ct][4 * e + 2], acc[ct][4 * e + 3]}, l);
+    if (hh == 0) sp_put_sum<D>(a, rg, r, h, i, m, l);
+  } else {
+    // The halves' sums over one reference: each hands over half of the entries and joins
+    // the others.
+    if (hh == 0) refs[half][w][li] = m;
+    lds_barrier();  // (and the slots are free)
+    const float mm = fmaxf(refs[0][w][li], refs[1][w][li]), f = __builtin_amdgcn_exp2f(m - mm);
+    if (hh == 0) sums[half][w][li] = l * f;
 #pragma unroll
-  for (int ct = 0; ct < NCT; ++ct)
-    if (ct / NH == half)
+    for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        f32x4 o = sh.parts[half][w][ct % NH * 4 + e][lane];
+      for (int e = 0; e < 4; ++e)
+        if (ct / NH != half)
+          sh.parts[ct / NH][w][ct % NH * 4 + e][lane] =
+              f32x4{acc[ct][4 * e] * f, acc[ct][4 * e + 1] * f, acc[ct][4 * e + 2] * f, acc[ct][4 * e + 3] * f};
+    lds_barrier();
+    if (!mine) return;
+    const float den = sums[0][w][li] + sums[1][w][li];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) o[k] += acc[ct][4 * e + k] * f;
-        sp_put<bf16, D>(a, rg, r, h, i, ct * kTile + row_of(4 * e, hh), o, den);
-      }
-  if (half == 0 && hh == 0) sp_put_sum<D>(a, rg, r, h, i, mm, den);
+    for (int ct = 0; ct < NCT; ++ct)
+      if (ct / NH == half)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          f32x4 o = sh.parts[half][w][ct % NH * 4 + e][lane];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) o[k] += acc[ct][4 * e + k] * f;
+          sp_put<bf16, D>(a, rg, r, h, i, ct * kTile + row_of(4 * e, hh), o, den);
+        }
+    if (half == 0 && hh == 0) sp_put_sum<D>(a, rg, r, h, i, mm, den);
+  }
 }
 
 // Merge of few rows' ranges: a workgroup per row, D / 4 threads per range, as many
@@ -740,13 +751,15 @@ __global__ __launch_bounds__(256) void hyb_q8_combine_kernel(SoftmaxPrefixArgs a
 // Which kernel, its workgroups for a range and KV head, and into how many ranges requests of
 // max_seen cached tokens are cut: the least estimated time (us).  The chip takes a
 // workgroup per CU at a time; one costs its start and end besides its tiles (at D = 128 0.19 us
-// of 32 columns and 0.55 of 128, fp32 1.36, at 64 0.14, 0.4 and 0.62), and more ranges than one cost
-// a merge and the partial rows.  (The numbers are fitted to 88 shapes of bf16, where what this
+// of 32 columns and 0.55 of 128, fp32 1.36, at 64 0.14, 0.4 and 0.62; two of 128 columns without
+// halves 1.04, at 64 0.75), and more ranges than one cost a merge and the partial rows.  (The numbers are fitted to 88 shapes of bf16, where what this
 // takes is within 0.4% of the best on average.  4 KV heads of 4 query heads, D = 128, blocks of 32,
 // the kernel of 32 columns against that of 128 at each one's best ranges: a window of 1024 of 16
-// requests 15 and 29 us, of 48 41 and 32; of 4096 of 4 requests 25 and 29, of 24 61 and 57.)
+// requests 15 and 29 us, of 48 41 and 32; of 4096 of 4 requests 25 and 29, of 24 61 and 57.  Without
+// halves against with them: a window of 1024 of 64 requests 38 and 36, of 128 52 and 66.)
 struct Q8Way {
-  bool block;
+  int columns;  // tiles of them per workgroup: 1 or 4
+  int halves;
   int wgs, ranges;
 };
 static Q8Way q8_way(const Shape& s, int max_seen) {
@@ -755,6 +768,12 @@ static Q8Way q8_way(const Shape& s, int max_seen) {
   const double rows = (double)s.B * s.Hq * s.L, row = (s.D + 2) / 1e6;  // a partial row's write and read
   Q8Way best = {};
   double least = 0;
+  auto take = [&](Q8Way w, double time) {
+    if (least == 0 || time < least * 0.98) {
+      least = time;
+      best = w;
+    }
+  };
   for (int block = 0; block <= (s.dtype == 1 && groups > 1 ? 1 : 0); ++block) {
     const int per = block ? (groups + 3) / 4 : groups;
     const double wgs = (double)s.B * s.Hkv * per;
@@ -764,13 +783,10 @@ static Q8Way q8_way(const Shape& s, int max_seen) {
     for (int rounds = 0; rounds <= 4; ++rounds) {
       const int k = rounds == 0 ? 1 : (int)std::min(256.0 * rounds / wgs, tiles / 4);
       if (k < 1) continue;
-      const double t =
-          std::ceil(wgs * k / 256) * (std::ceil(tiles / k) * tile + fixed) + (k > 1 ? 6.0 + rows * k * row : 0.0);
-      if (least == 0 || t < least * 0.98) {
-        least = t;
-        best = {block != 0, per, k};
-      }
+      take({block ? 4 : 1, 2, per, k},
+           std::ceil(wgs * k / 256) * (std::ceil(tiles / k) * tile + fixed) + (k > 1 ? 6.0 + rows * k * row : 0.0));
     }
+    if (block && wgs > 256) take({4, 1, per, 1}, std::ceil(wgs / 512) * (tiles * 1.04 * width + fixed));
   }
   return best;
 }
@@ -797,9 +813,11 @@ static hipError_t q8_go(const SoftmaxQ8Args& a, hipStream_t st) {
     // 24 of 8192, 100 MB at D = 64 and read again by the next call, 39 and 42; 16 blocks of 4 tiles of
     // columns, 55 and 63).
     const bool once = way.wgs == 1 && (double)a.s.B * a.s.Hkv * a.max_seen * 2 * D > 256e6;
-    done = way.block || once;
-    if (way.block)
-      hipLaunchKernelGGL((hyb_q8_block_kernel<D>), grid, dim3(kWave * 8), 0, st, a, cut);
+    done = way.columns == 4 || once;
+    if (way.columns == 4 && way.halves == 2)
+      hipLaunchKernelGGL((hyb_q8_block_kernel<D, 2>), grid, dim3(kWave * 8), 0, st, a, cut);
+    else if (way.columns == 4)
+      hipLaunchKernelGGL((hyb_q8_block_kernel<D, 1>), grid, dim3(kWave * 4), 0, st, a, cut);
     else if (once)
       hipLaunchKernelGGL((hyb_q8_token_kernel<T, D, true>), grid, threads, 0, st, a, cut);
   }

@@ -134,6 +134,8 @@ BLOCKS = [
     (4, 32, 16, 4, 128, 64, 32, [12000, 1, 5000, 0], ALL, 0, BF),
     (4, 32, 16, 4, 64, 32, 32, [16000, 31, 3000, 64], ALL, 0, BF),
     (16, 32, 16, 4, 64, 64, 64, [16000] + [(i * 71) % 260 for i in range(15)], ALL, 0, BF),
+    (9, 32, 128, 32, 128, 64, 32, [0, 1, 31, 32, 33, 200, 65, 129, 400], ALL, 0, BF),  # more workgroups than CUs
+    (20, 31, 34, 17, 64, 32, 32, [(i * 29) % 180 for i in range(20)], 70, 9, BF),
     (8, 32, 16, 4, 128, 128, 64, [9000] + [(i * 53) % 200 for i in range(7)], 8500, 70, BF)]
 CASES += BLOCKS
 
