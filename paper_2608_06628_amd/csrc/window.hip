@@ -379,7 +379,7 @@ __device__ inline WinUnit win_unit(const WindowArgs& a, int len, int g, int u) {
 // A wave's 32 queries take the keys j0 .. j0 + 31 (`full`, uniform: every query sees every one): m is the
 // reference of the weights in the log2 domain, l their sum, acc the weighted sums of V^T.
 template <int D>
-__device__ inline void win_take(typename WinF32<D>::Acc& acc, float& m, float& l, const typename WinF32<D>::Tile& kt,
+__device__ __attribute__((always_inline)) inline void win_take(typename WinF32<D>::Acc& acc, float& m, float& l, const typename WinF32<D>::Tile& kt,
                                 const typename WinF32<D>::Tile& vt, const float* qop, const WinRow& row, bool full,
                                 int sinks, int j0, float scale, int li, int hh) {
   f32x16 sc = win_rows_mma<D>(kt, qop, li, hh);
@@ -414,7 +414,7 @@ __device__ inline void win_take(typename WinF32<D>::Acc& acc, float& m, float& l
 }
 // The same for dQ: weights from the rows' lse (log2), times dP - delta.
 template <int D>
-__device__ inline void win_take_dq(typename WinF32<D>::Acc& acc, const typename WinF32<D>::Tile& kt,
+__device__ __attribute__((always_inline)) inline void win_take_dq(typename WinF32<D>::Acc& acc, const typename WinF32<D>::Tile& kt,
                                    const typename WinF32<D>::Tile& vt, const float* qop, const float* dop, const WinRow& row,
                                    bool full, int sinks, int j0, float scale, float lse, float delta, int li, int hh) {
   f32x16 sc = win_rows_mma<D>(kt, qop, li, hh);
@@ -635,9 +635,8 @@ struct WinFew {
   }
 };
 
-template <typename A>
+template <int D, typename A>
 __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_fwd_few_kernel(A a, int wgs) {
-  constexpr int D = 64;
   typedef WinF32<D, 1> C;
   __shared__ alignas(16) WinFew<D> sh;
   const int lane = threadIdx.x & (kWave - 1), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -679,9 +678,8 @@ __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_fwd_few_kernel(A a, 
   if (a.lse && w == 0 && hh == 0) a.lse[sq.lse(me.h, i)] = (mm + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
-template <typename A>
+template <int D, typename A>
 __global__ __launch_bounds__(kWave* kWinWaves) void hyb_win_dq_few_kernel(A a, int wgs) {
-  constexpr int D = 64;
   typedef WinF32<D, 1> C;
   __shared__ alignas(16) WinFew<D> sh;
   const int lane = threadIdx.x & (kWave - 1), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -1574,14 +1572,16 @@ static hipError_t win_ring_go(const A& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-// Whether n units of packed sequences (fp32, d = 64) have a workgroup each: where lists are long
-// and units few.  (us of a forward and a gradient so and otherwise: 5 sequences of 140 to 701, 8
-// heads, 545 units, 32 and 58, 141 and 189; 1 of 2048, 516, 74 and 103, 219 and 363; 16 of 64 to 1024,
-// 2240, 99 and 117, 351 and 377; but 16 of 128 to 2048, 4416, 295 and 273, and 20 of 5 to 100, 18.7
-// and 15.7.  At d = 128 a wave's tiles on their way need more registers than there are.)
+// Whether n units of packed sequences (fp32) have a workgroup each: where lists are long and units
+// few; at d = 128 one such workgroup fits a CU, at 64 two.  (us of a forward and a gradient so and
+// otherwise.  d = 64: 5 sequences of 140 to 701, 8 heads, 545 units, 32 and 58, 141 and 189; 1 of 2048,
+// 516, 74 and 103, 219 and 363; 16 of 64 to 1024, 2240, 99 and 117, 351 and 377; but 16 of 128 to
+// 2048, 4416, 295 and 273, and 20 of 5 to 100, 18.7 and 15.7.  d = 128: 2 of 175 and 350, 16 heads,
+// 278, 28 and 41, 99 and 149; 3 of 192, 8 heads, 156, 21 and 24, 70 and 95; 4 of 128 to 512, 672, 52 and 78,
+// 177 and 228; but 16 of 44 to 700, 1550, 144 and 106, 447 and 417.)
 static bool win_few(const PackedArgs& a, int n) {
   const long seen = std::min<long>(a.T, (long)a.window + std::min(a.n_sinks, a.T) + a.s.L);
-  return n <= 2560 && seen >= 8 * kTile;
+  return (n <= 640 && seen >= 4 * kTile) || (n <= (a.s.D == 64 ? 2560 : 1024) && seen >= 8 * kTile);
 }
 
 template <int D, typename A>
@@ -1589,16 +1589,14 @@ static hipError_t win_prefill_f32_go(const A& a, hipStream_t st) {
   const WinGrid<A> gr(a);
   const dim3 grid((unsigned)gr.n);
   if constexpr (std::is_same_v<A, PackedArgs>) {
-    if constexpr (D == 64) {
-      const WinGrid<A> one(a, 1);
-      if (win_few(a, one.busy)) {
-        hipLaunchKernelGGL((hyb_win_fwd_few_kernel<A>), dim3((unsigned)one.n), dim3(kWave * kWinWaves), 0, st, a, one.wgs);
-        return hipGetLastError();
-      }
+    const WinGrid<A> one(a, 1);
+    if (win_few(a, one.busy)) {
+      hipLaunchKernelGGL((hyb_win_fwd_few_kernel<D, A>), dim3((unsigned)one.n), dim3(kWave * kWinWaves), 0, st, a, one.wgs);
+      return hipGetLastError();
     }
     // Two units per workgroup while those have a CU each: a SIMD then has one wave of a
-    // step's products, not two (16 heads of d = 128, 1 sequence of 1024: 146 us with four
-    // units, 95 with two; of 125 26 and 18).
+    // step's products, not two (32 heads of d = 128, 1 sequence of 125: 26 us with four
+    // units, 18 with two).
     const WinGrid<A> two(a, 2);
     if (two.busy <= 256) {
       hipLaunchKernelGGL((hyb_win_fwd_kernel<D, 2, A, 2>), dim3((unsigned)two.n), dim3(kWave * 4), 0, st, a, two.wgs);
@@ -1701,11 +1699,11 @@ static void win_backward_kernels(const A& a, const WinParts& cut, hipStream_t st
     if (D == 128 || cut.halves) hipLaunchKernelGGL((hyb_win_dkv_ring_kernel<D, 2, A>), gk, dim3(kWave * 8), 0, st, a, cut);
   } else {
     bool few = false;
-    if constexpr (D == 64 && std::is_same_v<A, PackedArgs>) {
+    if constexpr (std::is_same_v<A, PackedArgs>) {
       const WinGrid<A> one(a, 1);
       few = win_few(a, one.busy);
       if (few)
-        hipLaunchKernelGGL((hyb_win_dq_few_kernel<A>), dim3((unsigned)one.n), dim3(kWave * kWinWaves), 0, st, a, one.wgs);
+        hipLaunchKernelGGL((hyb_win_dq_few_kernel<D, A>), dim3((unsigned)one.n), dim3(kWave * kWinWaves), 0, st, a, one.wgs);
     }
     if (!few) hipLaunchKernelGGL((hyb_win_dq_kernel<D, A>), gq, dim3(kWave * kWinWaves), 0, st, a, gr.wgs);
     hipLaunchKernelGGL((hyb_win_dkv_kernel<D, A>), gk, dim3(kWave * kWinWaves), 0, st, a, cut);

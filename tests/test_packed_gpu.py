@@ -95,6 +95,8 @@ LONG = [
     ([700, 600], 4, 4, 64, 32, 200, 64, FL, 3),
     ([701, 1, 300, 33, 257], 8, 4, 64, 1, ALL, 0, FL, 13),  # few units: a workgroup each
     ([600], 12, 4, 64, 7, ALL, 0, FL, 0),
+    ([300, 140, 1], 6, 2, 128, 5, ALL, 3, FL, 4),
+    ([520, 31], 4, 4, 128, 1, 300, 40, FL, 1),
     ([500, 480], 3, 1, 64, 1, 100, 170, FL, 2),
     ([125], 16, 2, 128, 1, ALL, 4, FL, 0)]                   # 16 parts
 
