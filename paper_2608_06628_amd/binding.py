@@ -881,9 +881,9 @@ def softmax_packed_backward(dev, q, k, v, token_start, out, lse, dout, block, wi
     act, odt = q.dtype, _odt(q.dtype, dq, out_f32)
     N, Hq, _ = q.shape
     dims, kv, at = _packed_args(dev, q, k, v, token_start, block, odt)
-    dq = torch.empty(q.shape, dtype=odt, device=q.device) if dq is None else dq
-    dk = torch.empty(kv, dtype=odt, device=q.device) if dk is None else dk
-    dv = torch.empty(kv, dtype=odt, device=q.device) if dv is None else dv
+    dq = _new(q, odt) if dq is None else dq
+    dk = _new(k, odt) if dk is None else dk
+    dv = _new(v, odt) if dv is None else dv
     if dims.batch == 0:  # no sequence: every row is behind the last
         return dq.zero_(), dk.zero_(), dv.zero_()
     if ws is None and N > 0:
