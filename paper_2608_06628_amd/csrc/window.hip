@@ -1539,6 +1539,14 @@ static bool win_halves(const WindowArgs& a, int n) {
   const long seen = std::min<long>(a.T, (long)a.window + std::min(a.n_sinks, a.T) + a.s.L);
   return n <= 512 && seen >= 32 * kTile;
 }
+// Packed (T is the mean length): the longest lists come first and end last.  (us of a forward in one
+// half and in two: 3 sequences of 375 to 1126, 12 heads of d = 128, 33 and 29; 12 of 75 to 900, 8 heads,
+// 33 and 27, at d = 64 22 and 20; 4 of 375 to 1500, 16 heads, 49 and 41; 1 of 400 15.3 and 15.6; but 20
+// of 15 to 300 16.5 and 23.)
+static bool win_halves(const PackedArgs& a, int n) {
+  const long seen = std::min<long>(a.T, (long)a.window + std::min(a.n_sinks, a.T) + a.s.L);
+  return n <= 512 && seen >= 10 * kTile;
+}
 
 // The grids of the queries' and keys' workgroups: `wgs` and `keys` per (request, KV head), or
 // packed per KV head; `busy` of the queries' are at work.
