@@ -482,19 +482,21 @@ __global__ __launch_bounds__(kWave * 4 * H, 2) void hyb_q8_block_kernel(SoftmaxQ
   auto entry = [&](int n) __attribute__((always_inline)) { return max(0, min(H * n + half - nb, nc)); };
   __syncthreads();  // (the plan's scratch is read, the places are there)
 
-  // The row of 16-code piece y: the rows whose pieces a write puts down at once (two, at
-  // d = 64 four) differ in the lowest bit of their swizzle, so that one's even chunks and the
-  // other's fall in distinct banks.
-  auto row_of_piece = [&](int y) __attribute__((always_inline)) {
-    const int x = y / CPR;
-    return D == 128 ? (x & ~7) | (x >> 1 & 3) | (x & 1) << 2 : (x & ~6) | (x & 2) << 1 | (x & 4) >> 1;
+  // 16-code piece y of a tile: a write puts down eight lanes' 16 bytes at once, so four pieces of
+  // a row go with four of the row four on, whose swizzle differs in the lowest bit: one's even
+  // chunks and the other's fall in distinct banks.
+  auto piece = [&](int y, int& row, int& c16) __attribute__((always_inline)) {
+    c16 = (y & 3) | (D == 128 ? y >> 1 & 4 : 0);
+    const int x = D == 128 ? y >> 4 : y >> 3;
+    row = (y & 4) | (x & 3) | (x >> 2) << 3;
   };
   uint4 next[A][PT];  // codes of tiles on their way
   int voff[PT], dst0[PT], dst1[PT];  // this thread's pieces: their offsets in a tile in the pools, and in a slot
   const int kvs = PT > 1 ? 0 : w * kWave / PK;
 #pragma unroll
   for (int u = 0; u < PT; ++u) {
-    const int y = (u * kWave * NW + w * kWave + lane) % PK, row = row_of_piece(y), c16 = y % CPR;
+    int row, c16;
+    piece((u * kWave * NW + w * kWave + lane) % PK, row, c16);
     voff[u] = row * t.stride + c16 * 16;
     dst0[u] = row * D + ((2 * c16) ^ RT::swz(row)) * 8;
     dst1[u] = row * D + ((2 * c16 + 1) ^ RT::swz(row)) * 8;
@@ -514,8 +516,9 @@ __global__ __launch_bounds__(kWave * 4 * H, 2) void hyb_q8_block_kernel(SoftmaxQ
       const int j0 = t.first_key(max(0, min(entry(n), nc - 1)));
 #pragma unroll
       for (int u = 0; u < PT; ++u) {
-        const int y = (u * kWave * NW + w * kWave + lane) % PK;
-        at[u] = t.row(j0, row_of_piece(y), t.whole(j0)) * t.stride + y % CPR * 16;
+        int row, c16;
+        piece((u * kWave * NW + w * kWave + lane) % PK, row, c16);
+        at[u] = t.row(j0, row, t.whole(j0)) * t.stride + c16 * 16;
       }
     }
 #pragma unroll
