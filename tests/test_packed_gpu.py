@@ -145,6 +145,19 @@ def test_many_sequences():
     check_backward(c, 1, ALL, 0, out, lse, grads)
 
 
+@pytest.mark.parametrize("dtype,n", [(FL, 260), (BF, 40)])
+def test_sequences_past_the_levels(dtype, n):
+    """256 sequences and more follow one another instead of going by levels (fp32: a workgroup per unit)."""
+    announce(f"packed, 258 sequences {dtype}")
+    c = make([n] * 256 + [0, n + 7], 1, 1, 64, dtype, 6, 3)
+    args = c["q"], c["k"], c["v"], c["start"]
+    out, lse = hb.softmax_packed_prefill(*args, 1, ALL)
+    grads = hb.softmax_packed_backward(*args, out, lse, c["dout"], 1, ALL)
+    torch.cuda.synchronize()
+    check_prefill(c, 1, ALL, 0, out, lse)
+    check_backward(c, 1, ALL, 0, out, lse, grads)
+
+
 def test_as_padded():
     """The padded call of the same sequences: outputs within a rounding each of 64 bits, so
     within two of each other; here, where the order of the sums is the same, equal."""
