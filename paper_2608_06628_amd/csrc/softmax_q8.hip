@@ -473,7 +473,7 @@ __global__ __launch_bounds__(kWave * 4 * H, 2) void hyb_q8_block_kernel(SoftmaxQ
   const Q8Tiles<D> t(a, rg, g, P, pages);
   const RT rt(lane);
   // The list: the block's tile first, if it is the range's, then the cached ones, nc of
-  // them; this half's tile n is the list's 2 n + half.  The halves have the same number:
+  // them; this half's tile n is the list's H n + half.  The halves have the same number:
   // one that is past the list's end takes the hidden one.
   const int nb = rg.hi > (P + kTile - 1) / kTile * kTile ? 1 : 0, nc = rg.nt - nb, ntiles = (rg.nt + H - 1) / H;
   const bool first_is_block = half < nb;
@@ -482,10 +482,9 @@ __global__ __launch_bounds__(kWave * 4 * H, 2) void hyb_q8_block_kernel(SoftmaxQ
     const size_t row = ((size_t)t.page(j0) << t.page_shift) + (j0 & ((1 << t.page_shift) - 1));
     const size_t off = nc > 0 ? row * t.stride : 0;
     places[e] = uint2{(uint32_t)off, (uint32_t)(off >> 32) | (e == nc || !t.whole(j0) ? kPartial : 0u)};
-    bytes[e] = nc > 0 ? (uint16_t)t.scales(a, g, j0) : 0;
   }
   auto entry = [&](int n) __attribute__((always_inline)) { return max(0, min(H * n + half - nb, nc)); };
-  __syncthreads();  // (the plan's scratch is read, the places are there)
+  lds_barrier();  // (the places are there)
 
   // 16-code piece y of a tile: a write puts down eight lanes' 16 bytes at once, so four pieces of
   // a row go with four of the row four on, whose swizzle differs in the lowest bit: one's even
@@ -616,6 +615,10 @@ __global__ __launch_bounds__(kWave * 4 * H, 2) void hyb_q8_block_kernel(SoftmaxQ
   };
 #pragma unroll
   for (int n = 0; n < A; ++n) fetch(n, places[entry(n)], next[n]);
+  // (the scales' bytes beside the first tiles)
+  for (int e = threadIdx.x; e <= nc; e += blockDim.x)
+    bytes[e] = nc > 0 ? (uint16_t)t.scales(a, g, t.first_key(max(0, min(e, nc - 1)))) : 0;
+  lds_barrier();  // (the bytes are there, the plan's scratch is read)
   if (first_is_block)
     put_block(ring[0]);
   else
