@@ -491,8 +491,9 @@ int kv_pages_plan(int32_t batch, int32_t max_pages, int32_t page_size,
  * [n_pages][page_size][Hkv][d], e4m3 (the OCP type without infinities); k_scales,
  * v_scales: [n_pages][page_size / scale_block][Hkv] bytes, the scale 2^(byte - 127)
  * of scale_block consecutive rows of a page at one KV head.  A cached value is its code
- * times its scale, exactly in bf16 and fp32.  page_size is a power of two from 32 to
- * 65536, scale_block one from 32 to page_size. */
+ * times its scale, also of a zeroed pool (2^-127): exactly in fp32, and in bf16 from byte 3 on
+ * (below, rounded to nearest even among bf16's subnormal numbers), up to where the types
+ * end.  page_size is a power of two from 32 to 65536, scale_block one from 32 to page_size. */
 typedef struct {
   int32_t tokens;      /* N >= 0, rows of k and v (0: nothing to do)         */
   int32_t batch;       /* B >= 0, requests                                   */

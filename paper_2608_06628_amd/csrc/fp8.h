@@ -1,9 +1,11 @@
 // fp8.h -- e4m3 codes with power-of-two scales.
 //
 // A scale is kept as its exponent plus 127 in a byte, so that 2^e is the float
-// of the bits byte << 23.  A code times a scale is exact in bf16 and fp32: it has four
-// significant bits, and the bytes are at least kMinScale, where the least code is
-// 2^-9 2^-117, a normal number.
+// of the bits byte << 23, but for byte 0, 2^-127, which is subnormal (and what a zeroed pool
+// holds).  The bytes written here are at least kMinScale, where the least code is 2^-9 2^-117,
+// a normal number, so that a code times a scale, of four significant bits, is exact in bf16 and
+// fp32.  Any scale is exact in fp32; bytes below 3 leave codes whose last bits are below
+// 2^-133, where bf16 ends, and which round there to nearest even.
 #pragma once
 
 #include "device.h"
@@ -12,7 +14,8 @@ namespace hyb {
 
 constexpr int kMinScale = 10;  // 2^-117
 
-__device__ inline float scale_of(int byte) { return __builtin_bit_cast(float, byte << 23); }
+// (Positive whatever the byte: -infinity times it, a hidden score, stays one.)
+__device__ inline float scale_of(int byte) { return __builtin_bit_cast(float, max(byte << 23, 0x400000)); }
 
 // The byte of the least e with m <= 448 2^e, for the bits of a finite m >= 0.
 // 448 is 1.75 2^8: the mantissa's part above 1.75 carries into the exponent.

@@ -1,0 +1,100 @@
+"""The 8-bit cache with scales that its own write does not leave: zeroed pools, whose scales are
+2^-127, and bytes below 10, as another writer of the format may leave them."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2608_06628_amd import binding as hb
+
+import _cache_ref as ref
+from _helpers import announce
+from test_softmax_q8_gpu import check, make, run
+
+pytestmark = pytest.mark.gpu
+BF, FL = torch.bfloat16, torch.float32
+ALL = 2 ** 31 - 1
+
+LENS = [1, 33, 70, 0, 200, 31]
+SHAPES = [  # B, L, Hq, Hkv, d, dtype: tokens, blocks by 32 columns, by 128, by 128 without halves
+    (3, 1, 4, 2, 64, BF), (3, 1, 8, 2, 128, BF), (3, 1, 4, 2, 64, FL), (2, 5, 4, 1, 128, FL), (3, 32, 4, 2, 64, BF),
+    (6, 32, 64, 16, 64, BF), (6, 32, 64, 16, 128, BF), (6, 32, 160, 80, 64, BF), (6, 32, 160, 80, 128, BF)]
+
+
+def cached(shape, window, sinks, byte, what="kv"):
+    """A case whose seen scales are all of one byte, in K or V or both."""
+    B, L, Hq, Hkv, d, dtype = shape
+    c = make(B, L, Hq, Hkv, d, 64, 32, LENS[:B], dtype, 40 + byte, window, sinks)
+    for x in what:
+        scales = c["cache"].host[x][1]
+        scales[scales != 255] = byte
+    c["cache"].send()
+    return c
+
+
+@pytest.mark.parametrize("byte,what", [(0, "k"), (0, "v"), (0, "kv"), (1, "kv"), (9, "k")])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_step(shape, byte, what):
+    """Tiles that the lengths and the window cut, under the least scales there are."""
+    announce(f"softmax q8 scale byte {byte} of {what}: {shape}")
+    check(cached(shape, ALL, 0, byte, what), what=f"byte {byte} of {what}")
+    check(cached(shape, 40, 3, byte, what), what=f"byte {byte} of {what}, a window")
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_step_over_zeroed_pools(shape):
+    """A pool as torch.zeros leaves it: every cached key and value is zero."""
+    announce(f"softmax q8 zeroed pools: {shape}")
+    for window, sinks in ((ALL, 0), (40, 3)):
+        c = cached(shape, window, sinks, 0)
+        for x in "kv":
+            for t in c["cache"].host[x]:
+                t[:] = 0
+        c["cache"].send()
+        check(c, what="zeroed pools")
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_values_of_the_least_scale(shape):
+    """Even weights (q is zero) over 64 tokens of which one is the block's, zero: the mean of codes times
+    2^-127, exact up to the order of a sum of numbers of 16 bits and a reciprocal (2 steps of fp32)."""
+    B, _, Hq, Hkv, d, dtype = shape
+    L = shape[1]
+    n = 64 - L
+    c = make(B, L, Hq, Hkv, d, 64, 32, [n] * B, dtype, 7, ALL, 0)
+    announce(f"softmax q8 values of the least scale: {shape}")
+    codes, scales = c["cache"].host["v"]
+    codes[:] = np.random.RandomState(8).randint(0x40, 0x7f, codes.shape)  # 2 .. 448, so that 2^-127 of it is normal
+    scales[:] = 0
+    c["cache"].send()
+    c["q"].zero_(), c["v"].zero_()
+    out = run(c, None, out_f32=True).double().cpu().numpy()
+    values = ref.values(*c["cache"].host["v"])
+    for b in range(B):
+        j = np.arange(n)
+        want = values[c["host"][b, j // 64], j % 64].sum(0) / 64
+        want = want.repeat(Hq // Hkv, 0)[None]
+        assert np.abs(out[b] - want).max() <= 2.0 ** -22 * np.abs(want).max()
+
+
+def every_byte():
+    """A pool of 256 pages of 32 rows with every code, page n under the scale byte n, and its values."""
+    codes = np.arange(2048).astype(np.uint8).reshape(1, 32, 1, 64).repeat(256, 0)
+    scales = np.arange(256).astype(np.uint8).reshape(256, 1, 1)
+    return codes, scales, torch.from_numpy(ref.values(codes, scales)).flatten(0, 1)
+
+
+@pytest.mark.parametrize("dtype", [BF, FL], ids=str)
+def test_read(dtype):
+    """Every code under every scale but 255: the value, rounded to nearest even where bf16 has fewer bits
+    (subnormal numbers), an infinity where the type ends."""
+    announce(f"read every scale byte {dtype}")
+    codes, scales, values = every_byte()
+    pool = torch.from_numpy(codes).cuda().view(torch.float8_e4m3fn)
+    bytes_ = torch.from_numpy(scales).cuda().view(torch.float8_e8m0fnu)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32).cuda()
+    k, v = hb.kv_pages_q8_read(pool, pool, bytes_, bytes_, i32([list(range(255))]), i32([0]), i32([0, 255 * 32]),
+                               tokens=255 * 32, dtype=dtype)
+    want = values[:255 * 32].float().to(dtype)
+    for t in (k, v):
+        assert torch.equal(t.isnan().cpu(), want.isnan())
+        assert torch.equal(torch.nan_to_num(t.cpu(), 3.0, 5.0, -5.0), torch.nan_to_num(want, 3.0, 5.0, -5.0))
