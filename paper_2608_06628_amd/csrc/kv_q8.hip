@@ -138,7 +138,7 @@ __global__ __launch_bounds__(kWave* kQ8Waves) void hyb_kv_q8_write_kernel(KvQ8Ar
   }
   const int byte = max(scale_byte(__builtin_amdgcn_readfirstlane(m)), old);
   if (w == 0 && lane == 0) *scale = (uint8_t)byte;
-  if (old != 0 && old < byte) {  // the block grows: its earlier rows (16 codes per lane)
+  if (r.at > 0 && old < byte) {  // the scale grows: the block's earlier rows (16 codes per lane)
     constexpr int LPC = D / 16;
     const float f = scale_of(max(old - byte + 127, 0));
     for (int i = (w * kWave + lane) / LPC; i < r.at; i += W * kWave / LPC) {

@@ -8,6 +8,7 @@ from paper_2608_06628_amd import binding as hb
 
 import _cache_ref as ref
 from _helpers import announce
+from test_kv_q8_gpu import same
 from test_softmax_q8_gpu import check, make, run
 
 pytestmark = pytest.mark.gpu
@@ -98,3 +99,29 @@ def test_read(dtype):
     for t in (k, v):
         assert torch.equal(t.isnan().cpu(), want.isnan())
         assert torch.equal(torch.nan_to_num(t.cpu(), 3.0, 5.0, -5.0), torch.nan_to_num(want, 3.0, 5.0, -5.0))
+
+
+@pytest.mark.parametrize("old", [0, 1, 9, 10, 253, 254])
+@pytest.mark.parametrize("dtype,H,d,page,sb", [(BF, 2, 128, 64, 32), (FL, 3, 64, 64, 64), (BF, 1, 64, 256, 256),
+                                               (FL, 2, 128, 1024, 512)])
+def test_write_goes_on(dtype, H, d, page, sb, old):
+    """Blocks that hold rows under any scale and go on: those rows are rounded again to the new scale
+    wherever that is larger, whatever the old one was."""
+    announce(f"write goes on from scale byte {old}: {dtype} {H} {d} {page} {sb}")
+    i32 = lambda x: torch.tensor(np.asarray(x), dtype=torch.int32).cuda()
+    held, new = [1, sb - 1, 5, sb // 2, 0, 17], [1, 1, sb, 3, 2, 0]
+    B = len(held)
+    table = np.random.RandomState(9).permutation(2 * B).reshape(B, 2).astype(np.int32)
+    start = np.concatenate([[0], np.cumsum(new)])
+    g = torch.Generator().manual_seed(old)
+    for size in (0.0, 1e-36, 1.0, 1e30):
+        cache = ref.Cache(2 * B, page, sb, H, d, 10)
+        for x in "kv":
+            cache.host[x][1][:] = old
+        cache.send()
+        k, v = ((torch.randn(int(start[-1]), H, d, generator=g) * size).to(dtype).cuda() for _ in "kv")
+        hb.kv_pages_q8_write(k, v, *cache.args, i32(table), i32(held), i32(start))
+        torch.cuda.synchronize()
+        for x, t in (("k", k), ("v", v)):
+            ref.write(*cache.host[x], t.double().cpu().numpy(), table, held, start.copy())
+            same(cache.codes(x), cache.host[x], f"{x}, new rows of {size}")
