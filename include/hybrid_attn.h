@@ -493,7 +493,8 @@ int kv_pages_plan(int32_t batch, int32_t max_pages, int32_t page_size,
  * of scale_block consecutive rows of a page at one KV head.  A cached value is its code
  * times its scale, also of a zeroed pool (2^-127): exactly in fp32, and in bf16 from byte 3 on
  * (below, rounded to nearest even among bf16's subnormal numbers), up to where the types
- * end.  page_size is a power of two from 32 to 65536, scale_block one from 32 to page_size. */
+ * end.  Byte 255 is no number: the values under it are NaN, and a block that goes on keeps it.
+ * page_size is a power of two from 32 to 65536, scale_block one from 32 to page_size. */
 typedef struct {
   int32_t tokens;      /* N >= 0, rows of k and v (0: nothing to do)         */
   int32_t batch;       /* B >= 0, requests                                   */

@@ -14,8 +14,11 @@ namespace hyb {
 
 constexpr int kMinScale = 10;  // 2^-117
 
-// (Positive whatever the byte: -infinity times it, a hidden score, stays one.)
-__device__ inline float scale_of(int byte) { return __builtin_bit_cast(float, max(byte << 23, 0x400000)); }
+// (Positive for every number: -infinity times it, a hidden score, stays one.)  NaN for byte 255,
+// as in the conversions, where an infinity would drop the tokens whose scores it makes negative.
+__device__ inline float scale_of(int byte) {
+  return __builtin_bit_cast(float, max(byte << 23 | (byte + 1) >> 8 << 22, 0x400000));
+}
 
 // The byte of the least e with m <= 448 2^e, for the bits of a finite m >= 0.
 // 448 is 1.75 2^8: the mantissa's part above 1.75 carries into the exponent.

@@ -105,7 +105,7 @@ __global__ __launch_bounds__(kWave* kQ8Waves) void hyb_kv_q8_write_kernel(KvQ8Ar
   const T* src = (const T*)(kv ? a.v : a.k) + r.src * stride + (long)g * D + lane % LPR * 8;
   uint8_t* const pool = kv ? a.v_pages : a.k_pages;
   uint8_t* const scale = (kv ? a.v_scales : a.k_scales) + (r.dst >> a.sb_shift) * a.Hkv + g;
-  const int old = r.n > 0 && r.at > 0 ? min((int)*scale, 254) : 0;
+  const int old = r.n > 0 && r.at > 0 ? *scale : 0;
   Q8Piece<T> x[NL];
   int m = 0;
   // This wave's rows, 32 at a time: w, w + W, ..; those past the last are the last again.
@@ -151,7 +151,7 @@ __global__ __launch_bounds__(kWave* kQ8Waves) void hyb_kv_q8_write_kernel(KvQ8Ar
       *p = uint4{fewer(c.x), fewer(c.y), fewer(c.z), fewer(c.w)};
     }
   }
-  const float f = scale_of(254 - byte);
+  const float f = scale_of(254 - min(byte, 254));  // (255, NaN, stays, whatever the codes)
   for (int c0 = w * kQ8Rows; c0 < r.n; c0 += W * kQ8Rows) {
     if (c0 != last || c0 != w * kQ8Rows) load(c0);  // (held where the wave has no more)
 #pragma unroll

@@ -125,3 +125,52 @@ def test_write_goes_on(dtype, H, d, page, sb, old):
         for x, t in (("k", k), ("v", v)):
             ref.write(*cache.host[x], t.double().cpu().numpy(), table, held, start.copy())
             same(cache.codes(x), cache.host[x], f"{x}, new rows of {size}")
+
+
+@pytest.mark.parametrize("dtype", [BF, FL], ids=str)
+def test_read_not_a_number(dtype):
+    """Byte 255 is the format's NaN: so is every value under it."""
+    announce(f"read scale byte 255 {dtype}")
+    codes, scales, _ = every_byte()
+    pool = torch.from_numpy(codes).cuda().view(torch.float8_e4m3fn)
+    bytes_ = torch.from_numpy(scales).cuda().view(torch.float8_e8m0fnu)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32).cuda()
+    k, v = hb.kv_pages_q8_read(pool, pool, bytes_, bytes_, i32([[255]]), i32([0]), i32([0, 32]), tokens=32, dtype=dtype)
+    assert bool(k.isnan().all()) and bool(v.isnan().all())
+
+
+@pytest.mark.parametrize("what", ["k", "v"])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_step_not_a_number(shape, what):
+    """A seen block of scale byte 255 makes its request's rows NaN at the query heads of its KV head,
+    whatever its codes and the queries are, and no others."""
+    B, L, Hq, Hkv, d, dtype = shape
+    announce(f"softmax q8 scale byte 255 of {what}: {shape}")
+    c = cached(shape, ALL, 0, 127)
+    codes, scales = c["cache"].host[what]
+    g, page = min(1, Hkv - 1), c["host"][1, 0]  # request 1 has 33 tokens: two blocks, the second cut
+    scales[page, 1, g] = 255
+    codes[page, 32, g] = np.where(np.arange(d) % 2, 0, 0x38 + 128 * (np.arange(d) // 2 % 2))
+    c["cache"].send()
+    out = run(c, None, out_f32=True)
+    heads = torch.arange(Hq) // (Hq // Hkv) == g
+    assert bool(out[1][:, heads].isnan().all())
+    assert not bool(out[1][:, ~heads].isnan().any())
+    assert not bool(out[[b for b in range(B) if b != 1]].isnan().any())
+
+
+def test_write_goes_on_from_not_a_number():
+    """A block that holds rows under scale byte 255, which are NaN, and goes on keeps it: no NaN becomes a
+    number."""
+    announce("write goes on from scale byte 255")
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32).cuda()
+    for dtype, sb in ((BF, 32), (FL, 64), (BF, 256)):
+        cache = ref.Cache(2, sb, sb, 2, 64, 11)
+        for x in "kv":
+            cache.host[x][1][:] = 255
+        cache.send()
+        k = torch.ones(sb, 2, 64, dtype=dtype, device="cuda")
+        hb.kv_pages_q8_write(k, k, *cache.args, i32([[0, 1]]), i32([5]), i32([0, sb]))
+        k2, v2 = hb.kv_pages_q8_read(*cache.args, i32([[0, 1]]), i32([0]), i32([0, sb + 5]), tokens=sb + 5, dtype=FL)
+        for t in (k2, v2):
+            assert bool(t[:sb].isnan().all()) and bool((t[sb:] == 1.0).all())  # (the second block starts over)
