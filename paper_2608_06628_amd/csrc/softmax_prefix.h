@@ -170,25 +170,8 @@ constexpr int kPlanInts = kPlanTiles + 2;
 template <int WIN>
 __device__ inline SpPlan sp_plan(const SoftmaxPrefixArgs& a, const SpCut& cut, int* tiles) {
   const int B = a.s.B, tid = threadIdx.x;
+  static_assert(WIN < 2, "an 8-bit cache's plan is sp_even_plan");
   if (a.n_split == 1) return SpPlan{1 << 24, true};
-  if constexpr (WIN == 2) {
-    // An even share of all tiles for B (n_split - 1) ranges, so that the requests'
-    // ranges, each rounded up, are at most B n_split; every wave works it out.
-    long sum = 0;
-    int most = 0;
-    for (int b = tid % kWave; b < B; b += kWave) {
-      const int nt = sp_tiles<WIN>(a, b);
-      sum += nt;
-      most = max(most, nt);
-    }
-    // (in two pieces: 2^31 tokens of each of many requests)
-    const long total = ((long)__builtin_amdgcn_readfirstlane(wave_all((int)(sum >> 24), AddOp{})) << 24) +
-                       __builtin_amdgcn_readfirstlane(wave_all((int)(sum & 0xffffff), AddOp{}));
-    most = __builtin_amdgcn_readfirstlane(wave_all(most, MaxOp{}));
-    const int share = cut.limit - B;
-    const int c = (int)min(max((total + share - 1) / share, 1L), (long)kMaxRange / kTile);
-    return SpPlan{c, most <= c};
-  }
   if (cut.c > 0) return SpPlan{cut.c, false};
   if (tid < kWave) {
     int total = 0, most = 0;
@@ -251,6 +234,28 @@ __device__ inline SpPlan sp_plan(const SoftmaxPrefixArgs& a, const SpCut& cut, i
   __syncthreads();
   return SpPlan{__builtin_amdgcn_readfirstlane(tiles[kPlanTiles]),
                 __builtin_amdgcn_readfirstlane(tiles[kPlanTiles + 1]) != 0};
+}
+
+// The plan of an 8-bit cache's kernels: an even share of all tiles for B (n_split - 1) ranges, so
+// that the requests' ranges, each rounded up, are at most B n_split.  Every wave works it out for
+// itself, without LDS and without a barrier.
+__device__ inline SpPlan sp_even_plan(const SoftmaxPrefixArgs& a, const SpCut& cut) {
+  if (a.n_split == 1) return SpPlan{1 << 24, true};
+  const int B = a.s.B;
+  long sum = 0;
+  int most = 0;
+  for (int b = threadIdx.x % kWave; b < B; b += kWave) {
+    const int nt = sp_tiles<2>(a, b);
+    sum += nt;
+    most = max(most, nt);
+  }
+  // (in two pieces: 2^31 tokens of each of many requests)
+  const long total = ((long)__builtin_amdgcn_readfirstlane(wave_all((int)(sum >> 24), AddOp{})) << 24) +
+                     __builtin_amdgcn_readfirstlane(wave_all((int)(sum & 0xffffff), AddOp{}));
+  most = __builtin_amdgcn_readfirstlane(wave_all(most, MaxOp{}));
+  const int share = cut.limit - B;
+  const int c = (int)min(max((total + share - 1) / share, 1L), (long)kMaxRange / kTile);
+  return SpPlan{c, most <= c};
 }
 
 // Ranges of a request of nt tiles.
@@ -361,8 +366,13 @@ template <typename T, int D, int WIN = 0>
 __global__ __launch_bounds__(256) void hyb_sp_combine_kernel(SoftmaxPrefixArgs a, SpCut cut) {
   constexpr int TPR = D / 4;              // threads per row
   constexpr int RPB = 256 / TPR;          // rows per unit
-  __shared__ alignas(16) int plan[kPlanInts];
-  const SpPlan p = sp_plan<WIN>(a, cut, plan);
+  SpPlan p;
+  if constexpr (WIN == 2) {
+    p = sp_even_plan(a, cut);
+  } else {
+    __shared__ alignas(16) int plan[kPlanInts];
+    p = sp_plan<WIN>(a, cut, plan);
+  }
   if (p.whole) return;  // every row is already written out
   const int Hq = a.s.Hq, L = a.s.L, lane = threadIdx.x & (kWave - 1);
   const int upb = (L + RPB - 1) / RPB;    // units of a (request, head)

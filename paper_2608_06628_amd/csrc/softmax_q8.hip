@@ -302,7 +302,6 @@ __global__ __launch_bounds__((q8_token_threads<T, D>())) void hyb_q8_token_kerne
       Slot ring[NW][R];
     } loop;
     f32x4 parts[NW][NCT * 4][kWave];
-    int plan[kPlanInts];
     __device__ Smem() {}
   };
   __shared__ alignas(16) Smem sh;
@@ -318,7 +317,7 @@ __global__ __launch_bounds__((q8_token_threads<T, D>())) void hyb_q8_token_kerne
   int at, hg;
   sp_place(q8_groups(a.s), at, hg);
   const int g = at % Hkv, r = at / Hkv;
-  const SpRange rg = sp_range<2>(a, sp_plan<2>(a, cut, sh.plan), r, lane);
+  const SpRange rg = sp_range<2>(a, sp_even_plan(a, cut), r, lane);
   if (rg.b < 0) return;  // uniform: past the plan's last range
   const int Lb = sp_block<2>(a, rg.b), P = min(max(a.prefix_len[rg.b], 0), a.max_prefix);
   // this lane's column: query i of head h
@@ -340,9 +339,9 @@ __global__ __launch_bounds__((q8_token_threads<T, D>())) void hyb_q8_token_kerne
     t.template copy<ONCE>(0, j0, s.k, lane);
     t.template copy<ONCE>(1, j0, s.v, lane);
   };
-  // The first tile beside the scales and the block (the plan's scratch, in the same place, was read
-  // before the barrier for the pages): one token over 32768 19.4 us after them, 18.7 so.  Not
-  // where the cache goes past the chip's caches: 64 requests of 16384 tokens 172 and 177.
+  // The first tile beside the scales and the block (its page is there since the barrier at the end
+  // of t's making): one token over 32768 19.4 us after them, 18.7 so.  Not where the cache goes
+  // past the chip's caches: 64 requests of 16384 tokens 172 and 177.
   if constexpr (!ONCE) issue(0, sh.loop.ring[w][0]);
   for (int e = threadIdx.x; e < nt; e += NW * kWave) bytes[e] = (uint16_t)t.scales(a, g, t.first_key(e));
   if (block) {  // rows past the block's are the last again
@@ -438,7 +437,6 @@ __global__ __launch_bounds__(kWave * 4 * H, 2) void hyb_q8_block_kernel(SoftmaxQ
   union Smem {
     Slot ring[H][R];
     f32x4 parts[H][NW][NH * 4][kWave];  // [for half]
-    int plan[kPlanInts];
     __device__ Smem() {}
   };
   __shared__ alignas(16) Smem sh;
@@ -459,7 +457,7 @@ __global__ __launch_bounds__(kWave * 4 * H, 2) void hyb_q8_block_kernel(SoftmaxQ
   int at, hg;
   sp_place((q8_groups(a.s) + NW - 1) / NW, at, hg);
   const int g = at % Hkv, r = at / Hkv;
-  const SpRange rg = sp_range<2>(a, sp_plan<2>(a, cut, sh.plan), r, lane);
+  const SpRange rg = sp_range<2>(a, sp_even_plan(a, cut), r, lane);
   if (rg.b < 0) return;  // uniform: past the plan's last range
   const int Lb = sp_block<2>(a, rg.b), P = min(max(a.prefix_len[rg.b], 0), a.max_prefix);
   const int col = (hg * NW + w) * kTile + li, hl = col / L, i = col - hl * L, h = g * G + hl;
@@ -618,7 +616,7 @@ __global__ __launch_bounds__(kWave * 4 * H, 2) void hyb_q8_block_kernel(SoftmaxQ
   // (the scales' bytes beside the first tiles)
   for (int e = threadIdx.x; e <= nc; e += blockDim.x)
     bytes[e] = nc > 0 ? (uint16_t)t.scales(a, g, t.first_key(max(0, min(e, nc - 1)))) : 0;
-  lds_barrier();  // (the bytes are there, the plan's scratch is read)
+  lds_barrier();  // (the bytes are there)
   if (first_is_block)
     put_block(ring[0]);
   else
@@ -708,10 +706,9 @@ __global__ __launch_bounds__(kWave * 4 * H, 2) void hyb_q8_block_kernel(SoftmaxQ
 template <typename T, int D>
 __global__ __launch_bounds__(256) void hyb_q8_combine_kernel(SoftmaxPrefixArgs a, SpCut cut) {
   constexpr int TPR = D / 4, NG = 256 / TPR;
-  __shared__ alignas(16) int plan[kPlanInts];
   __shared__ float most[NG], sums[NG];
   __shared__ f32x4 parts[NG][TPR];
-  const SpPlan p = sp_plan<2>(a, cut, plan);
+  const SpPlan p = sp_even_plan(a, cut);
   if (p.whole) return;  // every row is already written out
   const int Hq = a.s.Hq, L = a.s.L, lane = threadIdx.x & (kWave - 1);
   const int b = blockIdx.x / (Hq * L), h = blockIdx.x / L % Hq, i = blockIdx.x % L;
