@@ -548,7 +548,8 @@ int kv_pages_q8_read(const hyb_kv_q8_dims_t* dims, const void* k_pages,
  * dims->dtype, the cached tokens e4m3 with their scales.  Arguments and meaning otherwise
  * as there (a window of at least the prefix sees the whole cache), with any number of
  * query heads per KV head up to 65536 heads in all; a page number outside [0, n_pages) is
- * clamped into it.  bf16: the weights enter P V rounded to bf16, their sum takes them
+ * clamped into it.  Entries of q must be below 5e33 in magnitude (the codes' scores are summed
+ * before the keys' scale is applied).  bf16: the weights enter P V rounded to bf16, their sum takes them
  * unrounded.  ws/ws_bytes: at least hybrid_workspace_bytes(dims,
  * HYB_OP_WINDOW_STEP_Q8, min(max_pages * page_size, n_sinks + window + 64)) bytes.  out and
  * the workspace must not overlap each other or an input. */

@@ -16,7 +16,7 @@
 // columns, and one that converts a tile once for 128, chosen by time (q8_way).
 //
 // Measured, bf16, 16 and 4 heads of d = 128, calls one after the other: one token of 64 requests of 16384
-// tokens 173 us (6.2 TB/s), of one of 32768 19 us; 32 blocks of 32 over 32768 tokens 354 to 365 us (770
+// tokens 173 us (6.2 TB/s), of one of 32768 19 us; 32 blocks of 32 over 32768 tokens 349 to 365 us (770
 // TFLOP/s); 24 blocks of every length over a window of 1024 25 us.
 #include <algorithm>
 #include <cmath>
